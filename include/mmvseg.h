@@ -327,6 +327,111 @@ mmv_status mmv_stream_copy(const void *d_src, size_t in_bytes, void *d_dst, size
 mmv_status mmv_gather_reference(uint64_t nnz, const float *d_val, const int32_t *d_col, uint64_t n_cols,
                                 const float *d_x, float *d_partial, void *hip_stream);
 
+/* ---- A serving step over a ragged batch -----------------------------------------------------------------------------
+ * The requests of a batch are the segments of its packed token vector: request r owns the tokens offsets[r] ..
+ * offsets[r + 1] - 1.  Five calls that a model's step makes on such a batch: page tables and slots from the requests'
+ * lengths, new keys and values into the paged cache, attention of one token per request over that cache, and linear
+ * attention with a decay for each head, over prompts and for single tokens.  What the conventions above say holds here too,
+ * with these differences: lengths, tables and indices are read by the kernels alone, so that a step can be captured into a HIP
+ * graph and replayed as they change, and none of them is trusted: what would lie outside an array is left out as each call
+ * says.  Pointers to values are 16-byte aligned, pointers to 32- and 64-bit integers and fp32 aligned to their size; nothing is
+ * read beyond the arrays.  No call here leaves anything in its workspace that a later call or mmv_workspace_status needs. */
+typedef enum {
+    MMV_TYPE_F16 = 1,
+    MMV_TYPE_BF16 = 2,
+    MMV_TYPE_E4M3 = 5, /* 8 bits with 4 of exponent, largest value 448, no infinities (caches only) */
+    MMV_TYPE_INT_MAX = 0x7fffffff
+} mmv_type;
+
+/* Page tables and slots.  The cache is made of pages of `page` slots each; entry w of a request's row of the table names
+ * the page that holds its positions w * page .. (w + 1) * page - 1.  Before the call request r has d_cached[r] positions,
+ * whose pages are in its row; it gets d_new[r] more.  Pages that it needs beyond its own are taken from d_free in order,
+ * request by request, and written into its row.
+ *   d_cached, d_new  n int32 (negative: 0)
+ *   d_free      free_count page numbers
+ *   d_table     n rows of table_width int32, row r at d_table + r * table_stride
+ *   d_offsets   n + 1 int32: first token of every request, and their number (at most 2^31 - 1)
+ *   d_context   n int32: cached + new (at most 2^31 - 1)
+ *   d_slots     max_tokens int64: page * `page` + place in it of every token; -1 behind the last one, and for a token
+ *               that has no place: its row is too short, its page is not there (the row names a negative one) or the free
+ *               pages are used up
+ *   d_positions max_tokens int32: the token's position in its request; -1 behind the last one
+ *   d_used      two int64: free pages that the batch needs, tokens that it has.  A program compares them with free_count
+ *               and max_tokens; tokens from max_tokens on are left out, with the table entries that they would write.
+ *   d_ws        mmv_page_tables_workspace_bytes(n) bytes
+ * n < 2^22, max_tokens, free_count, table_width < 2^31, 1 <= page <= 2^16. */
+size_t mmv_page_tables_workspace_bytes(uint64_t n);
+mmv_status mmv_page_tables(uint64_t n, const int32_t *d_cached, const int32_t *d_new, const int32_t *d_free, uint64_t free_count,
+                           int32_t *d_table, uint64_t table_width, uint64_t table_stride, uint32_t page, uint64_t max_tokens,
+                           int32_t *d_offsets, int32_t *d_context, int64_t *d_slots, int32_t *d_positions, int64_t *d_used,
+                           void *d_ws, size_t ws_bytes, void *hip_stream);
+
+/* A paged cache of keys and values: component c of slot s of page p for head h is element
+ * p * page_stride + h * head_stride + s * slot_stride + c of d_k (d_v), so that pages may hold heads by slots or slots by
+ * heads.  Strides are in elements and multiples of 8, dim is a multiple of 8, at most 256; pages * page < 2^31.  A cache of
+ * MMV_TYPE_E4M3 holds key / k_scale and value / v_scale; the scales of the others are 1. */
+typedef struct {
+    void *d_k, *d_v;
+    mmv_type type;
+    uint32_t page, heads, dim;
+    uint64_t pages, page_stride, head_stride, slot_stride;
+    float k_scale, v_scale;
+} mmv_paged_cache;
+
+/* New keys and values into their slots.  Token t's values for head h are elements t * stride + h * dim ... of d_k (d_v),
+ * of `type`: the cache's, or any 16-bit one where that is MMV_TYPE_E4M3.  Values for an 8-bit cache are multiplied by 1 / scale, those beyond +-448 (infinities too)
+ * become +-448, NaN stays NaN, others are rounded to the nearest, ties to even.  A slot outside the cache is skipped (-1: the
+ * token has none); of two tokens with one slot either may win, value by value. */
+mmv_status mmv_cache_append(uint64_t tokens, const void *d_k, uint64_t k_stride, const void *d_v, uint64_t v_stride, mmv_type type,
+                            const int64_t *d_slots, const mmv_paged_cache *cache, void *hip_stream);
+
+/* Attention of one token for each of n rows (a request's newest one, whose key and value are in the cache already) over the
+ * first d_context[r] positions of its row of the table, or the last `window` of those (0: all of them):
+ *   s(p) = scale * q . k(p),   out = sum_p exp(s(p) - lse) v(p),   lse = log sum_p exp(s(p))
+ * Query head h reads the keys and values of cache head h / (q_heads / heads).  Tokens of one prompt can be given as rows of
+ * their own, with a context each.
+ *   d_q         row r's query for head h: elements r * q_stride + h * dim ..., of `type`, which is the cache's, or 16-bit for MMV_TYPE_E4M3
+ *   d_table, d_context  as mmv_page_tables leaves them.  A context is cut at table_width * page; positions in pages that the cache
+ *               does not have (-1) are left out.
+ *   d_out       n * q_heads * dim of `type`;  d_lse  n * q_heads fp32, or NULL
+ * A row without any position gets zeros and -infinity.  What lies in the cache at positions that are left out is not used,
+ * whatever it is.  Scores and sums are fp32; probabilities are rounded to `type` before they meet the values.
+ *   q_heads a multiple of the cache's heads, at most 16 times; page a multiple of 8.
+ *   d_ws        mmv_paged_attention_workspace_bytes(n, q_heads, heads, dim, table_width * page) bytes */
+size_t mmv_paged_attention_workspace_bytes(uint64_t n, uint32_t q_heads, uint32_t heads, uint32_t dim, uint64_t max_context);
+mmv_status mmv_paged_attention(uint64_t n, uint32_t q_heads, const void *d_q, uint64_t q_stride, mmv_type type,
+                               const mmv_paged_cache *cache, const int32_t *d_table, uint64_t table_width, uint64_t table_stride,
+                               const int32_t *d_context, float scale, uint32_t window, void *d_out, float *d_lse,
+                               void *d_ws, size_t ws_bytes, void *hip_stream);
+
+/* Linear attention with a decay for each head, over the packed tokens of n requests:
+ *   S_t = exp(log_decay) S_(t-1) + k_t v_t^T,   out_t = scale * q_t S_t
+ * where S is a dk x dv matrix for every request and head; it starts as the request's state in d_state_in and ends as that in
+ * d_state_out.  Head h reads the keys and values of head h / (heads / kv_heads).
+ *   d_q, d_k, d_v  token t's vector for head h: elements t * stride + h * dk (dv) ..., of `type` (16-bit)
+ *   d_offsets   n + 1 int32, non-decreasing (what they say beyond `tokens` or backwards is cut off); outputs of tokens that
+ *               belong to no request are not written
+ *   d_log_decay heads fp32, 0 or below (above 0 the states grow until they overflow)
+ *   d_state_in, d_state_out  `states` matrices of heads x dk x dv fp32; d_state_in NULL: zeros, d_state_out NULL: not kept.  They may
+ *               be the same array, and overlap in no other way
+ *   d_state_index  n int32: which of the states is the request's; NULL: the r-th.  A request whose index is outside has
+ *               none: it starts from zeros, and its state is not kept.  No two requests share one.
+ *   d_out       tokens * heads * dv of `type`
+ * States are fp32 throughout.  dk and dv are multiples of 8, dk <= 128, dv <= 256; heads, kv_heads <= 1024. */
+size_t mmv_decay_attention_workspace_bytes(uint64_t n, uint64_t tokens, uint32_t heads, uint32_t dk, uint32_t dv);
+mmv_status mmv_decay_attention(uint64_t n, uint64_t tokens, uint32_t heads, uint32_t kv_heads, uint32_t dk, uint32_t dv,
+                               const void *d_q, uint64_t q_stride, const void *d_k, uint64_t k_stride, const void *d_v, uint64_t v_stride,
+                               mmv_type type, const int32_t *d_offsets, const float *d_log_decay, float scale,
+                               const float *d_state_in, float *d_state_out, uint64_t states, const int32_t *d_state_index,
+                               void *d_out, void *d_ws, size_t ws_bytes, void *hip_stream);
+
+/* The same for one token of each of n requests: token r is request r's.  No workspace. */
+mmv_status mmv_decay_step(uint64_t n, uint32_t heads, uint32_t kv_heads, uint32_t dk, uint32_t dv,
+                          const void *d_q, uint64_t q_stride, const void *d_k, uint64_t k_stride, const void *d_v, uint64_t v_stride,
+                          mmv_type type, const float *d_log_decay, float scale,
+                          const float *d_state_in, float *d_state_out, uint64_t states, const int32_t *d_state_index,
+                          void *d_out, void *hip_stream);
+
 /* Instrumentation for benchmarks: from now on, every mmv_segscan / mmv_segsum /
  * mmv_spmv_coo call made by the calling host thread records `ev_start` (a
  * hipEvent_t passed as void*) on the call's stream immediately before its main

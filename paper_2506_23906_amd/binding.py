@@ -10,7 +10,9 @@ from __future__ import annotations
 
 import ctypes
 import importlib
+import math
 import os
+from typing import NamedTuple
 
 import torch  # imported before the library so that both share one HIP runtime
 
@@ -25,6 +27,7 @@ MMV_VARIANT_MFMA, MMV_VARIANT_SHUFFLE = 0, 1
 MMV_OP_SEGSCAN, MMV_OP_SEGSUM, MMV_OP_SPMV_COO = 0, 1, 2
 MMV_OP_SCAN, MMV_OP_COMPRESS, MMV_OP_SEGSUM_SCD, MMV_OP_SEGSCAN_SSCR, MMV_OP_SPMV_CSR = 3, 4, 5, 6, 7
 MMV_ELEM_I32, MMV_ELEM_F32 = 0, 1
+MMV_TYPE_F16, MMV_TYPE_BF16, MMV_TYPE_E4M3 = 1, 2, 5
 
 EXPORTS = [
     "mmv_workspace_bytes", "mmv_segscan", "mmv_segsum", "mmv_spmv_coo", "mmv_workspace_status",
@@ -32,6 +35,8 @@ EXPORTS = [
     "mmv_spmv_csr_workspace_bytes", "mmv_spmv_csr", "mmv_scan", "mmv_compress", "mmv_diff", "mmv_revert",
     "mmv_segsum_scd", "mmv_segscan_sscr", "mmv_segscan_static",
     "mmv_spmv_coo_prepare", "mmv_spmv_coo_run", "mmv_spmv_csr_prepare", "mmv_spmv_csr_run",
+    "mmv_page_tables_workspace_bytes", "mmv_page_tables", "mmv_cache_append", "mmv_paged_attention_workspace_bytes", "mmv_paged_attention",
+    "mmv_decay_attention_workspace_bytes", "mmv_decay_attention", "mmv_decay_step",
 ]
 STATIC_SCRATCH_BYTES = 1 << 20   # MMV_STATIC_SCRATCH_BYTES
 
@@ -107,6 +112,23 @@ def load() -> ctypes.CDLL:
     lib.mmv_segsum_scd.restype = i32
     lib.mmv_segscan_sscr.argtypes = [vp, vp, u64, vp, i32, i32, i32, vp, sz, vp]
     lib.mmv_segscan_sscr.restype = i32
+    u32, f32 = ctypes.c_uint32, ctypes.c_float
+    lib.mmv_page_tables_workspace_bytes.argtypes = [u64]
+    lib.mmv_page_tables_workspace_bytes.restype = sz
+    lib.mmv_page_tables.argtypes = [u64, vp, vp, vp, u64, vp, u64, u64, u32, u64, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.mmv_page_tables.restype = i32
+    lib.mmv_cache_append.argtypes = [u64, vp, u64, vp, u64, i32, vp, vp, vp]
+    lib.mmv_cache_append.restype = i32
+    lib.mmv_paged_attention_workspace_bytes.argtypes = [u64, u32, u32, u32, u64]
+    lib.mmv_paged_attention_workspace_bytes.restype = sz
+    lib.mmv_paged_attention.argtypes = [u64, u32, vp, u64, i32, vp, vp, u64, u64, vp, f32, u32, vp, vp, vp, sz, vp]
+    lib.mmv_paged_attention.restype = i32
+    lib.mmv_decay_attention_workspace_bytes.argtypes = [u64, u64, u32, u32, u32]
+    lib.mmv_decay_attention_workspace_bytes.restype = sz
+    lib.mmv_decay_attention.argtypes = [u64, u64, u32, u32, u32, u32, vp, u64, vp, u64, vp, u64, i32, vp, vp, f32, vp, vp, u64, vp, vp, vp, sz, vp]
+    lib.mmv_decay_attention.restype = i32
+    lib.mmv_decay_step.argtypes = [u64, u32, u32, u32, u32, vp, u64, vp, u64, vp, u64, i32, vp, f32, vp, vp, u64, vp, vp, vp]
+    lib.mmv_decay_step.restype = i32
     try:
         marshal = importlib.import_module(__package__ + "._marshal")
     except ImportError:
@@ -479,3 +501,181 @@ def mmv_segscan_sscr(x: torch.Tensor, flags: torch.Tensor, n: int | None = None,
                               _dev(ws, "ws"), ws.numel(), _stream_ptr(stream))
     _check(st, "mmv_segscan_sscr")
     return z
+
+
+# ---- a serving step over a ragged batch ---------------------------------------------------------------------------
+
+_VALUE_TYPES = {torch.float16: MMV_TYPE_F16, torch.bfloat16: MMV_TYPE_BF16}
+_CACHE_TYPES = {**_VALUE_TYPES, torch.float8_e4m3fn: MMV_TYPE_E4M3}
+
+
+class PageTables(NamedTuple):
+    """What mmv_page_tables leaves for the other calls of a step (beside the table itself)."""
+    offsets: torch.Tensor    # int32 [n + 1]: first token of every request, and their number
+    context: torch.Tensor    # int32 [n]: positions of every request, the new ones among them
+    slots: torch.Tensor      # int64 [max_tokens]: every token's slot in the cache, -1: none
+    positions: torch.Tensor  # int32 [max_tokens]: every token's position in its request, -1 behind the last one
+    used: torch.Tensor       # int64 [2]: free pages that the batch needs, tokens that it has
+
+
+class _CacheStruct(ctypes.Structure):   # mmv_paged_cache
+    _fields_ = [("d_k", ctypes.c_void_p), ("d_v", ctypes.c_void_p), ("type", ctypes.c_int), ("page", ctypes.c_uint32), ("heads", ctypes.c_uint32),
+                ("dim", ctypes.c_uint32), ("pages", ctypes.c_uint64), ("page_stride", ctypes.c_uint64), ("head_stride", ctypes.c_uint64),
+                ("slot_stride", ctypes.c_uint64), ("k_scale", ctypes.c_float), ("v_scale", ctypes.c_float)]
+
+
+class PagedCache:
+    """The keys and values of a layer in pages: two tensors [pages, heads, slots of a page, dim] of fp16, bf16 or e4m3 (any order of the first
+    three dimensions in memory: both tensors with the same strides).  An e4m3 cache holds key / k_scale and value / v_scale."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: float = 1.0, v_scale: float = 1.0):
+        if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype or k.device != v.device or k.stride() != v.stride():
+            raise MmvError("a cache is two tensors [pages, heads, slots, dim] of the same shape, type and strides")
+        if k.dtype not in _CACHE_TYPES:
+            raise MmvError("a cache holds float16, bfloat16 or float8_e4m3fn")
+        if not k.is_cuda or k.stride(3) != 1 or min(k.stride()) < 0:
+            raise MmvError("a cache lies in GPU memory, the values of a slot one after the other")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, float(k_scale), float(v_scale)
+        self._struct = _CacheStruct(k.data_ptr(), v.data_ptr(), _CACHE_TYPES[k.dtype], k.shape[2], k.shape[1], k.shape[3], k.shape[0],
+                                    k.stride(0), k.stride(1), k.stride(2), self.k_scale, self.v_scale)
+        self._ref = ctypes.addressof(self._struct)
+
+
+def _ints(t: torch.Tensor, name: str, dtype: torch.dtype, numel: int) -> int:
+    if t.dtype != dtype or t.numel() < numel:
+        raise MmvError("%s must hold %d values of %s" % (name, numel, dtype))
+    return _dev(t, name)
+
+
+def _tokens(t: torch.Tensor, name: str, shape: tuple, dtype: torch.dtype) -> tuple:
+    """(address, elements from token to token) of [tokens, heads, dim], the heads of a token one after the other."""
+    if not t.is_cuda or t.dtype != dtype or tuple(t.shape) != shape:
+        raise MmvError("%s must be %s of %s in GPU memory" % (name, list(shape), dtype))
+    if t.numel() and ((t.shape[2] > 1 and t.stride(2) != 1) or (t.shape[1] > 1 and t.stride(1) != t.shape[2])):
+        raise MmvError("%s: the heads of a token must lie one after the other" % name)
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else shape[1] * shape[2]
+
+
+def _table(t: torch.Tensor, n: int) -> tuple:
+    if not t.is_cuda or t.dtype != torch.int32 or t.dim() != 2 or t.shape[0] < n or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise MmvError("table must be int32 [%d, pages] in GPU memory, the entries of a row one after the other" % n)
+    return t.data_ptr(), t.shape[1], t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _out(out, name: str, shape: tuple, dtype: torch.dtype, device) -> torch.Tensor:
+    if out is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if tuple(out.shape) != shape or out.dtype != dtype:
+        raise MmvError("%s must be %s of %s" % (name, list(shape), dtype))
+    return out
+
+
+def _ws(ws, nbytes: int, device) -> tuple:
+    if ws is None and nbytes:
+        ws = workspace(nbytes, device)
+    return (None, 0, None) if ws is None else (_dev(ws, "ws"), ws.numel() * ws.element_size(), ws)
+
+
+def mmv_page_tables_workspace_bytes(n: int) -> int:
+    return int(load().mmv_page_tables_workspace_bytes(n))
+
+
+def mmv_page_tables(cached: torch.Tensor, new: torch.Tensor, free: torch.Tensor, table: torch.Tensor, page: int, max_tokens: int,
+                    out: PageTables | None = None, ws: torch.Tensor | None = None, stream=None) -> PageTables:
+    """Pages for the new tokens of every request (written into `table`) and the slot of every one; returns PageTables."""
+    lib, n, device = load(), new.numel(), new.device
+    if out is None:
+        out = PageTables(*(torch.empty(k, dtype=d, device=device) for k, d in
+                           ((n + 1, torch.int32), (n, torch.int32), (max_tokens, torch.int64), (max_tokens, torch.int32), (2, torch.int64))))
+    row, width, stride = _table(table, n)
+    w, w_bytes, ws = _ws(ws, mmv_page_tables_workspace_bytes(n), device)
+    st = lib.mmv_page_tables(n, _ints(cached, "cached", torch.int32, n), _ints(new, "new", torch.int32, n), _ints(free, "free", torch.int32, 0), free.numel(),
+                             row, width, stride, page, max_tokens, _ints(out.offsets, "offsets", torch.int32, n + 1),
+                             _ints(out.context, "context", torch.int32, n), _ints(out.slots, "slots", torch.int64, max_tokens),
+                             _ints(out.positions, "positions", torch.int32, max_tokens), _ints(out.used, "used", torch.int64, 2), w, w_bytes, _stream_ptr(stream))
+    _check(st, "mmv_page_tables")
+    return out
+
+
+def mmv_cache_append(k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, cache: PagedCache, stream=None) -> None:
+    """The keys and values [tokens, heads, dim] of new tokens into their slots."""
+    if k.dtype not in _VALUE_TYPES or k.dim() != 3:
+        raise MmvError("k and v must be [tokens, heads, dim] of float16 or bfloat16")
+    shape = (k.shape[0], cache.k.shape[1], cache.k.shape[3])
+    (pk, sk), (pv, sv) = _tokens(k, "k", shape, k.dtype), _tokens(v, "v", shape, k.dtype)
+    st = load().mmv_cache_append(shape[0], pk, sk, pv, sv, _VALUE_TYPES[k.dtype], _ints(slots, "slots", torch.int64, shape[0]), cache._ref, _stream_ptr(stream))
+    _check(st, "mmv_cache_append")
+
+
+def mmv_paged_attention_workspace_bytes(n: int, q_heads: int, heads: int, dim: int, max_context: int) -> int:
+    """max_context: entries of a row of the table times the slots of a page."""
+    return int(load().mmv_paged_attention_workspace_bytes(n, q_heads, heads, dim, max_context))
+
+
+def mmv_paged_attention(q: torch.Tensor, cache: PagedCache, table: torch.Tensor, context: torch.Tensor, scale: float | None = None, window: int = 0,
+                        out: torch.Tensor | None = None, lse: torch.Tensor | None = None, ws: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """Attention of one token q[r] ([rows, query heads, dim]) over the first context[r] positions of every row of the table, or the last
+    `window` of them; returns out like q.  scale: dim ** -0.5 if left out; lse: fp32 [rows, query heads], filled if given."""
+    if q.dtype not in _VALUE_TYPES or q.dim() != 3:
+        raise MmvError("q must be [rows, heads, dim] of float16 or bfloat16")
+    lib, (n, heads, dim), own = load(), q.shape, cache.k.shape
+    pq, sq = _tokens(q, "q", (n, heads, own[3]), q.dtype)
+    out = _out(out, "out", (n, heads, dim), q.dtype, q.device)
+    row, width, stride = _table(table, n)
+    if lse is not None:
+        lse = _out(lse, "lse", (n, heads), torch.float32, q.device)
+    w, w_bytes, ws = _ws(ws, mmv_paged_attention_workspace_bytes(n, heads, own[1], dim, width * own[2]), q.device)
+    st = lib.mmv_paged_attention(n, heads, pq, sq, _VALUE_TYPES[q.dtype], cache._ref, row, width, stride, _ints(context, "context", torch.int32, n),
+                                 1.0 / math.sqrt(dim) if scale is None else scale, window, _dev(out, "out"), None if lse is None else _dev(lse, "lse"),
+                                 w, w_bytes, _stream_ptr(stream))
+    _check(st, "mmv_paged_attention")
+    return out
+
+
+def _decay_arguments(q, k, v, log_decay, state_in, state_out, state_index, n, out):
+    if q.dtype not in _VALUE_TYPES or q.dim() != 3 or k.dim() != 3 or v.dim() != 3:
+        raise MmvError("q, k and v must be [tokens, heads, dim] of float16 or bfloat16")
+    (t, heads, dk), (kv, dv) = q.shape, v.shape[1:]
+    (pq, sq), (pk, sk), (pv, sv) = _tokens(q, "q", (t, heads, dk), q.dtype), _tokens(k, "k", (t, kv, dk), q.dtype), _tokens(v, "v", (t, kv, dv), q.dtype)
+    states = None
+    for name, s in (("state_in", state_in), ("state_out", state_out)):
+        if s is not None:
+            if s.dtype != torch.float32 or s.dim() != 4 or tuple(s.shape[1:]) != (heads, dk, dv) or s.shape[0] != (states or s.shape)[0]:
+                raise MmvError("%s must be [states, %d, %d, %d] of float32" % (name, heads, dk, dv))
+            states = s.shape
+    out = _out(out, "out", (t, heads, dv), q.dtype, q.device)
+    head = (heads, kv, dk, dv, pq, sq, pk, sk, pv, sv, _VALUE_TYPES[q.dtype])
+    tail = (_ints(log_decay, "log_decay", torch.float32, heads),)
+    state = (None if state_in is None else _dev(state_in, "state_in"), None if state_out is None else _dev(state_out, "state_out"), states[0] if states else 0,
+             None if state_index is None else _ints(state_index, "state_index", torch.int32, n), _dev(out, "out"))
+    return t, head, tail, state, out
+
+
+def mmv_decay_attention_workspace_bytes(n: int, tokens: int, heads: int, dk: int, dv: int) -> int:
+    return int(load().mmv_decay_attention_workspace_bytes(n, tokens, heads, dk, dv))
+
+
+def mmv_decay_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, offsets: torch.Tensor, log_decay: torch.Tensor, scale: float | None = None,
+                        state_in: torch.Tensor | None = None, state_out: torch.Tensor | None = None, state_index: torch.Tensor | None = None,
+                        out: torch.Tensor | None = None, ws: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """Linear attention with a decay for each head over packed requests; q [tokens, heads, dk], k [tokens, kv heads, dk], v [tokens, kv heads,
+    dv], states [states, heads, dk, dv] of fp32; returns out [tokens, heads, dv].  scale: dk ** -0.5 if left out."""
+    n = offsets.numel() - 1
+    if n < 0:
+        raise MmvError("offsets must hold the first token of every request, and their number")
+    t, head, decay, state, out = _decay_arguments(q, k, v, log_decay, state_in, state_out, state_index, n, out)
+    w, w_bytes, ws = _ws(ws, mmv_decay_attention_workspace_bytes(n, t, head[0], head[2], head[3]), q.device)
+    st = load().mmv_decay_attention(n, t, *head, _ints(offsets, "offsets", torch.int32, n + 1), *decay, head[2] ** -0.5 if scale is None else scale, *state,
+                                    w, w_bytes, _stream_ptr(stream))
+    _check(st, "mmv_decay_attention")
+    return out
+
+
+def mmv_decay_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_decay: torch.Tensor, state_in: torch.Tensor | None = None,
+                   state_out: torch.Tensor | None = None, scale: float | None = None, state_index: torch.Tensor | None = None,
+                   out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """mmv_decay_attention for one token of every request."""
+    t, head, decay, state, out = _decay_arguments(q, k, v, log_decay, state_in, state_out, state_index, q.shape[0], out)
+    st = load().mmv_decay_step(t, *head, *decay, head[2] ** -0.5 if scale is None else scale, *state, _stream_ptr(stream))
+    _check(st, "mmv_decay_step")
+    return out

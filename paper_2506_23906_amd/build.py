@@ -5,10 +5,12 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 SRC = os.path.join(HERE, "csrc", "mmvseg.hip")
+SERVING_SRC = os.path.join(HERE, "csrc", "serving.hip")
 LIB = os.path.join(HERE, "libmmvseg.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 MARSHAL_SRC = os.path.join(HERE, "csrc", "marshal.cpp")
@@ -26,8 +28,26 @@ def build(verbose: bool = False, extra: list[str] | None = None, out: str | None
     """Compiles the library; `extra` adds compiler flags (-D tunables), `out` names another output file."""
     lib = out or LIB
     tmp = lib + ".tmp.%d" % os.getpid()
-    cmd = [HIPCC] + FLAGS + (extra or []) + ["-o", tmp, SRC]
-    res = subprocess.run(cmd, capture_output=True, text=True)
+    flags = FLAGS + (extra or [])
+    compile_flags = [f for f in flags if f != "-shared"]
+    objects = ["%s.%s.tmp.%d.o" % (lib, os.path.basename(src), os.getpid()) for src in (SRC, SERVING_SRC)]
+    try:
+        with ThreadPoolExecutor() as pool:
+            list(pool.map(lambda pair: _hipcc(compile_flags + ["-c", "-o", pair[1], pair[0]], verbose), zip((SRC, SERVING_SRC), objects)))
+        _hipcc(flags + ["-o", tmp] + objects, verbose)
+    finally:
+        for o in objects:
+            if os.path.exists(o):
+                os.remove(o)
+    marshal = compile_marshal(verbose) if out is None else None
+    os.replace(tmp, lib)              # (both are there before either is replaced)
+    if marshal:
+        os.replace(marshal, MARSHAL_LIB)
+    return lib
+
+
+def _hipcc(args: list[str], verbose: bool) -> None:
+    res = subprocess.run([HIPCC] + args, capture_output=True, text=True)
     # the host pass does not know the packed-fp32 feature name; that note is harmless
     err = "\n".join(l for l in res.stderr.splitlines() if "packed-fp32-ops" not in l)
     if res.returncode != 0:
@@ -35,11 +55,6 @@ def build(verbose: bool = False, extra: list[str] | None = None, out: str | None
         raise RuntimeError("hipcc failed building libmmvseg.so")
     if verbose and err.strip():
         sys.stderr.write(err + "\n")
-    marshal = compile_marshal(verbose) if out is None else None
-    os.replace(tmp, lib)              # (both are there before either is replaced)
-    if marshal:
-        os.replace(marshal, MARSHAL_LIB)
-    return lib
 
 
 def compile_marshal(verbose: bool = False) -> str:
