@@ -1,79 +1,476 @@
 // libmmvseg, part of the translation unit serving.hip (included there, in order).
-// Attention of one token per row over a paged cache.
+// Attention of one token per row over a paged cache: split over the positions, parts joined.
 #pragma once
 
 namespace {
 
+// ---- paged attention ----------------------------------------------------------------------------------------------
+//
+// Bound by the bytes of the keys and values: each is read once, for all the query heads that share it, straight into
+// registers in the layout that the matrix cores take.  The unit of work is a tile of 32 positions of one (row, cache head); all
+// tiles of all rows are one list, row after row, and every wave takes an equal run of it, whatever the lengths are:
+// the rows are the segments of that list.  A wave keeps the running maximum and sum of its current segment; a segment
+// that lies within one wave's run is written at once, one that several waves share leaves partial results (maximum, sum,
+// unnormalised output) in the workspace, two for a wave at most, and a second launch joins them.
+//
+// A tile on the matrix cores (16x16x32), lane = 16 g + r:
+//   scores   S^T = K Q^T: row r of A is the key of position 8 (r / 4) + 4 t + r % 4 (t = 0, 1: two products), its 8 dims of a step those of
+//            g.  The result's lane (g, query r) then has the positions 8 g + 4 t + i: eight consecutive ones, and they are
+//   output   O^T = V^T P^T: ... the eight that the lane holds of B here, so probabilities go from one product to the next in their
+//            registers.  A lane loads 8 components of 8 consecutive positions' values (rows of the cache, coalesced)
+//            and exchanges 16-bit halves between pairs of positions: one v_perm for two values.
+// No LDS, no barrier.  Query heads beyond the group's are zero columns: the matrix cores have the time (about a tenth of
+// what the loads take).
 struct AttentionParams {
     const void *q, *k, *v;
-    uint64_t q_stride;                             // elements
-    uint64_t page_stride, head_stride, slot_stride;
+    uint64_t q_stride, head_stride;                // elements
+    uint32_t page_stride, slot_stride;
     const int32_t *table, *context;
-    uint64_t table_stride, max_context;
+    uint64_t table_stride;
     void *out;
     float *lse;
-    uint32_t n, q_heads, heads, group, dim, page, pages, window;
-    float score_by, out_by;
+    float *part_out, *part_ml;                     // [2 * workers][group][dim], [2 * workers][group][2]
+    uint64_t *sums;                                // [n + 1] tiles of a head before every row, and of all
+    uint32_t n, q_heads, heads, group, dim, page, pages, window, max_context, workers;
+    uint32_t groups_by, groups_shift, page_groups; // division by page / 8
+    float score_by, out_by;                        // scale * k_scale * log2(e), v_scale
+};
+constexpr uint32_t kTile = 32;                     // positions
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.693147180559945309417f;
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef bf16_t bf16x8 __attribute__((ext_vector_type(8)));
+typedef f16_t f16x8 __attribute__((ext_vector_type(8)));
+__device__ __forceinline__ f32x4 mfma_16x16x32(bf16_t, u32x4 a, u32x4 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mfma_16x16x32(f16_t, u32x4 a, u32x4 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+template <typename T> __device__ __forceinline__ uint32_t pack2(float a, float b) {
+    typedef T pair __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, (pair){from_f32<T>(a), from_f32<T>(b)});
+}
+// Two of a word's four 8-bit values as 16-bit ones (exact).
+template <bool kHigh> __device__ __forceinline__ uint32_t widen(bf16_t, uint32_t w) {
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)w, 1.f, kHigh));
+}
+template <bool kHigh> __device__ __forceinline__ uint32_t widen(f16_t, uint32_t w) {
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)w, 1.f, kHigh));
+}
+// Largest / sum over the four lanes that differ in g.
+__device__ __forceinline__ float over_g_max(float v) {
+    v = fmaxf(v, __shfl_xor(v, 16));
+    return fmaxf(v, __shfl_xor(v, 32));
+}
+__device__ __forceinline__ float over_g_sum(float v) {
+    v += __shfl_xor(v, 16);
+    return v + __shfl_xor(v, 32);
+}
+
+struct RowTiles {
+    uint32_t begin, end, first, count;   // positions [begin, end), tiles first .. first + count - 1
+};
+__device__ __forceinline__ RowTiles row_tiles(const AttentionParams &P, int32_t context) {
+    const uint32_t end = min(length_of(context), P.max_context), begin = P.window && end > P.window ? end - P.window : 0u;
+    const uint32_t first = begin / kTile;
+    return {begin, end, first, (end + kTile - 1) / kTile - first};
+}
+__device__ __forceinline__ uint64_t wave_total(uint64_t v) {
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) v += __shfl_xor(v, d);
+    return v;
+}
+__device__ __forceinline__ uint64_t uniform64(uint64_t v) {
+    return ((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(v >> 32)) << 32) | (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)v);
+}
+__device__ __forceinline__ uint32_t uniform(uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); }
+__device__ __forceinline__ uint64_t run_of(uint64_t tiles, uint32_t workers) { return (tiles + workers - 1) / workers; }
+
+// Where a wave is in the list of tiles (the same in all its lanes).
+struct Place {
+    uint32_t row, head, tile, first, last;   // the segment's tiles: first .. last - 1
+    uint32_t begin, end;                     // its positions
+};
+// Uniform loads through the scalar cache: they are not waited for along with the loads of keys and values.
+__device__ __forceinline__ int32_t scalar_load(const int32_t *p) { return *(const __attribute__((address_space(4))) int32_t *)(uintptr_t)p; }
+__device__ __forceinline__ void enter_row(const AttentionParams &P, Place &at) {
+    const RowTiles t = row_tiles(P, scalar_load(P.context + at.row));
+    at.first = t.first, at.last = t.first + t.count, at.begin = t.begin, at.end = t.end;
+}
+
+template <int KS> constexpr int dims_per_lane() { return KS <= 2 ? 4 : KS <= 4 ? 8 : KS <= 6 ? 12 : 16; }
+template <int KS> constexpr int certain_pieces() { return KS <= 2 ? 1 : KS == 3 ? 9 : KS == 4 ? 13 : KS == 5 ? 17 : 21; }   // of 8 dims, of any dim that takes this KS
+
+// kExact: dim = 32 KS, and a slot's values lie behind those of the slot before.
+template <int KS, bool kExact, typename T, bool kE4m3> struct Tile {
+    static constexpr int kDims = dims_per_lane<KS>();
+    static constexpr int kSize = kE4m3 ? 1 : 2;
+    static constexpr int kKeyWords = kE4m3 ? 2 : 4, kValueWords = kE4m3 ? kDims / 4 : kDims / 2;
+    uint32_t k[2][KS][kKeyWords], v[8][kValueWords];
+    const char *pk, *pv;
+    uint32_t pages_ok;   // bit i: the page of positions 8 i .. 8 i + 7 is there
+
+    // Addresses of a tile's rows for this lane.  Pages are looked up for 8 positions at a time: those of the lane's keys are the
+    // (r / 4)th of the tile's four, those of its values and scores the g-th.
+    __device__ __forceinline__ void find(const AttentionParams &P, const Place &at, uint32_t g, uint32_t r) {
+        const int32_t *row = P.table + (uint64_t)at.row * P.table_stride;
+        uint64_t off[4];
+        pages_ok = 0;
+        if (P.page_groups % 4 == 0) {   // a tile lies in one page
+            const uint32_t group = at.tile * 4, page = page_of(P, group);
+            off[0] = place_of(P, scalar_load(row + page), group - page * P.page_groups, 15u);
+#pragma unroll
+            for (int i = 1; i < 4; ++i) off[i] = off[0] + (uint32_t)(8 * i) * slot_stride(P);
+        } else {
+            int32_t id[4];
+            uint32_t inside[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t group = at.tile * 4 + i, page = page_of(P, group);
+                id[i] = -1;
+                if (group * 8 < at.end) id[i] = scalar_load(row + page);   // (behind it the row may end)
+                inside[i] = group - page * P.page_groups;
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) off[i] = place_of(P, id[i], inside[i], 1u << i);
+        }
+        const uint64_t head = (uint64_t)at.head * P.head_stride;
+        const uint64_t ok_ = head + pick(off, r >> 2) + (r & 3) * slot_stride(P), ov = head + pick(off, g);
+        pk = (const char *)P.k + kSize * ok_;
+        pv = (const char *)P.v + kSize * ov;
+    }
+    // Where eight positions begin in a page (relative to the head), and that it is there.  What is read for a page that is not, from page 0, is not used.
+    __device__ __forceinline__ uint64_t place_of(const AttentionParams &P, int32_t id, uint32_t inside, uint32_t bits) {
+        const bool ok = (uint32_t)id < P.pages;
+        pages_ok |= ok ? bits : 0u;
+        return (uint64_t)(ok ? (uint32_t)id : 0u) * P.page_stride + (uint64_t)(inside * 8) * slot_stride(P);
+    }
+    static __device__ __forceinline__ uint64_t pick(const uint64_t (&off)[4], uint32_t i) {
+        const uint64_t a = i & 1 ? off[1] : off[0], b = i & 1 ? off[3] : off[2];
+        return i & 2 ? b : a;
+    }
+    static __device__ __forceinline__ uint32_t page_of(const AttentionParams &P, uint32_t g8) { return P.groups_by ? __umulhi(g8, P.groups_by) >> P.groups_shift : g8 >> P.groups_shift; }
+    static __device__ __forceinline__ uint32_t slot_stride(const AttentionParams &P) { return kExact ? 32 * KS : P.slot_stride; }
+    template <int kWords> static __device__ __forceinline__ void load(uint32_t (&to)[kWords], const char *p) {
+        if constexpr (kWords == 4) {
+            const u32x4 w = *(const u32x4 *)p;
+            to[0] = w[0], to[1] = w[1], to[2] = w[2], to[3] = w[3];
+        } else if constexpr (kWords == 2) {
+            const u32x2 w = *(const u32x2 *)p;
+            to[0] = w[0], to[1] = w[1];
+        } else {
+            to[0] = *(const uint32_t *)p;
+        }
+    }
+    __device__ __forceinline__ void load_keys(const AttentionParams &P, uint32_t g) {
+        const uint32_t pieces = P.dim / 8;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const char *p = pk + (uint32_t)(t * 4 * kSize) * slot_stride(P);
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+                if constexpr (kExact && kE4m3) {   // 16 bytes for two steps: the dims of a step are those of this layout, of the queries too
+                    if (s % 2 == 0) {
+                        uint32_t both[4];
+                        load(both, p + s * 32 + g * 16);
+                        k[t][s][0] = both[0], k[t][s][1] = both[1], k[t][s + 1][0] = both[2], k[t][s + 1][1] = both[3];
+                    }
+                } else {
+                    uint32_t piece = s * 4 + g;
+                    if (!kExact && s * 4 + 3 >= certain_pieces<KS>()) piece = piece < pieces ? piece : 0;
+                    load(k[t][s], p + piece * 8 * kSize);
+                }
+            }
+        }
+    }
+    __device__ __forceinline__ void load_values(const AttentionParams &P, uint32_t r) {
+        constexpr int kFirst = kDims >= 8 ? 8 : 4, kSecond = kDims - kFirst;   // components of the lane's one or two pieces
+        const uint32_t first = kExact || r * kFirst < P.dim ? r * kFirst : 0;
+        const uint32_t second = kExact || 128 + r * (kSecond ? kSecond : 1) < P.dim ? 128 + r * (kSecond ? kSecond : 1) : 0;
+        constexpr int kWordsFirst = kFirst * kSize / 4, kWordsSecond = kSecond * kSize / 4;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const char *p = pv + (uint32_t)(j * kSize) * slot_stride(P);
+            uint32_t a[kWordsFirst];
+            load(a, p + first * kSize);
+#pragma unroll
+            for (int w = 0; w < kWordsFirst; ++w) v[j][w] = a[w];
+            if constexpr (kSecond > 0) {
+                uint32_t b[kWordsSecond];
+                load(b, p + second * kSize);
+#pragma unroll
+                for (int w = 0; w < kWordsSecond; ++w) v[j][kWordsFirst + w] = b[w];
+            }
+        }
+    }
+    // The lane's dims of step s: 8 from this one on.
+    static __device__ __forceinline__ uint32_t step_dim(int s, uint32_t g) { return kExact && kE4m3 ? (s / 2) * 64 + g * 16 + (s % 2) * 8 : s * 32 + g * 8; }
+    __device__ __forceinline__ void scores(const AttentionParams &P, const u32x4 (&q)[KS], uint32_t g, f32x4 (&S)[2]) const {
+        const uint32_t pieces = P.dim / 8;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            S[t] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+                u32x4 a;
+                if constexpr (kE4m3) {
+                    a = (u32x4){widen<false>(T(), k[t][s][0]), widen<true>(T(), k[t][s][0]), widen<false>(T(), k[t][s][1]), widen<true>(T(), k[t][s][1])};
+                } else {
+                    a = (u32x4){k[t][s][0], k[t][s][1], k[t][s][2], k[t][s][3]};
+                }
+                if (!kExact && s * 4 + 3 >= certain_pieces<KS>()) {   // (what was read twice, times zeros of the query: it may be infinite)
+                    const uint32_t keep = (uint32_t)(s * 4) + g < pieces ? ~0u : 0u;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) a[i] &= keep;
+                }
+                S[t] = mfma_16x16x32(T(), a, q[s], S[t]);
+            }
+        }
+    }
+    // Component c of the lane's values as the eight positions of a product's operand.
+    template <int c> __device__ __forceinline__ u32x4 column() const {
+        u32x4 a;
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+            if constexpr (kE4m3) {
+                constexpr uint32_t at = c & 3;
+                const uint32_t both = __builtin_amdgcn_perm(v[2 * m + 1][c / 4], v[2 * m][c / 4], at < 2 ? 0x05010400u : 0x07030602u);   // two components of both positions
+                a[m] = widen<(at & 1) != 0>(T(), both);
+            } else {
+                a[m] = __builtin_amdgcn_perm(v[2 * m + 1][c / 2], v[2 * m][c / 2], c % 2 ? 0x07060302u : 0x05040100u);
+            }
+        }
+        return a;
+    }
+    template <int c = 0> __device__ __forceinline__ void add_values(u32x4 p, f32x4 (&O)[kDims]) const {
+        if constexpr (c < kDims) {
+            O[c] = mfma_16x16x32(T(), column<c>(), p, O[c]);
+            add_values<c + 1>(p, O);
+        }
+    }
 };
 
-// One wave for a row and query head: a lane takes a position for the scores, then four components of the output.
-template <typename T, typename C> __global__ __launch_bounds__(64) void paged_attention_kernel(AttentionParams P) {
-    __shared__ float query[256], weight[64];
-    __shared__ uint64_t at_lds[64];
-    const uint32_t row = blockIdx.x / P.q_heads, qh = blockIdx.x % P.q_heads, lane = threadIdx.x;
-    const T *q = (const T *)P.q + row * P.q_stride + (uint64_t)qh * P.dim;
-    for (uint32_t c = lane; c < 256; c += 64) query[c] = c < P.dim ? to_f32(q[c]) : 0.f;
-    __syncthreads();
-    int64_t length = P.context[row];
-    if (length < 0) length = 0;
-    if ((uint64_t)length > P.max_context) length = (int64_t)P.max_context;
-    const int64_t begin = P.window && length > P.window ? length - P.window : 0;
-    const uint64_t head = (uint64_t)(qh / P.group) * P.head_stride;
-    float most = -INFINITY, sum = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int64_t first = begin; first < length; first += 64) {
-        const int64_t p = first + lane;
-        float s = -INFINITY;
-        uint64_t at = ~0ull;
-        if (p < length) {
-            const int32_t id = P.table[row * P.table_stride + p / P.page];
-            if ((uint32_t)id < P.pages) {
-                at = (uint64_t)id * P.page_stride + head + (uint64_t)(p % P.page) * P.slot_stride;
-                const C *k = (const C *)P.k + at;
-                s = 0.f;
-                for (uint32_t c = 0; c < P.dim; ++c) s += query[c] * to_f32(k[c]);
-                s *= P.score_by;
+// Four consecutive or eight components of a query's output, from the lane's registers: component c of lane index i (0 .. 3 here: 4 g + i).
+template <int kDims> __device__ __forceinline__ uint32_t dim_of(int c, uint32_t r) {
+    constexpr int kFirst = kDims >= 8 ? 8 : 4, kSecond = kDims - kFirst;
+    return c < kFirst ? r * kFirst + c : 128 + r * kSecond + (c - kFirst);
+}
+// What a wave has of a segment: the result where it has all of it, else a part for join_attention_kernel: in place 2 * worker where
+// the segment began in an earlier wave's run, in 2 * worker + 1 where it begins in this one's and goes on.
+template <int kDims, typename T> __device__ __forceinline__ void write_segment(const AttentionParams &P, const Place &at, uint32_t worker, bool begun, bool ended, uint32_t g, uint32_t r,
+                                                                             float most, float sum, const f32x4 (&O)[kDims], T) {
+    if (r >= P.group) return;   // (a column of zeros)
+    const uint64_t query = (uint64_t)at.row * P.q_heads + at.head * P.group + r;
+    if (!begun && ended) {
+        const float by = sum == 0.f ? 0.f : P.out_by / sum;
+        T *out = (T *)P.out + query * P.dim;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int c = 0; c < kDims; c += 4) {
+                const uint32_t d = dim_of<kDims>(c, 4 * g + i);
+                if (d < P.dim) *(u32x2 *)(out + d) = (u32x2){pack2<T>(O[c][i] * by, O[c + 1][i] * by), pack2<T>(O[c + 2][i] * by, O[c + 3][i] * by)};
             }
+        if (P.lse && g == 0) P.lse[query] = most == -INFINITY && sum == 0.f ? -INFINITY : (most + __builtin_amdgcn_logf(sum)) * kLn2;
+        return;
+    }
+    const uint64_t part = (uint64_t)(2 * worker + (begun ? 0 : 1)) * P.group + r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int c = 0; c < kDims; c += 4) {
+            const uint32_t d = dim_of<kDims>(c, 4 * g + i);
+            if (d < P.dim) *(f32x4 *)(P.part_out + part * P.dim + d) = (f32x4){O[c][i], O[c + 1][i], O[c + 2][i], O[c + 3][i]};
         }
-        float m = s;
-        for (int d = 32; d >= 1; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
-        m = fmaxf(m, most);
-        const float base = m == -INFINITY ? 0.f : m;
-        const float w = at == ~0ull ? 0.f : expf(s - base), by = expf(most - base);
-        most = m;
-        sum *= by;
-        for (int i = 0; i < 4; ++i) o[i] *= by;
-        weight[lane] = w;
-        at_lds[lane] = at;
-        __syncthreads();
-        for (int j = 0; j < 64; ++j) {
-            const uint64_t a = at_lds[j];
-            if (a == ~0ull) continue;
-            const float wj = weight[j];
-            sum += wj;
-            const C *v = (const C *)P.v + a;
+    if (g == 0) P.part_ml[2 * part] = most, P.part_ml[2 * part + 1] = sum;
+}
+
+template <int KS, bool kExact, typename T, bool kE4m3> __global__ __launch_bounds__(256, KS > 4 ? 1 : 2) void paged_attention_kernel(AttentionParams P) {
+    using TileT = Tile<KS, kExact, T, kE4m3>;
+    constexpr int kDims = TileT::kDims;
+    const uint32_t lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
+    const uint32_t worker = uniform(blockIdx.x * 4 + (threadIdx.x >> 6));
+    // the list's length, and this wave's run of it
+    uint64_t all = 0;
+    for (uint32_t i = lane; i < P.n; i += 64) all += row_tiles(P, P.context[i]).count;
+    all = uniform64(wave_total(all));
+    const uint64_t run = run_of(all * P.heads, P.workers), start = worker * run;
+    uint64_t left = start < all * P.heads ? min(run, all * P.heads - start) : 0;
+    if (worker == 0 || left) {
+        uint64_t before = 0, found_before = 0;
+        const uint64_t target = start / P.heads;
+        uint32_t row = 0;
+        bool found = false;
+        for (uint32_t first = 0; first < P.n && (worker == 0 || !found); first += 64) {
+            const uint32_t i = first + lane;
+            const uint64_t own = i < P.n ? row_tiles(P, P.context[i]).count : 0;
+            uint64_t upto = own;
+#pragma unroll
+            for (int d = 1; d < 64; d <<= 1) upto += shift_up64(upto, d, (int)lane);
+            if (worker == 0 && i < P.n) P.sums[i] = before + upto - own;
+            const uint64_t hit = __ballot(before + upto > target);
+            if (hit && !found) {
+                const int l = __builtin_ctzll(hit);
+                found = true;
+                row = first + l;
+                found_before = before + uniform64(__shfl(upto - own, l));
+            }
+            before += uniform64(__shfl(upto, 63));
+        }
+        if (worker == 0 && lane == 0) P.sums[P.n] = all;
+        if (!left) return;
+        Place at;
+        at.row = uniform(row);
+        enter_row(P, at);
+        const uint64_t inside = start - found_before * P.heads;
+        const uint32_t count = at.last - at.first;
+        at.head = uniform((uint32_t)(inside / count));
+        at.tile = at.first + uniform((uint32_t)(inside % count));
+        bool begun = at.tile != at.first;   // the current segment began in an earlier wave's run
+
+        TileT tile;
+        tile.find(P, at, g, r);
+        tile.load_keys(P, g);
+        tile.load_values(P, r);
+        u32x4 q[KS];
+        f32x4 O[kDims];
+        float most = -INFINITY, sum = 0.f;
+        bool fresh = true;
+        for (;;) {
+            if (fresh) {   // a new segment: its queries
+                fresh = false;
+                const T *pq = (const T *)P.q + (uint64_t)at.row * P.q_stride + (uint64_t)(at.head * P.group + r) * P.dim;
+#pragma unroll
+                for (int s = 0; s < KS; ++s) {
+                    const uint32_t d = TileT::step_dim(s, g);
+                    q[s] = (u32x4){0, 0, 0, 0};
+                    if (r < P.group && d < P.dim) q[s] = *(const u32x4 *)(pq + d);
+                }
+#pragma unroll
+                for (int c = 0; c < kDims; ++c) O[c] = (f32x4){0.f, 0.f, 0.f, 0.f};
+                most = -INFINITY, sum = 0.f;
+            }
+            f32x4 S[2];
+            tile.scores(P, q, g, S);
+            float s[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s[i] = S[i / 4][i % 4] * P.score_by;
+            const uint32_t pages_ok = tile.pages_ok;
+            // the next tile's place; its keys are on their way while this one's values are multiplied
+            const Place now = at;
+            --left;
+            if (left && ++at.tile == at.last) {
+                if (++at.head == P.heads) {
+                    at.head = 0;
+                    do {
+                        ++at.row;
+                        enter_row(P, at);
+                    } while (at.first == at.last);   // (a row without positions; a later one has some, as `left` says)
+                }
+                at.tile = at.first;
+            }
+            if (pages_ok != 15u || now.tile * kTile < now.begin || (now.tile + 1) * kTile > now.end) {
+                uint32_t keep = 0;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const uint32_t p = now.tile * kTile + 8 * g + i;
+                    if (((pages_ok >> g) & 1) && p >= now.begin && p < now.end) keep |= 1u << i;
+                    s[i] = (keep >> i) & 1 ? s[i] : -INFINITY;
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j)   // (0 times what lies there need not be 0)
+#pragma unroll
+                    for (int w = 0; w < TileT::kValueWords; ++w) tile.v[j][w] = (keep >> j) & 1 ? tile.v[j][w] : 0u;
+            }
+            tile.find(P, at, g, r);   // (behind the run's last tile: that one again, not used)
+            tile.load_keys(P, g);
+            float top = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
+            // Scores up to 2^8 above the base need no new one (nothing overflows: 16-bit floats reach 2^15).
+            if (__any(top > most + 8.f)) {
+                const float m = fmaxf(over_g_max(top), most), by = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(most - m);
+                most = m;
+                sum *= by;
+#pragma unroll
+                for (int c = 0; c < kDims; ++c) O[c] *= by;
+            }
+            const float base = most == -INFINITY ? 0.f : most;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                s[i] = __builtin_amdgcn_exp2f(s[i] - base);
+                sum += s[i];
+            }
+            // Probabilities are rounded to the values' 16 bits: the matrix cores take both operands of one type.
+            const u32x4 p = {pack2<T>(s[0], s[1]), pack2<T>(s[2], s[3]), pack2<T>(s[4], s[5]), pack2<T>(s[6], s[7])};
+            tile.add_values(p, O);
+            tile.load_values(P, r);
+            const bool ended = now.tile + 1 == now.last;
+            if (ended || !left) {
+                write_segment<kDims>(P, now, worker, begun, ended, g, r, most, over_g_sum(sum), O, T());
+                fresh = true, begun = false;
+            }
+            if (!left) break;
+        }
+    }
+}
+
+// Joins the parts of the segments that several waves share, and writes the rows without positions: one wave for a row and query head.
+template <typename T> __global__ __launch_bounds__(256) void join_attention_kernel(AttentionParams P) {
+    const uint32_t lane = threadIdx.x & 63, id = uniform(blockIdx.x * 4 + (threadIdx.x >> 6));
+    if (id >= P.n * P.q_heads) return;
+    const uint32_t row = id / P.q_heads, qh = id % P.q_heads, h = qh / P.group, q = qh % P.group;
+    const uint64_t before = P.sums[row], tiles = P.sums[row + 1] - before, all = P.sums[P.n] * P.heads;
+    T *out = (T *)P.out + (uint64_t)id * P.dim;
+    if (tiles == 0) {
+        for (uint32_t d = lane; d < P.dim; d += 64) out[d] = from_f32<T>(0.f);
+        if (P.lse && lane == 0) P.lse[id] = -INFINITY;
+        return;
+    }
+    const uint64_t from = before * P.heads + h * tiles, to = from + tiles, run = run_of(all, P.workers);
+    const uint32_t first = (uint32_t)(from / run), last = (uint32_t)((to - 1) / run);
+    if (first == last) return;   // (written by that wave)
+    const uint32_t first_slot = 2 * first + 1;   // (the segment begins in that wave's run)
+    float most = -INFINITY;
+    for (uint32_t w = first + lane; w <= last; w += 64) most = fmaxf(most, P.part_ml[2 * ((uint64_t)(w == first ? first_slot : 2 * w) * P.group + q)]);
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) most = fmaxf(most, __shfl_xor(most, d));
+    const float base = most == -INFINITY ? 0.f : most;
+    float sum = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+    for (uint32_t w0 = first; w0 <= last; w0 += 64) {
+        const uint32_t mine = w0 + lane;
+        float by = 0.f;
+        if (mine <= last) {
+            const float *ml = P.part_ml + 2 * ((uint64_t)(mine == first ? first_slot : 2 * mine) * P.group + q);
+            by = __builtin_amdgcn_exp2f(ml[0] - base);
+            sum += by * ml[1];
+        }
+        const uint32_t count = min(64u, last - w0 + 1);
+        for (uint32_t i0 = 0; i0 < count; i0 += 4) {   // (four parts' loads under way)
+            float part[4][4];
+#pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const uint32_t c = lane + 64 * i;
-                if (c < P.dim) o[i] += wj * to_f32(v[c]);
+                const uint32_t w = w0 + min(i0 + i, count - 1);
+                const float *from_part = P.part_out + ((uint64_t)(w == first ? first_slot : 2 * w) * P.group + q) * P.dim;
+#pragma unroll
+                for (int c = 0; c < 4; ++c) part[i][c] = lane + 64 * c < P.dim ? from_part[lane + 64 * c] : 0.f;
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float f = i0 + i < count ? __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, by), (int)(i0 + i) & 63)) : 0.f;
+#pragma unroll
+                for (int c = 0; c < 4; ++c) o[c] += f * part[i][c];
             }
         }
-        __syncthreads();
     }
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) sum += __shfl_xor(sum, d);
     const float by = sum == 0.f ? 0.f : P.out_by / sum;
-    for (int i = 0; i < 4; ++i) {
-        const uint32_t c = lane + 64 * i;
-        if (c < P.dim) ((T *)P.out)[((uint64_t)row * P.q_heads + qh) * P.dim + c] = from_f32<T>(o[i] * by);
-    }
-    if (P.lse && lane == 0) P.lse[(uint64_t)row * P.q_heads + qh] = most == -INFINITY && sum == 0.f ? -INFINITY : most + logf(sum);
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+        if (lane + 64 * c < P.dim) out[lane + 64 * c] = from_f32<T>(o[c] * by);
+    if (P.lse && lane == 0) P.lse[id] = sum == 0.f && most == -INFINITY ? -INFINITY : (most + __builtin_amdgcn_logf(sum)) * kLn2;
 }
 
 }  // namespace

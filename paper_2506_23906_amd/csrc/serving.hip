@@ -81,12 +81,13 @@ mmv_status mmv_paged_attention(uint64_t n, uint32_t q_heads, const void *d_q, ui
     if (const mmv_status st = check_workspace(d_ws, ws_bytes, attention_workspace(n, q_heads, cache->heads, cache->dim, table_width * cache->page))) return st;
     AttentionParams P = {};
     P.q = d_q, P.k = cache->d_k, P.v = cache->d_v, P.q_stride = q_stride;
-    P.page_stride = cache->page_stride, P.head_stride = cache->head_stride, P.slot_stride = cache->slot_stride;
-    P.table = d_table, P.context = d_context, P.table_stride = table_stride, P.max_context = table_width * cache->page;
+    P.page_stride = (uint32_t)cache->page_stride, P.head_stride = cache->head_stride, P.slot_stride = (uint32_t)cache->slot_stride;
+    P.table = d_table, P.context = d_context, P.table_stride = table_stride;
+    P.max_context = cache->pages ? (uint32_t)(table_width * cache->page) : 0u;   // (no pages: nothing to look at)
     P.out = d_out, P.lse = d_lse;
     P.n = (uint32_t)n, P.q_heads = q_heads, P.heads = cache->heads, P.group = q_heads / cache->heads, P.dim = cache->dim;
     P.page = cache->page, P.pages = (uint32_t)cache->pages, P.window = window;
-    P.score_by = scale * cache->k_scale, P.out_by = cache->v_scale;
+    P.score_by = scale * cache->k_scale * kLog2e, P.out_by = cache->v_scale;
     return attention_call(P, type, cache->type, d_ws, (hipStream_t)hip_stream);
 }
 

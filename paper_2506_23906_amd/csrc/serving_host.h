@@ -28,8 +28,8 @@ inline mmv_status check_cache(const mmv_paged_cache *c, int type) {
     if (!valid_value_type(type) || (own != MMV_TYPE_E4M3 && own != type)) return MMV_ERR_INVALID_ARG;
     if (c->page < 1 || c->page > 65536 || c->heads < 1 || c->heads > kMostHeads || c->dim < 8 || c->dim > 256 || c->dim % 8) return MMV_ERR_INVALID_ARG;
     if (c->pages >= k2to31 || c->pages * c->page >= k2to31 || c->page_stride % 8 || c->head_stride % 8 || c->slot_stride % 8) return MMV_ERR_INVALID_ARG;
-    // (the largest offset, in bytes, of a cache of 2^31 slots is far below 2^63: strides up to 2^30 are sense)
-    if (c->page_stride > (1ull << 40) || c->head_stride > (1ull << 40) || c->slot_stride > (1ull << 40)) return MMV_ERR_INVALID_ARG;
+    // (kernels hold the strides of pages and slots in 32 bits; heads may lie further apart)
+    if (c->page_stride >= k2to31 || c->head_stride > (1ull << 40) || c->slot_stride >= k2to31) return MMV_ERR_INVALID_ARG;
     if (own == MMV_TYPE_E4M3 ? !(c->k_scale > 0.f && c->v_scale > 0.f && c->k_scale < INFINITY && c->v_scale < INFINITY) : !(c->k_scale == 1.f && c->v_scale == 1.f)) return MMV_ERR_INVALID_ARG;
     if (c->pages && (!c->d_k || !c->d_v)) return MMV_ERR_NULL;
     return aligned_to(c->d_k, 16) && aligned_to(c->d_v, 16) ? MMV_OK : MMV_ERR_INVALID_ARG;
@@ -58,16 +58,57 @@ inline bool attention_sizes(uint64_t n, uint32_t q_heads, uint32_t heads, uint32
     return n < kMostRequests && heads >= 1 && heads <= kMostHeads && q_heads >= heads && q_heads % heads == 0 && q_heads / heads <= 16 && dim >= 8 && dim <= 256 && dim % 8 == 0 &&
            max_context < k2to31 && n * q_heads < k2to31;
 }
-inline size_t attention_workspace(uint64_t, uint32_t, uint32_t, uint32_t, uint64_t) { return 0; }
-mmv_status attention_call(const AttentionParams &P, int type, int cache_type, void *, hipStream_t s) {
-    const unsigned blocks = P.n * P.q_heads;
-    if (type == MMV_TYPE_F16) {
-        if (cache_type == MMV_TYPE_E4M3) paged_attention_kernel<f16_t, e4m3_t><<<blocks, 64, 0, s>>>(P);
-        else paged_attention_kernel<f16_t, f16_t><<<blocks, 64, 0, s>>>(P);
-    } else {
-        if (cache_type == MMV_TYPE_E4M3) paged_attention_kernel<bf16_t, e4m3_t><<<blocks, 64, 0, s>>>(P);
-        else paged_attention_kernel<bf16_t, bf16_t><<<blocks, 64, 0, s>>>(P);
-    }
+// Waves that share the list of tiles: those that the device holds at once (by the registers of the kernel for this dim), or one for every tile there
+// can be.
+constexpr uint32_t kUnits = 256;   // compute units of an MI355X
+inline uint32_t attention_blocks_per_unit(uint32_t dim) { return dim > 128 ? 1 : 2; }
+inline uint32_t attention_workers(uint64_t n, uint32_t heads, uint32_t dim, uint64_t max_context) {
+    const uint64_t tiles = n * heads * ceil_div(max_context, kTile), most = 4ull * kUnits * attention_blocks_per_unit(dim);
+    const uint64_t w = tiles < most ? tiles : most;
+    return w < 1 ? 1u : (uint32_t)w;
+}
+struct AttentionLayout {
+    size_t ml, out, total;
+};
+inline AttentionLayout attention_layout(uint64_t n, uint32_t q_heads, uint32_t heads, uint32_t dim, uint64_t max_context) {
+    const size_t parts = 2ull * attention_workers(n, heads, dim, max_context) * (q_heads / heads);
+    AttentionLayout L;
+    L.ml = round256(8 * (n + 1));
+    L.out = L.ml + round256(8 * parts);
+    L.total = L.out + round256(4 * parts * dim);
+    return L;
+}
+inline size_t attention_workspace(uint64_t n, uint32_t q_heads, uint32_t heads, uint32_t dim, uint64_t max_context) { return attention_layout(n, q_heads, heads, dim, max_context).total; }
+
+template <typename T, bool kE4m3> void launch_attention(const AttentionParams &P, hipStream_t s) {
+    const unsigned blocks = (P.workers + 3) / 4;
+    const bool packed = P.slot_stride == P.dim;
+    if (P.dim == 64 && packed) paged_attention_kernel<2, true, T, kE4m3><<<blocks, 256, 0, s>>>(P);
+    else if (P.dim == 128 && packed) paged_attention_kernel<4, true, T, kE4m3><<<blocks, 256, 0, s>>>(P);
+    else if (P.dim == 256 && packed) paged_attention_kernel<8, true, T, kE4m3><<<blocks, 256, 0, s>>>(P);
+    else if (P.dim <= 64) paged_attention_kernel<2, false, T, kE4m3><<<blocks, 256, 0, s>>>(P);
+    else if (P.dim <= 96) paged_attention_kernel<3, false, T, kE4m3><<<blocks, 256, 0, s>>>(P);
+    else if (P.dim <= 128) paged_attention_kernel<4, false, T, kE4m3><<<blocks, 256, 0, s>>>(P);
+    else if (P.dim <= 160) paged_attention_kernel<5, false, T, kE4m3><<<blocks, 256, 0, s>>>(P);
+    else paged_attention_kernel<8, false, T, kE4m3><<<blocks, 256, 0, s>>>(P);
+}
+mmv_status attention_call(AttentionParams P, int type, int cache_type, void *d_ws, hipStream_t s) {
+    const AttentionLayout L = attention_layout(P.n, P.q_heads, P.heads, P.dim, P.max_context);
+    P.sums = (uint64_t *)d_ws, P.part_ml = (float *)((char *)d_ws + L.ml), P.part_out = (float *)((char *)d_ws + L.out);
+    P.workers = attention_workers(P.n, P.heads, P.dim, P.max_context);
+    // Division of a number below 2^28 by page / 8: a shift, or a product's upper half and a shift (exact: the factor is at most 2^-28 of itself too large).
+    P.page_groups = P.page / 8;
+    uint32_t bits = 0;
+    while ((1u << bits) < P.page_groups) ++bits;
+    if ((1u << bits) == P.page_groups) P.groups_by = 0, P.groups_shift = bits;
+    else P.groups_by = (uint32_t)(((1ull << (31 + bits)) + P.page_groups - 1) / P.page_groups), P.groups_shift = bits - 1;
+    const bool e4m3 = cache_type == MMV_TYPE_E4M3;
+    if (type == MMV_TYPE_F16) e4m3 ? launch_attention<f16_t, true>(P, s) : launch_attention<f16_t, false>(P, s);
+    else e4m3 ? launch_attention<bf16_t, true>(P, s) : launch_attention<bf16_t, false>(P, s);
+    if (const mmv_status st = launched()) return st;
+    const unsigned blocks = (unsigned)ceil_div((uint64_t)P.n * P.q_heads, 4);
+    if (type == MMV_TYPE_F16) join_attention_kernel<f16_t><<<blocks, 256, 0, s>>>(P);
+    else join_attention_kernel<bf16_t><<<blocks, 256, 0, s>>>(P);
     return launched();
 }
 
