@@ -135,12 +135,49 @@ mmv_status decay_params(DecayParams &P, uint64_t n, uint64_t tokens, uint32_t he
     P.n = (uint32_t)n, P.heads = heads, P.group = heads / kv_heads, P.dk = dk, P.dv = dv, P.scale = scale;
     return MMV_OK;
 }
-inline size_t decay_workspace(uint64_t, uint64_t, uint32_t, uint32_t, uint32_t) { return 0; }
-mmv_status decay_call(const DecayParams &P, int type, void *, hipStream_t s) {
+// Tokens of a block of a prompt.
+inline uint32_t decay_block(uint64_t tokens, uint32_t heads) {
+    if (tokens <= 1024) return 1024;
+    const uint64_t even = ceil_div(tokens * heads, 1024 * kChunk) * kChunk;
+    return (uint32_t)(even < 256 ? 256 : even > 4096 ? 4096 : even);
+}
+inline uint64_t decay_blocks(uint64_t n, uint64_t tokens, uint32_t heads) { return n + tokens / decay_block(tokens, heads); }   // at most
+inline size_t decay_workspace(uint64_t n, uint64_t tokens, uint32_t heads, uint32_t dk, uint32_t dv) {
+    if (tokens <= decay_block(tokens, heads)) return 0;   // (one block for every request)
+    return round256(decay_blocks(n, tokens, heads) * heads * dk * dv * 4);
+}
+template <int KD, int NW, typename T> mmv_status launch_prompts(const PromptParams &P, hipStream_t s) {
+    const DecayParams &d = P.d;
+    const uint64_t groups = (uint64_t)P.blocks * d.heads;
+    if (groups >= k2to31) return MMV_ERR_INVALID_ARG;
+    if (P.block_states) {
+        decay_prompt_kernel<KD, NW, T, true><<<(unsigned)groups, 64 * NW, 0, s>>>(P);
+        if (const mmv_status st = launched()) return st;
+        const uint64_t slices = ceil_div((uint64_t)d.dk * d.dv, 1024) * d.heads * d.n;
+        if (slices >= k2to31) return MMV_ERR_INVALID_ARG;
+        decay_blocks_kernel<<<(unsigned)slices, 256, 0, s>>>(P);
+        if (const mmv_status st = launched()) return st;
+    }
+    decay_prompt_kernel<KD, NW, T, false><<<(unsigned)groups, 64 * NW, 0, s>>>(P);
+    return launched();
+}
+template <int KD, typename T> mmv_status launch_prompts_of(const PromptParams &P, hipStream_t s) {
+    const uint32_t dv = P.d.dv;
+    return dv <= 64 ? launch_prompts<KD, 2, T>(P, s) : dv <= 128 ? launch_prompts<KD, 4, T>(P, s) : dv <= 160 ? launch_prompts<KD, 5, T>(P, s) : launch_prompts<KD, 8, T>(P, s);
+}
+mmv_status decay_call(const DecayParams &d, int type, void *d_ws, hipStream_t s) {
+    PromptParams P = {};
+    P.d = d;
+    P.block = decay_block(d.tokens, d.heads);
+    P.blocks = (uint32_t)decay_blocks(d.n, d.tokens, d.heads);
+    P.block_states = d.tokens > P.block ? (float *)d_ws : nullptr;
+    if (type == MMV_TYPE_F16) return d.dk <= 64 ? launch_prompts_of<2, f16_t>(P, s) : launch_prompts_of<4, f16_t>(P, s);
+    return d.dk <= 64 ? launch_prompts_of<2, bf16_t>(P, s) : d.dk <= 96 ? launch_prompts_of<3, bf16_t>(P, s) : launch_prompts_of<4, bf16_t>(P, s);
+}
+mmv_status decay_step_call(const DecayParams &P, int type, hipStream_t s) {
     if (type == MMV_TYPE_F16) decay_kernel<f16_t><<<P.n * P.heads, kMostDv, 0, s>>>(P);
     else decay_kernel<bf16_t><<<P.n * P.heads, kMostDv, 0, s>>>(P);
     return launched();
 }
-mmv_status decay_step_call(const DecayParams &P, int type, hipStream_t s) { return decay_call(P, type, nullptr, s); }
 
 }  // namespace
