@@ -138,6 +138,8 @@ def load() -> ctypes.CDLL:
     if marshal is not None:
         marshal.bind(*(ctypes.cast(getattr(lib, name), vp).value for name in
                        ("mmv_segscan", "mmv_segsum", "mmv_scan", "mmv_compress", "mmv_spmv_coo", "mmv_spmv_csr", "mmv_spmv_coo_run", "mmv_spmv_csr_run")))
+        marshal.bind_serving(*(ctypes.cast(getattr(lib, name), vp).value for name in
+                               ("mmv_page_tables", "mmv_cache_append", "mmv_paged_attention", "mmv_decay_attention", "mmv_decay_step")))
     _lib, _marshal = lib, marshal
     return lib
 
@@ -583,6 +585,12 @@ def mmv_page_tables_workspace_bytes(n: int) -> int:
 def mmv_page_tables(cached: torch.Tensor, new: torch.Tensor, free: torch.Tensor, table: torch.Tensor, page: int, max_tokens: int,
                     out: PageTables | None = None, ws: torch.Tensor | None = None, stream=None) -> PageTables:
     """Pages for the new tokens of every request (written into `table`) and the slot of every one; returns PageTables."""
+    if _marshal is not None:
+        st = _marshal.page_tables(cached, new, free, table, page, max_tokens, out, ws, stream)
+        if st is not None:
+            if st:
+                _check(st, "mmv_page_tables")
+            return out
     lib, n, device = load(), new.numel(), new.device
     if out is None:
         out = PageTables(*(torch.empty(k, dtype=d, device=device) for k, d in
@@ -599,6 +607,12 @@ def mmv_page_tables(cached: torch.Tensor, new: torch.Tensor, free: torch.Tensor,
 
 def mmv_cache_append(k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, cache: PagedCache, stream=None) -> None:
     """The keys and values [tokens, heads, dim] of new tokens into their slots."""
+    if _marshal is not None:
+        st = _marshal.cache_append(k, v, slots, cache._ref, stream)
+        if st is not None:
+            if st:
+                _check(st, "mmv_cache_append")
+            return
     if k.dtype not in _VALUE_TYPES or k.dim() != 3:
         raise MmvError("k and v must be [tokens, heads, dim] of float16 or bfloat16")
     shape = (k.shape[0], cache.k.shape[1], cache.k.shape[3])
@@ -616,6 +630,12 @@ def mmv_paged_attention(q: torch.Tensor, cache: PagedCache, table: torch.Tensor,
                         out: torch.Tensor | None = None, lse: torch.Tensor | None = None, ws: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """Attention of one token q[r] ([rows, query heads, dim]) over the first context[r] positions of every row of the table, or the last
     `window` of them; returns out like q.  scale: dim ** -0.5 if left out; lse: fp32 [rows, query heads], filled if given."""
+    if _marshal is not None:
+        st = _marshal.paged_attention(q, cache._ref, table, context, scale, window, out, lse, ws, stream)
+        if st is not None:
+            if st:
+                _check(st, "mmv_paged_attention")
+            return out
     if q.dtype not in _VALUE_TYPES or q.dim() != 3:
         raise MmvError("q must be [rows, heads, dim] of float16 or bfloat16")
     lib, (n, heads, dim), own = load(), q.shape, cache.k.shape
@@ -660,6 +680,12 @@ def mmv_decay_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, offse
                         out: torch.Tensor | None = None, ws: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """Linear attention with a decay for each head over packed requests; q [tokens, heads, dk], k [tokens, kv heads, dk], v [tokens, kv heads,
     dv], states [states, heads, dk, dv] of fp32; returns out [tokens, heads, dv].  scale: dk ** -0.5 if left out."""
+    if _marshal is not None:
+        st = _marshal.decay_attention(q, k, v, offsets, log_decay, scale, state_in, state_out, state_index, out, ws, stream)
+        if st is not None:
+            if st:
+                _check(st, "mmv_decay_attention")
+            return out
     n = offsets.numel() - 1
     if n < 0:
         raise MmvError("offsets must hold the first token of every request, and their number")
@@ -675,6 +701,12 @@ def mmv_decay_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_decay:
                    state_out: torch.Tensor | None = None, scale: float | None = None, state_index: torch.Tensor | None = None,
                    out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """mmv_decay_attention for one token of every request."""
+    if _marshal is not None:
+        st = _marshal.decay_step(q, k, v, log_decay, state_in, state_out, scale, state_index, out, stream)
+        if st is not None:
+            if st:
+                _check(st, "mmv_decay_step")
+            return out
     t, head, decay, state, out = _decay_arguments(q, k, v, log_decay, state_in, state_out, state_index, q.shape[0], out)
     st = load().mmv_decay_step(t, *head, *decay, head[2] ** -0.5 if scale is None else scale, *state, _stream_ptr(stream))
     _check(st, "mmv_decay_step")

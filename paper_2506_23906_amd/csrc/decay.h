@@ -40,39 +40,58 @@ __device__ __forceinline__ Span span_of(const DecayParams &P, uint32_t r) {
     return {(uint32_t)a, (uint32_t)b};
 }
 
-// One workgroup for a request and head, token by token: a thread has a column of the state.
-template <typename T> __global__ __launch_bounds__(kMostDv) void decay_kernel(DecayParams P) {
+// ---- single tokens -------------------------------------------------------------------------------------------------
+//
+// Bound by reading and writing the state: 8 dk dv bytes for 4 dk dv operations.  A workgroup has one state; a thread takes four
+// columns (16 bytes) of every kth row, kRows of them loaded before the first is used, and the sums over the rows go through LDS.
+template <typename T, int kRows> __global__ __launch_bounds__(256) void decay_step_kernel(DecayParams P) {
     __shared__ float query[kMostDk], key[kMostDk];
-    const uint32_t r = blockIdx.x / P.heads, h = blockIdx.x % P.heads, c = threadIdx.x, kv = h / P.group;
-    const Span span = span_of(P, r);
-    const uint64_t state = state_of(P, r), matrix = (uint64_t)P.dk * P.dv;
-    const float decay = expf(head_decay(P, h));
-    float S[kMostDk];
+    __shared__ __align__(16) float part[256 * 4];
+    const uint32_t r = blockIdx.x / P.heads, h = blockIdx.x % P.heads, tid = threadIdx.x, kv = h / P.group;
+    const uint64_t state = state_of(P, r), at = (state * P.heads + h) * ((uint64_t)P.dk * P.dv);
+    const bool have = state != ~0ull;
+    const uint32_t quads = P.dv / 4, step = 256 / quads, first = tid / quads, c = (tid - first * quads) * 4;   // (threads beyond step * quads have no rows)
+    const bool live = first < step;
+    const float *in = P.state_in && have ? P.state_in + at + c : nullptr;
+    float *to = P.state_out && have ? P.state_out + at + c : nullptr;
+    f32x4 S[kRows];
+    const auto load = [&](uint32_t row) __attribute__((always_inline)) {
 #pragma unroll
-    for (uint32_t i = 0; i < kMostDk; ++i)
-        S[i] = P.state_in && state != ~0ull && i < P.dk && c < P.dv ? P.state_in[(state * P.heads + h) * matrix + (uint64_t)i * P.dv + c] : 0.f;
-    for (uint32_t t = span.begin; t < span.end; ++t) {
-        __syncthreads();
-        if (c < kMostDk) {
-            query[c] = c < P.dk ? to_f32(((const T *)P.q)[t * P.q_stride + (uint64_t)h * P.dk + c]) : 0.f;
-            key[c] = c < P.dk ? to_f32(((const T *)P.k)[t * P.k_stride + (uint64_t)kv * P.dk + c]) : 0.f;
+        for (int i = 0; i < kRows; ++i) {
+            S[i] = (f32x4){0.f, 0.f, 0.f, 0.f};
+            if (in && live && row + i * step < P.dk) S[i] = *(const f32x4 *)(in + (uint64_t)(row + i * step) * P.dv);
         }
-        __syncthreads();
-        const float v = c < P.dv ? to_f32(((const T *)P.v)[t * P.v_stride + (uint64_t)kv * P.dv + c]) : 0.f;
-        float o = 0.f;
-#pragma unroll
-        for (uint32_t i = 0; i < kMostDk; ++i) {
-            S[i] = S[i] * decay + key[i] * v;
-            o += query[i] * S[i];
-        }
-        if (c < P.dv) ((T *)P.out)[((uint64_t)t * P.heads + h) * P.dv + c] = from_f32<T>(o * P.scale);
+    };
+    load(first);
+    if (tid < P.dk) {
+        query[tid] = to_f32(((const T *)P.q)[r * P.q_stride + (uint64_t)h * P.dk + tid]);
+        key[tid] = to_f32(((const T *)P.k)[r * P.k_stride + (uint64_t)kv * P.dk + tid]);
     }
-    if (P.state_out && state != ~0ull && c < P.dv)
+    const T *pv = (const T *)P.v + r * P.v_stride + (uint64_t)kv * P.dv + c;
+    f32x4 v = {0.f, 0.f, 0.f, 0.f}, o = {0.f, 0.f, 0.f, 0.f};
+    if (live) v = (f32x4){to_f32(pv[0]), to_f32(pv[1]), to_f32(pv[2]), to_f32(pv[3])};
+    const float decay = __builtin_amdgcn_exp2f(head_decay(P, h) * kLog2e);
+    __syncthreads();
+    for (uint32_t row = first; live && row < P.dk; row += kRows * step) {
+        if (row != first) load(row);
 #pragma unroll
-        for (uint32_t i = 0; i < kMostDk; ++i)
-            if (i < P.dk) P.state_out[(state * P.heads + h) * matrix + (uint64_t)i * P.dv + c] = S[i];
+        for (int i = 0; i < kRows; ++i) {
+            const uint32_t d = row + i * step;
+            if (d < P.dk) {
+                S[i] = S[i] * decay + key[d] * v;
+                o += query[d] * S[i];
+                if (to) *(f32x4 *)(to + (uint64_t)d * P.dv) = S[i];
+            }
+        }
+    }
+    if (live) *(f32x4 *)&part[first * P.dv + c] = o;
+    __syncthreads();
+    if (tid < P.dv) {
+        float sum = 0.f;
+        for (uint32_t i = 0; i < step; ++i) sum += part[i * P.dv + tid];
+        ((T *)P.out)[((uint64_t)r * P.heads + h) * P.dv + tid] = from_f32<T>(sum * P.scale);
+    }
 }
-
 
 // ---- prompts ------------------------------------------------------------------------------------------------------
 //

@@ -30,7 +30,7 @@ struct AttentionParams {
     void *out;
     float *lse;
     float *part_out, *part_ml;                     // [2 * workers][group][dim], [2 * workers][group][2]
-    uint64_t *sums;                                // [n + 1] tiles of a head before every row, and of all
+    uint32_t *sums;                                // [n + 1] tiles of a head before every row, and of all
     uint32_t n, q_heads, heads, group, dim, page, pages, window, max_context, workers;
     uint32_t groups_by, groups_shift, page_groups; // division by page / 8
     float score_by, out_by;                        // scale * k_scale * log2(e), v_scale
@@ -78,16 +78,19 @@ __device__ __forceinline__ RowTiles row_tiles(const AttentionParams &P, int32_t 
     const uint32_t first = begin / kTile;
     return {begin, end, first, (end + kTile - 1) / kTile - first};
 }
-__device__ __forceinline__ uint64_t wave_total(uint64_t v) {
-#pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) v += __shfl_xor(v, d);
-    return v;
-}
-__device__ __forceinline__ uint64_t uniform64(uint64_t v) {
-    return ((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(v >> 32)) << 32) | (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)v);
-}
 __device__ __forceinline__ uint32_t uniform(uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); }
-__device__ __forceinline__ uint64_t run_of(uint64_t tiles, uint32_t workers) { return (tiles + workers - 1) / workers; }
+__device__ __forceinline__ uint32_t lane_value(uint32_t v, int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)v, lane); }
+// Inclusive sums over the lanes of a wave.
+__device__ __forceinline__ uint32_t wave_upto(uint32_t v) {
+    v += dpp_or_zero<0x111, 0xF>(v);
+    v += dpp_or_zero<0x112, 0xF>(v);
+    v += dpp_or_zero<0x114, 0xF>(v);
+    v += dpp_or_zero<0x118, 0xF>(v);
+    v += dpp_or_zero<0x142, 0xA>(v);
+    return v + dpp_or_zero<0x143, 0xC>(v);
+}
+// Tiles of a wave's run.  (The list has less than 2^32 tiles: checked on the host.)
+__device__ __forceinline__ uint32_t run_of(uint32_t tiles, uint32_t workers) { return tiles / workers + (tiles % workers ? 1u : 0u); }
 
 // Where a wave is in the list of tiles (the same in all its lanes).
 struct Place {
@@ -293,42 +296,42 @@ template <int KS, bool kExact, typename T, bool kE4m3> __global__ __launch_bound
     constexpr int kDims = TileT::kDims;
     const uint32_t lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
     const uint32_t worker = uniform(blockIdx.x * 4 + (threadIdx.x >> 6));
-    // the list's length, and this wave's run of it
-    uint64_t all = 0;
-    for (uint32_t i = lane; i < P.n; i += 64) all += row_tiles(P, P.context[i]).count;
-    all = uniform64(wave_total(all));
-    const uint64_t run = run_of(all * P.heads, P.workers), start = worker * run;
-    uint64_t left = start < all * P.heads ? min(run, all * P.heads - start) : 0;
+    // the list's length, this wave's run of it, and where that begins
+    uint32_t first_counts = lane < P.n ? row_tiles(P, P.context[lane]).count : 0u, all_rows = 0;
+    const uint32_t first_upto = wave_upto(first_counts);
+    all_rows = lane_value(first_upto, 63);
+    if (P.n > 64) {
+        uint32_t more = 0;
+        for (uint32_t i = 64 + lane; i < P.n; i += 64) more += row_tiles(P, P.context[i]).count;
+        all_rows += lane_value(wave_upto(more), 63);
+    }
+    const uint32_t all = all_rows * P.heads, run = run_of(all, P.workers), start = worker < P.workers && run ? worker * run : all;
+    uint32_t left = start < all && start / run == worker ? min(run, all - start) : 0;
     if (worker == 0 || left) {
-        uint64_t before = 0, found_before = 0;
-        const uint64_t target = start / P.heads;
-        uint32_t row = 0;
+        uint32_t before = 0, row = 0, rows_before = 0;
+        const uint32_t target = start / P.heads;
         bool found = false;
         for (uint32_t first = 0; first < P.n && (worker == 0 || !found); first += 64) {
-            const uint32_t i = first + lane;
-            const uint64_t own = i < P.n ? row_tiles(P, P.context[i]).count : 0;
-            uint64_t upto = own;
-#pragma unroll
-            for (int d = 1; d < 64; d <<= 1) upto += shift_up64(upto, d, (int)lane);
+            const uint32_t i = first + lane, own = first == 0 ? first_counts : i < P.n ? row_tiles(P, P.context[i]).count : 0u;
+            const uint32_t upto = first == 0 ? first_upto : wave_upto(own);
             if (worker == 0 && i < P.n) P.sums[i] = before + upto - own;
             const uint64_t hit = __ballot(before + upto > target);
             if (hit && !found) {
                 const int l = __builtin_ctzll(hit);
                 found = true;
                 row = first + l;
-                found_before = before + uniform64(__shfl(upto - own, l));
+                rows_before = before + lane_value(upto - own, l);
             }
-            before += uniform64(__shfl(upto, 63));
+            before += lane_value(upto, 63);
         }
-        if (worker == 0 && lane == 0) P.sums[P.n] = all;
+        if (worker == 0 && lane == 0) P.sums[P.n] = all_rows;
         if (!left) return;
         Place at;
         at.row = uniform(row);
         enter_row(P, at);
-        const uint64_t inside = start - found_before * P.heads;
-        const uint32_t count = at.last - at.first;
-        at.head = uniform((uint32_t)(inside / count));
-        at.tile = at.first + uniform((uint32_t)(inside % count));
+        const uint32_t inside = start - rows_before * P.heads, count = at.last - at.first;
+        at.head = uniform(inside / count);
+        at.tile = at.first + uniform(inside % count);
         bool begun = at.tile != at.first;   // the current segment began in an earlier wave's run
 
         TileT tile;
@@ -416,61 +419,70 @@ template <int KS, bool kExact, typename T, bool kE4m3> __global__ __launch_bound
     }
 }
 
-// Joins the parts of the segments that several waves share, and writes the rows without positions: one wave for a row and query head.
+// Joins the parts of the segments that several waves share, and writes the rows without positions: a workgroup for a row and query head.  Its
+// four waves take every fourth part each, eight of them under way at a time.
 template <typename T> __global__ __launch_bounds__(256) void join_attention_kernel(AttentionParams P) {
-    const uint32_t lane = threadIdx.x & 63, id = uniform(blockIdx.x * 4 + (threadIdx.x >> 6));
-    if (id >= P.n * P.q_heads) return;
-    const uint32_t row = id / P.q_heads, qh = id % P.q_heads, h = qh / P.group, q = qh % P.group;
-    const uint64_t before = P.sums[row], tiles = P.sums[row + 1] - before, all = P.sums[P.n] * P.heads;
+    __shared__ float lds[4][256 + 2];
+    const uint32_t lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), id = blockIdx.x;
+    const uint32_t row = id / P.q_heads, qh = id - row * P.q_heads, h = qh / P.group, q = qh - h * P.group;
+    const uint32_t before = (uint32_t)scalar_load((const int32_t *)P.sums + row), behind = (uint32_t)scalar_load((const int32_t *)P.sums + row + 1);
+    const uint32_t all = (uint32_t)scalar_load((const int32_t *)P.sums + P.n) * P.heads, tiles = behind - before;
     T *out = (T *)P.out + (uint64_t)id * P.dim;
     if (tiles == 0) {
-        for (uint32_t d = lane; d < P.dim; d += 64) out[d] = from_f32<T>(0.f);
-        if (P.lse && lane == 0) P.lse[id] = -INFINITY;
+        if (threadIdx.x < P.dim) out[threadIdx.x] = from_f32<T>(0.f);
+        if (P.lse && threadIdx.x == 0) P.lse[id] = -INFINITY;
         return;
     }
-    const uint64_t from = before * P.heads + h * tiles, to = from + tiles, run = run_of(all, P.workers);
-    const uint32_t first = (uint32_t)(from / run), last = (uint32_t)((to - 1) / run);
+    const uint32_t from = before * P.heads + h * tiles, run = run_of(all, P.workers), first = from / run, last = (from + tiles - 1) / run;
     if (first == last) return;   // (written by that wave)
-    const uint32_t first_slot = 2 * first + 1;   // (the segment begins in that wave's run)
-    float most = -INFINITY;
-    for (uint32_t w = first + lane; w <= last; w += 64) most = fmaxf(most, P.part_ml[2 * ((uint64_t)(w == first ? first_slot : 2 * w) * P.group + q)]);
+    // (the segment begins in the first wave's run: its part is that wave's second one)
+    const auto place = [&](uint32_t w) __attribute__((always_inline)) { return (uint64_t)(2 * w + (w == first ? 1 : 0)) * P.group + q; };
+    float most = -INFINITY, sum = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+    for (uint32_t w0 = first + wave; w0 <= last; w0 += 32) {
+        float part[8][4], m[8], l[8];
 #pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) most = fmaxf(most, __shfl_xor(most, d));
-    const float base = most == -INFINITY ? 0.f : most;
-    float sum = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-    for (uint32_t w0 = first; w0 <= last; w0 += 64) {
-        const uint32_t mine = w0 + lane;
-        float by = 0.f;
-        if (mine <= last) {
-            const float *ml = P.part_ml + 2 * ((uint64_t)(mine == first ? first_slot : 2 * mine) * P.group + q);
-            by = __builtin_amdgcn_exp2f(ml[0] - base);
-            sum += by * ml[1];
+        for (int i = 0; i < 8; ++i) {
+            const uint64_t at = place(min(w0 + 4 * i, last));
+            m[i] = P.part_ml[2 * at], l[i] = P.part_ml[2 * at + 1];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) part[i][c] = lane + 64 * c < P.dim ? P.part_out[at * P.dim + lane + 64 * c] : 0.f;
         }
-        const uint32_t count = min(64u, last - w0 + 1);
-        for (uint32_t i0 = 0; i0 < count; i0 += 4) {   // (four parts' loads under way)
-            float part[4][4];
+        float top = most;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t w = w0 + min(i0 + i, count - 1);
-                const float *from_part = P.part_out + ((uint64_t)(w == first ? first_slot : 2 * w) * P.group + q) * P.dim;
+        for (int i = 0; i < 8; ++i) {
+            if (w0 + 4 * i > last) m[i] = -INFINITY;
+            top = fmaxf(top, m[i]);
+        }
+        const float base = top == -INFINITY ? 0.f : top, by = __builtin_amdgcn_exp2f(most - base);
+        most = top, sum *= by;
 #pragma unroll
-                for (int c = 0; c < 4; ++c) part[i][c] = lane + 64 * c < P.dim ? from_part[lane + 64 * c] : 0.f;
-            }
+        for (int c = 0; c < 4; ++c) o[c] *= by;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float f = i0 + i < count ? __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, by), (int)(i0 + i) & 63)) : 0.f;
+        for (int i = 0; i < 8; ++i) {
+            const float f = w0 + 4 * i > last ? 0.f : __builtin_amdgcn_exp2f(m[i] - base);
+            if (f != 0.f) {   // (a part without positions has weight 0; one that is not a number keeps it)
+                sum += f * l[i];
 #pragma unroll
                 for (int c = 0; c < 4; ++c) o[c] += f * part[i][c];
             }
         }
     }
 #pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) sum += __shfl_xor(sum, d);
-    const float by = sum == 0.f ? 0.f : P.out_by / sum;
+    for (int c = 0; c < 4; ++c) lds[wave][lane + 64 * c] = o[c];
+    if (lane == 0) lds[wave][256] = most, lds[wave][257] = sum;
+    __syncthreads();
+    const uint32_t d = threadIdx.x;
+    float top = -INFINITY, total = 0.f, x = 0.f;
 #pragma unroll
-    for (int c = 0; c < 4; ++c)
-        if (lane + 64 * c < P.dim) out[lane + 64 * c] = from_f32<T>(o[c] * by);
-    if (P.lse && lane == 0) P.lse[id] = sum == 0.f && most == -INFINITY ? -INFINITY : (most + __builtin_amdgcn_logf(sum)) * kLn2;
+    for (int w = 0; w < 4; ++w) top = fmaxf(top, lds[w][256]);
+    const float base = top == -INFINITY ? 0.f : top;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        const float f = __builtin_amdgcn_exp2f(lds[w][256] - base);
+        if (f != 0.f) total += f * lds[w][257], x += f * lds[w][d];
+    }
+    if (d < P.dim) out[d] = from_f32<T>(total == 0.f ? 0.f : x * (P.out_by / total));
+    if (P.lse && d == 0) P.lse[id] = total == 0.f && top == -INFINITY ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * kLn2;
 }
 
 }  // namespace

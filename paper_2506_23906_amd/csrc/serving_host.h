@@ -56,7 +56,7 @@ mmv_status append_call(uint64_t tokens, const void *k, uint64_t k_stride, const 
 
 inline bool attention_sizes(uint64_t n, uint32_t q_heads, uint32_t heads, uint32_t dim, uint64_t max_context) {
     return n < kMostRequests && heads >= 1 && heads <= kMostHeads && q_heads >= heads && q_heads % heads == 0 && q_heads / heads <= 16 && dim >= 8 && dim <= 256 && dim % 8 == 0 &&
-           max_context < k2to31 && n * q_heads < k2to31;
+           max_context < k2to31 && n * q_heads < k2to31 && n * heads * ceil_div(max_context, kTile) < 2 * k2to31;
 }
 // Waves that share the list of tiles: those that the device holds at once (by the registers of the kernel for this dim), or one for every tile there
 // can be.
@@ -73,7 +73,7 @@ struct AttentionLayout {
 inline AttentionLayout attention_layout(uint64_t n, uint32_t q_heads, uint32_t heads, uint32_t dim, uint64_t max_context) {
     const size_t parts = 2ull * attention_workers(n, heads, dim, max_context) * (q_heads / heads);
     AttentionLayout L;
-    L.ml = round256(8 * (n + 1));
+    L.ml = round256(4 * (n + 1));
     L.out = L.ml + round256(8 * parts);
     L.total = L.out + round256(4 * parts * dim);
     return L;
@@ -94,7 +94,7 @@ template <typename T, bool kE4m3> void launch_attention(const AttentionParams &P
 }
 mmv_status attention_call(AttentionParams P, int type, int cache_type, void *d_ws, hipStream_t s) {
     const AttentionLayout L = attention_layout(P.n, P.q_heads, P.heads, P.dim, P.max_context);
-    P.sums = (uint64_t *)d_ws, P.part_ml = (float *)((char *)d_ws + L.ml), P.part_out = (float *)((char *)d_ws + L.out);
+    P.sums = (uint32_t *)d_ws, P.part_ml = (float *)((char *)d_ws + L.ml), P.part_out = (float *)((char *)d_ws + L.out);
     P.workers = attention_workers(P.n, P.heads, P.dim, P.max_context);
     // Division of a number below 2^28 by page / 8: a shift, or a product's upper half and a shift (exact: the factor is at most 2^-28 of itself too large).
     P.page_groups = P.page / 8;
@@ -106,7 +106,7 @@ mmv_status attention_call(AttentionParams P, int type, int cache_type, void *d_w
     if (type == MMV_TYPE_F16) e4m3 ? launch_attention<f16_t, true>(P, s) : launch_attention<f16_t, false>(P, s);
     else e4m3 ? launch_attention<bf16_t, true>(P, s) : launch_attention<bf16_t, false>(P, s);
     if (const mmv_status st = launched()) return st;
-    const unsigned blocks = (unsigned)ceil_div((uint64_t)P.n * P.q_heads, 4);
+    const unsigned blocks = P.n * P.q_heads;
     if (type == MMV_TYPE_F16) join_attention_kernel<f16_t><<<blocks, 256, 0, s>>>(P);
     else join_attention_kernel<bf16_t><<<blocks, 256, 0, s>>>(P);
     return launched();
@@ -174,9 +174,15 @@ mmv_status decay_call(const DecayParams &d, int type, void *d_ws, hipStream_t s)
     if (type == MMV_TYPE_F16) return d.dk <= 64 ? launch_prompts_of<2, f16_t>(P, s) : launch_prompts_of<4, f16_t>(P, s);
     return d.dk <= 64 ? launch_prompts_of<2, bf16_t>(P, s) : d.dk <= 96 ? launch_prompts_of<3, bf16_t>(P, s) : launch_prompts_of<4, bf16_t>(P, s);
 }
+template <typename T> void launch_step(const DecayParams &P, hipStream_t s) {
+    const uint32_t rows = (uint32_t)ceil_div(P.dk, 256 / (P.dv / 4));   // of a thread
+    if (rows <= 4) decay_step_kernel<T, 4><<<P.n * P.heads, 256, 0, s>>>(P);
+    else if (rows <= 8) decay_step_kernel<T, 8><<<P.n * P.heads, 256, 0, s>>>(P);
+    else decay_step_kernel<T, 16><<<P.n * P.heads, 256, 0, s>>>(P);
+}
 mmv_status decay_step_call(const DecayParams &P, int type, hipStream_t s) {
-    if (type == MMV_TYPE_F16) decay_kernel<f16_t><<<P.n * P.heads, kMostDv, 0, s>>>(P);
-    else decay_kernel<bf16_t><<<P.n * P.heads, kMostDv, 0, s>>>(P);
+    if (type == MMV_TYPE_F16) launch_step<f16_t>(P, s);
+    else launch_step<bf16_t>(P, s);
     return launched();
 }
 

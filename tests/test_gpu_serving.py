@@ -439,3 +439,37 @@ def test_a_captured_step_follows_its_lengths():
         d["free"][:len(free)] = ints(free)
         run_attention(cache, kc, vc, table, q[i], cached)   # eager work between the replays
         torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_the_calls_give_the_same_through_either_marshalling(native, monkeypatch):
+    """With every argument given, so that the extension takes the calls; and without it.  What it does not take raises in Python."""
+    B.load()
+    assert B._marshal is not None
+    if not native:
+        monkeypatch.setattr(B, "_marshal", None)
+    n, heads, dim, page = 3, 2, 64, 16
+    contexts = [20, 0, 33]
+    cache, kc, vc, table, q = attention_case(51, contexts, heads, 2, dim, page, F16, F16)
+    tables = B.PageTables(torch.empty(4, dtype=torch.int32, device="cuda"), torch.empty(3, dtype=torch.int32, device="cuda"), torch.empty(5, dtype=torch.int64, device="cuda"),
+                          torch.empty(5, dtype=torch.int32, device="cuda"), torch.empty(2, dtype=torch.int64, device="cuda"))
+    ws = B.workspace(1 << 20)
+    rows = ints(table)
+    got = B.mmv_page_tables(ints(contexts), ints([1, 1, 0]), ints([1, 0]), rows, page, 5, out=tables, ws=ws)
+    want = plain_tables(contexts, [1, 1, 0], [1, 0], table, page, 5)
+    assert got is tables and rows.tolist() == want["table"]
+    for name in ("offsets", "context", "slots", "positions", "used"):
+        assert getattr(got, name).tolist() == want[name], name
+    out, lse = torch.empty(n, 4, dim, dtype=F16, device="cuda"), torch.empty(n, 4, device="cuda")
+    assert B.mmv_paged_attention(q.cuda(), cache, ints(table), ints(contexts), scale=0.1, window=0, out=out, lse=lse, ws=ws) is out
+    want, want_lse, by, lse_by = plain_attention(q, kc, vc, table, contexts, 0.1, 0)
+    check(out, want, by, "out")
+    check(lse, want_lse, lse_by, "lse")
+    with pytest.raises(B.MmvError):
+        B.mmv_paged_attention(q.cuda(), cache, ints(table), ints(contexts), scale=0.1, out=out[:2], lse=lse, ws=ws)
+    with pytest.raises(B.MmvError):
+        B.mmv_paged_attention(q.cuda(), cache, ints(table), ints(contexts), scale=0.1, out=out, lse=lse, ws=ws[:256])
+    with pytest.raises(B.MmvError):
+        B.mmv_cache_append(q.cuda(), q.cuda(), ints([0, 1, 2], torch.int64), cache)   # (twice the heads)
+    with pytest.raises(B.MmvError):
+        B.mmv_page_tables(ints(contexts), ints([1, 1, 0]), ints([1, 0]), rows, page, 6, out=tables, ws=ws)
