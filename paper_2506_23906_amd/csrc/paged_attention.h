@@ -99,16 +99,16 @@ struct Place {
 };
 // Uniform loads through the scalar cache: they are not waited for along with the loads of keys and values.
 __device__ __forceinline__ int32_t scalar_load(const int32_t *p) { return *(const __attribute__((address_space(4))) int32_t *)(uintptr_t)p; }
-__device__ __forceinline__ void enter_row(const AttentionParams &P, Place &at) {
-    const RowTiles t = row_tiles(P, scalar_load(P.context + at.row));
+__device__ __forceinline__ void enter_row(const AttentionParams &P, Place &at, int32_t context) {
+    const RowTiles t = row_tiles(P, context);
     at.first = t.first, at.last = t.first + t.count, at.begin = t.begin, at.end = t.end;
 }
 
 template <int KS> constexpr int dims_per_lane() { return KS <= 2 ? 4 : KS <= 4 ? 8 : KS <= 6 ? 12 : 16; }
 template <int KS> constexpr int certain_pieces() { return KS <= 2 ? 1 : KS == 3 ? 9 : KS == 4 ? 13 : KS == 5 ? 17 : 21; }   // of 8 dims, of any dim that takes this KS
 
-// kExact: dim = 32 KS, and a slot's values lie behind those of the slot before.
-template <int KS, bool kExact, typename T, bool kE4m3> struct Tile {
+// kExact: dim = 32 KS, and a slot's values lie behind those of the slot before.  kStream: loads that leave the caches to others.
+template <int KS, bool kExact, bool kStream, typename T, bool kE4m3> struct Tile {
     static constexpr int kDims = dims_per_lane<KS>();
     static constexpr int kSize = kE4m3 ? 1 : 2;
     static constexpr int kKeyWords = kE4m3 ? 2 : 4, kValueWords = kE4m3 ? kDims / 4 : kDims / 2;
@@ -158,15 +158,12 @@ template <int KS, bool kExact, typename T, bool kE4m3> struct Tile {
     static __device__ __forceinline__ uint32_t page_of(const AttentionParams &P, uint32_t g8) { return P.groups_by ? __umulhi(g8, P.groups_by) >> P.groups_shift : g8 >> P.groups_shift; }
     static __device__ __forceinline__ uint32_t slot_stride(const AttentionParams &P) { return kExact ? 32 * KS : P.slot_stride; }
     template <int kWords> static __device__ __forceinline__ void load(uint32_t (&to)[kWords], const char *p) {
-        if constexpr (kWords == 4) {
-            const u32x4 w = *(const u32x4 *)p;
-            to[0] = w[0], to[1] = w[1], to[2] = w[2], to[3] = w[3];
-        } else if constexpr (kWords == 2) {
-            const u32x2 w = *(const u32x2 *)p;
-            to[0] = w[0], to[1] = w[1];
-        } else {
-            to[0] = *(const uint32_t *)p;
-        }
+        typedef uint32_t words __attribute__((ext_vector_type(kWords)));
+        words w;
+        if constexpr (kStream) w = __builtin_nontemporal_load((const words *)p);
+        else w = *(const words *)p;
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) to[i] = w[i];
     }
     __device__ __forceinline__ void load_keys(const AttentionParams &P, uint32_t g) {
         const uint32_t pieces = P.dim / 8;
@@ -291,28 +288,31 @@ template <int kDims, typename T> __device__ __forceinline__ void write_segment(c
     if (g == 0) P.part_ml[2 * part] = most, P.part_ml[2 * part + 1] = sum;
 }
 
-template <int KS, bool kExact, typename T, bool kE4m3> __global__ __launch_bounds__(256, KS > 4 ? 1 : 2) void paged_attention_kernel(AttentionParams P) {
-    using TileT = Tile<KS, kExact, T, kE4m3>;
+template <int KS, bool kExact, bool kStream, typename T, bool kE4m3> __global__ __launch_bounds__(256, KS > 4 ? 1 : 2) void paged_attention_kernel(AttentionParams P) {
+    using TileT = Tile<KS, kExact, kStream, T, kE4m3>;
     constexpr int kDims = TileT::kDims;
     const uint32_t lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
     const uint32_t worker = uniform(blockIdx.x * 4 + (threadIdx.x >> 6));
     // the list's length, this wave's run of it, and where that begins
-    uint32_t first_counts = lane < P.n ? row_tiles(P, P.context[lane]).count : 0u, all_rows = 0;
+    const int32_t first_context = lane < P.n ? P.context[lane] : 0;
+    const uint32_t first_counts = row_tiles(P, first_context).count;
     const uint32_t first_upto = wave_upto(first_counts);
-    all_rows = lane_value(first_upto, 63);
+    uint32_t all_rows = lane_value(first_upto, 63);
     if (P.n > 64) {
         uint32_t more = 0;
         for (uint32_t i = 64 + lane; i < P.n; i += 64) more += row_tiles(P, P.context[i]).count;
         all_rows += lane_value(wave_upto(more), 63);
     }
-    const uint32_t all = all_rows * P.heads, run = run_of(all, P.workers), start = worker < P.workers && run ? worker * run : all;
-    uint32_t left = start < all && start / run == worker ? min(run, all - start) : 0;
+    const uint32_t all = all_rows * P.heads, run = run_of(all, P.workers), start = (uint32_t)min((uint64_t)worker * run, (uint64_t)all);
+    uint32_t left = min(run, all - start);
     if (worker == 0 || left) {
-        uint32_t before = 0, row = 0, rows_before = 0;
+        uint32_t before = 0, row = 0, rows_before = 0, row_context = 0;
         const uint32_t target = start / P.heads;
         bool found = false;
         for (uint32_t first = 0; first < P.n && (worker == 0 || !found); first += 64) {
-            const uint32_t i = first + lane, own = first == 0 ? first_counts : i < P.n ? row_tiles(P, P.context[i]).count : 0u;
+            const uint32_t i = first + lane;
+            const int32_t context = first == 0 ? first_context : i < P.n ? P.context[i] : 0;
+            const uint32_t own = row_tiles(P, context).count;
             const uint32_t upto = first == 0 ? first_upto : wave_upto(own);
             if (worker == 0 && i < P.n) P.sums[i] = before + upto - own;
             const uint64_t hit = __ballot(before + upto > target);
@@ -320,6 +320,7 @@ template <int KS, bool kExact, typename T, bool kE4m3> __global__ __launch_bound
                 const int l = __builtin_ctzll(hit);
                 found = true;
                 row = first + l;
+                row_context = lane_value((uint32_t)context, l);
                 rows_before = before + lane_value(upto - own, l);
             }
             before += lane_value(upto, 63);
@@ -328,7 +329,7 @@ template <int KS, bool kExact, typename T, bool kE4m3> __global__ __launch_bound
         if (!left) return;
         Place at;
         at.row = uniform(row);
-        enter_row(P, at);
+        enter_row(P, at, (int32_t)row_context);
         const uint32_t inside = start - rows_before * P.heads, count = at.last - at.first;
         at.head = uniform(inside / count);
         at.tile = at.first + uniform(inside % count);
@@ -370,7 +371,7 @@ template <int KS, bool kExact, typename T, bool kE4m3> __global__ __launch_bound
                     at.head = 0;
                     do {
                         ++at.row;
-                        enter_row(P, at);
+                        enter_row(P, at, scalar_load(P.context + at.row));
                     } while (at.first == at.last);   // (a row without positions; a later one has some, as `left` says)
                 }
                 at.tile = at.first;

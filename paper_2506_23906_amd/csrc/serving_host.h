@@ -58,53 +58,63 @@ inline bool attention_sizes(uint64_t n, uint32_t q_heads, uint32_t heads, uint32
     return n < kMostRequests && heads >= 1 && heads <= kMostHeads && q_heads >= heads && q_heads % heads == 0 && q_heads / heads <= 16 && dim >= 8 && dim <= 256 && dim % 8 == 0 &&
            max_context < k2to31 && n * q_heads < k2to31 && n * heads * ceil_div(max_context, kTile) < 2 * k2to31;
 }
-// Waves that share the list of tiles: those that the device holds at once (by the registers of the kernel for this dim), or one for every tile there
-// can be.
+// Waves that share the list of tiles: as many as keep 64 KB of keys and values under way on every compute unit (a wave has a tile of both at a time), or
+// one for every tile there can be.  32 rows of 16000, us with 4 / 8 waves on a compute unit: 128 16-bit values (16 KB a tile) 316 / 322,
+// 128 8-bit ones 183 / 164, 64 16-bit ones 178 / 169; 12 and more waves are slower everywhere (48 ragged rows of 128 16-bit values 72 -> 75).
 constexpr uint32_t kUnits = 256;   // compute units of an MI355X
-inline uint32_t attention_blocks_per_unit(uint32_t dim) { return dim > 128 ? 1 : 2; }
-inline uint32_t attention_workers(uint64_t n, uint32_t heads, uint32_t dim, uint64_t max_context) {
-    const uint64_t tiles = n * heads * ceil_div(max_context, kTile), most = 4ull * kUnits * attention_blocks_per_unit(dim);
+inline uint32_t attention_workers(uint64_t n, uint32_t heads, uint32_t dim, uint64_t max_context, bool e4m3) {
+    const uint32_t tile_bytes = 2 * kTile * dim * (e4m3 ? 1 : 2);
+    const uint64_t tiles = n * heads * ceil_div(max_context, kTile), most = 4ull * kUnits * (tile_bytes > 8192 ? 1 : tile_bytes > 4096 ? 2 : 4);
     const uint64_t w = tiles < most ? tiles : most;
     return w < 1 ? 1u : (uint32_t)w;
 }
 struct AttentionLayout {
     size_t ml, out, total;
 };
-inline AttentionLayout attention_layout(uint64_t n, uint32_t q_heads, uint32_t heads, uint32_t dim, uint64_t max_context) {
-    const size_t parts = 2ull * attention_workers(n, heads, dim, max_context) * (q_heads / heads);
+inline AttentionLayout attention_layout(uint64_t n, uint32_t q_heads, uint32_t heads, uint32_t dim, uint64_t max_context, bool e4m3) {
+    const size_t parts = 2ull * attention_workers(n, heads, dim, max_context, e4m3) * (q_heads / heads);
     AttentionLayout L;
     L.ml = round256(4 * (n + 1));
     L.out = L.ml + round256(8 * parts);
     L.total = L.out + round256(4 * parts * dim);
     return L;
 }
-inline size_t attention_workspace(uint64_t n, uint32_t q_heads, uint32_t heads, uint32_t dim, uint64_t max_context) { return attention_layout(n, q_heads, heads, dim, max_context).total; }
+// (for a cache of either size of values)
+inline size_t attention_workspace(uint64_t n, uint32_t q_heads, uint32_t heads, uint32_t dim, uint64_t max_context) { return attention_layout(n, q_heads, heads, dim, max_context, true).total; }
 
-template <typename T, bool kE4m3> void launch_attention(const AttentionParams &P, hipStream_t s) {
+template <bool kStream, typename T, bool kE4m3> void launch_attention(const AttentionParams &P, hipStream_t s) {
     const unsigned blocks = (P.workers + 3) / 4;
     const bool packed = P.slot_stride == P.dim;
-    if (P.dim == 64 && packed) paged_attention_kernel<2, true, T, kE4m3><<<blocks, 256, 0, s>>>(P);
-    else if (P.dim == 128 && packed) paged_attention_kernel<4, true, T, kE4m3><<<blocks, 256, 0, s>>>(P);
-    else if (P.dim == 256 && packed) paged_attention_kernel<8, true, T, kE4m3><<<blocks, 256, 0, s>>>(P);
-    else if (P.dim <= 64) paged_attention_kernel<2, false, T, kE4m3><<<blocks, 256, 0, s>>>(P);
-    else if (P.dim <= 96) paged_attention_kernel<3, false, T, kE4m3><<<blocks, 256, 0, s>>>(P);
-    else if (P.dim <= 128) paged_attention_kernel<4, false, T, kE4m3><<<blocks, 256, 0, s>>>(P);
-    else if (P.dim <= 160) paged_attention_kernel<5, false, T, kE4m3><<<blocks, 256, 0, s>>>(P);
-    else paged_attention_kernel<8, false, T, kE4m3><<<blocks, 256, 0, s>>>(P);
+    if (P.dim == 64 && packed) paged_attention_kernel<2, true, kStream, T, kE4m3><<<blocks, 256, 0, s>>>(P);
+    else if (P.dim == 128 && packed) paged_attention_kernel<4, true, kStream, T, kE4m3><<<blocks, 256, 0, s>>>(P);
+    else if (P.dim == 256 && packed) paged_attention_kernel<8, true, kStream, T, kE4m3><<<blocks, 256, 0, s>>>(P);
+    else if (P.dim <= 64) paged_attention_kernel<2, false, kStream, T, kE4m3><<<blocks, 256, 0, s>>>(P);
+    else if (P.dim <= 96) paged_attention_kernel<3, false, kStream, T, kE4m3><<<blocks, 256, 0, s>>>(P);
+    else if (P.dim <= 128) paged_attention_kernel<4, false, kStream, T, kE4m3><<<blocks, 256, 0, s>>>(P);
+    else if (P.dim <= 160) paged_attention_kernel<5, false, kStream, T, kE4m3><<<blocks, 256, 0, s>>>(P);
+    else paged_attention_kernel<8, false, kStream, T, kE4m3><<<blocks, 256, 0, s>>>(P);
+}
+// A cache that the chip's own (256 MB on the memory side) cannot keep until the next call is read past it.  Us without / with: 48 rows of 330 MB 71.9 ->
+// 68.8, 16 rows of 730 MB 136 -> 123, 13 rows of 160 MB 36.7 -> 35.2; but 24 rows of 56 MB, three such caches in turn, 14.9 -> 16.5.
+constexpr uint64_t kStreamBytes = 128ull << 20;
+template <typename T, bool kE4m3> void launch_attention_over(const AttentionParams &P, hipStream_t s) {
+    const uint64_t bytes = 2ull * P.pages * P.page * P.heads * P.dim * (kE4m3 ? 1 : 2);
+    if (bytes > kStreamBytes) launch_attention<true, T, kE4m3>(P, s);
+    else launch_attention<false, T, kE4m3>(P, s);
 }
 mmv_status attention_call(AttentionParams P, int type, int cache_type, void *d_ws, hipStream_t s) {
-    const AttentionLayout L = attention_layout(P.n, P.q_heads, P.heads, P.dim, P.max_context);
+    const bool e4m3 = cache_type == MMV_TYPE_E4M3;
+    const AttentionLayout L = attention_layout(P.n, P.q_heads, P.heads, P.dim, P.max_context, e4m3);
     P.sums = (uint32_t *)d_ws, P.part_ml = (float *)((char *)d_ws + L.ml), P.part_out = (float *)((char *)d_ws + L.out);
-    P.workers = attention_workers(P.n, P.heads, P.dim, P.max_context);
+    P.workers = attention_workers(P.n, P.heads, P.dim, P.max_context, e4m3);
     // Division of a number below 2^28 by page / 8: a shift, or a product's upper half and a shift (exact: the factor is at most 2^-28 of itself too large).
     P.page_groups = P.page / 8;
     uint32_t bits = 0;
     while ((1u << bits) < P.page_groups) ++bits;
     if ((1u << bits) == P.page_groups) P.groups_by = 0, P.groups_shift = bits;
     else P.groups_by = (uint32_t)(((1ull << (31 + bits)) + P.page_groups - 1) / P.page_groups), P.groups_shift = bits - 1;
-    const bool e4m3 = cache_type == MMV_TYPE_E4M3;
-    if (type == MMV_TYPE_F16) e4m3 ? launch_attention<f16_t, true>(P, s) : launch_attention<f16_t, false>(P, s);
-    else e4m3 ? launch_attention<bf16_t, true>(P, s) : launch_attention<bf16_t, false>(P, s);
+    if (type == MMV_TYPE_F16) e4m3 ? launch_attention_over<f16_t, true>(P, s) : launch_attention_over<f16_t, false>(P, s);
+    else e4m3 ? launch_attention_over<bf16_t, true>(P, s) : launch_attention_over<bf16_t, false>(P, s);
     if (const mmv_status st = launched()) return st;
     const unsigned blocks = P.n * P.q_heads;
     if (type == MMV_TYPE_F16) join_attention_kernel<f16_t><<<blocks, 256, 0, s>>>(P);
