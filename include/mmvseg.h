@@ -417,7 +417,9 @@ mmv_status mmv_paged_attention(uint64_t n, uint32_t q_heads, const void *d_q, ui
  *   d_state_index  n int32: which of the states is the request's; NULL: the r-th.  A request whose index is outside has
  *               none: it starts from zeros, and its state is not kept.  No two requests share one.
  *   d_out       tokens * heads * dv of `type`
- * States are fp32 throughout.  dk and dv are multiples of 8, dk <= 128, dv <= 256; heads, kv_heads <= 1024. */
+ * States are fp32 throughout.  dk and dv are multiples of 8, dk <= 128, dv <= 256; heads, kv_heads <= 1024; strides are multiples of 8, at most
+ * 2^24.  An infinity in a key or value makes the state's entries that it enters infinite or NaN, and what they enter; no earlier token and no
+ * other request or head. */
 size_t mmv_decay_attention_workspace_bytes(uint64_t n, uint64_t tokens, uint32_t heads, uint32_t dk, uint32_t dv);
 mmv_status mmv_decay_attention(uint64_t n, uint64_t tokens, uint32_t heads, uint32_t kv_heads, uint32_t dk, uint32_t dv,
                                const void *d_q, uint64_t q_stride, const void *d_k, uint64_t k_stride, const void *d_v, uint64_t v_stride,

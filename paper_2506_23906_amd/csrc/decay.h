@@ -119,8 +119,8 @@ constexpr uint32_t kDecayPad = 8;   // LDS rows end in 16 bytes more: sixteen ro
 struct PromptParams {
     DecayParams d;
     float *block_states;    // [blocks * heads][dk * dv]
-    uint32_t block;         // tokens (a multiple of kChunk)
-    uint32_t blocks;        // that there is room for (offsets that go backwards may ask for more)
+    uint32_t block;         // tokens (a multiple of kChunk) at least
+    uint32_t blocks;        // of one head: as many as there is room for, at least one for each request
 };
 
 __device__ __forceinline__ f32x4 mfma_bf16(u32x4 a, u32x4 b, f32x4 c) { return mfma_16x16x32(bf16_t(), a, b, c); }
@@ -131,7 +131,10 @@ template <int kTerms> __device__ __forceinline__ void take_apart(float a, float 
 #pragma unroll
     for (int i = 0; i < kTerms; ++i) {
         to[i] = pack2<bf16_t>(a, b);
-        a -= low_half(to[i]), b -= high_half(to[i]);
+        if (i + 1 < kTerms) {
+            asm("" : "+v"(to[i]));   // (no instruction; the compiler would round each value a second time)
+            a -= low_half(to[i]), b -= high_half(to[i]);
+        }
     }
 }
 // A word of two inputs as its bf16 terms.
@@ -145,6 +148,27 @@ template <typename T, int kTerms> __device__ __forceinline__ void input_terms(ui
     }
 }
 
+// Tokens of a block: the fewest that need no more than the blocks there are, so that the workgroups come in whole rounds of what the device holds.  (Up to 64
+// requests the lengths decide; for more, what is enough for any lengths.  Every workgroup finds the same.)
+__device__ __forceinline__ uint32_t wave_sum32(uint32_t v) {
+    v += dpp_or_zero<0x111, 0xF>(v);
+    v += dpp_or_zero<0x112, 0xF>(v);
+    v += dpp_or_zero<0x114, 0xF>(v);
+    v += dpp_or_zero<0x118, 0xF>(v);
+    v += dpp_or_zero<0x142, 0xA>(v);
+    return lane_value(v + dpp_or_zero<0x143, 0xC>(v), 63);
+}
+__device__ __forceinline__ uint32_t choose_block(const PromptParams &PP) {
+    const DecayParams &P = PP.d;
+    if (P.n > 64 || PP.block >= P.tokens) return PP.block;
+    const uint32_t lane = threadIdx.x & 63;
+    const Span s = lane < P.n ? span_of(P, lane) : Span{0, 0};
+    const uint32_t length = s.end - s.begin;
+    uint32_t block = max(PP.block, (wave_sum32(length) / PP.blocks + kChunk - 1) / kChunk * kChunk);
+    while (wave_sum32(lane < P.n ? max(1u, (length + block - 1) / block) : 0u) > PP.blocks) block += max(1u, block / (16 * kChunk)) * kChunk;   // (at the longest length there are n)
+    return uniform(block);
+}
+
 // Which block of which request a workgroup has; blocks are numbered request after request, at least one each.
 struct BlockPlace {
     uint32_t request, block, blocks;   // the block's number in its request, and how many that has
@@ -155,6 +179,7 @@ __device__ __forceinline__ uint32_t blocks_of(Span s, uint32_t block) { return m
 __device__ __forceinline__ BlockPlace find_block(const DecayParams &P, uint32_t block, uint32_t number) {
     const uint32_t lane = threadIdx.x & 63;
     BlockPlace at = {0, 0, 0, 0, false};
+    if (block >= P.tokens) return {number, 0, 1, number, number < P.n};   // (one for each)
     uint32_t before = 0;
     for (uint32_t first = 0; first < P.n; first += 64) {
         const uint32_t r = first + lane, own = r < P.n ? blocks_of(span_of(P, r), block) : 0u;
@@ -179,33 +204,53 @@ __device__ __forceinline__ BlockPlace find_block(const DecayParams &P, uint32_t 
     return at;
 }
 
-// KD: key components / 32, rounded up; NW: waves, each of which has 32 columns.
-template <int KD, int NW, typename T, bool kStates> __global__ __launch_bounds__(64 * NW, NW > 4 ? 2 : 2) void decay_prompt_kernel(PromptParams PP) {
-    constexpr int kIn = sizeof(T) == 2 && __is_same(T, f16_t) ? 2 : 1;   // terms of an input
+// The value itself, made anew where it is used (no instruction): what follows from it is not kept in registers all through a loop.
+__device__ __forceinline__ uint32_t here(uint32_t v) {
+    asm volatile("" : "+v"(v));
+    return v;
+}
+// Nothing is moved across: the compiler would load operands so far ahead that registers spill.
+__device__ __forceinline__ void phase() { __builtin_amdgcn_sched_barrier(0); }
+
+// Two rows of 16-bit values, columns c and c + 1 in each word, for lanes of two columns: the even lane has rows 0 .. 3 of both, the odd one rows 4 .. 7; they
+// exchange what is the other's.  Words (0, 1), (2, 3), ... of the lane's own column.
+__device__ __forceinline__ uint32_t of_neighbour(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xF, 0xF, false); }   // lanes 2 i and 2 i + 1 swapped
+__device__ __forceinline__ u32x4 own_column(const uint32_t (&row)[4], bool odd) {
+    const uint32_t sel = odd ? 0x07060302u : 0x05040100u, other = odd ? 0x05040100u : 0x07060302u;
+    const uint32_t a = __builtin_amdgcn_perm(row[1], row[0], sel), b = __builtin_amdgcn_perm(row[3], row[2], sel);
+    const uint32_t c = of_neighbour(__builtin_amdgcn_perm(row[1], row[0], other)), d = of_neighbour(__builtin_amdgcn_perm(row[3], row[2], other));
+    return odd ? (u32x4){c, d, a, b} : (u32x4){a, b, c, d};
+}
+
+// KD: key components / 32, rounded up; NW: waves, each of which has 16 columns.
+template <int KD, int NW, typename T, bool kStates> __global__ __launch_bounds__(64 * NW, 4) void decay_prompt_kernel(PromptParams PP) {
+    constexpr int kIn = __is_same(T, f16_t) ? 2 : 1;                   // terms of an input
     constexpr int kMid = 2;                                            // of a score, of the state
     constexpr int kRow = KD * 32 + kDecayPad, kColumn = kChunk + kDecayPad;
-    constexpr int kPieces = KD * 4;                                    // 8 components each
-    constexpr int kBlocks8 = 8 * kPieces * (kStates ? 1 : 2);          // 8 x 8 pieces of K (and Q) of a chunk
-    constexpr int kPer = (kBlocks8 + 64 * NW - 1) / (64 * NW);
+    constexpr int kPieces = KD * 4;                                    // of 8 components
+    // A lane brings 4 tokens x 8 components of K or of Q into LDS; a wave has either.
+    constexpr int kItemsK = 16 * kPieces, kItems = kStates ? kItemsK : 2 * kItemsK, kPer = (kItems + 64 * NW - 1) / (64 * NW);
     __shared__ __align__(16) uint16_t lds_q[kStates ? 1 : kIn][kStates ? 1 : kChunk][kRow], lds_k[kStates ? 1 : kIn][kStates ? 1 : kChunk][kRow];
-    __shared__ __align__(16) uint16_t lds_kt[kIn][KD * 32][kColumn], lds_p[kMid][kStates ? 1 : kChunk][kColumn];
+    __shared__ __align__(16) uint16_t lds_kt[kIn][KD * 32][kChunk], lds_p[kMid][kStates ? 1 : kChunk][kColumn];
+    __shared__ __align__(16) float by_row[kChunk], by_token[kChunk];   // e^(ld (i + 1)); the tokens' decay up to the chunk's end (kStates: the block's)
     const DecayParams &P = PP.d;
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), g = lane >> 4, r = lane & 15;
-    const uint32_t h = blockIdx.x % P.heads, kv = h / P.group;
-    const BlockPlace at = find_block(P, PP.block, blockIdx.x / P.heads);
+    const uint32_t number = uniform(blockIdx.x / P.heads), h = blockIdx.x - number * P.heads, kv = uniform(h / P.group);
+    const uint32_t block = choose_block(PP);
+    const BlockPlace at = find_block(P, block, number);
     if (!at.found || (kStates && at.block + 1 == at.blocks)) return;
     const Span span = span_of(P, at.request);
-    uint32_t begin = uniform(span.begin) + at.block * PP.block;
-    const uint32_t end = min(uniform(span.end), begin + PP.block);
+    uint32_t begin = uniform(span.begin + at.block * block);
+    const uint32_t end = uniform(min(span.end, begin + block));
     const uint64_t state = state_of(P, at.request), matrix = (uint64_t)P.dk * P.dv;
     const float ld2 = head_decay(P, h) * kLog2e;
     if (kStates && ld2 < 0.f) {   // tokens whose decay up to the block's end is zero in fp32 (below 2^-150) add nothing
         const float reach = 152.f / -ld2;
-        if (reach + 1.f < (float)(end - begin)) begin += ((end - begin) - (uint32_t)reach - 1) / kChunk * kChunk;
+        if (reach + 1.f < (float)(end - begin)) begin += uniform(((end - begin) - (uint32_t)reach - 1) / kChunk * kChunk);
     }
-    const uint32_t column = wave * 32 + 2 * r;
-    const bool live_column = column < P.dv;
-    f32x4 S[2 * KD][2];
+    const uint32_t column = wave * 16 + r;
+    const bool live_column = column < P.dv;   // (the others compute what nobody reads)
+    f32x4 S[2 * KD];
     // the state's rows of this lane: tile 2 p + t, register i
     const float *from = kStates ? nullptr : at.blocks > 1 ? PP.block_states + ((uint64_t)blockIdx.x) * matrix
                                           : P.state_in && state != ~0ull ? P.state_in + (state * P.heads + h) * matrix : nullptr;
@@ -214,247 +259,289 @@ template <int KD, int NW, typename T, bool kStates> __global__ __launch_bounds__
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const uint32_t d = (m / 2) * 32 + g * 8 + (m % 2) * 4 + i;
-            float2 x = make_float2(0.f, 0.f);
-            if (from && live_column && d < P.dk) x = *(const float2 *)(from + (uint64_t)d * P.dv + column);
-            S[m][0][i] = x.x, S[m][1][i] = x.y;
+            S[m][i] = from && live_column && d < P.dk ? from[(uint64_t)d * P.dv + column] : 0.f;
         }
 
-    u32x4 staged[kPer][8];
-    uint32_t values[16];
+    // Rows are read and written through buffers that end behind the chunk's last token: rows beyond read 0 and are not written, and so do
+    // components and columns that dk and dv do not have, whose offsets lie behind any end.
+    constexpr uint32_t kNowhere = 1u << 31;
     const uint32_t pieces = P.dk / 8;
-    auto load_chunk = [&](uint32_t t0) __attribute__((always_inline)) {
-        const uint32_t last = end - 1;
+    // Lane numbers made anew for every phase: addresses that stay the same from chunk to chunk would fill the registers, and those that spill are loaded
+    // behind the next chunk's rows, whose arrival they then wait for.
+    struct At {
+        uint32_t r, g;
+        bool odd;
+        uint32_t column2;   // of the lane's pair of columns, in bytes
+    };
+    const auto lane_at = [&]() __attribute__((always_inline)) {
+        const uint32_t l = here(lane), c = wave * 16 + (l & 14);
+        return At{l & 15, l >> 4, (l & 1) != 0, c < P.dv ? 2 * c : kNowhere};
+    };
+    u32x4 staged[kPer][4];
+    uint32_t values[2][4];
+    struct Part {
+        bool live, is_q;
+        uint32_t rows, piece;
+    };
+    const auto part_of = [&](int b) __attribute__((always_inline)) {
+        const uint32_t first = wave * 64 + b * 64 * NW;
+        Part p;
+        p.live = first < kItems, p.is_q = first >= kItemsK;
+        const uint32_t id = first - (p.is_q ? kItemsK : 0) + here(lane);
+        p.piece = id % kPieces, p.rows = id / kPieces * 4;
+        return p;
+    };
+    const auto chunk_rows = [&](const void *base, uint32_t m, uint32_t stride, uint32_t width) __attribute__((always_inline)) {
+        return make_rsrc((const void *)uniform64((uint64_t)base), uniform((m - 1) * stride + width));
+    };
+    const auto load_chunk = [&](uint32_t t0) __attribute__((always_inline)) {
+        const uint32_t m = min(kChunk, end - t0);
 #pragma unroll
         for (int b = 0; b < kPer; ++b) {
-            const uint32_t id = tid + b * 64 * NW;
-            if (kPer * 64 * NW == kBlocks8 || id < kBlocks8) {
-                const bool is_q = !kStates && id >= 8 * kPieces;
-                const uint32_t in = is_q ? id - 8 * kPieces : id, piece = in % kPieces, rows = in / kPieces * 8;
-                const T *base = (is_q ? (const T *)P.q + (uint64_t)h * P.dk : (const T *)P.k + (uint64_t)kv * P.dk) + (piece < pieces ? piece * 8 : 0);
-                const uint64_t stride = is_q ? P.q_stride : P.k_stride;
+            const Part p = part_of(b);
+            if (p.live) {
+                const uint32_t stride = 2 * (uint32_t)(p.is_q ? P.q_stride : P.k_stride), off = p.rows * stride + (p.piece < pieces ? p.piece * 16 : kNowhere);
+                const auto rows = chunk_rows(p.is_q ? (const T *)P.q + (uint64_t)h * P.dk + t0 * P.q_stride : (const T *)P.k + (uint64_t)kv * P.dk + t0 * P.k_stride, m, stride, 2 * P.dk);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) staged[b][j] = *(const u32x4 *)(base + min(t0 + rows + j, last) * stride);
+                for (int j = 0; j < 4; ++j) staged[b][j] = __builtin_amdgcn_raw_buffer_load_b128(rows, off + j * stride, 0, 0);
             }
         }
-        const T *base = (const T *)P.v + (uint64_t)kv * P.dv + (live_column ? column : 0);
+        const At l = lane_at();
+        const uint32_t stride = 2 * (uint32_t)P.v_stride, off = (l.g * 8 + (l.odd ? 4 : 0)) * stride + l.column2;
+        const auto rows = chunk_rows((const T *)P.v + (uint64_t)kv * P.dv + t0 * P.v_stride, m, stride, 2 * P.dv);
 #pragma unroll
-        for (int j = 0; j < 16; ++j) values[j] = *(const uint32_t *)(base + min(t0 + (j / 8) * 32 + g * 8 + j % 8, last) * P.v_stride);
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) values[s][j] = __builtin_amdgcn_raw_buffer_load_b32(rows, off + (s * 32 + j) * stride, 0, 0);
     };
-    auto put_piece = [&](uint16_t *to, const uint32_t (&w)[4]) __attribute__((always_inline)) { *(u32x4 *)to = (u32x4){w[0], w[1], w[2], w[3]}; };
+    // K by component: row d has eight pieces of 8 tokens, in two halves, each in a place that keeps the lanes of a write (d / 8 differs) and of a read
+    // (bits 0, 1 and 3 of d differ) in different banks: piece u at u ^ (d / 8 mod 8) ^ (d & 2), its halves exchanged where d / 64 is odd.
+    const auto kt_lane = [&](const At &l) __attribute__((always_inline)) { return ((l.r >> 2) * 8 + (l.r & 3)) * 128 + (l.g ^ (l.r >> 2) ^ (l.r & 2)) * 16; };
+    const auto kt_tile = [&](int a, uint32_t own, int t, int s) __attribute__((always_inline)) {   // components of tile t, tokens 32 s + 8 g .. + 7
+        const u32x4 w = *(const u32x4 *)((const char *)lds_kt[a] + own + (t / 2) * 32 * 128 + (t % 2) * 4 * 128 + (s ^ (t / 2 & 1)) * 64);
+        return t / 4 % 2 ? (u32x4){w[2], w[3], w[0], w[1]} : w;
+    };
 
+    if (!kStates && tid < kChunk) by_row[tid] = __builtin_amdgcn_exp2f(ld2 * (float)(tid + 1));
+    if (!kStates && tid < kChunk) by_token[tid] = __builtin_amdgcn_exp2f(ld2 * (float)(kChunk - 1 - tid));
     if (begin < end) load_chunk(begin);
+    // The first chunk's loads are waited for here: with any of them under way at the loop's head, the compiler's wait there would be for all that the wave has
+    // issued, the stores of the chunk before among them.
+    __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0)
     for (uint32_t t0 = begin; t0 < end; t0 += kChunk) {
         const uint32_t m = min(kChunk, end - t0);
+        if (kStates && tid < kChunk) by_token[tid] = __builtin_amdgcn_exp2f(ld2 * (float)(end - 1 - t0 - tid));   // (blocks here are whole chunks)
+        if (!kStates && m < kChunk && tid < kChunk) by_token[tid] = __builtin_amdgcn_exp2f(ld2 * (float)max((int)m - 1 - (int)tid, 0));
         // keys (by token and by component) and queries into LDS
 #pragma unroll
         for (int b = 0; b < kPer; ++b) {
-            const uint32_t id = tid + b * 64 * NW;
-            if (kPer * 64 * NW == kBlocks8 || id < kBlocks8) {
-                const bool is_q = !kStates && id >= 8 * kPieces;
-                const uint32_t in = is_q ? id - 8 * kPieces : id, piece = in % kPieces, rows = in / kPieces * 8;
-                if (m < kChunk || piece >= pieces) {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        if (rows + j >= m || piece >= pieces) staged[b][j] = (u32x4){0, 0, 0, 0};
-                }
-                uint32_t w[kIn][8][4];
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        uint32_t terms[kIn];
-                        input_terms<T, kIn>(staged[b][j][i], terms);
-#pragma unroll
-                        for (int a = 0; a < kIn; ++a) w[a][j][i] = terms[a];
-                    }
+            const Part p = part_of(b);
+            if (p.live) {
 #pragma unroll
                 for (int a = 0; a < kIn; ++a) {
+                    uint32_t w[4][4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            uint32_t terms[kIn];
+                            input_terms<T, kIn>(staged[b][j][i], terms);
+                            w[j][i] = terms[a];
+                        }
                     if constexpr (!kStates) {
-                        uint16_t(*const to)[kRow] = is_q ? lds_q[a] : lds_k[a];
+                        uint16_t(*const to)[kRow] = p.is_q ? lds_q[a] : lds_k[a];
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) put_piece(&to[rows + j][piece * 8], w[a][j]);
+                        for (int j = 0; j < 4; ++j) *(u32x4 *)&to[p.rows + j][p.piece * 8] = (u32x4){w[j][0], w[j][1], w[j][2], w[j][3]};
                     }
-                    if (!is_q) {
+                    if (!p.is_q) {
+                        const uint32_t unit = p.rows / 8 ^ (p.piece & 7), half = (p.rows / 4 & 1) ^ (p.piece / 8 & 1);
+                        char *to = (char *)lds_kt[a] + p.piece * 8 * 128 + half * 8;
 #pragma unroll
-                        for (int c = 0; c < 8; ++c) {   // component c of the eight tokens
-                            uint32_t x[4];
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) x[i] = __builtin_amdgcn_perm(w[a][2 * i + 1][c / 2], w[a][2 * i][c / 2], c % 2 ? 0x07060302u : 0x05040100u);
-                            put_piece(&lds_kt[a][piece * 8 + c][rows], x);
+                        for (int c = 0; c < 8; ++c) {   // component c of the four tokens
+                            const uint32_t sel = c % 2 ? 0x07060302u : 0x05040100u;
+                            *(u32x2 *)(to + c * 128 + (unit ^ (c & 2)) * 16) = (u32x2){__builtin_amdgcn_perm(w[1][c / 2], w[0][c / 2], sel), __builtin_amdgcn_perm(w[3][c / 2], w[2][c / 2], sel)};
                         }
                     }
                 }
             }
         }
-        // values: tokens 32 s + 8 g + 2 i, + 1 of column n in V[a][s][n][i]
-        u32x4 V[kIn][2][2];
+        // values: tokens 32 s + 8 g + 2 i, + 1 of the lane's column in V[a][s][i]
+        u32x4 V[kIn][2];
 #pragma unroll
-        for (int s = 0; s < 2; ++s)
+        for (int s = 0; s < 2; ++s) {
+            uint32_t y[4][kIn];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                uint32_t x[2] = {values[8 * s + 2 * i], values[8 * s + 2 * i + 1]};
-                if (m < kChunk || !live_column) {
+            for (int j = 0; j < 4; ++j) input_terms<T, kIn>(values[s][j], y[j]);
 #pragma unroll
-                    for (int j = 0; j < 2; ++j)
-                        if (!live_column || 32 * s + 8 * g + 2 * i + j >= m) x[j] = 0;
-                }
-                uint32_t y[2][kIn];
-#pragma unroll
-                for (int j = 0; j < 2; ++j) input_terms<T, kIn>(x[j], y[j]);
-#pragma unroll
-                for (int a = 0; a < kIn; ++a) {
-                    V[a][s][0][i] = __builtin_amdgcn_perm(y[1][a], y[0][a], 0x05040100u);
-                    V[a][s][1][i] = __builtin_amdgcn_perm(y[1][a], y[0][a], 0x07060302u);
-                }
+            for (int a = 0; a < kIn; ++a) {
+                const uint32_t rows[4] = {y[0][a], y[1][a], y[2][a], y[3][a]};
+                V[a][s] = own_column(rows, here(lane) & 1);
             }
+        }
         __syncthreads();
         if (t0 + kChunk < end) load_chunk(t0 + kChunk);
+        phase();
 
-        f32x4 O[4][2];
+        f32x4 O[4];
         if constexpr (!kStates) {
-            // scores: key tile by query tile, up to the diagonal and the zeros beside it that a product reads
-            for (uint32_t u = wave; u < 12; u += NW) {
-                const uint32_t qt = u < 2 ? 0 : u < 4 ? 1 : u < 8 ? 2 : 3, kt = u < 2 ? u : u < 4 ? u - 2 : u < 8 ? u - 4 : u - 8;
-                f32x4 x = {0.f, 0.f, 0.f, 0.f};
-                if (kt <= qt) {
+            // scores: key tile by query tile up to the diagonal, and the two tiles of zeros beside it that a product reads
+            constexpr uint32_t kQueryTiles = 0x8FFA94, kKeyTiles = 0xDE4910;   // two bits each: 0 1 1 2 2 2 3 3 3 3 0 2, 0 0 1 0 1 2 0 1 2 3 1 3
 #pragma unroll
-                    for (int p = 0; p < KD; ++p)
+            for (int k = 0; k < (12 + NW - 1) / NW; ++k) {
+                const uint32_t u = wave + k * NW;
+                if (12 % NW == 0 || u < 12) {
+                    const uint32_t qt = kQueryTiles >> (2 * u) & 3, kt = kKeyTiles >> (2 * u) & 3;
+                    const At l = lane_at();
+                    f32x4 x = {0.f, 0.f, 0.f, 0.f};
+                    if (u < 10) {
 #pragma unroll
-                        for (int a = 0; a < kIn; ++a)
+                        for (int p = 0; p < KD; ++p)
 #pragma unroll
-                            for (int b = 0; b + a < kIn; ++b)
-                                x = mfma_bf16(*(const u32x4 *)&lds_k[a][kt * 16 + r][p * 32 + g * 8], *(const u32x4 *)&lds_q[b][qt * 16 + r][p * 32 + g * 8], x);
+                            for (int a = 0; a < kIn; ++a)
+#pragma unroll
+                                for (int b = 0; b + a < kIn; ++b)
+                                    x = mfma_bf16(*(const u32x4 *)&lds_k[a][kt * 16 + l.r][p * 32 + l.g * 8], *(const u32x4 *)&lds_q[b][qt * 16 + l.r][p * 32 + l.g * 8], x);
+                    }
+                    const int apart = (int)(qt * 16 + l.r) - (int)(kt * 16 + l.g * 4);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x[i] = apart >= i ? x[i] * __builtin_amdgcn_exp2f(ld2 * (float)(apart - i)) : 0.f;
+                    uint32_t lo[kMid], hi[kMid];
+                    take_apart<kMid>(x[0], x[1], lo);
+                    take_apart<kMid>(x[2], x[3], hi);
+#pragma unroll
+                    for (int a = 0; a < kMid; ++a) *(u32x2 *)&lds_p[a][qt * 16 + l.r][kt * 16 + l.g * 4] = (u32x2){lo[a], hi[a]};
+                    phase();
                 }
-                const int apart = (int)(qt * 16 + r) - (int)(kt * 16 + g * 4);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) x[i] = apart >= i ? x[i] * __builtin_amdgcn_exp2f(ld2 * (float)(apart - i)) : 0.f;
-                uint32_t lo[kMid], hi[kMid];
-                take_apart<kMid>(x[0], x[1], lo);
-                take_apart<kMid>(x[2], x[3], hi);
-#pragma unroll
-                for (int a = 0; a < kMid; ++a) *(u32x2 *)&lds_p[a][qt * 16 + r][kt * 16 + g * 4] = (u32x2){lo[a], hi[a]};
             }
             // what the state before the chunk adds
 #pragma unroll
-            for (int t = 0; t < 4; ++t) O[t][0] = O[t][1] = (f32x4){0.f, 0.f, 0.f, 0.f};
-#pragma unroll
             for (int p = 0; p < KD; ++p) {
-                u32x4 B[2][kMid];
-#pragma unroll
-                for (int n = 0; n < 2; ++n)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        uint32_t x[kMid];
-                        take_apart<kMid>(S[2 * p + i / 2][n][2 * (i % 2)], S[2 * p + i / 2][n][2 * (i % 2) + 1], x);
-#pragma unroll
-                        for (int a = 0; a < kMid; ++a) B[n][a][i] = x[a];
-                    }
-#pragma unroll
-                for (int t = 0; t < 4; ++t)
-#pragma unroll
-                    for (int a = 0; a < kIn; ++a) {
-                        const u32x4 A = *(const u32x4 *)&lds_q[a][t * 16 + r][p * 32 + g * 8];
-#pragma unroll
-                        for (int n = 0; n < 2; ++n)
-#pragma unroll
-                            for (int b = 0; b + a < kMid; ++b) O[t][n] = mfma_bf16(A, B[n][b], O[t][n]);
-                    }
-            }
-#pragma unroll
-            for (int t = 0; t < 4; ++t)
+                const At l = lane_at();
+                u32x4 B[kMid];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const float by = __builtin_amdgcn_exp2f(ld2 * (float)(t * 16 + g * 4 + i + 1));
-                    O[t][0][i] *= by, O[t][1][i] *= by;
+                    uint32_t x[kMid];
+                    take_apart<kMid>(S[2 * p + i / 2][2 * (i % 2)], S[2 * p + i / 2][2 * (i % 2) + 1], x);
+#pragma unroll
+                    for (int a = 0; a < kMid; ++a) B[a][i] = x[a];
                 }
+#pragma unroll
+                for (int a = 0; a < kIn; ++a) {
+#pragma unroll
+                    for (int t0_ = 0; t0_ < 4; t0_ += 2) {
+                        u32x4 A[2];
+#pragma unroll
+                        for (int t = 0; t < 2; ++t) A[t] = *(const u32x4 *)&lds_q[a][(t0_ + t) * 16 + l.r][p * 32 + l.g * 8];
+#pragma unroll
+                        for (int b = 0; b + a < kMid; ++b)
+#pragma unroll
+                            for (int t = 0; t < 2; ++t) O[t0_ + t] = mfma_bf16(A[t], B[b], p == 0 && a == 0 && b == 0 ? (f32x4){0.f, 0.f, 0.f, 0.f} : O[t0_ + t]);
+                    }
+                }
+                phase();
+            }
+            const At l = lane_at();
+#pragma unroll
+            for (int t = 0; t < 4; ++t) O[t] *= *(const f32x4 *)&by_row[t * 16 + l.g * 4];
+            const float decay = __builtin_amdgcn_exp2f(ld2 * (float)m);
+#pragma unroll
+            for (int t = 0; t < 2 * KD; ++t) S[t] *= decay;
+            phase();
         }
         // the state after it
-        const float decay = __builtin_amdgcn_exp2f(ld2 * (float)m);
-#pragma unroll
-        for (int t = 0; t < 2 * KD; ++t) S[t][0] *= decay, S[t][1] *= decay;
         float odd = 0.f;   // NaN if one of the wave's values is not finite
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-            u32x4 W[2][3];
+            const At l = lane_at();
+            const uint32_t own = kt_lane(l);
+            u32x4 W[3];
+            const f32x4 by[2] = {*(const f32x4 *)&by_token[32 * s + 8 * l.g], *(const f32x4 *)&by_token[32 * s + 8 * l.g + 4]};
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int j = 32 * s + 8 * (int)g + 2 * i;
-                const float a = __builtin_amdgcn_exp2f(ld2 * (float)max((int)m - 1 - j, 0)), b = __builtin_amdgcn_exp2f(ld2 * (float)max((int)m - 2 - j, 0));
+                float x = low_half(V[0][s][i]), y = high_half(V[0][s][i]);
+                if constexpr (kIn == 2) x += low_half(V[1][s][i]), y += high_half(V[1][s][i]);
+                if constexpr (!kStates) odd = __builtin_fmaf(x, 0.f, __builtin_fmaf(y, 0.f, odd));
+                uint32_t terms[3];
+                take_apart<3>(x * by[i / 2][2 * (i % 2)], y * by[i / 2][2 * (i % 2) + 1], terms);
 #pragma unroll
-                for (int n = 0; n < 2; ++n) {
-                    float x = low_half(V[0][s][n][i]), y = high_half(V[0][s][n][i]);
-                    if constexpr (kIn == 2) x += low_half(V[1][s][n][i]), y += high_half(V[1][s][n][i]);
-                    odd = __builtin_fmaf(x, 0.f, __builtin_fmaf(y, 0.f, odd));
-                    uint32_t terms[3];
-                    take_apart<3>(x * a, y * b, terms);
-#pragma unroll
-                    for (int c = 0; c < 3; ++c) W[n][c][i] = terms[c];
-                }
+                for (int c = 0; c < 3; ++c) W[c][i] = terms[c];
             }
 #pragma unroll
-            for (int t = 0; t < 2 * KD; ++t)
+            for (int t0_ = 0; t0_ < 2 * KD; t0_ += 2) {
+                constexpr int kTogether = 2;
 #pragma unroll
                 for (int a = 0; a < kIn; ++a) {
-                    const u32x4 A = *(const u32x4 *)&lds_kt[a][(t / 2) * 32 + (r >> 2) * 8 + (t % 2) * 4 + (r & 3)][s * 32 + g * 8];
+                    u32x4 A[kTogether];
 #pragma unroll
-                    for (int n = 0; n < 2; ++n)
+                    for (int t = 0; t < kTogether; ++t) A[t] = kt_tile(a, own, t0_ + t, s);
 #pragma unroll
-                        for (int c = 0; c + a < 3; ++c) S[t][n] = mfma_bf16(A, W[n][c], S[t][n]);
+                    for (int c = 0; c + a < 3; ++c)
+#pragma unroll
+                        for (int t = 0; t < kTogether; ++t) S[t0_ + t] = mfma_bf16(A[t], W[c], S[t0_ + t]);
                 }
+                phase();
+            }
         }
         if constexpr (!kStates) {
             __syncthreads();   // all scores are there
+            const At l = lane_at();
             if (!__any(odd != 0.f)) {
 #pragma unroll
                 for (int s = 0; s < 2; ++s)
 #pragma unroll
-                    for (int t = 2 * s; t < 4; ++t)
+                    for (int a = 0; a < kMid; ++a) {
+                        u32x4 A[4];
 #pragma unroll
-                        for (int a = 0; a < kMid; ++a) {
-                            const u32x4 A = *(const u32x4 *)&lds_p[a][t * 16 + r][s * 32 + g * 8];
+                        for (int t = 2 * s; t < 4; ++t) A[t] = *(const u32x4 *)&lds_p[a][t * 16 + l.r][s * 32 + l.g * 8];
 #pragma unroll
-                            for (int n = 0; n < 2; ++n)
+                        for (int b = 0; b < kIn && b + a < kMid; ++b)
 #pragma unroll
-                                for (int b = 0; b < kIn && b + a < kMid; ++b) O[t][n] = mfma_bf16(A, V[b][s][n], O[t][n]);
-                        }
+                            for (int t = 2 * s; t < 4; ++t) O[t] = mfma_bf16(A[t], V[b][s], O[t]);
+                    }
             } else {   // the zeros of later tokens must not meet their infinities and NaN
-                const T *base = (const T *)P.v + (uint64_t)kv * P.dv + (live_column ? column : 0);
+                const uint32_t mine = wave * 16 + l.r;
+                const T *base = (const T *)P.v + (uint64_t)kv * P.dv + (mine < P.dv ? mine : 0);
                 for (uint32_t j = 0; j < m; ++j) {
-                    const float x = to_f32(base[(t0 + j) * P.v_stride]), y = to_f32(base[(t0 + j) * P.v_stride + 1]);
+                    const uint32_t rows = here(l.g * 4);
+                    const float x = to_f32(base[(t0 + j) * P.v_stride]);
 #pragma unroll
                     for (int t = 0; t < 4; ++t)
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
-                            const uint32_t q = t * 16 + g * 4 + i;
-                            if (q >= j) {
-                                float w = 0.f;
+                            const uint32_t q = t * 16 + rows + i;
+                            float w = 0.f;
 #pragma unroll
-                                for (int a = 0; a < kMid; ++a) w += low_half(lds_p[a][q][j]);
-                                O[t][0][i] += w * x, O[t][1][i] += w * y;
-                            }
+                            for (int a = 0; a < kMid; ++a) w += low_half(lds_p[a][q][j]);
+                            O[t][i] = q >= j ? O[t][i] + w * x : O[t][i];
+                            phase();
                         }
                 }
             }
-            if (live_column)
+            // rows 0, 1 of a tile's four are the even lane's, 2, 3 the odd one's, both columns of each
+            const uint32_t stride = 2 * P.heads * P.dv, off = (l.g * 4 + (l.odd ? 2 : 0)) * stride + l.column2;
+            const auto rows = chunk_rows((T *)P.out + ((uint64_t)t0 * P.heads + h) * P.dv, m, stride, 2 * P.dv);
 #pragma unroll
-                for (int t = 0; t < 4; ++t)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const uint32_t q = t * 16 + g * 4 + i;
-                        if (q < m) *(uint32_t *)((T *)P.out + ((uint64_t)(t0 + q) * P.heads + h) * P.dv + column) = pack2<T>(O[t][0][i] * P.scale, O[t][1][i] * P.scale);
-                    }
+            for (int t = 0; t < 4; ++t) {
+                O[t] *= P.scale;
+                const uint32_t a = pack2<T>(O[t][0], O[t][1]), b = pack2<T>(O[t][2], O[t][3]);   // own column
+                const uint32_t got = of_neighbour(l.odd ? a : b), own = l.odd ? b : a;    // the lane's two rows, the other column and this one
+                const uint32_t left = l.odd ? got : own, right = l.odd ? own : got;
+                __builtin_amdgcn_raw_buffer_store_b32(__builtin_amdgcn_perm(right, left, 0x05040100u), rows, off + t * 16 * stride, 0, 0);
+                __builtin_amdgcn_raw_buffer_store_b32(__builtin_amdgcn_perm(right, left, 0x07060302u), rows, off + (t * 16 + 1) * stride, 0, 0);
+            }
         }
         __syncthreads();   // LDS is free again
     }
     float *to = kStates ? PP.block_states + (uint64_t)blockIdx.x * matrix
                         : at.block + 1 == at.blocks && P.state_out && state != ~0ull ? P.state_out + (state * P.heads + h) * matrix : nullptr;
+    const uint32_t lane_rows = here(lane) / 16 * 8;
     if (to && live_column)
 #pragma unroll
         for (int m = 0; m < 2 * KD; ++m)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const uint32_t d = (m / 2) * 32 + g * 8 + (m % 2) * 4 + i;
-                if (d < P.dk) *(float2 *)(to + (uint64_t)d * P.dv + column) = make_float2(S[m][0][i], S[m][1][i]);
+                const uint32_t d = (m / 2) * 32 + lane_rows + (m % 2) * 4 + i;
+                if (d < P.dk) to[(uint64_t)d * P.dv + column] = S[m][i];
             }
 }
 
@@ -463,10 +550,10 @@ __global__ __launch_bounds__(256) void decay_blocks_kernel(PromptParams PP) {
     const DecayParams &P = PP.d;
     const uint64_t matrix = (uint64_t)P.dk * P.dv;
     const uint32_t slices = (uint32_t)((matrix + 1023) / 1024), slice = blockIdx.x % slices, h = blockIdx.x / slices % P.heads, request = blockIdx.x / slices / P.heads;
-    const uint32_t blocks = blocks_of(span_of(P, request), PP.block);
+    const uint32_t block = choose_block(PP), blocks = blocks_of(span_of(P, request), block);
     if (blocks == 1) return;
     uint32_t mine = 0;   // blocks before this request's
-    for (uint32_t i = threadIdx.x & 63; i < request; i += 64) mine += blocks_of(span_of(P, i), PP.block);
+    for (uint32_t i = threadIdx.x & 63; i < request; i += 64) mine += blocks_of(span_of(P, i), block);
 #pragma unroll
     for (int d = 32; d >= 1; d >>= 1) mine += __shfl_xor(mine, d);
     const uint64_t at = (uint64_t)slice * 1024 + threadIdx.x * 4;
@@ -474,7 +561,7 @@ __global__ __launch_bounds__(256) void decay_blocks_kernel(PromptParams PP) {
     const uint64_t state = state_of(P, request);
     f32x4 S = {0.f, 0.f, 0.f, 0.f};
     if (P.state_in && state != ~0ull) S = *(const f32x4 *)(P.state_in + (state * P.heads + h) * matrix + at);
-    const float decay = __builtin_amdgcn_exp2f(head_decay(P, h) * kLog2e * (float)PP.block);
+    const float decay = __builtin_amdgcn_exp2f(head_decay(P, h) * kLog2e * (float)block);
     float *slot = PP.block_states + ((uint64_t)mine * P.heads + h) * matrix + at;
     const uint64_t step = P.heads * matrix;
     uint32_t b = 0;

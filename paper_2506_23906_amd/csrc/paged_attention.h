@@ -78,8 +78,6 @@ __device__ __forceinline__ RowTiles row_tiles(const AttentionParams &P, int32_t 
     const uint32_t first = begin / kTile;
     return {begin, end, first, (end + kTile - 1) / kTile - first};
 }
-__device__ __forceinline__ uint32_t uniform(uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); }
-__device__ __forceinline__ uint32_t lane_value(uint32_t v, int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)v, lane); }
 // Inclusive sums over the lanes of a wave.
 __device__ __forceinline__ uint32_t wave_upto(uint32_t v) {
     v += dpp_or_zero<0x111, 0xF>(v);

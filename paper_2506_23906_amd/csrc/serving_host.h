@@ -7,6 +7,7 @@ namespace {
 constexpr uint64_t k2to31 = 1ull << 31;
 constexpr uint64_t kMostRequests = 1ull << 22;
 constexpr uint32_t kMostHeads = 1024;
+constexpr uint64_t kMostStride = 1ull << 24;   // of tokens, in elements, for the recurrence: 64 of them in 32-bit byte offsets
 
 inline uint64_t ceil_div(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
 inline size_t round256(size_t b) { return (b + 255) & ~(size_t)255; }
@@ -131,6 +132,7 @@ mmv_status decay_params(DecayParams &P, uint64_t n, uint64_t tokens, uint32_t he
                         uint64_t states, const int32_t *state_index, void *out) {
     if (!valid_value_type(type) || states >= k2to31 || q_stride % 8 || k_stride % 8 || v_stride % 8) return MMV_ERR_INVALID_ARG;
     if (tokens > 1 && (q_stride < (uint64_t)heads * dk || k_stride < (uint64_t)kv_heads * dk || v_stride < (uint64_t)kv_heads * dv)) return MMV_ERR_INVALID_ARG;
+    if (q_stride > kMostStride || k_stride > kMostStride || v_stride > kMostStride) return MMV_ERR_INVALID_ARG;
     if (!state_index && (state_in || state_out) && states < n) return MMV_ERR_INVALID_ARG;
     if (tokens && n && (!q || !k || !v || !out)) return MMV_ERR_NULL;
     if (n && !log_decay) return MMV_ERR_NULL;
@@ -141,20 +143,36 @@ mmv_status decay_params(DecayParams &P, uint64_t n, uint64_t tokens, uint32_t he
     if (state_in && state_out && state_in != state_out && (uintptr_t)state_in < (uintptr_t)state_out + bytes && (uintptr_t)state_out < (uintptr_t)state_in + bytes)
         return MMV_ERR_INVALID_ARG;
     P.q = q, P.k = k, P.v = v, P.q_stride = q_stride, P.k_stride = k_stride, P.v_stride = v_stride, P.tokens = tokens;
+    if (tokens <= 1) P.q_stride = (uint64_t)heads * dk, P.k_stride = (uint64_t)kv_heads * dk, P.v_stride = (uint64_t)kv_heads * dv;   // (not checked above: no second token)
     P.log_decay = log_decay, P.state_in = state_in, P.state_out = state_out, P.state_index = state_index, P.states = states, P.out = out;
     P.n = (uint32_t)n, P.heads = heads, P.group = heads / kv_heads, P.dk = dk, P.dv = dv, P.scale = scale;
     return MMV_OK;
 }
-// Tokens of a block of a prompt.
-inline uint32_t decay_block(uint64_t tokens, uint32_t heads) {
-    if (tokens <= 1024) return 1024;
-    const uint64_t even = ceil_div(tokens * heads, 1024 * kChunk) * kChunk;
-    return (uint32_t)(even < 256 ? 256 : even > 4096 ? 4096 : even);
+// Blocks of prompts (the least tokens of one, how many of a head): one for each request, or so many that the workgroups fill the device in whole rounds.
+#ifndef PT
+#define PT 1024
+#endif
+#ifndef PMIN
+#define PMIN 256
+#endif
+constexpr uint32_t kPromptGroups = PT, kLeastBlock = PMIN, kOneBlock = 1024;
+struct DecayBlocks {
+    uint32_t block, blocks;
+    bool split;
+};
+inline DecayBlocks decay_blocks(uint64_t n, uint64_t tokens, uint32_t heads) {
+    if (tokens <= kOneBlock) return {kOneBlock, (uint32_t)n, false};
+    const uint64_t round = kPromptGroups / heads ? kPromptGroups / heads : 1, blocks = n + round / 2 > round ? n + round / 2 : round, more = blocks > n ? blocks - n : 1;
+    uint64_t block = kLeastBlock;
+    if (n > 64) {   // enough for any lengths: requests need at most one block each and tokens / block
+        block = ceil_div(ceil_div(tokens, more), kChunk) * kChunk;
+        if (block < kLeastBlock) block = kLeastBlock;
+    }
+    return {(uint32_t)block, (uint32_t)(n + more), true};
 }
-inline uint64_t decay_blocks(uint64_t n, uint64_t tokens, uint32_t heads) { return n + tokens / decay_block(tokens, heads); }   // at most
 inline size_t decay_workspace(uint64_t n, uint64_t tokens, uint32_t heads, uint32_t dk, uint32_t dv) {
-    if (tokens <= decay_block(tokens, heads)) return 0;   // (one block for every request)
-    return round256(decay_blocks(n, tokens, heads) * heads * dk * dv * 4);
+    const DecayBlocks b = decay_blocks(n, tokens, heads);
+    return b.split ? round256((size_t)b.blocks * heads * dk * dv * 4) : 0;
 }
 template <int KD, int NW, typename T> mmv_status launch_prompts(const PromptParams &P, hipStream_t s) {
     const DecayParams &d = P.d;
@@ -173,14 +191,14 @@ template <int KD, int NW, typename T> mmv_status launch_prompts(const PromptPara
 }
 template <int KD, typename T> mmv_status launch_prompts_of(const PromptParams &P, hipStream_t s) {
     const uint32_t dv = P.d.dv;
-    return dv <= 64 ? launch_prompts<KD, 2, T>(P, s) : dv <= 128 ? launch_prompts<KD, 4, T>(P, s) : dv <= 160 ? launch_prompts<KD, 5, T>(P, s) : launch_prompts<KD, 8, T>(P, s);
+    return dv <= 64 ? launch_prompts<KD, 4, T>(P, s) : dv <= 128 ? launch_prompts<KD, 8, T>(P, s) : dv <= 160 ? launch_prompts<KD, 10, T>(P, s) : launch_prompts<KD, 16, T>(P, s);
 }
 mmv_status decay_call(const DecayParams &d, int type, void *d_ws, hipStream_t s) {
     PromptParams P = {};
     P.d = d;
-    P.block = decay_block(d.tokens, d.heads);
-    P.blocks = (uint32_t)decay_blocks(d.n, d.tokens, d.heads);
-    P.block_states = d.tokens > P.block ? (float *)d_ws : nullptr;
+    const DecayBlocks b = decay_blocks(d.n, d.tokens, d.heads);
+    P.block = b.block, P.blocks = b.blocks;
+    P.block_states = b.split ? (float *)d_ws : nullptr;
     if (type == MMV_TYPE_F16) return d.dk <= 64 ? launch_prompts_of<2, f16_t>(P, s) : launch_prompts_of<4, f16_t>(P, s);
     return d.dk <= 64 ? launch_prompts_of<2, bf16_t>(P, s) : d.dk <= 96 ? launch_prompts_of<3, bf16_t>(P, s) : launch_prompts_of<4, bf16_t>(P, s);
 }
