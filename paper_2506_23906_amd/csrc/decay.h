@@ -126,16 +126,14 @@ struct PromptParams {
 __device__ __forceinline__ f32x4 mfma_bf16(u32x4 a, u32x4 b, f32x4 c) { return mfma_16x16x32(bf16_t(), a, b, c); }
 __device__ __forceinline__ float low_half(uint32_t w) { return __builtin_bit_cast(float, w << 16); }
 __device__ __forceinline__ float high_half(uint32_t w) { return __builtin_bit_cast(float, w & 0xFFFF0000u); }
-// Two values into kTerms words of bf16 pairs.
+// Two values into kTerms words of bf16 pairs: the upper halves of what is left each time, the last of it rounded.
 template <int kTerms> __device__ __forceinline__ void take_apart(float a, float b, uint32_t (&to)[kTerms]) {
 #pragma unroll
-    for (int i = 0; i < kTerms; ++i) {
-        to[i] = pack2<bf16_t>(a, b);
-        if (i + 1 < kTerms) {
-            asm("" : "+v"(to[i]));   // (no instruction; the compiler would round each value a second time)
-            a -= low_half(to[i]), b -= high_half(to[i]);
-        }
+    for (int i = 0; i + 1 < kTerms; ++i) {
+        to[i] = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, b), __builtin_bit_cast(uint32_t, a), 0x07060302u);
+        a -= high_half(__builtin_bit_cast(uint32_t, a)), b -= high_half(__builtin_bit_cast(uint32_t, b));
     }
+    to[kTerms - 1] = pack2<bf16_t>(a, b);
 }
 // A word of two inputs as its bf16 terms.
 template <typename T, int kTerms> __device__ __forceinline__ void input_terms(uint32_t w, uint32_t (&to)[kTerms]) {
@@ -232,10 +230,13 @@ template <int KD, int NW, typename T, bool kStates> __global__ __launch_bounds__
     constexpr int kItemsK = 16 * kPieces, kItems = kStates ? kItemsK : 2 * kItemsK, kPer = (kItems + 64 * NW - 1) / (64 * NW);
     __shared__ __align__(16) uint16_t lds_q[kStates ? 1 : kIn][kStates ? 1 : kChunk][kRow], lds_k[kStates ? 1 : kIn][kStates ? 1 : kChunk][kRow];
     __shared__ __align__(16) uint16_t lds_kt[kIn][KD * 32][kChunk], lds_p[kMid][kStates ? 1 : kChunk][kColumn];
-    __shared__ __align__(16) float by_row[kChunk], by_token[kChunk];   // e^(ld (i + 1)); the tokens' decay up to the chunk's end (kStates: the block's)
+    __shared__ __align__(16) float by_row[kChunk], by_token[kChunk];   // scale e^(ld (i + 1)); the tokens' decay up to the chunk's end (kStates: the block's)
     const DecayParams &P = PP.d;
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), g = lane >> 4, r = lane & 15;
-    const uint32_t number = uniform(blockIdx.x / P.heads), h = blockIdx.x - number * P.heads, kv = uniform(h / P.group);
+    // (The heads of a block are started in another order for every block: workgroups go round the eight dies in turn, and heads whose decay is fast have
+    // less to do here, on whichever die they are.)
+    const uint32_t number = uniform(blockIdx.x / P.heads), h = uniform((blockIdx.x - number * P.heads + number) % P.heads), kv = uniform(h / P.group);
+    const uint64_t slot = (uint64_t)number * P.heads + h;
     const uint32_t block = choose_block(PP);
     const BlockPlace at = find_block(P, block, number);
     if (!at.found || (kStates && at.block + 1 == at.blocks)) return;
@@ -252,7 +253,7 @@ template <int KD, int NW, typename T, bool kStates> __global__ __launch_bounds__
     const bool live_column = column < P.dv;   // (the others compute what nobody reads)
     f32x4 S[2 * KD];
     // the state's rows of this lane: tile 2 p + t, register i
-    const float *from = kStates ? nullptr : at.blocks > 1 ? PP.block_states + ((uint64_t)blockIdx.x) * matrix
+    const float *from = kStates ? nullptr : at.blocks > 1 ? PP.block_states + slot * matrix
                                           : P.state_in && state != ~0ull ? P.state_in + (state * P.heads + h) * matrix : nullptr;
 #pragma unroll
     for (int m = 0; m < 2 * KD; ++m)
@@ -322,7 +323,7 @@ template <int KD, int NW, typename T, bool kStates> __global__ __launch_bounds__
         return t / 4 % 2 ? (u32x4){w[2], w[3], w[0], w[1]} : w;
     };
 
-    if (!kStates && tid < kChunk) by_row[tid] = __builtin_amdgcn_exp2f(ld2 * (float)(tid + 1));
+    if (!kStates && tid < kChunk) by_row[tid] = P.scale * __builtin_amdgcn_exp2f(ld2 * (float)(tid + 1));
     if (!kStates && tid < kChunk) by_token[tid] = __builtin_amdgcn_exp2f(ld2 * (float)(kChunk - 1 - tid));
     if (begin < end) load_chunk(begin);
     // The first chunk's loads are waited for here: with any of them under way at the loop's head, the compiler's wait there would be for all that the wave has
@@ -404,7 +405,7 @@ template <int KD, int NW, typename T, bool kStates> __global__ __launch_bounds__
                     }
                     const int apart = (int)(qt * 16 + l.r) - (int)(kt * 16 + l.g * 4);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) x[i] = apart >= i ? x[i] * __builtin_amdgcn_exp2f(ld2 * (float)(apart - i)) : 0.f;
+                    for (int i = 0; i < 4; ++i) x[i] = apart >= i ? x[i] * (P.scale * __builtin_amdgcn_exp2f(ld2 * (float)(apart - i))) : 0.f;
                     uint32_t lo[kMid], hi[kMid];
                     take_apart<kMid>(x[0], x[1], lo);
                     take_apart<kMid>(x[2], x[3], hi);
@@ -522,7 +523,6 @@ template <int KD, int NW, typename T, bool kStates> __global__ __launch_bounds__
             const auto rows = chunk_rows((T *)P.out + ((uint64_t)t0 * P.heads + h) * P.dv, m, stride, 2 * P.dv);
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
-                O[t] *= P.scale;
                 const uint32_t a = pack2<T>(O[t][0], O[t][1]), b = pack2<T>(O[t][2], O[t][3]);   // own column
                 const uint32_t got = of_neighbour(l.odd ? a : b), own = l.odd ? b : a;    // the lane's two rows, the other column and this one
                 const uint32_t left = l.odd ? got : own, right = l.odd ? own : got;
@@ -532,7 +532,7 @@ template <int KD, int NW, typename T, bool kStates> __global__ __launch_bounds__
         }
         __syncthreads();   // LDS is free again
     }
-    float *to = kStates ? PP.block_states + (uint64_t)blockIdx.x * matrix
+    float *to = kStates ? PP.block_states + slot * matrix
                         : at.block + 1 == at.blocks && P.state_out && state != ~0ull ? P.state_out + (state * P.heads + h) * matrix : nullptr;
     const uint32_t lane_rows = here(lane) / 16 * 8;
     if (to && live_column)
