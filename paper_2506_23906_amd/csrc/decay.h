@@ -114,7 +114,6 @@ template <typename T, int kRows> __global__ __launch_bounds__(256) void decay_st
 // 16 bits: 2^-17 of a term, where one term alone (2^-9) would add as much error as that rounding.  Inputs in fp16 are two bf16 terms each (11 bits,
 // exact): with bf16's exponents no sum of products overflows that fp32 holds.
 constexpr uint32_t kChunk = 64;
-constexpr uint32_t kDecayPad = 8;   // LDS rows end in 16 bytes more: sixteen rows' 16-byte pieces lie in other banks
 
 struct PromptParams {
     DecayParams d;
@@ -221,15 +220,22 @@ __device__ __forceinline__ u32x4 own_column(const uint32_t (&row)[4], bool odd) 
 }
 
 // KD: key components / 32, rounded up; NW: waves, each of which has 16 columns.
-template <int KD, int NW, typename T, bool kStates> __global__ __launch_bounds__(64 * NW, 4) void decay_prompt_kernel(PromptParams PP) {
+// Waves on a SIMD that LDS leaves room for, at most four (128 registers each): the bound for the registers.
+template <int KD, int NW, typename T, bool kStates> constexpr int prompt_occupancy() {
+    constexpr int kIn = __is_same(T, f16_t) ? 2 : 1, kRow = KD == 2 ? 64 : 128;
+    constexpr int kBytes = 2 * (kIn * KD * 32 * (int)kChunk + (kStates ? 0 : 2 * kIn * (int)kChunk * kRow + 2 * (int)(kChunk * kChunk))) + 1024;
+    constexpr int kGroups = 160 * 1024 / kBytes, kWaves = kGroups * NW / 4;
+    return kWaves > 4 ? 4 : kWaves < 1 ? 1 : kWaves;
+}
+template <int KD, int NW, typename T, bool kStates> __global__ __launch_bounds__(64 * NW, (prompt_occupancy<KD, NW, T, kStates>())) void decay_prompt_kernel(PromptParams PP) {
     constexpr int kIn = __is_same(T, f16_t) ? 2 : 1;                   // terms of an input
     constexpr int kMid = 2;                                            // of a score, of the state
-    constexpr int kRow = KD * 32 + kDecayPad, kColumn = kChunk + kDecayPad;
+    constexpr int kRow = KD == 2 ? 64 : 128;                           // of K and Q in LDS
     constexpr int kPieces = KD * 4;                                    // of 8 components
     // A lane brings 4 tokens x 8 components of K or of Q into LDS; a wave has either.
     constexpr int kItemsK = 16 * kPieces, kItems = kStates ? kItemsK : 2 * kItemsK, kPer = (kItems + 64 * NW - 1) / (64 * NW);
     __shared__ __align__(16) uint16_t lds_q[kStates ? 1 : kIn][kStates ? 1 : kChunk][kRow], lds_k[kStates ? 1 : kIn][kStates ? 1 : kChunk][kRow];
-    __shared__ __align__(16) uint16_t lds_kt[kIn][KD * 32][kChunk], lds_p[kMid][kStates ? 1 : kChunk][kColumn];
+    __shared__ __align__(16) uint16_t lds_kt[kIn][KD * 32][kChunk], lds_p[kMid][kStates ? 1 : kChunk][kChunk];
     __shared__ __align__(16) float by_row[kChunk], by_token[kChunk];   // scale e^(ld (i + 1)); the tokens' decay up to the chunk's end (kStates: the block's)
     const DecayParams &P = PP.d;
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), g = lane >> 4, r = lane & 15;
@@ -278,6 +284,9 @@ template <int KD, int NW, typename T, bool kStates> __global__ __launch_bounds__
         const uint32_t l = here(lane), c = wave * 16 + (l & 14);
         return At{l & 15, l >> 4, (l & 1) != 0, c < P.dv ? 2 * c : kNowhere};
     };
+    // (three that every phase needs do stay)
+    const uint32_t own_row = here(kRow == 128 ? r * 256 + (g ^ r) * 16 : r * 128 + (g ^ r >> 1) * 16), own_score = here(r * 128 + (g ^ r >> 1) * 16),
+                   own_kt = here(((r >> 2) * 8 + (r & 3)) * 128 + (g ^ (r >> 1)) * 16);
     u32x4 staged[kPer][4];
     uint32_t values[2][4];
     struct Part {
@@ -315,11 +324,14 @@ template <int KD, int NW, typename T, bool kStates> __global__ __launch_bounds__
 #pragma unroll
             for (int j = 0; j < 4; ++j) values[s][j] = __builtin_amdgcn_raw_buffer_load_b32(rows, off + (s * 32 + j) * stride, 0, 0);
     };
-    // K by component: row d has eight pieces of 8 tokens, in two halves, each in a place that keeps the lanes of a write (d / 8 differs) and of a read
-    // (bits 0, 1 and 3 of d differ) in different banks: piece u at u ^ (d / 8 mod 8) ^ (d & 2), its halves exchanged where d / 64 is odd.
-    const auto kt_lane = [&](const At &l) __attribute__((always_inline)) { return ((l.r >> 2) * 8 + (l.r & 3)) * 128 + (l.g ^ (l.r >> 2) ^ (l.r & 2)) * 16; };
+    // LDS rows are pieces of 16 bytes, exchanged by the row's number so that sixteen lanes with as many rows find them in different banks whatever lanes
+    // of one product go together (at the rows' natural places a read of C took 4 cycles more of 8): row i of 256 bytes has piece u at u ^ (i mod 16), of
+    // 128 bytes at u ^ (i / 2 mod 8).  K by component, row d: piece u, 8 tokens, at u ^ (2 (d / 8 mod 4) + (d / 2 mod 2)) ^ (d / 32 mod 2), its two halves
+    // exchanged where d / 64 is odd: the lanes of a read have d = 8 (r / 4) + r % 4 + ..., those of a write d / 8 from 0 to 15.
+    const auto row_piece = [&](uint32_t row, uint32_t u) __attribute__((always_inline)) { return kRow == 128 ? row * 256 + ((u ^ (row & 15)) * 16) : row * 128 + ((u ^ (row >> 1 & 7)) * 16); };
+    const auto score_piece = [&](uint32_t row, uint32_t u) __attribute__((always_inline)) { return row * 128 + ((u ^ (row >> 1 & 7)) * 16); };
     const auto kt_tile = [&](int a, uint32_t own, int t, int s) __attribute__((always_inline)) {   // components of tile t, tokens 32 s + 8 g .. + 7
-        const u32x4 w = *(const u32x4 *)((const char *)lds_kt[a] + own + (t / 2) * 32 * 128 + (t % 2) * 4 * 128 + (s ^ (t / 2 & 1)) * 64);
+        const u32x4 w = *(const u32x4 *)((const char *)lds_kt[a] + (own ^ (s * 64) ^ (t / 2 % 2 * 16)) + (t / 2) * 32 * 128 + (t % 2) * 4 * 128);
         return t / 4 % 2 ? (u32x4){w[2], w[3], w[0], w[1]} : w;
     };
 
@@ -350,17 +362,17 @@ template <int KD, int NW, typename T, bool kStates> __global__ __launch_bounds__
                             w[j][i] = terms[a];
                         }
                     if constexpr (!kStates) {
-                        uint16_t(*const to)[kRow] = p.is_q ? lds_q[a] : lds_k[a];
+                        char *const to = p.is_q ? (char *)lds_q[a] : (char *)lds_k[a];
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) *(u32x4 *)&to[p.rows + j][p.piece * 8] = (u32x4){w[j][0], w[j][1], w[j][2], w[j][3]};
+                        for (int j = 0; j < 4; ++j) *(u32x4 *)(to + row_piece(p.rows + j, p.piece)) = (u32x4){w[j][0], w[j][1], w[j][2], w[j][3]};
                     }
                     if (!p.is_q) {
-                        const uint32_t unit = p.rows / 8 ^ (p.piece & 7), half = (p.rows / 4 & 1) ^ (p.piece / 8 & 1);
+                        const uint32_t unit = p.rows / 8 ^ (p.piece & 3) * 2 ^ (p.piece / 4 & 1), half = (p.rows / 4 & 1) ^ (p.piece / 8 & 1);
                         char *to = (char *)lds_kt[a] + p.piece * 8 * 128 + half * 8;
 #pragma unroll
                         for (int c = 0; c < 8; ++c) {   // component c of the four tokens
                             const uint32_t sel = c % 2 ? 0x07060302u : 0x05040100u;
-                            *(u32x2 *)(to + c * 128 + (unit ^ (c & 2)) * 16) = (u32x2){__builtin_amdgcn_perm(w[1][c / 2], w[0][c / 2], sel), __builtin_amdgcn_perm(w[3][c / 2], w[2][c / 2], sel)};
+                            *(u32x2 *)(to + c * 128 + (unit ^ (c / 2 & 1)) * 16) = (u32x2){__builtin_amdgcn_perm(w[1][c / 2], w[0][c / 2], sel), __builtin_amdgcn_perm(w[3][c / 2], w[2][c / 2], sel)};
                         }
                     }
                 }
@@ -401,23 +413,26 @@ template <int KD, int NW, typename T, bool kStates> __global__ __launch_bounds__
                             for (int a = 0; a < kIn; ++a)
 #pragma unroll
                                 for (int b = 0; b + a < kIn; ++b)
-                                    x = mfma_bf16(*(const u32x4 *)&lds_k[a][kt * 16 + l.r][p * 32 + l.g * 8], *(const u32x4 *)&lds_q[b][qt * 16 + l.r][p * 32 + l.g * 8], x);
+                                    x = mfma_bf16(*(const u32x4 *)((const char *)lds_k[a] + kt * 32 * kRow + (own_row ^ (p * 64))), *(const u32x4 *)((const char *)lds_q[b] + qt * 32 * kRow + (own_row ^ (p * 64))), x);
                     }
                     const int apart = (int)(qt * 16 + l.r) - (int)(kt * 16 + l.g * 4);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) x[i] = apart >= i ? x[i] * (P.scale * __builtin_amdgcn_exp2f(ld2 * (float)(apart - i))) : 0.f;
+                    for (int i = 0; i < 4; ++i) {
+                        const float by = P.scale * __builtin_amdgcn_exp2f(ld2 * (float)max(apart - i, 0));
+                        x[i] = apart >= i ? x[i] * by : 0.f;
+                    }
                     uint32_t lo[kMid], hi[kMid];
                     take_apart<kMid>(x[0], x[1], lo);
                     take_apart<kMid>(x[2], x[3], hi);
 #pragma unroll
-                    for (int a = 0; a < kMid; ++a) *(u32x2 *)&lds_p[a][qt * 16 + l.r][kt * 16 + l.g * 4] = (u32x2){lo[a], hi[a]};
+                    for (int a = 0; a < kMid; ++a) *(u32x2 *)((char *)lds_p[a] + score_piece(qt * 16 + l.r, kt * 2 + l.g / 2) + l.g % 2 * 8) = (u32x2){lo[a], hi[a]};
                     phase();
                 }
             }
             // what the state before the chunk adds
 #pragma unroll
             for (int p = 0; p < KD; ++p) {
-                const At l = lane_at();
+                const uint32_t own = own_row ^ (p * 64);
                 u32x4 B[kMid];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
@@ -432,7 +447,7 @@ template <int KD, int NW, typename T, bool kStates> __global__ __launch_bounds__
                     for (int t0_ = 0; t0_ < 4; t0_ += 2) {
                         u32x4 A[2];
 #pragma unroll
-                        for (int t = 0; t < 2; ++t) A[t] = *(const u32x4 *)&lds_q[a][(t0_ + t) * 16 + l.r][p * 32 + l.g * 8];
+                        for (int t = 0; t < 2; ++t) A[t] = *(const u32x4 *)((const char *)lds_q[a] + own + (t0_ + t) * 32 * kRow);
 #pragma unroll
                         for (int b = 0; b + a < kMid; ++b)
 #pragma unroll
@@ -454,7 +469,6 @@ template <int KD, int NW, typename T, bool kStates> __global__ __launch_bounds__
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
             const At l = lane_at();
-            const uint32_t own = kt_lane(l);
             u32x4 W[3];
             const f32x4 by[2] = {*(const f32x4 *)&by_token[32 * s + 8 * l.g], *(const f32x4 *)&by_token[32 * s + 8 * l.g + 4]};
 #pragma unroll
@@ -474,7 +488,7 @@ template <int KD, int NW, typename T, bool kStates> __global__ __launch_bounds__
                 for (int a = 0; a < kIn; ++a) {
                     u32x4 A[kTogether];
 #pragma unroll
-                    for (int t = 0; t < kTogether; ++t) A[t] = kt_tile(a, own, t0_ + t, s);
+                    for (int t = 0; t < kTogether; ++t) A[t] = kt_tile(a, own_kt, t0_ + t, s);
 #pragma unroll
                     for (int c = 0; c + a < 3; ++c)
 #pragma unroll
@@ -493,7 +507,7 @@ template <int KD, int NW, typename T, bool kStates> __global__ __launch_bounds__
                     for (int a = 0; a < kMid; ++a) {
                         u32x4 A[4];
 #pragma unroll
-                        for (int t = 2 * s; t < 4; ++t) A[t] = *(const u32x4 *)&lds_p[a][t * 16 + l.r][s * 32 + l.g * 8];
+                        for (int t = 2 * s; t < 4; ++t) A[t] = *(const u32x4 *)((const char *)lds_p[a] + (own_score ^ (s * 64)) + t * 16 * 128);
 #pragma unroll
                         for (int b = 0; b < kIn && b + a < kMid; ++b)
 #pragma unroll
@@ -512,7 +526,7 @@ template <int KD, int NW, typename T, bool kStates> __global__ __launch_bounds__
                             const uint32_t q = t * 16 + rows + i;
                             float w = 0.f;
 #pragma unroll
-                            for (int a = 0; a < kMid; ++a) w += low_half(lds_p[a][q][j]);
+                            for (int a = 0; a < kMid; ++a) w += low_half(*(const uint16_t *)((const char *)lds_p[a] + score_piece(q, j / 8) + j % 8 * 2));
                             O[t][i] = q >= j ? O[t][i] + w * x : O[t][i];
                             phase();
                         }

@@ -148,30 +148,34 @@ mmv_status decay_params(DecayParams &P, uint64_t n, uint64_t tokens, uint32_t he
     P.n = (uint32_t)n, P.heads = heads, P.group = heads / kv_heads, P.dk = dk, P.dv = dv, P.scale = scale;
     return MMV_OK;
 }
-// Blocks of prompts (the least tokens of one, how many of a head): one for each request, or so many that the workgroups fill the device in whole rounds.
-#ifndef PT
-#define PT 1024
-#endif
-#ifndef PMIN
-#define PMIN 256
-#endif
-constexpr uint32_t kPromptGroups = PT, kLeastBlock = PMIN, kOneBlock = 1024;
+// Blocks of prompts (the least tokens of one, how many of a head): one for each request, or so many that the workgroups make two whole rounds of what the
+// device holds at once (us with one round / two / three: prompts of 63000 tokens, 16 heads, 128 columns 467 / 434 / 449, four of 9600 tokens, 256 columns - / 165 / 200).
+// A block is as short as one chunk while the chunks of all heads are less than about one round (three prompts of 900 tokens, 8 heads, blocks of
+// 64 / 128 / 256 tokens at least 18.1 / 20.6 / 27.3; of 2500 tokens 23.8 / 24.9 / 33.2), beyond two chunks: below that the states' traffic shows (5000
+// tokens, 16 heads 39.2 / 34.2 / 35.2).  Up to 256 tokens a block for each request: one launch (one prompt of 200: 14.7, with blocks 16.4; of 300: 17.5, 16.0).
+constexpr uint32_t kRounds = 2, kOneBlock = 256;
+constexpr uint64_t kFewTokens = 20480;   // times heads
+constexpr uint32_t prompt_waves(uint32_t dv) { return dv <= 64 ? 4 : dv <= 128 ? 8 : dv <= 160 ? 10 : 16; }
 struct DecayBlocks {
     uint32_t block, blocks;
     bool split;
 };
-inline DecayBlocks decay_blocks(uint64_t n, uint64_t tokens, uint32_t heads) {
+inline DecayBlocks decay_blocks(uint64_t n, uint64_t tokens, uint32_t heads, uint32_t dk, uint32_t dv) {
     if (tokens <= kOneBlock) return {kOneBlock, (uint32_t)n, false};
-    const uint64_t round = kPromptGroups / heads ? kPromptGroups / heads : 1, blocks = n + round / 2 > round ? n + round / 2 : round, more = blocks > n ? blocks - n : 1;
-    uint64_t block = kLeastBlock;
+    const uint32_t by_waves = 16 / prompt_waves(dv), by_lds = dk <= 64 ? 3 : 2, on_unit = by_waves < by_lds ? by_waves : by_lds;   // workgroups on a compute unit
+    uint64_t blocks = kRounds * kUnits * on_unit / heads;
+    if (blocks < n + blocks / 2) blocks = n + blocks / 2;
+    if (blocks == n) ++blocks;
+    const uint64_t least = tokens * heads <= kFewTokens ? kChunk : 2 * kChunk;
+    uint64_t block = least;
     if (n > 64) {   // enough for any lengths: requests need at most one block each and tokens / block
-        block = ceil_div(ceil_div(tokens, more), kChunk) * kChunk;
-        if (block < kLeastBlock) block = kLeastBlock;
+        block = ceil_div(ceil_div(tokens, blocks - n), kChunk) * kChunk;
+        if (block < least) block = least;
     }
-    return {(uint32_t)block, (uint32_t)(n + more), true};
+    return {(uint32_t)block, (uint32_t)blocks, true};
 }
 inline size_t decay_workspace(uint64_t n, uint64_t tokens, uint32_t heads, uint32_t dk, uint32_t dv) {
-    const DecayBlocks b = decay_blocks(n, tokens, heads);
+    const DecayBlocks b = decay_blocks(n, tokens, heads, dk, dv);
     return b.split ? round256((size_t)b.blocks * heads * dk * dv * 4) : 0;
 }
 template <int KD, int NW, typename T> mmv_status launch_prompts(const PromptParams &P, hipStream_t s) {
@@ -190,13 +194,17 @@ template <int KD, int NW, typename T> mmv_status launch_prompts(const PromptPara
     return launched();
 }
 template <int KD, typename T> mmv_status launch_prompts_of(const PromptParams &P, hipStream_t s) {
-    const uint32_t dv = P.d.dv;
-    return dv <= 64 ? launch_prompts<KD, 4, T>(P, s) : dv <= 128 ? launch_prompts<KD, 8, T>(P, s) : dv <= 160 ? launch_prompts<KD, 10, T>(P, s) : launch_prompts<KD, 16, T>(P, s);
+    switch (prompt_waves(P.d.dv)) {
+        case 4: return launch_prompts<KD, 4, T>(P, s);
+        case 8: return launch_prompts<KD, 8, T>(P, s);
+        case 10: return launch_prompts<KD, 10, T>(P, s);
+        default: return launch_prompts<KD, 16, T>(P, s);
+    }
 }
 mmv_status decay_call(const DecayParams &d, int type, void *d_ws, hipStream_t s) {
     PromptParams P = {};
     P.d = d;
-    const DecayBlocks b = decay_blocks(d.n, d.tokens, d.heads);
+    const DecayBlocks b = decay_blocks(d.n, d.tokens, d.heads, d.dk, d.dv);
     P.block = b.block, P.blocks = b.blocks;
     P.block_states = b.split ? (float *)d_ws : nullptr;
     if (type == MMV_TYPE_F16) return d.dk <= 64 ? launch_prompts_of<2, f16_t>(P, s) : launch_prompts_of<4, f16_t>(P, s);
