@@ -59,7 +59,7 @@ template <typename T, int kRows> __global__ __launch_bounds__(256) void decay_st
 #pragma unroll
         for (int i = 0; i < kRows; ++i) {
             S[i] = (f32x4){0.f, 0.f, 0.f, 0.f};
-            if (in && live && row + i * step < P.dk) S[i] = *(const f32x4 *)(in + (uint64_t)(row + i * step) * P.dv);
+            if (in && live && row + i * step < P.dk) S[i] = __builtin_nontemporal_load((const f32x4 *)(in + (uint64_t)(row + i * step) * P.dv));
         }
     };
     load(first);
@@ -80,7 +80,7 @@ template <typename T, int kRows> __global__ __launch_bounds__(256) void decay_st
             if (d < P.dk) {
                 S[i] = S[i] * decay + key[d] * v;
                 o += query[d] * S[i];
-                if (to) *(f32x4 *)(to + (uint64_t)d * P.dv) = S[i];
+                if (to) __builtin_nontemporal_store(S[i], (f32x4 *)(to + (uint64_t)d * P.dv));
             }
         }
     }

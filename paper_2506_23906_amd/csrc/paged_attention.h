@@ -32,7 +32,7 @@ struct AttentionParams {
     float *part_out, *part_ml;                     // [2 * workers][group][dim], [2 * workers][group][2]
     uint32_t *sums;                                // [n + 1] tiles of a head before every row, and of all
     uint32_t n, q_heads, heads, group, dim, page, pages, window, max_context, workers;
-    uint32_t groups_by, groups_shift, page_groups; // division by page / 8
+    Divider page_groups;                           // page / 8
     float score_by, out_by;                        // scale * k_scale * log2(e), v_scale
 };
 constexpr uint32_t kTile = 32;                     // positions
@@ -120,9 +120,9 @@ template <int KS, bool kExact, bool kStream, typename T, bool kE4m3> struct Tile
         const int32_t *row = P.table + (uint64_t)at.row * P.table_stride;
         uint64_t off[4];
         pages_ok = 0;
-        if (P.page_groups % 4 == 0) {   // a tile lies in one page
+        if (P.page_groups.divisor % 4 == 0) {   // a tile lies in one page
             const uint32_t group = at.tile * 4, page = page_of(P, group);
-            off[0] = place_of(P, scalar_load(row + page), group - page * P.page_groups, 15u);
+            off[0] = place_of(P, scalar_load(row + page), group - page * P.page_groups.divisor, 15u);
 #pragma unroll
             for (int i = 1; i < 4; ++i) off[i] = off[0] + (uint32_t)(8 * i) * slot_stride(P);
         } else {
@@ -133,7 +133,7 @@ template <int KS, bool kExact, bool kStream, typename T, bool kE4m3> struct Tile
                 const uint32_t group = at.tile * 4 + i, page = page_of(P, group);
                 id[i] = -1;
                 if (group * 8 < at.end) id[i] = scalar_load(row + page);   // (behind it the row may end)
-                inside[i] = group - page * P.page_groups;
+                inside[i] = group - page * P.page_groups.divisor;
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i) off[i] = place_of(P, id[i], inside[i], 1u << i);
@@ -153,7 +153,7 @@ template <int KS, bool kExact, bool kStream, typename T, bool kE4m3> struct Tile
         const uint64_t a = i & 1 ? off[1] : off[0], b = i & 1 ? off[3] : off[2];
         return i & 2 ? b : a;
     }
-    static __device__ __forceinline__ uint32_t page_of(const AttentionParams &P, uint32_t g8) { return P.groups_by ? __umulhi(g8, P.groups_by) >> P.groups_shift : g8 >> P.groups_shift; }
+    static __device__ __forceinline__ uint32_t page_of(const AttentionParams &P, uint32_t g8) { return P.page_groups.quotient(g8); }
     static __device__ __forceinline__ uint32_t slot_stride(const AttentionParams &P) { return kExact ? 32 * KS : P.slot_stride; }
     template <int kWords> static __device__ __forceinline__ void load(uint32_t (&to)[kWords], const char *p) {
         typedef uint32_t words __attribute__((ext_vector_type(kWords)));

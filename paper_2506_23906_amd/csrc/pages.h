@@ -9,14 +9,16 @@ namespace {
 // Two exclusive sums over the requests (tokens, pages taken), then every token finds its request by bisection among the
 // first tokens.  Up to kTablesLocal requests every workgroup makes the sums itself, in LDS: the lengths are a few KB that
 // come from the L2, and a launch of their own would take longer than the whole call.  Beyond, one workgroup leaves them in
-// the workspace.  The call is bound by its launch and by the chain lengths -> sums -> bisection -> slot.
+// the workspace.  The call is bound by its launch and by the chain lengths -> sums -> bisection -> page -> slot: 256 decoding
+// requests take 3.3 us on the GPU, 100 prompts of 180000 tokens 4.5.  One token a thread: four consecutive ones, with one bisection and wide
+// stores, made both slower (4.4 and 5.0), as did sums by shuffles through LDS (6.4 for the prompts, where every workgroup makes them).
 constexpr uint32_t kTablesLocal = 2048;
 constexpr int kTablesThreads = 256;
-constexpr uint32_t kTablesTokens = 4 * kTablesThreads;   // tokens of a workgroup
 constexpr uint32_t kInt32Max = 0x7fffffffu;
 
 struct TablesParams {
-    uint32_t n, page, max_tokens, free_count, table_width;
+    uint32_t n, max_tokens, free_count, table_width;
+    Divider page;
     uint64_t table_stride;
     const int32_t *cached, *fresh, *free_pages;
     int32_t *table, *offsets, *context, *positions;
@@ -27,18 +29,21 @@ struct TablesParams {
 struct Sum2 {
     uint64_t tokens, pages;
 };
-__device__ __forceinline__ uint64_t shift_up64(uint64_t v, int by, int lane) {
-    const uint64_t o = __shfl_up(v, by);
-    return lane >= by ? o : 0;
+template <int kCtrl, int kRowMask> __device__ __forceinline__ uint64_t dpp64(uint64_t v) {
+    return ((uint64_t)dpp_or_zero<kCtrl, kRowMask>((uint32_t)(v >> 32)) << 32) | dpp_or_zero<kCtrl, kRowMask>((uint32_t)v);
+}
+__device__ __forceinline__ uint64_t wave_upto64(uint64_t v) {   // inclusive sums over the lanes
+    v += dpp64<0x111, 0xF>(v);
+    v += dpp64<0x112, 0xF>(v);
+    v += dpp64<0x114, 0xF>(v);
+    v += dpp64<0x118, 0xF>(v);
+    v += dpp64<0x142, 0xA>(v);
+    return v + dpp64<0x143, 0xC>(v);
 }
 // Inclusive sums over the threads of a workgroup; `total` is the sum over all of them.
 template <int kThreads> __device__ __forceinline__ Sum2 block_scan(Sum2 v, Sum2 *lds, Sum2 &total) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        v.tokens += shift_up64(v.tokens, d, lane);
-        v.pages += shift_up64(v.pages, d, lane);
-    }
+    v.tokens = wave_upto64(v.tokens), v.pages = wave_upto64(v.pages);
     if (lane == 63) lds[wave] = v;
     __syncthreads();
     Sum2 before = {0, 0};
@@ -54,21 +59,23 @@ template <int kThreads> __device__ __forceinline__ Sum2 block_scan(Sum2 v, Sum2 
 }
 __device__ __forceinline__ uint32_t cut32(uint64_t v) { return v > kInt32Max ? kInt32Max : (uint32_t)v; }
 __device__ __forceinline__ uint32_t length_of(int32_t v) { return v < 0 ? 0u : (uint32_t)v; }
-// Pages that request r takes: those that hold its positions, less those that hold the cached ones.
-__device__ __forceinline__ uint32_t pages_taken(uint32_t cached, uint32_t fresh, uint32_t page) {
-    const uint32_t held = (uint32_t)(((uint64_t)cached + page - 1) / page);
-    return (uint32_t)(((uint64_t)cached + fresh + page - 1) / page) - held;
+// Pages that hold `positions` (up to 2^32): a quotient of positions - 1 below 2^31, or of its halves.
+__device__ __forceinline__ uint32_t pages_of(uint64_t positions, const Divider &page) {
+    if (positions == 0) return 0;
+    const uint64_t last = positions - 1;
+    return (last >> 31 ? (uint32_t)(last / page.divisor) : page.quotient((uint32_t)last)) + 1;
 }
 
-// Sums over all requests, kThreads at a time: ends[r] and taken[r], cut at 2^31 - 1 (a token number never reaches that).
-template <int kThreads> __device__ __forceinline__ Sum2 sum_requests(const TablesParams &P, uint32_t *ends, uint32_t *taken, Sum2 *lds) {
+// Sums over all requests, kThreads at a time: ends[r] and taken[r], cut at 2^31 - 1 (a token number never reaches that), and the cached lengths beside them.
+template <int kThreads> __device__ __forceinline__ Sum2 sum_requests(const TablesParams &P, uint32_t *ends, uint32_t *taken, uint32_t *cached, Sum2 *lds) {
     Sum2 carry = {0, 0};
     for (uint32_t first = 0; first < P.n; first += kThreads) {
         const uint32_t r = first + threadIdx.x;
         Sum2 own = {0, 0}, total;
         if (r < P.n) {
-            const uint32_t fresh = length_of(P.fresh[r]);
-            own = {fresh, pages_taken(length_of(P.cached[r]), fresh, P.page)};
+            const uint32_t fresh = length_of(P.fresh[r]), old = length_of(P.cached[r]);
+            own = {fresh, pages_of((uint64_t)old + fresh, P.page) - pages_of(old, P.page)};
+            if (cached) cached[r] = old;
         }
         const Sum2 s = block_scan<kThreads>(own, lds, total);
         if (r < P.n) {
@@ -79,10 +86,6 @@ template <int kThreads> __device__ __forceinline__ Sum2 sum_requests(const Table
     }
     return carry;
 }
-__device__ __forceinline__ void write_request(const TablesParams &P, uint32_t r, uint32_t end) {
-    P.offsets[r + 1] = (int32_t)end;
-    P.context[r] = (int32_t)cut32((uint64_t)length_of(P.cached[r]) + length_of(P.fresh[r]));
-}
 __device__ __forceinline__ void write_totals(const TablesParams &P, Sum2 total) {
     P.used[0] = (int64_t)total.pages;
     P.used[1] = (int64_t)total.tokens;
@@ -91,61 +94,53 @@ __device__ __forceinline__ void write_totals(const TablesParams &P, Sum2 total) 
 
 __global__ __launch_bounds__(1024) void sum_requests_kernel(TablesParams P) {
     __shared__ Sum2 lds[16];
-    const Sum2 total = sum_requests<1024>(P, P.ends, P.taken, lds);
+    const Sum2 total = sum_requests<1024>(P, P.ends, P.taken, nullptr, lds);
     if (threadIdx.x == 0) write_totals(P, total);
 }
 
 template <bool kLocal> __global__ __launch_bounds__(kTablesThreads) void page_tables_kernel(TablesParams P) {
-    __shared__ uint32_t lds_ends[kLocal ? kTablesLocal : 1], lds_taken[kLocal ? kTablesLocal : 1];
+    __shared__ uint32_t lds_ends[kLocal ? kTablesLocal : 1], lds_taken[kLocal ? kTablesLocal : 1], lds_cached[kLocal ? kTablesLocal : 1];
     __shared__ Sum2 lds[kTablesThreads / 64];
     const uint32_t *ends = P.ends, *taken = P.taken;
     if constexpr (kLocal) {
-        const Sum2 total = sum_requests<kTablesThreads>(P, lds_ends, lds_taken, lds);
+        const Sum2 total = sum_requests<kTablesThreads>(P, lds_ends, lds_taken, lds_cached, lds);
         if (blockIdx.x == 0 && threadIdx.x == 0) write_totals(P, total);
         __syncthreads();
         ends = lds_ends, taken = lds_taken;
     }
-    for (uint32_t r = blockIdx.x * kTablesThreads + threadIdx.x; r < P.n; r += gridDim.x * kTablesThreads) write_request(P, r, ends[r]);
-    const uint32_t all = P.n ? ends[P.n - 1] : 0u;
-#pragma unroll
-    for (uint32_t i = 0; i < kTablesTokens; i += kTablesThreads) {
-        const uint64_t t64 = (uint64_t)blockIdx.x * kTablesTokens + i + threadIdx.x;
-        if (t64 >= P.max_tokens) return;
-        const uint32_t t = (uint32_t)t64;
-        int64_t slot = -1;
-        int32_t position = -1;
-        if (t < all) {
-            uint32_t lo = 0, hi = P.n - 1;   // the first request that ends behind t
-            while (lo < hi) {
-                const uint32_t mid = (lo + hi) >> 1;
-                if (ends[mid] > t) hi = mid;
-                else lo = mid + 1;
-            }
-            const uint32_t cached = length_of(P.cached[lo]), fresh = length_of(P.fresh[lo]);
-            const uint64_t at = (uint64_t)cached + (t - (lo ? ends[lo - 1] : 0u));
-            (void)fresh;
-            if (at <= kInt32Max) {
-                position = (int32_t)at;
-                const uint32_t where = (uint32_t)at / P.page, place = (uint32_t)at % P.page, held = (uint32_t)(((uint64_t)cached + P.page - 1) / P.page);
-                if (where < P.table_width) {
-                    int32_t *const entry = P.table + (uint64_t)lo * P.table_stride + where;
-                    int32_t id = -1;
-                    if (where < held) {
-                        id = *entry;
-                    } else {
-                        const uint64_t which = (uint64_t)taken[lo] + (where - held);
-                        if (which < P.free_count) {
-                            id = P.free_pages[which];
-                            if (place == 0) *entry = id;
-                        }
-                    }
-                    if (id >= 0) slot = (int64_t)id * P.page + place;
-                }
+    const auto cached_of = [&](uint32_t r) __attribute__((always_inline)) { return kLocal ? lds_cached[kLocal ? r : 0] : length_of(P.cached[r]); };
+    const uint64_t own = (uint64_t)blockIdx.x * kTablesThreads + threadIdx.x;
+    for (uint64_t r = own; r < P.n; r += (uint64_t)gridDim.x * kTablesThreads) {
+        P.offsets[r + 1] = (int32_t)ends[r];
+        P.context[r] = (int32_t)cut32((uint64_t)cached_of((uint32_t)r) + length_of(P.fresh[r]));
+    }
+    if (own >= P.max_tokens) return;
+    const uint32_t t = (uint32_t)own, all = P.n ? ends[P.n - 1] : 0u;
+    int64_t slot = -1;
+    int32_t position = -1;
+    if (t < all) {
+        uint32_t r = 0, hi = P.n - 1;   // the first request that ends behind t
+        while (r < hi) {
+            const uint32_t mid = (r + hi) >> 1;
+            if (ends[mid] > t) hi = mid;
+            else r = mid + 1;
+        }
+        const uint32_t cached = cached_of(r);
+        const uint64_t at = (uint64_t)cached + (t - (r ? ends[r - 1] : 0u));
+        if (at <= kInt32Max) {
+            position = (int32_t)at;
+            const uint32_t where = P.page.quotient((uint32_t)at), held = pages_of(cached, P.page), place = (uint32_t)at - where * P.page.divisor;
+            const uint64_t which = (uint64_t)taken[r] + (where - held);   // (of the free pages, behind those that the request has)
+            int32_t *const entry = P.table + (uint64_t)r * P.table_stride + where;
+            if (where < P.table_width && (where < held || which < P.free_count)) {
+                const int32_t id = where < held ? *entry : P.free_pages[which];
+                if (where >= held && place == 0) *entry = id;
+                if (id >= 0) slot = (int64_t)id * P.page.divisor + place;
             }
         }
-        P.slots[t] = slot;
-        P.positions[t] = position;
     }
+    P.slots[t] = slot;
+    P.positions[t] = position;
 }
 
 // ---- cache append -------------------------------------------------------------------------------------------------
@@ -157,8 +152,9 @@ struct AppendParams {
     uint64_t k_stride, v_stride;   // elements
     const int64_t *slots;
     void *cache_k, *cache_v;
-    uint64_t page_stride, head_stride, slot_stride, total;   // total: threads with work
-    uint32_t page, num_slots, pieces, head_pieces;           // pieces of eight values of a token, of a head
+    uint64_t page_stride, head_stride, slot_stride;
+    uint32_t total, num_slots;     // total: threads with work
+    Divider page, pieces, head_pieces;   // pieces of eight values of a token, of a head
     float k_by, v_by;
 };
 
@@ -177,15 +173,14 @@ template <typename T> __device__ __forceinline__ uint2 to_e4m3(const T *x, float
 }
 
 template <typename T, bool kE4m3> __global__ __launch_bounds__(256) void cache_append_kernel(AppendParams P) {
-    const uint64_t id = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+    const uint32_t id = blockIdx.x * 256 + threadIdx.x;
     if (id >= P.total) return;
-    const uint64_t t = id / P.pieces;
-    const uint32_t piece = (uint32_t)(id - t * P.pieces), h = piece / P.head_pieces, c = piece - h * P.head_pieces;
+    const uint32_t t = P.pieces.quotient(id), piece = id - t * P.pieces.divisor, h = P.head_pieces.quotient(piece), c = piece - h * P.head_pieces.divisor;
+    const uint4 k = *(const uint4 *)((const T *)P.k + t * P.k_stride + 8 * piece), v = *(const uint4 *)((const T *)P.v + t * P.v_stride + 8 * piece);
     const int64_t slot = P.slots[t];
     if ((uint64_t)slot >= P.num_slots) return;
-    const uint32_t p = (uint32_t)slot / P.page, in_page = (uint32_t)slot - p * P.page;
+    const uint32_t p = P.page.quotient((uint32_t)slot), in_page = (uint32_t)slot - p * P.page.divisor;
     const uint64_t to = (uint64_t)p * P.page_stride + (uint64_t)h * P.head_stride + (uint64_t)in_page * P.slot_stride + 8 * c;
-    const uint4 k = *(const uint4 *)((const T *)P.k + t * P.k_stride + 8 * piece), v = *(const uint4 *)((const T *)P.v + t * P.v_stride + 8 * piece);
     if constexpr (kE4m3) {
         *(uint2 *)((uint8_t *)P.cache_k + to) = to_e4m3((const T *)&k, P.k_by);
         *(uint2 *)((uint8_t *)P.cache_v + to) = to_e4m3((const T *)&v, P.v_by);

@@ -29,22 +29,11 @@ mmv_status mmv_page_tables(uint64_t n, const int32_t *d_cached, const int32_t *d
     if (!aligned_to(d_slots, 8) || !aligned_to(d_used, 8)) return MMV_ERR_INVALID_ARG;
     if (const mmv_status st = check_workspace(d_ws, ws_bytes, tables_workspace(n))) return st;
     TablesParams P = {};
-    P.n = (uint32_t)n, P.page = page, P.max_tokens = (uint32_t)max_tokens, P.free_count = (uint32_t)free_count;
+    P.n = (uint32_t)n, P.page = divider(page), P.max_tokens = (uint32_t)max_tokens, P.free_count = (uint32_t)free_count;
     P.table_width = d_table ? (uint32_t)table_width : 0u, P.table_stride = table_stride;
     P.cached = d_cached, P.fresh = d_new, P.free_pages = d_free, P.table = d_table;
     P.offsets = d_offsets, P.context = d_context, P.positions = d_positions, P.slots = d_slots, P.used = d_used;
-    hipStream_t s = (hipStream_t)hip_stream;
-    uint64_t blocks = ceil_div(max_tokens, kTablesTokens);
-    if (blocks < 1) blocks = 1;
-    if (n <= kTablesLocal) {
-        page_tables_kernel<true><<<(unsigned)blocks, kTablesThreads, 0, s>>>(P);
-        return launched();
-    }
-    P.ends = (uint32_t *)d_ws, P.taken = P.ends + n;
-    sum_requests_kernel<<<1, 1024, 0, s>>>(P);
-    if (const mmv_status st = launched()) return st;
-    page_tables_kernel<false><<<(unsigned)blocks, kTablesThreads, 0, s>>>(P);
-    return launched();
+    return tables_call(P, d_ws, (hipStream_t)hip_stream);
 }
 
 mmv_status mmv_cache_append(uint64_t tokens, const void *d_k, uint64_t k_stride, const void *d_v, uint64_t v_stride, mmv_type type,

@@ -22,6 +22,20 @@ inline mmv_status check_workspace(const void *ws, size_t bytes, size_t needed) {
 
 inline size_t tables_workspace(uint64_t n) { return n <= kTablesLocal ? 0 : round256(8 * n); }
 
+mmv_status tables_call(TablesParams P, void *d_ws, hipStream_t s) {
+    const uint64_t blocks = ceil_div(P.max_tokens, kTablesThreads);
+    const unsigned grid = blocks ? (unsigned)blocks : 1;
+    if (P.n <= kTablesLocal) {
+        page_tables_kernel<true><<<grid, kTablesThreads, 0, s>>>(P);
+        return launched();
+    }
+    P.ends = (uint32_t *)d_ws, P.taken = P.ends + P.n;
+    sum_requests_kernel<<<1, 1024, 0, s>>>(P);
+    if (const mmv_status st = launched()) return st;
+    page_tables_kernel<false><<<grid, kTablesThreads, 0, s>>>(P);
+    return launched();
+}
+
 // The cache itself, and that values of `type` can go into it and be multiplied with it.
 inline mmv_status check_cache(const mmv_paged_cache *c, int type) {
     if (!c) return MMV_ERR_NULL;
@@ -39,20 +53,21 @@ inline mmv_status check_cache(const mmv_paged_cache *c, int type) {
 mmv_status append_call(uint64_t tokens, const void *k, uint64_t k_stride, const void *v, uint64_t v_stride, int type, const int64_t *slots,
                        const mmv_paged_cache &c, hipStream_t s) {
     AppendParams P = {};
-    P.k = k, P.v = v, P.k_stride = k_stride, P.v_stride = v_stride, P.slots = slots;
+    P.k_stride = k_stride, P.v_stride = v_stride;
     P.cache_k = c.d_k, P.cache_v = c.d_v, P.page_stride = c.page_stride, P.head_stride = c.head_stride, P.slot_stride = c.slot_stride;
-    P.page = c.page, P.num_slots = (uint32_t)(c.pages * c.page), P.head_pieces = c.dim / 8, P.pieces = c.heads * P.head_pieces;
-    P.total = tokens * P.pieces;
+    P.page = divider(c.page), P.num_slots = (uint32_t)(c.pages * c.page), P.head_pieces = divider(c.dim / 8), P.pieces = divider(c.heads * (c.dim / 8));
     P.k_by = (float)(1.0 / c.k_scale), P.v_by = (float)(1.0 / c.v_scale);
-    const uint64_t blocks = ceil_div(P.total, 256);
-    if (blocks >= k2to31) return MMV_ERR_INVALID_ARG;
-    if (c.type == MMV_TYPE_E4M3) {
-        if (type == MMV_TYPE_F16) cache_append_kernel<f16_t, true><<<(unsigned)blocks, 256, 0, s>>>(P);
-        else cache_append_kernel<bf16_t, true><<<(unsigned)blocks, 256, 0, s>>>(P);
-    } else {
-        cache_append_kernel<bf16_t, false><<<(unsigned)blocks, 256, 0, s>>>(P);   // (bits are copied: one kernel for both types)
+    const uint64_t most = (k2to31 - 256) / P.pieces.divisor;   // tokens of a launch: its pieces have numbers below 2^31
+    for (uint64_t first = 0; first < tokens; first += most) {
+        P.total = (uint32_t)((tokens - first < most ? tokens - first : most) * P.pieces.divisor);
+        P.k = (const char *)k + 2 * first * k_stride, P.v = (const char *)v + 2 * first * v_stride, P.slots = slots + first;
+        const unsigned blocks = (unsigned)ceil_div(P.total, 256);
+        if (c.type != MMV_TYPE_E4M3) cache_append_kernel<bf16_t, false><<<blocks, 256, 0, s>>>(P);   // (bits are copied: one kernel for both types)
+        else if (type == MMV_TYPE_F16) cache_append_kernel<f16_t, true><<<blocks, 256, 0, s>>>(P);
+        else cache_append_kernel<bf16_t, true><<<blocks, 256, 0, s>>>(P);
+        if (const mmv_status st = launched()) return st;
     }
-    return launched();
+    return MMV_OK;
 }
 
 inline bool attention_sizes(uint64_t n, uint32_t q_heads, uint32_t heads, uint32_t dim, uint64_t max_context) {
@@ -108,12 +123,7 @@ mmv_status attention_call(AttentionParams P, int type, int cache_type, void *d_w
     const AttentionLayout L = attention_layout(P.n, P.q_heads, P.heads, P.dim, P.max_context, e4m3);
     P.sums = (uint32_t *)d_ws, P.part_ml = (float *)((char *)d_ws + L.ml), P.part_out = (float *)((char *)d_ws + L.out);
     P.workers = attention_workers(P.n, P.heads, P.dim, P.max_context, e4m3);
-    // Division of a number below 2^28 by page / 8: a shift, or a product's upper half and a shift (exact: the factor is at most 2^-28 of itself too large).
-    P.page_groups = P.page / 8;
-    uint32_t bits = 0;
-    while ((1u << bits) < P.page_groups) ++bits;
-    if ((1u << bits) == P.page_groups) P.groups_by = 0, P.groups_shift = bits;
-    else P.groups_by = (uint32_t)(((1ull << (31 + bits)) + P.page_groups - 1) / P.page_groups), P.groups_shift = bits - 1;
+    P.page_groups = divider(P.page / 8);
     if (type == MMV_TYPE_F16) e4m3 ? launch_attention_over<f16_t, true>(P, s) : launch_attention_over<f16_t, false>(P, s);
     else e4m3 ? launch_attention_over<bf16_t, true>(P, s) : launch_attention_over<bf16_t, false>(P, s);
     if (const mmv_status st = launched()) return st;

@@ -30,4 +30,17 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t make_rsrc(const void *p, uint3
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), 0, (int)bytes, 0x00027000);
 }
 
+// Division of numbers below 2^31 by one of at most 2^17: a shift, or the upper half of a product and a shift (the factor is too large by less than 2^-31 of
+// itself, so the quotient is exact).
+struct Divider {
+    uint32_t by, shift, divisor;
+    __device__ __forceinline__ uint32_t quotient(uint32_t v) const { return by ? __umulhi(v, by) >> shift : v >> shift; }
+};
+inline Divider divider(uint32_t d) {
+    uint32_t bits = 0;
+    while ((1u << bits) < d) ++bits;
+    if ((1u << bits) == d) return {0, bits, d};
+    return {(uint32_t)(((1ull << (31 + bits)) + d - 1) / d), bits - 1, d};
+}
+
 }  // namespace
