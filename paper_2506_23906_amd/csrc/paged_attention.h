@@ -286,9 +286,98 @@ template <int kDims, typename T> __device__ __forceinline__ void write_segment(c
     if (g == 0) P.part_ml[2 * part] = most, P.part_ml[2 * part + 1] = sum;
 }
 
-template <int KS, bool kExact, bool kStream, typename T, bool kE4m3> __global__ __launch_bounds__(256, KS > 4 ? 1 : 2) void paged_attention_kernel(AttentionParams P) {
+// `left` tiles of the list from a place on; at the end of every segment, and of the run, finish(place, begun, ended, maximum, sum, output) has what the wave has of it: begun:
+// the segment began before the run (given for the first one), ended: it ends here.
+template <int KS, bool kExact, bool kStream, typename T, bool kE4m3, typename Finish>
+__device__ __forceinline__ void attention_run(const AttentionParams &P, Place at, uint32_t left, bool begun, uint32_t g, uint32_t r, Finish finish) {
     using TileT = Tile<KS, kExact, kStream, T, kE4m3>;
     constexpr int kDims = TileT::kDims;
+            TileT tile;
+            tile.find(P, at, g, r);
+            tile.load_keys(P, g);
+            tile.load_values(P, r);
+            u32x4 q[KS];
+            f32x4 O[kDims];
+            float most = -INFINITY, sum = 0.f;
+            bool fresh = true;
+            for (;;) {
+                if (fresh) {   // a new segment: its queries
+                    fresh = false;
+                    const T *pq = (const T *)P.q + (uint64_t)at.row * P.q_stride + (uint64_t)(at.head * P.group + r) * P.dim;
+    #pragma unroll
+                    for (int s = 0; s < KS; ++s) {
+                        const uint32_t d = TileT::step_dim(s, g);
+                        q[s] = (u32x4){0, 0, 0, 0};
+                        if (r < P.group && d < P.dim) q[s] = *(const u32x4 *)(pq + d);
+                    }
+    #pragma unroll
+                    for (int c = 0; c < kDims; ++c) O[c] = (f32x4){0.f, 0.f, 0.f, 0.f};
+                    most = -INFINITY, sum = 0.f;
+                }
+                f32x4 S[2];
+                tile.scores(P, q, g, S);
+                float s[8];
+    #pragma unroll
+                for (int i = 0; i < 8; ++i) s[i] = S[i / 4][i % 4] * P.score_by;
+                const uint32_t pages_ok = tile.pages_ok;
+                // the next tile's place; its keys are on their way while this one's values are multiplied
+                const Place now = at;
+                --left;
+                if (left && ++at.tile == at.last) {
+                    if (++at.head == P.heads) {
+                        at.head = 0;
+                        do {
+                            ++at.row;
+                            enter_row(P, at, scalar_load(P.context + at.row));
+                        } while (at.first == at.last);   // (a row without positions; a later one has some, as `left` says)
+                    }
+                    at.tile = at.first;
+                }
+                if (pages_ok != 15u || now.tile * kTile < now.begin || (now.tile + 1) * kTile > now.end) {
+                    uint32_t keep = 0;
+    #pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const uint32_t p = now.tile * kTile + 8 * g + i;
+                        if (((pages_ok >> g) & 1) && p >= now.begin && p < now.end) keep |= 1u << i;
+                        s[i] = (keep >> i) & 1 ? s[i] : -INFINITY;
+                    }
+    #pragma unroll
+                    for (int j = 0; j < 8; ++j)   // (0 times what lies there need not be 0)
+    #pragma unroll
+                        for (int w = 0; w < TileT::kValueWords; ++w) tile.v[j][w] = (keep >> j) & 1 ? tile.v[j][w] : 0u;
+                }
+                tile.find(P, at, g, r);   // (behind the run's last tile: that one again, not used)
+                tile.load_keys(P, g);
+                float top = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
+                // Scores up to 2^8 above the base need no new one (nothing overflows: 16-bit floats reach 2^15).
+                if (__any(top > most + 8.f)) {
+                    const float m = fmaxf(over_g_max(top), most), by = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(most - m);
+                    most = m;
+                    sum *= by;
+    #pragma unroll
+                    for (int c = 0; c < kDims; ++c) O[c] *= by;
+                }
+                const float base = most == -INFINITY ? 0.f : most;
+    #pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    s[i] = __builtin_amdgcn_exp2f(s[i] - base);
+                    sum += s[i];
+                }
+                // Probabilities are rounded to the values' 16 bits: the matrix cores take both operands of one type.
+                const u32x4 p = {pack2<T>(s[0], s[1]), pack2<T>(s[2], s[3]), pack2<T>(s[4], s[5]), pack2<T>(s[6], s[7])};
+                tile.add_values(p, O);
+                tile.load_values(P, r);
+                const bool ended = now.tile + 1 == now.last;
+                if (ended || !left) {
+                    finish(now, begun, ended, most, over_g_sum(sum), O);
+                    fresh = true, begun = false;
+                }
+                if (!left) break;
+            }
+}
+
+template <int KS, bool kExact, bool kStream, typename T, bool kE4m3> __global__ __launch_bounds__(256, KS > 4 ? 1 : 2) void paged_attention_kernel(AttentionParams P) {
+    constexpr int kDims = dims_per_lane<KS>();
     const uint32_t lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
     const uint32_t worker = uniform(blockIdx.x * 4 + (threadIdx.x >> 6));
     // the list's length, this wave's run of it, and where that begins
@@ -331,90 +420,63 @@ template <int KS, bool kExact, bool kStream, typename T, bool kE4m3> __global__ 
         const uint32_t inside = start - rows_before * P.heads, count = at.last - at.first;
         at.head = uniform(inside / count);
         at.tile = at.first + uniform(inside % count);
-        bool begun = at.tile != at.first;   // the current segment began in an earlier wave's run
+        attention_run<KS, kExact, kStream, T, kE4m3>(P, at, left, at.tile != at.first, g, r,
+                                                     [&](const Place &now, bool begun, bool ended, float most, float sum, const f32x4 (&O)[kDims]) __attribute__((always_inline)) {
+                                                         write_segment<kDims>(P, now, worker, begun, ended, g, r, most, sum, O, T());
+                                                     });
+    }
+}
 
-        TileT tile;
-        tile.find(P, at, g, r);
-        tile.load_keys(P, g);
-        tile.load_values(P, r);
-        u32x4 q[KS];
-        f32x4 O[kDims];
-        float most = -INFINITY, sum = 0.f;
-        bool fresh = true;
-        for (;;) {
-            if (fresh) {   // a new segment: its queries
-                fresh = false;
-                const T *pq = (const T *)P.q + (uint64_t)at.row * P.q_stride + (uint64_t)(at.head * P.group + r) * P.dim;
+// Where no segment has more tiles than a few for each of at most eight waves: a workgroup has one, and joins its waves' parts in LDS.  One launch, and no sums
+// over the rows ahead of the first load.
+constexpr uint32_t kWholeWaves = 8;
+template <int KS, bool kExact, bool kStream, typename T, bool kE4m3> __global__ __launch_bounds__(64 * kWholeWaves, 2) void whole_attention_kernel(AttentionParams P) {
+    constexpr int kDims = dims_per_lane<KS>();
+    __shared__ float ml[kWholeWaves][16][2];
+    extern __shared__ __align__(16) float parts[];   // [waves][group][dim]
+    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), waves = blockDim.x / 64, g = lane >> 4, r = lane & 15;
+    Place at;
+    at.row = uniform(blockIdx.x / P.heads), at.head = blockIdx.x - at.row * P.heads;
+    enter_row(P, at, scalar_load(P.context + at.row));
+    const uint32_t count = at.last - at.first, run = (count + waves - 1) / waves, start = min(wave * run, count), left = min(run, count - start);
+    if (left) {
+        at.tile = at.first + start;
+        attention_run<KS, kExact, kStream, T, kE4m3>(P, at, left, false, g, r,
+                                                     [&](const Place &, bool, bool, float most, float sum, const f32x4 (&O)[kDims]) __attribute__((always_inline)) {
+                                                         if (run == count) write_segment<kDims>(P, at, 0, false, true, g, r, most, sum, O, T());   // (this wave has all of it)
+                                                         if (r >= P.group || run == count) return;
+                                                         float *const part = parts + (wave * P.group + r) * P.dim;
 #pragma unroll
-                for (int s = 0; s < KS; ++s) {
-                    const uint32_t d = TileT::step_dim(s, g);
-                    q[s] = (u32x4){0, 0, 0, 0};
-                    if (r < P.group && d < P.dim) q[s] = *(const u32x4 *)(pq + d);
-                }
+                                                         for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int c = 0; c < kDims; ++c) O[c] = (f32x4){0.f, 0.f, 0.f, 0.f};
-                most = -INFINITY, sum = 0.f;
-            }
-            f32x4 S[2];
-            tile.scores(P, q, g, S);
-            float s[8];
+                                                             for (int c = 0; c < kDims; c += 4) {
+                                                                 const uint32_t d = dim_of<kDims>(c, 4 * g + i);
+                                                                 if (d < P.dim) *(f32x4 *)(part + d) = (f32x4){O[c][i], O[c + 1][i], O[c + 2][i], O[c + 3][i]};
+                                                             }
+                                                         if (g == 0) ml[wave][r][0] = most, ml[wave][r][1] = sum;
+                                                     });
+    }
+    if (run == count && count) return;
+    __syncthreads();
+    // (every thread makes the waves' factors anew: one more barrier for making them once takes longer)
+    const uint64_t first = (uint64_t)at.row * P.q_heads + (uint64_t)at.head * P.group;
+    const uint32_t used = count ? (count + run - 1) / run : 0;
+    for (uint32_t id = tid; id < P.group * P.dim; id += 64 * waves) {
+        const uint32_t q = id / P.dim;
+        float most[kWholeWaves], top = -INFINITY, total = 0.f, x = 0.f;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) s[i] = S[i / 4][i % 4] * P.score_by;
-            const uint32_t pages_ok = tile.pages_ok;
-            // the next tile's place; its keys are on their way while this one's values are multiplied
-            const Place now = at;
-            --left;
-            if (left && ++at.tile == at.last) {
-                if (++at.head == P.heads) {
-                    at.head = 0;
-                    do {
-                        ++at.row;
-                        enter_row(P, at, scalar_load(P.context + at.row));
-                    } while (at.first == at.last);   // (a row without positions; a later one has some, as `left` says)
-                }
-                at.tile = at.first;
-            }
-            if (pages_ok != 15u || now.tile * kTile < now.begin || (now.tile + 1) * kTile > now.end) {
-                uint32_t keep = 0;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const uint32_t p = now.tile * kTile + 8 * g + i;
-                    if (((pages_ok >> g) & 1) && p >= now.begin && p < now.end) keep |= 1u << i;
-                    s[i] = (keep >> i) & 1 ? s[i] : -INFINITY;
-                }
-#pragma unroll
-                for (int j = 0; j < 8; ++j)   // (0 times what lies there need not be 0)
-#pragma unroll
-                    for (int w = 0; w < TileT::kValueWords; ++w) tile.v[j][w] = (keep >> j) & 1 ? tile.v[j][w] : 0u;
-            }
-            tile.find(P, at, g, r);   // (behind the run's last tile: that one again, not used)
-            tile.load_keys(P, g);
-            float top = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
-            // Scores up to 2^8 above the base need no new one (nothing overflows: 16-bit floats reach 2^15).
-            if (__any(top > most + 8.f)) {
-                const float m = fmaxf(over_g_max(top), most), by = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(most - m);
-                most = m;
-                sum *= by;
-#pragma unroll
-                for (int c = 0; c < kDims; ++c) O[c] *= by;
-            }
-            const float base = most == -INFINITY ? 0.f : most;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                s[i] = __builtin_amdgcn_exp2f(s[i] - base);
-                sum += s[i];
-            }
-            // Probabilities are rounded to the values' 16 bits: the matrix cores take both operands of one type.
-            const u32x4 p = {pack2<T>(s[0], s[1]), pack2<T>(s[2], s[3]), pack2<T>(s[4], s[5]), pack2<T>(s[6], s[7])};
-            tile.add_values(p, O);
-            tile.load_values(P, r);
-            const bool ended = now.tile + 1 == now.last;
-            if (ended || !left) {
-                write_segment<kDims>(P, now, worker, begun, ended, g, r, most, over_g_sum(sum), O, T());
-                fresh = true, begun = false;
-            }
-            if (!left) break;
+        for (uint32_t w = 0; w < kWholeWaves; ++w) {
+            most[w] = w < used ? ml[w][q][0] : -INFINITY;
+            top = fmaxf(top, most[w]);
         }
+        const float base = top == -INFINITY ? 0.f : top;
+#pragma unroll
+        for (uint32_t w = 0; w < kWholeWaves; ++w) {
+            const float f = __builtin_amdgcn_exp2f(most[w] - base);
+            if (w < used && f != 0.f) total += f * ml[w][q][1], x += f * parts[w * P.group * P.dim + id];   // (a part without positions has weight 0; one that is not a number keeps it)
+        }
+        ((T *)P.out)[first * P.dim + id] = from_f32<T>(total == 0.f ? 0.f : x * (P.out_by / total));
+        if (P.lse && id == q * P.dim) P.lse[first + q] = total == 0.f && top == -INFINITY ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * kLn2;
     }
 }
 

@@ -98,17 +98,32 @@ inline AttentionLayout attention_layout(uint64_t n, uint32_t q_heads, uint32_t h
 // (for a cache of either size of values)
 inline size_t attention_workspace(uint64_t n, uint32_t q_heads, uint32_t heads, uint32_t dim, uint64_t max_context) { return attention_layout(n, q_heads, heads, dim, max_context, true).total; }
 
+// One workgroup for a segment, of as many waves as it can have tiles (by the table, or the window), eight at most; 0: the list of tiles.  Us, list / whole segments:
+// 8 segments of 100 positions 9.4 / 5.6, of 250 9.4 / 7.9, of 500 9.5 / 10.5; 64 ragged ones up to 500 9.8 / 9.2, up to 1000 10.7 / 14.0; 384 in a window
+// of 1024 15.0 / 13.9; 1024 of 350 51.3 / 49.5; 2048 up to 1000 74.8 / 90.8.  So: two tiles for a wave at most, or more where the segments
+// keep the device busy by themselves; and not many rounds of workgroups, each of which begins with loads that nothing hides.
+inline uint32_t whole_waves(const AttentionParams &P) {
+    const uint64_t positions = P.window && P.window < P.max_context ? (uint64_t)P.window + kTile - 1 : P.max_context;
+    const uint64_t tiles = positions ? ceil_div(positions, kTile) : 1, waves = tiles < kWholeWaves ? tiles : kWholeWaves, steps = ceil_div(tiles, waves);
+    const uint64_t segments = (uint64_t)P.n * P.heads, rounds = ceil_div(segments * waves, 2 * kUnits * kWholeWaves);
+    return (steps <= 2 || segments >= kUnits) && steps * rounds <= 6 && P.group * P.dim <= 2048 ? (uint32_t)waves : 0u;   // (their parts fit 64 KB of LDS)
+}
+template <int KS, bool kExact, bool kStream, typename T, bool kE4m3> void launch_attention_kernel(const AttentionParams &P, hipStream_t s) {
+    if (const uint32_t waves = whole_waves(P))
+        whole_attention_kernel<KS, kExact, kStream, T, kE4m3><<<P.n * P.heads, 64 * waves, waves * P.group * P.dim * 4, s>>>(P);
+    else
+        paged_attention_kernel<KS, kExact, kStream, T, kE4m3><<<(P.workers + 3) / 4, 256, 0, s>>>(P);
+}
 template <bool kStream, typename T, bool kE4m3> void launch_attention(const AttentionParams &P, hipStream_t s) {
-    const unsigned blocks = (P.workers + 3) / 4;
     const bool packed = P.slot_stride == P.dim;
-    if (P.dim == 64 && packed) paged_attention_kernel<2, true, kStream, T, kE4m3><<<blocks, 256, 0, s>>>(P);
-    else if (P.dim == 128 && packed) paged_attention_kernel<4, true, kStream, T, kE4m3><<<blocks, 256, 0, s>>>(P);
-    else if (P.dim == 256 && packed) paged_attention_kernel<8, true, kStream, T, kE4m3><<<blocks, 256, 0, s>>>(P);
-    else if (P.dim <= 64) paged_attention_kernel<2, false, kStream, T, kE4m3><<<blocks, 256, 0, s>>>(P);
-    else if (P.dim <= 96) paged_attention_kernel<3, false, kStream, T, kE4m3><<<blocks, 256, 0, s>>>(P);
-    else if (P.dim <= 128) paged_attention_kernel<4, false, kStream, T, kE4m3><<<blocks, 256, 0, s>>>(P);
-    else if (P.dim <= 160) paged_attention_kernel<5, false, kStream, T, kE4m3><<<blocks, 256, 0, s>>>(P);
-    else paged_attention_kernel<8, false, kStream, T, kE4m3><<<blocks, 256, 0, s>>>(P);
+    if (P.dim == 64 && packed) launch_attention_kernel<2, true, kStream, T, kE4m3>(P, s);
+    else if (P.dim == 128 && packed) launch_attention_kernel<4, true, kStream, T, kE4m3>(P, s);
+    else if (P.dim == 256 && packed) launch_attention_kernel<8, true, kStream, T, kE4m3>(P, s);
+    else if (P.dim <= 64) launch_attention_kernel<2, false, kStream, T, kE4m3>(P, s);
+    else if (P.dim <= 96) launch_attention_kernel<3, false, kStream, T, kE4m3>(P, s);
+    else if (P.dim <= 128) launch_attention_kernel<4, false, kStream, T, kE4m3>(P, s);
+    else if (P.dim <= 160) launch_attention_kernel<5, false, kStream, T, kE4m3>(P, s);
+    else launch_attention_kernel<8, false, kStream, T, kE4m3>(P, s);
 }
 // A cache that the chip's own (256 MB on the memory side) cannot keep until the next call is read past it.  Us without / with: 48 rows of 330 MB 71.9 ->
 // 68.8, 16 rows of 730 MB 136 -> 123, 13 rows of 160 MB 36.7 -> 35.2; but 24 rows of 56 MB, three such caches in turn, 14.9 -> 16.5.
@@ -127,6 +142,7 @@ mmv_status attention_call(AttentionParams P, int type, int cache_type, void *d_w
     if (type == MMV_TYPE_F16) e4m3 ? launch_attention_over<f16_t, true>(P, s) : launch_attention_over<f16_t, false>(P, s);
     else e4m3 ? launch_attention_over<bf16_t, true>(P, s) : launch_attention_over<bf16_t, false>(P, s);
     if (const mmv_status st = launched()) return st;
+    if (whole_waves(P)) return MMV_OK;   // (nothing to join)
     const unsigned blocks = P.n * P.q_heads;
     if (type == MMV_TYPE_F16) join_attention_kernel<f16_t><<<blocks, 256, 0, s>>>(P);
     else join_attention_kernel<bf16_t><<<blocks, 256, 0, s>>>(P);
