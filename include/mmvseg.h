@@ -395,7 +395,7 @@ mmv_status mmv_cache_append(uint64_t tokens, const void *d_k, uint64_t k_stride,
  *               does not have (-1) are left out.
  *   d_out       n * q_heads * dim of `type`;  d_lse  n * q_heads fp32, or NULL
  * A row without any position gets zeros and -infinity.  What lies in the cache at positions that are left out is not used,
- * whatever it is.  Scores and sums are fp32; probabilities are rounded to `type` before they meet the values.
+ * whatever it is.  Scores and sums are fp32; probabilities meet the values in fp16, or in 16 bits of mantissa with bf16.
  *   q_heads a multiple of the cache's heads, at most 16 times; page a multiple of 8; n * heads * table_width * page / 32 < 2^32.
  *   d_ws        mmv_paged_attention_workspace_bytes(n, q_heads, heads, dim, table_width * page) bytes */
 size_t mmv_paged_attention_workspace_bytes(uint64_t n, uint32_t q_heads, uint32_t heads, uint32_t dim, uint64_t max_context);

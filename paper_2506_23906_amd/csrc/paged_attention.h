@@ -60,6 +60,20 @@ template <bool kHigh> __device__ __forceinline__ uint32_t widen(bf16_t, uint32_t
 template <bool kHigh> __device__ __forceinline__ uint32_t widen(f16_t, uint32_t w) {
     return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)w, 1.f, kHigh));
 }
+// Probabilities meet the values in 16 bits, as the matrix cores take both operands of one type.  In bf16 they are two terms, the upper 8 bits and the rounded rest
+// (16 bits together): rounded once they added as much error as the rounding of the result (1.4 times the error of exact ones; fp16, 11 bits, 1.1 to 1.2 times,
+// is left at one).  The rest is never quite zero: a value's infinity times a positive probability stays that infinity.
+template <typename T> constexpr int kTerms = __is_same(T, bf16_t) ? 2 : 1;
+template <typename T> __device__ __forceinline__ void probability_terms(float a, float b, uint32_t (&to)[kTerms<T>]) {
+    if constexpr (kTerms<T> == 1) {
+        to[0] = pack2<T>(a, b);
+    } else {
+        const uint32_t x = __builtin_bit_cast(uint32_t, a), y = __builtin_bit_cast(uint32_t, b);
+        to[0] = __builtin_amdgcn_perm(y, x, 0x07060302u);
+        const float rest_a = a - __builtin_bit_cast(float, x & 0xFFFF0000u), rest_b = b - __builtin_bit_cast(float, y & 0xFFFF0000u);
+        to[1] = pack2<T>(rest_a < 1e-35f ? 1e-35f : rest_a, rest_b < 1e-35f ? 1e-35f : rest_b);
+    }
+}
 // Largest / sum over the four lanes that differ in g.
 __device__ __forceinline__ float over_g_max(float v) {
     v = fmaxf(v, __shfl_xor(v, 16));
@@ -243,9 +257,11 @@ template <int KS, bool kExact, bool kStream, typename T, bool kE4m3> struct Tile
         }
         return a;
     }
-    template <int c = 0> __device__ __forceinline__ void add_values(u32x4 p, f32x4 (&O)[kDims]) const {
+    template <int c = 0> __device__ __forceinline__ void add_values(const u32x4 (&p)[kTerms<T>], f32x4 (&O)[kDims]) const {
         if constexpr (c < kDims) {
-            O[c] = mfma_16x16x32(T(), column<c>(), p, O[c]);
+            const u32x4 a = column<c>();
+#pragma unroll
+            for (int i = 0; i < kTerms<T>; ++i) O[c] = mfma_16x16x32(T(), a, p[i], O[c]);
             add_values<c + 1>(p, O);
         }
     }
@@ -363,8 +379,14 @@ __device__ __forceinline__ void attention_run(const AttentionParams &P, Place at
                     s[i] = __builtin_amdgcn_exp2f(s[i] - base);
                     sum += s[i];
                 }
-                // Probabilities are rounded to the values' 16 bits: the matrix cores take both operands of one type.
-                const u32x4 p = {pack2<T>(s[0], s[1]), pack2<T>(s[2], s[3]), pack2<T>(s[4], s[5]), pack2<T>(s[6], s[7])};
+                u32x4 p[kTerms<T>];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    uint32_t terms[kTerms<T>];
+                    probability_terms<T>(s[2 * i], s[2 * i + 1], terms);
+#pragma unroll
+                    for (int t = 0; t < kTerms<T>; ++t) p[t][i] = terms[t];
+                }
                 tile.add_values(p, O);
                 tile.load_values(P, r);
                 const bool ended = now.tile + 1 == now.last;
@@ -427,11 +449,12 @@ template <int KS, bool kExact, bool kStream, typename T, bool kE4m3> __global__ 
     }
 }
 
-// Where no segment has more tiles than a few for each of at most eight waves: a workgroup has one, and joins its waves' parts in LDS.  One launch, and no sums
-// over the rows ahead of the first load.
-constexpr uint32_t kWholeWaves = 8;
-template <int KS, bool kExact, bool kStream, typename T, bool kE4m3> __global__ __launch_bounds__(64 * kWholeWaves, 2) void whole_attention_kernel(AttentionParams P) {
+// Where no segment has more tiles than a few for each of at most eight waves (four beyond 128 dims, which take more than half of a SIMD's registers): a workgroup has
+// one, and joins its waves' parts in LDS.  One launch, and no sums over the rows ahead of the first load.
+constexpr uint32_t whole_waves_most(uint32_t dim) { return dim <= 128 ? 8 : 4; }
+template <int KS, bool kExact, bool kStream, typename T, bool kE4m3> __global__ __launch_bounds__(64 * whole_waves_most(32 * KS), KS > 4 ? 1 : 2) void whole_attention_kernel(AttentionParams P) {
     constexpr int kDims = dims_per_lane<KS>();
+    constexpr uint32_t kWholeWaves = whole_waves_most(32 * KS);
     __shared__ float ml[kWholeWaves][16][2];
     extern __shared__ __align__(16) float parts[];   // [waves][group][dim]
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), waves = blockDim.x / 64, g = lane >> 4, r = lane & 15;

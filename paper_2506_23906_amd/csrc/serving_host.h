@@ -98,14 +98,14 @@ inline AttentionLayout attention_layout(uint64_t n, uint32_t q_heads, uint32_t h
 // (for a cache of either size of values)
 inline size_t attention_workspace(uint64_t n, uint32_t q_heads, uint32_t heads, uint32_t dim, uint64_t max_context) { return attention_layout(n, q_heads, heads, dim, max_context, true).total; }
 
-// One workgroup for a segment, of as many waves as it can have tiles (by the table, or the window), eight at most; 0: the list of tiles.  Us, list / whole segments:
+// One workgroup for a segment, of as many waves as it can have tiles (by the table, or the window); 0: the list of tiles.  Us, list / whole segments:
 // 8 segments of 100 positions 9.4 / 5.6, of 250 9.4 / 7.9, of 500 9.5 / 10.5; 64 ragged ones up to 500 9.8 / 9.2, up to 1000 10.7 / 14.0; 384 in a window
 // of 1024 15.0 / 13.9; 1024 of 350 51.3 / 49.5; 2048 up to 1000 74.8 / 90.8.  So: two tiles for a wave at most, or more where the segments
 // keep the device busy by themselves; and not many rounds of workgroups, each of which begins with loads that nothing hides.
 inline uint32_t whole_waves(const AttentionParams &P) {
     const uint64_t positions = P.window && P.window < P.max_context ? (uint64_t)P.window + kTile - 1 : P.max_context;
-    const uint64_t tiles = positions ? ceil_div(positions, kTile) : 1, waves = tiles < kWholeWaves ? tiles : kWholeWaves, steps = ceil_div(tiles, waves);
-    const uint64_t segments = (uint64_t)P.n * P.heads, rounds = ceil_div(segments * waves, 2 * kUnits * kWholeWaves);
+    const uint64_t tiles = positions ? ceil_div(positions, kTile) : 1, most = whole_waves_most(P.dim), waves = tiles < most ? tiles : most, steps = ceil_div(tiles, waves);
+    const uint64_t segments = (uint64_t)P.n * P.heads, rounds = ceil_div(segments * waves, 2 * kUnits * most);
     return (steps <= 2 || segments >= kUnits) && steps * rounds <= 6 && P.group * P.dim <= 2048 ? (uint32_t)waves : 0u;   // (their parts fit 64 KB of LDS)
 }
 template <int KS, bool kExact, bool kStream, typename T, bool kE4m3> void launch_attention_kernel(const AttentionParams &P, hipStream_t s) {

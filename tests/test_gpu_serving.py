@@ -473,3 +473,34 @@ def test_the_calls_give_the_same_through_either_marshalling(native, monkeypatch)
         B.mmv_cache_append(q.cuda(), q.cuda(), ints([0, 1, 2], torch.int64), cache)   # (twice the heads)
     with pytest.raises(B.MmvError):
         B.mmv_page_tables(ints(contexts), ints([1, 1, 0]), ints([1, 0]), rows, page, 6, out=tables, ws=ws)
+
+
+@pytest.mark.parametrize("columns", [0, 3000])   # a narrow table: a workgroup for a segment; a wide one: the list of tiles
+@pytest.mark.parametrize("heads,group,dim,page,dtype,cache_type", [(2, 4, 128, 16, BF16, BF16), (1, 3, 72, 8, F16, F16), (2, 2, 64, 32, BF16, E4M3), (1, 8, 256, 8, BF16, BF16), (2, 1, 160, 24, F16, E4M3)])
+def test_attention_does_not_use_what_is_left_out_in_either_form(columns, heads, group, dim, page, dtype, cache_type):
+    """NaN in all that is not to be seen: behind the context, before the window, in pages of nobody and of rows that are not there."""
+    contexts, window = [37, 5, 0, 129, 64, 200, 32, 1], 90
+    cache, kc, vc, table, q = attention_case(8, contexts, heads, group, dim, page, dtype, cache_type)
+    seen = {(table[r][p // page], p % page) for r, c in enumerate(contexts) for p in range(max(0, c - window), c)}
+    for x, on_gpu in ((kc, cache.k), (vc, cache.v)):
+        raw = x.view(torch.uint8) if cache_type == E4M3 else x
+        for i in range(x.shape[0]):
+            for s in range(page):
+                if (i, s) not in seen:
+                    raw[i, :, s] = 0x7F if cache_type == E4M3 else (NAN, math.inf, -math.inf)[(i + s) % 3]
+        (on_gpu.view(torch.uint8) if cache_type == E4M3 else on_gpu).copy_(raw)
+    table = [row + [-1] * columns for row in table]
+    run_attention(cache, kc, vc, table, q, contexts, window=window, what="window")
+    run_attention(cache, kc, vc, table, q, contexts, window=29, what="a narrower window")
+    table[3][2], table[5][-1 - columns], table[4] = 10 ** 9, -7, [-1] * len(table[4])
+    run_attention(cache, kc, vc, table, q, contexts, window=window, what="pages that are not there")
+    contexts = [-1] * 8
+    out = run_attention(cache, kc, vc, table, q, contexts)
+    assert bool((out == 0).all())
+
+
+def test_attention_over_a_cache_without_pages():
+    k = torch.empty(0, 2, 16, 64, dtype=BF16, device="cuda")
+    lse = torch.zeros(3, 4, device="cuda")
+    out = B.mmv_paged_attention(torch.ones(3, 4, 64, dtype=BF16, device="cuda"), B.PagedCache(k, k.clone()), ints([[-1, 0], [1, 2], [5, -1]]), ints([5, 30, 0]), lse=lse)
+    assert bool((out == 0).all()) and bool((lse == -math.inf).all())
