@@ -504,16 +504,16 @@ template <int KS, bool kExact, bool kStream, typename T, bool kE4m3> __global__ 
 }
 
 // Joins the parts of the segments that several waves share, and writes the rows without positions: a workgroup for a row and query head.  Its
-// four waves take every fourth part each, eight of them under way at a time.
-template <typename T> __global__ __launch_bounds__(256) void join_attention_kernel(AttentionParams P) {
-    __shared__ float lds[4][256 + 2];
+// kWaves waves take every kWaves-th part each, eight of them under way at a time.
+template <typename T, int kWaves> __global__ __launch_bounds__(64 * kWaves) void join_attention_kernel(AttentionParams P) {
+    __shared__ float lds[kWaves][256 + 2];
     const uint32_t lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), id = blockIdx.x;
     const uint32_t row = id / P.q_heads, qh = id - row * P.q_heads, h = qh / P.group, q = qh - h * P.group;
     const uint32_t before = (uint32_t)scalar_load((const int32_t *)P.sums + row), behind = (uint32_t)scalar_load((const int32_t *)P.sums + row + 1);
     const uint32_t all = (uint32_t)scalar_load((const int32_t *)P.sums + P.n) * P.heads, tiles = behind - before;
     T *out = (T *)P.out + (uint64_t)id * P.dim;
     if (tiles == 0) {
-        if (threadIdx.x < P.dim) out[threadIdx.x] = from_f32<T>(0.f);
+        for (uint32_t d = threadIdx.x; d < P.dim; d += 64 * kWaves) out[d] = from_f32<T>(0.f);
         if (P.lse && threadIdx.x == 0) P.lse[id] = -INFINITY;
         return;
     }
@@ -522,11 +522,11 @@ template <typename T> __global__ __launch_bounds__(256) void join_attention_kern
     // (the segment begins in the first wave's run: its part is that wave's second one)
     const auto place = [&](uint32_t w) __attribute__((always_inline)) { return (uint64_t)(2 * w + (w == first ? 1 : 0)) * P.group + q; };
     float most = -INFINITY, sum = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-    for (uint32_t w0 = first + wave; w0 <= last; w0 += 32) {
+    for (uint32_t w0 = first + wave; w0 <= last; w0 += 8 * kWaves) {
         float part[8][4], m[8], l[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const uint64_t at = place(min(w0 + 4 * i, last));
+            const uint64_t at = place(min(w0 + kWaves * i, last));
             m[i] = P.part_ml[2 * at], l[i] = P.part_ml[2 * at + 1];
 #pragma unroll
             for (int c = 0; c < 4; ++c) part[i][c] = lane + 64 * c < P.dim ? P.part_out[at * P.dim + lane + 64 * c] : 0.f;
@@ -534,7 +534,7 @@ template <typename T> __global__ __launch_bounds__(256) void join_attention_kern
         float top = most;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            if (w0 + 4 * i > last) m[i] = -INFINITY;
+            if (w0 + kWaves * i > last) m[i] = -INFINITY;
             top = fmaxf(top, m[i]);
         }
         const float base = top == -INFINITY ? 0.f : top, by = __builtin_amdgcn_exp2f(most - base);
@@ -543,7 +543,7 @@ template <typename T> __global__ __launch_bounds__(256) void join_attention_kern
         for (int c = 0; c < 4; ++c) o[c] *= by;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const float f = w0 + 4 * i > last ? 0.f : __builtin_amdgcn_exp2f(m[i] - base);
+            const float f = w0 + kWaves * i > last ? 0.f : __builtin_amdgcn_exp2f(m[i] - base);
             if (f != 0.f) {   // (a part without positions has weight 0; one that is not a number keeps it)
                 sum += f * l[i];
 #pragma unroll
@@ -555,18 +555,20 @@ template <typename T> __global__ __launch_bounds__(256) void join_attention_kern
     for (int c = 0; c < 4; ++c) lds[wave][lane + 64 * c] = o[c];
     if (lane == 0) lds[wave][256] = most, lds[wave][257] = sum;
     __syncthreads();
-    const uint32_t d = threadIdx.x;
-    float top = -INFINITY, total = 0.f, x = 0.f;
+    float top = -INFINITY;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) top = fmaxf(top, lds[w][256]);
+    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, lds[w][256]);
     const float base = top == -INFINITY ? 0.f : top;
+    for (uint32_t d = threadIdx.x; d < P.dim; d += 64 * kWaves) {
+        float total = 0.f, x = 0.f;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
-        const float f = __builtin_amdgcn_exp2f(lds[w][256] - base);
-        if (f != 0.f) total += f * lds[w][257], x += f * lds[w][d];
+        for (int w = 0; w < kWaves; ++w) {
+            const float f = __builtin_amdgcn_exp2f(lds[w][256] - base);
+            if (f != 0.f) total += f * lds[w][257], x += f * lds[w][d];
+        }
+        out[d] = from_f32<T>(total == 0.f ? 0.f : x * (P.out_by / total));
+        if (P.lse && d == 0) P.lse[id] = total == 0.f && top == -INFINITY ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * kLn2;
     }
-    if (d < P.dim) out[d] = from_f32<T>(total == 0.f ? 0.f : x * (P.out_by / total));
-    if (P.lse && d == 0) P.lse[id] = total == 0.f && top == -INFINITY ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * kLn2;
 }
 
 }  // namespace

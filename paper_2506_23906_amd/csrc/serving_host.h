@@ -133,6 +133,17 @@ template <typename T, bool kE4m3> void launch_attention_over(const AttentionPara
     if (bytes > kStreamBytes) launch_attention<true, T, kE4m3>(P, s);
     else launch_attention<false, T, kE4m3>(P, s);
 }
+// Many segments have few parts each and fill the device with two waves a workgroup; fewer segments have more parts, which four waves take at
+// once.  Two and four waves, of whole calls: 96 rows of 20 query heads 37.5 and 41.1 us, 100 of 14 12.5 and 13.0; 67 rows of 16 19.5 and
+// 17.2, 7 of 32 24.9 and 17.0.
+constexpr uint32_t kManyJoins = 1280;
+
+template <typename T> void launch_join(const AttentionParams &P, hipStream_t s) {
+    const uint32_t blocks = P.n * P.q_heads;
+    if (blocks > kManyJoins) join_attention_kernel<T, 2><<<blocks, 128, 0, s>>>(P);
+    else join_attention_kernel<T, 4><<<blocks, 256, 0, s>>>(P);
+}
+
 mmv_status attention_call(AttentionParams P, int type, int cache_type, void *d_ws, hipStream_t s) {
     const bool e4m3 = cache_type == MMV_TYPE_E4M3;
     const AttentionLayout L = attention_layout(P.n, P.q_heads, P.heads, P.dim, P.max_context, e4m3);
@@ -143,9 +154,8 @@ mmv_status attention_call(AttentionParams P, int type, int cache_type, void *d_w
     else e4m3 ? launch_attention_over<bf16_t, true>(P, s) : launch_attention_over<bf16_t, false>(P, s);
     if (const mmv_status st = launched()) return st;
     if (whole_waves(P)) return MMV_OK;   // (nothing to join)
-    const unsigned blocks = P.n * P.q_heads;
-    if (type == MMV_TYPE_F16) join_attention_kernel<f16_t><<<blocks, 256, 0, s>>>(P);
-    else join_attention_kernel<bf16_t><<<blocks, 256, 0, s>>>(P);
+    if (type == MMV_TYPE_F16) launch_join<f16_t>(P, s);
+    else launch_join<bf16_t>(P, s);
     return launched();
 }
 

@@ -66,7 +66,7 @@ WHOLE, LIST, JOIN, PROMPT, BLOCKS = "whole_attention_kernel", "paged_attention_k
     ("attention(3, 2)", [(WHOLE, 24, 64)]), ("attention(3, 16)", [(WHOLE, 24, 512)]), ("attention(3, 32)", [(WHOLE, 24, 512)]),
     ("attention(3, 33)", [(LIST, 102, 256), (JOIN, 96, 256)]), ("attention(3, 1000)", [(LIST, 256, 256), (JOIN, 96, 256)]),
     # a window bounds them too; enough segments keep the device busy with longer ones; too many would come in rounds
-    ("attention(3, 1000, window=225)", [(WHOLE, 24, 512)]), ("attention(40, 80)", [(WHOLE, 320, 512)]), ("attention(400, 80)", [(LIST, 256, 256), (JOIN, 12800, 256)]),
+    ("attention(3, 1000, window=225)", [(WHOLE, 24, 512)]), ("attention(40, 80)", [(WHOLE, 320, 512)]), ("attention(400, 80)", [(LIST, 256, 256), (JOIN, 12800, 128)]),
     ("attention(3, 2, heads=1, group=16)", [(WHOLE, 3, 64)]),
     ("decay(3, 256)", [(PROMPT, 24, 256)]), ("decay(3, 257)", [(PROMPT, 8 * 192, 256), (BLOCKS, 96, 256), (PROMPT, 8 * 192, 256)]),
     ("decay(3, 9000, 16, 128, 128)", [(PROMPT, 1024, 512), (BLOCKS, 768, 256), (PROMPT, 1024, 512)]), ("decay(3, 0)", [(PROMPT, 24, 256)]),
