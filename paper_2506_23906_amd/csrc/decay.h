@@ -239,22 +239,16 @@ template <int KD, int NW, typename T, bool kStates> __global__ __launch_bounds__
     __shared__ __align__(16) float by_row[kChunk], by_token[kChunk];   // scale e^(ld (i + 1)); the tokens' decay up to the chunk's end (kStates: the block's)
     const DecayParams &P = PP.d;
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), g = lane >> 4, r = lane & 15;
-    // (The heads of a block are started in another order for every block: workgroups go round the eight dies in turn, and heads whose decay is fast have
-    // less to do here, on whichever die they are.)
-    const uint32_t number = uniform(blockIdx.x / P.heads), h = uniform((blockIdx.x - number * P.heads + number) % P.heads), kv = uniform(h / P.group);
+    const uint32_t number = uniform(blockIdx.x / P.heads), h = uniform(blockIdx.x - number * P.heads), kv = uniform(h / P.group);
     const uint64_t slot = (uint64_t)number * P.heads + h;
     const uint32_t block = choose_block(PP);
     const BlockPlace at = find_block(P, block, number);
     if (!at.found || (kStates && at.block + 1 == at.blocks)) return;
     const Span span = span_of(P, at.request);
-    uint32_t begin = uniform(span.begin + at.block * block);
+    const uint32_t begin = uniform(span.begin + at.block * block);
     const uint32_t end = uniform(min(span.end, begin + block));
     const uint64_t state = state_of(P, at.request), matrix = (uint64_t)P.dk * P.dv;
     const float ld2 = head_decay(P, h) * kLog2e;
-    if (kStates && ld2 < 0.f) {   // tokens whose decay up to the block's end is zero in fp32 (below 2^-150) add nothing
-        const float reach = 152.f / -ld2;
-        if (reach + 1.f < (float)(end - begin)) begin += uniform(((end - begin) - (uint32_t)reach - 1) / kChunk * kChunk);
-    }
     const uint32_t column = wave * 16 + r;
     const bool live_column = column < P.dv;   // (the others compute what nobody reads)
     f32x4 S[2 * KD];

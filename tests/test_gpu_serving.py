@@ -390,6 +390,26 @@ def test_decay_keeps_what_is_not_finite_in_its_request_and_head(step):
     assert torch.equal(torch.isnan(state.cpu()), torch.isnan(final))
 
 
+def test_decay_keeps_what_is_not_finite_however_fast_the_decay():
+    """In a prompt of several blocks a NaN stays in the state as it does token by token, also where the decay since is zero in fp32."""
+    lengths, heads, dk, dv = [900, 300], 4, 64, 64
+    tokens, n = sum(lengths), len(lengths)
+    q, k, v = (normal(i, tokens, heads, 64) for i in range(3))
+    v[3, :, 7] = NAN
+    k[910, 1, 5] = math.inf
+    ld, ends = decays(heads, "hard"), [0, 900, 1200]
+    state = torch.zeros(n, heads, dk, dv, device="cuda")
+    out = B.mmv_decay_attention(q.cuda(), k.cuda(), v.cuda(), ints(ends), ld.cuda(), scale=1.0, state_out=state).cpu()
+    assert bool(out[3:900, :, 7].isnan().all()) and bool(state[0, :, :, 7].isnan().all())
+    assert not bool((~out[910:, 1].isfinite()).logical_not().any()) and not bool(state[1, 1, 5].isfinite().any())
+    other = out.clone()
+    other[3:900, :, 7], other[910:, 1] = 0, 0
+    assert bool(other.isfinite().all())
+    rest = state.clone()
+    rest[0, :, :, 7], rest[1, 1, 5] = 0, 0
+    assert bool(rest.isfinite().all())
+
+
 # ---- a step in a graph --------------------------------------------------------------------------------------------
 
 
