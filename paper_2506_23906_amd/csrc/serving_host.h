@@ -184,12 +184,15 @@ mmv_status decay_params(DecayParams &P, uint64_t n, uint64_t tokens, uint32_t he
     P.n = (uint32_t)n, P.heads = heads, P.group = heads / kv_heads, P.dk = dk, P.dv = dv, P.scale = scale;
     return MMV_OK;
 }
-// Blocks of prompts (the least tokens of one, how many of a head): one for each request, or so many that the workgroups make two whole rounds of what the
-// device holds at once (us with one round / two / three: prompts of 63000 tokens, 16 heads, 128 columns 467 / 434 / 449, four of 9600 tokens, 256 columns - / 165 / 200).
+// Blocks of prompts (the least tokens of one, how many of a head): one for each request, or so many that the workgroups make whole rounds of what the
+// device holds at once.  One round has the fewest states to add up and to pass on; but every request's last block is shorter than the others, which
+// leaves a part of a single round idle where a request has few blocks, so more than a third as many requests as blocks take two rounds.  Us with one
+// round / two / three, 128 columns: 16 heads (32 blocks of a round), 4 requests of up to 16000 tokens 103 / 120 / 137, 8 179 / 197 / 216, 10 237 / 238 /
+// 255, 16 417 / 357 / 369, 12 of up to 32768 468 / 456 / 472; 8 heads (64 blocks), 16 of up to 8000 121 / 139 / 148, 24 174 / 185 / 199.
 // A block is as short as one chunk while the chunks of all heads are less than about one round (three prompts of 900 tokens, 8 heads, blocks of
 // 64 / 128 / 256 tokens at least 18.1 / 20.6 / 27.3; of 2500 tokens 23.8 / 24.9 / 33.2), beyond two chunks: below that the states' traffic shows (5000
 // tokens, 16 heads 39.2 / 34.2 / 35.2).  Up to 256 tokens a block for each request: one launch (one prompt of 200: 14.7, with blocks 16.4; of 300: 17.5, 16.0).
-constexpr uint32_t kRounds = 2, kOneBlock = 256;
+constexpr uint32_t kOneBlock = 256;
 constexpr uint64_t kFewTokens = 20480;   // times heads
 constexpr uint32_t prompt_waves(uint32_t dv) { return dv <= 64 ? 4 : dv <= 128 ? 8 : dv <= 160 ? 10 : 16; }
 struct DecayBlocks {
@@ -199,7 +202,8 @@ struct DecayBlocks {
 inline DecayBlocks decay_blocks(uint64_t n, uint64_t tokens, uint32_t heads, uint32_t dk, uint32_t dv) {
     if (tokens <= kOneBlock) return {kOneBlock, (uint32_t)n, false};
     const uint32_t by_waves = 16 / prompt_waves(dv), by_lds = dk <= 64 ? 3 : 2, on_unit = by_waves < by_lds ? by_waves : by_lds;   // workgroups on a compute unit
-    uint64_t blocks = kRounds * kUnits * on_unit / heads;
+    const uint64_t round = kUnits * on_unit / heads;
+    uint64_t blocks = 3 * n <= round ? round : 2 * round;
     if (blocks < n + blocks / 2) blocks = n + blocks / 2;
     if (blocks == n) ++blocks;
     const uint64_t least = tokens * heads <= kFewTokens ? kChunk : 2 * kChunk;

@@ -68,8 +68,9 @@ WHOLE, LIST, JOIN, PROMPT, BLOCKS = "whole_attention_kernel", "paged_attention_k
     # a window bounds them too; enough segments keep the device busy with longer ones; too many would come in rounds
     ("attention(3, 1000, window=225)", [(WHOLE, 24, 512)]), ("attention(40, 80)", [(WHOLE, 320, 512)]), ("attention(400, 80)", [(LIST, 256, 256), (JOIN, 12800, 128)]),
     ("attention(3, 2, heads=1, group=16)", [(WHOLE, 3, 64)]),
-    ("decay(3, 256)", [(PROMPT, 24, 256)]), ("decay(3, 257)", [(PROMPT, 8 * 192, 256), (BLOCKS, 96, 256), (PROMPT, 8 * 192, 256)]),
-    ("decay(3, 9000, 16, 128, 128)", [(PROMPT, 1024, 512), (BLOCKS, 768, 256), (PROMPT, 1024, 512)]), ("decay(3, 0)", [(PROMPT, 24, 256)]),
+    ("decay(3, 256)", [(PROMPT, 24, 256)]), ("decay(3, 257)", [(PROMPT, 8 * 96, 256), (BLOCKS, 96, 256), (PROMPT, 8 * 96, 256)]),
+    ("decay(3, 9000, 16, 128, 128)", [(PROMPT, 512, 512), (BLOCKS, 768, 256), (PROMPT, 512, 512)]), ("decay(3, 0)", [(PROMPT, 24, 256)]),
+    ("decay(11, 9000, 16, 128, 128)", [(PROMPT, 1024, 512), (BLOCKS, 2816, 256), (PROMPT, 1024, 512)]),
     ("step(5)", [("decay_step_kernel", 40, 256)]),
 ])
 def test_launches(record, call, want):
