@@ -43,7 +43,9 @@ __device__ __forceinline__ Span span_of(const DecayParams &P, uint32_t r) {
 // ---- single tokens -------------------------------------------------------------------------------------------------
 //
 // Bound by reading and writing the state: 8 dk dv bytes for 4 dk dv operations.  A workgroup has one state; a thread takes four
-// columns (16 bytes) of every kth row, kRows of them loaded before the first is used, and the sums over the rows go through LDS.
+// columns (16 bytes) of every kth row, kRows of them loaded before the first is used, and the sums over the rows go through LDS.  States are read and
+// written past the caches: no other call needs them before the next step.  128 requests of 32 heads, 128 x 128: 101 us (through the caches 108), 5.3 TB/s;
+// 64 requests 51 (58).
 template <typename T, int kRows> __global__ __launch_bounds__(256) void decay_step_kernel(DecayParams P) {
     __shared__ float query[kMostDk], key[kMostDk];
     __shared__ __align__(16) float part[256 * 4];
@@ -97,7 +99,7 @@ template <typename T, int kRows> __global__ __launch_bounds__(256) void decay_st
 //
 // Chunks of 64 tokens on the matrix cores.  With i, j counted from the chunk's beginning, m tokens in it and S the state before it,
 //   out_i = scale (sum_(j <= i) e^(ld (i - j)) (q_i . k_j) v_j + e^(ld (i + 1)) q_i S),   S' = e^(ld m) S + sum_j e^(ld (m - 1 - j)) k_j v_j^T
-// A workgroup takes a block of a request's tokens for one head, chunk after chunk, every wave 32 columns of v, out and S, which stays
+// A workgroup takes a block of a request's tokens for one head, chunk after chunk, every wave 16 columns of v, out and S, which stays
 // in its registers (fp32).  Blocks of one request depend on each other through the state alone: for requests of several, a first
 // launch adds up what every block but the last adds to the state (kStates), a second one turns those into the state before each block, and
 // the third does all blocks at once.
@@ -105,12 +107,16 @@ template <typename T, int kRows> __global__ __launch_bounds__(256) void decay_st
 // Layout (products 16x16x32, lane = 16 g + r).  Row r of a state tile's K^T operand is key component 32 p + 8 (r / 4) + 4 t + r % 4, so that
 // a lane's parts of the tiles (p, 0) and (p, 1) are the components 32 p + 8 g + 0..7: eight consecutive ones, the state's operand in q S without
 // an exchange between lanes.  Scores are made as K Q^T: four consecutive keys of one query in a lane, one 8-byte write to LDS.
-// A lane loads two columns of eight consecutive tokens' values (from memory into registers: waves share no values) and exchanges halves: columns
-// 2 r and 2 r + 1 are column r of the wave's two tiles.
+// Pairs of lanes load two columns, four consecutive tokens' values each (from memory into registers: waves share no values), and exchange what is the
+// other's, so that each has eight tokens of its own column.
+//
+// What bounds it: vector instructions (56 % of the time of the blocks' launch; matrix ones 30 %) in phases between barriers, which two workgroups on a
+// compute unit overlap in part.  12 prompts of 63000 tokens together, 16 heads, 128 columns: 457 us (states 125, blocks 23, prompts 300 to 310; floor 161),
+// 3.6 TB/s; 3 prompts of 1000 tokens, 8 heads of 64: 17.6 us, three launches of 4 to 7.
 //
 // Rounding.  The matrix cores take 16-bit operands.  What is no 16-bit input is taken apart into bf16 terms, x = x0 + x1 + ...,
-// each the rounding of what the ones before it left (8 bits each): values times their decay into three, which is fp32's
-// 24 bits (their sums are the states, fp32 results), the state and the scores into two where they meet q and v, whose result is rounded to
+// each the upper half of what the ones before it left (8 bits), the last one rounded: values times their decay into three, which is fp32's
+// 24 bits (their sums are the states, fp32 results: 1.4e-7 off), the state and the scores into two where they meet q and v, whose result is rounded to
 // 16 bits: 2^-17 of a term, where one term alone (2^-9) would add as much error as that rounding.  Inputs in fp16 are two bf16 terms each (11 bits,
 // exact): with bf16's exponents no sum of products overflows that fp32 holds.
 constexpr uint32_t kChunk = 64;
@@ -538,7 +544,9 @@ template <int KD, int NW, typename T, bool kStates> __global__ __launch_bounds__
                 __builtin_amdgcn_raw_buffer_store_b32(__builtin_amdgcn_perm(right, left, 0x07060302u), rows, off + (t * 16 + 1) * stride, 0, 0);
             }
         }
-        __syncthreads();   // LDS is free again
+        // Keys and queries are free again.  (Without kStates that holds from the barrier above on; the scores, still read, are next written behind the next
+        // chunk's first barrier.)
+        if constexpr (kStates) __syncthreads();
     }
     float *to = kStates ? PP.block_states + slot * matrix
                         : at.block + 1 == at.blocks && P.state_out && state != ~0ull ? P.state_out + (state * P.heads + h) * matrix : nullptr;

@@ -19,8 +19,9 @@ namespace {
 //   output   O^T = V^T P^T: ... the eight that the lane holds of B here, so probabilities go from one product to the next in their
 //            registers.  A lane loads 8 components of 8 consecutive positions' values (rows of the cache, coalesced)
 //            and exchanges 16-bit halves between pairs of positions: one v_perm for two values.
-// No LDS, no barrier.  Query heads beyond the group's are zero columns: the matrix cores have the time (about a tenth of
-// what the loads take).
+// No LDS and no barrier in the loop.  Query heads beyond the group's are zero columns: the matrix cores have the time (about a tenth of
+// what the loads take).  Whole calls: 48 ragged rows of up to 8192 positions (330 MB in bf16) 67.6 us, 62 of them in the list's kernel, 5.3 TB/s;
+// 16 of up to 65536 (717 MB in e4m3) 123 us, 117 of them, 6.1 TB/s; one row of 1000 9.8 us, the lives of two launches.
 struct AttentionParams {
     const void *q, *k, *v;
     uint64_t q_stride, head_stride;                // elements
@@ -504,7 +505,7 @@ template <int KS, bool kExact, bool kStream, typename T, bool kE4m3> __global__ 
 }
 
 // Joins the parts of the segments that several waves share, and writes the rows without positions: a workgroup for a row and query head.  Its
-// kWaves waves take every kWaves-th part each, eight of them under way at a time.
+// kWaves waves take every kWaves-th part each, eight of them under way at a time.  Bound by its life: 3 to 5 us (row sums, then parts, then LDS).
 template <typename T, int kWaves> __global__ __launch_bounds__(64 * kWaves) void join_attention_kernel(AttentionParams P) {
     __shared__ float lds[kWaves][256 + 2];
     const uint32_t lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), id = blockIdx.x;

