@@ -368,7 +368,7 @@ mmv_status mmv_page_tables(uint64_t n, const int32_t *d_cached, const int32_t *d
 
 /* A paged cache of keys and values: component c of slot s of page p for head h is element
  * p * page_stride + h * head_stride + s * slot_stride + c of d_k (d_v), so that pages may hold heads by slots or slots by
- * heads.  Strides are in elements and multiples of 8 (of pages and slots below 2^31), dim is a multiple of 8, at most 256; pages * page < 2^31.  A cache of
+ * heads.  Strides are in elements and multiples of 8 (of pages below 2^31, of slots below 2^28), dim is a multiple of 8, at most 256; pages * page < 2^31.  A cache of
  * MMV_TYPE_E4M3 holds key / k_scale and value / v_scale; the scales of the others are 1. */
 typedef struct {
     void *d_k, *d_v;

@@ -139,7 +139,7 @@ template <int KS, bool kExact, bool kStream, typename T, bool kE4m3> struct Tile
             const uint32_t group = at.tile * 4, page = page_of(P, group);
             off[0] = place_of(P, scalar_load(row + page), group - page * P.page_groups.divisor, 15u);
 #pragma unroll
-            for (int i = 1; i < 4; ++i) off[i] = off[0] + (uint32_t)(8 * i) * slot_stride(P);
+            for (int i = 1; i < 4; ++i) off[i] = off[0] + (uint64_t)(8 * i) * slot_stride(P);
         } else {
             int32_t id[4];
             uint32_t inside[4];

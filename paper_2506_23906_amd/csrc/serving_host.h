@@ -43,8 +43,8 @@ inline mmv_status check_cache(const mmv_paged_cache *c, int type) {
     if (!valid_value_type(type) || (own != MMV_TYPE_E4M3 && own != type)) return MMV_ERR_INVALID_ARG;
     if (c->page < 1 || c->page > 65536 || c->heads < 1 || c->heads > kMostHeads || c->dim < 8 || c->dim > 256 || c->dim % 8) return MMV_ERR_INVALID_ARG;
     if (c->pages >= k2to31 || c->pages * c->page >= k2to31 || c->page_stride % 8 || c->head_stride % 8 || c->slot_stride % 8) return MMV_ERR_INVALID_ARG;
-    // (kernels hold the strides of pages and slots in 32 bits; heads may lie further apart)
-    if (c->page_stride >= k2to31 || c->head_stride > (1ull << 40) || c->slot_stride >= k2to31) return MMV_ERR_INVALID_ARG;
+    // (kernels hold the strides of pages and slots in 32 bits, the bytes of seven slots too; heads may lie further apart)
+    if (c->page_stride >= k2to31 || c->head_stride > (1ull << 40) || c->slot_stride >= (1ull << 28)) return MMV_ERR_INVALID_ARG;
     if (own == MMV_TYPE_E4M3 ? !(c->k_scale > 0.f && c->v_scale > 0.f && c->k_scale < INFINITY && c->v_scale < INFINITY) : !(c->k_scale == 1.f && c->v_scale == 1.f)) return MMV_ERR_INVALID_ARG;
     if (c->pages && (!c->d_k || !c->d_v)) return MMV_ERR_NULL;
     return aligned_to(c->d_k, 16) && aligned_to(c->d_v, 16) ? MMV_OK : MMV_ERR_INVALID_ARG;

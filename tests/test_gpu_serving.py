@@ -277,6 +277,26 @@ def test_attention_and_append_beyond_32_bit_offsets():
     check(out, want, by, "far pages")
 
 
+def test_attention_of_slots_that_lie_far_apart():
+    """Pages side by side, slot behind slot: 24 slots are more than 2^32 elements."""
+    heads, page, dim, pages, context = 1, 32, 64, 2_900_000, 75
+    k, v = (torch.empty(page, pages, heads, dim, dtype=torch.uint8, device="cuda").view(E4M3).permute(1, 2, 0, 3) for _ in "kv")
+    assert 24 * k.stride(2) > 2 ** 32
+    cache, table = B.PagedCache(k, v, 0.02, 0.03), [[pages - 1, 7, pages - 2]]
+    new_k, new_v = normal(1, context, heads, dim), normal(2, context, heads, dim)
+    slots = [table[0][i // page] * page + i % page for i in range(context)]
+    B.mmv_cache_append(new_k.cuda(), new_v.cuda(), ints(slots, torch.int64), cache)
+    small = torch.zeros(2, 3, heads, page, dim, dtype=torch.uint8).view(E4M3)
+    for x, s, by in ((new_k, small[0], 0.02), (new_v, small[1], 0.03)):
+        held = e4m3(x, by)
+        for t in range(context):
+            s[t // page, :, t % page] = held[t]
+    q = normal(3, 1, 4, dim)
+    out = B.mmv_paged_attention(q.cuda(), cache, ints(table), ints([context]))
+    want, _, by, _ = plain_attention(q, small[0], small[1], [[0, 1, 2]], [context], dim ** -0.5, 0, 0.02, 0.03)
+    check(out, want, by, "far slots")
+
+
 # ---- linear attention with decay ----------------------------------------------------------------------------------
 
 

@@ -39,7 +39,7 @@ def cache(k=A, v=A, type=B.MMV_TYPE_BF16, page=16, heads=2, dim=64, pages=10, st
 
 
 BAD_CACHES = [dict(page=0), dict(page=65544), dict(heads=0), dict(heads=1025), dict(dim=4), dict(dim=68), dict(dim=264), dict(pages=1 << 31), dict(pages=1 << 28), dict(strides=(2047, 1024, 64)),
-              dict(strides=(2048, 1023, 64)), dict(strides=(2048, 1024, 65)), dict(strides=(1 << 41, 1024, 64)), dict(k=A + 8), dict(v=A + 8), dict(scales=(0.5, 1.0)),
+              dict(strides=(2048, 1023, 64)), dict(strides=(2048, 1024, 65)), dict(strides=(1 << 41, 1024, 64)), dict(strides=(2048, 1024, 1 << 28)), dict(k=A + 8), dict(v=A + 8), dict(scales=(0.5, 1.0)),
               dict(type=B.MMV_TYPE_F16), dict(type=0), dict(type=7), dict(type=B.MMV_TYPE_E4M3, scales=(0.0, 1.0)), dict(type=B.MMV_TYPE_E4M3, scales=(1.0, float("inf"))),
               dict(type=B.MMV_TYPE_E4M3, scales=(1.0, float("nan")))]
 
