@@ -335,7 +335,8 @@ mmv_status mmv_gather_reference(uint64_t nnz, const float *d_val, const int32_t 
  * with these differences: lengths, tables and indices are read by the kernels alone, so that a step can be captured into a HIP
  * graph and replayed as they change, and none of them is trusted: what would lie outside an array is left out as each call
  * says.  Pointers to values are 16-byte aligned, pointers to 32- and 64-bit integers and fp32 aligned to their size; nothing is
- * read beyond the arrays.  No call here leaves anything in its workspace that a later call or mmv_workspace_status needs. */
+ * read beyond the arrays.  What a call writes overlaps nothing else that it reads or writes, but where it says so (the lengths after a step are
+ * a copy of d_context, not d_cached itself).  No call here leaves anything in its workspace that a later call or mmv_workspace_status needs. */
 typedef enum {
     MMV_TYPE_F16 = 1,
     MMV_TYPE_BF16 = 2,

@@ -111,7 +111,7 @@ template <typename T, int kRows> __global__ __launch_bounds__(256) void decay_st
 // other's, so that each has eight tokens of its own column.
 //
 // What bounds it: vector instructions (56 % of the time of the blocks' launch; matrix ones 30 %) in phases between barriers, which two workgroups on a
-// compute unit overlap in part.  12 prompts of 63000 tokens together, 16 heads, 128 columns: 457 us (states 125, blocks 23, prompts 300 to 310; floor 161),
+// compute unit overlap in part.  12 prompts of 63000 tokens together, 16 heads, 128 columns: 460 us (states 140, blocks 22, prompts 290 to 310; floor 161),
 // 3.6 TB/s; 3 prompts of 1000 tokens, 8 heads of 64: 17.6 us, three launches of 4 to 7.
 //
 // Rounding.  The matrix cores take 16-bit operands.  What is no 16-bit input is taken apart into bf16 terms, x = x0 + x1 + ...,
