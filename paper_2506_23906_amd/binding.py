@@ -572,6 +572,12 @@ def _out(out, name: str, shape: tuple, dtype: torch.dtype, device) -> torch.Tens
     return out
 
 
+def _made_current(stream):
+    """For a call on another stream than the current one: what it allocates (results, scratch) then belongs to that stream, so that no work on
+    the current one has it before or gets it while the call's kernels run."""
+    return torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream.cuda_stream)))
+
+
 def _ws(ws, nbytes: int, device) -> tuple:
     if ws is None and nbytes:
         ws = workspace(nbytes, device)
@@ -585,6 +591,9 @@ def mmv_page_tables_workspace_bytes(n: int) -> int:
 def mmv_page_tables(cached: torch.Tensor, new: torch.Tensor, free: torch.Tensor, table: torch.Tensor, page: int, max_tokens: int,
                     out: PageTables | None = None, ws: torch.Tensor | None = None, stream=None) -> PageTables:
     """Pages for the new tokens of every request (written into `table`) and the slot of every one; returns PageTables."""
+    if stream is not None:
+        with _made_current(stream):
+            return mmv_page_tables(cached, new, free, table, page, max_tokens, out, ws)
     if _marshal is not None:
         st = _marshal.page_tables(cached, new, free, table, page, max_tokens, out, ws, stream)
         if st is not None:
@@ -630,6 +639,9 @@ def mmv_paged_attention(q: torch.Tensor, cache: PagedCache, table: torch.Tensor,
                         out: torch.Tensor | None = None, lse: torch.Tensor | None = None, ws: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """Attention of one token q[r] ([rows, query heads, dim]) over the first context[r] positions of every row of the table, or the last
     `window` of them; returns out like q.  scale: dim ** -0.5 if left out; lse: fp32 [rows, query heads], filled if given."""
+    if stream is not None:
+        with _made_current(stream):
+            return mmv_paged_attention(q, cache, table, context, scale, window, out, lse, ws)
     if _marshal is not None:
         st = _marshal.paged_attention(q, cache._ref, table, context, scale, window, out, lse, ws, stream)
         if st is not None:
@@ -680,6 +692,9 @@ def mmv_decay_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, offse
                         out: torch.Tensor | None = None, ws: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """Linear attention with a decay for each head over packed requests; q [tokens, heads, dk], k [tokens, kv heads, dk], v [tokens, kv heads,
     dv], states [states, heads, dk, dv] of fp32; returns out [tokens, heads, dv].  scale: dk ** -0.5 if left out."""
+    if stream is not None:
+        with _made_current(stream):
+            return mmv_decay_attention(q, k, v, offsets, log_decay, scale, state_in, state_out, state_index, out, ws)
     if _marshal is not None:
         st = _marshal.decay_attention(q, k, v, offsets, log_decay, scale, state_in, state_out, state_index, out, ws, stream)
         if st is not None:
@@ -701,6 +716,9 @@ def mmv_decay_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_decay:
                    state_out: torch.Tensor | None = None, scale: float | None = None, state_index: torch.Tensor | None = None,
                    out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """mmv_decay_attention for one token of every request."""
+    if stream is not None:
+        with _made_current(stream):
+            return mmv_decay_step(q, k, v, log_decay, state_in, state_out, scale, state_index, out)
     if _marshal is not None:
         st = _marshal.decay_step(q, k, v, log_decay, state_in, state_out, scale, state_index, out, stream)
         if st is not None:

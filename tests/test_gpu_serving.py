@@ -433,6 +433,32 @@ def test_decay_keeps_what_is_not_finite_however_fast_the_decay():
 # ---- a step in a graph --------------------------------------------------------------------------------------------
 
 
+def test_what_a_call_on_another_stream_allocates_is_that_streams(monkeypatch):
+    """Scratch and results of a call with `stream`: allocated where its kernels run, and the same as on the current stream."""
+    made, own = [], B.workspace
+    monkeypatch.setattr(B, "workspace", lambda *a: made.append(torch.cuda.current_stream()) or own(*a))
+    side = torch.cuda.Stream()
+    n, heads, dim, page, width = 3, 2, 64, 16, 80
+    table = torch.randperm(n * width, generator=torch.Generator().manual_seed(3), dtype=torch.int64).to(torch.int32).view(n, width).cuda()
+    cache = B.PagedCache(*(normal(i, n * width, heads, page, dim).cuda() for i in (1, 2)))
+    q, k, v = (normal(i, 900, heads, dim).cuda() for i in (3, 4, 5))
+    context, offsets, ld = ints([1200, 3, 700]), ints([0, 400, 400, 900]), decays(heads).cuda()
+    many = 4000
+    cached, new, free, pages = ints([5] * many), ints([1] * many), ints([]), ints(list(range(many)))[:, None]
+    side.wait_stream(torch.cuda.current_stream())
+    for call in (lambda **s: B.mmv_paged_attention(q[:n], cache, table, context, **s), lambda **s: B.mmv_decay_attention(q, k, v, offsets, ld, **s),
+                 lambda **s: B.mmv_decay_step(q[:n], k[:n], v[:n], ld, **s),
+                 lambda **s: B.mmv_page_tables(cached, new, free, pages, page, many, **s).slots):
+        here = call()
+        torch.cuda.synchronize()
+        made.clear()
+        there = call(stream=side)
+        assert all(s == side for s in made)
+        side.synchronize()
+        assert torch.equal(here, there)
+    assert made
+
+
 def test_a_captured_step_follows_its_lengths():
     """Tables, append, attention and the single-token recurrence in one graph, replayed as the requests grow; eager work in between."""
     n, heads, group, dim, page, width = 5, 2, 4, 64, 16, 8
