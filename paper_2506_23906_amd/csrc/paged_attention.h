@@ -450,6 +450,9 @@ template <int KS, bool kExact, bool kStream, typename T, bool kE4m3> __global__ 
     }
 }
 
+// Joining parts: the largest maximum is the base, and every part counts, with weight 2^(its maximum - the base), whatever that is.  A part of scores that are no numbers has no
+// maximum (-infinity) but a sum that is none either, and 0 times that stays no number, as it does for a wave that has the whole segment; a part without positions adds zeros.
+
 // Where no segment has more tiles than a few for each of at most eight waves (four beyond 128 dims, which take more than half of a SIMD's registers): a workgroup has
 // one, and joins its waves' parts in LDS.  One launch, and no sums over the rows ahead of the first load.
 constexpr uint32_t whole_waves_most(uint32_t dim) { return dim <= 128 ? 8 : 4; }
@@ -497,7 +500,7 @@ template <int KS, bool kExact, bool kStream, typename T, bool kE4m3> __global__ 
 #pragma unroll
         for (uint32_t w = 0; w < kWholeWaves; ++w) {
             const float f = __builtin_amdgcn_exp2f(most[w] - base);
-            if (w < used && f != 0.f) total += f * ml[w][q][1], x += f * parts[w * P.group * P.dim + id];   // (a part without positions has weight 0; one that is not a number keeps it)
+            if (w < used) total += f * ml[w][q][1], x += f * parts[w * P.group * P.dim + id];
         }
         ((T *)P.out)[first * P.dim + id] = from_f32<T>(total == 0.f ? 0.f : x * (P.out_by / total));
         if (P.lse && id == q * P.dim) P.lse[first + q] = total == 0.f && top == -INFINITY ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * kLn2;
@@ -544,8 +547,8 @@ template <typename T, int kWaves> __global__ __launch_bounds__(64 * kWaves) void
         for (int c = 0; c < 4; ++c) o[c] *= by;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const float f = w0 + kWaves * i > last ? 0.f : __builtin_amdgcn_exp2f(m[i] - base);
-            if (f != 0.f) {   // (a part without positions has weight 0; one that is not a number keeps it)
+            const float f = __builtin_amdgcn_exp2f(m[i] - base);
+            if (w0 + kWaves * i <= last) {
                 sum += f * l[i];
 #pragma unroll
                 for (int c = 0; c < 4; ++c) o[c] += f * part[i][c];
@@ -565,7 +568,7 @@ template <typename T, int kWaves> __global__ __launch_bounds__(64 * kWaves) void
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) {
             const float f = __builtin_amdgcn_exp2f(lds[w][256] - base);
-            if (f != 0.f) total += f * lds[w][257], x += f * lds[w][d];
+            total += f * lds[w][257], x += f * lds[w][d];
         }
         out[d] = from_f32<T>(total == 0.f ? 0.f : x * (P.out_by / total));
         if (P.lse && d == 0) P.lse[id] = total == 0.f && top == -INFINITY ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * kLn2;
