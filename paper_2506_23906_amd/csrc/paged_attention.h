@@ -63,7 +63,8 @@ template <bool kHigh> __device__ __forceinline__ uint32_t widen(f16_t, uint32_t 
 }
 // Probabilities meet the values in 16 bits, as the matrix cores take both operands of one type.  In bf16 they are two terms, the upper 8 bits and the rounded rest
 // (16 bits together): rounded once they added as much error as the rounding of the result (1.4 times the error of exact ones; fp16, 11 bits, 1.1 to 1.2 times,
-// is left at one).  The rest is never quite zero: a value's infinity times a positive probability stays that infinity.
+// is left at one).  The rest is at least 2^-20 of the probability: a value's infinity times a positive probability stays that infinity, and what has no
+// weight adds nothing.
 template <typename T> constexpr int kTerms = __is_same(T, bf16_t) ? 2 : 1;
 template <typename T> __device__ __forceinline__ void probability_terms(float a, float b, uint32_t (&to)[kTerms<T>]) {
     if constexpr (kTerms<T> == 1) {
@@ -72,7 +73,7 @@ template <typename T> __device__ __forceinline__ void probability_terms(float a,
         const uint32_t x = __builtin_bit_cast(uint32_t, a), y = __builtin_bit_cast(uint32_t, b);
         to[0] = __builtin_amdgcn_perm(y, x, 0x07060302u);
         const float rest_a = a - __builtin_bit_cast(float, x & 0xFFFF0000u), rest_b = b - __builtin_bit_cast(float, y & 0xFFFF0000u);
-        to[1] = pack2<T>(rest_a < 1e-35f ? 1e-35f : rest_a, rest_b < 1e-35f ? 1e-35f : rest_b);
+        to[1] = pack2<T>(fmaxf(rest_a, a * 0x1p-20f), fmaxf(rest_b, b * 0x1p-20f));
     }
 }
 // Largest / sum over the four lanes that differ in g.

@@ -118,3 +118,23 @@ def test_infinite_values_reach_their_component_alone(form, dtype):
     keep[0, :4, 9] = keep[0, 4:, 3] = keep[1, 4:, 63] = False
     check(out[keep], want[keep], by[keep], "the other components")
     check(lse, want_lse, lse_by, "lse")
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("form", FORMS)
+def test_large_finite_values_without_weight_add_nothing(form, dtype):
+    """Values near the largest of the type at positions whose probability is 0 in 32 bits."""
+    print(form, dtype, flush=True)
+    k, v, table, q, contexts = case(form, dtype, dtype)
+    q[:, :, 0] = 8.0
+    for row in (0, 1):
+        put(k, table, row, 1, 0.0)
+        put(k, table, row, 1, 1000.0, dims=0)     # (exp(-900) of the others beside it)
+    want, want_lse, by, lse_by = plain_attention(q, k, v, table, contexts, 0.125, 0)
+    large = 1e35 if dtype == BF16 else 65504.0    # (times the probabilities of a part that has no other base still finite in 32 bits)
+    for row in (0, 1):
+        for p in range(3, contexts[row], 5):
+            put(v, table, row, p, large, dims=slice(7, 40))
+    out, lse = run(k, v, table, q, contexts)
+    check(out, want, by, "out")
+    check(lse, want_lse, lse_by, "lse")
