@@ -316,7 +316,7 @@ __device__ __forceinline__ void attention_run(const AttentionParams &P, Place at
             tile.load_values(P, r);
             u32x4 q[KS];
             f32x4 O[kDims];
-            float most = -INFINITY, sum = 0.f;
+            float most = -INFINITY, sum = 0.f, recent = 0.f;   // (the probabilities of up to 32 tiles are added up before they meet the rest: of small ones beside a large sum little is lost)
             bool fresh = true;
             for (;;) {
                 if (fresh) {   // a new segment: its queries
@@ -330,7 +330,7 @@ __device__ __forceinline__ void attention_run(const AttentionParams &P, Place at
                     }
     #pragma unroll
                     for (int c = 0; c < kDims; ++c) O[c] = (f32x4){0.f, 0.f, 0.f, 0.f};
-                    most = -INFINITY, sum = 0.f;
+                    most = -INFINITY, sum = 0.f, recent = 0.f;
                 }
                 f32x4 S[2];
                 tile.scores(P, q, g, S);
@@ -371,7 +371,7 @@ __device__ __forceinline__ void attention_run(const AttentionParams &P, Place at
                 if (__any(top > most + 8.f)) {
                     const float m = fmaxf(over_g_max(top), most), by = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(most - m);
                     most = m;
-                    sum *= by;
+                    sum *= by, recent *= by;
     #pragma unroll
                     for (int c = 0; c < kDims; ++c) O[c] *= by;
                 }
@@ -379,7 +379,7 @@ __device__ __forceinline__ void attention_run(const AttentionParams &P, Place at
     #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     s[i] = __builtin_amdgcn_exp2f(s[i] - base);
-                    sum += s[i];
+                    recent += s[i];
                 }
                 u32x4 p[kTerms<T>];
 #pragma unroll
@@ -392,6 +392,7 @@ __device__ __forceinline__ void attention_run(const AttentionParams &P, Place at
                 tile.add_values(p, O);
                 tile.load_values(P, r);
                 const bool ended = now.tile + 1 == now.last;
+                if (now.tile % 32 == 31 || ended || !left) sum += recent, recent = 0.f;
                 if (ended || !left) {
                     finish(now, begun, ended, most, over_g_sum(sum), O);
                     fresh = true, begun = false;

@@ -1,0 +1,39 @@
+"""The bounds of tests/serving_rounding.py notice a term that is left out.  No GPU: the mistake is planted in a plain form."""
+import pytest
+import torch
+
+import serving_rounding as R
+
+@pytest.mark.parametrize("dtype", [R.BF16, R.F16])
+@pytest.mark.parametrize("case", [R.cancelling_state, R.cancelling_scores])
+def test_states_and_scores(case, dtype):
+    *_, terms, want, by = case(dtype, 70)
+    off = [abs(float(R.split(terms, R.BF16, n).sum()) - want) for n in (1, 2)]
+    assert off[1] <= by / 4 and off[0] >= 4 * by
+
+
+@pytest.mark.parametrize("dtype", [R.BF16, R.F16])
+@pytest.mark.parametrize("tokens", [40, 700])
+def test_decayed_values(tokens, dtype):
+    *_, values, by_decay, by = R.decayed_values(dtype, tokens)
+    off = [(R.split(values * by_decay, R.BF16, n) - values * by_decay).abs() / by for n in (2, 3)]
+    assert float(off[1].max()) < 0.25 and float(off[0].max()) > 2
+
+
+def test_flat_tail_sum():
+    """Weights that one lane adds up (8 of every 32) in 32 bits: one by one beside the first one, and by 256."""
+    *_, scale, _, _, want, by = R.flat_tail(R.BF16, 1.0)
+    weights = torch.exp(torch.full((1 << 14,), -scale, dtype=torch.float64)).float()
+    weights[0] = 1.0
+    rest = 3 * (1 << 14) * float(weights[1])
+    one_by_one = torch.zeros(())
+    for w in weights:
+        one_by_one = one_by_one + w
+    by_256 = torch.zeros(())
+    for part in weights.view(-1, 256):
+        own = torch.zeros(())
+        for w in part:
+            own = own + w
+        by_256 = by_256 + own
+    off = [abs(torch.log(torch.tensor(float(x) + rest, dtype=torch.float64)).item() - want) for x in (one_by_one, by_256)]
+    assert off[0] > 4 * by and off[1] <= by
