@@ -34,7 +34,7 @@ struct AttentionParams {
     uint32_t *sums;                                // [n + 1] tiles of a head before every row, and of all
     uint32_t n, q_heads, heads, group, dim, page, pages, window, max_context, workers;
     Divider page_groups;                           // page / 8
-    float score_by, out_by;                        // scale * k_scale * log2(e), v_scale
+    float score_by, out_by;                        // scale * k_scale * log2(e), v_scale / 2^kScaleBits
 };
 constexpr uint32_t kTile = 32;                     // positions
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.693147180559945309417f;
@@ -61,20 +61,28 @@ template <bool kHigh> __device__ __forceinline__ uint32_t widen(bf16_t, uint32_t
 template <bool kHigh> __device__ __forceinline__ uint32_t widen(f16_t, uint32_t w) {
     return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)w, 1.f, kHigh));
 }
-// Probabilities meet the values in 16 bits, as the matrix cores take both operands of one type.  In bf16 they are two terms, the upper 8 bits and the rounded rest
-// (16 bits together): rounded once they added as much error as the rounding of the result (1.4 times the error of exact ones; fp16, 11 bits, 1.1 to 1.2 times,
-// is left at one).  The rest is at least 2^-20 of the probability: a value's infinity times a positive probability stays that infinity, and what has no
-// weight adds nothing.
-template <typename T> constexpr int kTerms = __is_same(T, bf16_t) ? 2 : 1;
-template <typename T> __device__ __forceinline__ void probability_terms(float a, float b, uint32_t (&to)[kTerms<T>]) {
-    if constexpr (kTerms<T> == 1) {
-        to[0] = pack2<T>(a, b);
-    } else {
-        const uint32_t x = __builtin_bit_cast(uint32_t, a), y = __builtin_bit_cast(uint32_t, b);
-        to[0] = __builtin_amdgcn_perm(y, x, 0x07060302u);
-        const float rest_a = a - __builtin_bit_cast(float, x & 0xFFFF0000u), rest_b = b - __builtin_bit_cast(float, y & 0xFFFF0000u);
-        to[1] = pack2<T>(fmaxf(rest_a, a * 0x1p-20f), fmaxf(rest_b, b * 0x1p-20f));
-    }
+// Probabilities meet the values in 16 bits, as the matrix cores take both operands of one type, and as two terms, what is cut off at the type's precision and the rounded rest:
+// 16 bits together in bf16, 22 in fp16.  Rounded once they would add as much error as the rounding of the result (1.4 times the error of exact ones in bf16, 1.2
+// times in fp16).
+// The rest is never zero beside a first term that is not (kInfinite: but for 8-bit caches, which hold no infinities): a value's infinity times a probability stays that
+// infinity, and what has no weight adds nothing.  In bf16 it is at least 2^-20 of the probability.  fp16 has few exponents: there probabilities are scaled by 2^12 (which the result's factor takes back), above a base that lies at most
+// 2^3 below them, so that the largest product's is 2^15, fp16's full precision goes down to 2^-26 of the largest probability and its least value is 2^-36 of that, which is
+// also what the rest is at least; scaled by nothing, a tail of 65536 positions at 2^-25 of one beside it (2^-9 of the result) was lost.
+template <typename T> constexpr int kScaleBits = __is_same(T, bf16_t) ? 0 : 12;
+template <typename T> constexpr float kMostAbove = __is_same(T, bf16_t) ? 8.f : 3.f;   // of a score above the base, in bits
+template <bool kInfinite> __device__ __forceinline__ void probability_terms(bf16_t, float a, float b, uint32_t (&to)[2]) {
+    const uint32_t x = __builtin_bit_cast(uint32_t, a), y = __builtin_bit_cast(uint32_t, b);
+    to[0] = __builtin_amdgcn_perm(y, x, 0x07060302u);
+    const float rest_a = a - __builtin_bit_cast(float, x & 0xFFFF0000u), rest_b = b - __builtin_bit_cast(float, y & 0xFFFF0000u);
+    to[1] = kInfinite ? pack2<bf16_t>(fmaxf(rest_a, a * 0x1p-20f), fmaxf(rest_b, b * 0x1p-20f)) : pack2<bf16_t>(rest_a, rest_b);
+}
+template <bool kInfinite> __device__ __forceinline__ void probability_terms(f16_t, float a, float b, uint32_t (&to)[2]) {
+    typedef f16_t pair __attribute__((ext_vector_type(2)));
+    a *= 0x1p12f, b *= 0x1p12f;
+    to[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(a, b));
+    const pair cut = __builtin_bit_cast(pair, to[0]);
+    const float cut_a = (float)cut[0], cut_b = (float)cut[1];
+    to[1] = kInfinite ? pack2<f16_t>(fmaxf(a - cut_a, fminf(cut_a, 0x1p-24f)), fmaxf(b - cut_b, fminf(cut_b, 0x1p-24f))) : pack2<f16_t>(a - cut_a, b - cut_b);
 }
 // Largest / sum over the four lanes that differ in g.
 __device__ __forceinline__ float over_g_max(float v) {
@@ -259,11 +267,11 @@ template <int KS, bool kExact, bool kStream, typename T, bool kE4m3> struct Tile
         }
         return a;
     }
-    template <int c = 0> __device__ __forceinline__ void add_values(const u32x4 (&p)[kTerms<T>], f32x4 (&O)[kDims]) const {
+    template <int c = 0> __device__ __forceinline__ void add_values(const u32x4 (&p)[2], f32x4 (&O)[kDims]) const {
         if constexpr (c < kDims) {
             const u32x4 a = column<c>();
 #pragma unroll
-            for (int i = 0; i < kTerms<T>; ++i) O[c] = mfma_16x16x32(T(), a, p[i], O[c]);
+            for (int i = 0; i < 2; ++i) O[c] = mfma_16x16x32(T(), a, p[i], O[c]);
             add_values<c + 1>(p, O);
         }
     }
@@ -367,8 +375,8 @@ __device__ __forceinline__ void attention_run(const AttentionParams &P, Place at
                 tile.find(P, at, g, r);   // (behind the run's last tile: that one again, not used)
                 tile.load_keys(P, g);
                 float top = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
-                // Scores up to 2^8 above the base need no new one (nothing overflows: 16-bit floats reach 2^15).
-                if (__any(top > most + 8.f)) {
+                // Scores a few bits above the base need no new one (nothing overflows: 16-bit floats reach 2^15).
+                if (__any(top > most + kMostAbove<T>)) {
                     const float m = fmaxf(over_g_max(top), most), by = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(most - m);
                     most = m;
                     sum *= by, recent *= by;
@@ -381,13 +389,12 @@ __device__ __forceinline__ void attention_run(const AttentionParams &P, Place at
                     s[i] = __builtin_amdgcn_exp2f(s[i] - base);
                     recent += s[i];
                 }
-                u32x4 p[kTerms<T>];
+                u32x4 p[2];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    uint32_t terms[kTerms<T>];
-                    probability_terms<T>(s[2 * i], s[2 * i + 1], terms);
-#pragma unroll
-                    for (int t = 0; t < kTerms<T>; ++t) p[t][i] = terms[t];
+                    uint32_t terms[2];
+                    probability_terms<!kE4m3>(T(), s[2 * i], s[2 * i + 1], terms);
+                    p[0][i] = terms[0], p[1][i] = terms[1];
                 }
                 tile.add_values(p, O);
                 tile.load_values(P, r);

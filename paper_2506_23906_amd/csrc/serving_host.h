@@ -150,6 +150,7 @@ mmv_status attention_call(AttentionParams P, int type, int cache_type, void *d_w
     P.sums = (uint32_t *)d_ws, P.part_ml = (float *)((char *)d_ws + L.ml), P.part_out = (float *)((char *)d_ws + L.out);
     P.workers = attention_workers(P.n, P.heads, P.dim, P.max_context, e4m3);
     P.page_groups = divider(P.page / 8);
+    P.out_by *= type == MMV_TYPE_F16 ? 1.f / (1 << kScaleBits<f16_t>) : 1.f;
     if (type == MMV_TYPE_F16) e4m3 ? launch_attention_over<f16_t, true>(P, s) : launch_attention_over<f16_t, false>(P, s);
     else e4m3 ? launch_attention_over<bf16_t, true>(P, s) : launch_attention_over<bf16_t, false>(P, s);
     if (const mmv_status st = launched()) return st;

@@ -17,6 +17,15 @@ def close(got, want, by, what):
     assert bool((off <= by).all()), "%s: %.3g off, bound %.3g" % (what, float(off.max()), float(torch.as_tensor(by).max()))
 
 
+@pytest.mark.parametrize("columns", [4, 900])   # a workgroup for the segment, the list of tiles
+@pytest.mark.parametrize("dtype,cache_type", [(R.BF16, R.BF16), (R.F16, R.F16), (R.BF16, R.E4M3), (R.F16, R.E4M3)])
+def test_probabilities(dtype, cache_type, columns):
+    print(dtype, cache_type, columns, flush=True)
+    q, k, v, scale, weights, values, want, by = R.cancelling_probabilities(dtype, cache_type)
+    out = B.mmv_paged_attention(q.cuda(), B.PagedCache(k.cuda(), v.cuda()), ints([[0, 1, 2, 3] + [-1] * (columns - 4)]), ints([61]), scale=scale)
+    close(out, want, by, "out")
+
+
 @pytest.mark.parametrize("dtype", [R.BF16, R.F16])
 def test_a_flat_tail_counts_in_the_sum(dtype):
     """4096 rows, so that a wave has whole rows of 65536 positions."""
@@ -27,6 +36,18 @@ def test_a_flat_tail_counts_in_the_sum(dtype):
     lse = torch.empty(n, 1, device="cuda")
     B.mmv_paged_attention(q.expand(n, 1, 8).contiguous().cuda(), B.PagedCache(k.cuda(), v.cuda()), table, torch.full((n,), 1 << 16, dtype=torch.int32, device="cuda"), scale=scale, lse=lse)
     close(lse, want_lse, lse_by, "lse")
+
+
+@pytest.mark.parametrize("dtype", [R.BF16, R.F16])
+@pytest.mark.parametrize("first_value", [0.0, 1.0])
+def test_a_flat_tail_keeps_its_weight(first_value, dtype):
+    """4096 rows, so that a wave has whole rows of 65536 positions."""
+    q, k, v, scale, want, by, _, _ = R.flat_tail(dtype, first_value)
+    n, pages = 4096, (1 << 16) // 16
+    table = torch.ones(n, pages, dtype=torch.int32, device="cuda")
+    table[:, 0] = 0
+    out = B.mmv_paged_attention(q.expand(n, 1, 8).contiguous().cuda(), B.PagedCache(k.cuda(), v.cuda()), table, torch.full((n,), 1 << 16, dtype=torch.int32, device="cuda"), scale=scale)
+    close(out, want, by, "out")
 
 
 @pytest.mark.parametrize("dtype", [R.BF16, R.F16])

@@ -4,6 +4,16 @@ import torch
 
 import serving_rounding as R
 
+TYPES = [(R.BF16, R.BF16), (R.F16, R.F16), (R.BF16, R.E4M3), (R.F16, R.E4M3)]
+
+
+@pytest.mark.parametrize("dtype,cache_type", TYPES)
+def test_probabilities(dtype, cache_type):
+    *_, weights, values, want, by = R.cancelling_probabilities(dtype, cache_type)
+    off = [abs(float(R.split(weights, dtype, terms) @ values / weights.sum()) - want) for terms in (1, 2)]
+    assert off[1] <= by / 4 and off[0] >= 4 * by
+
+
 @pytest.mark.parametrize("dtype", [R.BF16, R.F16])
 @pytest.mark.parametrize("case", [R.cancelling_state, R.cancelling_scores])
 def test_states_and_scores(case, dtype):
@@ -18,6 +28,15 @@ def test_decayed_values(tokens, dtype):
     *_, values, by_decay, by = R.decayed_values(dtype, tokens)
     off = [(R.split(values * by_decay, R.BF16, n) - values * by_decay).abs() / by for n in (2, 3)]
     assert float(off[1].max()) < 0.25 and float(off[0].max()) > 2
+
+
+@pytest.mark.parametrize("first_value", [0.0, 1.0])
+def test_flat_tail(first_value):
+    """Probabilities as multiples of fp16's least value, with the largest at 1 and at 2^12."""
+    *_, scale, want, by, _, _ = R.flat_tail(R.F16, first_value)
+    n, p = (1 << 16) - 1, torch.exp(torch.tensor(-scale, dtype=torch.float64))
+    got = [(first_value + n * float((p * 2.0 ** up).to(R.F16)) * 2.0 ** -up) / (1 + n * float(p)) for up in (0, 12)]
+    assert abs(got[1] - want) <= by / 2 and abs(got[0] - want) > by
 
 
 def test_flat_tail_sum():
