@@ -65,12 +65,13 @@ def split(fused: torch.Tensor, shape: Shape, kv: int):
 
 
 class Server:
-    """Caches, states, tables and workspaces of up to `requests` requests of up to `longest` positions, and the steps on them."""
+    """Caches, states, tables and workspaces of up to `requests` requests of up to `longest` positions (in whole pages), and the steps on them.  A request that steps past them keeps
+    its pages and takes no others': its further tokens have no place in the cache, and see the positions that have."""
 
     def __init__(self, shape: Shape, w: dict, requests: int, longest: int, device="cuda"):
         self.shape, self.w, self.n, self.device = shape, w, requests, device
         self.columns = -(-longest // shape.page)
-        pages = requests * self.columns
+        pages = requests * (self.columns + 1)    # (a full request asks for one more in a step, at the end of a page; it is not given, but those behind it in the list go to the others)
         scale = shape.scale if shape.cache == torch.float8_e4m3fn else 1.0
 
         def cache():
@@ -81,6 +82,8 @@ class Server:
         self.states = [None if i % 2 == 0 else torch.zeros(requests, shape.heads, shape.dim, shape.dim, device=device) for i in range(shape.layers)]
         self.table = torch.full((requests, self.columns), -1, dtype=torch.int32, device=device)
         self.free = torch.randperm(pages, generator=torch.Generator().manual_seed(1)).int().to(device)
+        self.after = torch.empty_like(self.free)
+        self.selected = torch.zeros(1, dtype=torch.int64, device=device)
         self.cached = torch.zeros(requests, dtype=torch.int32, device=device)
         self.one_each = torch.ones(requests, dtype=torch.int32, device=device)
         self.next = torch.zeros(requests, dtype=torch.int64, device=device)      # every request's newest token, which has no key and value yet
@@ -97,9 +100,17 @@ class Server:
         return B.mmv_page_tables(self.cached, new, self.free, self.table, self.shape.page, tokens, ws=ws)
 
     def _took(self, tables):
-        """The pages that are used up leave the list of free ones; the new tokens are cached ones."""
-        at = torch.arange(self.free.numel(), device=self.device) + tables.used[0]
-        self.free.copy_(self.free[at.clamp(max=self.free.numel() - 1)])
+        """Free pages that are in the table now leave the list, the others move up (-1 behind them: no page); the new tokens are cached ones."""
+        pages = self.free.numel()
+        gone = torch.zeros(pages + 1, dtype=torch.uint8, device=self.device)
+        gone.scatter_(0, torch.where(self.table >= 0, self.table, pages).flatten().long(), 1)
+        gone[pages:].fill_(1)
+        free = 1 - gone[torch.where(self.free >= 0, self.free, pages).long()]
+        if "free" not in self._kept:
+            self._kept["free"] = B.new_workspace(B.MMV_OP_COMPRESS, B.MMV_I8_I32, B.MMV_FLAGS_U8, pages, self.device)
+        self.after.fill_(-1)
+        B.mmv_compress(self.free, free, pages, out=self.after, count=self.selected, ws=self._kept["free"])
+        self.free.copy_(self.after)
         self.cached.copy_(tables.context)
 
     def _layers(self, tokens, tables, table, context, recurrence):
@@ -117,9 +128,11 @@ class Server:
         return x
 
     def prompts(self, tokens: torch.Tensor, lengths: torch.Tensor) -> torch.Tensor:
-        """The packed tokens of all requests' prompts (none of them empty); returns every token's hidden state.  A token attends to those before it as a row
-        of its own."""
+        """The packed tokens of all requests' prompts (none of them empty, none that does not fit behind what is cached); returns every token's hidden state.  A token attends to
+        those before it as a row of its own."""
         count, shape = tokens.numel(), self.shape
+        if int((self.cached + lengths).max()) > self.columns * shape.page:
+            raise ValueError("a prompt is longer than the pages of a request")
         tables = self._tables(lengths, count)
         request = torch.searchsorted(tables.offsets[1:].contiguous(), torch.arange(count, dtype=torch.int32, device=self.device), right=True)
 
