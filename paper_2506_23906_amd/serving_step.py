@@ -91,6 +91,7 @@ class Server:
         self._kept = {}
 
     def _workspace(self, key, nbytes):
+        """Scratch by its use; one that a step uses is never asked for in another size, since a captured step goes on using it."""
         if key not in self._kept or self._kept[key].numel() < nbytes:
             self._kept[key] = B.workspace(nbytes, self.device)
         return self._kept[key]
@@ -113,7 +114,7 @@ class Server:
         self.free.copy_(self.after)
         self.cached.copy_(tables.context)
 
-    def _layers(self, tokens, tables, table, context, recurrence):
+    def _layers(self, use, tokens, tables, table, context, recurrence):
         shape, x = self.shape, self.w["embedding"][tokens]
         for i in range(shape.layers):
             kv = shape.kv_heads if i % 2 == 0 else shape.heads
@@ -121,7 +122,7 @@ class Server:
             if i % 2 == 0:
                 B.mmv_cache_append(k, v, tables.slots, self.caches[i])
                 nbytes = B.mmv_paged_attention_workspace_bytes(q.shape[0], shape.heads, kv, shape.dim, self.columns * shape.page)
-                o = B.mmv_paged_attention(q, self.caches[i], table, context, ws=self._workspace("attention", nbytes))
+                o = B.mmv_paged_attention(q, self.caches[i], table, context, ws=self._workspace("attention of " + use, nbytes))
             else:
                 o = recurrence(q, k, v, self.states[i])
             x = x + o.flatten(1) @ self.w["out"][i]
@@ -137,10 +138,10 @@ class Server:
         request = torch.searchsorted(tables.offsets[1:].contiguous(), torch.arange(count, dtype=torch.int32, device=self.device), right=True)
 
         def recurrence(q, k, v, state):
-            ws = self._workspace("prompts", B.mmv_decay_attention_workspace_bytes(self.n, count, shape.heads, shape.dim, shape.dim))
+            ws = self._workspace("recurrence of prompts", B.mmv_decay_attention_workspace_bytes(self.n, count, shape.heads, shape.dim, shape.dim))
             return B.mmv_decay_attention(q, k, v, tables.offsets, self.w["decay"], state_in=state, state_out=state, ws=ws)
 
-        x = self._layers(tokens, tables, self.table[request], tables.positions + 1, recurrence)
+        x = self._layers("prompts", tokens, tables, self.table[request], tables.positions + 1, recurrence)
         self.next.copy_((x[tables.offsets[1:].long() - 1] @ self.w["embedding"].T).argmax(-1))
         self._took(tables)
         return x
@@ -148,7 +149,7 @@ class Server:
     def step(self) -> torch.Tensor:
         """One more token for every request; returns the hidden states, and leaves the next tokens in `next`."""
         tables = self._tables(self.one_each, self.n)
-        x = self._layers(self.next, tables, self.table, tables.context,
+        x = self._layers("a step", self.next, tables, self.table, tables.context,
                          lambda q, k, v, state: B.mmv_decay_step(q, k, v, self.w["decay"], state, state))
         self.next.copy_((x @ self.w["embedding"].T).argmax(-1))
         self._took(tables)

@@ -39,3 +39,22 @@ def test_replays_of_requests_past_the_longest():
         torch.ones(1000, device="cuda").sum().item()
     held = a.table[a.table >= 0].tolist()
     assert len(held) == len(set(held)) == 12 and a.cached.tolist() == [47, 25, 33, 40]
+
+
+def test_replays_after_longer_prompts():
+    """Prompts of many more tokens than before come in between a captured step and its replays; what they were given is given back to the allocator and written over."""
+    a, b = servers(3, 200, layers=4)
+    for s in (a, b):
+        give(s, [2, 1, 1], 1)
+        s.step()
+    a.capture()
+    for i in range(6):
+        if i % 2 == 0:
+            for s in (a, b):
+                give(s, [10 + 20 * i, 20, 9], 2 + i)
+            taken = [torch.full((1 << 20,), 0xFF, dtype=torch.uint8, device="cuda") for _ in range(32)]
+            del taken
+            b.next.copy_(a.next)
+        x, y = a.replay().clone(), b.step()
+        b.next.copy_(a.next)
+        same(a, b, x, y, i)

@@ -86,3 +86,15 @@ def test_the_free_pages_keep_their_order(calls):
     for _ in range(8):
         s.step()
     assert s.free.tolist() == first[9:] + [-1] * 9
+
+
+def test_a_steps_scratch_is_its_own(calls):
+    """A captured step goes on using the scratch it was recorded with: prompts of more tokens may not replace it."""
+    s = server(3, 80)
+    prompts(s, [2, 1, 1])
+    s.step()
+    own = calls.scratch[-1]
+    prompts(s, [30, 20, 9])
+    assert calls.scratch[-1].numel() >= 59000
+    s.step()
+    assert calls.scratch[-1] is own
