@@ -400,7 +400,7 @@ mmv_status mmv_cache_append(uint64_t tokens, const void *d_k, uint64_t k_stride,
  * row's largest count as 0.  A query that is not a number, and a key that is none for all the queries that read it, make out and lse not a number.  An infinite
  * value makes its component that infinity, or not a number if its probability is below 2^-36 (fp16), 2^-100 (bf16) of the largest.  Before they are divided by their
  * sum, probabilities are up to 2^8 times what they end as: sums of bf16 values near 2^120 overflow.
- *   q_heads a multiple of the cache's heads, at most 16 times; page a multiple of 8; n * heads * table_width * page / 32 < 2^32.
+ *   n < 2^22, n * q_heads < 2^31, q_heads a multiple of the cache's heads, at most 16 times; n * heads * table_width * page / 32 < 2^32; page a multiple of 8.
  *   d_ws        mmv_paged_attention_workspace_bytes(n, q_heads, heads, dim, table_width * page) bytes */
 size_t mmv_paged_attention_workspace_bytes(uint64_t n, uint32_t q_heads, uint32_t heads, uint32_t dim, uint64_t max_context);
 mmv_status mmv_paged_attention(uint64_t n, uint32_t q_heads, const void *d_q, uint64_t q_stride, mmv_type type,
@@ -421,7 +421,7 @@ mmv_status mmv_paged_attention(uint64_t n, uint32_t q_heads, const void *d_q, ui
  *   d_state_index  n int32: which of the states is the request's; NULL: the r-th.  A request whose index is outside has
  *               none: it starts from zeros, and its state is not kept.  No two requests share one.
  *   d_out       tokens * heads * dv of `type`
- * States are fp32 throughout.  dk and dv are multiples of 8, dk <= 128, dv <= 256; heads, kv_heads <= 1024; strides are multiples of 8, at most
+ * States are fp32 throughout.  n < 2^22, n * heads < 2^31, tokens < 2^31; dk and dv are multiples of 8, dk <= 128, dv <= 256; heads, kv_heads <= 1024; strides are multiples of 8, at most
  * 2^24.  An infinity in a key or value makes the state's entries that it enters infinite or NaN, and what they enter; no earlier token and no
  * other request or head. */
 size_t mmv_decay_attention_workspace_bytes(uint64_t n, uint64_t tokens, uint32_t heads, uint32_t dk, uint32_t dv);

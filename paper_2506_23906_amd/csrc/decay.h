@@ -15,6 +15,7 @@ struct DecayParams {
     uint64_t states;
     void *out;
     uint32_t n, heads, group, dk, dv;
+    uint32_t first;                                  // request of a step's launch
     float scale;
 };
 constexpr uint32_t kMostDk = 128, kMostDv = 256;
@@ -49,7 +50,7 @@ __device__ __forceinline__ Span span_of(const DecayParams &P, uint32_t r) {
 template <typename T, int kRows> __global__ __launch_bounds__(256) void decay_step_kernel(DecayParams P) {
     __shared__ float query[kMostDk], key[kMostDk];
     __shared__ __align__(16) float part[256 * 4];
-    const uint32_t r = blockIdx.x / P.heads, h = blockIdx.x % P.heads, tid = threadIdx.x, kv = h / P.group;
+    const uint32_t r = P.first + blockIdx.x / P.heads, h = blockIdx.x % P.heads, tid = threadIdx.x, kv = h / P.group;
     const uint64_t state = state_of(P, r), at = (state * P.heads + h) * ((uint64_t)P.dk * P.dv);
     const bool have = state != ~0ull;
     const uint32_t quads = P.dv / 4, step = 256 / quads, first = tid / quads, c = (tid - first * quads) * 4;   // (threads beyond step * quads have no rows)
@@ -126,6 +127,7 @@ struct PromptParams {
     float *block_states;    // [blocks * heads][dk * dv]
     uint32_t block;         // tokens (a multiple of kChunk) at least
     uint32_t blocks;        // of one head: as many as there is room for, at least one for each request
+    uint32_t first_block, first_request;   // of a launch
 };
 
 __device__ __forceinline__ f32x4 mfma_bf16(u32x4 a, u32x4 b, f32x4 c) { return mfma_16x16x32(bf16_t(), a, b, c); }
@@ -245,7 +247,7 @@ template <int KD, int NW, typename T, bool kStates> __global__ __launch_bounds__
     __shared__ __align__(16) float by_row[kChunk], by_token[kChunk];   // scale e^(ld (i + 1)); the tokens' decay up to the chunk's end (kStates: the block's)
     const DecayParams &P = PP.d;
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), g = lane >> 4, r = lane & 15;
-    const uint32_t number = uniform(blockIdx.x / P.heads), h = uniform(blockIdx.x - number * P.heads), kv = uniform(h / P.group);
+    const uint32_t in_launch = uniform(blockIdx.x / P.heads), h = uniform(blockIdx.x - in_launch * P.heads), kv = uniform(h / P.group), number = PP.first_block + in_launch;
     const uint64_t slot = (uint64_t)number * P.heads + h;
     const uint32_t block = choose_block(PP);
     const BlockPlace at = find_block(P, block, number);
@@ -565,7 +567,7 @@ template <int KD, int NW, typename T, bool kStates> __global__ __launch_bounds__
 __global__ __launch_bounds__(256) void decay_blocks_kernel(PromptParams PP) {
     const DecayParams &P = PP.d;
     const uint64_t matrix = (uint64_t)P.dk * P.dv;
-    const uint32_t slices = (uint32_t)((matrix + 1023) / 1024), slice = blockIdx.x % slices, h = blockIdx.x / slices % P.heads, request = blockIdx.x / slices / P.heads;
+    const uint32_t slices = (uint32_t)((matrix + 1023) / 1024), slice = blockIdx.x % slices, h = blockIdx.x / slices % P.heads, request = PP.first_request + blockIdx.x / slices / P.heads;
     const uint32_t block = choose_block(PP), blocks = blocks_of(span_of(P, request), block);
     if (blocks == 1) return;
     uint32_t mine = 0;   // blocks before this request's

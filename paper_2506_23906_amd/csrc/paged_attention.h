@@ -33,6 +33,7 @@ struct AttentionParams {
     float *part_out, *part_ml;                     // [2 * workers][group][dim], [2 * workers][group][2]
     uint32_t *sums;                                // [n + 1] tiles of a head before every row, and of all
     uint32_t n, q_heads, heads, group, dim, page, pages, window, max_context, workers;
+    uint32_t first_row;                            // of a joining launch
     Divider page_groups;                           // page / 8
     float score_by, out_by;                        // scale * k_scale * log2(e), v_scale / 2^kScaleBits
 };
@@ -520,7 +521,7 @@ template <int KS, bool kExact, bool kStream, typename T, bool kE4m3> __global__ 
 // kWaves waves take every kWaves-th part each, eight of them under way at a time.  Bound by its life: 3 to 5 us (row sums, then parts, then LDS).
 template <typename T, int kWaves> __global__ __launch_bounds__(64 * kWaves) void join_attention_kernel(AttentionParams P) {
     __shared__ float lds[kWaves][256 + 2];
-    const uint32_t lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), id = blockIdx.x;
+    const uint32_t lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), id = P.first_row * P.q_heads + blockIdx.x;
     const uint32_t row = id / P.q_heads, qh = id - row * P.q_heads, h = qh / P.group, q = qh - h * P.group;
     const uint32_t before = (uint32_t)scalar_load((const int32_t *)P.sums + row), behind = (uint32_t)scalar_load((const int32_t *)P.sums + row + 1);
     const uint32_t all = (uint32_t)scalar_load((const int32_t *)P.sums + P.n) * P.heads, tiles = behind - before;

@@ -13,6 +13,8 @@ inline uint64_t ceil_div(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
 inline size_t round256(size_t b) { return (b + 255) & ~(size_t)255; }
 inline bool aligned_to(const void *p, uintptr_t by) { return (uintptr_t)p % by == 0; }
 inline mmv_status launched() { return hipGetLastError() == hipSuccess ? MMV_OK : MMV_ERR_HIP; }
+// A launch has fewer than 2^32 threads: so many rows (requests, blocks) of `each` workgroups go into one.
+inline uint32_t most_of_a_launch(uint32_t threads, uint64_t each) { return (uint32_t)(((1ull << 32) - 1) / threads / each); }
 inline bool valid_value_type(int t) { return t == MMV_TYPE_F16 || t == MMV_TYPE_BF16; }
 inline mmv_status check_workspace(const void *ws, size_t bytes, size_t needed) {
     if (!needed) return MMV_OK;
@@ -138,10 +140,17 @@ template <typename T, bool kE4m3> void launch_attention_over(const AttentionPara
 // 17.2, 7 of 32 24.9 and 17.0.
 constexpr uint32_t kManyJoins = 1280;
 
-template <typename T> void launch_join(const AttentionParams &P, hipStream_t s) {
-    const uint32_t blocks = P.n * P.q_heads;
-    if (blocks > kManyJoins) join_attention_kernel<T, 2><<<blocks, 128, 0, s>>>(P);
-    else join_attention_kernel<T, 4><<<blocks, 256, 0, s>>>(P);
+template <typename T> mmv_status launch_join(AttentionParams P, hipStream_t s) {
+    if (P.n * P.q_heads <= kManyJoins) {
+        join_attention_kernel<T, 4><<<P.n * P.q_heads, 256, 0, s>>>(P);
+        return launched();
+    }
+    const uint32_t most = most_of_a_launch(128, P.q_heads);
+    for (; P.first_row < P.n; P.first_row += most) {
+        join_attention_kernel<T, 2><<<(P.n - P.first_row < most ? P.n - P.first_row : most) * P.q_heads, 128, 0, s>>>(P);
+        if (const mmv_status st = launched()) return st;
+    }
+    return MMV_OK;
 }
 
 mmv_status attention_call(AttentionParams P, int type, int cache_type, void *d_ws, hipStream_t s) {
@@ -155,9 +164,7 @@ mmv_status attention_call(AttentionParams P, int type, int cache_type, void *d_w
     else e4m3 ? launch_attention_over<bf16_t, true>(P, s) : launch_attention_over<bf16_t, false>(P, s);
     if (const mmv_status st = launched()) return st;
     if (whole_waves(P)) return MMV_OK;   // (nothing to join)
-    if (type == MMV_TYPE_F16) launch_join<f16_t>(P, s);
-    else launch_join<bf16_t>(P, s);
-    return launched();
+    return type == MMV_TYPE_F16 ? launch_join<f16_t>(P, s) : launch_join<bf16_t>(P, s);
 }
 
 inline bool decay_sizes(uint64_t n, uint64_t tokens, uint32_t heads, uint32_t kv_heads, uint32_t dk, uint32_t dv) {
@@ -219,20 +226,28 @@ inline size_t decay_workspace(uint64_t n, uint64_t tokens, uint32_t heads, uint3
     const DecayBlocks b = decay_blocks(n, tokens, heads, dk, dv);
     return b.split ? round256((size_t)b.blocks * heads * dk * dv * 4) : 0;
 }
-template <int KD, int NW, typename T> mmv_status launch_prompts(const PromptParams &P, hipStream_t s) {
-    const DecayParams &d = P.d;
-    const uint64_t groups = (uint64_t)P.blocks * d.heads;
-    if (groups >= k2to31) return MMV_ERR_INVALID_ARG;
-    if (P.block_states) {
-        decay_prompt_kernel<KD, NW, T, true><<<(unsigned)groups, 64 * NW, 0, s>>>(P);
-        if (const mmv_status st = launched()) return st;
-        const uint64_t slices = ceil_div((uint64_t)d.dk * d.dv, 1024) * d.heads * d.n;
-        if (slices >= k2to31) return MMV_ERR_INVALID_ARG;
-        decay_blocks_kernel<<<(unsigned)slices, 256, 0, s>>>(P);
+template <int KD, int NW, typename T, bool kStates> mmv_status launch_blocks(PromptParams P, hipStream_t s) {
+    const uint32_t most = most_of_a_launch(64 * NW, P.d.heads);
+    for (; P.first_block < P.blocks; P.first_block += most) {
+        decay_prompt_kernel<KD, NW, T, kStates><<<(P.blocks - P.first_block < most ? P.blocks - P.first_block : most) * P.d.heads, 64 * NW, 0, s>>>(P);
         if (const mmv_status st = launched()) return st;
     }
-    decay_prompt_kernel<KD, NW, T, false><<<(unsigned)groups, 64 * NW, 0, s>>>(P);
-    return launched();
+    return MMV_OK;
+}
+inline mmv_status launch_block_states(PromptParams P, hipStream_t s) {
+    const uint32_t each = (uint32_t)ceil_div((uint64_t)P.d.dk * P.d.dv, 1024) * P.d.heads, most = most_of_a_launch(256, each);
+    for (; P.first_request < P.d.n; P.first_request += most) {
+        decay_blocks_kernel<<<(P.d.n - P.first_request < most ? P.d.n - P.first_request : most) * each, 256, 0, s>>>(P);
+        if (const mmv_status st = launched()) return st;
+    }
+    return MMV_OK;
+}
+template <int KD, int NW, typename T> mmv_status launch_prompts(const PromptParams &P, hipStream_t s) {
+    if (P.block_states) {
+        if (const mmv_status st = launch_blocks<KD, NW, T, true>(P, s)) return st;
+        if (const mmv_status st = launch_block_states(P, s)) return st;
+    }
+    return launch_blocks<KD, NW, T, false>(P, s);
 }
 template <int KD, typename T> mmv_status launch_prompts_of(const PromptParams &P, hipStream_t s) {
     switch (prompt_waves(P.d.dv)) {
@@ -251,16 +266,17 @@ mmv_status decay_call(const DecayParams &d, int type, void *d_ws, hipStream_t s)
     if (type == MMV_TYPE_F16) return d.dk <= 64 ? launch_prompts_of<2, f16_t>(P, s) : launch_prompts_of<4, f16_t>(P, s);
     return d.dk <= 64 ? launch_prompts_of<2, bf16_t>(P, s) : d.dk <= 96 ? launch_prompts_of<3, bf16_t>(P, s) : launch_prompts_of<4, bf16_t>(P, s);
 }
-template <typename T> void launch_step(const DecayParams &P, hipStream_t s) {
-    const uint32_t rows = (uint32_t)ceil_div(P.dk, 256 / (P.dv / 4));   // of a thread
-    if (rows <= 4) decay_step_kernel<T, 4><<<P.n * P.heads, 256, 0, s>>>(P);
-    else if (rows <= 8) decay_step_kernel<T, 8><<<P.n * P.heads, 256, 0, s>>>(P);
-    else decay_step_kernel<T, 16><<<P.n * P.heads, 256, 0, s>>>(P);
+template <typename T> mmv_status launch_step(DecayParams P, hipStream_t s) {
+    const uint32_t rows = (uint32_t)ceil_div(P.dk, 256 / (P.dv / 4)), most = most_of_a_launch(256, P.heads);   // rows: of a thread
+    for (; P.first < P.n; P.first += most) {
+        const uint32_t blocks = (P.n - P.first < most ? P.n - P.first : most) * P.heads;
+        if (rows <= 4) decay_step_kernel<T, 4><<<blocks, 256, 0, s>>>(P);
+        else if (rows <= 8) decay_step_kernel<T, 8><<<blocks, 256, 0, s>>>(P);
+        else decay_step_kernel<T, 16><<<blocks, 256, 0, s>>>(P);
+        if (const mmv_status st = launched()) return st;
+    }
+    return MMV_OK;
 }
-mmv_status decay_step_call(const DecayParams &P, int type, hipStream_t s) {
-    if (type == MMV_TYPE_F16) launch_step<f16_t>(P, s);
-    else launch_step<bf16_t>(P, s);
-    return launched();
-}
+mmv_status decay_step_call(const DecayParams &P, int type, hipStream_t s) { return type == MMV_TYPE_F16 ? launch_step<f16_t>(P, s) : launch_step<bf16_t>(P, s); }
 
 }  // namespace
