@@ -369,7 +369,7 @@ mmv_status mmv_page_tables(uint64_t n, const int32_t *d_cached, const int32_t *d
 
 /* A paged cache of keys and values: component c of slot s of page p for head h is element
  * p * page_stride + h * head_stride + s * slot_stride + c of d_k (d_v), so that pages may hold heads by slots or slots by
- * heads.  Strides are in elements and multiples of 8 (of pages below 2^31, of slots below 2^28), dim is a multiple of 8, at most 256; pages * page < 2^31.  A cache of
+ * heads.  Tables and append take pages of any size, attention those of a multiple of 8 slots.  Strides are in elements and multiples of 8 (of pages below 2^31, of slots below 2^28), dim is a multiple of 8, at most 256; pages * page < 2^31.  A cache of
  * MMV_TYPE_E4M3 holds key / k_scale and value / v_scale; the scales of the others are 1. */
 typedef struct {
     void *d_k, *d_v;
@@ -400,7 +400,8 @@ mmv_status mmv_cache_append(uint64_t tokens, const void *d_k, uint64_t k_stride,
  * row's largest count as 0.  A query that is not a number, and a key that is none for all the queries that read it, make out and lse not a number.  An infinite
  * value makes its component that infinity, or not a number if its probability is below 2^-36 (fp16), 2^-100 (bf16) of the largest.  Before they are divided by their
  * sum, probabilities are up to 2^8 times what they end as: sums of bf16 values near 2^120 overflow.
- *   n < 2^22, n * q_heads < 2^31, q_heads a multiple of the cache's heads, at most 16 times; n * heads * table_width * page / 32 < 2^32; page a multiple of 8.
+ *   n < 2^22, n * q_heads < 2^31, q_heads a multiple of the cache's heads, at most 16 times; n * heads * table_width * page / 32 < 2^32; page a multiple of 8
+ *   (positions are looked up and loaded eight at a time).
  *   d_ws        mmv_paged_attention_workspace_bytes(n, q_heads, heads, dim, table_width * page) bytes */
 size_t mmv_paged_attention_workspace_bytes(uint64_t n, uint32_t q_heads, uint32_t heads, uint32_t dim, uint64_t max_context);
 mmv_status mmv_paged_attention(uint64_t n, uint32_t q_heads, const void *d_q, uint64_t q_stride, mmv_type type,

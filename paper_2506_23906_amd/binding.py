@@ -528,7 +528,8 @@ class _CacheStruct(ctypes.Structure):   # mmv_paged_cache
 
 class PagedCache:
     """The keys and values of a layer in pages: two tensors [pages, heads, slots of a page, dim] of fp16, bf16 or e4m3 (any order of the first
-    three dimensions in memory: both tensors with the same strides).  An e4m3 cache holds key / k_scale and value / v_scale."""
+    three dimensions in memory: both tensors with the same strides).  An e4m3 cache holds key / k_scale and value / v_scale.  mmv_paged_attention takes
+    pages of a multiple of 8 slots."""
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: float = 1.0, v_scale: float = 1.0):
         if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype or k.device != v.device or k.stride() != v.stride():
