@@ -124,9 +124,10 @@ constexpr uint32_t kChunk = 64;
 
 struct PromptParams {
     DecayParams d;
-    float *block_states;    // [blocks * heads][dk * dv]
+    float *block_states;    // [slots * heads][dk * dv]
     uint32_t block;         // tokens (a multiple of kChunk) at least
     uint32_t blocks;        // of one head: as many as there is room for, at least one for each request
+    uint32_t slots;         // of the states of blocks: as many as the requests of several blocks can have together
     uint32_t first_block, first_request;   // of a launch
 };
 
@@ -163,6 +164,8 @@ __device__ __forceinline__ uint32_t wave_sum32(uint32_t v) {
     v += dpp_or_zero<0x142, 0xA>(v);
     return lane_value(v + dpp_or_zero<0x143, 0xC>(v), 63);
 }
+__device__ __forceinline__ uint32_t blocks_of(Span s, uint32_t block) { return max(1u, (s.end - s.begin + block - 1) / block); }
+__device__ __forceinline__ uint32_t slots_of(uint32_t blocks) { return blocks > 1 ? blocks : 0u; }   // (a request of one block starts from its own state)
 __device__ __forceinline__ uint32_t choose_block(const PromptParams &PP) {
     const DecayParams &P = PP.d;
     if (P.n > 64 || PP.block >= P.tokens) return PP.block;
@@ -170,22 +173,25 @@ __device__ __forceinline__ uint32_t choose_block(const PromptParams &PP) {
     const Span s = lane < P.n ? span_of(P, lane) : Span{0, 0};
     const uint32_t length = s.end - s.begin;
     uint32_t block = max(PP.block, (wave_sum32(length) / PP.blocks + kChunk - 1) / kChunk * kChunk);
-    while (wave_sum32(lane < P.n ? max(1u, (length + block - 1) / block) : 0u) > PP.blocks) block += max(1u, block / (16 * kChunk)) * kChunk;   // (at the longest length there are n)
-    return uniform(block);
+    for (;;) {   // (at the longest length there are n blocks and no slots)
+        const uint32_t own = lane < P.n ? blocks_of(s, block) : 0u;
+        if (wave_sum32(own) <= PP.blocks && wave_sum32(slots_of(own)) <= PP.slots) return uniform(block);
+        block += max(1u, block / (16 * kChunk)) * kChunk;
+    }
 }
 
 // Which block of which request a workgroup has; blocks are numbered request after request, at least one each.
 struct BlockPlace {
     uint32_t request, block, blocks;   // the block's number in its request, and how many that has
-    uint32_t first;                    // number of the request's first block
+    uint32_t slot;                     // its state's, if there are several
     bool found;
 };
-__device__ __forceinline__ uint32_t blocks_of(Span s, uint32_t block) { return max(1u, (s.end - s.begin + block - 1) / block); }
-__device__ __forceinline__ BlockPlace find_block(const DecayParams &P, uint32_t block, uint32_t number) {
+__device__ __forceinline__ BlockPlace find_block(const PromptParams &PP, uint32_t block, uint32_t number) {
+    const DecayParams &P = PP.d;
     const uint32_t lane = threadIdx.x & 63;
     BlockPlace at = {0, 0, 0, 0, false};
-    if (block >= P.tokens) return {number, 0, 1, number, number < P.n};   // (one for each)
-    uint32_t before = 0;
+    if (block >= P.tokens) return {number, 0, 1, 0, number < P.n};   // (one for each)
+    uint32_t before = 0, slots_before = 0;
     for (uint32_t first = 0; first < P.n; first += 64) {
         const uint32_t r = first + lane, own = r < P.n ? blocks_of(span_of(P, r), block) : 0u;
         uint32_t upto = own;
@@ -199,12 +205,14 @@ __device__ __forceinline__ BlockPlace find_block(const DecayParams &P, uint32_t 
             const int l = __builtin_ctzll(hit);
             at.request = uniform(first + l);
             at.blocks = uniform(__shfl(own, l));
-            at.first = uniform(before + __shfl(upto, l)) - at.blocks;
-            at.block = number - at.first;
-            at.found = true;
+            at.block = number - (uniform(before + __shfl(upto, l)) - at.blocks);
+            const uint32_t first_slot = slots_before + wave_sum32((int)lane < l ? slots_of(own) : 0u);
+            at.slot = first_slot + at.block;
+            at.found = at.blocks == 1 || first_slot + at.blocks <= PP.slots;   // (no more than there are, unless offsets go backwards)
             return at;
         }
         before += uniform(__shfl(upto, 63));
+        slots_before += wave_sum32(slots_of(own));
     }
     return at;
 }
@@ -248,10 +256,10 @@ template <int KD, int NW, typename T, bool kStates> __global__ __launch_bounds__
     const DecayParams &P = PP.d;
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), g = lane >> 4, r = lane & 15;
     const uint32_t in_launch = uniform(blockIdx.x / P.heads), h = uniform(blockIdx.x - in_launch * P.heads), kv = uniform(h / P.group), number = PP.first_block + in_launch;
-    const uint64_t slot = (uint64_t)number * P.heads + h;
     const uint32_t block = choose_block(PP);
-    const BlockPlace at = find_block(P, block, number);
+    const BlockPlace at = find_block(PP, block, number);
     if (!at.found || (kStates && at.block + 1 == at.blocks)) return;
+    const uint64_t slot = (uint64_t)at.slot * P.heads + h;
     const Span span = span_of(P, at.request);
     const uint32_t begin = uniform(span.begin + at.block * block);
     const uint32_t end = uniform(min(span.end, begin + block));
@@ -570,12 +578,12 @@ __global__ __launch_bounds__(256) void decay_blocks_kernel(PromptParams PP) {
     const uint32_t slices = (uint32_t)((matrix + 1023) / 1024), slice = blockIdx.x % slices, h = blockIdx.x / slices % P.heads, request = PP.first_request + blockIdx.x / slices / P.heads;
     const uint32_t block = choose_block(PP), blocks = blocks_of(span_of(P, request), block);
     if (blocks == 1) return;
-    uint32_t mine = 0;   // blocks before this request's
-    for (uint32_t i = threadIdx.x & 63; i < request; i += 64) mine += blocks_of(span_of(P, i), block);
+    uint32_t mine = 0;   // slots before this request's
+    for (uint32_t i = threadIdx.x & 63; i < request; i += 64) mine += slots_of(blocks_of(span_of(P, i), block));
 #pragma unroll
     for (int d = 32; d >= 1; d >>= 1) mine += __shfl_xor(mine, d);
     const uint64_t at = (uint64_t)slice * 1024 + threadIdx.x * 4;
-    if (at >= matrix || mine + blocks > PP.blocks) return;
+    if (at >= matrix || mine + blocks > PP.slots) return;
     const uint64_t state = state_of(P, request);
     f32x4 S = {0.f, 0.f, 0.f, 0.f};
     if (P.state_in && state != ~0ull) S = *(const f32x4 *)(P.state_in + (state * P.heads + h) * matrix + at);

@@ -203,12 +203,13 @@ mmv_status decay_params(DecayParams &P, uint64_t n, uint64_t tokens, uint32_t he
 constexpr uint32_t kOneBlock = 256;
 constexpr uint64_t kFewTokens = 20480;   // times heads
 constexpr uint32_t prompt_waves(uint32_t dv) { return dv <= 64 ? 4 : dv <= 128 ? 8 : dv <= 160 ? 10 : 16; }
+// slots: the states that are kept, those of requests of several blocks alone (1000 prompts of 100 tokens, 16 heads of 128 x 128: 66 MB; one for every block 1.1 GB).
 struct DecayBlocks {
-    uint32_t block, blocks;
+    uint32_t block, blocks, slots;
     bool split;
 };
 inline DecayBlocks decay_blocks(uint64_t n, uint64_t tokens, uint32_t heads, uint32_t dk, uint32_t dv) {
-    if (tokens <= kOneBlock) return {kOneBlock, (uint32_t)n, false};
+    if (tokens <= kOneBlock) return {kOneBlock, (uint32_t)n, 0, false};
     const uint32_t by_waves = 16 / prompt_waves(dv), by_lds = dk <= 64 ? 3 : 2, on_unit = by_waves < by_lds ? by_waves : by_lds;   // workgroups on a compute unit
     const uint64_t round = kUnits * on_unit / heads;
     uint64_t blocks = 3 * n <= round ? round : 2 * round;
@@ -220,11 +221,12 @@ inline DecayBlocks decay_blocks(uint64_t n, uint64_t tokens, uint32_t heads, uin
         block = ceil_div(ceil_div(tokens, blocks - n), kChunk) * kChunk;
         if (block < least) block = least;
     }
-    return {(uint32_t)block, (uint32_t)blocks, true};
+    const uint64_t slots = 2 * tokens / block;   // (a length of more than one block fills more than half of its blocks)
+    return {(uint32_t)block, (uint32_t)blocks, (uint32_t)(slots < blocks ? slots : blocks), true};
 }
 inline size_t decay_workspace(uint64_t n, uint64_t tokens, uint32_t heads, uint32_t dk, uint32_t dv) {
     const DecayBlocks b = decay_blocks(n, tokens, heads, dk, dv);
-    return b.split ? round256((size_t)b.blocks * heads * dk * dv * 4) : 0;
+    return b.split ? round256((size_t)b.slots * heads * dk * dv * 4) : 0;
 }
 template <int KD, int NW, typename T, bool kStates> mmv_status launch_blocks(PromptParams P, hipStream_t s) {
     const uint32_t most = most_of_a_launch(64 * NW, P.d.heads);
@@ -261,7 +263,7 @@ mmv_status decay_call(const DecayParams &d, int type, void *d_ws, hipStream_t s)
     PromptParams P = {};
     P.d = d;
     const DecayBlocks b = decay_blocks(d.n, d.tokens, d.heads, d.dk, d.dv);
-    P.block = b.block, P.blocks = b.blocks;
+    P.block = b.block, P.blocks = b.blocks, P.slots = b.slots;
     P.block_states = b.split ? (float *)d_ws : nullptr;
     if (type == MMV_TYPE_F16) return d.dk <= 64 ? launch_prompts_of<2, f16_t>(P, s) : launch_prompts_of<4, f16_t>(P, s);
     return d.dk <= 64 ? launch_prompts_of<2, bf16_t>(P, s) : d.dk <= 96 ? launch_prompts_of<3, bf16_t>(P, s) : launch_prompts_of<4, bf16_t>(P, s);
