@@ -197,6 +197,9 @@ mmv_status decay_params(DecayParams &P, uint64_t n, uint64_t tokens, uint32_t he
 // leaves a part of a single round idle where a request has few blocks, so more than a third as many requests as blocks take two rounds.  Us with one
 // round / two / three, 128 columns: 16 heads (32 blocks of a round), 4 requests of up to 16000 tokens 103 / 120 / 137, 8 179 / 197 / 216, 10 237 / 238 /
 // 255, 16 417 / 357 / 369, 12 of up to 32768 468 / 456 / 472; 8 heads (64 blocks), 16 of up to 8000 121 / 139 / 148, 24 174 / 185 / 199.
+// The workgroups that fit are bf16's.  fp16's take twice the LDS for keys and queries, and one fits where two do (beyond 64 key components), two where three do: what is one round here is two of
+// theirs.  Counting those that fit gives half the blocks, whose unequal ends cost about what the states save: us with bf16's count / fp16's own, 16 heads of 128 x 128, 4
+// requests of up to 16000 267 / 285, 24 of 4000 382 / 371, 80 of 3000 749 / 576, 12 of 32768 1325 / 1404; 64 x 64 657 / 567; 8 heads of 80 x 112, 30 of 8000 424 / 458.
 // A block is as short as one chunk while the chunks of all heads are less than about one round (three prompts of 900 tokens, 8 heads, blocks of
 // 64 / 128 / 256 tokens at least 18.1 / 20.6 / 27.3; of 2500 tokens 23.8 / 24.9 / 33.2), beyond two chunks: below that the states' traffic shows (5000
 // tokens, 16 heads 39.2 / 34.2 / 35.2).  Up to 256 tokens a block for each request: one launch (one prompt of 200: 14.7, with blocks 16.4; of 300: 17.5, 16.0).
@@ -210,7 +213,7 @@ struct DecayBlocks {
 };
 inline DecayBlocks decay_blocks(uint64_t n, uint64_t tokens, uint32_t heads, uint32_t dk, uint32_t dv) {
     if (tokens <= kOneBlock) return {kOneBlock, (uint32_t)n, 0, false};
-    const uint32_t by_waves = 16 / prompt_waves(dv), by_lds = dk <= 64 ? 3 : 2, on_unit = by_waves < by_lds ? by_waves : by_lds;   // workgroups on a compute unit
+    const uint32_t by_waves = 16 / prompt_waves(dv), by_lds = dk <= 64 ? 3 : 2, on_unit = by_waves < by_lds ? by_waves : by_lds;   // workgroups on a compute unit, of bf16
     const uint64_t round = kUnits * on_unit / heads;
     uint64_t blocks = 3 * n <= round ? round : 2 * round;
     if (blocks < n + blocks / 2) blocks = n + blocks / 2;
