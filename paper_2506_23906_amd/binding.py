@@ -559,6 +559,12 @@ def _tokens(t: torch.Tensor, name: str, shape: tuple, dtype: torch.dtype) -> tup
     return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else shape[1] * shape[2]
 
 
+def _u32(v: int, name: str) -> int:   # (ctypes would cut it off)
+    if v != int(v) or not 0 <= v < 1 << 32:
+        raise MmvError("%s must be a whole number below 2^32, not negative" % name)
+    return int(v)
+
+
 def _table(t: torch.Tensor, n: int) -> tuple:
     if not t.is_cuda or t.dtype != torch.int32 or t.dim() != 2 or t.shape[0] < n or (t.shape[1] > 1 and t.stride(1) != 1):
         raise MmvError("table must be int32 [%d, pages] in GPU memory, the entries of a row one after the other" % n)
@@ -601,6 +607,7 @@ def mmv_page_tables(cached: torch.Tensor, new: torch.Tensor, free: torch.Tensor,
             if st:
                 _check(st, "mmv_page_tables")
             return out
+    page = _u32(page, "page")
     lib, n, device = load(), new.numel(), new.device
     if out is None:
         out = PageTables(*(torch.empty(k, dtype=d, device=device) for k, d in
@@ -649,6 +656,7 @@ def mmv_paged_attention(q: torch.Tensor, cache: PagedCache, table: torch.Tensor,
             if st:
                 _check(st, "mmv_paged_attention")
             return out
+    window = _u32(window, "window")
     if q.dtype not in _VALUE_TYPES or q.dim() != 3:
         raise MmvError("q must be [rows, heads, dim] of float16 or bfloat16")
     lib, (n, heads, dim), own = load(), q.shape, cache.k.shape
