@@ -1,18 +1,14 @@
 // libmmvseg, part of the translation unit serving.hip (included there, in order).
-// The 16- and 8-bit values of queries, caches and states' inputs; moves between lanes.
+// The 16-bit values of queries, caches and states' inputs; moves between lanes.
 #pragma once
 
 namespace {
 
 using f16_t = _Float16;
 using bf16_t = __bf16;
-struct e4m3_t {
-    uint8_t bits;
-};
 
 __device__ __forceinline__ float to_f32(f16_t v) { return (float)v; }
 __device__ __forceinline__ float to_f32(bf16_t v) { return __builtin_bit_cast(float, (uint32_t)__builtin_bit_cast(uint16_t, v) << 16); }
-__device__ __forceinline__ float to_f32(e4m3_t v) { return __builtin_amdgcn_cvt_f32_fp8((int)v.bits, 0); }
 template <typename T> __device__ __forceinline__ T from_f32(float v) { return (T)v; }   // to the nearest, ties to even
 
 // Every lane reads the lane that the control word names (row_shr n = 0x110 + n inside rows of 16 lanes, row_bcast 15 / 31 = 0x142 / 0x143);
