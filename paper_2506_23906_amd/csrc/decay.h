@@ -112,8 +112,8 @@ template <typename T, int kRows> __global__ __launch_bounds__(256) void decay_st
 // other's, so that each has eight tokens of its own column.
 //
 // What bounds it: vector instructions (56 % of the time of the blocks' launch; matrix ones 30 %) in phases between barriers, which two workgroups on a
-// compute unit overlap in part.  12 prompts of 63000 tokens together, 16 heads, 128 columns: 460 us (states 140, blocks 22, prompts 290 to 310; floor 161),
-// 3.6 TB/s; 3 prompts of 1000 tokens, 8 heads of 64: 17.6 us, three launches of 4 to 7.
+// compute unit overlap in part.  12 prompts of 63000 tokens together, 16 heads, 128 columns: 458 to 473 us (states 141 to 148, blocks 22, prompts 287 to 315; floor 161),
+// 3.6 TB/s; 3 prompts of 1000 tokens, 8 heads of 64: 17.8 us, three launches of 5 to 8.
 //
 // Rounding.  The matrix cores take 16-bit operands.  What is no 16-bit input is taken apart into bf16 terms, x = x0 + x1 + ...,
 // each the upper half of what the ones before it left (8 bits), the last one rounded: values times their decay into three, which is fp32's
@@ -222,7 +222,8 @@ __device__ __forceinline__ uint32_t here(uint32_t v) {
     asm volatile("" : "+v"(v));
     return v;
 }
-// Nothing is moved across: the compiler would load operands so far ahead that registers spill.
+// Nothing is moved across: the compiler would load operands so far ahead that registers spill.  (3 do all the same in bf16 with more than 96 key
+// components and 64 columns, 22 in fp16 with more than 64 and 160.)
 __device__ __forceinline__ void phase() { __builtin_amdgcn_sched_barrier(0); }
 
 // Two rows of 16-bit values, columns c and c + 1 in each word, for lanes of two columns: the even lane has rows 0 .. 3 of both, the odd one rows 4 .. 7; they
