@@ -396,9 +396,9 @@ mmv_status mmv_cache_append(uint64_t tokens, const void *d_k, uint64_t k_stride,
  *               does not have (-1) are left out.
  *   d_out       n * q_heads * dim of `type`;  d_lse  n * q_heads fp32, or NULL
  * A row without any position gets zeros and -infinity.  What lies in the cache at positions that are left out is not used,
- * whatever it is.  Scores and sums are fp32; probabilities meet the values with 16 bits of mantissa in bf16, with 22 in fp16, where those below 2^-36 of the
+ * whatever it is.  Scores and sums are fp32; probabilities meet the values with 24 bits of mantissa in bf16, with 22 in fp16, where those below 2^-36 of the
  * row's largest count as 0.  A query that is not a number, and a key that is none for all the queries that read it, make out and lse not a number.  An infinite
- * value makes its component that infinity, or not a number if its probability is below 2^-36 (fp16), 2^-100 (bf16) of the largest.  Before they are divided by their
+ * value makes its component that infinity, or not a number if its probability is below 2^-36 (fp16), 2^-90 (bf16) of the largest.  Before they are divided by their
  * sum, probabilities are up to 2^8 times what they end as: sums of bf16 values near 2^120 overflow.
  *   n < 2^22, n * q_heads < 2^31, q_heads a multiple of the cache's heads, at most 16 times; n * heads * table_width * page / 32 < 2^32; page a multiple of 8
  *   (positions are looked up and loaded eight at a time).

@@ -62,20 +62,26 @@ template <bool kHigh> __device__ __forceinline__ uint32_t widen(bf16_t, uint32_t
 template <bool kHigh> __device__ __forceinline__ uint32_t widen(f16_t, uint32_t w) {
     return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)w, 1.f, kHigh));
 }
-// Probabilities meet the values in 16 bits, as the matrix cores take both operands of one type, and as two terms, what is cut off at the type's precision and the rounded rest:
-// 16 bits together in bf16, 22 in fp16.  Rounded once they would add as much error as the rounding of the result (1.4 times the error of exact ones in bf16, 1.2
-// times in fp16).
-// The rest is never zero beside a first term that is not (kInfinite: but for 8-bit caches, which hold no infinities): a value's infinity times a probability stays that
-// infinity, and what has no weight adds nothing.  In bf16 it is at least 2^-20 of the probability.  fp16 has few exponents: there probabilities are scaled by 2^12 (which the result's factor takes back), above a base that lies at most
-// 2^3 below them, so that the largest product's is 2^15, fp16's full precision goes down to 2^-26 of the largest probability and its least value is 2^-36 of that, which is
-// also what the rest is at least; scaled by nothing, a tail of 65536 positions at 2^-25 of one beside it (2^-9 of the result) was lost.
+// Probabilities meet the values in 16 bits, as the matrix cores take both operands of one type, and as terms, each what is cut off at the type's precision of what the ones before it
+// left, the last one rounded: three in bf16 (24 bits), two in fp16 (22).  Rounded once they would add as much error as the rounding of the result (1.4 times the error of exact
+// ones in bf16, 1.2 times in fp16); bf16's third term, below that rounding by 2^-8, takes no time (48 ragged rows 68.1 us with two, 68.4 with three; 123.3 and 123.4 of 8-bit values).
+// No term is zero beside a first one that is not (kInfinite: but for 8-bit caches, which hold no infinities): a value's infinity times a probability stays that
+// infinity, and what has no weight adds nothing.  In bf16 each is at least 2^-30 of the probability.  fp16 has few exponents: there probabilities are scaled by 2^12 (which the result's
+// factor takes back), above a base that lies at most 2^3 below them, so that the largest product's is 2^15, fp16's full precision goes down to 2^-26 of the largest probability and its
+// least value is 2^-36 of that, which is also what the second term is at least; scaled by nothing, a tail of 65536 positions at 2^-25 of one beside it (2^-9 of the result) was lost.
 template <typename T> constexpr int kScaleBits = __is_same(T, bf16_t) ? 0 : 12;
 template <typename T> constexpr float kMostAbove = __is_same(T, bf16_t) ? 8.f : 3.f;   // of a score above the base, in bits
-template <bool kInfinite> __device__ __forceinline__ void probability_terms(bf16_t, float a, float b, uint32_t (&to)[2]) {
-    const uint32_t x = __builtin_bit_cast(uint32_t, a), y = __builtin_bit_cast(uint32_t, b);
-    to[0] = __builtin_amdgcn_perm(y, x, 0x07060302u);
-    const float rest_a = a - __builtin_bit_cast(float, x & 0xFFFF0000u), rest_b = b - __builtin_bit_cast(float, y & 0xFFFF0000u);
-    to[1] = kInfinite ? pack2<bf16_t>(fmaxf(rest_a, a * 0x1p-20f), fmaxf(rest_b, b * 0x1p-20f)) : pack2<bf16_t>(rest_a, rest_b);
+template <typename T> constexpr int kTerms = __is_same(T, bf16_t) ? 3 : 2;
+template <bool kInfinite> __device__ __forceinline__ void probability_terms(bf16_t, float a, float b, uint32_t (&to)[3]) {
+    const float least_a = a * 0x1p-30f, least_b = b * 0x1p-30f;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const uint32_t x = __builtin_bit_cast(uint32_t, a), y = __builtin_bit_cast(uint32_t, b);
+        to[i] = __builtin_amdgcn_perm(y, x, 0x07060302u);
+        a -= __builtin_bit_cast(float, x & 0xFFFF0000u), b -= __builtin_bit_cast(float, y & 0xFFFF0000u);
+        if (kInfinite) a = fmaxf(a, least_a), b = fmaxf(b, least_b);
+    }
+    to[2] = pack2<bf16_t>(a, b);
 }
 template <bool kInfinite> __device__ __forceinline__ void probability_terms(f16_t, float a, float b, uint32_t (&to)[2]) {
     typedef f16_t pair __attribute__((ext_vector_type(2)));
@@ -268,11 +274,11 @@ template <int KS, bool kExact, bool kStream, typename T, bool kE4m3> struct Tile
         }
         return a;
     }
-    template <int c = 0> __device__ __forceinline__ void add_values(const u32x4 (&p)[2], f32x4 (&O)[kDims]) const {
+    template <int c = 0> __device__ __forceinline__ void add_values(const u32x4 (&p)[kTerms<T>], f32x4 (&O)[kDims]) const {
         if constexpr (c < kDims) {
             const u32x4 a = column<c>();
 #pragma unroll
-            for (int i = 0; i < 2; ++i) O[c] = mfma_16x16x32(T(), a, p[i], O[c]);
+            for (int i = 0; i < kTerms<T>; ++i) O[c] = mfma_16x16x32(T(), a, p[i], O[c]);
             add_values<c + 1>(p, O);
         }
     }
@@ -390,12 +396,13 @@ __device__ __forceinline__ void attention_run(const AttentionParams &P, Place at
                     s[i] = __builtin_amdgcn_exp2f(s[i] - base);
                     recent += s[i];
                 }
-                u32x4 p[2];
+                u32x4 p[kTerms<T>];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    uint32_t terms[2];
+                    uint32_t terms[kTerms<T>];
                     probability_terms<!kE4m3>(T(), s[2 * i], s[2 * i + 1], terms);
-                    p[0][i] = terms[0], p[1][i] = terms[1];
+#pragma unroll
+                    for (int t = 0; t < kTerms<T>; ++t) p[t][i] = terms[t];
                 }
                 tile.add_values(p, O);
                 tile.load_values(P, r);

@@ -38,6 +38,19 @@ def cancelling_probabilities(dtype, cache_type, dim=64, page=16):
     return q.to(dtype), k[:, None].to(cache_type), v[:, None].to(cache_type), scale, weights, values, want, by
 
 
+def probabilities_of_24_bits(dim=64, page=16):
+    """The same for bf16's third term: seven positions whose sum cancels to 3e-6, and whose weights are 0.95 * 2^-17 from what two terms of 8 bits, the first cut off, can say."""
+    p = 0.5 * (1.0 + (171 / 128 - 0.95 * 2.0 ** -8) * 2.0 ** -8)
+    q, k, v = torch.zeros(1, 1, dim), torch.zeros(4, page, dim), torch.zeros(4, page, dim)
+    q[..., 0], k.view(-1, dim)[1:7, 0] = 1.0, -1.0
+    v.view(-1, dim)[0], v.view(-1, dim)[1:7] = 193 / 64, -1.0
+    scale = float(torch.tensor(-math.log(p), dtype=torch.float32))
+    weights, values = torch.tensor([1.0] + [math.exp(-scale)] * 6, dtype=torch.float64), v.view(-1, dim)[:7, 0].double()
+    want = float(weights @ values / weights.sum())
+    by = (2.0 ** -24 + 2.0 ** -29 + (7 + 8) * EPS) * float(weights @ values.abs() / weights.sum()) + U[BF16] * abs(want)
+    return q.to(BF16), k[:, None].to(BF16), v[:, None].to(BF16), scale, weights, values, want, by
+
+
 def flat_tail(dtype, first_value, dim=8, page=16, positions=1 << 16, below=25.3):
     """One position of weight 1 and 65535 of 2^-25.3 and value 1: the others' weight together is 1.6e-3.  Page 0 has the first 16, page 1 any 16 others.  Returns q, k, v, the scale,
     a component's result and bound, and lse with its bound."""

@@ -26,6 +26,13 @@ def test_probabilities(dtype, cache_type, columns):
     close(out, want, by, "out")
 
 
+@pytest.mark.parametrize("columns", [4, 900])
+def test_probabilities_of_24_bits(columns):
+    q, k, v, scale, weights, values, want, by = R.probabilities_of_24_bits()
+    out = B.mmv_paged_attention(q.cuda(), B.PagedCache(k.cuda(), v.cuda()), ints([[0, 1, 2, 3] + [-1] * (columns - 4)]), ints([7]), scale=scale)
+    close(out, want, by, "out")
+
+
 @pytest.mark.parametrize("dtype", [R.BF16, R.F16])
 def test_a_flat_tail_counts_in_the_sum(dtype):
     """4096 rows, so that a wave has whole rows of 65536 positions."""

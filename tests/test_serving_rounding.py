@@ -14,6 +14,16 @@ def test_probabilities(dtype, cache_type):
     assert off[1] <= by / 4 and off[0] >= 4 * by
 
 
+def test_probabilities_of_24_bits():
+    *_, weights, values, want, by = R.probabilities_of_24_bits()
+    off, held = [], torch.zeros_like(weights)
+    for _ in range(3):
+        left = weights - held
+        off.append(abs(float((held + left.to(R.BF16).double()) @ values / weights.sum()) - want))     # this term rounded, the last one
+        held = held + (left.float().view(torch.int32) & -65536).view(torch.float32).double()          # cut off, with one to follow
+    assert off[2] <= by / 4 and off[1] >= 4 * by
+
+
 @pytest.mark.parametrize("dtype", [R.BF16, R.F16])
 @pytest.mark.parametrize("case", [R.cancelling_state, R.cancelling_scores])
 def test_states_and_scores(case, dtype):
