@@ -20,8 +20,8 @@ namespace {
 //            registers.  A lane loads 8 components of 8 consecutive positions' values (rows of the cache, coalesced)
 //            and exchanges 16-bit halves between pairs of positions: one v_perm for two values.
 // No LDS and no barrier in the loop.  Query heads beyond the group's are zero columns: the matrix cores have the time (about a tenth of
-// what the loads take).  Whole calls: 48 ragged rows of up to 8192 positions (330 MB in bf16) 67.9 us, 62 of them in the list's kernel, 5.3 TB/s;
-// 16 of up to 65536 (717 MB in e4m3) 124 us, 117 of them, 6.1 TB/s; one row of 1000 9.4 us, the lives of two launches.
+// what the loads take).  Whole calls: 48 ragged rows of up to 8192 positions (330 MB in bf16) 68.2 us, 62 of them in the list's kernel, 5.3 TB/s;
+// 16 of up to 65536 (717 MB in e4m3) 123 us, 117 of them, 6.1 TB/s; one row of 1000 9.5 us, the lives of two launches.
 struct AttentionParams {
     const void *q, *k, *v;
     uint64_t q_stride, head_stride;                // elements
