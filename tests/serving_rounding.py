@@ -1,6 +1,6 @@
 """Inputs whose exact results nearly cancel, so that every bit of what lies between shows, with bounds that count the roundings of each term and nothing more.
 
-The matrix cores take 16-bit operands.  A probability, a score or a state that meets them is split into two terms, a value times its decay into three; the
+The matrix cores take 16-bit operands.  What meets them is split into two terms (a probability in fp16, a score, a state) or three (a probability in bf16, a value times its decay); the
 bounds here hold for those splits and not if the last term is left out (tests/test_serving_rounding.py tries both on the CPU)."""
 import math
 
@@ -9,8 +9,8 @@ import torch
 from serving_util import EPS, U
 
 BF16, F16, E4M3 = torch.bfloat16, torch.float16, torch.float8_e4m3fn
-# Two terms: what the first leaves, cut off, is below 2^-7 (bf16), 2^-10 (fp16) of the value, and the second rounds that.  What keeps a probability's second term
-# from zero adds 2^-20 of it (bf16), or half of fp16's least value, 2^-36 of the largest probability.
+# Two terms: what the first leaves, cut off, is below 2^-7 (bf16), 2^-10 (fp16) of the value, and the second rounds that.  What keeps a probability's later
+# terms from zero adds less than 2^-20 of it (bf16), or half of fp16's least value, 2^-36 of the largest probability.
 TWO = {BF16: 2.0 ** -7 * U[BF16], F16: 2.0 ** -10 * U[F16]}
 GUARD, LEAST = {BF16: 2.0 ** -20, F16: 0.0}, {BF16: 0.0, F16: 2.0 ** -36}
 
