@@ -329,9 +329,10 @@ mmv_status mmv_gather_reference(uint64_t nnz, const float *d_val, const int32_t 
 
 /* ---- A serving step over a ragged batch -----------------------------------------------------------------------------
  * The requests of a batch are the segments of its packed token vector: request r owns the tokens offsets[r] ..
- * offsets[r + 1] - 1.  Five calls that a model's step makes on such a batch: page tables and slots from the requests'
- * lengths, new keys and values into the paged cache, attention of one token per request over that cache, and linear
- * attention with a decay for each head, over prompts and for single tokens.  What the conventions above say holds here too,
+ * offsets[r + 1] - 1.  The calls that a model's step makes on such a batch: page tables and slots from the requests'
+ * lengths, new keys and values into the paged cache, attention of one token per request over that cache, the same for a cache
+ * of 8-bit values with a scale for each block of slots and head, which can be read back; and two recurrences, linear
+ * attention with a decay for each head and the gated delta rule, over prompts and for single tokens.  What the conventions above say holds here too,
  * with these differences: lengths, tables and indices are read by the kernels alone, so that a step can be captured into a HIP
  * graph and replayed as they change, and none of them is trusted: what would lie outside an array is left out as each call
  * says.  Pointers to values are 16-byte aligned, pointers to 32- and 64-bit integers and fp32 aligned to their size; nothing is
@@ -341,6 +342,7 @@ typedef enum {
     MMV_TYPE_F16 = 1,
     MMV_TYPE_BF16 = 2,
     MMV_TYPE_E4M3 = 5, /* 8 bits with 4 of exponent, largest value 448, no infinities (caches only) */
+    MMV_TYPE_I8 = 6,   /* whole numbers from -127 to 127 (caches in blocks only) */
     MMV_TYPE_INT_MAX = 0x7fffffff
 } mmv_type;
 
@@ -436,6 +438,73 @@ mmv_status mmv_decay_attention(uint64_t n, uint64_t tokens, uint32_t heads, uint
 mmv_status mmv_decay_step(uint64_t n, uint32_t heads, uint32_t kv_heads, uint32_t dk, uint32_t dv,
                           const void *d_q, uint64_t q_stride, const void *d_k, uint64_t k_stride, const void *d_v, uint64_t v_stride,
                           mmv_type type, const float *d_log_decay, float scale,
+                          const float *d_state_in, float *d_state_out, uint64_t states, const int32_t *d_state_index,
+                          void *d_out, void *hip_stream);
+
+/* A paged cache of 8-bit values (MMV_TYPE_I8 or MMV_TYPE_E4M3) in which every block of `block` neighbouring slots of a page has a scale for each head,
+ * of its keys and of its values: component c of slot s of page p for head h stands for
+ *   code * scale,   code: element p * page_stride + h * head_stride + s * slot_stride + c of d_k (d_v),
+ *                   scale: element (p * heads + h) * (page / block) + s / block of d_k_scales (d_v_scales).
+ * block is a multiple of 8 and divides page; the rest is as in mmv_paged_cache. */
+typedef struct {
+    void *d_k, *d_v;
+    float *d_k_scales, *d_v_scales;
+    mmv_type type;
+    uint32_t page, heads, dim, block;
+    uint64_t pages, page_stride, head_stride, slot_stride;
+} mmv_block_cache;
+
+/* New keys and values into their slots, quantised on the way.  d_k, d_v, d_slots as for mmv_cache_append; `type` is any 16-bit one.  Neighbouring
+ * tokens whose slots lie in one block are a run, and for every run, head and kind
+ *   wanted = max(largest |x| of the run, 2^-100) * (1 / Q),  Q = 127 (MMV_TYPE_I8) or 448 (MMV_TYPE_E4M3)
+ *   scale  = wanted, if the block's first slot is among the run's: the block begins anew; else the larger of wanted and the scale that it has
+ *   code   = x * (1 / scale) rounded to the nearest, ties to even, at most Q in magnitude
+ * all in fp32, each operation rounded.  Where the scale of a block that does not begin anew grows, what all its slots hold is rounded again:
+ * code * (scale before * (1 / scale)).  So a block is filled from its first slot on, as mmv_page_tables hands them out; what is in the slots of a block that begins anew is
+ * left as it was and stands for nothing until it is written.  Scales of blocks that never began have to be numbers (zeros, say).
+ * Infinities count as the largest finite value of `type`.  What is not a number stays so in MMV_TYPE_E4M3; MMV_TYPE_I8 has no code for it, and the block's scale becomes
+ * not a number (what is written then has the code -127), until the block begins anew.  A slot outside the cache is skipped.  Tokens of one block have to be neighbours, in any order: of two runs of one block either may win, code by code and
+ * scale, and so of two tokens with one slot.  tokens < 2^26. */
+mmv_status mmv_block_append(uint64_t tokens, const void *d_k, uint64_t k_stride, const void *d_v, uint64_t v_stride, mmv_type type,
+                            const int64_t *d_slots, const mmv_block_cache *cache, void *hip_stream);
+
+/* Keys and values of n requests out of the cache, packed: token t of request r (offsets[r] <= t < offsets[r + 1]) is its position
+ * first[r] + t - offsets[r]; its head h's values go to elements t * stride + h * dim ... of d_k (d_v), of `type` (16-bit): code * scale, rounded.
+ *   d_offsets   n + 1 int32, non-decreasing (where they are not, a token may be left out); tokens that belong to no request are not written
+ *   d_first     n int32, or NULL: zeros
+ *   d_table     as mmv_page_tables leaves it.  A position outside the row, or in a page that the cache does not have, gives zeros. */
+mmv_status mmv_block_read(uint64_t n, uint64_t tokens, const int32_t *d_offsets, const int32_t *d_first, const int32_t *d_table, uint64_t table_width,
+                          uint64_t table_stride, const mmv_block_cache *cache, mmv_type type, void *d_k, uint64_t k_stride, void *d_v, uint64_t v_stride,
+                          void *hip_stream);
+
+/* mmv_paged_attention over such a cache; `type` is any 16-bit one.  Probabilities times the values' scale meet the codes with 24 bits of mantissa whatever the
+ * type is; those whose product with the scale is below 2^-110 may count as 0.  A scale that is not a number makes out (a key's: lse too) not a number for the rows and heads that
+ * read its block.
+ *   d_ws        mmv_paged_attention_workspace_bytes(n, q_heads, heads, dim, table_width * page) bytes */
+mmv_status mmv_block_attention(uint64_t n, uint32_t q_heads, const void *d_q, uint64_t q_stride, mmv_type type, const mmv_block_cache *cache,
+                               const int32_t *d_table, uint64_t table_width, uint64_t table_stride, const int32_t *d_context, float scale, uint32_t window,
+                               void *d_out, float *d_lse, void *d_ws, size_t ws_bytes, void *hip_stream);
+
+/* The gated delta rule over the packed tokens of n requests:
+ *   S' = exp(log_decay_t) S_(t-1),   S_t = S' + beta_t k_t (v_t - k_t S')^T,   out_t = scale * q_t S_t
+ * where S is a dk x dv matrix for every request and head, as in mmv_decay_attention.  Head h has values, log_decay and beta of its own and reads the query
+ * and key of head h / (heads / k_heads).
+ *   d_q, d_k    token t's vector for head h: elements t * stride + h * dk ..., of `type` (16-bit).  Keys are not normalised here: with beta |k|^2 above 2 states grow
+ *   d_v         elements t * stride + h * dv ... for each of `heads` heads
+ *   d_log_decay, d_beta  tokens * heads fp32; log_decay 0 or below (below -200 as -200), beta from 0 to 1, or to 2
+ *   d_offsets, d_state_in, d_state_out, d_state_index, d_out, limits  as for mmv_decay_attention
+ * States and what a token writes are fp32 throughout.  An infinity, or what is not a number, in a token reaches no earlier token and no other request or head. */
+size_t mmv_delta_attention_workspace_bytes(uint64_t n, uint64_t tokens, uint32_t heads, uint32_t dk, uint32_t dv);
+mmv_status mmv_delta_attention(uint64_t n, uint64_t tokens, uint32_t heads, uint32_t k_heads, uint32_t dk, uint32_t dv,
+                               const void *d_q, uint64_t q_stride, const void *d_k, uint64_t k_stride, const void *d_v, uint64_t v_stride,
+                               mmv_type type, const int32_t *d_offsets, const float *d_log_decay, const float *d_beta, float scale,
+                               const float *d_state_in, float *d_state_out, uint64_t states, const int32_t *d_state_index,
+                               void *d_out, void *d_ws, size_t ws_bytes, void *hip_stream);
+
+/* The same for one token of each of n requests: token r is request r's.  No workspace. */
+mmv_status mmv_delta_step(uint64_t n, uint32_t heads, uint32_t k_heads, uint32_t dk, uint32_t dv,
+                          const void *d_q, uint64_t q_stride, const void *d_k, uint64_t k_stride, const void *d_v, uint64_t v_stride,
+                          mmv_type type, const float *d_log_decay, const float *d_beta, float scale,
                           const float *d_state_in, float *d_state_out, uint64_t states, const int32_t *d_state_index,
                           void *d_out, void *hip_stream);
 

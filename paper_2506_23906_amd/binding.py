@@ -27,7 +27,7 @@ MMV_VARIANT_MFMA, MMV_VARIANT_SHUFFLE = 0, 1
 MMV_OP_SEGSCAN, MMV_OP_SEGSUM, MMV_OP_SPMV_COO = 0, 1, 2
 MMV_OP_SCAN, MMV_OP_COMPRESS, MMV_OP_SEGSUM_SCD, MMV_OP_SEGSCAN_SSCR, MMV_OP_SPMV_CSR = 3, 4, 5, 6, 7
 MMV_ELEM_I32, MMV_ELEM_F32 = 0, 1
-MMV_TYPE_F16, MMV_TYPE_BF16, MMV_TYPE_E4M3 = 1, 2, 5
+MMV_TYPE_F16, MMV_TYPE_BF16, MMV_TYPE_E4M3, MMV_TYPE_I8 = 1, 2, 5, 6
 
 EXPORTS = [
     "mmv_workspace_bytes", "mmv_segscan", "mmv_segsum", "mmv_spmv_coo", "mmv_workspace_status",
@@ -37,6 +37,7 @@ EXPORTS = [
     "mmv_spmv_coo_prepare", "mmv_spmv_coo_run", "mmv_spmv_csr_prepare", "mmv_spmv_csr_run",
     "mmv_page_tables_workspace_bytes", "mmv_page_tables", "mmv_cache_append", "mmv_paged_attention_workspace_bytes", "mmv_paged_attention",
     "mmv_decay_attention_workspace_bytes", "mmv_decay_attention", "mmv_decay_step",
+    "mmv_block_append", "mmv_block_read", "mmv_block_attention", "mmv_delta_attention_workspace_bytes", "mmv_delta_attention", "mmv_delta_step",
 ]
 STATIC_SCRATCH_BYTES = 1 << 20   # MMV_STATIC_SCRATCH_BYTES
 
@@ -129,6 +130,18 @@ def load() -> ctypes.CDLL:
     lib.mmv_decay_attention.restype = i32
     lib.mmv_decay_step.argtypes = [u64, u32, u32, u32, u32, vp, u64, vp, u64, vp, u64, i32, vp, f32, vp, vp, u64, vp, vp, vp]
     lib.mmv_decay_step.restype = i32
+    lib.mmv_block_append.argtypes = [u64, vp, u64, vp, u64, i32, vp, vp, vp]
+    lib.mmv_block_append.restype = i32
+    lib.mmv_block_read.argtypes = [u64, u64, vp, vp, vp, u64, u64, vp, i32, vp, u64, vp, u64, vp]
+    lib.mmv_block_read.restype = i32
+    lib.mmv_block_attention.argtypes = lib.mmv_paged_attention.argtypes
+    lib.mmv_block_attention.restype = i32
+    lib.mmv_delta_attention_workspace_bytes.argtypes = [u64, u64, u32, u32, u32]
+    lib.mmv_delta_attention_workspace_bytes.restype = sz
+    lib.mmv_delta_attention.argtypes = [u64, u64, u32, u32, u32, u32, vp, u64, vp, u64, vp, u64, i32, vp, vp, vp, f32, vp, vp, u64, vp, vp, vp, sz, vp]
+    lib.mmv_delta_attention.restype = i32
+    lib.mmv_delta_step.argtypes = [u64, u32, u32, u32, u32, vp, u64, vp, u64, vp, u64, i32, vp, vp, f32, vp, vp, u64, vp, vp, vp]
+    lib.mmv_delta_step.restype = i32
     try:
         marshal = importlib.import_module(__package__ + "._marshal")
     except ImportError:
@@ -139,7 +152,8 @@ def load() -> ctypes.CDLL:
         marshal.bind(*(ctypes.cast(getattr(lib, name), vp).value for name in
                        ("mmv_segscan", "mmv_segsum", "mmv_scan", "mmv_compress", "mmv_spmv_coo", "mmv_spmv_csr", "mmv_spmv_coo_run", "mmv_spmv_csr_run")))
         marshal.bind_serving(*(ctypes.cast(getattr(lib, name), vp).value for name in
-                               ("mmv_page_tables", "mmv_cache_append", "mmv_paged_attention", "mmv_decay_attention", "mmv_decay_step")))
+                               ("mmv_page_tables", "mmv_cache_append", "mmv_paged_attention", "mmv_decay_attention", "mmv_decay_step",
+                                "mmv_block_append", "mmv_block_read", "mmv_block_attention", "mmv_delta_attention", "mmv_delta_step")))
     _lib, _marshal = lib, marshal
     return lib
 
@@ -643,6 +657,24 @@ def mmv_paged_attention_workspace_bytes(n: int, q_heads: int, heads: int, dim: i
     return int(load().mmv_paged_attention_workspace_bytes(n, q_heads, heads, dim, max_context))
 
 
+def _attention(name, ref, q, cache, table, context, scale, window, out, lse, ws, stream):
+    window = _u32(window, "window")
+    if q.dtype not in _VALUE_TYPES or q.dim() != 3:
+        raise MmvError("q must be [rows, heads, dim] of float16 or bfloat16")
+    lib, (n, heads, dim), own = load(), q.shape, cache.k.shape
+    pq, sq = _tokens(q, "q", (n, heads, own[3]), q.dtype)
+    out = _out(out, "out", (n, heads, dim), q.dtype, q.device)
+    row, width, stride = _table(table, n)
+    if lse is not None:
+        lse = _out(lse, "lse", (n, heads), torch.float32, q.device)
+    w, w_bytes, ws = _ws(ws, mmv_paged_attention_workspace_bytes(n, heads, own[1], dim, width * own[2]), q.device)
+    st = getattr(lib, name)(n, heads, pq, sq, _VALUE_TYPES[q.dtype], ref, row, width, stride, _ints(context, "context", torch.int32, n),
+                            1.0 / math.sqrt(dim) if scale is None else scale, window, _dev(out, "out"), None if lse is None else _dev(lse, "lse"),
+                            w, w_bytes, _stream_ptr(stream))
+    _check(st, name)
+    return out
+
+
 def mmv_paged_attention(q: torch.Tensor, cache: PagedCache, table: torch.Tensor, context: torch.Tensor, scale: float | None = None, window: int = 0,
                         out: torch.Tensor | None = None, lse: torch.Tensor | None = None, ws: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """Attention of one token q[r] ([rows, query heads, dim]) over the first context[r] positions of every row of the table, or the last
@@ -656,21 +688,18 @@ def mmv_paged_attention(q: torch.Tensor, cache: PagedCache, table: torch.Tensor,
             if st:
                 _check(st, "mmv_paged_attention")
             return out
-    window = _u32(window, "window")
-    if q.dtype not in _VALUE_TYPES or q.dim() != 3:
-        raise MmvError("q must be [rows, heads, dim] of float16 or bfloat16")
-    lib, (n, heads, dim), own = load(), q.shape, cache.k.shape
-    pq, sq = _tokens(q, "q", (n, heads, own[3]), q.dtype)
-    out = _out(out, "out", (n, heads, dim), q.dtype, q.device)
-    row, width, stride = _table(table, n)
-    if lse is not None:
-        lse = _out(lse, "lse", (n, heads), torch.float32, q.device)
-    w, w_bytes, ws = _ws(ws, mmv_paged_attention_workspace_bytes(n, heads, own[1], dim, width * own[2]), q.device)
-    st = lib.mmv_paged_attention(n, heads, pq, sq, _VALUE_TYPES[q.dtype], cache._ref, row, width, stride, _ints(context, "context", torch.int32, n),
-                                 1.0 / math.sqrt(dim) if scale is None else scale, window, _dev(out, "out"), None if lse is None else _dev(lse, "lse"),
-                                 w, w_bytes, _stream_ptr(stream))
-    _check(st, "mmv_paged_attention")
-    return out
+    return _attention("mmv_paged_attention", cache._ref, q, cache, table, context, scale, window, out, lse, ws, stream)
+
+
+def _states(heads, dk, dv, state_in, state_out, state_index, n):
+    states = None
+    for name, s in (("state_in", state_in), ("state_out", state_out)):
+        if s is not None:
+            if s.dtype != torch.float32 or s.dim() != 4 or tuple(s.shape[1:]) != (heads, dk, dv) or s.shape[0] != (states or s.shape)[0]:
+                raise MmvError("%s must be [states, %d, %d, %d] of float32" % (name, heads, dk, dv))
+            states = s.shape
+    return (None if state_in is None else _dev(state_in, "state_in"), None if state_out is None else _dev(state_out, "state_out"), states[0] if states else 0,
+            None if state_index is None else _ints(state_index, "state_index", torch.int32, n))
 
 
 def _decay_arguments(q, k, v, log_decay, state_in, state_out, state_index, n, out):
@@ -678,18 +707,11 @@ def _decay_arguments(q, k, v, log_decay, state_in, state_out, state_index, n, ou
         raise MmvError("q, k and v must be [tokens, heads, dim] of float16 or bfloat16")
     (t, heads, dk), (kv, dv) = q.shape, v.shape[1:]
     (pq, sq), (pk, sk), (pv, sv) = _tokens(q, "q", (t, heads, dk), q.dtype), _tokens(k, "k", (t, kv, dk), q.dtype), _tokens(v, "v", (t, kv, dv), q.dtype)
-    states = None
-    for name, s in (("state_in", state_in), ("state_out", state_out)):
-        if s is not None:
-            if s.dtype != torch.float32 or s.dim() != 4 or tuple(s.shape[1:]) != (heads, dk, dv) or s.shape[0] != (states or s.shape)[0]:
-                raise MmvError("%s must be [states, %d, %d, %d] of float32" % (name, heads, dk, dv))
-            states = s.shape
+    state = _states(heads, dk, dv, state_in, state_out, state_index, n)
     out = _out(out, "out", (t, heads, dv), q.dtype, q.device)
     head = (heads, kv, dk, dv, pq, sq, pk, sk, pv, sv, _VALUE_TYPES[q.dtype])
     tail = (_ints(log_decay, "log_decay", torch.float32, heads),)
-    state = (None if state_in is None else _dev(state_in, "state_in"), None if state_out is None else _dev(state_out, "state_out"), states[0] if states else 0,
-             None if state_index is None else _ints(state_index, "state_index", torch.int32, n), _dev(out, "out"))
-    return t, head, tail, state, out
+    return t, head, tail, state + (_dev(out, "out"),), out
 
 
 def mmv_decay_attention_workspace_bytes(n: int, tokens: int, heads: int, dk: int, dv: int) -> int:
@@ -737,4 +759,177 @@ def mmv_decay_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_decay:
     t, head, decay, state, out = _decay_arguments(q, k, v, log_decay, state_in, state_out, state_index, q.shape[0], out)
     st = load().mmv_decay_step(t, *head, *decay, head[2] ** -0.5 if scale is None else scale, *state, _stream_ptr(stream))
     _check(st, "mmv_decay_step")
+    return out
+
+
+# ---- a cache of 8-bit values with a scale for each block of slots and head ------------------------------------------
+
+_BLOCK_TYPES = {torch.int8: MMV_TYPE_I8, torch.float8_e4m3fn: MMV_TYPE_E4M3}
+
+
+class _BlockCacheStruct(ctypes.Structure):   # mmv_block_cache
+    _fields_ = [("d_k", ctypes.c_void_p), ("d_v", ctypes.c_void_p), ("d_k_scales", ctypes.c_void_p), ("d_v_scales", ctypes.c_void_p), ("type", ctypes.c_int),
+                ("page", ctypes.c_uint32), ("heads", ctypes.c_uint32), ("dim", ctypes.c_uint32), ("block", ctypes.c_uint32), ("pages", ctypes.c_uint64),
+                ("page_stride", ctypes.c_uint64), ("head_stride", ctypes.c_uint64), ("slot_stride", ctypes.c_uint64)]
+
+
+class BlockCache:
+    """The keys and values of a layer in pages of 8-bit codes: two tensors [pages, heads, slots of a page, dim] of int8 or e4m3 (any order of the first three
+    dimensions in memory: both with the same strides), and their scales, two fp32 tensors [pages, heads, blocks of a page] (zeros to begin with): a block is a
+    multiple of 8 neighbouring slots, and its values are code * scale."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scales: torch.Tensor, v_scales: torch.Tensor):
+        if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype or k.device != v.device or k.stride() != v.stride():
+            raise MmvError("a cache is two tensors [pages, heads, slots, dim] of the same shape, type and strides")
+        if k.dtype not in _BLOCK_TYPES:
+            raise MmvError("a cache in blocks holds int8 or float8_e4m3fn")
+        if not k.is_cuda or k.stride(3) != 1 or min(k.stride()) < 0:
+            raise MmvError("a cache lies in GPU memory, the values of a slot one after the other")
+        for name, s in (("k_scales", k_scales), ("v_scales", v_scales)):
+            if s.dim() != 3 or s.dtype != torch.float32 or s.shape[:2] != k.shape[:2] or s.shape != k_scales.shape or s.device != k.device or not s.is_contiguous():
+                raise MmvError("%s must be [%d, %d, blocks of a page] of float32 beside the cache, contiguous" % (name, k.shape[0], k.shape[1]))
+        blocks = k_scales.shape[2]
+        if blocks < 1 or k.shape[2] % blocks or k.shape[2] // blocks % 8:
+            raise MmvError("a page has whole blocks of a multiple of 8 slots")
+        self.k, self.v, self.k_scales, self.v_scales, self.block = k, v, k_scales, v_scales, k.shape[2] // blocks
+        self._struct = _BlockCacheStruct(k.data_ptr(), v.data_ptr(), k_scales.data_ptr(), v_scales.data_ptr(), _BLOCK_TYPES[k.dtype], k.shape[2], k.shape[1], k.shape[3],
+                                         self.block, k.shape[0], k.stride(0), k.stride(1), k.stride(2))
+        self._blocks_ref = ctypes.addressof(self._struct)   # (not PagedCache's name: neither is taken for the other)
+
+
+def _blocks(cache) -> int:
+    if type(cache) is not BlockCache:
+        raise MmvError("cache must be a BlockCache")
+    return cache._blocks_ref
+
+
+def mmv_block_append(k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, cache: BlockCache, stream=None) -> None:
+    """The keys and values [tokens, heads, dim] of new tokens into their slots, quantised; tokens of one block are neighbours."""
+    ref = _blocks(cache)
+    if _marshal is not None:
+        st = _marshal.block_append(k, v, slots, ref, stream)
+        if st is not None:
+            if st:
+                _check(st, "mmv_block_append")
+            return
+    if k.dtype not in _VALUE_TYPES or k.dim() != 3:
+        raise MmvError("k and v must be [tokens, heads, dim] of float16 or bfloat16")
+    shape = (k.shape[0], cache.k.shape[1], cache.k.shape[3])
+    (pk, sk), (pv, sv) = _tokens(k, "k", shape, k.dtype), _tokens(v, "v", shape, k.dtype)
+    st = load().mmv_block_append(shape[0], pk, sk, pv, sv, _VALUE_TYPES[k.dtype], _ints(slots, "slots", torch.int64, shape[0]), ref, _stream_ptr(stream))
+    _check(st, "mmv_block_append")
+
+
+def mmv_block_read(cache: BlockCache, table: torch.Tensor, offsets: torch.Tensor, tokens: int | None = None, dtype: torch.dtype = torch.bfloat16,
+                   first: torch.Tensor | None = None, out: tuple | None = None, stream=None) -> tuple:
+    """Keys and values of every request's positions first[r] (0 if left out) to first[r] + offsets[r + 1] - offsets[r] - 1, packed; returns (k, v), two
+    [tokens, heads, dim] of dtype, or `out` filled in: two such tensors, views of others too."""
+    if stream is not None:
+        with _made_current(stream):
+            return mmv_block_read(cache, table, offsets, tokens, dtype, first, out)
+    ref = _blocks(cache)
+    if _marshal is not None:
+        st = _marshal.block_read(ref, table, offsets, first, out, stream)
+        if st is not None:
+            if st:
+                _check(st, "mmv_block_read")
+            return out
+    n = offsets.numel() - 1
+    if n < 0:
+        raise MmvError("offsets must hold the first token of every request, and their number")
+    if out is None:
+        if tokens is None or dtype not in _VALUE_TYPES:
+            raise MmvError("without out, tokens must be their number and dtype float16 or bfloat16")
+        out = tuple(torch.empty(tokens, cache.k.shape[1], cache.k.shape[3], dtype=dtype, device=cache.k.device) for _ in "kv")
+    k, v = out
+    if k.dtype not in _VALUE_TYPES or k.dim() != 3:
+        raise MmvError("out must be two [tokens, heads, dim] of float16 or bfloat16")
+    shape = (k.shape[0], cache.k.shape[1], cache.k.shape[3])
+    (pk, sk), (pv, sv) = _tokens(k, "k", shape, k.dtype), _tokens(v, "v", shape, k.dtype)
+    row, width, stride = _table(table, n)
+    st = load().mmv_block_read(n, shape[0], _ints(offsets, "offsets", torch.int32, n + 1), None if first is None else _ints(first, "first", torch.int32, n),
+                               row, width, stride, ref, _VALUE_TYPES[k.dtype], pk, sk, pv, sv, _stream_ptr(stream))
+    _check(st, "mmv_block_read")
+    return out
+
+
+def mmv_block_attention(q: torch.Tensor, cache: BlockCache, table: torch.Tensor, context: torch.Tensor, scale: float | None = None, window: int = 0,
+                        out: torch.Tensor | None = None, lse: torch.Tensor | None = None, ws: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """mmv_paged_attention over a cache in blocks (and the same workspace)."""
+    if stream is not None:
+        with _made_current(stream):
+            return mmv_block_attention(q, cache, table, context, scale, window, out, lse, ws)
+    ref = _blocks(cache)
+    if _marshal is not None:
+        st = _marshal.block_attention(q, ref, table, context, scale, window, out, lse, ws, stream)
+        if st is not None:
+            if st:
+                _check(st, "mmv_block_attention")
+            return out
+    return _attention("mmv_block_attention", ref, q, cache, table, context, scale, window, out, lse, ws, stream)
+
+
+# ---- the gated delta rule -------------------------------------------------------------------------------------------
+
+
+def _delta_arguments(q, k, v, log_decay, beta, state_in, state_out, state_index, n, out):
+    if q.dtype not in _VALUE_TYPES or q.dim() != 3 or k.dim() != 3 or v.dim() != 3:
+        raise MmvError("q, k and v must be [tokens, heads, dim] of float16 or bfloat16")
+    (t, shared, dk), (heads, dv) = q.shape, v.shape[1:]
+    (pq, sq), (pk, sk), (pv, sv) = _tokens(q, "q", (t, shared, dk), q.dtype), _tokens(k, "k", (t, shared, dk), q.dtype), _tokens(v, "v", (t, heads, dv), q.dtype)
+    for name, x in (("log_decay", log_decay), ("beta", beta)):
+        if tuple(x.shape) != (t, heads):
+            raise MmvError("%s must be [%d, %d] of float32" % (name, t, heads))
+    state = _states(heads, dk, dv, state_in, state_out, state_index, n)
+    out = _out(out, "out", (t, heads, dv), q.dtype, q.device)
+    head = (heads, shared, dk, dv, pq, sq, pk, sk, pv, sv, _VALUE_TYPES[q.dtype])
+    gates = (_ints(log_decay, "log_decay", torch.float32, t * heads), _ints(beta, "beta", torch.float32, t * heads))
+    return t, head, gates, state + (_dev(out, "out"),), out
+
+
+def mmv_delta_attention_workspace_bytes(n: int, tokens: int, heads: int, dk: int, dv: int) -> int:
+    return int(load().mmv_delta_attention_workspace_bytes(n, tokens, heads, dk, dv))
+
+
+def mmv_delta_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, offsets: torch.Tensor, log_decay: torch.Tensor, beta: torch.Tensor,
+                        scale: float | None = None, state_in: torch.Tensor | None = None, state_out: torch.Tensor | None = None,
+                        state_index: torch.Tensor | None = None, out: torch.Tensor | None = None, ws: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """The gated delta rule over packed requests; q and k [tokens, key heads, dk], v [tokens, heads, dv], log_decay and beta [tokens, heads] of fp32, states
+    [states, heads, dk, dv] of fp32; returns out [tokens, heads, dv].  scale: dk ** -0.5 if left out."""
+    if stream is not None:
+        with _made_current(stream):
+            return mmv_delta_attention(q, k, v, offsets, log_decay, beta, scale, state_in, state_out, state_index, out, ws)
+    if _marshal is not None:
+        st = _marshal.delta_attention(q, k, v, offsets, log_decay, beta, scale, state_in, state_out, state_index, out, ws, stream)
+        if st is not None:
+            if st:
+                _check(st, "mmv_delta_attention")
+            return out
+    n = offsets.numel() - 1
+    if n < 0:
+        raise MmvError("offsets must hold the first token of every request, and their number")
+    t, head, gates, state, out = _delta_arguments(q, k, v, log_decay, beta, state_in, state_out, state_index, n, out)
+    w, w_bytes, ws = _ws(ws, mmv_delta_attention_workspace_bytes(n, t, head[0], head[2], head[3]), q.device)
+    st = load().mmv_delta_attention(n, t, *head, _ints(offsets, "offsets", torch.int32, n + 1), *gates, head[2] ** -0.5 if scale is None else scale, *state,
+                                    w, w_bytes, _stream_ptr(stream))
+    _check(st, "mmv_delta_attention")
+    return out
+
+
+def mmv_delta_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_decay: torch.Tensor, beta: torch.Tensor, state_in: torch.Tensor | None = None,
+                   state_out: torch.Tensor | None = None, scale: float | None = None, state_index: torch.Tensor | None = None,
+                   out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """mmv_delta_attention for one token of every request."""
+    if stream is not None:
+        with _made_current(stream):
+            return mmv_delta_step(q, k, v, log_decay, beta, state_in, state_out, scale, state_index, out)
+    if _marshal is not None:
+        st = _marshal.delta_step(q, k, v, log_decay, beta, state_in, state_out, scale, state_index, out, stream)
+        if st is not None:
+            if st:
+                _check(st, "mmv_delta_step")
+            return out
+    t, head, gates, state, out = _delta_arguments(q, k, v, log_decay, beta, state_in, state_out, state_index, q.shape[0], out)
+    st = load().mmv_delta_step(t, *head, *gates, head[2] ** -0.5 if scale is None else scale, *state, _stream_ptr(stream))
+    _check(st, "mmv_delta_step")
     return out

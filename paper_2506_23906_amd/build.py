@@ -10,7 +10,7 @@ from concurrent.futures import ThreadPoolExecutor
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 SRC = os.path.join(HERE, "csrc", "mmvseg.hip")
-SERVING_SRC = os.path.join(HERE, "csrc", "serving.hip")
+SERVING_SRCS = [os.path.join(HERE, "csrc", name) for name in ("serving.hip", "block.hip", "delta.hip")]
 LIB = os.path.join(HERE, "libmmvseg.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 MARSHAL_SRC = os.path.join(HERE, "csrc", "marshal.cpp")
@@ -30,10 +30,11 @@ def build(verbose: bool = False, extra: list[str] | None = None, out: str | None
     tmp = lib + ".tmp.%d" % os.getpid()
     flags = FLAGS + (extra or [])
     compile_flags = [f for f in flags if f != "-shared"]
-    objects = ["%s.%s.tmp.%d.o" % (lib, os.path.basename(src), os.getpid()) for src in (SRC, SERVING_SRC)]
+    sources = [SRC] + SERVING_SRCS
+    objects = ["%s.%s.tmp.%d.o" % (lib, os.path.basename(src), os.getpid()) for src in sources]
     try:
         with ThreadPoolExecutor() as pool:
-            list(pool.map(lambda pair: _hipcc(compile_flags + ["-c", "-o", pair[1], pair[0]], verbose), zip((SRC, SERVING_SRC), objects)))
+            list(pool.map(lambda pair: _hipcc(compile_flags + ["-c", "-o", pair[1], pair[0]], verbose), zip(sources, objects)))
         _hipcc(flags + ["-o", tmp] + objects, verbose)
     finally:
         for o in objects:

@@ -1,0 +1,234 @@
+// libmmvseg, part of the translation unit block.hip (included there, in order).
+// A cache of 8-bit values with a scale for each block of slots and head: written, and read back.
+#pragma once
+
+namespace {
+
+struct BlockCacheParams {
+    void *k, *v;
+    float *k_scales, *v_scales;                        // [pages][heads][blocks of a page]
+    uint64_t page_stride, head_stride, slot_stride;    // values
+    uint32_t heads, page_blocks, block, num_slots, pages;
+    Divider page_of_block, slots, pieces;              // blocks of a page, slots of a block, dim / 8
+};
+
+// Eight values of 8 bits (two words) as fp32, and back: to the nearest, ties to even, at most +-127 or +-448 (NaN stays one in e4m3).
+template <bool kInt8> __device__ __forceinline__ void to_floats(uint2 w, float (&x)[8]) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const uint32_t u = i ? w.y : w.x;
+        if constexpr (kInt8) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[4 * i + j] = (float)(int8_t)(u >> (8 * j));
+        } else {
+            typedef float pair __attribute__((ext_vector_type(2)));
+            const pair a = __builtin_amdgcn_cvt_pk_f32_fp8((int)u, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)u, true);
+            x[4 * i] = a[0], x[4 * i + 1] = a[1], x[4 * i + 2] = b[0], x[4 * i + 3] = b[1];
+        }
+    }
+}
+template <bool kInt8> __device__ __forceinline__ uint32_t to_codes(float a, float b, float c, float d) {
+    if constexpr (kInt8) {
+        const auto code = [](float x) __attribute__((always_inline)) { return (uint32_t)(int)__builtin_rintf(fminf(fmaxf(x, -127.f), 127.f)); };
+        const uint32_t lo = __builtin_amdgcn_perm(code(b), code(a), 0x0c0c0400u), hi = __builtin_amdgcn_perm(code(d), code(c), 0x0c0c0400u);
+        return lo | hi << 16;
+    } else {
+        const auto most = [](float x) __attribute__((always_inline)) { return x > 448.f ? 448.f : x < -448.f ? -448.f : x; };
+        int w = __builtin_amdgcn_cvt_pk_fp8_f32(most(a), most(b), 0, false);
+        return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(most(c), most(d), w, true);
+    }
+}
+template <bool kInt8> __device__ __forceinline__ uint2 to_codes(const float (&x)[8], float by) {
+    return make_uint2(to_codes<kInt8>(x[0] * by, x[1] * by, x[2] * by, x[3] * by), to_codes<kInt8>(x[4] * by, x[5] * by, x[6] * by, x[7] * by));
+}
+template <typename T> __device__ __forceinline__ void values_of(uint4 w, float (&x)[8]) {
+    const T *t = (const T *)&w;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = to_f32(t[i]);
+}
+
+// ---- writing -------------------------------------------------------------------------------------------------------
+//
+// The unit of work is a run: neighbouring tokens whose slots lie in one block.  A wave has the runs that begin among `window` tokens, for one head,
+// the keys or the values: it finds the largest value, makes the block's scale, rounds what the block holds already to that scale where it grows, and
+// writes.  Up to kHeld x 64 pieces of eight values stay in registers from the first read on; longer runs are read twice.
+struct BlockAppendParams {
+    BlockCacheParams c;
+    const void *x[2];              // keys, values
+    uint64_t stride[2];            // from token to token, in values
+    const int64_t *slots;
+    uint32_t tokens, window, first_window, windows;   // windows: of a launch
+};
+constexpr int kHeld = 4;
+constexpr float kLeastLargest = 0x1p-100f;   // what the largest value of a run counts as at least: the scale's reciprocal is finite
+
+template <typename T> constexpr uint32_t kInfinity = __is_same(T, bf16_t) ? 0x7F80u : 0x7C00u;   // bits; above them: not a number
+// Bits of the largest magnitude of eight values (as whole numbers: the order of floats), two side by side.
+__device__ __forceinline__ uint32_t larger_halves(uint32_t a, uint32_t b) {
+    typedef uint16_t pair __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(pair, a), __builtin_bit_cast(pair, b)));
+}
+__device__ __forceinline__ uint32_t largest_bits(uint4 w) {
+    constexpr uint32_t kAbs = 0x7FFF7FFFu;
+    return larger_halves(larger_halves(w.x & kAbs, w.y & kAbs), larger_halves(w.z & kAbs, w.w & kAbs));
+}
+__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) v = max(v, (uint32_t)__shfl_xor((int)v, d));
+    return uniform(v);
+}
+
+template <typename T, bool kInt8> __global__ __launch_bounds__(256) void block_append_kernel(BlockAppendParams P) {
+    const BlockCacheParams &C = P.c;
+    const uint32_t lane = threadIdx.x & 63, unit = uniform(blockIdx.x * 4 + (threadIdx.x >> 6)), pair = unit >> 1, which = unit & 1;
+    const uint32_t in_launch = pair / C.heads, h = pair - in_launch * C.heads;
+    if (in_launch >= P.windows) return;
+    const uint32_t pieces = C.pieces.divisor, from = (P.first_window + in_launch) * P.window;
+    const T *const x = (const T *)(which ? P.x[1] : P.x[0]) + (uint64_t)h * pieces * 8;
+    const uint64_t stride = which ? P.stride[1] : P.stride[0];
+    uint8_t *const codes = (uint8_t *)(which ? C.v : C.k);
+    float *const scales = which ? C.v_scales : C.k_scales;
+    const auto block_of = [&](int64_t slot) __attribute__((always_inline)) { return (uint64_t)slot < C.num_slots ? (int32_t)C.slots.quotient((uint32_t)slot) : -1; };
+    const auto slot_of = [&](uint64_t t) __attribute__((always_inline)) { return t < P.tokens ? P.slots[t] : (int64_t)-1; };
+    // lane l: token from - 1 + l
+    const int64_t slot = from + lane ? slot_of((uint64_t)from + lane - 1) : -1;
+    const int32_t own = block_of(slot), before = __shfl_up(own, 1);
+    uint64_t starts = __ballot(lane >= 1 && lane <= P.window && own >= 0 && own != before);
+    while (starts) {
+        const int l = __builtin_ctzll(starts);
+        starts &= starts - 1;
+        const int32_t block = (int32_t)lane_value((uint32_t)own, l);
+        const uint32_t first = from + l - 1, first_slot = (uint32_t)block * C.block;
+        const uint32_t page = C.page_of_block.quotient((uint32_t)block), in_page = (uint32_t)block - page * C.page_blocks;
+        uint8_t *const to = codes + (uint64_t)page * C.page_stride + (uint64_t)h * C.head_stride + (uint64_t)in_page * C.block * C.slot_stride;
+        float *const scale_at = scales + ((uint64_t)page * C.heads + h) * C.page_blocks + in_page;
+        const float held_scale = *scale_at;
+        // the run's tokens, and whether the block's first slot is among theirs
+        const uint64_t here = __ballot(own == block) >> l, firsts = __ballot((uint64_t)slot == first_slot) >> l;
+        uint32_t count = here == ~0ull ? 64 : __builtin_ctzll(~here);
+        bool anew = (firsts & (count == 64 ? ~0ull : (1ull << count) - 1)) != 0;
+        if (count == 64 - (uint32_t)l) {
+            for (;;) {
+                const int64_t s = slot_of((uint64_t)first + count + lane);
+                const uint64_t same = __ballot(block_of(s) == block);
+                const uint32_t more = same == ~0ull ? 64 : __builtin_ctzll(~same);
+                anew |= (__ballot((uint64_t)s == first_slot) & (more == 64 ? ~0ull : (1ull << more) - 1)) != 0;
+                count += more;
+                if (more < 64) break;
+            }
+        }
+        const uint32_t items = count * pieces;   // (fewer than 2^31: fewer than 2^26 tokens)
+        const auto item = [&](uint32_t id) __attribute__((always_inline)) {
+            const uint32_t row = C.pieces.quotient(id), piece = id - row * pieces;
+            return *(const uint4 *)(x + (uint64_t)(first + row) * stride + 8 * piece);
+        };
+        uint4 held[kHeld];
+        uint32_t largest = 0;
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i) {
+            held[i] = make_uint4(0, 0, 0, 0);
+            if (lane + 64 * i < items) held[i] = item(lane + 64 * i);
+        }
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i) largest = larger_halves(largest, largest_bits(held[i]));
+        for (uint32_t id = lane + 64 * kHeld; id < items; id += 64) largest = larger_halves(largest, largest_bits(item(id)));
+        uint32_t bits = wave_max(max(largest & 0xFFFFu, largest >> 16));
+        bool not_a_number = false;
+        if (bits >= kInfinity<T>) {   // (seldom) infinities count as the type's largest value, what is not a number does not count
+            not_a_number = bits > kInfinity<T>;
+            uint32_t most = 0;
+            for (uint32_t id = lane; id < items; id += 64) {
+                const uint4 w = item(id);
+                const uint16_t *b = (const uint16_t *)&w;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const uint32_t u = b[i] & 0x7FFFu;
+                    most = max(most, u > kInfinity<T> ? 0u : min(u, kInfinity<T> - 1));
+                }
+            }
+            bits = wave_max(most);
+        }
+        const float top = to_f32(__builtin_bit_cast(T, (uint16_t)bits));
+        float wanted = fmaxf(top, kLeastLargest) * (kInt8 ? 1.f / 127.f : 1.f / 448.f);
+        if (kInt8 && not_a_number) wanted = NAN;   // (whole numbers have no code for it: the whole block is none)
+        const float scale = anew || held_scale < wanted ? wanted : held_scale == held_scale && wanted != wanted ? wanted : held_scale;
+        const float inverse = 1.f / scale;
+        if (!anew && held_scale < scale) {
+            const float by = held_scale * inverse;
+            const uint32_t all = C.block * pieces;
+            for (uint32_t id = lane; id < all; id += 64) {
+                const uint32_t row = C.pieces.quotient(id), piece = id - row * pieces;
+                uint2 *const at = (uint2 *)(to + (uint64_t)row * C.slot_stride + 8 * piece);
+                float y[8];
+                to_floats<kInt8>(*at, y);
+                *at = to_codes<kInt8>(y, by);
+            }
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // (stored before the run's own rows, some of which lie there too)
+        }
+        const auto store = [&](uint32_t id, uint4 w) __attribute__((always_inline)) {
+            const uint32_t row = C.pieces.quotient(id), piece = id - row * pieces;
+            const uint32_t in_block = (uint32_t)P.slots[first + row] - first_slot;
+            float y[8];
+            values_of<T>(w, y);
+            *(uint2 *)(to + (uint64_t)in_block * C.slot_stride + 8 * piece) = to_codes<kInt8>(y, inverse);
+        };
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i)
+            if (lane + 64 * i < items) store(lane + 64 * i, held[i]);
+        for (uint32_t id = lane + 64 * kHeld; id < items; id += 64) store(id, item(id));
+        if (lane == 0) *scale_at = scale;
+    }
+}
+
+// ---- reading -------------------------------------------------------------------------------------------------------
+//
+// A thread brings eight values of a key and the same eight of a value: the token's request by bisection, its page, code times scale.
+struct BlockReadParams {
+    BlockCacheParams c;
+    const int32_t *offsets, *first, *table;
+    uint64_t table_stride;
+    uint32_t n, tokens, table_width, first_token;
+    Divider token_pieces, page;      // heads * dim / 8, slots of a page
+    uint64_t total;                  // pieces of a launch
+    void *k, *v;
+    uint64_t k_stride, v_stride;
+};
+
+template <typename T, bool kInt8> __global__ __launch_bounds__(256) void block_read_kernel(BlockReadParams P) {
+    const BlockCacheParams &C = P.c;
+    const uint32_t id = blockIdx.x * 256 + threadIdx.x;
+    if (id >= P.total) return;
+    const uint32_t in_launch = P.token_pieces.quotient(id), inside = id - in_launch * P.token_pieces.divisor, t = P.first_token + in_launch;
+    const uint32_t h = C.pieces.quotient(inside), piece = inside - h * C.pieces.divisor;
+    uint32_t r = 0, hi = P.n;   // the last request that begins at t or before it
+    while (hi - r > 1) {
+        const uint32_t mid = (r + hi) >> 1;
+        if (P.offsets[mid] <= (int32_t)t) r = mid;
+        else hi = mid;
+    }
+    const int32_t begin = P.offsets[r];
+    if ((int32_t)t < begin || (int32_t)t >= P.offsets[r + 1]) return;   // (nobody's)
+    const int64_t position = (int64_t)(t - (uint32_t)begin) + (P.first ? P.first[r] : 0);
+    uint4 out[2] = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
+    const uint32_t where = position >= 0 && position <= 0x7fffffff ? P.page.quotient((uint32_t)position) : ~0u;
+    if (where < P.table_width) {
+        const uint32_t page = (uint32_t)P.table[(uint64_t)r * P.table_stride + where];
+        if (page < C.pages) {
+            const uint32_t slot = (uint32_t)position - where * P.page.divisor, block = C.slots.quotient(slot);
+            const uint64_t at = (uint64_t)page * C.page_stride + (uint64_t)h * C.head_stride + (uint64_t)slot * C.slot_stride + 8 * piece;
+            const uint64_t scale_at = ((uint64_t)page * C.heads + h) * C.page_blocks + block;
+            const uint2 w[2] = {*(const uint2 *)((const uint8_t *)C.k + at), *(const uint2 *)((const uint8_t *)C.v + at)};
+            const float by[2] = {C.k_scales[scale_at], C.v_scales[scale_at]};
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                float y[8];
+                to_floats<kInt8>(w[i], y);
+                out[i] = make_uint4(pack2<T>(y[0] * by[i], y[1] * by[i]), pack2<T>(y[2] * by[i], y[3] * by[i]), pack2<T>(y[4] * by[i], y[5] * by[i]), pack2<T>(y[6] * by[i], y[7] * by[i]));
+            }
+        }
+    }
+    *(uint4 *)((T *)P.k + t * P.k_stride + 8 * inside) = out[0];
+    *(uint4 *)((T *)P.v + t * P.v_stride + 8 * inside) = out[1];
+}
+
+}  // namespace

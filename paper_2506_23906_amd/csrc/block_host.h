@@ -1,0 +1,62 @@
+// libmmvseg, part of the translation unit block.hip (included there, in order).
+// Host side of the calls on a cache of 8-bit values in blocks: argument checks, launches.
+#pragma once
+
+namespace {
+
+constexpr uint64_t kMostAppended = 1ull << 26;   // tokens of a call: the pieces of any run have numbers below 2^31
+
+inline mmv_status check_block_cache(const mmv_block_cache *c) {
+    if (!c) return MMV_ERR_NULL;
+    if (c->type != MMV_TYPE_I8 && c->type != MMV_TYPE_E4M3) return MMV_ERR_INVALID_ARG;
+    if (c->page < 8 || c->page > 65536 || c->heads < 1 || c->heads > kMostHeads || c->dim < 8 || c->dim > 256 || c->dim % 8) return MMV_ERR_INVALID_ARG;
+    if (c->block < 8 || c->block % 8 || c->page % c->block) return MMV_ERR_INVALID_ARG;
+    if (c->pages >= k2to31 || c->pages * c->page >= k2to31 || c->page_stride % 8 || c->head_stride % 8 || c->slot_stride % 8) return MMV_ERR_INVALID_ARG;
+    // (kernels hold the strides of pages and slots in 32 bits, the bytes of seven slots too; heads may lie further apart)
+    if (c->page_stride >= k2to31 || c->head_stride > (1ull << 40) || c->slot_stride >= (1ull << 28)) return MMV_ERR_INVALID_ARG;
+    if (c->pages && (!c->d_k || !c->d_v || !c->d_k_scales || !c->d_v_scales)) return MMV_ERR_NULL;
+    return aligned_to(c->d_k, 16) && aligned_to(c->d_v, 16) && aligned_to(c->d_k_scales, 4) && aligned_to(c->d_v_scales, 4) ? MMV_OK : MMV_ERR_INVALID_ARG;
+}
+inline BlockCacheParams block_cache_params(const mmv_block_cache &c) {
+    BlockCacheParams C = {};
+    C.k = c.d_k, C.v = c.d_v, C.k_scales = c.d_k_scales, C.v_scales = c.d_v_scales;
+    C.page_stride = c.page_stride, C.head_stride = c.head_stride, C.slot_stride = c.slot_stride;
+    C.heads = c.heads, C.page_blocks = c.page / c.block, C.block = c.block, C.num_slots = (uint32_t)(c.pages * c.page), C.pages = (uint32_t)c.pages;
+    C.page_of_block = divider(C.page_blocks), C.slots = divider(c.block), C.pieces = divider(c.dim / 8);
+    return C;
+}
+
+// Tokens whose runs one wave looks after: one where there are few waves' worth of them (every run in a wave of its own, at once), else as many as a
+// block holds: most windows of a prompt then have one run to begin.
+constexpr uint64_t kFewWaves = 16384;
+mmv_status block_append_call(BlockAppendParams P, int type, bool int8, hipStream_t s) {
+    const uint64_t each = 2ull * P.c.heads;
+    P.window = P.tokens * each <= kFewWaves ? 1 : P.c.block < 32 ? P.c.block : 32;
+    const uint64_t windows = ceil_div(P.tokens, P.window), most = ((1ull << 32) - 256) / 64 / each;
+    for (uint64_t first = 0; first < windows; first += most) {
+        P.first_window = (uint32_t)first, P.windows = (uint32_t)(windows - first < most ? windows - first : most);
+        const unsigned blocks = (unsigned)ceil_div(P.windows * each, 4);
+        if (type == MMV_TYPE_F16) int8 ? block_append_kernel<f16_t, true><<<blocks, 256, 0, s>>>(P) : block_append_kernel<f16_t, false><<<blocks, 256, 0, s>>>(P);
+        else int8 ? block_append_kernel<bf16_t, true><<<blocks, 256, 0, s>>>(P) : block_append_kernel<bf16_t, false><<<blocks, 256, 0, s>>>(P);
+        if (const mmv_status st = launched()) return st;
+    }
+    return MMV_OK;
+}
+mmv_status block_read_call(BlockReadParams P, int type, bool int8, hipStream_t s) {
+    const uint64_t each = P.token_pieces.divisor, most = (k2to31 - 256) / each;   // tokens of a launch: its pieces have numbers below 2^31
+    for (uint64_t first = 0; first < P.tokens; first += most) {
+        P.first_token = (uint32_t)first, P.total = (P.tokens - first < most ? P.tokens - first : most) * each;
+        const unsigned blocks = (unsigned)ceil_div(P.total, 256);
+        if (type == MMV_TYPE_F16) int8 ? block_read_kernel<f16_t, true><<<blocks, 256, 0, s>>>(P) : block_read_kernel<f16_t, false><<<blocks, 256, 0, s>>>(P);
+        else int8 ? block_read_kernel<bf16_t, true><<<blocks, 256, 0, s>>>(P) : block_read_kernel<bf16_t, false><<<blocks, 256, 0, s>>>(P);
+        if (const mmv_status st = launched()) return st;
+    }
+    return MMV_OK;
+}
+
+mmv_status block_attention_over(const AttentionParams &P, int type, int cache_type, void *d_ws, hipStream_t s) {
+    if (type == MMV_TYPE_F16) return cache_type == MMV_TYPE_I8 ? attention_call<f16_t, kBlocksInt8>(P, d_ws, s) : attention_call<f16_t, kBlocksE4m3>(P, d_ws, s);
+    return cache_type == MMV_TYPE_I8 ? attention_call<bf16_t, kBlocksInt8>(P, d_ws, s) : attention_call<bf16_t, kBlocksE4m3>(P, d_ws, s);
+}
+
+}  // namespace

@@ -132,29 +132,6 @@ struct PromptParams {
     uint32_t first_block, first_request;   // of a launch
 };
 
-__device__ __forceinline__ f32x4 mfma_bf16(u32x4 a, u32x4 b, f32x4 c) { return mfma_16x16x32(bf16_t(), a, b, c); }
-__device__ __forceinline__ float low_half(uint32_t w) { return __builtin_bit_cast(float, w << 16); }
-__device__ __forceinline__ float high_half(uint32_t w) { return __builtin_bit_cast(float, w & 0xFFFF0000u); }
-// Two values into kTerms words of bf16 pairs: the upper halves of what is left each time, the last of it rounded.
-template <int kTerms> __device__ __forceinline__ void take_apart(float a, float b, uint32_t (&to)[kTerms]) {
-#pragma unroll
-    for (int i = 0; i + 1 < kTerms; ++i) {
-        to[i] = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, b), __builtin_bit_cast(uint32_t, a), 0x07060302u);
-        a -= high_half(__builtin_bit_cast(uint32_t, a)), b -= high_half(__builtin_bit_cast(uint32_t, b));
-    }
-    to[kTerms - 1] = pack2<bf16_t>(a, b);
-}
-// A word of two inputs as its bf16 terms.
-template <typename T, int kTerms> __device__ __forceinline__ void input_terms(uint32_t w, uint32_t (&to)[kTerms]) {
-    if constexpr (kTerms == 1) {
-        to[0] = w;
-    } else {
-        typedef f16_t pair __attribute__((ext_vector_type(2)));
-        const pair h = __builtin_bit_cast(pair, w);
-        take_apart<kTerms>((float)h[0], (float)h[1], to);
-    }
-}
-
 // Tokens of a block: the fewest that need no more than the blocks there are, so that the workgroups come in whole rounds of what the device holds.  (Up to 64
 // requests the lengths decide; for more, what is enough for any lengths.  Every workgroup finds the same.)
 __device__ __forceinline__ uint32_t wave_sum32(uint32_t v) {

@@ -1,0 +1,52 @@
+// libmmvseg, part of the translation unit delta.hip (included there, in order).
+// Host side of the gated delta rule: argument checks, workspaces, launches.
+#pragma once
+
+namespace {
+
+inline bool delta_sizes(uint64_t n, uint64_t tokens, uint32_t heads, uint32_t k_heads, uint32_t dk, uint32_t dv) {
+    return n < kMostRequests && tokens < k2to31 && heads >= 1 && heads <= kMostHeads && k_heads >= 1 && k_heads <= heads && heads % k_heads == 0 && dk >= 8 && dk <= kMostDk &&
+           dk % 8 == 0 && dv >= 8 && dv <= kMostDv && dv % 8 == 0 && n * heads < k2to31;
+}
+mmv_status delta_params(DeltaParams &P, uint64_t n, uint64_t tokens, uint32_t heads, uint32_t k_heads, uint32_t dk, uint32_t dv, const void *q, uint64_t q_stride, const void *k,
+                        uint64_t k_stride, const void *v, uint64_t v_stride, int type, const float *log_decay, const float *beta, float scale, const float *state_in,
+                        float *state_out, uint64_t states, const int32_t *state_index, void *out) {
+    if (!valid_value_type(type) || states >= k2to31 || q_stride % 8 || k_stride % 8 || v_stride % 8) return MMV_ERR_INVALID_ARG;
+    if (tokens > 1 && (q_stride < (uint64_t)k_heads * dk || k_stride < (uint64_t)k_heads * dk || v_stride < (uint64_t)heads * dv)) return MMV_ERR_INVALID_ARG;
+    if (q_stride > kMostStride || k_stride > kMostStride || v_stride > kMostStride) return MMV_ERR_INVALID_ARG;
+    if (!state_index && (state_in || state_out) && states < n) return MMV_ERR_INVALID_ARG;
+    if (tokens && n && (!q || !k || !v || !out || !log_decay || !beta)) return MMV_ERR_NULL;
+    for (const void *p : {q, k, v, (const void *)out, (const void *)state_in, (const void *)state_out})
+        if (!aligned_to(p, 16)) return MMV_ERR_INVALID_ARG;
+    if (!aligned_to(log_decay, 4) || !aligned_to(beta, 4) || !aligned_to(state_index, 4)) return MMV_ERR_INVALID_ARG;
+    const uint64_t bytes = states * heads * dk * dv * 4;
+    if (state_in && state_out && state_in != state_out && (uintptr_t)state_in < (uintptr_t)state_out + bytes && (uintptr_t)state_out < (uintptr_t)state_in + bytes)
+        return MMV_ERR_INVALID_ARG;
+    P.q = q, P.k = k, P.v = v, P.q_stride = q_stride, P.k_stride = k_stride, P.v_stride = v_stride, P.tokens = tokens;
+    if (tokens <= 1) P.q_stride = P.k_stride = (uint64_t)k_heads * dk, P.v_stride = (uint64_t)heads * dv;   // (not checked above: no second token)
+    P.log_decay = log_decay, P.beta = beta, P.state_in = state_in, P.state_out = state_out, P.state_index = state_index, P.states = states, P.out = out;
+    P.n = (uint32_t)n, P.heads = heads, P.group = heads / k_heads, P.dk = dk, P.dv = dv, P.scale = scale;
+    return MMV_OK;
+}
+
+// Columns of a workgroup: equal shares of at most 128, in eights; threads of the same columns: as many as there is room for, a power of two.
+template <typename T> mmv_status launch_tokens(DeltaParams P, hipStream_t s) {
+    const uint32_t slices = (P.dv + 127) / 128, slice = (uint32_t)ceil_div(P.dv, 8 * slices) * 8;
+    uint32_t step = 64;
+    while (step * (slice / 4) > 256) step /= 2;
+    const uint32_t rows = (uint32_t)ceil_div(P.dk, step), each = P.heads * slices, most = most_of_a_launch(256, each);   // rows: of a thread
+    for (; P.first < P.n; P.first += most) {
+        const uint32_t blocks = (P.n - P.first < most ? P.n - P.first : most) * each;
+        if (rows <= 4) delta_tokens_kernel<T, 4><<<blocks, 256, 0, s>>>(P, slices, slice, step);
+        else if (rows <= 8) delta_tokens_kernel<T, 8><<<blocks, 256, 0, s>>>(P, slices, slice, step);
+        else delta_tokens_kernel<T, 16><<<blocks, 256, 0, s>>>(P, slices, slice, step);
+        if (const mmv_status st = launched()) return st;
+    }
+    return MMV_OK;
+}
+mmv_status delta_step_call(const DeltaParams &P, int type, hipStream_t s) { return type == MMV_TYPE_F16 ? launch_tokens<f16_t>(P, s) : launch_tokens<bf16_t>(P, s); }
+
+inline size_t delta_workspace(uint64_t, uint64_t, uint32_t, uint32_t, uint32_t) { return 0; }
+mmv_status delta_call(const DeltaParams &P, int type, void *, hipStream_t s) { return type == MMV_TYPE_F16 ? launch_tokens<f16_t>(P, s) : launch_tokens<bf16_t>(P, s); }
+
+}  // namespace

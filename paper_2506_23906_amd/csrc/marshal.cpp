@@ -167,6 +167,11 @@ struct {
     decltype(&mmv_paged_attention) paged_attention;
     decltype(&mmv_decay_attention) decay_attention;
     decltype(&mmv_decay_step) decay_step;
+    decltype(&mmv_block_append) block_append;
+    decltype(&mmv_block_read) block_read;
+    decltype(&mmv_block_attention) block_attention;
+    decltype(&mmv_delta_attention) delta_attention;
+    decltype(&mmv_delta_step) delta_step;
 } g_serving;
 
 const at::Tensor &tensor(PyObject *o, at::ScalarType type) {
@@ -221,9 +226,9 @@ uint32_t number32(PyObject *o) {
     if (v < 0 || v > 0x7fffffffL) throw LeftToPython();
     return (uint32_t)v;
 }
-const mmv_paged_cache *cache_of(PyObject *address) {
+template <typename Cache = mmv_paged_cache> const Cache *cache_of(PyObject *address) {   // (the address of binding.py's own structure)
     if (!PyLong_CheckExact(address)) throw LeftToPython();
-    return (const mmv_paged_cache *)PyLong_AsVoidPtr(address);
+    return (const Cache *)PyLong_AsVoidPtr(address);
 }
 struct Scratch {
     void *ptr;
@@ -252,24 +257,24 @@ PyObject *page_tables(PyObject *, PyObject *const *a, Py_ssize_t count) {
         return g_serving.page_tables(n, cached, fresh, free_pages, free_count, table.ptr, table.width, table.stride, page, most, offsets, context, slots, positions, used, ws.ptr, ws.bytes, s);
     });
 }
-// cache_append(k, v, slots, address of the cache, stream)
-PyObject *cache_append(PyObject *, PyObject *const *a, Py_ssize_t count) {
+// cache_append, block_append(k, v, slots, address of the cache, stream)
+template <typename Cache, typename Entry> PyObject *append(Entry entry, PyObject *const *a, Py_ssize_t count) {
     return guarded(count, 5, [&] {
         const at::ScalarType type = value_of(a[0], 3);
-        const mmv_paged_cache *cache = cache_of(a[3]);
+        const Cache *cache = cache_of<Cache>(a[3]);
         const int64_t n = THPVariable_Unpack(a[0]).size(0);
         const Tokens k = tokens(a[0], type, n, cache->heads, cache->dim), v = tokens(a[1], type, n, cache->heads, cache->dim);
         const auto *slots = array_of<const int64_t>(a[2], at::kLong, n);
         void *const s = stream(a[4]);
         WithoutGil free;
-        return g_serving.cache_append(n, k.ptr, k.stride, v.ptr, v.stride, type_of(type), slots, cache, s);
+        return entry(n, k.ptr, k.stride, v.ptr, v.stride, type_of(type), slots, cache, s);
     });
 }
-// paged_attention(q, address of the cache, table, context, scale, window, out, lse, ws, stream)
-PyObject *paged_attention(PyObject *, PyObject *const *a, Py_ssize_t count) {
+// paged_attention, block_attention(q, address of the cache, table, context, scale, window, out, lse, ws, stream)
+template <typename Cache, typename Entry> PyObject *attention(Entry entry, PyObject *const *a, Py_ssize_t count) {
     return guarded(count, 10, [&] {
         const at::ScalarType type = value_of(a[0], 3);
-        const mmv_paged_cache *cache = cache_of(a[1]);
+        const Cache *cache = cache_of<Cache>(a[1]);
         const at::Tensor &t = THPVariable_Unpack(a[0]);
         const int64_t n = t.size(0), heads = t.size(1), dim = cache->dim;
         const Tokens q = tokens(a[0], type, n, heads, dim);
@@ -282,19 +287,54 @@ PyObject *paged_attention(PyObject *, PyObject *const *a, Py_ssize_t count) {
         const Scratch ws = scratch(a[8]);
         void *const s = stream(a[9]);
         WithoutGil free;
-        return g_serving.paged_attention(n, heads, q.ptr, q.stride, type_of(type), cache, table.ptr, table.width, table.stride, context, scale, window, out, lse, ws.ptr, ws.bytes, s);
+        return entry(n, heads, q.ptr, q.stride, type_of(type), cache, table.ptr, table.width, table.stride, context, scale, window, out, lse, ws.ptr, ws.bytes, s);
     });
 }
-// What both recurrences take: q, k, v, log_decay, scale, state_in, state_out, state_index, out
+PyObject *cache_append(PyObject *, PyObject *const *a, Py_ssize_t n) { return append<mmv_paged_cache>(g_serving.cache_append, a, n); }
+PyObject *block_append(PyObject *, PyObject *const *a, Py_ssize_t n) { return append<mmv_block_cache>(g_serving.block_append, a, n); }
+PyObject *paged_attention(PyObject *, PyObject *const *a, Py_ssize_t n) { return attention<mmv_paged_cache>(g_serving.paged_attention, a, n); }
+PyObject *block_attention(PyObject *, PyObject *const *a, Py_ssize_t n) { return attention<mmv_block_cache>(g_serving.block_attention, a, n); }
+// block_read(address of the cache, table, offsets, first, out, stream)
+PyObject *block_read(PyObject *, PyObject *const *a, Py_ssize_t count) {
+    return guarded(count, 6, [&] {
+        const mmv_block_cache *cache = cache_of<mmv_block_cache>(a[0]);
+        if (!PyTuple_CheckExact(a[4]) || PyTuple_GET_SIZE(a[4]) != 2) throw LeftToPython();
+        PyObject *const ok = PyTuple_GET_ITEM(a[4], 0), *const ov = PyTuple_GET_ITEM(a[4], 1);
+        const at::ScalarType type = value_of(ok, 3);
+        const int64_t n = tensor(a[2], at::kInt).numel() - 1, count_out = THPVariable_Unpack(ok).size(0);
+        if (n < 0) throw LeftToPython();
+        const auto *offsets = array_of<const int32_t>(a[2], at::kInt, n + 1), *first = a[3] == Py_None ? nullptr : array_of<const int32_t>(a[3], at::kInt, n);
+        const Rows table = rows(a[1], n);
+        const Tokens k = tokens(ok, type, count_out, cache->heads, cache->dim), v = tokens(ov, type, count_out, cache->heads, cache->dim);
+        void *const s = stream(a[5]);
+        WithoutGil free;
+        return g_serving.block_read(n, count_out, offsets, first, table.ptr, table.width, table.stride, cache, type_of(type), (void *)k.ptr, k.stride, (void *)v.ptr, v.stride, s);
+    });
+}
+// What the recurrences take: q, k, v, log_decay (the delta rule beta too), scale, state_in, state_out, state_index, out
 struct Recurrence {
     at::ScalarType type;
     int64_t n, heads, kv, dk, dv;
     Tokens q, k, v;
-    const float *log_decay, *in;
+    const float *log_decay, *beta, *in;
     float *out_states, scale;
     uint64_t states;
     const int32_t *index;
     void *out;
+    void set_states(PyObject *from, PyObject *to, PyObject *which, PyObject *result, int64_t requests) {   // (fewer than 0: one for each token)
+        int64_t count = -1;
+        const auto state = [&](PyObject *o) -> float * {
+            if (o == Py_None) return nullptr;
+            const at::Tensor &t = tensor(o, at::kFloat);
+            if (!t.is_contiguous() || t.dim() != 4 || t.size(1) != heads || t.size(2) != dk || t.size(3) != dv || (count >= 0 && t.size(0) != count)) throw LeftToPython();
+            count = t.size(0);
+            return (float *)t.data_ptr();
+        };
+        in = state(from), out_states = state(to);
+        states = count < 0 ? 0 : count;
+        index = which == Py_None ? nullptr : array_of<const int32_t>(which, at::kInt, requests < 0 ? n : requests);
+        out = shaped<void>(result, type, {n, heads, dv});
+    }
 };
 Recurrence recurrence(PyObject *q, PyObject *k, PyObject *v, PyObject *log_decay, PyObject *scale, PyObject *in, PyObject *out_states, PyObject *index, PyObject *out, int64_t requests) {
     Recurrence R = {};
@@ -305,18 +345,7 @@ Recurrence recurrence(PyObject *q, PyObject *k, PyObject *v, PyObject *log_decay
     R.q = tokens(q, R.type, R.n, R.heads, R.dk), R.k = tokens(k, R.type, R.n, R.kv, R.dk), R.v = tokens(v, R.type, R.n, R.kv, R.dv);
     R.log_decay = array_of<const float>(log_decay, at::kFloat, R.heads);
     R.scale = real(scale);
-    int64_t states = -1;
-    const auto state = [&](PyObject *o) -> float * {
-        if (o == Py_None) return nullptr;
-        const at::Tensor &t = tensor(o, at::kFloat);
-        if (!t.is_contiguous() || t.dim() != 4 || t.size(1) != R.heads || t.size(2) != R.dk || t.size(3) != R.dv || (states >= 0 && t.size(0) != states)) throw LeftToPython();
-        states = t.size(0);
-        return (float *)t.data_ptr();
-    };
-    R.in = state(in), R.out_states = state(out_states);
-    R.states = states < 0 ? 0 : states;
-    R.index = index == Py_None ? nullptr : array_of<const int32_t>(index, at::kInt, requests < 0 ? R.n : requests);
-    R.out = shaped<void>(out, R.type, {R.n, R.heads, R.dv});
+    R.set_states(in, out_states, index, out, requests);
     return R;
 }
 // decay_attention(q, k, v, offsets, log_decay, scale, state_in, state_out, state_index, out, ws, stream)
@@ -343,19 +372,58 @@ PyObject *decay_step(PyObject *, PyObject *const *a, Py_ssize_t count) {
                                     R.states, R.index, R.out, s);
     });
 }
-// bind_serving(addresses of mmv_page_tables, mmv_cache_append, mmv_paged_attention, mmv_decay_attention, mmv_decay_step)
+Recurrence delta_rule(PyObject *q, PyObject *k, PyObject *v, PyObject *log_decay, PyObject *beta, PyObject *scale, PyObject *in, PyObject *out_states, PyObject *index, PyObject *out,
+                      int64_t requests) {
+    Recurrence R = {};
+    R.type = value_of(q, 3);
+    value_of(v, 3);
+    const at::Tensor &tq = THPVariable_Unpack(q), &tv = THPVariable_Unpack(v);
+    R.n = tq.size(0), R.kv = tq.size(1), R.dk = tq.size(2), R.heads = tv.size(1), R.dv = tv.size(2);
+    R.q = tokens(q, R.type, R.n, R.kv, R.dk), R.k = tokens(k, R.type, R.n, R.kv, R.dk), R.v = tokens(v, R.type, R.n, R.heads, R.dv);
+    R.log_decay = shaped<const float>(log_decay, at::kFloat, {R.n, R.heads}), R.beta = shaped<const float>(beta, at::kFloat, {R.n, R.heads});
+    R.scale = real(scale);
+    R.set_states(in, out_states, index, out, requests);
+    return R;
+}
+// delta_attention(q, k, v, offsets, log_decay, beta, scale, state_in, state_out, state_index, out, ws, stream)
+PyObject *delta_attention(PyObject *, PyObject *const *a, Py_ssize_t count) {
+    return guarded(count, 13, [&] {
+        const int64_t n = tensor(a[3], at::kInt).numel() - 1;
+        if (n < 0) throw LeftToPython();
+        const auto *offsets = array_of<const int32_t>(a[3], at::kInt, n + 1);
+        const Recurrence R = delta_rule(a[0], a[1], a[2], a[4], a[5], a[6], a[7], a[8], a[9], a[10], n);
+        const Scratch ws = scratch(a[11]);
+        void *const s = stream(a[12]);
+        WithoutGil free;
+        return g_serving.delta_attention(n, R.n, R.heads, R.kv, R.dk, R.dv, R.q.ptr, R.q.stride, R.k.ptr, R.k.stride, R.v.ptr, R.v.stride, type_of(R.type), offsets, R.log_decay, R.beta,
+                                         R.scale, R.in, R.out_states, R.states, R.index, R.out, ws.ptr, ws.bytes, s);
+    });
+}
+// delta_step(q, k, v, log_decay, beta, state_in, state_out, scale, state_index, out, stream)
+PyObject *delta_step(PyObject *, PyObject *const *a, Py_ssize_t count) {
+    return guarded(count, 11, [&] {
+        const Recurrence R = delta_rule(a[0], a[1], a[2], a[3], a[4], a[7], a[5], a[6], a[8], a[9], -1);
+        void *const s = stream(a[10]);
+        WithoutGil free;
+        return g_serving.delta_step(R.n, R.heads, R.kv, R.dk, R.dv, R.q.ptr, R.q.stride, R.k.ptr, R.k.stride, R.v.ptr, R.v.stride, type_of(R.type), R.log_decay, R.beta, R.scale, R.in,
+                                    R.out_states, R.states, R.index, R.out, s);
+    });
+}
+// bind_serving(addresses of mmv_page_tables, mmv_cache_append, mmv_paged_attention, mmv_decay_attention, mmv_decay_step, mmv_block_append, mmv_block_read,
+// mmv_block_attention, mmv_delta_attention, mmv_delta_step)
 PyObject *bind_serving(PyObject *, PyObject *const *a, Py_ssize_t count) {
-    void *p[5];
-    if (count != 5) {
-        PyErr_SetString(PyExc_TypeError, "bind_serving takes five addresses");
+    void *p[10];
+    if (count != 10) {
+        PyErr_SetString(PyExc_TypeError, "bind_serving takes ten addresses");
         return nullptr;
     }
-    for (int i = 0; i < 5; ++i) {
+    for (int i = 0; i < 10; ++i) {
         p[i] = PyLong_AsVoidPtr(a[i]);
         if (!p[i] && PyErr_Occurred()) return nullptr;
     }
     g_serving = {(decltype(&mmv_page_tables))p[0], (decltype(&mmv_cache_append))p[1], (decltype(&mmv_paged_attention))p[2], (decltype(&mmv_decay_attention))p[3],
-                 (decltype(&mmv_decay_step))p[4]};
+                 (decltype(&mmv_decay_step))p[4], (decltype(&mmv_block_append))p[5], (decltype(&mmv_block_read))p[6], (decltype(&mmv_block_attention))p[7],
+                 (decltype(&mmv_delta_attention))p[8], (decltype(&mmv_delta_step))p[9]};
     Py_RETURN_NONE;
 }
 
@@ -379,7 +447,8 @@ PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t count) {
 PyMethodDef g_methods[] = {MMV_METHOD(bind),     MMV_METHOD(segscan),      MMV_METHOD(segsum),       MMV_METHOD(scan),
                            MMV_METHOD(compress), MMV_METHOD(spmv_coo),     MMV_METHOD(spmv_csr),     MMV_METHOD(spmv_coo_run),
                            MMV_METHOD(spmv_csr_run), MMV_METHOD(page_tables),  MMV_METHOD(cache_append), MMV_METHOD(paged_attention),
-                           MMV_METHOD(decay_attention), MMV_METHOD(decay_step), MMV_METHOD(bind_serving), {nullptr, nullptr, 0, nullptr}};
+                           MMV_METHOD(decay_attention), MMV_METHOD(decay_step), MMV_METHOD(block_append), MMV_METHOD(block_read), MMV_METHOD(block_attention),
+                           MMV_METHOD(delta_attention), MMV_METHOD(delta_step), MMV_METHOD(bind_serving), {nullptr, nullptr, 0, nullptr}};
 #undef MMV_METHOD
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_marshal", "Argument marshalling of the calls of libmmvseg.so.", -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -22,6 +22,14 @@ namespace {
 // No LDS and no barrier in the loop.  Query heads beyond the group's are zero columns: the matrix cores have the time (about a tenth of
 // what the loads take).  Whole calls: 48 ragged rows of up to 8192 positions (330 MB in bf16) 68.2 us, 62 of them in the list's kernel, 5.3 TB/s;
 // 16 of up to 65536 (717 MB in e4m3) 123 us, 117 of them, 6.1 TB/s; one row of 1000 9.5 us, the lives of two launches.
+//
+// Kinds of caches: 16-bit values of the queries' type, e4m3 with one scale for all keys and one for all values (factors of all scores and of the result), and
+// 8-bit values (e4m3, whole numbers) with a scale for each block of slots and head.  A block has a multiple of 8 slots and a lane eight consecutive positions in
+// both products, so that a lane needs one scale of each kind for a tile: a factor of its scores, and of its probabilities before they meet the values.
+enum : int { kSixteenBits, kE4m3, kBlocksE4m3, kBlocksInt8 };
+constexpr bool eight_bits(int cache) { return cache != kSixteenBits; }
+constexpr bool in_blocks(int cache) { return cache == kBlocksE4m3 || cache == kBlocksInt8; }
+
 struct AttentionParams {
     const void *q, *k, *v;
     uint64_t q_stride, head_stride;                // elements
@@ -35,32 +43,33 @@ struct AttentionParams {
     uint32_t n, q_heads, heads, group, dim, page, pages, window, max_context, workers;
     uint32_t first_row;                            // of a joining launch
     Divider page_groups;                           // page / 8
+    Divider block_groups;                          // (caches in blocks) block / 8
+    uint32_t head_scales;                          // blocks of a page
+    const float *k_scales, *v_scales;              // [pages][heads][blocks of a page]
     float score_by, out_by;                        // scale * k_scale * log2(e), v_scale / 2^kScaleBits
 };
 constexpr uint32_t kTile = 32;                     // positions
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.693147180559945309417f;
 
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-typedef bf16_t bf16x8 __attribute__((ext_vector_type(8)));
-typedef f16_t f16x8 __attribute__((ext_vector_type(8)));
-__device__ __forceinline__ f32x4 mfma_16x16x32(bf16_t, u32x4 a, u32x4 b, f32x4 c) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
-}
-__device__ __forceinline__ f32x4 mfma_16x16x32(f16_t, u32x4 a, u32x4 b, f32x4 c) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
-}
-template <typename T> __device__ __forceinline__ uint32_t pack2(float a, float b) {
-    typedef T pair __attribute__((ext_vector_type(2)));
-    return __builtin_bit_cast(uint32_t, (pair){from_f32<T>(a), from_f32<T>(b)});
-}
 // Two of a word's four 8-bit values as 16-bit ones (exact).
 template <bool kHigh> __device__ __forceinline__ uint32_t widen(bf16_t, uint32_t w) {
     return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)w, 1.f, kHigh));
 }
 template <bool kHigh> __device__ __forceinline__ uint32_t widen(f16_t, uint32_t w) {
     return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)w, 1.f, kHigh));
+}
+// The same of whole numbers: at most 8 bits, exact in both types.
+template <bool kHigh> __device__ __forceinline__ uint32_t widen_int8(bf16_t, uint32_t w) {
+    const float a = (float)(int8_t)(w >> (kHigh ? 16 : 0)), b = (float)(int8_t)(w >> (kHigh ? 24 : 8));
+    return __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, b), __builtin_bit_cast(uint32_t, a), 0x07060302u);
+}
+template <bool kHigh> __device__ __forceinline__ uint32_t widen_int8(f16_t, uint32_t w) {
+    const float a = (float)(int8_t)(w >> (kHigh ? 16 : 0)), b = (float)(int8_t)(w >> (kHigh ? 24 : 8));
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(a, b));
+}
+template <int kCache, bool kHigh, typename T> __device__ __forceinline__ uint32_t widen_of(T t, uint32_t w) {
+    if constexpr (kCache == kBlocksInt8) return widen_int8<kHigh>(t, w);
+    else return widen<kHigh>(t, w);
 }
 // Probabilities meet the values in 16 bits, as the matrix cores take both operands of one type, and as terms, each what is cut off at the type's precision of what the ones before it
 // left, the last one rounded: three in bf16 (24 bits), two in fp16 (22).  Rounded once they would add as much error as the rounding of the result (1.4 times the error of exact
@@ -136,14 +145,23 @@ __device__ __forceinline__ void enter_row(const AttentionParams &P, Place &at, i
 template <int KS> constexpr int dims_per_lane() { return KS <= 2 ? 4 : KS <= 4 ? 8 : KS <= 6 ? 12 : 16; }
 template <int KS> constexpr int certain_pieces() { return KS <= 2 ? 1 : KS == 3 ? 9 : KS == 4 ? 13 : KS == 5 ? 17 : 21; }   // of 8 dims, of any dim that takes this KS
 
+// The type in which probabilities and values meet.  Probabilities times a block's scale have any size: bf16, whatever the queries' type (8-bit values are exact in it).
+template <typename T, int kCache> struct ValueOperandOf { using type = T; };
+template <typename T> struct ValueOperandOf<T, kBlocksE4m3> { using type = bf16_t; };
+template <typename T> struct ValueOperandOf<T, kBlocksInt8> { using type = bf16_t; };
+template <typename T, int kCache> using ValueOperand = typename ValueOperandOf<T, kCache>::type;
+
 // kExact: dim = 32 KS, and a slot's values lie behind those of the slot before.  kStream: loads that leave the caches to others.
-template <int KS, bool kExact, bool kStream, typename T, bool kE4m3> struct Tile {
+template <int KS, bool kExact, bool kStream, typename T, int kCache> struct Tile {
     static constexpr int kDims = dims_per_lane<KS>();
-    static constexpr int kSize = kE4m3 ? 1 : 2;
-    static constexpr int kKeyWords = kE4m3 ? 2 : 4, kValueWords = kE4m3 ? kDims / 4 : kDims / 2;
+    static constexpr bool kEight = eight_bits(kCache), kBlocks = in_blocks(kCache);
+    using V = ValueOperand<T, kCache>;
+    static constexpr int kSize = kEight ? 1 : 2;
+    static constexpr int kKeyWords = kEight ? 2 : 4, kValueWords = kEight ? kDims / 4 : kDims / 2;
     uint32_t k[2][KS][kKeyWords], v[8][kValueWords];
     const char *pk, *pv;
     uint32_t pages_ok;   // bit i: the page of positions 8 i .. 8 i + 7 is there
+    float k_scale, v_scale;   // (caches in blocks) of the lane's eight positions
 
     // Addresses of a tile's rows for this lane.  Pages are looked up for 8 positions at a time: those of the lane's keys are the
     // (r / 4)th of the tile's four, those of its values and scores the g-th.
@@ -156,6 +174,7 @@ template <int KS, bool kExact, bool kStream, typename T, bool kE4m3> struct Tile
             off[0] = place_of(P, scalar_load(row + page), group - page * P.page_groups.divisor, 15u);
 #pragma unroll
             for (int i = 1; i < 4; ++i) off[i] = off[0] + (uint64_t)(8 * i) * slot_stride(P);
+            if constexpr (kBlocks) load_scales(P, at.head, pages_ok ? (uint32_t)scalar_load(row + page) : 0u, group - page * P.page_groups.divisor + g);
         } else {
             int32_t id[4];
             uint32_t inside[4];
@@ -168,6 +187,10 @@ template <int KS, bool kExact, bool kStream, typename T, bool kE4m3> struct Tile
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i) off[i] = place_of(P, id[i], inside[i], 1u << i);
+            if constexpr (kBlocks) {
+                const uint32_t own = pick(id, g);
+                load_scales(P, at.head, own < P.pages ? own : 0u, pick(inside, g));
+            }
         }
         const uint64_t head = (uint64_t)at.head * P.head_stride;
         const uint64_t ok_ = head + pick(off, r >> 2) + (r & 3) * slot_stride(P), ov = head + pick(off, g);
@@ -180,9 +203,14 @@ template <int KS, bool kExact, bool kStream, typename T, bool kE4m3> struct Tile
         pages_ok |= ok ? bits : 0u;
         return (uint64_t)(ok ? (uint32_t)id : 0u) * P.page_stride + (uint64_t)(inside * 8) * slot_stride(P);
     }
-    static __device__ __forceinline__ uint64_t pick(const uint64_t (&off)[4], uint32_t i) {
-        const uint64_t a = i & 1 ? off[1] : off[0], b = i & 1 ? off[3] : off[2];
+    template <typename N> static __device__ __forceinline__ N pick(const N (&off)[4], uint32_t i) {
+        const N a = i & 1 ? off[1] : off[0], b = i & 1 ? off[3] : off[2];
         return i & 2 ? b : a;
+    }
+    // The scales of eight positions, `inside` of them (in eights) into a page.
+    __device__ __forceinline__ void load_scales(const AttentionParams &P, uint32_t head, uint32_t page, uint32_t inside) {
+        const uint64_t i = ((uint64_t)page * P.heads + head) * P.head_scales + P.block_groups.quotient(inside);
+        k_scale = P.k_scales[i], v_scale = P.v_scales[i];
     }
     static __device__ __forceinline__ uint32_t page_of(const AttentionParams &P, uint32_t g8) { return P.page_groups.quotient(g8); }
     static __device__ __forceinline__ uint32_t slot_stride(const AttentionParams &P) { return kExact ? 32 * KS : P.slot_stride; }
@@ -201,7 +229,7 @@ template <int KS, bool kExact, bool kStream, typename T, bool kE4m3> struct Tile
             const char *p = pk + (uint32_t)(t * 4 * kSize) * slot_stride(P);
 #pragma unroll
             for (int s = 0; s < KS; ++s) {
-                if constexpr (kExact && kE4m3) {   // 16 bytes for two steps: the dims of a step are those of this layout, of the queries too
+                if constexpr (kExact && kEight) {   // 16 bytes for two steps: the dims of a step are those of this layout, of the queries too
                     if (s % 2 == 0) {
                         uint32_t both[4];
                         load(both, p + s * 32 + g * 16);
@@ -236,7 +264,7 @@ template <int KS, bool kExact, bool kStream, typename T, bool kE4m3> struct Tile
         }
     }
     // The lane's dims of step s: 8 from this one on.
-    static __device__ __forceinline__ uint32_t step_dim(int s, uint32_t g) { return kExact && kE4m3 ? (s / 2) * 64 + g * 16 + (s % 2) * 8 : s * 32 + g * 8; }
+    static __device__ __forceinline__ uint32_t step_dim(int s, uint32_t g) { return kExact && kEight ? (s / 2) * 64 + g * 16 + (s % 2) * 8 : s * 32 + g * 8; }
     __device__ __forceinline__ void scores(const AttentionParams &P, const u32x4 (&q)[KS], uint32_t g, f32x4 (&S)[2]) const {
         const uint32_t pieces = P.dim / 8;
 #pragma unroll
@@ -245,8 +273,8 @@ template <int KS, bool kExact, bool kStream, typename T, bool kE4m3> struct Tile
 #pragma unroll
             for (int s = 0; s < KS; ++s) {
                 u32x4 a;
-                if constexpr (kE4m3) {
-                    a = (u32x4){widen<false>(T(), k[t][s][0]), widen<true>(T(), k[t][s][0]), widen<false>(T(), k[t][s][1]), widen<true>(T(), k[t][s][1])};
+                if constexpr (kEight) {
+                    a = (u32x4){widen_of<kCache, false>(T(), k[t][s][0]), widen_of<kCache, true>(T(), k[t][s][0]), widen_of<kCache, false>(T(), k[t][s][1]), widen_of<kCache, true>(T(), k[t][s][1])};
                 } else {
                     a = (u32x4){k[t][s][0], k[t][s][1], k[t][s][2], k[t][s][3]};
                 }
@@ -264,21 +292,21 @@ template <int KS, bool kExact, bool kStream, typename T, bool kE4m3> struct Tile
         u32x4 a;
 #pragma unroll
         for (int m = 0; m < 4; ++m) {
-            if constexpr (kE4m3) {
+            if constexpr (kEight) {
                 constexpr uint32_t at = c & 3;
                 const uint32_t both = __builtin_amdgcn_perm(v[2 * m + 1][c / 4], v[2 * m][c / 4], at < 2 ? 0x05010400u : 0x07030602u);   // two components of both positions
-                a[m] = widen<(at & 1) != 0>(T(), both);
+                a[m] = widen_of<kCache, (at & 1) != 0>(V(), both);
             } else {
                 a[m] = __builtin_amdgcn_perm(v[2 * m + 1][c / 2], v[2 * m][c / 2], c % 2 ? 0x07060302u : 0x05040100u);
             }
         }
         return a;
     }
-    template <int c = 0> __device__ __forceinline__ void add_values(const u32x4 (&p)[kTerms<T>], f32x4 (&O)[kDims]) const {
+    template <int c = 0> __device__ __forceinline__ void add_values(const u32x4 (&p)[kTerms<V>], f32x4 (&O)[kDims]) const {
         if constexpr (c < kDims) {
             const u32x4 a = column<c>();
 #pragma unroll
-            for (int i = 0; i < kTerms<T>; ++i) O[c] = mfma_16x16x32(T(), a, p[i], O[c]);
+            for (int i = 0; i < kTerms<V>; ++i) O[c] = mfma_16x16x32(V(), a, p[i], O[c]);
             add_values<c + 1>(p, O);
         }
     }
@@ -321,9 +349,10 @@ template <int kDims, typename T> __device__ __forceinline__ void write_segment(c
 
 // `left` tiles of the list from a place on; at the end of every segment, and of the run, finish(place, begun, ended, maximum, sum, output) has what the wave has of it: begun:
 // the segment began before the run (given for the first one), ended: it ends here.
-template <int KS, bool kExact, bool kStream, typename T, bool kE4m3, typename Finish>
+template <int KS, bool kExact, bool kStream, typename T, int kCache, typename Finish>
 __device__ __forceinline__ void attention_run(const AttentionParams &P, Place at, uint32_t left, bool begun, uint32_t g, uint32_t r, Finish finish) {
-    using TileT = Tile<KS, kExact, kStream, T, kE4m3>;
+    using TileT = Tile<KS, kExact, kStream, T, kCache>;
+    using V = typename TileT::V;
     constexpr int kDims = TileT::kDims;
             TileT tile;
             tile.find(P, at, g, r);
@@ -351,8 +380,9 @@ __device__ __forceinline__ void attention_run(const AttentionParams &P, Place at
                 tile.scores(P, q, g, S);
                 float s[8];
     #pragma unroll
-                for (int i = 0; i < 8; ++i) s[i] = S[i / 4][i % 4] * P.score_by;
+                for (int i = 0; i < 8; ++i) s[i] = S[i / 4][i % 4] * (TileT::kBlocks ? P.score_by * tile.k_scale : P.score_by);
                 const uint32_t pages_ok = tile.pages_ok;
+                float v_scale = TileT::kBlocks ? tile.v_scale : 1.f;
                 // the next tile's place; its keys are on their way while this one's values are multiplied
                 const Place now = at;
                 --left;
@@ -374,6 +404,7 @@ __device__ __forceinline__ void attention_run(const AttentionParams &P, Place at
                         if (((pages_ok >> g) & 1) && p >= now.begin && p < now.end) keep |= 1u << i;
                         s[i] = (keep >> i) & 1 ? s[i] : -INFINITY;
                     }
+                    if (TileT::kBlocks && !keep) v_scale = 0.f;   // (of a block that holds nothing that counts: it may be anything)
     #pragma unroll
                     for (int j = 0; j < 8; ++j)   // (0 times what lies there need not be 0)
     #pragma unroll
@@ -383,7 +414,7 @@ __device__ __forceinline__ void attention_run(const AttentionParams &P, Place at
                 tile.load_keys(P, g);
                 float top = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
                 // Scores a few bits above the base need no new one (nothing overflows: 16-bit floats reach 2^15).
-                if (__any(top > most + kMostAbove<T>)) {
+                if (__any(top > most + kMostAbove<V>)) {
                     const float m = fmaxf(over_g_max(top), most), by = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(most - m);
                     most = m;
                     sum *= by, recent *= by;
@@ -396,13 +427,14 @@ __device__ __forceinline__ void attention_run(const AttentionParams &P, Place at
                     s[i] = __builtin_amdgcn_exp2f(s[i] - base);
                     recent += s[i];
                 }
-                u32x4 p[kTerms<T>];
+                u32x4 p[kTerms<V>];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    uint32_t terms[kTerms<T>];
-                    probability_terms<!kE4m3>(T(), s[2 * i], s[2 * i + 1], terms);
+                    uint32_t terms[kTerms<V>];
+                    if constexpr (TileT::kBlocks) s[2 * i] *= v_scale, s[2 * i + 1] *= v_scale;
+                    probability_terms<!eight_bits(kCache)>(V(), s[2 * i], s[2 * i + 1], terms);
 #pragma unroll
-                    for (int t = 0; t < kTerms<T>; ++t) p[t][i] = terms[t];
+                    for (int t = 0; t < kTerms<V>; ++t) p[t][i] = terms[t];
                 }
                 tile.add_values(p, O);
                 tile.load_values(P, r);
@@ -416,7 +448,7 @@ __device__ __forceinline__ void attention_run(const AttentionParams &P, Place at
             }
 }
 
-template <int KS, bool kExact, bool kStream, typename T, bool kE4m3> __global__ __launch_bounds__(256, KS > 4 ? 1 : 2) void paged_attention_kernel(AttentionParams P) {
+template <int KS, bool kExact, bool kStream, typename T, int kCache> __global__ __launch_bounds__(256, KS > 4 ? 1 : 2) void paged_attention_kernel(AttentionParams P) {
     constexpr int kDims = dims_per_lane<KS>();
     const uint32_t lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
     const uint32_t worker = uniform(blockIdx.x * 4 + (threadIdx.x >> 6));
@@ -460,7 +492,7 @@ template <int KS, bool kExact, bool kStream, typename T, bool kE4m3> __global__ 
         const uint32_t inside = start - rows_before * P.heads, count = at.last - at.first;
         at.head = uniform(inside / count);
         at.tile = at.first + uniform(inside % count);
-        attention_run<KS, kExact, kStream, T, kE4m3>(P, at, left, at.tile != at.first, g, r,
+        attention_run<KS, kExact, kStream, T, kCache>(P, at, left, at.tile != at.first, g, r,
                                                      [&](const Place &now, bool begun, bool ended, float most, float sum, const f32x4 (&O)[kDims]) __attribute__((always_inline)) {
                                                          write_segment<kDims>(P, now, worker, begun, ended, g, r, most, sum, O, T());
                                                      });
@@ -473,7 +505,7 @@ template <int KS, bool kExact, bool kStream, typename T, bool kE4m3> __global__ 
 // Where no segment has more tiles than a few for each of at most eight waves (four beyond 128 dims, which take more than half of a SIMD's registers): a workgroup has
 // one, and joins its waves' parts in LDS.  One launch, and no sums over the rows ahead of the first load.
 constexpr uint32_t whole_waves_most(uint32_t dim) { return dim <= 128 ? 8 : 4; }
-template <int KS, bool kExact, bool kStream, typename T, bool kE4m3> __global__ __launch_bounds__(64 * whole_waves_most(32 * KS), KS > 4 ? 1 : 2) void whole_attention_kernel(AttentionParams P) {
+template <int KS, bool kExact, bool kStream, typename T, int kCache> __global__ __launch_bounds__(64 * whole_waves_most(32 * KS), KS > 4 ? 1 : 2) void whole_attention_kernel(AttentionParams P) {
     constexpr int kDims = dims_per_lane<KS>();
     constexpr uint32_t kWholeWaves = whole_waves_most(32 * KS);
     __shared__ float ml[kWholeWaves][16][2];
@@ -485,7 +517,7 @@ template <int KS, bool kExact, bool kStream, typename T, bool kE4m3> __global__ 
     const uint32_t count = at.last - at.first, run = (count + waves - 1) / waves, start = min(wave * run, count), left = min(run, count - start);
     if (left) {
         at.tile = at.first + start;
-        attention_run<KS, kExact, kStream, T, kE4m3>(P, at, left, false, g, r,
+        attention_run<KS, kExact, kStream, T, kCache>(P, at, left, false, g, r,
                                                      [&](const Place &, bool, bool, float most, float sum, const f32x4 (&O)[kDims]) __attribute__((always_inline)) {
                                                          if (run == count) write_segment<kDims>(P, at, 0, false, true, g, r, most, sum, O, T());   // (this wave has all of it)
                                                          if (r >= P.group || run == count) return;

@@ -58,7 +58,6 @@ template <int kThreads> __device__ __forceinline__ Sum2 block_scan(Sum2 v, Sum2 
     return {v.tokens + before.tokens, v.pages + before.pages};
 }
 __device__ __forceinline__ uint32_t cut32(uint64_t v) { return v > kInt32Max ? kInt32Max : (uint32_t)v; }
-__device__ __forceinline__ uint32_t length_of(int32_t v) { return v < 0 ? 0u : (uint32_t)v; }
 // Pages that hold `positions` (up to 2^32): a quotient of positions - 1 below 2^31, or of its halves.
 __device__ __forceinline__ uint32_t pages_of(uint64_t positions, const Divider &page) {
     if (positions == 0) return 0;

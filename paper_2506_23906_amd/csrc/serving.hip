@@ -9,6 +9,8 @@
 #include "pages.h"
 #include "paged_attention.h"
 #include "decay.h"
+#include "call_checks.h"
+#include "attention_host.h"
 #include "serving_host.h"
 
 extern "C" {
@@ -77,7 +79,7 @@ mmv_status mmv_paged_attention(uint64_t n, uint32_t q_heads, const void *d_q, ui
     P.n = (uint32_t)n, P.q_heads = q_heads, P.heads = cache->heads, P.group = q_heads / cache->heads, P.dim = cache->dim;
     P.page = cache->page, P.pages = (uint32_t)cache->pages, P.window = window;
     P.score_by = scale * cache->k_scale * kLog2e, P.out_by = cache->v_scale;
-    return attention_call(P, type, cache->type, d_ws, (hipStream_t)hip_stream);
+    return attention_over(P, type, cache->type, d_ws, (hipStream_t)hip_stream);
 }
 
 size_t mmv_decay_attention_workspace_bytes(uint64_t n, uint64_t tokens, uint32_t heads, uint32_t dk, uint32_t dv) {

@@ -1,5 +1,5 @@
 // libmmvseg, part of the translation unit serving.hip (included there, in order).
-// The 16-bit values of queries, caches and states' inputs; moves between lanes.
+// The 16-bit values of queries, caches and states' inputs, their products on the matrix cores and terms of 16 bits; moves between lanes.
 #pragma once
 
 namespace {
@@ -37,6 +37,49 @@ inline Divider divider(uint32_t d) {
     while ((1u << bits) < d) ++bits;
     if ((1u << bits) == d) return {0, bits, d};
     return {(uint32_t)(((1ull << (31 + bits)) + d - 1) / d), bits - 1, d};
+}
+
+// Lengths that the device alone knows.
+__device__ __forceinline__ uint32_t length_of(int32_t v) { return v < 0 ? 0u : (uint32_t)v; }
+
+// ---- products of 16-bit values -------------------------------------------------------------------------------------
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef bf16_t bf16x8 __attribute__((ext_vector_type(8)));
+typedef f16_t f16x8 __attribute__((ext_vector_type(8)));
+__device__ __forceinline__ f32x4 mfma_16x16x32(bf16_t, u32x4 a, u32x4 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mfma_16x16x32(f16_t, u32x4 a, u32x4 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+template <typename T> __device__ __forceinline__ uint32_t pack2(float a, float b) {
+    typedef T pair __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, (pair){from_f32<T>(a), from_f32<T>(b)});
+}
+__device__ __forceinline__ f32x4 mfma_bf16(u32x4 a, u32x4 b, f32x4 c) { return mfma_16x16x32(bf16_t(), a, b, c); }
+__device__ __forceinline__ float low_half(uint32_t w) { return __builtin_bit_cast(float, w << 16); }
+__device__ __forceinline__ float high_half(uint32_t w) { return __builtin_bit_cast(float, w & 0xFFFF0000u); }
+// Two values into kTerms words of bf16 pairs: the upper halves of what is left each time, the last of it rounded.
+template <int kTerms> __device__ __forceinline__ void take_apart(float a, float b, uint32_t (&to)[kTerms]) {
+#pragma unroll
+    for (int i = 0; i + 1 < kTerms; ++i) {
+        to[i] = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, b), __builtin_bit_cast(uint32_t, a), 0x07060302u);
+        a -= high_half(__builtin_bit_cast(uint32_t, a)), b -= high_half(__builtin_bit_cast(uint32_t, b));
+    }
+    to[kTerms - 1] = pack2<bf16_t>(a, b);
+}
+// A word of two inputs as its bf16 terms.
+template <typename T, int kTerms> __device__ __forceinline__ void input_terms(uint32_t w, uint32_t (&to)[kTerms]) {
+    if constexpr (kTerms == 1) {
+        to[0] = w;
+    } else {
+        typedef f16_t pair __attribute__((ext_vector_type(2)));
+        const pair h = __builtin_bit_cast(pair, w);
+        take_apart<kTerms>((float)h[0], (float)h[1], to);
+    }
 }
 
 }  // namespace
