@@ -110,4 +110,523 @@ template <typename T, int kRows> __global__ __launch_bounds__(256) void delta_to
     }
 }
 
+// ---- prompts: chunks -----------------------------------------------------------------------------------------------
+//
+// Chunks of 64 tokens on the matrix cores.  With i, j counted from the chunk's beginning, G_i the sum of log_decay up to i, S the state before the chunk and u_i what token i writes,
+//   u_i = beta_i (v_i - e^(G_i) k_i S - sum_(j < i) e^(G_i - G_j) (k_i . k_j) u_j)     or   (I + L) U = diag(beta) (V - diag(e^G) K S)
+//   out_i = scale (e^(G_i) q_i S + sum_(j <= i) e^(G_i - G_j) (q_i . k_j) u_j),   S' = e^(G_63) S + sum_j e^(G_63 - G_j) k_j u_j^T
+// What does not depend on the state is made for all chunks and heads at once (delta_chunks_kernel): T = (I + L)^-1 diag(beta), the scores
+// W_ij = scale e^(G_i - G_j) (q_i . k_j), and the decays.  delta_prompt_kernel then goes through a request's chunks: R = V - diag(e^G) K S, U = T R, the outputs, the next state.
+constexpr uint32_t kChunk = 64;
+
+// What a chunk of a head leaves: matrices as operands of 16x16x32 products, 1 KB (64 lanes of 16 bytes) each: rows 32 s + 8 (r / 4) + 4 t + r % 4 (s, t = 0, 1), columns 32 c + 8 g + 0..7 in
+// lane 16 g + r, c <= s (above the diagonal there is nothing): the operands (s, t, c) = (0,0,0) (0,1,0) (1,0,0) (1,1,0) (1,0,1) (1,1,1), T in three bf16 terms, W in two.
+constexpr uint32_t kOperands = 6, kTermsT = 3, kTermsW = 2;
+constexpr uint32_t kMatrixPieces = kOperands * (kTermsT + kTermsW) * 64;                        // of 16 bytes
+constexpr uint32_t kChunkBytes = kMatrixPieces * 16 + 3 * kChunk * 4 + 256 - 3 * kChunk * 4 % 256;   // behind the matrices: e^(G_i), scale e^(G_i), e^(G_63 - G_i)
+
+struct DeltaPromptParams {
+    DeltaParams d;
+    char *chunks;            // [chunks of all requests][heads] of kChunkBytes
+    uint32_t most_chunks;    // as many as there is room for
+    uint32_t first;          // chunk, or request, of a launch
+};
+
+__device__ __forceinline__ uint32_t wave_sum32(uint32_t v) {
+    v += dpp_or_zero<0x111, 0xF>(v);
+    v += dpp_or_zero<0x112, 0xF>(v);
+    v += dpp_or_zero<0x114, 0xF>(v);
+    v += dpp_or_zero<0x118, 0xF>(v);
+    v += dpp_or_zero<0x142, 0xA>(v);
+    return lane_value(v + dpp_or_zero<0x143, 0xC>(v), 63);
+}
+__device__ __forceinline__ uint32_t chunks_of(Span s) { return (s.end - s.begin + kChunk - 1) / kChunk; }
+
+// Which request chunk `number` is of, and its first token; chunks are numbered request after request.
+struct ChunkPlace {
+    uint32_t request, begin, end;   // the chunk's tokens
+    bool found;
+};
+__device__ __forceinline__ ChunkPlace find_chunk(const DeltaParams &P, uint32_t number) {
+    const uint32_t lane = threadIdx.x & 63;
+    uint32_t before = 0;
+    for (uint32_t first = 0; first < P.n; first += 64) {
+        const uint32_t r = first + lane;
+        const Span s = r < P.n ? span_of(P, r) : Span{0, 0};
+        const uint32_t own = chunks_of(s);
+        uint32_t upto = own;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const uint32_t o = __shfl_up(upto, d);
+            upto += lane >= (uint32_t)d ? o : 0u;
+        }
+        const uint64_t hit = __ballot(before + upto > number);
+        if (hit) {
+            const int l = __builtin_ctzll(hit);
+            const uint32_t inside = number - (before + lane_value(upto - own, l));
+            const uint32_t begin = lane_value(s.begin, l) + inside * kChunk, end = lane_value(s.end, l);
+            return {first + l, begin, end - begin < kChunk ? end : begin + kChunk, true};
+        }
+        before += lane_value(upto, 63);
+    }
+    return {0, 0, 0, false};
+}
+// Chunks of the requests before this one.
+__device__ __forceinline__ uint32_t chunks_before(const DeltaParams &P, uint32_t request) {
+    uint32_t mine = 0;
+    for (uint32_t i = threadIdx.x & 63; i < request; i += 64) mine += chunks_of(span_of(P, i));
+    return wave_sum32(mine);
+}
+
+__device__ __forceinline__ f32x4 mfma_f32(float a, float b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
+
+// T and W of one chunk and head.  Wave w makes the rows 16 w .. 16 w + 15 of K K^T and Q K^T, straight from memory; then the inverse of its 16x16 block on the diagonal of I + L, a column a lane,
+// by substitution (which loses nothing where keys are alike, as powers of L would); then wave j the blocks below the diagonal of block column j,
+//   T_ij = -T_ii sum_(j <= m < i) L_im T_mj,
+// in fp32 products (16x16x4): the column of a step of the operand is 4 g + step, so that a result's registers are the next product's operand.
+template <typename T> __global__ __launch_bounds__(256) void delta_chunks_kernel(DeltaPromptParams PP) {
+    constexpr uint32_t kWide = kChunk + 4;
+    __shared__ __align__(16) float L[kChunk][kWide], X[kChunk][kWide];
+    __shared__ double upto[kChunk];
+    __shared__ float betas[kChunk];
+    const DeltaParams &P = PP.d;
+    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), g = lane >> 4, r = lane & 15;
+    const uint32_t in_launch = uniform(blockIdx.x / P.heads), h = uniform(blockIdx.x - in_launch * P.heads), shared = uniform(h / P.group), number = PP.first + in_launch;
+    const ChunkPlace at = find_chunk(P, number);
+    if (!at.found || number >= PP.most_chunks) return;
+    const uint32_t t0 = uniform(at.begin), m = uniform(at.end - at.begin), pieces = P.dk / 8;
+    char *const to = PP.chunks + ((uint64_t)number * P.heads + h) * kChunkBytes;
+    float *const decays = (float *)(to + kMatrixPieces * 16);
+
+    // keys and queries of a tile of 16 tokens, a row a lane: components 32 p + 8 g + 0..7 (rows and components that are not there read 0)
+    const auto rows_of = [&](const void *base, uint64_t stride) __attribute__((always_inline)) {
+        return make_rsrc((const void *)uniform64((uint64_t)((const T *)base + (uint64_t)shared * P.dk + t0 * stride)), uniform((m - 1) * 2 * (uint32_t)stride + 2 * P.dk));
+    };
+    const auto k_rows = rows_of(P.k, P.k_stride), q_rows = rows_of(P.q, P.q_stride);
+    u32x4 own_k[4], own_q[4];
+    const auto load = [&](u32x4 (&x)[4], auto rows, uint32_t tile, uint64_t stride) __attribute__((always_inline)) {
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {
+            const uint32_t off = (tile * 16 + r) * 2 * (uint32_t)stride + (p * 4 + g < pieces ? (p * 4 + g) * 16 : 1u << 31);
+            x[p] = __builtin_amdgcn_raw_buffer_load_b128(rows, off, 0, 0);
+        }
+    };
+    load(own_k, k_rows, wave, P.k_stride);
+    load(own_q, q_rows, wave, P.q_stride);
+    if (wave == 0) {
+        const uint64_t at_token = (uint64_t)(t0 + lane) * P.heads + h;
+        double sum = lane < m ? (double)at_least_200(P.log_decay[at_token]) : 0.0;
+        betas[lane] = lane < m ? P.beta[at_token] : 0.f;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const double o = __shfl_up(sum, d);
+            if (lane >= (uint32_t)d) sum += o;
+        }
+        upto[lane] = sum;
+        const double last = __shfl(sum, 63);
+        const float by = exp_of((float)sum);
+        decays[lane] = by, decays[64 + lane] = P.scale * by, decays[128 + lane] = exp_of((float)(last - sum));
+    }
+    __syncthreads();
+    for (uint32_t tile = 0; tile < 4; ++tile) {
+        f32x4 a = {0.f, 0.f, 0.f, 0.f}, b = a;
+        if (tile <= wave) {
+            u32x4 k[4];
+            load(k, k_rows, tile, P.k_stride);
+#pragma unroll
+            for (int p = 0; p < 4; ++p) a = mfma_16x16x32(T(), own_k[p], k[p], a), b = mfma_16x16x32(T(), own_q[p], k[p], b);
+        }
+        const uint32_t j = tile * 16 + r;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t i = wave * 16 + 4 * g + e;
+            const float decay = i >= j ? exp_of((float)(upto[i] - upto[j])) : 0.f;
+            L[i][j] = i > j ? a[e] * (betas[i] * decay) : 0.f;
+            X[i][j] = i >= j ? b[e] * (P.scale * decay) : 0.f;
+        }
+    }
+    __syncthreads();
+    const auto operand_row = [&](uint32_t f) __attribute__((always_inline)) { return (f >= 2 ? 32 : 0) + 8 * (r >> 2) + 4 * (f & 1) + (r & 3); };
+    const auto operand_column = [&](uint32_t f) __attribute__((always_inline)) { return (f >= 4 ? 32 : 0) + 8 * g; };
+    u32x4 *const places = (u32x4 *)to + lane;
+    for (uint32_t f = wave; f < kOperands; f += 4) {
+        const float *x = &X[operand_row(f)][operand_column(f)];
+        u32x4 out[kTermsW];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            uint32_t terms[kTermsW];
+            take_apart<kTermsW>(x[2 * i], x[2 * i + 1], terms);
+#pragma unroll
+            for (uint32_t c = 0; c < kTermsW; ++c) out[c][i] = terms[c];
+        }
+#pragma unroll
+        for (uint32_t c = 0; c < kTermsW; ++c) places[(kOperands * kTermsT + f * kTermsW + c) * 64] = out[c];
+    }
+    float column[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        float x = (uint32_t)i == r ? 1.f : 0.f;
+#pragma unroll
+        for (int k = 0; k < i; ++k) x = __builtin_fmaf(-L[wave * 16 + i][wave * 16 + k], column[k], x);
+        column[i] = x;
+    }
+    __syncthreads();   // (X is free)
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+        if ((uint32_t)i / 4 == g) X[wave * 16 + i][wave * 16 + r] = column[i];
+    if (wave == 3) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) X[4 * g + e][16 + r] = 0.f, X[32 + 4 * g + e][48 + r] = 0.f;
+    }
+    __syncthreads();
+    if (wave < 3) {
+        f32x4 below[4];   // blocks (i, wave)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if ((uint32_t)i == wave) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) below[i][e] = X[i * 16 + 4 * g + e][i * 16 + r];
+            } else if ((uint32_t)i > wave) {
+                f32x4 sum = {0.f, 0.f, 0.f, 0.f}, x = sum;
+#pragma unroll
+                for (int k = 0; k < i; ++k)
+                    if ((uint32_t)k >= wave) {
+                        const f32x4 l = *(const f32x4 *)&L[i * 16 + r][k * 16 + 4 * g];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) sum = mfma_f32(l[e], below[k][e], sum);
+                    }
+                const f32x4 d = *(const f32x4 *)&X[i * 16 + r][i * 16 + 4 * g];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x = mfma_f32(d[e], -sum[e], x);
+                below[i] = x;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) X[i * 16 + 4 * g + e][wave * 16 + r] = x[e];
+            }
+        }
+    }
+    __syncthreads();
+    for (uint32_t f = wave; f < kOperands; f += 4) {
+        const float *x = &X[operand_row(f)][operand_column(f)], *by = &betas[operand_column(f)];
+        u32x4 out[kTermsT];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            uint32_t terms[kTermsT];
+            take_apart<kTermsT>(x[2 * i] * by[2 * i], x[2 * i + 1] * by[2 * i + 1], terms);
+#pragma unroll
+            for (uint32_t c = 0; c < kTermsT; ++c) out[c][i] = terms[c];
+        }
+#pragma unroll
+        for (uint32_t c = 0; c < kTermsT; ++c) places[(f * kTermsT + c) * 64] = out[c];
+    }
+}
+
+__device__ __forceinline__ uint32_t of_neighbour(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xF, 0xF, false); }   // lanes 2 i and 2 i + 1 swapped
+// Two rows of 16-bit values, columns c and c + 1 in each word, for lanes of two columns: the even lane has rows 0 .. 3 of both, the odd one rows 4 .. 7; they
+// exchange what is the other's.  Words (0, 1), (2, 3), ... of the lane's own column.
+__device__ __forceinline__ u32x4 own_column(const uint32_t (&row)[4], bool odd) {
+    const uint32_t sel = odd ? 0x07060302u : 0x05040100u, other = odd ? 0x05040100u : 0x07060302u;
+    const uint32_t a = __builtin_amdgcn_perm(row[1], row[0], sel), b = __builtin_amdgcn_perm(row[3], row[2], sel);
+    const uint32_t c = of_neighbour(__builtin_amdgcn_perm(row[1], row[0], other)), d = of_neighbour(__builtin_amdgcn_perm(row[3], row[2], other));
+    return odd ? (u32x4){c, d, a, b} : (u32x4){a, b, c, d};
+}
+
+// A workgroup takes a request's chunks for one head and 64 columns, a wave 16 of them, whose state stays in its registers (fp32).
+// Layout (products 16x16x32, lane = 16 g + r): the lane has column r and, of a pair of result tiles, the rows 32 s + 8 g + 0..7 (operand rows are those of kOperands' comment): as B of
+// the next product those are its own, so the state goes into K S and Q S, R into T R, U into W U and K^T U, each from the registers where it is.
+// What is no 16-bit input meets the matrix cores as bf16 terms, each the upper half of what the ones before left, the last one rounded: three (fp32's 24 bits) of T, the state, R and U on
+// their way to a state, two of the state and of U where they meet q and W, whose result is rounded to 16 bits.  Inputs in fp16 are two terms each (exact).
+constexpr int kDeltaWaves = 4;
+template <int KD, typename T> __global__ __launch_bounds__(64 * kDeltaWaves, __is_same(T, f16_t) && KD > 2 ? 1 : 2) void delta_prompt_kernel(DeltaPromptParams PP, uint32_t slices) {
+    constexpr int NW = kDeltaWaves, kIn = __is_same(T, f16_t) ? 2 : 1, kRow = KD == 2 ? 64 : 128, kPieces = KD * 4;
+    constexpr int kItemsK = 16 * kPieces, kItems = 2 * kItemsK, kPer = (kItems + 64 * NW - 1) / (64 * NW);
+    constexpr int kMatrixPer = (kMatrixPieces + 64 * NW - 1) / (64 * NW);
+    __shared__ __align__(16) uint16_t lds_q[kIn][kChunk][kRow], lds_k[kIn][kChunk][kRow], lds_kt[kIn][KD * 32][kChunk];
+    __shared__ __align__(16) u32x4 lds_m[kMatrixPieces];
+    __shared__ __align__(16) float lds_d[3 * kChunk];
+    const DeltaParams &P = PP.d;
+    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), g = lane >> 4, r = lane & 15;
+    const uint32_t unit = uniform(blockIdx.x / slices), slice = uniform(blockIdx.x - unit * slices), in_launch = uniform(unit / P.heads), h = uniform(unit - in_launch * P.heads);
+    const uint32_t request = PP.first + in_launch, shared = uniform(h / P.group);
+    const Span span = span_of(P, request);
+    const uint32_t begin = uniform(span.begin), end = uniform(span.end);
+    const uint64_t state = state_of(P, request), matrix = (uint64_t)P.dk * P.dv, state_at = (state * P.heads + h) * matrix;
+    uint32_t number = chunks_before(P, request);
+    if (begin < end && number + (end - begin + kChunk - 1) / kChunk > PP.most_chunks) return;   // (offsets that go backwards)
+    const uint32_t column = slice * (16 * NW) + wave * 16 + r;
+    const bool live_column = column < P.dv, live_wave = slice * (16 * NW) + wave * 16 < P.dv;
+    f32x4 S[2 * KD];
+    const float *from = P.state_in && state != ~0ull ? P.state_in + state_at : nullptr;
+#pragma unroll
+    for (int i = 0; i < 2 * KD; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t d = (i / 2) * 32 + g * 8 + (i % 2) * 4 + e;
+            S[i][e] = from && live_column && d < P.dk ? from[(uint64_t)d * P.dv + column] : 0.f;
+        }
+    constexpr uint32_t kNowhere = 1u << 31;
+    const uint32_t pieces = P.dk / 8;
+    const bool odd_lane = lane & 1;
+    const uint32_t column2 = (column & ~1u) < P.dv ? 2 * (column & ~1u) : kNowhere;   // of the lane's pair of columns, in bytes
+    u32x4 staged[kPer][4], matrices[kMatrixPer];
+    float decays = 0.f;
+    uint32_t values[2][4];
+    const auto chunk_rows = [&](const void *base, uint32_t m, uint32_t stride, uint32_t width) __attribute__((always_inline)) {
+        return make_rsrc((const void *)uniform64((uint64_t)base), uniform((m - 1) * stride + width));
+    };
+    const auto load_chunk = [&](uint32_t t0, uint32_t chunk) __attribute__((always_inline)) {
+        const uint32_t m = min(kChunk, end - t0);
+#pragma unroll
+        for (int b = 0; b < kPer; ++b) {
+            const uint32_t first = wave * 64 + b * 64 * NW;
+            if (first < kItems) {
+                const bool is_q = first >= kItemsK;
+                const uint32_t id = first - (is_q ? kItemsK : 0) + lane, piece = id % kPieces, row = id / kPieces * 4;
+                const uint32_t stride = 2 * (uint32_t)(is_q ? P.q_stride : P.k_stride), off = row * stride + (piece < pieces ? piece * 16 : kNowhere);
+                const auto rows = chunk_rows(is_q ? (const T *)P.q + (uint64_t)shared * P.dk + t0 * P.q_stride : (const T *)P.k + (uint64_t)shared * P.dk + t0 * P.k_stride, m, stride, 2 * P.dk);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) staged[b][j] = __builtin_amdgcn_raw_buffer_load_b128(rows, off + j * stride, 0, 0);
+            }
+        }
+        const char *const made = PP.chunks + ((uint64_t)chunk * P.heads + h) * kChunkBytes;
+#pragma unroll
+        for (int b = 0; b < kMatrixPer; ++b)
+            if (b * 64 * NW + wave * 64 < kMatrixPieces) matrices[b] = ((const u32x4 *)made)[b * 64 * NW + tid];
+        if (tid < 3 * kChunk) decays = ((const float *)(made + kMatrixPieces * 16))[tid];
+        const uint32_t stride = 2 * (uint32_t)P.v_stride, off = (g * 8 + (odd_lane ? 4 : 0)) * stride + column2;
+        const auto rows = chunk_rows((const T *)P.v + (uint64_t)h * P.dv + t0 * P.v_stride, m, stride, 2 * P.dv);
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) values[s][j] = __builtin_amdgcn_raw_buffer_load_b32(rows, off + (s * 32 + j) * stride, 0, 0);
+    };
+    // LDS rows are pieces of 16 bytes, exchanged by the row's number so that the sixteen rows of an operand, 8 (r / 4) + r % 4 + ..., lie in different banks.  K by component as in
+    // rows d: piece u, 8 tokens, at u ^ (2 (d / 8 mod 4) + (d / 2 mod 2)) ^ (d / 32 mod 2), its two halves exchanged where d / 64 is odd: the lanes of a read have d = 8 (r / 4) +
+    // r % 4 + ..., those of a write d / 8 from 0 to 15.
+    const auto row_piece = [&](uint32_t row, uint32_t u) __attribute__((always_inline)) {
+        return kRow == 128 ? row * 256 + ((u ^ (row & 3) ^ (row >> 3 & 3) * 4) * 16) : row * 128 + ((u ^ (row >> 1 & 1) ^ (row >> 3 & 3) * 2) * 16);
+    };
+    const uint32_t own_kt = ((r >> 2) * 8 + (r & 3)) * 128 + (g ^ (r >> 1)) * 16;
+    const auto kt_tile = [&](int a, int t, int s) __attribute__((always_inline)) {   // components of tile t, tokens 32 s + 8 g .. + 7
+        const u32x4 w = *(const u32x4 *)((const char *)lds_kt[a] + (own_kt ^ (s * 64) ^ (t / 2 % 2 * 16)) + (t / 2) * 32 * 128 + (t % 2) * 4 * 128);
+        return t / 4 % 2 ? (u32x4){w[2], w[3], w[0], w[1]} : w;
+    };
+    const auto operand = [&](const uint16_t *plane, int tile, int p) __attribute__((always_inline)) {   // rows of tile (s, t) = (tile / 2, tile % 2)
+        const uint32_t row = (tile / 2) * 32 + (tile % 2) * 4 + 8 * (r >> 2) + (r & 3);
+        return *(const u32x4 *)((const char *)plane + row_piece(row, p * 4 + g));
+    };
+    if (begin < end) load_chunk(begin, number);
+    for (uint32_t t0 = begin; t0 < end; t0 += kChunk, ++number) {
+        const uint32_t m = min(kChunk, end - t0);
+#pragma unroll
+        for (int b = 0; b < kPer; ++b) {
+            const uint32_t first = wave * 64 + b * 64 * NW;
+            if (first < kItems) {
+                const bool is_q = first >= kItemsK;
+                const uint32_t id = first - (is_q ? kItemsK : 0) + lane, piece = id % kPieces, row = id / kPieces * 4;
+#pragma unroll
+                for (int a = 0; a < kIn; ++a) {
+                    uint32_t w[4][4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            uint32_t terms[kIn];
+                            input_terms<T, kIn>(staged[b][j][i], terms);
+                            w[j][i] = terms[a];
+                        }
+                    char *const to = is_q ? (char *)lds_q[a] : (char *)lds_k[a];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) *(u32x4 *)(to + row_piece(row + j, piece)) = (u32x4){w[j][0], w[j][1], w[j][2], w[j][3]};
+                    if (!is_q) {
+                        const uint32_t place = row / 8 ^ (piece & 3) * 2 ^ (piece / 4 & 1), half = (row / 4 & 1) ^ (piece / 8 & 1);
+                        char *const kt = (char *)lds_kt[a] + piece * 8 * 128 + half * 8;
+#pragma unroll
+                        for (int c = 0; c < 8; ++c) {   // component c of the four tokens
+                            const uint32_t sel = c % 2 ? 0x07060302u : 0x05040100u;
+                            *(u32x2 *)(kt + c * 128 + (place ^ (c / 2 & 1)) * 16) = (u32x2){__builtin_amdgcn_perm(w[1][c / 2], w[0][c / 2], sel), __builtin_amdgcn_perm(w[3][c / 2], w[2][c / 2], sel)};
+                        }
+                    }
+                }
+            }
+        }
+#pragma unroll
+        for (int b = 0; b < kMatrixPer; ++b)
+            if (b * 64 * NW + wave * 64 < kMatrixPieces) lds_m[b * 64 * NW + tid] = matrices[b];
+        if (tid < 3 * kChunk) lds_d[tid] = decays;
+        // values: tokens 32 s + 8 g + 2 i, + 1 of the lane's column
+        f32x4 R[4];
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const u32x4 own = own_column(values[s], odd_lane);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if constexpr (kIn == 1) {
+                    R[2 * s + i / 2][2 * (i % 2)] = low_half(own[i]), R[2 * s + i / 2][2 * (i % 2) + 1] = high_half(own[i]);
+                } else {
+                    typedef f16_t pair __attribute__((ext_vector_type(2)));
+                    const uint32_t w = own[i];   // (of an element of a vector itself, a bit cast takes the first)
+                    const pair x = __builtin_bit_cast(pair, w);
+                    R[2 * s + i / 2][2 * (i % 2)] = (float)x[0], R[2 * s + i / 2][2 * (i % 2) + 1] = (float)x[1];
+                }
+            }
+        }
+        __syncthreads();
+        if (t0 + kChunk < end) load_chunk(t0 + kChunk, number + 1);
+        if (live_wave) {
+            // K S and Q S
+            f32x4 O[4], Y[4];
+#pragma unroll
+            for (int p = 0; p < KD; ++p) {
+                u32x4 B[3];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    uint32_t x[3];
+                    take_apart<3>(S[2 * p + i / 2][2 * (i % 2)], S[2 * p + i / 2][2 * (i % 2) + 1], x);
+#pragma unroll
+                    for (int c = 0; c < 3; ++c) B[c][i] = x[c];
+                }
+#pragma unroll
+                for (int tile = 0; tile < 4; ++tile) {
+#pragma unroll
+                    for (int a = 0; a < kIn; ++a) {
+                        const u32x4 k = operand(&lds_k[a][0][0], tile, p), q = operand(&lds_q[a][0][0], tile, p);
+#pragma unroll
+                        for (int c = 0; c + a < 3; ++c) Y[tile] = mfma_bf16(k, B[c], p == 0 && a == 0 && c == 0 ? (f32x4){0.f, 0.f, 0.f, 0.f} : Y[tile]);
+#pragma unroll
+                        for (int c = 0; c + a < 2; ++c) O[tile] = mfma_bf16(q, B[c], p == 0 && a == 0 && c == 0 ? (f32x4){0.f, 0.f, 0.f, 0.f} : O[tile]);
+                    }
+                }
+            }
+            const auto decay_of = [&](int which, int tile) __attribute__((always_inline)) { return *(const f32x4 *)&lds_d[which * kChunk + (tile / 2) * 32 + g * 8 + (tile % 2) * 4]; };
+#pragma unroll
+            for (int tile = 0; tile < 4; ++tile) R[tile] -= decay_of(0, tile) * Y[tile], O[tile] *= decay_of(1, tile);
+            // U = T R
+            f32x4 U[4];
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                u32x4 B[3];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    uint32_t x[3];
+                    take_apart<3>(R[2 * s + i / 2][2 * (i % 2)], R[2 * s + i / 2][2 * (i % 2) + 1], x);
+#pragma unroll
+                    for (int c = 0; c < 3; ++c) B[c][i] = x[c];
+                }
+#pragma unroll
+                for (int f = s == 0 ? 0 : 4; f < (s == 0 ? 4 : 6); ++f) {
+                    const int tile = f < 4 ? f : f - 2;
+#pragma unroll
+                    for (int a = 0; a < 3; ++a) {
+                        const u32x4 A = lds_m[(f * kTermsT + a) * 64 + lane];
+#pragma unroll
+                        for (int c = 0; c + a < 3; ++c) U[tile] = mfma_bf16(A, B[c], f < 4 && a == 0 && c == 0 ? (f32x4){0.f, 0.f, 0.f, 0.f} : U[tile]);
+                    }
+                }
+            }
+            float odd = 0.f;   // NaN if anything that is written is not finite
+#pragma unroll
+            for (int tile = 0; tile < 4; ++tile)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) odd = __builtin_fmaf(U[tile][e], 0.f, odd);
+            T *const out = (T *)P.out + ((uint64_t)t0 * P.heads + h) * P.dv;
+            if (!__any(odd != 0.f)) {
+                const float decay = lds_d[kChunk - 1];
+#pragma unroll
+                for (int i = 0; i < 2 * KD; ++i) S[i] *= decay;
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    u32x4 B[2], D[3];
+                    const f32x4 by[2] = {decay_of(2, 2 * s), decay_of(2, 2 * s + 1)};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float x = U[2 * s + i / 2][2 * (i % 2)], y = U[2 * s + i / 2][2 * (i % 2) + 1];
+                        uint32_t two[2], three[3];
+                        take_apart<2>(x, y, two);
+                        take_apart<3>(x * by[i / 2][2 * (i % 2)], y * by[i / 2][2 * (i % 2) + 1], three);
+#pragma unroll
+                        for (int c = 0; c < 2; ++c) B[c][i] = two[c];
+#pragma unroll
+                        for (int c = 0; c < 3; ++c) D[c][i] = three[c];
+                    }
+#pragma unroll
+                    for (int f = s == 0 ? 0 : 4; f < (s == 0 ? 4 : 6); ++f) {
+                        const int tile = f < 4 ? f : f - 2;
+#pragma unroll
+                        for (int a = 0; a < 2; ++a) {
+                            const u32x4 A = lds_m[(kOperands * kTermsT + f * kTermsW + a) * 64 + lane];
+#pragma unroll
+                            for (int c = 0; c + a < 2; ++c) O[tile] = mfma_bf16(A, B[c], O[tile]);
+                        }
+                    }
+#pragma unroll
+                    for (int i = 0; i < 2 * KD; ++i)
+#pragma unroll
+                        for (int a = 0; a < kIn; ++a) {
+                            const u32x4 A = kt_tile(a, i, s);
+#pragma unroll
+                            for (int c = 0; c + a < 3; ++c) S[i] = mfma_bf16(A, D[c], S[i]);
+                        }
+                }
+                // tokens 0, 1 of a tile's four are the even lane's, 2, 3 the odd one's, both columns of each
+                const uint32_t stride = 2 * P.heads * P.dv;
+                const auto rows = chunk_rows(out, m, stride, 2 * P.dv);
+#pragma unroll
+                for (int tile = 0; tile < 4; ++tile) {
+                    const uint32_t a = pack2<T>(O[tile][0], O[tile][1]), b = pack2<T>(O[tile][2], O[tile][3]);   // own column
+                    const uint32_t got = of_neighbour(odd_lane ? a : b), own = odd_lane ? b : a;              // the lane's two tokens, the other column and this one
+                    const uint32_t left = odd_lane ? got : own, right = odd_lane ? own : got;
+                    const uint32_t off = ((tile / 2) * 32 + g * 8 + (tile % 2) * 4 + (odd_lane ? 2 : 0)) * stride + column2;
+                    __builtin_amdgcn_raw_buffer_store_b32(__builtin_amdgcn_perm(right, left, 0x05040100u), rows, off, 0, 0);
+                    __builtin_amdgcn_raw_buffer_store_b32(__builtin_amdgcn_perm(right, left, 0x07060302u), rows, off + stride, 0, 0);
+                }
+            } else {   // token by token: what is not finite must not meet the zeros of earlier ones
+                const T *const pv = (const T *)P.v + (uint64_t)h * P.dv + (live_column ? column : 0);
+                for (uint32_t j = 0; j < m; ++j) {
+                    const uint64_t at_token = (uint64_t)(t0 + j) * P.heads + h;
+                    const float by = exp_of(P.log_decay[at_token]), beta = P.beta[at_token], v = to_f32(pv[(t0 + j) * P.v_stride]);
+                    const auto component = [&](const uint16_t (*plane)[kChunk][kRow], int p, int c) __attribute__((always_inline)) {   // 32 p + 8 g + c
+                        float x = 0.f;
+#pragma unroll
+                        for (int a = 0; a < kIn; ++a) x += low_half(*(const uint16_t *)((const char *)plane[a] + row_piece(j, p * 4 + g) + 2 * c));
+                        return x;
+                    };
+                    float y = 0.f, o = 0.f;
+#pragma unroll
+                    for (int p = 0; p < KD; ++p)
+#pragma unroll
+                        for (int c = 0; c < 8; ++c) {
+                            const float x = S[2 * p + c / 4][c % 4] * by;
+                            S[2 * p + c / 4][c % 4] = x;
+                            if (p * 32 + g * 8 < P.dk) y += component(lds_k, p, c) * x;
+                        }
+                    y += __shfl_xor(y, 16);
+                    y += __shfl_xor(y, 32);
+                    const float u = beta * (v - y);
+#pragma unroll
+                    for (int p = 0; p < KD; ++p)
+#pragma unroll
+                        for (int c = 0; c < 8; ++c)
+                            if (p * 32 + g * 8 < P.dk) {
+                                S[2 * p + c / 4][c % 4] += component(lds_k, p, c) * u;
+                                o += component(lds_q, p, c) * S[2 * p + c / 4][c % 4];
+                            }
+                    o += __shfl_xor(o, 16);
+                    o += __shfl_xor(o, 32);
+                    if (live_column && g == 0) out[(uint64_t)j * P.heads * P.dv + column] = from_f32<T>(o * P.scale);
+                }
+            }
+        }
+        __syncthreads();   // (keys, queries and matrices are free)
+    }
+    float *to = P.state_out && state != ~0ull ? P.state_out + state_at : nullptr;
+    if (to && live_column)
+#pragma unroll
+        for (int i = 0; i < 2 * KD; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t d = (i / 2) * 32 + g * 8 + (i % 2) * 4 + e;
+                if (d < P.dk) to[(uint64_t)d * P.dv + column] = S[i][e];
+            }
+}
+
 }  // namespace

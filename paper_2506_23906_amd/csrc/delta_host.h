@@ -46,7 +46,36 @@ template <typename T> mmv_status launch_tokens(DeltaParams P, hipStream_t s) {
 }
 mmv_status delta_step_call(const DeltaParams &P, int type, hipStream_t s) { return type == MMV_TYPE_F16 ? launch_tokens<f16_t>(P, s) : launch_tokens<bf16_t>(P, s); }
 
-inline size_t delta_workspace(uint64_t, uint64_t, uint32_t, uint32_t, uint32_t) { return 0; }
-mmv_status delta_call(const DeltaParams &P, int type, void *, hipStream_t s) { return type == MMV_TYPE_F16 ? launch_tokens<f16_t>(P, s) : launch_tokens<bf16_t>(P, s); }
+// Chunks that the requests can have together.
+inline uint64_t delta_chunks(uint64_t n, uint64_t tokens) { return tokens / kChunk + (n < tokens ? n : tokens); }
+inline size_t delta_workspace(uint64_t n, uint64_t tokens, uint32_t heads, uint32_t, uint32_t) { return (size_t)delta_chunks(n, tokens) * heads * kChunkBytes; }
+template <typename T> mmv_status launch_chunks(DeltaPromptParams P, hipStream_t s) {
+    const uint32_t most = most_of_a_launch(256, P.d.heads);
+    for (; P.first < P.most_chunks; P.first += most) {
+        delta_chunks_kernel<T><<<(P.most_chunks - P.first < most ? P.most_chunks - P.first : most) * P.d.heads, 256, 0, s>>>(P);
+        if (const mmv_status st = launched()) return st;
+    }
+    return MMV_OK;
+}
+template <int KD, typename T> mmv_status launch_delta_prompts(DeltaPromptParams P, hipStream_t s) {
+    const uint32_t slices = (uint32_t)ceil_div(P.d.dv, 16 * kDeltaWaves), each = P.d.heads * slices, most = most_of_a_launch(64 * kDeltaWaves, each);
+    for (; P.first < P.d.n; P.first += most) {
+        delta_prompt_kernel<KD, T><<<(P.d.n - P.first < most ? P.d.n - P.first : most) * each, 64 * kDeltaWaves, 0, s>>>(P, slices);
+        if (const mmv_status st = launched()) return st;
+    }
+    return MMV_OK;
+}
+template <typename T> mmv_status delta_prompts(const DeltaPromptParams &P, hipStream_t s) {
+    if (const mmv_status st = launch_chunks<T>(P, s)) return st;
+    if (P.d.dk <= 64) return launch_delta_prompts<2, T>(P, s);
+    if constexpr (__is_same(T, bf16_t))
+        if (P.d.dk <= 96) return launch_delta_prompts<3, T>(P, s);
+    return launch_delta_prompts<4, T>(P, s);
+}
+mmv_status delta_call(const DeltaParams &d, int type, void *d_ws, hipStream_t s) {
+    DeltaPromptParams P = {};
+    P.d = d, P.chunks = (char *)d_ws, P.most_chunks = (uint32_t)delta_chunks(d.n, d.tokens);
+    return type == MMV_TYPE_F16 ? delta_prompts<f16_t>(P, s) : delta_prompts<bf16_t>(P, s);
+}
 
 }  // namespace
