@@ -115,15 +115,16 @@ template <typename T, int kRows> __global__ __launch_bounds__(256) void delta_to
 // Chunks of 64 tokens on the matrix cores.  With i, j counted from the chunk's beginning, G_i the sum of log_decay up to i, S the state before the chunk and u_i what token i writes,
 //   u_i = beta_i (v_i - e^(G_i) k_i S - sum_(j < i) e^(G_i - G_j) (k_i . k_j) u_j)     or   (I + L) U = diag(beta) (V - diag(e^G) K S)
 //   out_i = scale (e^(G_i) q_i S + sum_(j <= i) e^(G_i - G_j) (q_i . k_j) u_j),   S' = e^(G_63) S + sum_j e^(G_63 - G_j) k_j u_j^T
-// What does not depend on the state is made for all chunks and heads at once (delta_chunks_kernel): T = (I + L)^-1 diag(beta), the scores
-// W_ij = scale e^(G_i - G_j) (q_i . k_j), and the decays.  delta_prompt_kernel then goes through a request's chunks: R = V - diag(e^G) K S, U = T R, the outputs, the next state.
+// What does not depend on the state is made for all chunks and heads at once (delta_chunks_kernel): T = (I + L)^-1 diag(beta) and, with the scores W_ij = scale e^(G_i - G_j) (q_i . k_j),
+//   E = diag(e^(G_63 - G)) T,   M = W T.
+// delta_prompt_kernel then goes through a request's chunks: R = V - diag(e^G) K S, out = scale diag(e^G) Q S + M R, S' = e^(G_63) S + K^T E R.
 constexpr uint32_t kChunk = 64;
 
 // What a chunk of a head leaves: matrices as operands of 16x16x32 products, 1 KB (64 lanes of 16 bytes) each: rows 32 s + 8 (r / 4) + 4 t + r % 4 (s, t = 0, 1), columns 32 c + 8 g + 0..7 in
-// lane 16 g + r, c <= s (above the diagonal there is nothing): the operands (s, t, c) = (0,0,0) (0,1,0) (1,0,0) (1,1,0) (1,0,1) (1,1,1), T in three bf16 terms, W in two.
-constexpr uint32_t kOperands = 6, kTermsT = 3, kTermsW = 2;
-constexpr uint32_t kMatrixPieces = kOperands * (kTermsT + kTermsW) * 64;                        // of 16 bytes
-constexpr uint32_t kChunkBytes = kMatrixPieces * 16 + 3 * kChunk * 4 + 256 - 3 * kChunk * 4 % 256;   // behind the matrices: e^(G_i), scale e^(G_i), e^(G_63 - G_i)
+// lane 16 g + r, c <= s (above the diagonal there is nothing): the operands (s, t, c) = (0,0,0) (0,1,0) (1,0,0) (1,1,0) (1,0,1) (1,1,1), E in three bf16 terms, M in two.
+constexpr uint32_t kOperands = 6, kTermsE = 3, kTermsM = 2;
+constexpr uint32_t kMatrixPieces = kOperands * (kTermsE + kTermsM) * 64;                        // of 16 bytes
+constexpr uint32_t kChunkBytes = kMatrixPieces * 16 + 512;                                     // behind the matrices: e^(G_i), scale e^(G_i)
 
 struct DeltaPromptParams {
     DeltaParams d;
@@ -178,17 +179,20 @@ __device__ __forceinline__ uint32_t chunks_before(const DeltaParams &P, uint32_t
     return wave_sum32(mine);
 }
 
+template <int k> struct Number {
+    static constexpr int value = k;
+};
 __device__ __forceinline__ f32x4 mfma_f32(float a, float b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
 
-// T and W of one chunk and head.  Wave w makes the rows 16 w .. 16 w + 15 of K K^T and Q K^T, straight from memory; then the inverse of its 16x16 block on the diagonal of I + L, a column a lane,
-// by substitution (which loses nothing where keys are alike, as powers of L would); then wave j the blocks below the diagonal of block column j,
-//   T_ij = -T_ii sum_(j <= m < i) L_im T_mj,
+// E and M of one chunk and head.  Wave w makes the rows 16 w .. 16 w + 15 of K K^T and Q K^T, straight from memory; then the first one the inverses of the four 16x16 blocks on the diagonal of
+// I + L, a column a lane, by substitution (which loses nothing where keys are alike, as powers of L would); then wave j the blocks below the diagonal of block column j, and those of M,
+//   T_ij = -T_ii sum_(j <= m < i) L_im T_mj,   M_ij = sum_(j <= m <= i) W_im T_mj
 // in fp32 products (16x16x4): the column of a step of the operand is 4 g + step, so that a result's registers are the next product's operand.
-template <typename T> __global__ __launch_bounds__(256) void delta_chunks_kernel(DeltaPromptParams PP) {
+template <typename T> __global__ __launch_bounds__(256, 4) void delta_chunks_kernel(DeltaPromptParams PP) {
     constexpr uint32_t kWide = kChunk + 4;
-    __shared__ __align__(16) float L[kChunk][kWide], X[kChunk][kWide];
+    __shared__ __align__(16) float LW[kChunk][kWide], X[kChunk][kWide];   // below the diagonal L, from it on W transposed; T, later M
     __shared__ double upto[kChunk];
-    __shared__ float betas[kChunk];
+    __shared__ float betas[kChunk], left[kChunk];
     const DeltaParams &P = PP.d;
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), g = lane >> 4, r = lane & 15;
     const uint32_t in_launch = uniform(blockIdx.x / P.heads), h = uniform(blockIdx.x - in_launch * P.heads), shared = uniform(h / P.group), number = PP.first + in_launch;
@@ -203,7 +207,7 @@ template <typename T> __global__ __launch_bounds__(256) void delta_chunks_kernel
         return make_rsrc((const void *)uniform64((uint64_t)((const T *)base + (uint64_t)shared * P.dk + t0 * stride)), uniform((m - 1) * 2 * (uint32_t)stride + 2 * P.dk));
     };
     const auto k_rows = rows_of(P.k, P.k_stride), q_rows = rows_of(P.q, P.q_stride);
-    u32x4 own_k[4], own_q[4];
+    u32x4 own_k[4], own_q[4], k[4][4];
     const auto load = [&](u32x4 (&x)[4], auto rows, uint32_t tile, uint64_t stride) __attribute__((always_inline)) {
 #pragma unroll
         for (int p = 0; p < 4; ++p) {
@@ -211,113 +215,132 @@ template <typename T> __global__ __launch_bounds__(256) void delta_chunks_kernel
             x[p] = __builtin_amdgcn_raw_buffer_load_b128(rows, off, 0, 0);
         }
     };
+    double sum = 0.0;
+    float beta = 0.f;
+    if (wave == 0 && lane < m) {
+        const uint64_t at_token = (uint64_t)(t0 + lane) * P.heads + h;
+        sum = (double)at_least_200(P.log_decay[at_token]), beta = P.beta[at_token];
+    }
     load(own_k, k_rows, wave, P.k_stride);
     load(own_q, q_rows, wave, P.q_stride);
+#pragma unroll
+    for (int tile = 0; tile < 4; ++tile)
+        if ((uint32_t)tile < wave) load(k[tile], k_rows, tile, P.k_stride);
     if (wave == 0) {
-        const uint64_t at_token = (uint64_t)(t0 + lane) * P.heads + h;
-        double sum = lane < m ? (double)at_least_200(P.log_decay[at_token]) : 0.0;
-        betas[lane] = lane < m ? P.beta[at_token] : 0.f;
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1) {
             const double o = __shfl_up(sum, d);
             if (lane >= (uint32_t)d) sum += o;
         }
-        upto[lane] = sum;
         const double last = __shfl(sum, 63);
         const float by = exp_of((float)sum);
-        decays[lane] = by, decays[64 + lane] = P.scale * by, decays[128 + lane] = exp_of((float)(last - sum));
+        upto[lane] = sum, betas[lane] = beta, left[lane] = exp_of((float)(last - sum));
+        decays[lane] = by, decays[64 + lane] = P.scale * by;
     }
     __syncthreads();
-    for (uint32_t tile = 0; tile < 4; ++tile) {
-        f32x4 a = {0.f, 0.f, 0.f, 0.f}, b = a;
-        if (tile <= wave) {
-            u32x4 k[4];
-            load(k, k_rows, tile, P.k_stride);
 #pragma unroll
-            for (int p = 0; p < 4; ++p) a = mfma_16x16x32(T(), own_k[p], k[p], a), b = mfma_16x16x32(T(), own_q[p], k[p], b);
-        }
-        const uint32_t j = tile * 16 + r;
+    for (int tile = 0; tile < 4; ++tile)
+        if ((uint32_t)tile <= wave) {
+            f32x4 a = {0.f, 0.f, 0.f, 0.f}, b = a;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const uint32_t i = wave * 16 + 4 * g + e;
-            const float decay = i >= j ? exp_of((float)(upto[i] - upto[j])) : 0.f;
-            L[i][j] = i > j ? a[e] * (betas[i] * decay) : 0.f;
-            X[i][j] = i >= j ? b[e] * (P.scale * decay) : 0.f;
+            for (int p = 0; p < 4; ++p) {
+                const u32x4 x = (uint32_t)tile == wave ? own_k[p] : k[tile][p];
+                a = mfma_16x16x32(T(), own_k[p], x, a), b = mfma_16x16x32(T(), own_q[p], x, b);
+            }
+            const uint32_t j = tile * 16 + r;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t i = wave * 16 + 4 * g + e;
+                if (i >= j) {
+                    const float decay = exp_of((float)(upto[i] - upto[j]));
+                    LW[j][i] = b[e] * (P.scale * decay);
+                    if (i > j) LW[i][j] = a[e] * (betas[i] * decay);
+                }
+            }
         }
-    }
     __syncthreads();
-    const auto operand_row = [&](uint32_t f) __attribute__((always_inline)) { return (f >= 2 ? 32 : 0) + 8 * (r >> 2) + 4 * (f & 1) + (r & 3); };
-    const auto operand_column = [&](uint32_t f) __attribute__((always_inline)) { return (f >= 4 ? 32 : 0) + 8 * g; };
-    u32x4 *const places = (u32x4 *)to + lane;
-    for (uint32_t f = wave; f < kOperands; f += 4) {
-        const float *x = &X[operand_row(f)][operand_column(f)];
-        u32x4 out[kTermsW];
+    if (wave == 0) {
+        const float (*const block)[kWide] = (const float (*)[kWide])&LW[16 * g][16 * g];
+        float column[16];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            uint32_t terms[kTermsW];
-            take_apart<kTermsW>(x[2 * i], x[2 * i + 1], terms);
+        for (int i = 0; i < 16; ++i) {
+            float x = (uint32_t)i == r ? 1.f : 0.f;
 #pragma unroll
-            for (uint32_t c = 0; c < kTermsW; ++c) out[c][i] = terms[c];
+            for (int c = 0; c < i; ++c) x = __builtin_fmaf(-block[i][c], column[c], x);
+            column[i] = x;
+            X[16 * g + i][16 * g + r] = x;
         }
-#pragma unroll
-        for (uint32_t c = 0; c < kTermsW; ++c) places[(kOperands * kTermsT + f * kTermsW + c) * 64] = out[c];
-    }
-    float column[16];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        float x = (uint32_t)i == r ? 1.f : 0.f;
-#pragma unroll
-        for (int k = 0; k < i; ++k) x = __builtin_fmaf(-L[wave * 16 + i][wave * 16 + k], column[k], x);
-        column[i] = x;
-    }
-    __syncthreads();   // (X is free)
-#pragma unroll
-    for (int i = 0; i < 16; ++i)
-        if ((uint32_t)i / 4 == g) X[wave * 16 + i][wave * 16 + r] = column[i];
-    if (wave == 3) {
+    } else if (wave == 3) {   // (what operands have above the diagonal)
 #pragma unroll
         for (int e = 0; e < 4; ++e) X[4 * g + e][16 + r] = 0.f, X[32 + 4 * g + e][48 + r] = 0.f;
     }
     __syncthreads();
-    if (wave < 3) {
-        f32x4 below[4];   // blocks (i, wave)
+    f32x4 T_[4];   // blocks (i, wave)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if ((uint32_t)i == wave) {
+    for (int i = 0; i < 4; ++i) {
+        if ((uint32_t)i == wave) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) below[i][e] = X[i * 16 + 4 * g + e][i * 16 + r];
-            } else if ((uint32_t)i > wave) {
-                f32x4 sum = {0.f, 0.f, 0.f, 0.f}, x = sum;
+            for (int e = 0; e < 4; ++e) T_[i][e] = X[i * 16 + 4 * g + e][i * 16 + r];
+        } else if ((uint32_t)i > wave) {
+            f32x4 x = {0.f, 0.f, 0.f, 0.f}, y = x;
 #pragma unroll
-                for (int k = 0; k < i; ++k)
-                    if ((uint32_t)k >= wave) {
-                        const f32x4 l = *(const f32x4 *)&L[i * 16 + r][k * 16 + 4 * g];
+            for (int c = 0; c < i; ++c)
+                if ((uint32_t)c >= wave) {
+                    const f32x4 l = *(const f32x4 *)&LW[i * 16 + r][c * 16 + 4 * g];
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) sum = mfma_f32(l[e], below[k][e], sum);
+                    for (int e = 0; e < 4; ++e) x = mfma_f32(l[e], T_[c][e], x);
+                }
+            const f32x4 d = *(const f32x4 *)&X[i * 16 + r][i * 16 + 4 * g];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y = mfma_f32(d[e], -x[e], y);
+            T_[i] = y;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) X[i * 16 + 4 * g + e][wave * 16 + r] = y[e];
+        }
+    }
+    f32x4 M[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if ((uint32_t)i >= wave) {
+            M[i] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int c = 0; c <= i; ++c)
+                if ((uint32_t)c >= wave) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const uint32_t column = c * 16 + 4 * g + e, row = i * 16 + r;
+                        M[i] = mfma_f32(c < i || column <= row ? LW[column][row] : 0.f, T_[c][e], M[i]);
                     }
-                const f32x4 d = *(const f32x4 *)&X[i * 16 + r][i * 16 + 4 * g];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) x = mfma_f32(d[e], -sum[e], x);
-                below[i] = x;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) X[i * 16 + 4 * g + e][wave * 16 + r] = x[e];
-            }
+                }
         }
-    }
     __syncthreads();
-    for (uint32_t f = wave; f < kOperands; f += 4) {
-        const float *x = &X[operand_row(f)][operand_column(f)], *by = &betas[operand_column(f)];
-        u32x4 out[kTermsT];
+    const auto write_operands = [&](auto terms_of, uint32_t first, auto rows_by) __attribute__((always_inline)) {
+        constexpr int kTerms = decltype(terms_of)::value;
+        for (uint32_t f = wave; f < kOperands; f += 4) {
+            const uint32_t row = (f >= 2 ? 32 : 0) + 8 * (r >> 2) + 4 * (f & 1) + (r & 3), column = (f >= 4 ? 32 : 0) + 8 * g;
+            const float *const x = &X[row][column], *const by = &betas[column], row_by = rows_by(row);
+            u32x4 out[kTerms];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            uint32_t terms[kTermsT];
-            take_apart<kTermsT>(x[2 * i] * by[2 * i], x[2 * i + 1] * by[2 * i + 1], terms);
+            for (int i = 0; i < 4; ++i) {
+                uint32_t terms[kTerms];
+                take_apart<kTerms>(x[2 * i] * by[2 * i] * row_by, x[2 * i + 1] * by[2 * i + 1] * row_by, terms);
 #pragma unroll
-            for (uint32_t c = 0; c < kTermsT; ++c) out[c][i] = terms[c];
+                for (int c = 0; c < kTerms; ++c) out[c][i] = terms[c];
+            }
+#pragma unroll
+            for (int c = 0; c < kTerms; ++c) ((u32x4 *)to)[(first + f * kTerms + c) * 64 + lane] = out[c];
         }
+    };
+    write_operands(Number<kTermsE>(), 0, [&](uint32_t row) __attribute__((always_inline)) { return left[row]; });
+    __syncthreads();
 #pragma unroll
-        for (uint32_t c = 0; c < kTermsT; ++c) places[(f * kTermsT + c) * 64] = out[c];
-    }
+    for (int i = 0; i < 4; ++i)
+        if ((uint32_t)i >= wave) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) X[i * 16 + 4 * g + e][wave * 16 + r] = M[i][e];
+        }
+    __syncthreads();
+    write_operands(Number<kTermsM>(), kOperands * kTermsE, [](uint32_t) __attribute__((always_inline)) { return 1.f; });
 }
 
 __device__ __forceinline__ uint32_t of_neighbour(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xF, 0xF, false); }   // lanes 2 i and 2 i + 1 swapped
@@ -332,9 +355,9 @@ __device__ __forceinline__ u32x4 own_column(const uint32_t (&row)[4], bool odd) 
 
 // A workgroup takes a request's chunks for one head and 64 columns, a wave 16 of them, whose state stays in its registers (fp32).
 // Layout (products 16x16x32, lane = 16 g + r): the lane has column r and, of a pair of result tiles, the rows 32 s + 8 g + 0..7 (operand rows are those of kOperands' comment): as B of
-// the next product those are its own, so the state goes into K S and Q S, R into T R, U into W U and K^T U, each from the registers where it is.
-// What is no 16-bit input meets the matrix cores as bf16 terms, each the upper half of what the ones before left, the last one rounded: three (fp32's 24 bits) of T, the state, R and U on
-// their way to a state, two of the state and of U where they meet q and W, whose result is rounded to 16 bits.  Inputs in fp16 are two terms each (exact).
+// the next product those are its own, so the state goes into K S and Q S, R into M R and E R, and that into K^T E R, each from the registers where it is.
+// What is no 16-bit input meets the matrix cores as bf16 terms, each the upper half of what the ones before left, the last one rounded: three (fp32's 24 bits) of E, the state, R and E R on
+// their way to a state, two of the state, M and R on their way to an output, which is rounded to 16 bits.  Inputs in fp16 are two terms each (exact).
 constexpr int kDeltaWaves = 4;
 template <int KD, typename T> __global__ __launch_bounds__(64 * kDeltaWaves, __is_same(T, f16_t) && KD > 2 ? 1 : 2) void delta_prompt_kernel(DeltaPromptParams PP, uint32_t slices) {
     constexpr int NW = kDeltaWaves, kIn = __is_same(T, f16_t) ? 2 : 1, kRow = KD == 2 ? 64 : 128, kPieces = KD * 4;
@@ -342,7 +365,7 @@ template <int KD, typename T> __global__ __launch_bounds__(64 * kDeltaWaves, __i
     constexpr int kMatrixPer = (kMatrixPieces + 64 * NW - 1) / (64 * NW);
     __shared__ __align__(16) uint16_t lds_q[kIn][kChunk][kRow], lds_k[kIn][kChunk][kRow], lds_kt[kIn][KD * 32][kChunk];
     __shared__ __align__(16) u32x4 lds_m[kMatrixPieces];
-    __shared__ __align__(16) float lds_d[3 * kChunk];
+    __shared__ __align__(16) float lds_d[2 * kChunk];
     const DeltaParams &P = PP.d;
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), g = lane >> 4, r = lane & 15;
     const uint32_t unit = uniform(blockIdx.x / slices), slice = uniform(blockIdx.x - unit * slices), in_launch = uniform(unit / P.heads), h = uniform(unit - in_launch * P.heads);
@@ -391,7 +414,7 @@ template <int KD, typename T> __global__ __launch_bounds__(64 * kDeltaWaves, __i
 #pragma unroll
         for (int b = 0; b < kMatrixPer; ++b)
             if (b * 64 * NW + wave * 64 < kMatrixPieces) matrices[b] = ((const u32x4 *)made)[b * 64 * NW + tid];
-        if (tid < 3 * kChunk) decays = ((const float *)(made + kMatrixPieces * 16))[tid];
+        if (tid < 2 * kChunk) decays = ((const float *)(made + kMatrixPieces * 16))[tid];
         const uint32_t stride = 2 * (uint32_t)P.v_stride, off = (g * 8 + (odd_lane ? 4 : 0)) * stride + column2;
         const auto rows = chunk_rows((const T *)P.v + (uint64_t)h * P.dv + t0 * P.v_stride, m, stride, 2 * P.dv);
 #pragma unroll
@@ -452,7 +475,7 @@ template <int KD, typename T> __global__ __launch_bounds__(64 * kDeltaWaves, __i
 #pragma unroll
         for (int b = 0; b < kMatrixPer; ++b)
             if (b * 64 * NW + wave * 64 < kMatrixPieces) lds_m[b * 64 * NW + tid] = matrices[b];
-        if (tid < 3 * kChunk) lds_d[tid] = decays;
+        if (tid < 2 * kChunk) lds_d[tid] = decays;
         // values: tokens 32 s + 8 g + 2 i, + 1 of the lane's column
         f32x4 R[4];
 #pragma unroll
@@ -486,21 +509,26 @@ template <int KD, typename T> __global__ __launch_bounds__(64 * kDeltaWaves, __i
                     for (int c = 0; c < 3; ++c) B[c][i] = x[c];
                 }
 #pragma unroll
-                for (int tile = 0; tile < 4; ++tile) {
+                for (int a = 0; a < kIn; ++a) {
+                    u32x4 A[4];
 #pragma unroll
-                    for (int a = 0; a < kIn; ++a) {
-                        const u32x4 k = operand(&lds_k[a][0][0], tile, p), q = operand(&lds_q[a][0][0], tile, p);
+                    for (int tile = 0; tile < 4; ++tile) A[tile] = operand(&lds_k[a][0][0], tile, p);
 #pragma unroll
-                        for (int c = 0; c + a < 3; ++c) Y[tile] = mfma_bf16(k, B[c], p == 0 && a == 0 && c == 0 ? (f32x4){0.f, 0.f, 0.f, 0.f} : Y[tile]);
+                    for (int c = 0; c + a < 3; ++c)
 #pragma unroll
-                        for (int c = 0; c + a < 2; ++c) O[tile] = mfma_bf16(q, B[c], p == 0 && a == 0 && c == 0 ? (f32x4){0.f, 0.f, 0.f, 0.f} : O[tile]);
-                    }
+                        for (int tile = 0; tile < 4; ++tile) Y[tile] = mfma_bf16(A[tile], B[c], p == 0 && a == 0 && c == 0 ? (f32x4){0.f, 0.f, 0.f, 0.f} : Y[tile]);
+#pragma unroll
+                    for (int tile = 0; tile < 4; ++tile) A[tile] = operand(&lds_q[a][0][0], tile, p);
+#pragma unroll
+                    for (int c = 0; c + a < 2; ++c)
+#pragma unroll
+                        for (int tile = 0; tile < 4; ++tile) O[tile] = mfma_bf16(A[tile], B[c], p == 0 && a == 0 && c == 0 ? (f32x4){0.f, 0.f, 0.f, 0.f} : O[tile]);
                 }
             }
             const auto decay_of = [&](int which, int tile) __attribute__((always_inline)) { return *(const f32x4 *)&lds_d[which * kChunk + (tile / 2) * 32 + g * 8 + (tile % 2) * 4]; };
 #pragma unroll
             for (int tile = 0; tile < 4; ++tile) R[tile] -= decay_of(0, tile) * Y[tile], O[tile] *= decay_of(1, tile);
-            // U = T R
+            // U = E R, and M R
             f32x4 U[4];
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
@@ -512,15 +540,32 @@ template <int KD, typename T> __global__ __launch_bounds__(64 * kDeltaWaves, __i
 #pragma unroll
                     for (int c = 0; c < 3; ++c) B[c][i] = x[c];
                 }
+                const int first = s == 0 ? 0 : 4, last = s == 0 ? 4 : 6;   // operands; the tile of one behind the fourth is two before it
 #pragma unroll
-                for (int f = s == 0 ? 0 : 4; f < (s == 0 ? 4 : 6); ++f) {
-                    const int tile = f < 4 ? f : f - 2;
+                for (int a = 0; a < 3; ++a) {
+                    u32x4 A[4];
 #pragma unroll
-                    for (int a = 0; a < 3; ++a) {
-                        const u32x4 A = lds_m[(f * kTermsT + a) * 64 + lane];
+                    for (int f = first; f < last; ++f) A[f - first] = lds_m[(f * kTermsE + a) * 64 + lane];
 #pragma unroll
-                        for (int c = 0; c + a < 3; ++c) U[tile] = mfma_bf16(A, B[c], f < 4 && a == 0 && c == 0 ? (f32x4){0.f, 0.f, 0.f, 0.f} : U[tile]);
-                    }
+                    for (int c = 0; c + a < 3; ++c)
+#pragma unroll
+                        for (int f = first; f < last; ++f) {
+                            const int tile = f < 4 ? f : f - 2;
+                            U[tile] = mfma_bf16(A[f - first], B[c], f < 4 && a == 0 && c == 0 ? (f32x4){0.f, 0.f, 0.f, 0.f} : U[tile]);
+                        }
+                }
+#pragma unroll
+                for (int a = 0; a < 2; ++a) {
+                    u32x4 A[4];
+#pragma unroll
+                    for (int f = first; f < last; ++f) A[f - first] = lds_m[(kOperands * kTermsE + f * kTermsM + a) * 64 + lane];
+#pragma unroll
+                    for (int c = 0; c + a < 2; ++c)
+#pragma unroll
+                        for (int f = first; f < last; ++f) {
+                            const int tile = f < 4 ? f : f - 2;
+                            O[tile] = mfma_bf16(A[f - first], B[c], O[tile]);
+                        }
                 }
             }
             float odd = 0.f;   // NaN if anything that is written is not finite
@@ -535,36 +580,25 @@ template <int KD, typename T> __global__ __launch_bounds__(64 * kDeltaWaves, __i
                 for (int i = 0; i < 2 * KD; ++i) S[i] *= decay;
 #pragma unroll
                 for (int s = 0; s < 2; ++s) {
-                    u32x4 B[2], D[3];
-                    const f32x4 by[2] = {decay_of(2, 2 * s), decay_of(2, 2 * s + 1)};
+                    u32x4 B[3];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const float x = U[2 * s + i / 2][2 * (i % 2)], y = U[2 * s + i / 2][2 * (i % 2) + 1];
-                        uint32_t two[2], three[3];
-                        take_apart<2>(x, y, two);
-                        take_apart<3>(x * by[i / 2][2 * (i % 2)], y * by[i / 2][2 * (i % 2) + 1], three);
+                        uint32_t x[3];
+                        take_apart<3>(U[2 * s + i / 2][2 * (i % 2)], U[2 * s + i / 2][2 * (i % 2) + 1], x);
 #pragma unroll
-                        for (int c = 0; c < 2; ++c) B[c][i] = two[c];
-#pragma unroll
-                        for (int c = 0; c < 3; ++c) D[c][i] = three[c];
+                        for (int c = 0; c < 3; ++c) B[c][i] = x[c];
                     }
 #pragma unroll
-                    for (int f = s == 0 ? 0 : 4; f < (s == 0 ? 4 : 6); ++f) {
-                        const int tile = f < 4 ? f : f - 2;
-#pragma unroll
-                        for (int a = 0; a < 2; ++a) {
-                            const u32x4 A = lds_m[(kOperands * kTermsT + f * kTermsW + a) * 64 + lane];
-#pragma unroll
-                            for (int c = 0; c + a < 2; ++c) O[tile] = mfma_bf16(A, B[c], O[tile]);
-                        }
-                    }
-#pragma unroll
-                    for (int i = 0; i < 2 * KD; ++i)
+                    for (int first = 0; first < 2 * KD; first += 2)
 #pragma unroll
                         for (int a = 0; a < kIn; ++a) {
-                            const u32x4 A = kt_tile(a, i, s);
+                            u32x4 A[2];
 #pragma unroll
-                            for (int c = 0; c + a < 3; ++c) S[i] = mfma_bf16(A, D[c], S[i]);
+                            for (int i = 0; i < 2; ++i) A[i] = kt_tile(a, first + i, s);
+#pragma unroll
+                            for (int c = 0; c + a < 3; ++c)
+#pragma unroll
+                                for (int i = 0; i < 2; ++i) S[first + i] = mfma_bf16(A[i], B[c], S[first + i]);
                         }
                 }
                 // tokens 0, 1 of a tile's four are the even lane's, 2, 3 the odd one's, both columns of each
