@@ -130,7 +130,9 @@ struct DeltaPromptParams {
     DeltaParams d;
     char *chunks;            // [chunks of all requests][heads] of kChunkBytes
     uint32_t most_chunks;    // as many as there is room for
-    uint32_t first;          // chunk, or request, of a launch
+    uint32_t first;          // chunk of a launch
+    float *block_states;     // [slots][heads][dk][dv + dk]; null: requests are not taken apart
+    uint32_t round, slots;   // blocks of a head that the device has at once; states of blocks that there is room for
 };
 
 __device__ __forceinline__ uint32_t wave_sum32(uint32_t v) {
@@ -172,16 +174,86 @@ __device__ __forceinline__ ChunkPlace find_chunk(const DeltaParams &P, uint32_t 
     }
     return {0, 0, 0, false};
 }
-// Chunks of the requests before this one.
-__device__ __forceinline__ uint32_t chunks_before(const DeltaParams &P, uint32_t request) {
-    uint32_t mine = 0;
-    for (uint32_t i = threadIdx.x & 63; i < request; i += 64) mine += chunks_of(span_of(P, i));
-    return wave_sum32(mine);
+
+// Requests in blocks.  Chunks of a request depend on each other through the state.  Where few long requests would leave the device idle they are taken apart into blocks of as many chunks: what a
+// block makes of a state, S -> A S + B, is found for all blocks at once (A from the columns of the identity, B from a state of zeros), then the state before each block, then all blocks' outputs.
+// That is 2.3 times the work, so it is done where the longest request has over kApart times an even share of the chunks.
+constexpr uint32_t kApart = 3, kBlockRounds = 3, kLeastBlock = 4, kLeastApart = 16;
+struct BlockPlan {
+    uint32_t chunks, blocks;   // chunks of a block (~0: all of a request), blocks in all
+};
+__device__ __forceinline__ uint32_t blocks_in(uint32_t chunks, uint32_t block) { return block == ~0u ? 1u : max(1u, (chunks + block - 1) / block); }
+__device__ __forceinline__ BlockPlan plan_blocks(const DeltaPromptParams &PP) {
+    const DeltaParams &P = PP.d;
+    if (!PP.block_states) return {~0u, P.n};
+    const uint32_t lane = threadIdx.x & 63;
+    uint32_t all = 0, most = 0;
+    for (uint32_t r = lane; r < P.n; r += 64) {
+        const uint32_t own = chunks_of(span_of(P, r));
+        all += own, most = max(most, own);
+    }
+    all = wave_sum32(all);
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) most = max(most, (uint32_t)__shfl_xor((int)most, d));
+    most = uniform(most);
+    if (most < kLeastApart || (uint64_t)most * PP.round <= (uint64_t)kApart * all) return {~0u, P.n};
+    const uint32_t block = max(kLeastBlock, (all + kBlockRounds * PP.round - 1) / (kBlockRounds * PP.round));
+    uint32_t blocks = 0;
+    for (uint32_t r = lane; r < P.n; r += 64) blocks += blocks_in(chunks_of(span_of(P, r)), block);
+    return {block, wave_sum32(blocks)};
+}
+// Which block of which request has a number, counted request after request.
+struct BlockPlace {
+    uint32_t request, block, blocks;   // the block's number in its request, and how many that has
+    uint32_t slot, chunk;              // its state's place, if there are several; its first chunk
+    bool found;
+};
+__device__ __forceinline__ BlockPlace find_block(const DeltaPromptParams &PP, uint32_t block, uint32_t number) {
+    const DeltaParams &P = PP.d;
+    const uint32_t lane = threadIdx.x & 63;
+    uint32_t before = 0, chunks_before = 0, slots_before = 0;
+    for (uint32_t first = 0; first < P.n; first += 64) {
+        const uint32_t r = first + lane, chunks = r < P.n ? chunks_of(span_of(P, r)) : 0u, own = r < P.n ? blocks_in(chunks, block) : 0u, slots = own > 1 ? own : 0u;
+        uint32_t upto = own;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const uint32_t o = __shfl_up(upto, d);
+            upto += lane >= (uint32_t)d ? o : 0u;
+        }
+        const uint64_t hit = __ballot(before + upto > number);
+        if (hit) {
+            const int l = __builtin_ctzll(hit);
+            BlockPlace at;
+            at.request = first + l, at.blocks = lane_value(own, l), at.block = number - (before + lane_value(upto, l) - at.blocks);
+            const uint32_t first_slot = slots_before + wave_sum32((int)lane < l ? slots : 0u);
+            at.slot = first_slot + at.block, at.chunk = chunks_before + wave_sum32((int)lane < l ? chunks : 0u) + (at.block ? at.block * block : 0u);
+            at.found = at.blocks == 1 || first_slot + at.blocks <= PP.slots;   // (there is room for all of them, unless offsets go backwards)
+            return at;
+        }
+        before += lane_value(upto, 63), chunks_before += wave_sum32(chunks), slots_before += wave_sum32(slots);
+    }
+    return {0, 0, 0, 0, 0, false};
 }
 
+// Eight values of a lane as the three terms of an operand.
+__device__ __forceinline__ void three_terms(const f32x4 (&x)[2], u32x4 (&to)[3]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        uint32_t terms[3];
+        take_apart<3>(x[i / 2][2 * (i % 2)], x[i / 2][2 * (i % 2) + 1], terms);
+#pragma unroll
+        for (int c = 0; c < 3; ++c) to[c][i] = terms[c];
+    }
+}
 template <int k> struct Number {
     static constexpr int value = k;
 };
+template <int first, int behind, typename Step> __device__ __forceinline__ void in_order(const Step &step) {
+    if constexpr (first < behind) {
+        step(Number<first>());
+        in_order<first + 1, behind>(step);
+    }
+}
 __device__ __forceinline__ f32x4 mfma_f32(float a, float b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
 
 // E and M of one chunk and head.  Wave w makes the rows 16 w .. 16 w + 15 of K K^T and Q K^T, straight from memory; then the first one the inverses of the four 16x16 blocks on the diagonal of
@@ -353,59 +425,81 @@ __device__ __forceinline__ u32x4 own_column(const uint32_t (&row)[4], bool odd) 
     return odd ? (u32x4){c, d, a, b} : (u32x4){a, b, c, d};
 }
 
-// A workgroup takes a request's chunks for one head and 64 columns, a wave 16 of them, whose state stays in its registers (fp32).
-// Layout (products 16x16x32, lane = 16 g + r): the lane has column r and, of a pair of result tiles, the rows 32 s + 8 g + 0..7 (operand rows are those of kOperands' comment): as B of
-// the next product those are its own, so the state goes into K S and Q S, R into M R and E R, and that into K^T E R, each from the registers where it is.
+// A workgroup takes a request's chunks for one head and 16 NW columns, a wave 16 of them, whose state stays in its registers (fp32).
+// Layout (products 16x16x32, lane = 16 g + r): the lane has column r and, of a pair of result tiles, the rows 32 s + 8 g + 0..7 (operand rows are those of kOperands' comment): as B
+// of the next product those are its own, so the state goes into K S and Q S, R into M R and E R, and that into K^T E R, each from the registers where it is.
 // What is no 16-bit input meets the matrix cores as bf16 terms, each the upper half of what the ones before left, the last one rounded: three (fp32's 24 bits) of E, the state, R and E R on
 // their way to a state, two of the state, M and R on their way to an output, which is rounded to 16 bits.  Inputs in fp16 are two terms each (exact).
+// kStates: what blocks make of a state (columns dv and on: of the identity), without outputs.
 constexpr int kDeltaWaves = 4;
-template <int KD, typename T> __global__ __launch_bounds__(64 * kDeltaWaves, __is_same(T, f16_t) && KD > 2 ? 1 : 2) void delta_prompt_kernel(DeltaPromptParams PP, uint32_t slices) {
+template <int KD, typename T, bool kStates> __global__ __launch_bounds__(64 * kDeltaWaves, !__is_same(T, f16_t) || KD == 2 ? 2 : 1) void delta_prompt_kernel(DeltaPromptParams PP, uint32_t slices) {
     constexpr int NW = kDeltaWaves, kIn = __is_same(T, f16_t) ? 2 : 1, kRow = KD == 2 ? 64 : 128, kPieces = KD * 4;
-    constexpr int kItemsK = 16 * kPieces, kItems = 2 * kItemsK, kPer = (kItems + 64 * NW - 1) / (64 * NW);
-    constexpr int kMatrixPer = (kMatrixPieces + 64 * NW - 1) / (64 * NW);
-    __shared__ __align__(16) uint16_t lds_q[kIn][kChunk][kRow], lds_k[kIn][kChunk][kRow], lds_kt[kIn][KD * 32][kChunk];
-    __shared__ __align__(16) u32x4 lds_m[kMatrixPieces];
+    constexpr int kItemsK = 16 * kPieces, kItems = kStates ? kItemsK : 2 * kItemsK, kPer = (kItems + 64 * NW - 1) / (64 * NW);
+    constexpr uint32_t kMatrix = kStates ? kOperands * kTermsE * 64 : kMatrixPieces;
+    constexpr int kMatrixPer = (kMatrix + 64 * NW - 1) / (64 * NW);
+    __shared__ __align__(16) uint16_t lds_q[kStates ? 1 : kIn][kStates ? 1 : kChunk][kRow], lds_k[kIn][kChunk][kRow], lds_kt[kIn][KD * 32][kChunk];
+    __shared__ __align__(16) u32x4 lds_m[kMatrix];
     __shared__ __align__(16) float lds_d[2 * kChunk];
     const DeltaParams &P = PP.d;
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), g = lane >> 4, r = lane & 15;
-    const uint32_t unit = uniform(blockIdx.x / slices), slice = uniform(blockIdx.x - unit * slices), in_launch = uniform(unit / P.heads), h = uniform(unit - in_launch * P.heads);
-    const uint32_t request = PP.first + in_launch, shared = uniform(h / P.group);
-    const Span span = span_of(P, request);
-    const uint32_t begin = uniform(span.begin), end = uniform(span.end);
-    const uint64_t state = state_of(P, request), matrix = (uint64_t)P.dk * P.dv, state_at = (state * P.heads + h) * matrix;
-    uint32_t number = chunks_before(P, request);
-    if (begin < end && number + (end - begin + kChunk - 1) / kChunk > PP.most_chunks) return;   // (offsets that go backwards)
-    const uint32_t column = slice * (16 * NW) + wave * 16 + r;
-    const bool live_column = column < P.dv, live_wave = slice * (16 * NW) + wave * 16 < P.dv;
+    const BlockPlan plan = plan_blocks(PP);
+    if (kStates && plan.chunks == ~0u) return;
+    const uint32_t each = P.heads * slices;
+    for (uint64_t item = blockIdx.x; item < (uint64_t)plan.blocks * each; item += gridDim.x) {
+    const uint32_t in_order_ = uniform((uint32_t)(item / each)), rest = uniform((uint32_t)(item - (uint64_t)in_order_ * each)), h = uniform(rest / slices), slice = uniform(rest - h * slices);
+    const uint32_t shared = uniform(h / P.group);
+    const BlockPlace at = find_block(PP, plan.chunks, in_order_);
+    const Span span = span_of(P, at.request);
+    const uint32_t block_tokens = plan.chunks == ~0u ? 0u : plan.chunks * kChunk;
+    const uint32_t begin = uniform(span.begin + at.block * block_tokens), end = uniform(at.block + 1 == at.blocks ? span.end : begin + block_tokens);
+    uint32_t number = uniform(at.chunk);
+    if (!at.found || (kStates && at.block + 1 == at.blocks)) continue;
+    if (begin < end && number + (end - begin + kChunk - 1) / kChunk > PP.most_chunks) continue;   // (offsets that go backwards)
+    const uint64_t state = state_of(P, at.request), state_at = (state * P.heads + h) * ((uint64_t)P.dk * P.dv);
+    float *const block_state = PP.block_states + ((uint64_t)at.slot * P.heads + h) * ((uint64_t)P.dk * (P.dv + P.dk));
+    const uint32_t column = (slice * NW + wave) * 16 + r, columns = kStates ? P.dv + P.dk : P.dv;
+    const bool live_column = column < columns, live_wave = (slice * NW + wave) * 16 < columns;   // (columns that are not there compute what nobody reads)
     f32x4 S[2 * KD];
-    const float *from = P.state_in && state != ~0ull ? P.state_in + state_at : nullptr;
+    const float *const from = kStates ? nullptr : at.blocks > 1 ? block_state : P.state_in && state != ~0ull ? P.state_in + state_at : nullptr;
+    const uint32_t from_stride = at.blocks > 1 ? P.dv + P.dk : P.dv;
 #pragma unroll
     for (int i = 0; i < 2 * KD; ++i)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const uint32_t d = (i / 2) * 32 + g * 8 + (i % 2) * 4 + e;
-            S[i][e] = from && live_column && d < P.dk ? from[(uint64_t)d * P.dv + column] : 0.f;
+            S[i][e] = kStates ? (column == P.dv + d ? 1.f : 0.f) : from && live_column && d < P.dk ? from[(uint64_t)d * from_stride + column] : 0.f;
         }
     constexpr uint32_t kNowhere = 1u << 31;
     const uint32_t pieces = P.dk / 8;
     const bool odd_lane = lane & 1;
-    const uint32_t column2 = (column & ~1u) < P.dv ? 2 * (column & ~1u) : kNowhere;   // of the lane's pair of columns, in bytes
+        const uint32_t column2 = (column & ~1u) < P.dv ? 2 * (column & ~1u) : kNowhere;   // of the lane's pair of columns, in bytes
     u32x4 staged[kPer][4], matrices[kMatrixPer];
     float decays = 0.f;
     uint32_t values[2][4];
     const auto chunk_rows = [&](const void *base, uint32_t m, uint32_t stride, uint32_t width) __attribute__((always_inline)) {
         return make_rsrc((const void *)uniform64((uint64_t)base), uniform((m - 1) * stride + width));
     };
+    // A lane brings 4 tokens x 8 components of K or of Q into LDS; a wave has either.
+    struct Part {
+        bool live, is_q;
+        uint32_t row, piece;
+    };
+    const auto part_of = [&](int b) __attribute__((always_inline)) {
+        const uint32_t first = (kItemsK % (64 * NW) ? wave * 64 : 0u) + b * 64 * NW, rest = kItemsK % (64 * NW) ? 0u : wave * 64;   // (known when compiled where they divide)
+        Part p;
+        p.live = first < kItems, p.is_q = !kStates && first >= kItemsK;
+        const uint32_t id = first + rest - (p.is_q ? kItemsK : 0) + lane;
+        p.piece = id % kPieces, p.row = id / kPieces * 4;
+        return p;
+    };
     const auto load_chunk = [&](uint32_t t0, uint32_t chunk) __attribute__((always_inline)) {
         const uint32_t m = min(kChunk, end - t0);
 #pragma unroll
         for (int b = 0; b < kPer; ++b) {
-            const uint32_t first = wave * 64 + b * 64 * NW;
-            if (first < kItems) {
-                const bool is_q = first >= kItemsK;
-                const uint32_t id = first - (is_q ? kItemsK : 0) + lane, piece = id % kPieces, row = id / kPieces * 4;
-                const uint32_t stride = 2 * (uint32_t)(is_q ? P.q_stride : P.k_stride), off = row * stride + (piece < pieces ? piece * 16 : kNowhere);
-                const auto rows = chunk_rows(is_q ? (const T *)P.q + (uint64_t)shared * P.dk + t0 * P.q_stride : (const T *)P.k + (uint64_t)shared * P.dk + t0 * P.k_stride, m, stride, 2 * P.dk);
+            const Part p = part_of(b);
+            if (p.live) {
+                const uint32_t stride = 2 * (uint32_t)(p.is_q ? P.q_stride : P.k_stride), off = p.row * stride + (p.piece < pieces ? p.piece * 16 : kNowhere);
+                const auto rows = chunk_rows(p.is_q ? (const T *)P.q + (uint64_t)shared * P.dk + t0 * P.q_stride : (const T *)P.k + (uint64_t)shared * P.dk + t0 * P.k_stride, m, stride, 2 * P.dk);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) staged[b][j] = __builtin_amdgcn_raw_buffer_load_b128(rows, off + j * stride, 0, 0);
             }
@@ -413,14 +507,14 @@ template <int KD, typename T> __global__ __launch_bounds__(64 * kDeltaWaves, __i
         const char *const made = PP.chunks + ((uint64_t)chunk * P.heads + h) * kChunkBytes;
 #pragma unroll
         for (int b = 0; b < kMatrixPer; ++b)
-            if (b * 64 * NW + wave * 64 < kMatrixPieces) matrices[b] = ((const u32x4 *)made)[b * 64 * NW + tid];
+            if (b * 64 * NW + wave * 64 < kMatrix) matrices[b] = ((const u32x4 *)made)[b * 64 * NW + tid];
         if (tid < 2 * kChunk) decays = ((const float *)(made + kMatrixPieces * 16))[tid];
-        const uint32_t stride = 2 * (uint32_t)P.v_stride, off = (g * 8 + (odd_lane ? 4 : 0)) * stride + column2;
+        const uint32_t stride = 2 * (uint32_t)P.v_stride, off = (g * 8 + (odd_lane ? 4 : 0)) * stride;
         const auto rows = chunk_rows((const T *)P.v + (uint64_t)h * P.dv + t0 * P.v_stride, m, stride, 2 * P.dv);
 #pragma unroll
-        for (int s = 0; s < 2; ++s)
+            for (int s = 0; s < 2; ++s)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) values[s][j] = __builtin_amdgcn_raw_buffer_load_b32(rows, off + (s * 32 + j) * stride, 0, 0);
+                for (int j = 0; j < 4; ++j) values[s][j] = __builtin_amdgcn_raw_buffer_load_b32(rows, off + (s * 32 + j) * stride + column2, 0, 0);
     };
     // LDS rows are pieces of 16 bytes, exchanged by the row's number so that the sixteen rows of an operand, 8 (r / 4) + r % 4 + ..., lie in different banks.  K by component as in
     // rows d: piece u, 8 tokens, at u ^ (2 (d / 8 mod 4) + (d / 2 mod 2)) ^ (d / 32 mod 2), its two halves exchanged where d / 64 is odd: the lanes of a read have d = 8 (r / 4) +
@@ -433,19 +527,21 @@ template <int KD, typename T> __global__ __launch_bounds__(64 * kDeltaWaves, __i
         const u32x4 w = *(const u32x4 *)((const char *)lds_kt[a] + (own_kt ^ (s * 64) ^ (t / 2 % 2 * 16)) + (t / 2) * 32 * 128 + (t % 2) * 4 * 128);
         return t / 4 % 2 ? (u32x4){w[2], w[3], w[0], w[1]} : w;
     };
-    const auto operand = [&](const uint16_t *plane, int tile, int p) __attribute__((always_inline)) {   // rows of tile (s, t) = (tile / 2, tile % 2)
-        const uint32_t row = (tile / 2) * 32 + (tile % 2) * 4 + 8 * (r >> 2) + (r & 3);
-        return *(const u32x4 *)((const char *)plane + row_piece(row, p * 4 + g));
+    // Rows of tile (s, t) = (tile / 2, tile % 2), 32 s + 4 t behind the lane's own: pieces there are exchanged by the same bits.
+    const uint32_t own_rows = row_piece(8 * (r >> 2) + (r & 3), g);
+    const auto operand = [&](const uint16_t *plane, int tile, int p) __attribute__((always_inline)) {
+        return *(const u32x4 *)((const char *)plane + (own_rows ^ (p * 64)) + ((tile / 2) * 32 + (tile % 2) * 4) * 2 * kRow);
     };
     if (begin < end) load_chunk(begin, number);
+    // The first chunk's loads are waited for here: with any of them under way at the loop's head, the compiler's wait there would be for all that the wave has
+    // issued, the stores of the chunk before among them.
+    __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0)
     for (uint32_t t0 = begin; t0 < end; t0 += kChunk, ++number) {
         const uint32_t m = min(kChunk, end - t0);
 #pragma unroll
         for (int b = 0; b < kPer; ++b) {
-            const uint32_t first = wave * 64 + b * 64 * NW;
-            if (first < kItems) {
-                const bool is_q = first >= kItemsK;
-                const uint32_t id = first - (is_q ? kItemsK : 0) + lane, piece = id % kPieces, row = id / kPieces * 4;
+            const Part p = part_of(b);
+            if (p.live) {
 #pragma unroll
                 for (int a = 0; a < kIn; ++a) {
                     uint32_t w[4][4];
@@ -457,12 +553,12 @@ template <int KD, typename T> __global__ __launch_bounds__(64 * kDeltaWaves, __i
                             input_terms<T, kIn>(staged[b][j][i], terms);
                             w[j][i] = terms[a];
                         }
-                    char *const to = is_q ? (char *)lds_q[a] : (char *)lds_k[a];
+                    char *const to = p.is_q ? (char *)lds_q[a] : (char *)lds_k[a];
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) *(u32x4 *)(to + row_piece(row + j, piece)) = (u32x4){w[j][0], w[j][1], w[j][2], w[j][3]};
-                    if (!is_q) {
-                        const uint32_t place = row / 8 ^ (piece & 3) * 2 ^ (piece / 4 & 1), half = (row / 4 & 1) ^ (piece / 8 & 1);
-                        char *const kt = (char *)lds_kt[a] + piece * 8 * 128 + half * 8;
+                    for (int j = 0; j < 4; ++j) *(u32x4 *)(to + row_piece(p.row + j, p.piece)) = (u32x4){w[j][0], w[j][1], w[j][2], w[j][3]};
+                    if (!p.is_q) {
+                        const uint32_t place = p.row / 8 ^ (p.piece & 3) * 2 ^ (p.piece / 4 & 1), half = (p.row / 4 & 1) ^ (p.piece / 8 & 1);
+                        char *const kt = (char *)lds_kt[a] + p.piece * 8 * 128 + half * 8;
 #pragma unroll
                         for (int c = 0; c < 8; ++c) {   // component c of the four tokens
                             const uint32_t sel = c % 2 ? 0x07060302u : 0x05040100u;
@@ -474,163 +570,142 @@ template <int KD, typename T> __global__ __launch_bounds__(64 * kDeltaWaves, __i
         }
 #pragma unroll
         for (int b = 0; b < kMatrixPer; ++b)
-            if (b * 64 * NW + wave * 64 < kMatrixPieces) lds_m[b * 64 * NW + tid] = matrices[b];
+            if (b * 64 * NW + wave * 64 < kMatrix) lds_m[b * 64 * NW + tid] = matrices[b];
         if (tid < 2 * kChunk) lds_d[tid] = decays;
-        // values: tokens 32 s + 8 g + 2 i, + 1 of the lane's column
-        f32x4 R[4];
+        // values: tokens 32 s + 8 g + 2 i, + 1 of the lane's columns
+        u32x4 V[2];
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            const u32x4 own = own_column(values[s], odd_lane);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if constexpr (kIn == 1) {
-                    R[2 * s + i / 2][2 * (i % 2)] = low_half(own[i]), R[2 * s + i / 2][2 * (i % 2) + 1] = high_half(own[i]);
-                } else {
-                    typedef f16_t pair __attribute__((ext_vector_type(2)));
-                    const uint32_t w = own[i];   // (of an element of a vector itself, a bit cast takes the first)
-                    const pair x = __builtin_bit_cast(pair, w);
-                    R[2 * s + i / 2][2 * (i % 2)] = (float)x[0], R[2 * s + i / 2][2 * (i % 2) + 1] = (float)x[1];
-                }
-            }
-        }
+            for (int s = 0; s < 2; ++s) V[s] = own_column(values[s], odd_lane);
         __syncthreads();
         if (t0 + kChunk < end) load_chunk(t0 + kChunk, number + 1);
         if (live_wave) {
-            // K S and Q S
-            f32x4 O[4], Y[4];
+            const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+            f32x4 O[4], R[4], U[4];
+            u32x4 A[2][4], B[2][3];
+            // The products of a chunk in steps of up to four rows of operands, whose loads from LDS are under way while the step before is multiplied (in order: nothing is moved from step to step).
+            //   0 ..: K S and Q S by 32 components and term of the inputs; then E R by its terms and M R by its, for the tokens 32 s .. 32 s + 31; then K^T E R
+            constexpr int kOfS = kStates ? 1 : 2, kOfR = kStates ? kTermsE : kTermsE + kTermsM;   // (states alone: without queries and M)
+            constexpr int kState = kOfS * kIn * KD, kSystem = kState + 2 * kOfR, kUpdate = 2 * ((2 * KD + 3) / 4) * kIn, kSteps = kSystem + kUpdate;
+            const auto fetch = [&](auto number) __attribute__((always_inline)) {
+                constexpr int k = decltype(number)::value;
+                u32x4 (&to)[4] = A[k % 2];
+                if constexpr (k < kState) {
+                    constexpr int p = k / (kOfS * kIn), a = k / kOfS % kIn;
 #pragma unroll
-            for (int p = 0; p < KD; ++p) {
-                u32x4 B[3];
+                    for (int tile = 0; tile < 4; ++tile) to[tile] = operand(k % kOfS ? &lds_q[a][0][0] : &lds_k[a][0][0], tile, p);
+                } else if constexpr (k < kSystem) {
+                    constexpr int s = (k - kState) / kOfR, a = (k - kState) % kOfR, first = s == 0 ? 0 : 4, last = s == 0 ? 4 : 6;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    uint32_t x[3];
-                    take_apart<3>(S[2 * p + i / 2][2 * (i % 2)], S[2 * p + i / 2][2 * (i % 2) + 1], x);
+                    for (int f = first; f < last; ++f) to[f - first] = lds_m[(a < kTermsE ? f * kTermsE + a : kOperands * kTermsE + f * kTermsM + a - kTermsE) * 64 + lane];
+                } else if constexpr (k < kSteps) {
+                    constexpr int a = (k - kSystem) % kIn, each = kUpdate / 2, s = (k - kSystem) / each, first = (k - kSystem) % each / kIn * 4;
 #pragma unroll
-                    for (int c = 0; c < 3; ++c) B[c][i] = x[c];
+                    for (int i = 0; i < 4 && first + i < 2 * KD; ++i) to[i] = kt_tile(a, first + i, s);
                 }
+            };
+            const auto step = [&](auto number) __attribute__((always_inline)) {
+                constexpr int k = decltype(number)::value;
+                fetch(Number<k + 1>());
+                const u32x4 (&from)[4] = A[k % 2];
+                if constexpr (k < kState) {
+                    constexpr int p = k / (kOfS * kIn), a = k / kOfS % kIn, terms = (k % kOfS ? 2 : 3) - a;
+                    f32x4 (&to)[4] = k % kOfS ? O : R;
 #pragma unroll
-                for (int a = 0; a < kIn; ++a) {
-                    u32x4 A[4];
+                    for (int c = 0; c < terms; ++c)
 #pragma unroll
-                    for (int tile = 0; tile < 4; ++tile) A[tile] = operand(&lds_k[a][0][0], tile, p);
+                        for (int tile = 0; tile < 4; ++tile) to[tile] = mfma_bf16(from[tile], B[p % 2][c], p == 0 && a == 0 && c == 0 ? zero : to[tile]);
+                    if constexpr (k % (kOfS * kIn) == kOfS - 1 && p + 1 < KD) three_terms({S[2 * p + 2], S[2 * p + 3]}, B[(p + 1) % 2]);
+                } else if constexpr (k < kSystem) {
+                    constexpr int s = (k - kState) / kOfR, a = (k - kState) % kOfR, first = s == 0 ? 0 : 4, last = s == 0 ? 4 : 6;   // operands; the tile of one behind the fourth is two before it
+                    constexpr int terms = a < kTermsE ? kTermsE - a : kTermsM - (a - kTermsE);
+#pragma unroll
+                    for (int c = 0; c < terms; ++c)
+#pragma unroll
+                        for (int f = first; f < last; ++f) {
+                            const int tile = f < 4 ? f : f - 2;
+                            if (a < kTermsE) U[tile] = mfma_bf16(from[f - first], B[s][c], f < 4 && a == 0 && c == 0 ? zero : U[tile]);
+                            else O[tile] = mfma_bf16(from[f - first], B[s][c], O[tile]);
+                        }
+                    if constexpr (s == 0 && a == 0) three_terms({R[2], R[3]}, B[1]);
+                } else {
+                    constexpr int a = (k - kSystem) % kIn, each = kUpdate / 2, s = (k - kSystem) / each, first = (k - kSystem) % each / kIn * 4;
 #pragma unroll
                     for (int c = 0; c + a < 3; ++c)
 #pragma unroll
-                        for (int tile = 0; tile < 4; ++tile) Y[tile] = mfma_bf16(A[tile], B[c], p == 0 && a == 0 && c == 0 ? (f32x4){0.f, 0.f, 0.f, 0.f} : Y[tile]);
-#pragma unroll
-                    for (int tile = 0; tile < 4; ++tile) A[tile] = operand(&lds_q[a][0][0], tile, p);
-#pragma unroll
-                    for (int c = 0; c + a < 2; ++c)
-#pragma unroll
-                        for (int tile = 0; tile < 4; ++tile) O[tile] = mfma_bf16(A[tile], B[c], p == 0 && a == 0 && c == 0 ? (f32x4){0.f, 0.f, 0.f, 0.f} : O[tile]);
+                        for (int i = 0; i < 4 && first + i < 2 * KD; ++i) S[first + i] = mfma_bf16(from[i], B[s][c], S[first + i]);
+                    if constexpr (s == 0 && (k - kSystem) % each == 0) three_terms({U[2], U[3]}, B[1]);
                 }
-            }
+                __builtin_amdgcn_sched_barrier(0);
+            };
+            three_terms({S[0], S[1]}, B[0]);
+            fetch(Number<0>());
+            in_order<0, kState>(step);
+            // R, from the values
             const auto decay_of = [&](int which, int tile) __attribute__((always_inline)) { return *(const f32x4 *)&lds_d[which * kChunk + (tile / 2) * 32 + g * 8 + (tile % 2) * 4]; };
 #pragma unroll
-            for (int tile = 0; tile < 4; ++tile) R[tile] -= decay_of(0, tile) * Y[tile], O[tile] *= decay_of(1, tile);
-            // U = E R, and M R
-            f32x4 U[4];
+            for (int tile = 0; tile < 4; ++tile) {
+                const f32x4 by = decay_of(0, tile);
+                if (!kStates) O[tile] *= decay_of(1, tile);
 #pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                u32x4 B[3];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    uint32_t x[3];
-                    take_apart<3>(R[2 * s + i / 2][2 * (i % 2)], R[2 * s + i / 2][2 * (i % 2) + 1], x);
-#pragma unroll
-                    for (int c = 0; c < 3; ++c) B[c][i] = x[c];
-                }
-                const int first = s == 0 ? 0 : 4, last = s == 0 ? 4 : 6;   // operands; the tile of one behind the fourth is two before it
-#pragma unroll
-                for (int a = 0; a < 3; ++a) {
-                    u32x4 A[4];
-#pragma unroll
-                    for (int f = first; f < last; ++f) A[f - first] = lds_m[(f * kTermsE + a) * 64 + lane];
-#pragma unroll
-                    for (int c = 0; c + a < 3; ++c)
-#pragma unroll
-                        for (int f = first; f < last; ++f) {
-                            const int tile = f < 4 ? f : f - 2;
-                            U[tile] = mfma_bf16(A[f - first], B[c], f < 4 && a == 0 && c == 0 ? (f32x4){0.f, 0.f, 0.f, 0.f} : U[tile]);
-                        }
-                }
-#pragma unroll
-                for (int a = 0; a < 2; ++a) {
-                    u32x4 A[4];
-#pragma unroll
-                    for (int f = first; f < last; ++f) A[f - first] = lds_m[(kOperands * kTermsE + f * kTermsM + a) * 64 + lane];
-#pragma unroll
-                    for (int c = 0; c + a < 2; ++c)
-#pragma unroll
-                        for (int f = first; f < last; ++f) {
-                            const int tile = f < 4 ? f : f - 2;
-                            O[tile] = mfma_bf16(A[f - first], B[c], O[tile]);
-                        }
+                for (int i = 0; i < 2; ++i) {
+                    const uint32_t w = V[tile / 2][tile % 2 * 2 + i];   // (of an element of a vector itself, a bit cast takes the first)
+                    float x, y;
+                    if constexpr (kIn == 1) {
+                        x = low_half(w), y = high_half(w);
+                    } else {
+                        typedef f16_t pair __attribute__((ext_vector_type(2)));
+                        const pair both = __builtin_bit_cast(pair, w);
+                        x = (float)both[0], y = (float)both[1];
+                    }
+                    R[tile][2 * i] = x - by[2 * i] * R[tile][2 * i], R[tile][2 * i + 1] = y - by[2 * i + 1] * R[tile][2 * i + 1];
                 }
             }
+            three_terms({R[0], R[1]}, B[0]);
+            in_order<kState, kSystem>(step);
             float odd = 0.f;   // NaN if anything that is written is not finite
 #pragma unroll
-            for (int tile = 0; tile < 4; ++tile)
+                for (int tile = 0; tile < 4; ++tile)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) odd = __builtin_fmaf(U[tile][e], 0.f, odd);
+                    for (int e = 0; e < 4; ++e) odd = __builtin_fmaf(U[tile][e], 0.f, odd);
             T *const out = (T *)P.out + ((uint64_t)t0 * P.heads + h) * P.dv;
-            if (!__any(odd != 0.f)) {
+            if (kStates || !__any(odd != 0.f)) {   // (what is not finite leaves no finite state)
                 const float decay = lds_d[kChunk - 1];
 #pragma unroll
                 for (int i = 0; i < 2 * KD; ++i) S[i] *= decay;
+                three_terms({U[0], U[1]}, B[0]);
+                in_order<kSystem, kSteps>(step);
+                __builtin_amdgcn_s_waitcnt(0x0F70);   // (the next chunk's loads, under way all this time: waited for behind the stores they would be waited for with those)
+                if constexpr (!kStates) {   // tokens 0, 1 of a tile's four are the even lane's, 2, 3 the odd one's, both columns of each
+                    const uint32_t stride = 2 * P.heads * P.dv;
+                    const auto rows = chunk_rows(out, m, stride, 2 * P.dv);
 #pragma unroll
-                for (int s = 0; s < 2; ++s) {
-                    u32x4 B[3];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        uint32_t x[3];
-                        take_apart<3>(U[2 * s + i / 2][2 * (i % 2)], U[2 * s + i / 2][2 * (i % 2) + 1], x);
-#pragma unroll
-                        for (int c = 0; c < 3; ++c) B[c][i] = x[c];
+                    for (int tile = 0; tile < 4; ++tile) {
+                        const uint32_t a = pack2<T>(O[tile][0], O[tile][1]), b = pack2<T>(O[tile][2], O[tile][3]);   // own column
+                        const uint32_t got = of_neighbour(odd_lane ? a : b), own = odd_lane ? b : a;              // the lane's two tokens, the other column and this one
+                        const uint32_t left = odd_lane ? got : own, right = odd_lane ? own : got;
+                        const uint32_t off = ((tile / 2) * 32 + g * 8 + (tile % 2) * 4 + (odd_lane ? 2 : 0)) * stride + column2;
+                        __builtin_amdgcn_raw_buffer_store_b32(__builtin_amdgcn_perm(right, left, 0x05040100u), rows, off, 0, 0);
+                        __builtin_amdgcn_raw_buffer_store_b32(__builtin_amdgcn_perm(right, left, 0x07060302u), rows, off + stride, 0, 0);
                     }
-#pragma unroll
-                    for (int first = 0; first < 2 * KD; first += 2)
-#pragma unroll
-                        for (int a = 0; a < kIn; ++a) {
-                            u32x4 A[2];
-#pragma unroll
-                            for (int i = 0; i < 2; ++i) A[i] = kt_tile(a, first + i, s);
-#pragma unroll
-                            for (int c = 0; c + a < 3; ++c)
-#pragma unroll
-                                for (int i = 0; i < 2; ++i) S[first + i] = mfma_bf16(A[i], B[c], S[first + i]);
-                        }
                 }
-                // tokens 0, 1 of a tile's four are the even lane's, 2, 3 the odd one's, both columns of each
-                const uint32_t stride = 2 * P.heads * P.dv;
-                const auto rows = chunk_rows(out, m, stride, 2 * P.dv);
-#pragma unroll
-                for (int tile = 0; tile < 4; ++tile) {
-                    const uint32_t a = pack2<T>(O[tile][0], O[tile][1]), b = pack2<T>(O[tile][2], O[tile][3]);   // own column
-                    const uint32_t got = of_neighbour(odd_lane ? a : b), own = odd_lane ? b : a;              // the lane's two tokens, the other column and this one
-                    const uint32_t left = odd_lane ? got : own, right = odd_lane ? own : got;
-                    const uint32_t off = ((tile / 2) * 32 + g * 8 + (tile % 2) * 4 + (odd_lane ? 2 : 0)) * stride + column2;
-                    __builtin_amdgcn_raw_buffer_store_b32(__builtin_amdgcn_perm(right, left, 0x05040100u), rows, off, 0, 0);
-                    __builtin_amdgcn_raw_buffer_store_b32(__builtin_amdgcn_perm(right, left, 0x07060302u), rows, off + stride, 0, 0);
-                }
-            } else {   // token by token: what is not finite must not meet the zeros of earlier ones
-                const T *const pv = (const T *)P.v + (uint64_t)h * P.dv + (live_column ? column : 0);
+            } else if constexpr (!kStates) {   // token by token: what is not finite must not meet the zeros of earlier ones
                 for (uint32_t j = 0; j < m; ++j) {
                     const uint64_t at_token = (uint64_t)(t0 + j) * P.heads + h;
-                    const float by = exp_of(P.log_decay[at_token]), beta = P.beta[at_token], v = to_f32(pv[(t0 + j) * P.v_stride]);
+                    const float by = exp_of(P.log_decay[at_token]), beta = P.beta[at_token];
                     const auto component = [&](const uint16_t (*plane)[kChunk][kRow], int p, int c) __attribute__((always_inline)) {   // 32 p + 8 g + c
                         float x = 0.f;
 #pragma unroll
                         for (int a = 0; a < kIn; ++a) x += low_half(*(const uint16_t *)((const char *)plane[a] + row_piece(j, p * 4 + g) + 2 * c));
                         return x;
                     };
+                    const float v = live_column ? to_f32(((const T *)P.v)[(t0 + j) * P.v_stride + (uint64_t)h * P.dv + column]) : 0.f;
                     float y = 0.f, o = 0.f;
 #pragma unroll
                     for (int p = 0; p < KD; ++p)
 #pragma unroll
                         for (int c = 0; c < 8; ++c) {
-                            const float x = S[2 * p + c / 4][c % 4] * by;
-                            S[2 * p + c / 4][c % 4] = x;
+                            float &x = ((float *)&S[2 * p + c / 4])[c % 4];
+                            x *= by;
                             if (p * 32 + g * 8 < P.dk) y += component(lds_k, p, c) * x;
                         }
                     y += __shfl_xor(y, 16);
@@ -641,8 +716,9 @@ template <int KD, typename T> __global__ __launch_bounds__(64 * kDeltaWaves, __i
 #pragma unroll
                         for (int c = 0; c < 8; ++c)
                             if (p * 32 + g * 8 < P.dk) {
-                                S[2 * p + c / 4][c % 4] += component(lds_k, p, c) * u;
-                                o += component(lds_q, p, c) * S[2 * p + c / 4][c % 4];
+                                float &x = ((float *)&S[2 * p + c / 4])[c % 4];
+                                x += component(lds_k, p, c) * u;
+                                o += component(lds_q, p, c) * x;
                             }
                     o += __shfl_xor(o, 16);
                     o += __shfl_xor(o, 32);
@@ -652,15 +728,93 @@ template <int KD, typename T> __global__ __launch_bounds__(64 * kDeltaWaves, __i
         }
         __syncthreads();   // (keys, queries and matrices are free)
     }
-    float *to = P.state_out && state != ~0ull ? P.state_out + state_at : nullptr;
+    float *const to = kStates ? block_state : at.block + 1 == at.blocks && P.state_out && state != ~0ull ? P.state_out + state_at : nullptr;
+    const uint32_t to_stride = kStates ? P.dv + P.dk : P.dv;
     if (to && live_column)
 #pragma unroll
         for (int i = 0; i < 2 * KD; ++i)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const uint32_t d = (i / 2) * 32 + g * 8 + (i % 2) * 4 + e;
-                if (d < P.dk) to[(uint64_t)d * P.dv + column] = S[i][e];
+                if (d < P.dk) to[(uint64_t)d * to_stride + column] = S[i][e];
             }
+    }
+}
+
+// The state before each block of the requests that are taken apart, over the blocks' B: S_(b + 1) = A_b S_b + B_b.  A workgroup has 16 columns, wave w the rows 32 w .. 32 w + 31; the rows
+// go from wave to wave through LDS.  Both operands are fp32: three terms each.
+template <int KD> __global__ __launch_bounds__(64 * KD) void delta_states_kernel(DeltaPromptParams PP) {
+    __shared__ __align__(16) float state_rows[2][16][KD * 32 + 4];
+    const DeltaParams &P = PP.d;
+    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), g = lane >> 4, r = lane & 15;
+    const BlockPlan plan = plan_blocks(PP);
+    if (plan.chunks == ~0u) return;
+    const uint32_t slices = (P.dv + 15) / 16, each = P.heads * slices, wide = P.dv + P.dk;
+    for (uint64_t item = blockIdx.x; item < (uint64_t)P.n * each; item += gridDim.x) {
+        const uint32_t request = uniform((uint32_t)(item / each)), rest = uniform((uint32_t)(item - (uint64_t)request * each)), h = uniform(rest / slices), slice = uniform(rest - h * slices);
+        const uint32_t blocks = uniform(blocks_in(chunks_of(span_of(P, request)), plan.chunks));
+        if (blocks == 1) continue;
+        uint32_t mine = 0;   // slots before this request's
+        for (uint32_t i = lane; i < request; i += 64) {
+            const uint32_t b = blocks_in(chunks_of(span_of(P, i)), plan.chunks);
+            mine += b > 1 ? b : 0u;
+        }
+        const uint32_t slot = wave_sum32(mine), column = slice * 16 + r, first_row = wave * 32 + g * 8;
+        if (slot + blocks > PP.slots) continue;
+        const uint64_t step = P.heads * (uint64_t)P.dk * wide, state = state_of(P, request);
+        float *const matrices = PP.block_states + ((uint64_t)slot * P.heads + h) * ((uint64_t)P.dk * wide);
+        const bool live = column < P.dv && first_row < P.dk;
+        f32x4 x[2], A[2][KD][2], B[2];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            x[i / 4][i % 4] = live && P.state_in && state != ~0ull ? P.state_in[(state * P.heads + h) * ((uint64_t)P.dk * P.dv) + (uint64_t)(first_row + i) * P.dv + column] : 0.f;
+        const auto load = [&](uint32_t b) __attribute__((always_inline)) {
+            const float *const from = matrices + b * step;
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const uint32_t row = wave * 32 + 8 * (r >> 2) + 4 * t + (r & 3);
+#pragma unroll
+                for (int p = 0; p < KD; ++p)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        A[t][p][i] = (f32x4){0.f, 0.f, 0.f, 0.f};
+                        if (row < P.dk && p * 32 + g * 8 < P.dk) A[t][p][i] = *(const f32x4 *)(from + (uint64_t)row * wide + P.dv + p * 32 + g * 8 + 4 * i);
+                    }
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) B[i / 4][i % 4] = live ? from[(uint64_t)(first_row + i) * wide + column] : 0.f;
+        };
+        load(0);
+        for (uint32_t b = 0; b < blocks; ++b) {
+            if (live)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) matrices[b * step + (uint64_t)(first_row + i) * wide + column] = x[i / 4][i % 4];
+            if (b + 1 == blocks) break;
+            float (*const rows)[KD * 32 + 4] = state_rows[b & 1];
+            *(f32x4 *)&rows[r][first_row] = x[0], *(f32x4 *)&rows[r][first_row + 4] = x[1];
+            __syncthreads();   // (one barrier a block: the other rows are written behind it)
+            u32x4 a[2][KD][3];
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int p = 0; p < KD; ++p) three_terms(A[t][p], a[t][p]);
+            x[0] = B[0], x[1] = B[1];
+            if (b + 2 < blocks) load(b + 1);
+#pragma unroll
+            for (int p = 0; p < KD; ++p) {
+                const f32x4 s[2] = {*(const f32x4 *)&rows[r][p * 32 + g * 8], *(const f32x4 *)&rows[r][p * 32 + g * 8 + 4]};
+                u32x4 terms[3];
+                three_terms(s, terms);
+#pragma unroll
+                for (int i = 0; i < 3; ++i)
+#pragma unroll
+                    for (int c = 0; c + i < 3; ++c)
+#pragma unroll
+                        for (int t = 0; t < 2; ++t) x[t] = mfma_bf16(a[t][p][i], terms[c], x[t]);
+            }
+        }
+        __syncthreads();   // (the rows are free)
+    }
 }
 
 }  // namespace

@@ -2,6 +2,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+
 #include "mmvseg.h"
 
 #include "values.h"

@@ -46,9 +46,20 @@ template <typename T> mmv_status launch_tokens(DeltaParams P, hipStream_t s) {
 }
 mmv_status delta_step_call(const DeltaParams &P, int type, hipStream_t s) { return type == MMV_TYPE_F16 ? launch_tokens<f16_t>(P, s) : launch_tokens<bf16_t>(P, s); }
 
-// Chunks that the requests can have together.
+// Chunks that the requests can have together, and blocks of a head that the device has at once (two workgroups on a compute unit).
 inline uint64_t delta_chunks(uint64_t n, uint64_t tokens) { return tokens / kChunk + (n < tokens ? n : tokens); }
-inline size_t delta_workspace(uint64_t n, uint64_t tokens, uint32_t heads, uint32_t, uint32_t) { return (size_t)delta_chunks(n, tokens) * heads * kChunkBytes; }
+inline uint32_t delta_slices(uint32_t columns) { return (columns + 16 * kDeltaWaves - 1) / (16 * kDeltaWaves); }
+// States of blocks: a request of more than one block fills more than half of its own, and a block is as large as the plan on the device makes it, or kLeastBlock.  0: never taken apart.
+inline uint32_t delta_round(uint32_t heads, uint32_t dv) { return 2 * kUnits / (heads * delta_slices(dv)); }
+inline uint64_t delta_slots(uint64_t n, uint64_t tokens, uint32_t heads, uint32_t dv) {
+    const uint64_t chunks = delta_chunks(n, tokens), round = delta_round(heads, dv), most = 2 * kBlockRounds * round;
+    if (round <= kApart || tokens <= (kLeastApart - 1) * kChunk) return 0;
+    return 2 * chunks / kLeastBlock < most ? 2 * chunks / kLeastBlock : most;
+}
+inline size_t delta_chunk_bytes(uint64_t n, uint64_t tokens, uint32_t heads) { return (size_t)delta_chunks(n, tokens) * heads * kChunkBytes; }
+inline size_t delta_workspace(uint64_t n, uint64_t tokens, uint32_t heads, uint32_t dk, uint32_t dv) {
+    return delta_chunk_bytes(n, tokens, heads) + round256((size_t)delta_slots(n, tokens, heads, dv) * heads * dk * (dk + dv) * 4);
+}
 template <typename T> mmv_status launch_chunks(DeltaPromptParams P, hipStream_t s) {
     const uint32_t most = most_of_a_launch(256, P.d.heads);
     for (; P.first < P.most_chunks; P.first += most) {
@@ -57,13 +68,21 @@ template <typename T> mmv_status launch_chunks(DeltaPromptParams P, hipStream_t 
     }
     return MMV_OK;
 }
-template <int KD, typename T> mmv_status launch_delta_prompts(DeltaPromptParams P, hipStream_t s) {
-    const uint32_t slices = (uint32_t)ceil_div(P.d.dv, 16 * kDeltaWaves), each = P.d.heads * slices, most = most_of_a_launch(64 * kDeltaWaves, each);
-    for (; P.first < P.d.n; P.first += most) {
-        delta_prompt_kernel<KD, T><<<(P.d.n - P.first < most ? P.d.n - P.first : most) * each, 64 * kDeltaWaves, 0, s>>>(P, slices);
+// Workgroups go on to the next block by themselves: where nothing is taken apart, the launches for that are of as many as the device holds.
+constexpr uint64_t kMostWorkgroups = 1u << 22;
+template <int KD, typename T> mmv_status launch_delta_prompts(const DeltaPromptParams &P, hipStream_t s) {
+    if (P.block_states) {
+        const uint32_t slices = delta_slices(P.d.dv + P.d.dk);
+        delta_prompt_kernel<KD, T, true><<<4 * kUnits, 64 * kDeltaWaves, 0, s>>>(P, slices);
+        if (const mmv_status st = launched()) return st;
+        delta_states_kernel<KD><<<4 * kUnits, 64 * KD, 0, s>>>(P);
         if (const mmv_status st = launched()) return st;
     }
-    return MMV_OK;
+    const uint32_t slices = delta_slices(P.d.dv);
+    uint64_t blocks = (uint64_t)P.d.n * P.d.heads * slices;
+    if (P.block_states && blocks < 4 * kUnits) blocks = 4 * kUnits;
+    delta_prompt_kernel<KD, T, false><<<(unsigned)(blocks < kMostWorkgroups ? blocks : kMostWorkgroups), 64 * kDeltaWaves, 0, s>>>(P, slices);
+    return launched();
 }
 template <typename T> mmv_status delta_prompts(const DeltaPromptParams &P, hipStream_t s) {
     if (const mmv_status st = launch_chunks<T>(P, s)) return st;
@@ -75,6 +94,8 @@ template <typename T> mmv_status delta_prompts(const DeltaPromptParams &P, hipSt
 mmv_status delta_call(const DeltaParams &d, int type, void *d_ws, hipStream_t s) {
     DeltaPromptParams P = {};
     P.d = d, P.chunks = (char *)d_ws, P.most_chunks = (uint32_t)delta_chunks(d.n, d.tokens);
+    P.slots = (uint32_t)delta_slots(d.n, d.tokens, d.heads, d.dv), P.round = delta_round(d.heads, d.dv);
+    if (P.slots) P.block_states = (float *)((char *)d_ws + delta_chunk_bytes(d.n, d.tokens, d.heads));
     return type == MMV_TYPE_F16 ? delta_prompts<f16_t>(P, s) : delta_prompts<bf16_t>(P, s);
 }
 
