@@ -178,7 +178,7 @@ __device__ __forceinline__ ChunkPlace find_chunk(const DeltaParams &P, uint32_t 
 // Requests in blocks.  Chunks of a request depend on each other through the state.  Where few long requests would leave the device idle they are taken apart into blocks of as many chunks: what a
 // block makes of a state, S -> A S + B, is found for all blocks at once (A from the columns of the identity, B from a state of zeros), then the state before each block, then all blocks' outputs.
 // That is 2.3 times the work, so it is done where the longest request has over kApart times an even share of the chunks.
-constexpr uint32_t kApart = 3, kBlockRounds = 3, kLeastBlock = 4, kLeastApart = 16;
+constexpr uint32_t kApart = 3, kLeastBlock = 4, kLeastApart = 16;
 struct BlockPlan {
     uint32_t chunks, blocks;   // chunks of a block (~0: all of a request), blocks in all
 };
@@ -197,7 +197,7 @@ __device__ __forceinline__ BlockPlan plan_blocks(const DeltaPromptParams &PP) {
     for (int d = 1; d < 64; d <<= 1) most = max(most, (uint32_t)__shfl_xor((int)most, d));
     most = uniform(most);
     if (most < kLeastApart || (uint64_t)most * PP.round <= (uint64_t)kApart * all) return {~0u, P.n};
-    const uint32_t block = max(kLeastBlock, (all + kBlockRounds * PP.round - 1) / (kBlockRounds * PP.round));
+    const uint32_t block = max(kLeastBlock, (all + PP.round - 1) / PP.round);
     uint32_t blocks = 0;
     for (uint32_t r = lane; r < P.n; r += 64) blocks += blocks_in(chunks_of(span_of(P, r)), block);
     return {block, wave_sum32(blocks)};
@@ -235,6 +235,11 @@ __device__ __forceinline__ BlockPlace find_block(const DeltaPromptParams &PP, ui
     return {0, 0, 0, 0, 0, false};
 }
 
+// The value itself, made anew where it is used (no instruction): what follows from it is not kept in registers all through a loop.
+__device__ __forceinline__ uint32_t here(uint32_t v) {
+    asm volatile("" : "+v"(v));
+    return v;
+}
 // Eight values of a lane as the three terms of an operand.
 __device__ __forceinline__ void three_terms(const f32x4 (&x)[2], u32x4 (&to)[3]) {
 #pragma unroll
@@ -347,43 +352,41 @@ template <typename T> __global__ __launch_bounds__(256, 4) void delta_chunks_ker
         for (int e = 0; e < 4; ++e) X[4 * g + e][16 + r] = 0.f, X[32 + 4 * g + e][48 + r] = 0.f;
     }
     __syncthreads();
-    f32x4 T_[4];   // blocks (i, wave)
+    f32x4 T_[4], M[4];   // blocks (i, wave); before a block of T is there, the sum that it is made of.  (products of as many blocks as there are, in turn: none waits for the one before)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if ((uint32_t)i == wave) {
+    for (int i = 0; i < 4; ++i) T_[i] = M[i] = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int e = 0; e < 4; ++e) T_[i][e] = X[i * 16 + 4 * g + e][i * 16 + r];
-        } else if ((uint32_t)i > wave) {
-            f32x4 x = {0.f, 0.f, 0.f, 0.f}, y = x;
+    for (int c = 0; c < 4; ++c)
+        if ((uint32_t)c >= wave) {
+            if ((uint32_t)c == wave) {
 #pragma unroll
-            for (int c = 0; c < i; ++c)
-                if ((uint32_t)c >= wave) {
-                    const f32x4 l = *(const f32x4 *)&LW[i * 16 + r][c * 16 + 4 * g];
+                for (int e = 0; e < 4; ++e) T_[c][e] = X[c * 16 + 4 * g + e][c * 16 + r];
+            } else {
+                const f32x4 d = *(const f32x4 *)&X[c * 16 + r][c * 16 + 4 * g];
+                f32x4 y = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) x = mfma_f32(l[e], T_[c][e], x);
+                for (int e = 0; e < 4; ++e) y = mfma_f32(d[e], -T_[c][e], y);
+                T_[c] = y;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) X[c * 16 + 4 * g + e][wave * 16 + r] = y[e];
+            }
+            f32x4 l[4], w[4];
+#pragma unroll
+            for (int i = c; i < 4; ++i) {
+                if (i > c) l[i] = *(const f32x4 *)&LW[i * 16 + r][c * 16 + 4 * g];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t column = c * 16 + 4 * g + e, row = i * 16 + r;
+                    w[i][e] = c < i || column <= row ? LW[column][row] : 0.f;
                 }
-            const f32x4 d = *(const f32x4 *)&X[i * 16 + r][i * 16 + 4 * g];
+            }
 #pragma unroll
-            for (int e = 0; e < 4; ++e) y = mfma_f32(d[e], -x[e], y);
-            T_[i] = y;
+            for (int e = 0; e < 4; ++e) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) X[i * 16 + 4 * g + e][wave * 16 + r] = y[e];
-        }
-    }
-    f32x4 M[4];
+                for (int i = c + 1; i < 4; ++i) T_[i] = mfma_f32(l[i][e], T_[c][e], T_[i]);
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-        if ((uint32_t)i >= wave) {
-            M[i] = (f32x4){0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int c = 0; c <= i; ++c)
-                if ((uint32_t)c >= wave) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const uint32_t column = c * 16 + 4 * g + e, row = i * 16 + r;
-                        M[i] = mfma_f32(c < i || column <= row ? LW[column][row] : 0.f, T_[c][e], M[i]);
-                    }
-                }
+                for (int i = c; i < 4; ++i) M[i] = mfma_f32(w[i][e], T_[c][e], M[i]);
+            }
         }
     __syncthreads();
     const auto write_operands = [&](auto terms_of, uint32_t first, auto rows_by) __attribute__((always_inline)) {
@@ -441,11 +444,11 @@ template <int KD, typename T, bool kStates> __global__ __launch_bounds__(64 * kD
     __shared__ __align__(16) u32x4 lds_m[kMatrix];
     __shared__ __align__(16) float lds_d[2 * kChunk];
     const DeltaParams &P = PP.d;
-    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), g = lane >> 4, r = lane & 15;
     const BlockPlan plan = plan_blocks(PP);
     if (kStates && plan.chunks == ~0u) return;
     const uint32_t each = P.heads * slices;
     for (uint64_t item = blockIdx.x; item < (uint64_t)plan.blocks * each; item += gridDim.x) {
+    const uint32_t tid = here(threadIdx.x), lane = tid & 63, wave = uniform(tid >> 6), g = lane >> 4, r = lane & 15;
     const uint32_t in_order_ = uniform((uint32_t)(item / each)), rest = uniform((uint32_t)(item - (uint64_t)in_order_ * each)), h = uniform(rest / slices), slice = uniform(rest - h * slices);
     const uint32_t shared = uniform(h / P.group);
     const BlockPlace at = find_block(PP, plan.chunks, in_order_);
@@ -479,6 +482,7 @@ template <int KD, typename T, bool kStates> __global__ __launch_bounds__(64 * kD
     const auto chunk_rows = [&](const void *base, uint32_t m, uint32_t stride, uint32_t width) __attribute__((always_inline)) {
         return make_rsrc((const void *)uniform64((uint64_t)base), uniform((m - 1) * stride + width));
     };
+    const auto anew = [&](uint32_t v) __attribute__((always_inline)) { return KD > 2 ? here(v) : v; };   // (addresses that stay would fill the registers)
     // A lane brings 4 tokens x 8 components of K or of Q into LDS; a wave has either.
     struct Part {
         bool live, is_q;
@@ -488,7 +492,7 @@ template <int KD, typename T, bool kStates> __global__ __launch_bounds__(64 * kD
         const uint32_t first = (kItemsK % (64 * NW) ? wave * 64 : 0u) + b * 64 * NW, rest = kItemsK % (64 * NW) ? 0u : wave * 64;   // (known when compiled where they divide)
         Part p;
         p.live = first < kItems, p.is_q = !kStates && first >= kItemsK;
-        const uint32_t id = first + rest - (p.is_q ? kItemsK : 0) + lane;
+        const uint32_t id = first + rest - (p.is_q ? kItemsK : 0) + anew(lane);
         p.piece = id % kPieces, p.row = id / kPieces * 4;
         return p;
     };
@@ -507,9 +511,9 @@ template <int KD, typename T, bool kStates> __global__ __launch_bounds__(64 * kD
         const char *const made = PP.chunks + ((uint64_t)chunk * P.heads + h) * kChunkBytes;
 #pragma unroll
         for (int b = 0; b < kMatrixPer; ++b)
-            if (b * 64 * NW + wave * 64 < kMatrix) matrices[b] = ((const u32x4 *)made)[b * 64 * NW + tid];
+            if (b * 64 * NW + wave * 64 < kMatrix) matrices[b] = ((const u32x4 *)made)[b * 64 * NW + anew(tid)];
         if (tid < 2 * kChunk) decays = ((const float *)(made + kMatrixPieces * 16))[tid];
-        const uint32_t stride = 2 * (uint32_t)P.v_stride, off = (g * 8 + (odd_lane ? 4 : 0)) * stride;
+        const uint32_t stride = 2 * (uint32_t)P.v_stride, off = (anew(g) * 8 + (odd_lane ? 4 : 0)) * stride;
         const auto rows = chunk_rows((const T *)P.v + (uint64_t)h * P.dv + t0 * P.v_stride, m, stride, 2 * P.dv);
 #pragma unroll
             for (int s = 0; s < 2; ++s)
@@ -581,14 +585,16 @@ template <int KD, typename T, bool kStates> __global__ __launch_bounds__(64 * kD
         if (live_wave) {
             const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
             f32x4 O[4], R[4], U[4];
-            u32x4 A[2][4], B[2][3];
-            // The products of a chunk in steps of up to four rows of operands, whose loads from LDS are under way while the step before is multiplied (in order: nothing is moved from step to step).
-            //   0 ..: K S and Q S by 32 components and term of the inputs; then E R by its terms and M R by its, for the tokens 32 s .. 32 s + 31; then K^T E R
+            constexpr bool kAhead = KD == 2;
+            u32x4 A[kAhead ? 2 : 1][4], B[2][3];
+            // The products of a chunk in steps of up to four rows of operands: K S and Q S by 32 components and term of the inputs; then E R by its terms and M R by its, for the tokens
+            // 32 s .. 32 s + 31; then K^T E R.  kAhead: a step's loads from LDS are under way while the step before is multiplied, and nothing is moved from step to step (up to 64 components:
+            // 3 prompts of 900 tokens 42 -> 39 us; with more there are no registers for it).
             constexpr int kOfS = kStates ? 1 : 2, kOfR = kStates ? kTermsE : kTermsE + kTermsM;   // (states alone: without queries and M)
             constexpr int kState = kOfS * kIn * KD, kSystem = kState + 2 * kOfR, kUpdate = 2 * ((2 * KD + 3) / 4) * kIn, kSteps = kSystem + kUpdate;
             const auto fetch = [&](auto number) __attribute__((always_inline)) {
                 constexpr int k = decltype(number)::value;
-                u32x4 (&to)[4] = A[k % 2];
+                u32x4 (&to)[4] = A[kAhead ? k % 2 : 0];
                 if constexpr (k < kState) {
                     constexpr int p = k / (kOfS * kIn), a = k / kOfS % kIn;
 #pragma unroll
@@ -605,8 +611,9 @@ template <int KD, typename T, bool kStates> __global__ __launch_bounds__(64 * kD
             };
             const auto step = [&](auto number) __attribute__((always_inline)) {
                 constexpr int k = decltype(number)::value;
-                fetch(Number<k + 1>());
-                const u32x4 (&from)[4] = A[k % 2];
+                if constexpr (kAhead) fetch(Number<k + 1>());
+                else fetch(number);
+                const u32x4 (&from)[4] = A[kAhead ? k % 2 : 0];
                 if constexpr (k < kState) {
                     constexpr int p = k / (kOfS * kIn), a = k / kOfS % kIn, terms = (k % kOfS ? 2 : 3) - a;
                     f32x4 (&to)[4] = k % kOfS ? O : R;
@@ -635,10 +642,10 @@ template <int KD, typename T, bool kStates> __global__ __launch_bounds__(64 * kD
                         for (int i = 0; i < 4 && first + i < 2 * KD; ++i) S[first + i] = mfma_bf16(from[i], B[s][c], S[first + i]);
                     if constexpr (s == 0 && (k - kSystem) % each == 0) three_terms({U[2], U[3]}, B[1]);
                 }
-                __builtin_amdgcn_sched_barrier(0);
+                if constexpr (kAhead) __builtin_amdgcn_sched_barrier(0);
             };
             three_terms({S[0], S[1]}, B[0]);
-            fetch(Number<0>());
+            if constexpr (kAhead) fetch(Number<0>());
             in_order<0, kState>(step);
             // R, from the values
             const auto decay_of = [&](int which, int tile) __attribute__((always_inline)) { return *(const f32x4 *)&lds_d[which * kChunk + (tile / 2) * 32 + g * 8 + (tile % 2) * 4]; };
@@ -677,13 +684,14 @@ template <int KD, typename T, bool kStates> __global__ __launch_bounds__(64 * kD
                 __builtin_amdgcn_s_waitcnt(0x0F70);   // (the next chunk's loads, under way all this time: waited for behind the stores they would be waited for with those)
                 if constexpr (!kStates) {   // tokens 0, 1 of a tile's four are the even lane's, 2, 3 the odd one's, both columns of each
                     const uint32_t stride = 2 * P.heads * P.dv;
+                    const uint32_t own = (anew(g) * 8 + (odd_lane ? 2 : 0)) * stride + column2;
                     const auto rows = chunk_rows(out, m, stride, 2 * P.dv);
 #pragma unroll
                     for (int tile = 0; tile < 4; ++tile) {
                         const uint32_t a = pack2<T>(O[tile][0], O[tile][1]), b = pack2<T>(O[tile][2], O[tile][3]);   // own column
-                        const uint32_t got = of_neighbour(odd_lane ? a : b), own = odd_lane ? b : a;              // the lane's two tokens, the other column and this one
-                        const uint32_t left = odd_lane ? got : own, right = odd_lane ? own : got;
-                        const uint32_t off = ((tile / 2) * 32 + g * 8 + (tile % 2) * 4 + (odd_lane ? 2 : 0)) * stride + column2;
+                        const uint32_t got = of_neighbour(odd_lane ? a : b), mine = odd_lane ? b : a;              // the lane's two tokens, the other column and this one
+                        const uint32_t left = odd_lane ? got : mine, right = odd_lane ? mine : got;
+                        const uint32_t off = own + ((tile / 2) * 32 + (tile % 2) * 4) * stride;
                         __builtin_amdgcn_raw_buffer_store_b32(__builtin_amdgcn_perm(right, left, 0x05040100u), rows, off, 0, 0);
                         __builtin_amdgcn_raw_buffer_store_b32(__builtin_amdgcn_perm(right, left, 0x07060302u), rows, off + stride, 0, 0);
                     }

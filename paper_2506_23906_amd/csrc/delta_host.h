@@ -52,7 +52,7 @@ inline uint32_t delta_slices(uint32_t columns) { return (columns + 16 * kDeltaWa
 // States of blocks: a request of more than one block fills more than half of its own, and a block is as large as the plan on the device makes it, or kLeastBlock.  0: never taken apart.
 inline uint32_t delta_round(uint32_t heads, uint32_t dv) { return 2 * kUnits / (heads * delta_slices(dv)); }
 inline uint64_t delta_slots(uint64_t n, uint64_t tokens, uint32_t heads, uint32_t dv) {
-    const uint64_t chunks = delta_chunks(n, tokens), round = delta_round(heads, dv), most = 2 * kBlockRounds * round;
+    const uint64_t chunks = delta_chunks(n, tokens), round = delta_round(heads, dv), most = 2 * round;
     if (round <= kApart || tokens <= (kLeastApart - 1) * kChunk) return 0;
     return 2 * chunks / kLeastBlock < most ? 2 * chunks / kLeastBlock : most;
 }
