@@ -44,7 +44,7 @@ mmv_status mmv_block_read(uint64_t n, uint64_t tokens, const int32_t *d_offsets,
     BlockReadParams P = {};
     P.c = block_cache_params(*cache);
     P.offsets = d_offsets, P.first = d_first, P.table = d_table, P.table_stride = table_stride, P.table_width = (uint32_t)table_width;
-    P.n = (uint32_t)n, P.tokens = (uint32_t)tokens, P.token_pieces = divider((uint32_t)(values / 8)), P.page = divider(cache->page);
+    P.n = (uint32_t)n, P.tokens = (uint32_t)tokens, P.token_pieces = (uint32_t)(values / 8), P.page = divider(cache->page);
     P.k = d_k, P.v = d_v, P.k_stride = k_stride, P.v_stride = v_stride;
     return block_read_call(P, type, cache->type == MMV_TYPE_I8, (hipStream_t)hip_stream);
 }

@@ -27,26 +27,34 @@ inline BlockCacheParams block_cache_params(const mmv_block_cache &c) {
 }
 
 // Tokens whose runs one wave looks after: one where there are few waves' worth of them (every run in a wave of its own, at once), else as many as a
-// block holds: most windows of a prompt then have one run to begin.
+// block holds: most windows of a prompt then have one run to begin (windows of 16 and 8 tokens for blocks of 32 take 11 % and 40 % longer, by the waves that find nothing to do).
 constexpr uint64_t kFewWaves = 16384;
+template <int kHeld> mmv_status launch_append(const BlockAppendParams &P, unsigned blocks, int type, bool int8, hipStream_t s) {
+    if (type == MMV_TYPE_F16) int8 ? block_append_kernel<kHeld, f16_t, true><<<blocks, 256, 0, s>>>(P) : block_append_kernel<kHeld, f16_t, false><<<blocks, 256, 0, s>>>(P);
+    else int8 ? block_append_kernel<kHeld, bf16_t, true><<<blocks, 256, 0, s>>>(P) : block_append_kernel<kHeld, bf16_t, false><<<blocks, 256, 0, s>>>(P);
+    return launched();
+}
+// Registers for the runs that there can be, or for their first part where they are too long anyway: us with 2 / 4 / 8 times 64 pieces, 17600 tokens of 8 heads of 128 (16 pieces) in blocks of
+// 8 24.1 / 27.7 / 32.8, of 16 24.3 / 22.9 / 24.0, of 32 28.9 / 27.7 / 25.1, of 64 30.9 / 31.8 / 33.8; single tokens 4.4 / 4.7 / 5.2.
 mmv_status block_append_call(BlockAppendParams P, int type, bool int8, hipStream_t s) {
     const uint64_t each = 2ull * P.c.heads;
     P.window = P.tokens * each <= kFewWaves ? 1 : P.c.block < 32 ? P.c.block : 32;
+    const uint32_t pieces = P.window == 1 ? 0 : P.c.block * P.c.pieces.divisor;
     const uint64_t windows = ceil_div(P.tokens, P.window), most = ((1ull << 32) - 256) / 64 / each;
     for (uint64_t first = 0; first < windows; first += most) {
         P.first_window = (uint32_t)first, P.windows = (uint32_t)(windows - first < most ? windows - first : most);
         const unsigned blocks = (unsigned)ceil_div(P.windows * each, 4);
-        if (type == MMV_TYPE_F16) int8 ? block_append_kernel<f16_t, true><<<blocks, 256, 0, s>>>(P) : block_append_kernel<f16_t, false><<<blocks, 256, 0, s>>>(P);
-        else int8 ? block_append_kernel<bf16_t, true><<<blocks, 256, 0, s>>>(P) : block_append_kernel<bf16_t, false><<<blocks, 256, 0, s>>>(P);
-        if (const mmv_status st = launched()) return st;
+        const mmv_status st = pieces <= 128 || pieces > 512 ? launch_append<2>(P, blocks, type, int8, s) : pieces <= 256 ? launch_append<4>(P, blocks, type, int8, s) : launch_append<8>(P, blocks, type, int8, s);
+        if (st) return st;
     }
     return MMV_OK;
 }
 mmv_status block_read_call(BlockReadParams P, int type, bool int8, hipStream_t s) {
-    const uint64_t each = P.token_pieces.divisor, most = (k2to31 - 256) / each;   // tokens of a launch: its pieces have numbers below 2^31
+    const uint64_t most = (1ull << 26) * kReadTokens - 4 * kReadTokens;   // tokens of a launch: fewer than 2^32 threads
     for (uint64_t first = 0; first < P.tokens; first += most) {
-        P.first_token = (uint32_t)first, P.total = (P.tokens - first < most ? P.tokens - first : most) * each;
-        const unsigned blocks = (unsigned)ceil_div(P.total, 256);
+        P.first_token = (uint32_t)first;
+        const uint64_t tokens = P.tokens - first < most ? P.tokens - first : most;
+        const unsigned blocks = (unsigned)ceil_div(tokens, 4 * kReadTokens);
         if (type == MMV_TYPE_F16) int8 ? block_read_kernel<f16_t, true><<<blocks, 256, 0, s>>>(P) : block_read_kernel<f16_t, false><<<blocks, 256, 0, s>>>(P);
         else int8 ? block_read_kernel<bf16_t, true><<<blocks, 256, 0, s>>>(P) : block_read_kernel<bf16_t, false><<<blocks, 256, 0, s>>>(P);
         if (const mmv_status st = launched()) return st;

@@ -135,8 +135,6 @@ struct Place {
     uint32_t row, head, tile, first, last;   // the segment's tiles: first .. last - 1
     uint32_t begin, end;                     // its positions
 };
-// Uniform loads through the scalar cache: they are not waited for along with the loads of keys and values.
-__device__ __forceinline__ int32_t scalar_load(const int32_t *p) { return *(const __attribute__((address_space(4))) int32_t *)(uintptr_t)p; }
 __device__ __forceinline__ void enter_row(const AttentionParams &P, Place &at, int32_t context) {
     const RowTiles t = row_tiles(P, context);
     at.first = t.first, at.last = t.first + t.count, at.begin = t.begin, at.end = t.end;
