@@ -182,15 +182,14 @@ template <int kHeld, typename T, bool kInt8> __global__ __launch_bounds__(256) v
 
 // ---- reading -------------------------------------------------------------------------------------------------------
 //
-// A wave brings four neighbouring tokens, eight values of a key and of a value a lane at a time: which request a token is of, its page and slot are the same for all lanes and
-// come through the scalar cache; the loads of all four are under way together.
-constexpr uint32_t kReadTokens = 4;
+// A lane brings eight values of a key and of a value of one token at a time; a token has as many neighbouring lanes as it has such pieces (a power of two, at most the wave), so that tokens of
+// few heads share a wave.  The wave finds the request of its first token among 64 at a time, a lane goes on from there.  What is written is not read again soon: it goes past the caches.
 struct BlockReadParams {
     BlockCacheParams c;
     const int32_t *offsets, *first, *table;
     uint64_t table_stride;
     uint32_t n, tokens, table_width, first_token;      // first_token: of a launch
-    uint32_t token_pieces;                             // heads * dim / 8
+    uint32_t token_pieces, lanes;                      // heads * dim / 8; lanes of a token: 2^lanes
     Divider page;                                      // slots of a page
     void *k, *v;
     uint64_t k_stride, v_stride;
@@ -198,7 +197,7 @@ struct BlockReadParams {
 
 template <typename T, bool kInt8> __global__ __launch_bounds__(256) void block_read_kernel(BlockReadParams P) {
     const BlockCacheParams &C = P.c;
-    const uint32_t lane = threadIdx.x & 63, t0 = P.first_token + uniform(blockIdx.x * 4 + (threadIdx.x >> 6)) * kReadTokens;
+    const uint32_t lane = threadIdx.x & 63, t0 = P.first_token + (uniform(blockIdx.x * 4 + (threadIdx.x >> 6)) << (6 - P.lanes)), t = t0 + (lane >> P.lanes);
     if (t0 >= P.tokens) return;
     // the last request that begins at t0 or before it: 64 at a time, then the beginnings from it on, one a lane
     uint32_t from = 0;
@@ -209,65 +208,37 @@ template <typename T, bool kInt8> __global__ __launch_bounds__(256) void block_r
         from += last * step, size = min(step, size - last * step);
     }
     const int32_t begins = from + lane <= P.n ? P.offsets[from + lane] : 0x7fffffff;   // (behind the last one: where that ends)
-    bool mine[kReadTokens], there[kReadTokens];   // somebody's, and in the cache
-    uint32_t request[kReadTokens];
-    int64_t position[kReadTokens];
-#pragma unroll
-    for (uint32_t i = 0; i < kReadTokens; ++i) {
-        const int32_t t = (int32_t)(t0 + i);
-        const uint64_t not_behind = __ballot(from + lane < P.n && begins <= t);
-        const uint32_t l = not_behind == ~0ull ? 63u : max(1u, (uint32_t)__builtin_ctzll(~not_behind)) - 1;
-        uint32_t r = from + l;
-        int32_t begin = (int32_t)lane_value((uint32_t)begins, l), end = (int32_t)lane_value((uint32_t)begins, l < 63 ? l + 1 : 63);
-        if (l == 63) {   // (64 requests that begin within four tokens)
-            while (r + 1 < P.n && scalar_load(P.offsets + r + 1) <= t) ++r;
-            begin = scalar_load(P.offsets + r), end = scalar_load(P.offsets + r + 1);
-        }
-        request[i] = r, mine[i] = t >= begin && t < end && (uint32_t)t < P.tokens, position[i] = (int64_t)t - begin;
-    }
-    if (P.first)
-#pragma unroll
-        for (uint32_t i = 0; i < kReadTokens; ++i) position[i] += scalar_load(P.first + request[i]);
-    uint64_t codes_at[kReadTokens], scales_at[kReadTokens];
-    uint32_t page[kReadTokens];
-#pragma unroll
-    for (uint32_t i = 0; i < kReadTokens; ++i) {
-        const uint32_t where = position[i] >= 0 && position[i] <= 0x7fffffff ? P.page.quotient((uint32_t)position[i]) : ~0u;
-        there[i] = mine[i] && where < P.table_width;
-        page[i] = ~0u;
-        if (P.table_width) page[i] = (uint32_t)scalar_load(P.table + (uint64_t)request[i] * P.table_stride + (there[i] ? where : 0u));
-    }
-#pragma unroll
-    for (uint32_t i = 0; i < kReadTokens; ++i) {
-        there[i] = there[i] && page[i] < C.pages;
-        const uint32_t p = there[i] ? page[i] : 0u, at = there[i] ? (uint32_t)position[i] : 0u, slot = at - P.page.quotient(at) * P.page.divisor;
-        codes_at[i] = (uint64_t)p * C.page_stride + (uint64_t)slot * C.slot_stride;
-        scales_at[i] = (uint64_t)p * C.heads * C.page_blocks + C.slots.quotient(slot);
-    }
-    for (uint32_t inside = lane; inside < P.token_pieces; inside += 64) {
+    const uint64_t not_behind = __ballot(from + lane < P.n && begins <= (int32_t)t0);
+    const uint32_t l = not_behind == ~0ull ? 63u : max(1u, (uint32_t)__builtin_ctzll(~not_behind)) - 1;
+    uint32_t r = from + l;
+    int32_t begin = (int32_t)lane_value((uint32_t)begins, l), end = l < 63 ? (int32_t)lane_value((uint32_t)begins, l + 1) : P.offsets[r + 1];
+    while (end <= (int32_t)t && r + 1 < P.n) begin = end, ++r, end = P.offsets[r + 1];
+    if ((int32_t)t < begin || (int32_t)t >= end || t >= P.tokens) return;   // (nobody's)
+    const int64_t position = (int64_t)t - begin + (P.first ? P.first[r] : 0);
+    const uint32_t where = position >= 0 && position <= 0x7fffffff ? P.page.quotient((uint32_t)position) : ~0u;
+    uint32_t page = ~0u;
+    if (where < P.table_width) page = (uint32_t)P.table[(uint64_t)r * P.table_stride + where];
+    const bool there = page < C.pages;
+    const uint32_t slot = there ? (uint32_t)position - where * P.page.divisor : 0u;
+    const uint64_t codes_at = (uint64_t)page * C.page_stride + (uint64_t)slot * C.slot_stride, scales_at = (uint64_t)page * C.heads * C.page_blocks + C.slots.quotient(slot);
+    for (uint32_t inside = lane & ((1u << P.lanes) - 1); inside < P.token_pieces; inside += 1u << P.lanes) {
         const uint32_t h = C.pieces.quotient(inside), piece = inside - h * C.pieces.divisor;
-        uint2 codes[kReadTokens][2];
-        float by[kReadTokens][2];
-#pragma unroll
-        for (uint32_t i = 0; i < kReadTokens; ++i) {
-            codes[i][0] = codes[i][1] = make_uint2(0, 0), by[i][0] = by[i][1] = 0.f;
-            if (there[i]) {
-                const uint64_t at = codes_at[i] + (uint64_t)h * C.head_stride + 8 * piece, scale = scales_at[i] + (uint64_t)h * C.page_blocks;
-                codes[i][0] = *(const uint2 *)((const uint8_t *)C.k + at), codes[i][1] = *(const uint2 *)((const uint8_t *)C.v + at);
-                by[i][0] = C.k_scales[scale], by[i][1] = C.v_scales[scale];
-            }
+        uint2 codes[2] = {make_uint2(0, 0), make_uint2(0, 0)};
+        float by[2] = {0.f, 0.f};
+        if (there) {
+            const uint64_t at = codes_at + (uint64_t)h * C.head_stride + 8 * piece, scale = scales_at + (uint64_t)h * C.page_blocks;
+            codes[0] = *(const uint2 *)((const uint8_t *)C.k + at), codes[1] = *(const uint2 *)((const uint8_t *)C.v + at);
+            by[0] = C.k_scales[scale], by[1] = C.v_scales[scale];
         }
 #pragma unroll
-        for (uint32_t i = 0; i < kReadTokens; ++i)
-            if (mine[i])
+        for (int x = 0; x < 2; ++x) {
+            float y[8];
+            to_floats<kInt8>(codes[x], y);
 #pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    float y[8];
-                    to_floats<kInt8>(codes[i][x], y);
-                    const float b = by[i][x];
-                    T *const to = (T *)(x ? P.v : P.k) + (t0 + i) * (x ? P.v_stride : P.k_stride) + 8 * inside;
-                    *(uint4 *)to = make_uint4(pack2<T>(y[0] * b, y[1] * b), pack2<T>(y[2] * b, y[3] * b), pack2<T>(y[4] * b, y[5] * b), pack2<T>(y[6] * b, y[7] * b));
-                }
+            for (int i = 0; i < 8; ++i) y[i] *= by[x];
+            const u32x4 w = {pack2<T>(y[0], y[1]), pack2<T>(y[2], y[3]), pack2<T>(y[4], y[5]), pack2<T>(y[6], y[7])};
+            __builtin_nontemporal_store(w, (u32x4 *)((T *)(x ? P.v : P.k) + t * (x ? P.v_stride : P.k_stride) + 8 * inside));
+        }
     }
 }
 

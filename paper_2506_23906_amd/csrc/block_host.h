@@ -50,11 +50,12 @@ mmv_status block_append_call(BlockAppendParams P, int type, bool int8, hipStream
     return MMV_OK;
 }
 mmv_status block_read_call(BlockReadParams P, int type, bool int8, hipStream_t s) {
-    const uint64_t most = (1ull << 26) * kReadTokens - 4 * kReadTokens;   // tokens of a launch: fewer than 2^32 threads
+    while (P.lanes < 6 && 1u << P.lanes < P.token_pieces) ++P.lanes;
+    const uint64_t each = 4u << (6 - P.lanes), most = ((1ull << 24) - 1) * each;   // tokens of a workgroup; of a launch: fewer than 2^32 threads
     for (uint64_t first = 0; first < P.tokens; first += most) {
         P.first_token = (uint32_t)first;
         const uint64_t tokens = P.tokens - first < most ? P.tokens - first : most;
-        const unsigned blocks = (unsigned)ceil_div(tokens, 4 * kReadTokens);
+        const unsigned blocks = (unsigned)ceil_div(tokens, each);
         if (type == MMV_TYPE_F16) int8 ? block_read_kernel<f16_t, true><<<blocks, 256, 0, s>>>(P) : block_read_kernel<f16_t, false><<<blocks, 256, 0, s>>>(P);
         else int8 ? block_read_kernel<bf16_t, true><<<blocks, 256, 0, s>>>(P) : block_read_kernel<bf16_t, false><<<blocks, 256, 0, s>>>(P);
         if (const mmv_status st = launched()) return st;
