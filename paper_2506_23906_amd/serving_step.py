@@ -1,7 +1,7 @@
 """A serving step that runs the calls for ragged batches together, as a small model with random weights.
 
-The model has layers of two kinds, by turns: attention over a paged cache, and linear attention with a decay for each head.  A batch of
-prompts goes in as one packed token vector, whose segments are the requests; after that every step adds one token to each request.
+The model has layers of two kinds, by turns: attention over a paged cache (16-bit, 8-bit with one scale, or 8-bit with a scale for each block of slots and head), and a recurrence, which is
+linear attention with a decay for each head or the gated delta rule.  A batch of prompts goes in as one packed token vector, whose segments are the requests; after that every step adds one token to each request.
 
     python -m paper_2506_23906_amd.serving_step --requests 16 --prompt 300 --steps 64
 
@@ -25,8 +25,10 @@ class Shape(NamedTuple):
     dim: int = 64
     vocabulary: int = 1000
     page: int = 16
-    cache: torch.dtype = torch.bfloat16   # or float8_e4m3fn
-    scale: float = 0.05      # of an 8-bit cache's keys and values
+    cache: torch.dtype = torch.bfloat16   # or float8_e4m3fn; in blocks int8 or float8_e4m3fn
+    scale: float = 0.05      # of an 8-bit cache's keys and values, where it has one for all
+    block: int = 0           # slots of a page that share a scale (a multiple of 8): an 8-bit cache in blocks
+    recurrence: str = "decay"   # or "delta"
 
     @property
     def kv_heads(self) -> int:
@@ -50,12 +52,26 @@ def weights(shape: Shape, seed: int = 0, device="cuda") -> dict:
         w["in"].append(normal(shape.width, (shape.heads + 2 * kv) * shape.dim, by=shape.width ** -0.5))
         w["out"].append(normal(shape.width, shape.width, by=0.5 * shape.width ** -0.5))
     w["decay"] = torch.tensor([-(2.0 ** (-8.0 * (h + 1) / shape.heads)) for h in range(shape.heads)], device=device)
+    if shape.recurrence == "delta":   # every token's decay and how much of its value is written, for each head
+        w["gates"] = [normal(shape.width, 2 * shape.heads, by=shape.width ** -0.5) if i % 2 else None for i in range(shape.layers)]
     return w
 
 
 def normalised(x: torch.Tensor) -> torch.Tensor:
     x = x.float()
     return (x * torch.rsqrt(x.square().mean(-1, keepdim=True) + 1e-6)).to(torch.bfloat16)
+
+
+def unit(x: torch.Tensor) -> torch.Tensor:
+    """Vectors of length 1 (the delta rule's keys and queries)."""
+    y = x.float()
+    return (y * torch.rsqrt(y.square().sum(-1, keepdim=True) + 1e-6)).to(x.dtype)
+
+
+def gates(x: torch.Tensor, w: torch.Tensor, heads: int):
+    """log_decay and beta of the delta rule, [tokens, heads] each, of normalised hidden states."""
+    log_decay, beta = (x @ w).float().split(heads, dim=1)
+    return -0.1 * torch.nn.functional.softplus(log_decay), torch.sigmoid(beta)
 
 
 def split(fused: torch.Tensor, shape: Shape, kv: int):
@@ -76,6 +92,9 @@ class Server:
 
         def cache():
             size = (pages, shape.kv_heads, shape.page, shape.dim)
+            if shape.block:
+                scales = (torch.zeros(pages, shape.kv_heads, shape.page // shape.block, device=device) for _ in "kv")
+                return B.BlockCache(*(torch.zeros(size, dtype=torch.uint8, device=device).view(shape.cache) for _ in "kv"), *scales)
             return B.PagedCache(*(torch.zeros(size, dtype=torch.uint8 if shape.cache.itemsize == 1 else shape.cache, device=device).view(shape.cache) for _ in "kv"), scale, scale)
 
         self.caches = [cache() if i % 2 == 0 else None for i in range(shape.layers)]
@@ -116,13 +135,17 @@ class Server:
 
     def _layers(self, use, tokens, tables, table, context, recurrence):
         shape, x = self.shape, self.w["embedding"][tokens]
+        append, attention = (B.mmv_block_append, B.mmv_block_attention) if shape.block else (B.mmv_cache_append, B.mmv_paged_attention)
         for i in range(shape.layers):
             kv = shape.kv_heads if i % 2 == 0 else shape.heads
-            q, k, v = split(normalised(x) @ self.w["in"][i], shape, kv)
+            y = normalised(x)
+            q, k, v = split(y @ self.w["in"][i], shape, kv)
             if i % 2 == 0:
-                B.mmv_cache_append(k, v, tables.slots, self.caches[i])
+                append(k, v, tables.slots, self.caches[i])
                 nbytes = B.mmv_paged_attention_workspace_bytes(q.shape[0], shape.heads, kv, shape.dim, self.columns * shape.page)
-                o = B.mmv_paged_attention(q, self.caches[i], table, context, ws=self._workspace("attention of " + use, nbytes))
+                o = attention(q, self.caches[i], table, context, ws=self._workspace("attention of " + use, nbytes))
+            elif shape.recurrence == "delta":
+                o = recurrence(unit(q), unit(k), v, self.states[i], *gates(y, self.w["gates"][i], shape.heads))
             else:
                 o = recurrence(q, k, v, self.states[i])
             x = x + o.flatten(1) @ self.w["out"][i]
@@ -137,7 +160,10 @@ class Server:
         tables = self._tables(lengths, count)
         request = torch.searchsorted(tables.offsets[1:].contiguous(), torch.arange(count, dtype=torch.int32, device=self.device), right=True)
 
-        def recurrence(q, k, v, state):
+        def recurrence(q, k, v, state, *gates):
+            if gates:
+                ws = self._workspace("recurrence of prompts", B.mmv_delta_attention_workspace_bytes(self.n, count, shape.heads, shape.dim, shape.dim))
+                return B.mmv_delta_attention(q, k, v, tables.offsets, *gates, state_in=state, state_out=state, ws=ws)
             ws = self._workspace("recurrence of prompts", B.mmv_decay_attention_workspace_bytes(self.n, count, shape.heads, shape.dim, shape.dim))
             return B.mmv_decay_attention(q, k, v, tables.offsets, self.w["decay"], state_in=state, state_out=state, ws=ws)
 
@@ -149,8 +175,11 @@ class Server:
     def step(self) -> torch.Tensor:
         """One more token for every request; returns the hidden states, and leaves the next tokens in `next`."""
         tables = self._tables(self.one_each, self.n)
-        x = self._layers("a step", self.next, tables, self.table, tables.context,
-                         lambda q, k, v, state: B.mmv_decay_step(q, k, v, self.w["decay"], state, state))
+
+        def recurrence(q, k, v, state, *gates):
+            return B.mmv_delta_step(q, k, v, *gates, state, state) if gates else B.mmv_decay_step(q, k, v, self.w["decay"], state, state)
+
+        x = self._layers("a step", self.next, tables, self.table, tables.context, recurrence)
         self.next.copy_((x @ self.w["embedding"].T).argmax(-1))
         self._took(tables)
         return x
@@ -171,9 +200,10 @@ def main() -> None:
     ap.add_argument("--requests", type=int, default=16)
     ap.add_argument("--prompt", type=int, default=300, help="longest prompt; lengths are spread from a tenth of it")
     ap.add_argument("--steps", type=int, default=64)
-    ap.add_argument("--cache", choices=["bf16", "e4m3"], default="bf16")
+    ap.add_argument("--cache", choices=["bf16", "e4m3", "e4m3-blocks", "int8-blocks"], default="bf16")
+    ap.add_argument("--recurrence", choices=["decay", "delta"], default="decay")
     a = ap.parse_args()
-    shape = Shape(cache={"bf16": torch.bfloat16, "e4m3": torch.float8_e4m3fn}[a.cache])
+    shape = Shape(cache={"bf16": torch.bfloat16, "e4m3": torch.float8_e4m3fn, "int8": torch.int8}[a.cache.split("-")[0]], block=16 if a.cache.endswith("blocks") else 0, recurrence=a.recurrence)
     lengths = [max(1, round(a.prompt * 10 ** (i / max(1, a.requests - 1) - 1))) for i in range(a.requests)]
     server = Server(shape, weights(shape), a.requests, max(lengths) + 2 * a.steps + 3)
     tokens = torch.randint(shape.vocabulary, (sum(lengths),), generator=torch.Generator().manual_seed(3)).cuda()
