@@ -29,22 +29,20 @@ mmv_status delta_params(DeltaParams &P, uint64_t n, uint64_t tokens, uint32_t he
     return MMV_OK;
 }
 
-// Columns of a workgroup: equal shares of at most 128, in eights; threads of the same columns: as many as there is room for, a power of two.
-template <typename T> mmv_status launch_tokens(DeltaParams P, hipStream_t s) {
-    const uint32_t slices = (P.dv + 127) / 128, slice = (uint32_t)ceil_div(P.dv, 8 * slices) * 8;
-    uint32_t step = 64;
-    while (step * (slice / 4) > 256) step /= 2;
-    const uint32_t rows = (uint32_t)ceil_div(P.dk, step), each = P.heads * slices, most = most_of_a_launch(256, each);   // rows: of a thread
+// Rows that the threads of a workgroup have at once (16 at most: their sums are joined one by one), and of a thread.
+template <typename T, int kThreads> mmv_status launch_step(DeltaParams P, hipStream_t s) {
+    const uint32_t fit = kThreads / (P.dv / 4), step = fit < 16 ? fit : 16, rows = (uint32_t)ceil_div(P.dk, step), most = most_of_a_launch(kThreads, P.heads);
     for (; P.first < P.n; P.first += most) {
-        const uint32_t blocks = (P.n - P.first < most ? P.n - P.first : most) * each;
-        if (rows <= 4) delta_tokens_kernel<T, 4><<<blocks, 256, 0, s>>>(P, slices, slice, step);
-        else if (rows <= 8) delta_tokens_kernel<T, 8><<<blocks, 256, 0, s>>>(P, slices, slice, step);
-        else delta_tokens_kernel<T, 16><<<blocks, 256, 0, s>>>(P, slices, slice, step);
+        const uint32_t blocks = (P.n - P.first < most ? P.n - P.first : most) * P.heads;
+        if (rows <= 4) delta_step_kernel<T, 4, kThreads><<<blocks, kThreads, 0, s>>>(P, step);
+        else if (rows <= 8) delta_step_kernel<T, 8, kThreads><<<blocks, kThreads, 0, s>>>(P, step);
+        else delta_step_kernel<T, 16, kThreads><<<blocks, kThreads, 0, s>>>(P, step);
         if (const mmv_status st = launched()) return st;
     }
     return MMV_OK;
 }
-mmv_status delta_step_call(const DeltaParams &P, int type, hipStream_t s) { return type == MMV_TYPE_F16 ? launch_tokens<f16_t>(P, s) : launch_tokens<bf16_t>(P, s); }
+template <typename T> mmv_status launch_steps(const DeltaParams &P, hipStream_t s) { return step_threads(P.dv) == 512 ? launch_step<T, 512>(P, s) : launch_step<T, 256>(P, s); }
+mmv_status delta_step_call(const DeltaParams &P, int type, hipStream_t s) { return type == MMV_TYPE_F16 ? launch_steps<f16_t>(P, s) : launch_steps<bf16_t>(P, s); }
 
 // Chunks that the requests can have together, and blocks of a head that the device has at once (two workgroups on a compute unit).
 inline uint64_t delta_chunks(uint64_t n, uint64_t tokens) { return tokens / kChunk + (n < tokens ? n : tokens); }

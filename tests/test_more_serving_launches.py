@@ -51,7 +51,7 @@ def record(tmp_path_factory, libmmvseg_path):
     return run
 
 
-APPEND, READ, CHUNKS, PROMPT, STATES, TOKENS = "block_append_kernel", "block_read_kernel", "delta_chunks_kernel", "delta_prompt_kernel", "delta_states_kernel", "delta_tokens_kernel"
+APPEND, READ, CHUNKS, PROMPT, STATES, X, "block_read_kernel", "delta_chunks_kernel", "delta_prompt_kernel", "delta_states_kernel", "delta_step_kernel"
 WHOLE, LIST, JOIN = "whole_attention_kernel", "paged_attention_kernel", "join_attention_kernel"
 
 
@@ -69,7 +69,7 @@ WHOLE, LIST, JOIN = "whole_attention_kernel", "paged_attention_kernel", "join_at
     ("delta(700, 9000, dk=128, dv=256, type=1)", [(CHUNKS, 6720, 256), (PROMPT, 1024, 256), (STATES, 1024, 256), (PROMPT, 22400, 256)]),
     ("delta(3, 9000, heads=64, dk=96, dv=128)", [(CHUNKS, 9152, 256), (PROMPT, 1024, 256), (STATES, 1024, 192), (PROMPT, 1024, 256)]),
     ("delta(3, 9000, heads=128, dk=96, dv=128)", [(CHUNKS, 18304, 256), (PROMPT, 768, 256)]),   # (two of a head at once: nothing to gain)
-    ("step(5)", [(TOKENS, 40, 256)]), ("step(5, dv=256)", [(TOKENS, 80, 256)]),
+    ("step(5)", [(STEP, 40, 256)]), ("step(5, dv=256)", [(STEP, 40, 512)]),
 ])
 def test_launches(record, call, want):
     assert record(call) == want
