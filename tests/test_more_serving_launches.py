@@ -51,7 +51,7 @@ def record(tmp_path_factory, libmmvseg_path):
     return run
 
 
-APPEND, READ, CHUNKS, PROMPT, STATES, X, "block_read_kernel", "delta_chunks_kernel", "delta_prompt_kernel", "delta_states_kernel", "delta_step_kernel"
+APPEND, READ, CHUNKS, PROMPT, STATES, STEP = "block_append_kernel", "block_read_kernel", "delta_chunks_kernel", "delta_prompt_kernel", "delta_states_kernel", "delta_step_kernel"
 WHOLE, LIST, JOIN = "whole_attention_kernel", "paged_attention_kernel", "join_attention_kernel"
 
 
