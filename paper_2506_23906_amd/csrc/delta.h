@@ -266,9 +266,11 @@ __device__ __forceinline__ f32x4 mfma_f32(float a, float b, f32x4 c) { return __
 // I + L, a column a lane, by substitution (which loses nothing where keys are alike, as powers of L would); then wave j the blocks below the diagonal of block column j, and those of M,
 //   T_ij = -T_ii sum_(j <= m < i) L_im T_mj,   M_ij = sum_(j <= m <= i) W_im T_mj
 // in fp32 products (16x16x4): the column of a step of the operand is 4 g + step, so that a result's registers are the next product's operand.
-template <typename T> __global__ __launch_bounds__(256, 4) void delta_chunks_kernel(DeltaPromptParams PP) {
-    constexpr uint32_t kWide = kChunk + 4;
-    __shared__ __align__(16) float LW[kChunk][kWide], X[kChunk][kWide];   // below the diagonal L, from it on W transposed; T, later M
+template <typename T> __global__ __launch_bounds__(256, 5) void delta_chunks_kernel(DeltaPromptParams PP) {
+    constexpr uint32_t kWide = kChunk + 4, kHalf = kChunk / 2, kNarrow = kHalf + 4;
+    // below the diagonal L, from it on W transposed; T, later M, the first 32 rows without columns 32 .. 63: five workgroups on a compute unit.  Before T is there, keys lie in its place.
+    __shared__ __align__(16) float LW[kChunk][kWide], X_[kHalf * (kNarrow + kWide)];
+    const auto X = [&](uint32_t row) __attribute__((always_inline)) { return X_ + (row < kHalf ? row * kNarrow : kHalf * kNarrow + (row - kHalf) * kWide); };
     __shared__ double upto[kChunk];
     __shared__ float betas[kChunk], left[kChunk];
     const DeltaParams &P = PP.d;
@@ -285,7 +287,8 @@ template <typename T> __global__ __launch_bounds__(256, 4) void delta_chunks_ker
         return make_rsrc((const void *)uniform64((uint64_t)((const T *)base + (uint64_t)shared * P.dk + t0 * stride)), uniform((m - 1) * 2 * (uint32_t)stride + 2 * P.dk));
     };
     const auto k_rows = rows_of(P.k, P.k_stride), q_rows = rows_of(P.q, P.q_stride);
-    u32x4 own_k[4], own_q[4], k[4][4];
+    u32x4 own_k[4], own_q[4];
+    u32x4 *const keys = (u32x4 *)X_ + lane;   // of the first three tiles, [tile][p][lane]
     const auto load = [&](u32x4 (&x)[4], auto rows, uint32_t tile, uint64_t stride) __attribute__((always_inline)) {
 #pragma unroll
         for (int p = 0; p < 4; ++p) {
@@ -301,9 +304,9 @@ template <typename T> __global__ __launch_bounds__(256, 4) void delta_chunks_ker
     }
     load(own_k, k_rows, wave, P.k_stride);
     load(own_q, q_rows, wave, P.q_stride);
+    if (wave < 3)
 #pragma unroll
-    for (int tile = 0; tile < 4; ++tile)
-        if ((uint32_t)tile < wave) load(k[tile], k_rows, tile, P.k_stride);
+        for (int p = 0; p < 4; ++p) keys[(wave * 4 + p) * 64] = own_k[p];
     if (wave == 0) {
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1) {
@@ -322,7 +325,8 @@ template <typename T> __global__ __launch_bounds__(256, 4) void delta_chunks_ker
             f32x4 a = {0.f, 0.f, 0.f, 0.f}, b = a;
 #pragma unroll
             for (int p = 0; p < 4; ++p) {
-                const u32x4 x = (uint32_t)tile == wave ? own_k[p] : k[tile][p];
+                u32x4 x = own_k[p];
+                if ((uint32_t)tile < wave) x = keys[(tile * 4 + p) * 64];
                 a = mfma_16x16x32(T(), own_k[p], x, a), b = mfma_16x16x32(T(), own_q[p], x, b);
             }
             const uint32_t j = tile * 16 + r;
@@ -346,11 +350,11 @@ template <typename T> __global__ __launch_bounds__(256, 4) void delta_chunks_ker
 #pragma unroll
             for (int c = 0; c < i; ++c) x = __builtin_fmaf(-block[i][c], column[c], x);
             column[i] = x;
-            X[16 * g + i][16 * g + r] = x;
+            X(16 * g + i)[16 * g + r] = x;
         }
     } else if (wave == 3) {   // (what operands have above the diagonal)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) X[4 * g + e][16 + r] = 0.f, X[32 + 4 * g + e][48 + r] = 0.f;
+        for (int e = 0; e < 4; ++e) X(4 * g + e)[16 + r] = 0.f, X(32 + 4 * g + e)[48 + r] = 0.f;
     }
     __syncthreads();
     f32x4 T_[4], M[4];   // blocks (i, wave); before a block of T is there, the sum that it is made of.  (products of as many blocks as there are, in turn: none waits for the one before)
@@ -361,15 +365,15 @@ template <typename T> __global__ __launch_bounds__(256, 4) void delta_chunks_ker
         if ((uint32_t)c >= wave) {
             if ((uint32_t)c == wave) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) T_[c][e] = X[c * 16 + 4 * g + e][c * 16 + r];
+                for (int e = 0; e < 4; ++e) T_[c][e] = X(c * 16 + 4 * g + e)[c * 16 + r];
             } else {
-                const f32x4 d = *(const f32x4 *)&X[c * 16 + r][c * 16 + 4 * g];
+                const f32x4 d = *(const f32x4 *)&X(c * 16 + r)[c * 16 + 4 * g];
                 f32x4 y = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int e = 0; e < 4; ++e) y = mfma_f32(d[e], -T_[c][e], y);
                 T_[c] = y;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) X[c * 16 + 4 * g + e][wave * 16 + r] = y[e];
+                for (int e = 0; e < 4; ++e) X(c * 16 + 4 * g + e)[wave * 16 + r] = y[e];
             }
             f32x4 l[4], w[4];
 #pragma unroll
@@ -394,7 +398,7 @@ template <typename T> __global__ __launch_bounds__(256, 4) void delta_chunks_ker
         constexpr int kTerms = decltype(terms_of)::value;
         for (uint32_t f = wave; f < kOperands; f += 4) {
             const uint32_t row = (f >= 2 ? 32 : 0) + 8 * (r >> 2) + 4 * (f & 1) + (r & 3), column = (f >= 4 ? 32 : 0) + 8 * g;
-            const float *const x = &X[row][column], *const by = &betas[column], row_by = rows_by(row);
+            const float *const x = X(row) + column, *const by = &betas[column], row_by = rows_by(row);
             u32x4 out[kTerms];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -413,7 +417,7 @@ template <typename T> __global__ __launch_bounds__(256, 4) void delta_chunks_ker
     for (int i = 0; i < 4; ++i)
         if ((uint32_t)i >= wave) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) X[i * 16 + 4 * g + e][wave * 16 + r] = M[i][e];
+            for (int e = 0; e < 4; ++e) X(i * 16 + 4 * g + e)[wave * 16 + r] = M[i][e];
         }
     __syncthreads();
     write_operands(Number<kTermsM>(), kOperands * kTermsE, [](uint32_t) __attribute__((always_inline)) { return 1.f; });
