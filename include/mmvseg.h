@@ -463,8 +463,8 @@ typedef struct {
  * code * (scale before * (1 / scale)).  So a block is filled from its first slot on, as mmv_page_tables hands them out; what is in the slots of a block that begins anew is
  * left as it was and stands for nothing until it is written.  Scales of blocks that never began have to be numbers (zeros, say).
  * Infinities count as the largest finite value of `type`.  What is not a number stays so in MMV_TYPE_E4M3; MMV_TYPE_I8 has no code for it, and the block's scale becomes
- * not a number (what is written then has the code -127), until the block begins anew.  A slot outside the cache is skipped.  Tokens of one block have to be neighbours, in any order: of two runs of one block either may win, code by code and
- * scale, and so of two tokens with one slot.  tokens < 2^26. */
+ * not a number (what is written then has the code -127), until the block begins anew.  A slot outside the cache is skipped.  Tokens of one block have to be neighbours, in any order: what a block with two runs, or the slot of two tokens,
+ * holds afterwards is not defined (no other block changes).  tokens < 2^26. */
 mmv_status mmv_block_append(uint64_t tokens, const void *d_k, uint64_t k_stride, const void *d_v, uint64_t v_stride, mmv_type type,
                             const int64_t *d_slots, const mmv_block_cache *cache, void *hip_stream);
 

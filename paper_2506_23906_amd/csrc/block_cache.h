@@ -184,6 +184,7 @@ template <int kHeld, typename T, bool kInt8> __global__ __launch_bounds__(256) v
 //
 // A lane brings eight values of a key and of a value of one token at a time; a token has as many neighbouring lanes as it has such pieces (a power of two, at most the wave), so that tokens of
 // few heads share a wave.  The wave finds the request of its first token among 64 at a time, a lane goes on from there.  What is written is not read again soon: it goes past the caches.
+// Bound by memory: 62000 tokens of 8 heads of 128 70.9 us (384 MB, 5.4 TB/s; a copy 6.5); 100 tokens, where the search and the table's entry wait for each other, 2.9 us.
 struct BlockReadParams {
     BlockCacheParams c;
     const int32_t *offsets, *first, *table;

@@ -50,7 +50,8 @@ __device__ __forceinline__ Span span_of(const DeltaParams &P, uint32_t r) {
 // Bound by reading and writing the state: 8 dk dv bytes for 6 dk dv operations.  A workgroup has one state; a thread takes four columns (16 bytes) of every `step`-th row, so that a pass of the
 // workgroup is one run of memory, and all its rows are loaded before the first is used and stay in registers.  k S' and q S' are added up in one pass and joined in LDS.  States are read and written
 // past the caches: no other call needs them before the next step.  (Rows in neighbouring lanes, whose sums need no LDS, read less than whole lines where dv is no multiple of 32: 200 requests of 16
-// heads of 64 x 160 118 us, so 60.)  128 requests of 32 heads, 128 x 128: 103 us, 5.2 TB/s.
+// heads of 64 x 160 118 us, so 60.)  128 requests of 32 heads, 128 x 128: 103 us, 5.2 TB/s; 4 of 8 heads of 64 x 64, all of it waiting for memory once, 4.8.
+// 512 threads where 256 would have more than sixteen rows of four columns each (128 registers for the state).
 constexpr uint32_t step_threads(uint32_t dv) { return dv > 128 ? 512 : 256; }
 template <typename T, int kRows, int kThreads> __global__ __launch_bounds__(kThreads, kRows > 8 ? 4 : 6) void delta_step_kernel(DeltaParams P, uint32_t step) {
     __shared__ float query[kMostDk], key[kMostDk], qk[16];
@@ -178,8 +179,12 @@ __device__ __forceinline__ ChunkPlace find_chunk(const DeltaParams &P, uint32_t 
 
 // Requests in blocks.  Chunks of a request depend on each other through the state.  Where few long requests would leave the device idle they are taken apart into blocks of as many chunks: what a
 // block makes of a state, S -> A S + B, is found for all blocks at once (A from the columns of the identity, B from a state of zeros), then the state before each block, then all blocks' outputs.
-// That is 2.3 times the work, so it is done where the longest request has over kApart times an even share of the chunks.
-constexpr uint32_t kApart = 3, kLeastBlock = 4, kLeastApart = 16;
+// That is 2.3 times the work and two more launches, so it is done where the longest request has more than 13 / 4 of an even share of the chunks and ten more, 16 at least (a call that cannot have so many is not charged with the two launches): us of a call, whole / in blocks, where
+// the longest of the requests has as many chunks and as many times an even share (16 heads of 128 x 128; 8 of 64 x 64 and 4 of 128 x 256 change sides at the same places):
+//   16 chunks, 6 times 99 / 105, 12 times 95 / 85;   32, 4 times 193 / 205, 6 times 183 / 170;   64, 3 times 453 / 525, 4 times 391 / 348;   128, 3 times 874 / 947, 4 times 769 / 638
+// Blocks have four chunks at least: 16 chunks, 12 times: 2 93, 4 85, 8 97 us; and as many as fill the device once: filled 3, 2, 1 times, one of 32768 tokens 843, 773, 709 us.
+constexpr uint32_t kLeastBlock = 4, kLeastApart = 16, kApartFixed = 10, kApartQuarters = 13;
+__host__ __device__ constexpr bool worth_taking_apart(uint64_t most, uint64_t all, uint32_t round) { return most >= kLeastApart && 4 * (most - kApartFixed) * round > kApartQuarters * all; }
 struct BlockPlan {
     uint32_t chunks, blocks;   // chunks of a block (~0: all of a request), blocks in all
 };
@@ -197,7 +202,7 @@ __device__ __forceinline__ BlockPlan plan_blocks(const DeltaPromptParams &PP) {
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) most = max(most, (uint32_t)__shfl_xor((int)most, d));
     most = uniform(most);
-    if (most < kLeastApart || (uint64_t)most * PP.round <= (uint64_t)kApart * all) return {~0u, P.n};
+    if (!worth_taking_apart(most, all, PP.round)) return {~0u, P.n};
     const uint32_t block = max(kLeastBlock, (all + PP.round - 1) / PP.round);
     uint32_t blocks = 0;
     for (uint32_t r = lane; r < P.n; r += 64) blocks += blocks_in(chunks_of(span_of(P, r)), block);
@@ -228,7 +233,7 @@ __device__ __forceinline__ BlockPlace find_block(const DeltaPromptParams &PP, ui
             at.request = first + l, at.blocks = lane_value(own, l), at.block = number - (before + lane_value(upto, l) - at.blocks);
             const uint32_t first_slot = slots_before + wave_sum32((int)lane < l ? slots : 0u);
             at.slot = first_slot + at.block, at.chunk = chunks_before + wave_sum32((int)lane < l ? chunks : 0u) + (at.block ? at.block * block : 0u);
-            at.found = at.blocks == 1 || first_slot + at.blocks <= PP.slots;   // (there is room for all of them, unless offsets go backwards)
+            at.found = at.blocks == 1 || (first_slot <= PP.slots && at.blocks <= PP.slots - first_slot);   // (there is room for all of them, unless offsets go backwards)
             return at;
         }
         before += lane_value(upto, 63), chunks_before += wave_sum32(chunks), slots_before += wave_sum32(slots);
@@ -266,6 +271,9 @@ __device__ __forceinline__ f32x4 mfma_f32(float a, float b, f32x4 c) { return __
 // I + L, a column a lane, by substitution (which loses nothing where keys are alike, as powers of L would); then wave j the blocks below the diagonal of block column j, and those of M,
 //   T_ij = -T_ii sum_(j <= m < i) L_im T_mj,   M_ij = sum_(j <= m <= i) W_im T_mj
 // in fp32 products (16x16x4): the column of a step of the operand is 4 g + step, so that a result's registers are the next product's operand.
+// fp32, not bf16 terms: with keys alike and beta 2, T's entries cancel in sums of 64.  Bound by the phases of a workgroup, which wait for each other (32 KB written for 16 KB of keys and queries
+// read, 2.3 TB/s): 24 prompts of 24000 tokens in all, 16 heads, 90 us; one of 45000, 171 us.  Five workgroups on a compute unit, for which keys go through T's place in LDS and T's empty quarter
+// is left out, for four 96 and 185 us.
 template <typename T> __global__ __launch_bounds__(256, 5) void delta_chunks_kernel(DeltaPromptParams PP) {
     constexpr uint32_t kWide = kChunk + 4, kHalf = kChunk / 2, kNarrow = kHalf + 4;
     // below the diagonal L, from it on W transposed; T, later M, the first 32 rows without columns 32 .. 63: five workgroups on a compute unit.  Before T is there, keys lie in its place.
@@ -437,7 +445,11 @@ __device__ __forceinline__ u32x4 own_column(const uint32_t (&row)[4], bool odd) 
 // Layout (products 16x16x32, lane = 16 g + r): the lane has column r and, of a pair of result tiles, the rows 32 s + 8 g + 0..7 (operand rows are those of kOperands' comment): as B
 // of the next product those are its own, so the state goes into K S and Q S, R into M R and E R, and that into K^T E R, each from the registers where it is.
 // What is no 16-bit input meets the matrix cores as bf16 terms, each the upper half of what the ones before left, the last one rounded: three (fp32's 24 bits) of E, the state, R and E R on
-// their way to a state, two of the state, M and R on their way to an output, which is rounded to 16 bits.  Inputs in fp16 are two terms each (exact).
+// their way to a state, two of the state, M and R on their way to an output, which is rounded to 16 bits: 2^-16 relative to the largest summand, beside bf16's 2^-8 and fp16's 2^-11 (rms errors of
+// fp16 outputs 2.082e-4, with a state in fp32 products 2.074e-4; of states 1.9e-7).  Inputs in fp16 are two terms each (exact).
+// Bound by matrix instructions and the waits between a chunk's three dependent products (24 prompts of 24000 tokens in all, 16 heads, 128 x 128, bf16: 386 us; a copy that only multiplies reaches
+// 906 TFLOP/s of terms, 74 % of what a large library product does).  Four waves, two workgroups on a compute unit: a workgroup of eight waves 448 us where four had 443, and one of 45000 tokens
+// in blocks 2197, so 1763; two groups of 16 columns to a wave, which halve the reads of LDS, need twice the registers and are slower.
 // kStates: what blocks make of a state (columns dv and on: of the identity), without outputs.
 constexpr int kDeltaWaves = 4;
 template <int KD, typename T, bool kStates> __global__ __launch_bounds__(64 * kDeltaWaves, !__is_same(T, f16_t) || KD == 2 ? 2 : 1) void delta_prompt_kernel(DeltaPromptParams PP, uint32_t slices) {
@@ -453,309 +465,309 @@ template <int KD, typename T, bool kStates> __global__ __launch_bounds__(64 * kD
     if (kStates && plan.chunks == ~0u) return;
     const uint32_t each = P.heads * slices;
     for (uint64_t item = blockIdx.x; item < (uint64_t)plan.blocks * each; item += gridDim.x) {
-    const uint32_t tid = here(threadIdx.x), lane = tid & 63, wave = uniform(tid >> 6), g = lane >> 4, r = lane & 15;
-    const uint32_t in_order_ = uniform((uint32_t)(item / each)), rest = uniform((uint32_t)(item - (uint64_t)in_order_ * each)), h = uniform(rest / slices), slice = uniform(rest - h * slices);
-    const uint32_t shared = uniform(h / P.group);
-    const BlockPlace at = find_block(PP, plan.chunks, in_order_);
-    const Span span = span_of(P, at.request);
-    const uint32_t block_tokens = plan.chunks == ~0u ? 0u : plan.chunks * kChunk;
-    const uint32_t begin = uniform(span.begin + at.block * block_tokens), end = uniform(at.block + 1 == at.blocks ? span.end : begin + block_tokens);
-    uint32_t number = uniform(at.chunk);
-    if (!at.found || (kStates && at.block + 1 == at.blocks)) continue;
-    if (begin < end && number + (end - begin + kChunk - 1) / kChunk > PP.most_chunks) continue;   // (offsets that go backwards)
-    const uint64_t state = state_of(P, at.request), state_at = (state * P.heads + h) * ((uint64_t)P.dk * P.dv);
-    float *const block_state = PP.block_states + ((uint64_t)at.slot * P.heads + h) * ((uint64_t)P.dk * (P.dv + P.dk));
-    const uint32_t column = (slice * NW + wave) * 16 + r, columns = kStates ? P.dv + P.dk : P.dv;
-    const bool live_column = column < columns, live_wave = (slice * NW + wave) * 16 < columns;   // (columns that are not there compute what nobody reads)
-    f32x4 S[2 * KD];
-    const float *const from = kStates ? nullptr : at.blocks > 1 ? block_state : P.state_in && state != ~0ull ? P.state_in + state_at : nullptr;
-    const uint32_t from_stride = at.blocks > 1 ? P.dv + P.dk : P.dv;
-#pragma unroll
-    for (int i = 0; i < 2 * KD; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const uint32_t d = (i / 2) * 32 + g * 8 + (i % 2) * 4 + e;
-            S[i][e] = kStates ? (column == P.dv + d ? 1.f : 0.f) : from && live_column && d < P.dk ? from[(uint64_t)d * from_stride + column] : 0.f;
-        }
-    constexpr uint32_t kNowhere = 1u << 31;
-    const uint32_t pieces = P.dk / 8;
-    const bool odd_lane = lane & 1;
-        const uint32_t column2 = (column & ~1u) < P.dv ? 2 * (column & ~1u) : kNowhere;   // of the lane's pair of columns, in bytes
-    u32x4 staged[kPer][4], matrices[kMatrixPer];
-    float decays = 0.f;
-    uint32_t values[2][4];
-    const auto chunk_rows = [&](const void *base, uint32_t m, uint32_t stride, uint32_t width) __attribute__((always_inline)) {
-        return make_rsrc((const void *)uniform64((uint64_t)base), uniform((m - 1) * stride + width));
-    };
-    const auto anew = [&](uint32_t v) __attribute__((always_inline)) { return KD > 2 ? here(v) : v; };   // (addresses that stay would fill the registers)
-    // A lane brings 4 tokens x 8 components of K or of Q into LDS; a wave has either.
-    struct Part {
-        bool live, is_q;
-        uint32_t row, piece;
-    };
-    const auto part_of = [&](int b) __attribute__((always_inline)) {
-        const uint32_t first = (kItemsK % (64 * NW) ? wave * 64 : 0u) + b * 64 * NW, rest = kItemsK % (64 * NW) ? 0u : wave * 64;   // (known when compiled where they divide)
-        Part p;
-        p.live = first < kItems, p.is_q = !kStates && first >= kItemsK;
-        const uint32_t id = first + rest - (p.is_q ? kItemsK : 0) + anew(lane);
-        p.piece = id % kPieces, p.row = id / kPieces * 4;
-        return p;
-    };
-    const auto load_chunk = [&](uint32_t t0, uint32_t chunk) __attribute__((always_inline)) {
-        const uint32_t m = min(kChunk, end - t0);
-#pragma unroll
-        for (int b = 0; b < kPer; ++b) {
-            const Part p = part_of(b);
-            if (p.live) {
-                const uint32_t stride = 2 * (uint32_t)(p.is_q ? P.q_stride : P.k_stride), off = p.row * stride + (p.piece < pieces ? p.piece * 16 : kNowhere);
-                const auto rows = chunk_rows(p.is_q ? (const T *)P.q + (uint64_t)shared * P.dk + t0 * P.q_stride : (const T *)P.k + (uint64_t)shared * P.dk + t0 * P.k_stride, m, stride, 2 * P.dk);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) staged[b][j] = __builtin_amdgcn_raw_buffer_load_b128(rows, off + j * stride, 0, 0);
-            }
-        }
-        const char *const made = PP.chunks + ((uint64_t)chunk * P.heads + h) * kChunkBytes;
-#pragma unroll
-        for (int b = 0; b < kMatrixPer; ++b)
-            if (b * 64 * NW + wave * 64 < kMatrix) matrices[b] = ((const u32x4 *)made)[b * 64 * NW + anew(tid)];
-        if (tid < 2 * kChunk) decays = ((const float *)(made + kMatrixPieces * 16))[tid];
-        const uint32_t stride = 2 * (uint32_t)P.v_stride, off = (anew(g) * 8 + (odd_lane ? 4 : 0)) * stride;
-        const auto rows = chunk_rows((const T *)P.v + (uint64_t)h * P.dv + t0 * P.v_stride, m, stride, 2 * P.dv);
-#pragma unroll
-            for (int s = 0; s < 2; ++s)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) values[s][j] = __builtin_amdgcn_raw_buffer_load_b32(rows, off + (s * 32 + j) * stride + column2, 0, 0);
-    };
-    // LDS rows are pieces of 16 bytes, exchanged by the row's number so that the sixteen rows of an operand, 8 (r / 4) + r % 4 + ..., lie in different banks.  K by component as in
-    // rows d: piece u, 8 tokens, at u ^ (2 (d / 8 mod 4) + (d / 2 mod 2)) ^ (d / 32 mod 2), its two halves exchanged where d / 64 is odd: the lanes of a read have d = 8 (r / 4) +
-    // r % 4 + ..., those of a write d / 8 from 0 to 15.
-    const auto row_piece = [&](uint32_t row, uint32_t u) __attribute__((always_inline)) {
-        return kRow == 128 ? row * 256 + ((u ^ (row & 3) ^ (row >> 3 & 3) * 4) * 16) : row * 128 + ((u ^ (row >> 1 & 1) ^ (row >> 3 & 3) * 2) * 16);
-    };
-    const uint32_t own_kt = ((r >> 2) * 8 + (r & 3)) * 128 + (g ^ (r >> 1)) * 16;
-    const auto kt_tile = [&](int a, int t, int s) __attribute__((always_inline)) {   // components of tile t, tokens 32 s + 8 g .. + 7
-        const u32x4 w = *(const u32x4 *)((const char *)lds_kt[a] + (own_kt ^ (s * 64) ^ (t / 2 % 2 * 16)) + (t / 2) * 32 * 128 + (t % 2) * 4 * 128);
-        return t / 4 % 2 ? (u32x4){w[2], w[3], w[0], w[1]} : w;
-    };
-    // Rows of tile (s, t) = (tile / 2, tile % 2), 32 s + 4 t behind the lane's own: pieces there are exchanged by the same bits.
-    const uint32_t own_rows = row_piece(8 * (r >> 2) + (r & 3), g);
-    const auto operand = [&](const uint16_t *plane, int tile, int p) __attribute__((always_inline)) {
-        return *(const u32x4 *)((const char *)plane + (own_rows ^ (p * 64)) + ((tile / 2) * 32 + (tile % 2) * 4) * 2 * kRow);
-    };
-    if (begin < end) load_chunk(begin, number);
-    // The first chunk's loads are waited for here: with any of them under way at the loop's head, the compiler's wait there would be for all that the wave has
-    // issued, the stores of the chunk before among them.
-    __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0)
-    for (uint32_t t0 = begin; t0 < end; t0 += kChunk, ++number) {
-        const uint32_t m = min(kChunk, end - t0);
-#pragma unroll
-        for (int b = 0; b < kPer; ++b) {
-            const Part p = part_of(b);
-            if (p.live) {
-#pragma unroll
-                for (int a = 0; a < kIn; ++a) {
-                    uint32_t w[4][4];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            uint32_t terms[kIn];
-                            input_terms<T, kIn>(staged[b][j][i], terms);
-                            w[j][i] = terms[a];
-                        }
-                    char *const to = p.is_q ? (char *)lds_q[a] : (char *)lds_k[a];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) *(u32x4 *)(to + row_piece(p.row + j, p.piece)) = (u32x4){w[j][0], w[j][1], w[j][2], w[j][3]};
-                    if (!p.is_q) {
-                        const uint32_t place = p.row / 8 ^ (p.piece & 3) * 2 ^ (p.piece / 4 & 1), half = (p.row / 4 & 1) ^ (p.piece / 8 & 1);
-                        char *const kt = (char *)lds_kt[a] + p.piece * 8 * 128 + half * 8;
-#pragma unroll
-                        for (int c = 0; c < 8; ++c) {   // component c of the four tokens
-                            const uint32_t sel = c % 2 ? 0x07060302u : 0x05040100u;
-                            *(u32x2 *)(kt + c * 128 + (place ^ (c / 2 & 1)) * 16) = (u32x2){__builtin_amdgcn_perm(w[1][c / 2], w[0][c / 2], sel), __builtin_amdgcn_perm(w[3][c / 2], w[2][c / 2], sel)};
-                        }
-                    }
-                }
-            }
-        }
-#pragma unroll
-        for (int b = 0; b < kMatrixPer; ++b)
-            if (b * 64 * NW + wave * 64 < kMatrix) lds_m[b * 64 * NW + tid] = matrices[b];
-        if (tid < 2 * kChunk) lds_d[tid] = decays;
-        // values: tokens 32 s + 8 g + 2 i, + 1 of the lane's columns
-        u32x4 V[2];
-#pragma unroll
-            for (int s = 0; s < 2; ++s) V[s] = own_column(values[s], odd_lane);
-        __syncthreads();
-        if (t0 + kChunk < end) load_chunk(t0 + kChunk, number + 1);
-        if (live_wave) {
-            const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-            f32x4 O[4], R[4], U[4];
-            constexpr bool kAhead = KD == 2;
-            u32x4 A[kAhead ? 2 : 1][4], B[2][3];
-            // The products of a chunk in steps of up to four rows of operands: K S and Q S by 32 components and term of the inputs; then E R by its terms and M R by its, for the tokens
-            // 32 s .. 32 s + 31; then K^T E R.  kAhead: a step's loads from LDS are under way while the step before is multiplied, and nothing is moved from step to step (up to 64 components:
-            // 3 prompts of 900 tokens 42 -> 39 us; with more there are no registers for it).
-            constexpr int kOfS = kStates ? 1 : 2, kOfR = kStates ? kTermsE : kTermsE + kTermsM;   // (states alone: without queries and M)
-            constexpr int kState = kOfS * kIn * KD, kSystem = kState + 2 * kOfR, kUpdate = 2 * ((2 * KD + 3) / 4) * kIn, kSteps = kSystem + kUpdate;
-            const auto fetch = [&](auto number) __attribute__((always_inline)) {
-                constexpr int k = decltype(number)::value;
-                u32x4 (&to)[4] = A[kAhead ? k % 2 : 0];
-                if constexpr (k < kState) {
-                    constexpr int p = k / (kOfS * kIn), a = k / kOfS % kIn;
-#pragma unroll
-                    for (int tile = 0; tile < 4; ++tile) to[tile] = operand(k % kOfS ? &lds_q[a][0][0] : &lds_k[a][0][0], tile, p);
-                } else if constexpr (k < kSystem) {
-                    constexpr int s = (k - kState) / kOfR, a = (k - kState) % kOfR, first = s == 0 ? 0 : 4, last = s == 0 ? 4 : 6;
-#pragma unroll
-                    for (int f = first; f < last; ++f) to[f - first] = lds_m[(a < kTermsE ? f * kTermsE + a : kOperands * kTermsE + f * kTermsM + a - kTermsE) * 64 + lane];
-                } else if constexpr (k < kSteps) {
-                    constexpr int a = (k - kSystem) % kIn, each = kUpdate / 2, s = (k - kSystem) / each, first = (k - kSystem) % each / kIn * 4;
-#pragma unroll
-                    for (int i = 0; i < 4 && first + i < 2 * KD; ++i) to[i] = kt_tile(a, first + i, s);
-                }
-            };
-            const auto step = [&](auto number) __attribute__((always_inline)) {
-                constexpr int k = decltype(number)::value;
-                if constexpr (kAhead) fetch(Number<k + 1>());
-                else fetch(number);
-                const u32x4 (&from)[4] = A[kAhead ? k % 2 : 0];
-                if constexpr (k < kState) {
-                    constexpr int p = k / (kOfS * kIn), a = k / kOfS % kIn, terms = (k % kOfS ? 2 : 3) - a;
-                    f32x4 (&to)[4] = k % kOfS ? O : R;
-#pragma unroll
-                    for (int c = 0; c < terms; ++c)
-#pragma unroll
-                        for (int tile = 0; tile < 4; ++tile) to[tile] = mfma_bf16(from[tile], B[p % 2][c], p == 0 && a == 0 && c == 0 ? zero : to[tile]);
-                    if constexpr (k % (kOfS * kIn) == kOfS - 1 && p + 1 < KD) three_terms({S[2 * p + 2], S[2 * p + 3]}, B[(p + 1) % 2]);
-                } else if constexpr (k < kSystem) {
-                    constexpr int s = (k - kState) / kOfR, a = (k - kState) % kOfR, first = s == 0 ? 0 : 4, last = s == 0 ? 4 : 6;   // operands; the tile of one behind the fourth is two before it
-                    constexpr int terms = a < kTermsE ? kTermsE - a : kTermsM - (a - kTermsE);
-#pragma unroll
-                    for (int c = 0; c < terms; ++c)
-#pragma unroll
-                        for (int f = first; f < last; ++f) {
-                            const int tile = f < 4 ? f : f - 2;
-                            if (a < kTermsE) U[tile] = mfma_bf16(from[f - first], B[s][c], f < 4 && a == 0 && c == 0 ? zero : U[tile]);
-                            else O[tile] = mfma_bf16(from[f - first], B[s][c], O[tile]);
-                        }
-                    if constexpr (s == 0 && a == 0) three_terms({R[2], R[3]}, B[1]);
-                } else {
-                    constexpr int a = (k - kSystem) % kIn, each = kUpdate / 2, s = (k - kSystem) / each, first = (k - kSystem) % each / kIn * 4;
-#pragma unroll
-                    for (int c = 0; c + a < 3; ++c)
-#pragma unroll
-                        for (int i = 0; i < 4 && first + i < 2 * KD; ++i) S[first + i] = mfma_bf16(from[i], B[s][c], S[first + i]);
-                    if constexpr (s == 0 && (k - kSystem) % each == 0) three_terms({U[2], U[3]}, B[1]);
-                }
-                if constexpr (kAhead) __builtin_amdgcn_sched_barrier(0);
-            };
-            three_terms({S[0], S[1]}, B[0]);
-            if constexpr (kAhead) fetch(Number<0>());
-            in_order<0, kState>(step);
-            // R, from the values
-            const auto decay_of = [&](int which, int tile) __attribute__((always_inline)) { return *(const f32x4 *)&lds_d[which * kChunk + (tile / 2) * 32 + g * 8 + (tile % 2) * 4]; };
-#pragma unroll
-            for (int tile = 0; tile < 4; ++tile) {
-                const f32x4 by = decay_of(0, tile);
-                if (!kStates) O[tile] *= decay_of(1, tile);
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const uint32_t w = V[tile / 2][tile % 2 * 2 + i];   // (of an element of a vector itself, a bit cast takes the first)
-                    float x, y;
-                    if constexpr (kIn == 1) {
-                        x = low_half(w), y = high_half(w);
-                    } else {
-                        typedef f16_t pair __attribute__((ext_vector_type(2)));
-                        const pair both = __builtin_bit_cast(pair, w);
-                        x = (float)both[0], y = (float)both[1];
-                    }
-                    R[tile][2 * i] = x - by[2 * i] * R[tile][2 * i], R[tile][2 * i + 1] = y - by[2 * i + 1] * R[tile][2 * i + 1];
-                }
-            }
-            three_terms({R[0], R[1]}, B[0]);
-            in_order<kState, kSystem>(step);
-            float odd = 0.f;   // NaN if anything that is written is not finite
-#pragma unroll
-                for (int tile = 0; tile < 4; ++tile)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) odd = __builtin_fmaf(U[tile][e], 0.f, odd);
-            T *const out = (T *)P.out + ((uint64_t)t0 * P.heads + h) * P.dv;
-            if (kStates || !__any(odd != 0.f)) {   // (what is not finite leaves no finite state)
-                const float decay = lds_d[kChunk - 1];
-#pragma unroll
-                for (int i = 0; i < 2 * KD; ++i) S[i] *= decay;
-                three_terms({U[0], U[1]}, B[0]);
-                in_order<kSystem, kSteps>(step);
-                __builtin_amdgcn_s_waitcnt(0x0F70);   // (the next chunk's loads, under way all this time: waited for behind the stores they would be waited for with those)
-                if constexpr (!kStates) {   // tokens 0, 1 of a tile's four are the even lane's, 2, 3 the odd one's, both columns of each
-                    const uint32_t stride = 2 * P.heads * P.dv;
-                    const uint32_t own = (anew(g) * 8 + (odd_lane ? 2 : 0)) * stride + column2;
-                    const auto rows = chunk_rows(out, m, stride, 2 * P.dv);
-#pragma unroll
-                    for (int tile = 0; tile < 4; ++tile) {
-                        const uint32_t a = pack2<T>(O[tile][0], O[tile][1]), b = pack2<T>(O[tile][2], O[tile][3]);   // own column
-                        const uint32_t got = of_neighbour(odd_lane ? a : b), mine = odd_lane ? b : a;              // the lane's two tokens, the other column and this one
-                        const uint32_t left = odd_lane ? got : mine, right = odd_lane ? mine : got;
-                        const uint32_t off = own + ((tile / 2) * 32 + (tile % 2) * 4) * stride;
-                        __builtin_amdgcn_raw_buffer_store_b32(__builtin_amdgcn_perm(right, left, 0x05040100u), rows, off, 0, 0);
-                        __builtin_amdgcn_raw_buffer_store_b32(__builtin_amdgcn_perm(right, left, 0x07060302u), rows, off + stride, 0, 0);
-                    }
-                }
-            } else if constexpr (!kStates) {   // token by token: what is not finite must not meet the zeros of earlier ones
-                for (uint32_t j = 0; j < m; ++j) {
-                    const uint64_t at_token = (uint64_t)(t0 + j) * P.heads + h;
-                    const float by = exp_of(P.log_decay[at_token]), beta = P.beta[at_token];
-                    const auto component = [&](const uint16_t (*plane)[kChunk][kRow], int p, int c) __attribute__((always_inline)) {   // 32 p + 8 g + c
-                        float x = 0.f;
-#pragma unroll
-                        for (int a = 0; a < kIn; ++a) x += low_half(*(const uint16_t *)((const char *)plane[a] + row_piece(j, p * 4 + g) + 2 * c));
-                        return x;
-                    };
-                    const float v = live_column ? to_f32(((const T *)P.v)[(t0 + j) * P.v_stride + (uint64_t)h * P.dv + column]) : 0.f;
-                    float y = 0.f, o = 0.f;
-#pragma unroll
-                    for (int p = 0; p < KD; ++p)
-#pragma unroll
-                        for (int c = 0; c < 8; ++c) {
-                            float &x = ((float *)&S[2 * p + c / 4])[c % 4];
-                            x *= by;
-                            if (p * 32 + g * 8 < P.dk) y += component(lds_k, p, c) * x;
-                        }
-                    y += __shfl_xor(y, 16);
-                    y += __shfl_xor(y, 32);
-                    const float u = beta * (v - y);
-#pragma unroll
-                    for (int p = 0; p < KD; ++p)
-#pragma unroll
-                        for (int c = 0; c < 8; ++c)
-                            if (p * 32 + g * 8 < P.dk) {
-                                float &x = ((float *)&S[2 * p + c / 4])[c % 4];
-                                x += component(lds_k, p, c) * u;
-                                o += component(lds_q, p, c) * x;
-                            }
-                    o += __shfl_xor(o, 16);
-                    o += __shfl_xor(o, 32);
-                    if (live_column && g == 0) out[(uint64_t)j * P.heads * P.dv + column] = from_f32<T>(o * P.scale);
-                }
-            }
-        }
-        __syncthreads();   // (keys, queries and matrices are free)
-    }
-    float *const to = kStates ? block_state : at.block + 1 == at.blocks && P.state_out && state != ~0ull ? P.state_out + state_at : nullptr;
-    const uint32_t to_stride = kStates ? P.dv + P.dk : P.dv;
-    if (to && live_column)
+        const uint32_t tid = here(threadIdx.x), lane = tid & 63, wave = uniform(tid >> 6), g = lane >> 4, r = lane & 15;
+        const uint32_t ordinal = uniform((uint32_t)(item / each)), rest = uniform((uint32_t)(item - (uint64_t)ordinal * each)), h = uniform(rest / slices), slice = uniform(rest - h * slices);
+        const uint32_t shared = uniform(h / P.group);
+        const BlockPlace at = find_block(PP, plan.chunks, ordinal);
+        const Span span = span_of(P, at.request);
+        const uint32_t block_tokens = plan.chunks == ~0u ? 0u : plan.chunks * kChunk;
+        const uint32_t begin = uniform(span.begin + at.block * block_tokens), end = uniform(at.block + 1 == at.blocks ? span.end : begin + block_tokens);
+        uint32_t number = uniform(at.chunk);
+        if (!at.found || (kStates && at.block + 1 == at.blocks)) continue;
+        if (begin < end && (number > PP.most_chunks || (end - begin + kChunk - 1) / kChunk > PP.most_chunks - number)) continue;   // (offsets that go backwards)
+        const uint64_t state = state_of(P, at.request), state_at = (state * P.heads + h) * ((uint64_t)P.dk * P.dv);
+        float *const block_state = PP.block_states + ((uint64_t)at.slot * P.heads + h) * ((uint64_t)P.dk * (P.dv + P.dk));
+        const uint32_t column = (slice * NW + wave) * 16 + r, columns = kStates ? P.dv + P.dk : P.dv;
+        const bool live_column = column < columns, live_wave = (slice * NW + wave) * 16 < columns;   // (columns that are not there compute what nobody reads)
+        f32x4 S[2 * KD];
+        const float *const from = kStates ? nullptr : at.blocks > 1 ? block_state : P.state_in && state != ~0ull ? P.state_in + state_at : nullptr;
+        const uint32_t from_stride = at.blocks > 1 ? P.dv + P.dk : P.dv;
 #pragma unroll
         for (int i = 0; i < 2 * KD; ++i)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const uint32_t d = (i / 2) * 32 + g * 8 + (i % 2) * 4 + e;
-                if (d < P.dk) to[(uint64_t)d * to_stride + column] = S[i][e];
+                S[i][e] = kStates ? (column == P.dv + d ? 1.f : 0.f) : from && live_column && d < P.dk ? from[(uint64_t)d * from_stride + column] : 0.f;
             }
+        constexpr uint32_t kNowhere = 1u << 31;
+        const uint32_t pieces = P.dk / 8;
+        const bool odd_lane = lane & 1;
+        const uint32_t column2 = (column & ~1u) < P.dv ? 2 * (column & ~1u) : kNowhere;   // of the lane's pair of columns, in bytes
+        u32x4 staged[kPer][4], matrices[kMatrixPer];
+        float decays = 0.f;
+        uint32_t values[2][4];
+        const auto chunk_rows = [&](const void *base, uint32_t m, uint32_t stride, uint32_t width) __attribute__((always_inline)) {
+            return make_rsrc((const void *)uniform64((uint64_t)base), uniform((m - 1) * stride + width));
+        };
+        const auto anew = [&](uint32_t v) __attribute__((always_inline)) { return KD > 2 ? here(v) : v; };   // (addresses that stay would fill the registers)
+        // A lane brings 4 tokens x 8 components of K or of Q into LDS; a wave has either.
+        struct Part {
+            bool live, is_q;
+            uint32_t row, piece;
+        };
+        const auto part_of = [&](int b) __attribute__((always_inline)) {
+            const uint32_t first = (kItemsK % (64 * NW) ? wave * 64 : 0u) + b * 64 * NW, rest = kItemsK % (64 * NW) ? 0u : wave * 64;   // (known when compiled where they divide)
+            Part p;
+            p.live = first < kItems, p.is_q = !kStates && first >= kItemsK;
+            const uint32_t id = first + rest - (p.is_q ? kItemsK : 0) + anew(lane);
+            p.piece = id % kPieces, p.row = id / kPieces * 4;
+            return p;
+        };
+        const auto load_chunk = [&](uint32_t t0, uint32_t chunk) __attribute__((always_inline)) {
+            const uint32_t m = min(kChunk, end - t0);
+#pragma unroll
+            for (int b = 0; b < kPer; ++b) {
+                const Part p = part_of(b);
+                if (p.live) {
+                    const uint32_t stride = 2 * (uint32_t)(p.is_q ? P.q_stride : P.k_stride), off = p.row * stride + (p.piece < pieces ? p.piece * 16 : kNowhere);
+                    const auto rows = chunk_rows(p.is_q ? (const T *)P.q + (uint64_t)shared * P.dk + t0 * P.q_stride : (const T *)P.k + (uint64_t)shared * P.dk + t0 * P.k_stride, m, stride, 2 * P.dk);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) staged[b][j] = __builtin_amdgcn_raw_buffer_load_b128(rows, off + j * stride, 0, 0);
+                }
+            }
+            const char *const made = PP.chunks + ((uint64_t)chunk * P.heads + h) * kChunkBytes;
+#pragma unroll
+            for (int b = 0; b < kMatrixPer; ++b)
+                if (b * 64 * NW + wave * 64 < kMatrix) matrices[b] = ((const u32x4 *)made)[b * 64 * NW + anew(tid)];
+            if (tid < 2 * kChunk) decays = ((const float *)(made + kMatrixPieces * 16))[tid];
+            const uint32_t stride = 2 * (uint32_t)P.v_stride, off = (anew(g) * 8 + (odd_lane ? 4 : 0)) * stride;
+            const auto rows = chunk_rows((const T *)P.v + (uint64_t)h * P.dv + t0 * P.v_stride, m, stride, 2 * P.dv);
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) values[s][j] = __builtin_amdgcn_raw_buffer_load_b32(rows, off + (s * 32 + j) * stride + column2, 0, 0);
+        };
+        // LDS rows are pieces of 16 bytes, exchanged by the row's number so that the sixteen rows of an operand, 8 (r / 4) + r % 4 + ..., lie in different banks.  K by component as in
+        // rows d: piece u, 8 tokens, at u ^ (2 (d / 8 mod 4) + (d / 2 mod 2)) ^ (d / 32 mod 2), its two halves exchanged where d / 64 is odd: the lanes of a read have d = 8 (r / 4) +
+        // r % 4 + ..., those of a write d / 8 from 0 to 15.
+        const auto row_piece = [&](uint32_t row, uint32_t u) __attribute__((always_inline)) {
+            return kRow == 128 ? row * 256 + ((u ^ (row & 3) ^ (row >> 3 & 3) * 4) * 16) : row * 128 + ((u ^ (row >> 1 & 1) ^ (row >> 3 & 3) * 2) * 16);
+        };
+        const uint32_t own_kt = ((r >> 2) * 8 + (r & 3)) * 128 + (g ^ (r >> 1)) * 16;
+        const auto kt_tile = [&](int a, int t, int s) __attribute__((always_inline)) {   // components of tile t, tokens 32 s + 8 g .. + 7
+            const u32x4 w = *(const u32x4 *)((const char *)lds_kt[a] + (own_kt ^ (s * 64) ^ (t / 2 % 2 * 16)) + (t / 2) * 32 * 128 + (t % 2) * 4 * 128);
+            return t / 4 % 2 ? (u32x4){w[2], w[3], w[0], w[1]} : w;
+        };
+        // Rows of tile (s, t) = (tile / 2, tile % 2), 32 s + 4 t behind the lane's own: pieces there are exchanged by the same bits.
+        const uint32_t own_rows = row_piece(8 * (r >> 2) + (r & 3), g);
+        const auto operand = [&](const uint16_t *plane, int tile, int p) __attribute__((always_inline)) {
+            return *(const u32x4 *)((const char *)plane + (own_rows ^ (p * 64)) + ((tile / 2) * 32 + (tile % 2) * 4) * 2 * kRow);
+        };
+        if (begin < end) load_chunk(begin, number);
+        // The first chunk's loads are waited for here: with any of them under way at the loop's head, the compiler's wait there would be for all that the wave has
+        // issued, the stores of the chunk before among them.
+        __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0)
+        for (uint32_t t0 = begin; t0 < end; t0 += kChunk, ++number) {
+            const uint32_t m = min(kChunk, end - t0);
+#pragma unroll
+            for (int b = 0; b < kPer; ++b) {
+                const Part p = part_of(b);
+                if (p.live) {
+#pragma unroll
+                    for (int a = 0; a < kIn; ++a) {
+                        uint32_t w[4][4];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                uint32_t terms[kIn];
+                                input_terms<T, kIn>(staged[b][j][i], terms);
+                                w[j][i] = terms[a];
+                            }
+                        char *const to = p.is_q ? (char *)lds_q[a] : (char *)lds_k[a];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) *(u32x4 *)(to + row_piece(p.row + j, p.piece)) = (u32x4){w[j][0], w[j][1], w[j][2], w[j][3]};
+                        if (!p.is_q) {
+                            const uint32_t place = p.row / 8 ^ (p.piece & 3) * 2 ^ (p.piece / 4 & 1), half = (p.row / 4 & 1) ^ (p.piece / 8 & 1);
+                            char *const kt = (char *)lds_kt[a] + p.piece * 8 * 128 + half * 8;
+#pragma unroll
+                            for (int c = 0; c < 8; ++c) {   // component c of the four tokens
+                                const uint32_t sel = c % 2 ? 0x07060302u : 0x05040100u;
+                                *(u32x2 *)(kt + c * 128 + (place ^ (c / 2 & 1)) * 16) = (u32x2){__builtin_amdgcn_perm(w[1][c / 2], w[0][c / 2], sel), __builtin_amdgcn_perm(w[3][c / 2], w[2][c / 2], sel)};
+                            }
+                        }
+                    }
+                }
+            }
+#pragma unroll
+            for (int b = 0; b < kMatrixPer; ++b)
+                if (b * 64 * NW + wave * 64 < kMatrix) lds_m[b * 64 * NW + tid] = matrices[b];
+            if (tid < 2 * kChunk) lds_d[tid] = decays;
+            // values: tokens 32 s + 8 g + 2 i, + 1 of the lane's columns
+            u32x4 V[2];
+#pragma unroll
+            for (int s = 0; s < 2; ++s) V[s] = own_column(values[s], odd_lane);
+            __syncthreads();
+            if (t0 + kChunk < end) load_chunk(t0 + kChunk, number + 1);
+            if (live_wave) {
+                const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+                f32x4 O[4], R[4], U[4];
+                constexpr bool kAhead = KD == 2;
+                u32x4 A[kAhead ? 2 : 1][4], B[2][3];
+                // The products of a chunk in steps of up to four rows of operands: K S and Q S by 32 components and term of the inputs; then E R by its terms and M R by its, for the tokens
+                // 32 s .. 32 s + 31; then K^T E R.  kAhead: a step's loads from LDS are under way while the step before is multiplied, and nothing is moved from step to step (up to 64 components:
+                // 3 prompts of 900 tokens 42 -> 39 us; with more there are no registers for it).
+                constexpr int kOfS = kStates ? 1 : 2, kOfR = kStates ? kTermsE : kTermsE + kTermsM;   // (states alone: without queries and M)
+                constexpr int kState = kOfS * kIn * KD, kSystem = kState + 2 * kOfR, kUpdate = 2 * ((2 * KD + 3) / 4) * kIn, kSteps = kSystem + kUpdate;
+                const auto fetch = [&](auto number) __attribute__((always_inline)) {
+                    constexpr int k = decltype(number)::value;
+                    u32x4 (&to)[4] = A[kAhead ? k % 2 : 0];
+                    if constexpr (k < kState) {
+                        constexpr int p = k / (kOfS * kIn), a = k / kOfS % kIn;
+#pragma unroll
+                        for (int tile = 0; tile < 4; ++tile) to[tile] = operand(k % kOfS ? &lds_q[a][0][0] : &lds_k[a][0][0], tile, p);
+                    } else if constexpr (k < kSystem) {
+                        constexpr int s = (k - kState) / kOfR, a = (k - kState) % kOfR, first = s == 0 ? 0 : 4, last = s == 0 ? 4 : 6;
+#pragma unroll
+                        for (int f = first; f < last; ++f) to[f - first] = lds_m[(a < kTermsE ? f * kTermsE + a : kOperands * kTermsE + f * kTermsM + a - kTermsE) * 64 + lane];
+                    } else if constexpr (k < kSteps) {
+                        constexpr int a = (k - kSystem) % kIn, each = kUpdate / 2, s = (k - kSystem) / each, first = (k - kSystem) % each / kIn * 4;
+#pragma unroll
+                        for (int i = 0; i < 4 && first + i < 2 * KD; ++i) to[i] = kt_tile(a, first + i, s);
+                    }
+                };
+                const auto step = [&](auto number) __attribute__((always_inline)) {
+                    constexpr int k = decltype(number)::value;
+                    if constexpr (kAhead) fetch(Number<k + 1>());
+                    else fetch(number);
+                    const u32x4 (&from)[4] = A[kAhead ? k % 2 : 0];
+                    if constexpr (k < kState) {
+                        constexpr int p = k / (kOfS * kIn), a = k / kOfS % kIn, terms = (k % kOfS ? 2 : 3) - a;
+                        f32x4 (&to)[4] = k % kOfS ? O : R;
+#pragma unroll
+                        for (int c = 0; c < terms; ++c)
+#pragma unroll
+                            for (int tile = 0; tile < 4; ++tile) to[tile] = mfma_bf16(from[tile], B[p % 2][c], p == 0 && a == 0 && c == 0 ? zero : to[tile]);
+                        if constexpr (k % (kOfS * kIn) == kOfS - 1 && p + 1 < KD) three_terms({S[2 * p + 2], S[2 * p + 3]}, B[(p + 1) % 2]);
+                    } else if constexpr (k < kSystem) {
+                        constexpr int s = (k - kState) / kOfR, a = (k - kState) % kOfR, first = s == 0 ? 0 : 4, last = s == 0 ? 4 : 6;   // operands; the tile of one behind the fourth is two before it
+                        constexpr int terms = a < kTermsE ? kTermsE - a : kTermsM - (a - kTermsE);
+#pragma unroll
+                        for (int c = 0; c < terms; ++c)
+#pragma unroll
+                            for (int f = first; f < last; ++f) {
+                                const int tile = f < 4 ? f : f - 2;
+                                if (a < kTermsE) U[tile] = mfma_bf16(from[f - first], B[s][c], f < 4 && a == 0 && c == 0 ? zero : U[tile]);
+                                else O[tile] = mfma_bf16(from[f - first], B[s][c], O[tile]);
+                            }
+                        if constexpr (s == 0 && a == 0) three_terms({R[2], R[3]}, B[1]);
+                    } else {
+                        constexpr int a = (k - kSystem) % kIn, each = kUpdate / 2, s = (k - kSystem) / each, first = (k - kSystem) % each / kIn * 4;
+#pragma unroll
+                        for (int c = 0; c + a < 3; ++c)
+#pragma unroll
+                            for (int i = 0; i < 4 && first + i < 2 * KD; ++i) S[first + i] = mfma_bf16(from[i], B[s][c], S[first + i]);
+                        if constexpr (s == 0 && (k - kSystem) % each == 0) three_terms({U[2], U[3]}, B[1]);
+                    }
+                    if constexpr (kAhead) __builtin_amdgcn_sched_barrier(0);
+                };
+                three_terms({S[0], S[1]}, B[0]);
+                if constexpr (kAhead) fetch(Number<0>());
+                in_order<0, kState>(step);
+                // R, from the values
+                const auto decay_of = [&](int which, int tile) __attribute__((always_inline)) { return *(const f32x4 *)&lds_d[which * kChunk + (tile / 2) * 32 + g * 8 + (tile % 2) * 4]; };
+#pragma unroll
+                for (int tile = 0; tile < 4; ++tile) {
+                    const f32x4 by = decay_of(0, tile);
+                    if (!kStates) O[tile] *= decay_of(1, tile);
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const uint32_t w = V[tile / 2][tile % 2 * 2 + i];   // (of an element of a vector itself, a bit cast takes the first)
+                        float x, y;
+                        if constexpr (kIn == 1) {
+                            x = low_half(w), y = high_half(w);
+                        } else {
+                            typedef f16_t pair __attribute__((ext_vector_type(2)));
+                            const pair both = __builtin_bit_cast(pair, w);
+                            x = (float)both[0], y = (float)both[1];
+                        }
+                        R[tile][2 * i] = x - by[2 * i] * R[tile][2 * i], R[tile][2 * i + 1] = y - by[2 * i + 1] * R[tile][2 * i + 1];
+                    }
+                }
+                three_terms({R[0], R[1]}, B[0]);
+                in_order<kState, kSystem>(step);
+                float odd = 0.f;   // NaN if anything that is written is not finite
+#pragma unroll
+                for (int tile = 0; tile < 4; ++tile)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) odd = __builtin_fmaf(U[tile][e], 0.f, odd);
+                T *const out = (T *)P.out + ((uint64_t)t0 * P.heads + h) * P.dv;
+                if (kStates || !__any(odd != 0.f)) {   // (what is not finite leaves no finite state)
+                    const float decay = lds_d[kChunk - 1];
+#pragma unroll
+                    for (int i = 0; i < 2 * KD; ++i) S[i] *= decay;
+                    three_terms({U[0], U[1]}, B[0]);
+                    in_order<kSystem, kSteps>(step);
+                    __builtin_amdgcn_s_waitcnt(0x0F70);   // (the next chunk's loads, under way all this time: waited for behind the stores they would be waited for with those)
+                    if constexpr (!kStates) {   // tokens 0, 1 of a tile's four are the even lane's, 2, 3 the odd one's, both columns of each
+                        const uint32_t stride = 2 * P.heads * P.dv;
+                        const uint32_t own = (anew(g) * 8 + (odd_lane ? 2 : 0)) * stride + column2;
+                        const auto rows = chunk_rows(out, m, stride, 2 * P.dv);
+#pragma unroll
+                        for (int tile = 0; tile < 4; ++tile) {
+                            const uint32_t a = pack2<T>(O[tile][0], O[tile][1]), b = pack2<T>(O[tile][2], O[tile][3]);   // own column
+                            const uint32_t got = of_neighbour(odd_lane ? a : b), mine = odd_lane ? b : a;              // the lane's two tokens, the other column and this one
+                            const uint32_t left = odd_lane ? got : mine, right = odd_lane ? mine : got;
+                            const uint32_t off = own + ((tile / 2) * 32 + (tile % 2) * 4) * stride;
+                            __builtin_amdgcn_raw_buffer_store_b32(__builtin_amdgcn_perm(right, left, 0x05040100u), rows, off, 0, 0);
+                            __builtin_amdgcn_raw_buffer_store_b32(__builtin_amdgcn_perm(right, left, 0x07060302u), rows, off + stride, 0, 0);
+                        }
+                    }
+                } else if constexpr (!kStates) {   // token by token: what is not finite must not meet the zeros of earlier ones
+                    for (uint32_t j = 0; j < m; ++j) {
+                        const uint64_t at_token = (uint64_t)(t0 + j) * P.heads + h;
+                        const float by = exp_of(P.log_decay[at_token]), beta = P.beta[at_token];
+                        const auto component = [&](const uint16_t (*plane)[kChunk][kRow], int p, int c) __attribute__((always_inline)) {   // 32 p + 8 g + c
+                            float x = 0.f;
+#pragma unroll
+                            for (int a = 0; a < kIn; ++a) x += low_half(*(const uint16_t *)((const char *)plane[a] + row_piece(j, p * 4 + g) + 2 * c));
+                            return x;
+                        };
+                        const float v = live_column ? to_f32(((const T *)P.v)[(t0 + j) * P.v_stride + (uint64_t)h * P.dv + column]) : 0.f;
+                        float y = 0.f, o = 0.f;
+#pragma unroll
+                        for (int p = 0; p < KD; ++p)
+#pragma unroll
+                            for (int c = 0; c < 8; ++c) {
+                                float &x = ((float *)&S[2 * p + c / 4])[c % 4];
+                                x *= by;
+                                if (p * 32 + g * 8 < P.dk) y += component(lds_k, p, c) * x;
+                            }
+                        y += __shfl_xor(y, 16);
+                        y += __shfl_xor(y, 32);
+                        const float u = beta * (v - y);
+#pragma unroll
+                        for (int p = 0; p < KD; ++p)
+#pragma unroll
+                            for (int c = 0; c < 8; ++c)
+                                if (p * 32 + g * 8 < P.dk) {
+                                    float &x = ((float *)&S[2 * p + c / 4])[c % 4];
+                                    x += component(lds_k, p, c) * u;
+                                    o += component(lds_q, p, c) * x;
+                                }
+                        o += __shfl_xor(o, 16);
+                        o += __shfl_xor(o, 32);
+                        if (live_column && g == 0) out[(uint64_t)j * P.heads * P.dv + column] = from_f32<T>(o * P.scale);
+                    }
+                }
+            }
+            __syncthreads();   // (keys, queries and matrices are free)
+        }
+        float *const to = kStates ? block_state : at.block + 1 == at.blocks && P.state_out && state != ~0ull ? P.state_out + state_at : nullptr;
+        const uint32_t to_stride = kStates ? P.dv + P.dk : P.dv;
+        if (to && live_column)
+#pragma unroll
+            for (int i = 0; i < 2 * KD; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t d = (i / 2) * 32 + g * 8 + (i % 2) * 4 + e;
+                    if (d < P.dk) to[(uint64_t)d * to_stride + column] = S[i][e];
+                }
     }
 }
 
 // The state before each block of the requests that are taken apart, over the blocks' B: S_(b + 1) = A_b S_b + B_b.  A workgroup has 16 columns, wave w the rows 32 w .. 32 w + 31; the rows
-// go from wave to wave through LDS.  Both operands are fp32: three terms each.
+// go from wave to wave through LDS.  Both operands are fp32: three terms each.  Bound by the way from one block's state to the next, once for each block: 45000 tokens in 32 blocks of 16 heads 46 us.
 template <int KD> __global__ __launch_bounds__(64 * KD) void delta_states_kernel(DeltaPromptParams PP) {
     __shared__ __align__(16) float state_rows[2][16][KD * 32 + 4];
     const DeltaParams &P = PP.d;
@@ -773,7 +785,7 @@ template <int KD> __global__ __launch_bounds__(64 * KD) void delta_states_kernel
             mine += b > 1 ? b : 0u;
         }
         const uint32_t slot = wave_sum32(mine), column = slice * 16 + r, first_row = wave * 32 + g * 8;
-        if (slot + blocks > PP.slots) continue;
+        if (slot > PP.slots || blocks > PP.slots - slot) continue;
         const uint64_t step = P.heads * (uint64_t)P.dk * wide, state = state_of(P, request);
         float *const matrices = PP.block_states + ((uint64_t)slot * P.heads + h) * ((uint64_t)P.dk * wide);
         const bool live = column < P.dv && first_row < P.dk;

@@ -29,7 +29,8 @@ mmv_status delta_params(DeltaParams &P, uint64_t n, uint64_t tokens, uint32_t he
     return MMV_OK;
 }
 
-// Rows that the threads of a workgroup have at once (16 at most: their sums are joined one by one), and of a thread.
+// Rows that the threads of a workgroup have at once (16 at most: their sums are joined one by one), and of a thread: as few registers as hold them, for more waves (128 requests of 32 heads of
+// 64 x 64, four rows a thread: 32.3 us, with registers for sixteen 37.3; 200 of 16 heads of 64 x 160, eight: 60.0, 65.4).
 template <typename T, int kThreads> mmv_status launch_step(DeltaParams P, hipStream_t s) {
     const uint32_t fit = kThreads / (P.dv / 4), step = fit < 16 ? fit : 16, rows = (uint32_t)ceil_div(P.dk, step), most = most_of_a_launch(kThreads, P.heads);
     for (; P.first < P.n; P.first += most) {
@@ -51,7 +52,8 @@ inline uint32_t delta_slices(uint32_t columns) { return (columns + 16 * kDeltaWa
 inline uint32_t delta_round(uint32_t heads, uint32_t dv) { return 2 * kUnits / (heads * delta_slices(dv)); }
 inline uint64_t delta_slots(uint64_t n, uint64_t tokens, uint32_t heads, uint32_t dv) {
     const uint64_t chunks = delta_chunks(n, tokens), round = delta_round(heads, dv), most = 2 * round;
-    if (round <= kApart || tokens <= (kLeastApart - 1) * kChunk) return 0;
+    const uint64_t longest = ceil_div(tokens, kChunk);
+    if (!worth_taking_apart(longest, longest, (uint32_t)round)) return 0;   // (all tokens in one request: nothing is more uneven)
     return 2 * chunks / kLeastBlock < most ? 2 * chunks / kLeastBlock : most;
 }
 inline size_t delta_chunk_bytes(uint64_t n, uint64_t tokens, uint32_t heads) { return (size_t)delta_chunks(n, tokens) * heads * kChunkBytes; }
