@@ -121,6 +121,8 @@ template <typename T, int kRows, int kThreads> __global__ __launch_bounds__(kThr
 //   E = diag(e^(G_63 - G)) T,   M = W T.
 // delta_prompt_kernel then goes through a request's chunks: R = V - diag(e^G) K S, out = scale diag(e^G) Q S + M R, S' = e^(G_63) S + K^T E R.
 constexpr uint32_t kChunk = 64;
+// Workgroups go to the eight dies in turn, and each has a cache of its own: of `each` (the heads of a chunk; of a request, with their slices of columns), neighbours, which read the same, to one.
+__device__ __forceinline__ uint32_t by_die(uint32_t i, uint32_t each) { return each % 8 ? i : (i & 7) * (each / 8) + i / 8; }
 
 // What a chunk of a head leaves: matrices as operands of 16x16x32 products, 1 KB (64 lanes of 16 bytes) each: rows 32 s + 8 (r / 4) + 4 t + r % 4 (s, t = 0, 1), columns 32 c + 8 g + 0..7 in
 // lane 16 g + r, c <= s (above the diagonal there is nothing): the operands (s, t, c) = (0,0,0) (0,1,0) (1,0,0) (1,1,0) (1,0,1) (1,1,1), E in three bf16 terms, M in two.
@@ -185,9 +187,11 @@ __device__ __forceinline__ ChunkPlace find_chunk(const DeltaParams &P, uint32_t 
 // Blocks have four chunks at least: 16 chunks, 12 times: 2 93, 4 85, 8 97 us; and as many as fill the device once: filled 3, 2, 1 times, one of 32768 tokens 843, 773, 709 us.
 constexpr uint32_t kLeastBlock = 4, kLeastApart = 16, kApartFixed = 10, kApartQuarters = 13;
 __host__ __device__ constexpr bool worth_taking_apart(uint64_t most, uint64_t all, uint32_t round) { return most >= kLeastApart && 4 * (most - kApartFixed) * round > kApartQuarters * all; }
+constexpr uint32_t kMostOrdered = 256;
 struct BlockPlan {
     uint32_t chunks, blocks;   // chunks of a block (~0: all of a request), blocks in all
 };
+__host__ __device__ constexpr uint32_t delta_slices(uint32_t columns, uint32_t waves) { return (columns + 16 * waves - 1) / (16 * waves); }
 __device__ __forceinline__ uint32_t blocks_in(uint32_t chunks, uint32_t block) { return block == ~0u ? 1u : max(1u, (chunks + block - 1) / block); }
 __device__ __forceinline__ BlockPlan plan_blocks(const DeltaPromptParams &PP) {
     const DeltaParams &P = PP.d;
@@ -241,21 +245,66 @@ __device__ __forceinline__ BlockPlace find_block(const DeltaPromptParams &PP, ui
     return {0, 0, 0, 0, 0, false};
 }
 
+// The same where requests are whole and more than the device takes at once: the longest first, so that none of them begins when the others are done (24 requests of 64 to 4096 tokens, the longest
+// ones last: 380 us as they come, 290).  Up to 256 requests: a lane has four of them, and the length that a place in that order has is found by bisection.
+__device__ __forceinline__ BlockPlace find_longest(const DeltaParams &P, uint32_t place) {
+    const uint32_t lane = threadIdx.x & 63;
+    uint32_t chunks[kMostOrdered / 64], most = 0;   // and one: 0 where there is no request
+#pragma unroll
+    for (uint32_t j = 0; j < kMostOrdered / 64; ++j) {
+        const uint32_t r = j * 64 + lane;
+        chunks[j] = r < P.n ? chunks_of(span_of(P, r)) + 1 : 0u;
+        most = max(most, chunks[j]);
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) most = max(most, (uint32_t)__shfl_xor((int)most, d));
+    const auto as_long = [&](uint32_t least) __attribute__((always_inline)) {
+        uint32_t n = 0;
+#pragma unroll
+        for (uint32_t j = 0; j < kMostOrdered / 64; ++j) n += __builtin_popcountll(__ballot(chunks[j] >= least));
+        return n;
+    };
+    uint32_t own = 1, behind = uniform(most) + 1;   // more than `place` requests have as many as `own`, no more than `place` as many as `behind`
+    while (behind - own > 1) {
+        const uint32_t middle = own + (behind - own) / 2;
+        (as_long(middle) > place ? own : behind) = middle;
+    }
+    uint32_t left = place - as_long(own + 1);
+    BlockPlace at = {0, 0, 1, 0, 0, true};
+    bool found = false;
+#pragma unroll
+    for (uint32_t j = 0; j < kMostOrdered / 64; ++j) {
+        uint64_t same = __ballot(chunks[j] == own);
+        const uint32_t here = __builtin_popcountll(same);
+        if (!found && left < here) {
+            for (uint32_t i = 0; i < left; ++i) same &= same - 1;
+            at.request = j * 64 + __builtin_ctzll(same), found = true;
+        }
+        left -= found ? 0u : here;
+    }
+    uint32_t before = 0;
+#pragma unroll
+    for (uint32_t j = 0; j < kMostOrdered / 64; ++j) before += j * 64 + lane < at.request ? chunks[j] - 1 : 0u;
+    at.chunk = wave_sum32(before);
+    return at;
+}
+
 // The value itself, made anew where it is used (no instruction): what follows from it is not kept in registers all through a loop.
 __device__ __forceinline__ uint32_t here(uint32_t v) {
     asm volatile("" : "+v"(v));
     return v;
 }
-// Eight values of a lane as the three terms of an operand.
-__device__ __forceinline__ void three_terms(const f32x4 (&x)[2], u32x4 (&to)[3]) {
+// Four values of a lane as the three terms of half an operand, and eight.
+template <int half> __device__ __forceinline__ void half_terms(f32x4 x, u32x4 (&to)[3]) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < 2; ++i) {
         uint32_t terms[3];
-        take_apart<3>(x[i / 2][2 * (i % 2)], x[i / 2][2 * (i % 2) + 1], terms);
+        take_apart<3>(x[2 * i], x[2 * i + 1], terms);
 #pragma unroll
-        for (int c = 0; c < 3; ++c) to[c][i] = terms[c];
+        for (int c = 0; c < 3; ++c) to[c][2 * half + i] = terms[c];
     }
 }
+__device__ __forceinline__ void three_terms(const f32x4 (&x)[2], u32x4 (&to)[3]) { half_terms<0>(x[0], to), half_terms<1>(x[1], to); }
 template <int k> struct Number {
     static constexpr int value = k;
 };
@@ -283,7 +332,7 @@ template <typename T> __global__ __launch_bounds__(256, 5) void delta_chunks_ker
     __shared__ float betas[kChunk], left[kChunk];
     const DeltaParams &P = PP.d;
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), g = lane >> 4, r = lane & 15;
-    const uint32_t in_launch = uniform(blockIdx.x / P.heads), h = uniform(blockIdx.x - in_launch * P.heads), shared = uniform(h / P.group), number = PP.first + in_launch;
+    const uint32_t in_launch = uniform(blockIdx.x / P.heads), h = uniform(by_die(blockIdx.x - in_launch * P.heads, P.heads)), shared = uniform(h / P.group), number = PP.first + in_launch;
     const ChunkPlace at = find_chunk(P, number);
     if (!at.found || number >= PP.most_chunks) return;
     const uint32_t t0 = uniform(at.begin), m = uniform(at.end - at.begin), pieces = P.dk / 8;
@@ -451,24 +500,37 @@ __device__ __forceinline__ u32x4 own_column(const uint32_t (&row)[4], bool odd) 
 // 906 TFLOP/s of terms, 74 % of what a large library product does).  Four waves, two workgroups on a compute unit: a workgroup of eight waves 448 us where four had 443, and one of 45000 tokens
 // in blocks 2197, so 1763; two groups of 16 columns to a wave, which halve the reads of LDS, need twice the registers and are slower.
 // kStates: what blocks make of a state (columns dv and on: of the identity), without outputs.
-constexpr int kDeltaWaves = 4;
-template <int KD, typename T, bool kStates> __global__ __launch_bounds__(64 * kDeltaWaves, !__is_same(T, f16_t) || KD == 2 ? 2 : 1) void delta_prompt_kernel(DeltaPromptParams PP, uint32_t slices) {
-    constexpr int NW = kDeltaWaves, kIn = __is_same(T, f16_t) ? 2 : 1, kRow = KD == 2 ? 64 : 128, kPieces = KD * 4;
+constexpr size_t kLdsBytes = 160 * 1024;
+template <int KD, int kIn, bool kStates> struct DeltaStage {   // what a chunk needs in LDS; planes of terms
+    static constexpr uint32_t kRow = KD == 2 ? 64 : 128, kMatrix = kStates ? kOperands * kTermsE * 64 : kMatrixPieces;
+    uint16_t k[kIn][kChunk][kRow], q[kStates ? 0 : kIn][kChunk][kRow], kt[kIn][KD * 32][kChunk];
+};
+// A barrier for what lies in LDS alone: output stores stay under way (loads into LDS are waited for where the next chunk is taken in).
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+template <int KD, typename T, bool kStates, int kCompute> __global__ __launch_bounds__(512, 2) void delta_prompt_kernel(DeltaPromptParams PP) {
+    constexpr int NW = kCompute, kIn = __is_same(T, f16_t) ? 2 : 1, kPieces = KD * 4;
+    typedef DeltaStage<KD, kIn, kStates> Stage;
+    constexpr uint32_t kRow = Stage::kRow;
+    constexpr bool kApart = kCompute < 8;   // four waves compute, four bring the chunks
+    struct Matrices {
+        u32x4 m[Stage::kMatrix];
+        float d[2 * kChunk];
+    };
+    constexpr int kStages = 2 * (sizeof(Stage) + sizeof(Matrices)) <= kLdsBytes ? 2 : 1;
     constexpr int kItemsK = 16 * kPieces, kItems = kStates ? kItemsK : 2 * kItemsK, kPer = (kItems + 64 * NW - 1) / (64 * NW);
-    constexpr uint32_t kMatrix = kStates ? kOperands * kTermsE * 64 : kMatrixPieces;
-    constexpr int kMatrixPer = (kMatrix + 64 * NW - 1) / (64 * NW);
-    __shared__ __align__(16) uint16_t lds_q[kStates ? 1 : kIn][kStates ? 1 : kChunk][kRow], lds_k[kIn][kChunk][kRow], lds_kt[kIn][KD * 32][kChunk];
-    __shared__ __align__(16) u32x4 lds_m[kMatrix];
-    __shared__ __align__(16) float lds_d[2 * kChunk];
+    constexpr uint32_t kMatrix = Stage::kMatrix;
+    __shared__ __align__(16) Stage stages[kStages];
+    __shared__ __align__(16) Matrices made[2];
     const DeltaParams &P = PP.d;
     const BlockPlan plan = plan_blocks(PP);
     if (kStates && plan.chunks == ~0u) return;
-    const uint32_t each = P.heads * slices;
+    const uint32_t slices = delta_slices(kStates ? P.dv + P.dk : P.dv, kCompute), each = P.heads * slices;
     for (uint64_t item = blockIdx.x; item < (uint64_t)plan.blocks * each; item += gridDim.x) {
-        const uint32_t tid = here(threadIdx.x), lane = tid & 63, wave = uniform(tid >> 6), g = lane >> 4, r = lane & 15;
-        const uint32_t ordinal = uniform((uint32_t)(item / each)), rest = uniform((uint32_t)(item - (uint64_t)ordinal * each)), h = uniform(rest / slices), slice = uniform(rest - h * slices);
+        const uint32_t tid = here(threadIdx.x) & (64 * NW - 1), lane = tid & 63, wave = uniform(tid >> 6), g = lane >> 4, r = lane & 15;
+        const uint32_t ordinal = uniform((uint32_t)(item / each)), rest = uniform(by_die((uint32_t)(item - (uint64_t)ordinal * each), each)), h = uniform(rest / slices), slice = uniform(rest - h * slices);
         const uint32_t shared = uniform(h / P.group);
-        const BlockPlace at = find_block(PP, plan.chunks, ordinal);
+        const bool ordered = plan.chunks == ~0u && P.n <= kMostOrdered && (uint64_t)P.n * each > kUnits;
+        const BlockPlace at = ordered ? find_longest(P, ordinal) : find_block(PP, plan.chunks, ordinal);
         const Span span = span_of(P, at.request);
         const uint32_t block_tokens = plan.chunks == ~0u ? 0u : plan.chunks * kChunk;
         const uint32_t begin = uniform(span.begin + at.block * block_tokens), end = uniform(at.block + 1 == at.blocks ? span.end : begin + block_tokens);
@@ -477,29 +539,16 @@ template <int KD, typename T, bool kStates> __global__ __launch_bounds__(64 * kD
         if (begin < end && (number > PP.most_chunks || (end - begin + kChunk - 1) / kChunk > PP.most_chunks - number)) continue;   // (offsets that go backwards)
         const uint64_t state = state_of(P, at.request), state_at = (state * P.heads + h) * ((uint64_t)P.dk * P.dv);
         float *const block_state = PP.block_states + ((uint64_t)at.slot * P.heads + h) * ((uint64_t)P.dk * (P.dv + P.dk));
-        const uint32_t column = (slice * NW + wave) * 16 + r, columns = kStates ? P.dv + P.dk : P.dv;
-        const bool live_column = column < columns, live_wave = (slice * NW + wave) * 16 < columns;   // (columns that are not there compute what nobody reads)
-        f32x4 S[2 * KD];
-        const float *const from = kStates ? nullptr : at.blocks > 1 ? block_state : P.state_in && state != ~0ull ? P.state_in + state_at : nullptr;
-        const uint32_t from_stride = at.blocks > 1 ? P.dv + P.dk : P.dv;
-#pragma unroll
-        for (int i = 0; i < 2 * KD; ++i)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const uint32_t d = (i / 2) * 32 + g * 8 + (i % 2) * 4 + e;
-                S[i][e] = kStates ? (column == P.dv + d ? 1.f : 0.f) : from && live_column && d < P.dk ? from[(uint64_t)d * from_stride + column] : 0.f;
-            }
+        const uint32_t column = (slice * kCompute + wave) * 16 + r, columns = kStates ? P.dv + P.dk : P.dv;
+        const bool live_column = column < columns, live_wave = (slice * kCompute + wave) * 16 < columns;   // (columns that are not there compute what nobody reads)
         constexpr uint32_t kNowhere = 1u << 31;
         const uint32_t pieces = P.dk / 8;
         const bool odd_lane = lane & 1;
         const uint32_t column2 = (column & ~1u) < P.dv ? 2 * (column & ~1u) : kNowhere;   // of the lane's pair of columns, in bytes
-        u32x4 staged[kPer][4], matrices[kMatrixPer];
-        float decays = 0.f;
-        uint32_t values[2][4];
         const auto chunk_rows = [&](const void *base, uint32_t m, uint32_t stride, uint32_t width) __attribute__((always_inline)) {
             return make_rsrc((const void *)uniform64((uint64_t)base), uniform((m - 1) * stride + width));
         };
-        const auto anew = [&](uint32_t v) __attribute__((always_inline)) { return KD > 2 ? here(v) : v; };   // (addresses that stay would fill the registers)
+        const auto anew = [&](uint32_t v) __attribute__((always_inline)) { return here(v); };   // (addresses that stay would fill the registers)
         // A lane brings 4 tokens x 8 components of K or of Q into LDS; a wave has either.
         struct Part {
             bool live, is_q;
@@ -513,7 +562,18 @@ template <int KD, typename T, bool kStates> __global__ __launch_bounds__(64 * kD
             p.piece = id % kPieces, p.row = id / kPieces * 4;
             return p;
         };
-        const auto load_chunk = [&](uint32_t t0, uint32_t chunk) __attribute__((always_inline)) {
+        // LDS rows are pieces of 16 bytes, exchanged by the row's number so that the sixteen rows of an operand, 8 (r / 4) + r % 4 + ..., lie in different banks.  K by component as in
+        // rows d: piece u, 8 tokens, at u ^ (2 (d / 8 mod 4) + (d / 2 mod 2)) ^ (d / 32 mod 2), its two halves exchanged where d / 64 is odd: the lanes of a read have d = 8 (r / 4) +
+        // r % 4 + ..., those of a write d / 8 from 0 to 15.
+        const auto row_piece = [&](uint32_t row, uint32_t u) __attribute__((always_inline)) {
+            return kRow == 128 ? row * 256 + ((u ^ (row & 3) ^ (row >> 3 & 3) * 4) * 16) : row * 128 + ((u ^ (row >> 1 & 1) ^ (row >> 3 & 3) * 2) * 16);
+        };
+        const uint32_t own_kt = ((r >> 2) * 8 + (r & 3)) * 128 + (g ^ (r >> 1)) * 16;
+        // Rows of tile (s, t) = (tile / 2, tile % 2), 32 s + 4 t behind the lane's own: pieces there are exchanged by the same bits.
+        const uint32_t own_rows = row_piece(8 * (r >> 2) + (r & 3), g);
+        u32x4 staged[kPer][4];
+        float decays = 0.f;
+        const auto load_chunk = [&](uint32_t t0) __attribute__((always_inline)) {
             const uint32_t m = min(kChunk, end - t0);
 #pragma unroll
             for (int b = 0; b < kPer; ++b) {
@@ -525,40 +585,20 @@ template <int KD, typename T, bool kStates> __global__ __launch_bounds__(64 * kD
                     for (int j = 0; j < 4; ++j) staged[b][j] = __builtin_amdgcn_raw_buffer_load_b128(rows, off + j * stride, 0, 0);
                 }
             }
-            const char *const made = PP.chunks + ((uint64_t)chunk * P.heads + h) * kChunkBytes;
+        };
+        // Matrices go from memory straight into LDS, 1 KB a wave at a time.
+        const auto bring_matrices = [&](uint32_t chunk, Matrices &to) __attribute__((always_inline)) {
+            const char *const from = PP.chunks + ((uint64_t)chunk * P.heads + h) * kChunkBytes;
 #pragma unroll
-            for (int b = 0; b < kMatrixPer; ++b)
-                if (b * 64 * NW + wave * 64 < kMatrix) matrices[b] = ((const u32x4 *)made)[b * 64 * NW + anew(tid)];
-            if (tid < 2 * kChunk) decays = ((const float *)(made + kMatrixPieces * 16))[tid];
-            const uint32_t stride = 2 * (uint32_t)P.v_stride, off = (anew(g) * 8 + (odd_lane ? 4 : 0)) * stride;
-            const auto rows = chunk_rows((const T *)P.v + (uint64_t)h * P.dv + t0 * P.v_stride, m, stride, 2 * P.dv);
-#pragma unroll
-            for (int s = 0; s < 2; ++s)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) values[s][j] = __builtin_amdgcn_raw_buffer_load_b32(rows, off + (s * 32 + j) * stride + column2, 0, 0);
+            for (uint32_t b = 0; b < kMatrix; b += 64 * NW)
+                if (b + wave * 64 < kMatrix) __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(from + (b + tid) * 16), (__attribute__((address_space(3))) void *)&to.m[b + wave * 64], 16, 0, 0);
+            if (tid < 2 * kChunk) decays = ((const float *)(from + kMatrixPieces * 16))[tid];
         };
-        // LDS rows are pieces of 16 bytes, exchanged by the row's number so that the sixteen rows of an operand, 8 (r / 4) + r % 4 + ..., lie in different banks.  K by component as in
-        // rows d: piece u, 8 tokens, at u ^ (2 (d / 8 mod 4) + (d / 2 mod 2)) ^ (d / 32 mod 2), its two halves exchanged where d / 64 is odd: the lanes of a read have d = 8 (r / 4) +
-        // r % 4 + ..., those of a write d / 8 from 0 to 15.
-        const auto row_piece = [&](uint32_t row, uint32_t u) __attribute__((always_inline)) {
-            return kRow == 128 ? row * 256 + ((u ^ (row & 3) ^ (row >> 3 & 3) * 4) * 16) : row * 128 + ((u ^ (row >> 1 & 1) ^ (row >> 3 & 3) * 2) * 16);
+        const auto have_matrices = [&](Matrices &to) __attribute__((always_inline)) {
+            __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0)
+            if (tid < 2 * kChunk) to.d[tid] = decays;
         };
-        const uint32_t own_kt = ((r >> 2) * 8 + (r & 3)) * 128 + (g ^ (r >> 1)) * 16;
-        const auto kt_tile = [&](int a, int t, int s) __attribute__((always_inline)) {   // components of tile t, tokens 32 s + 8 g .. + 7
-            const u32x4 w = *(const u32x4 *)((const char *)lds_kt[a] + (own_kt ^ (s * 64) ^ (t / 2 % 2 * 16)) + (t / 2) * 32 * 128 + (t % 2) * 4 * 128);
-            return t / 4 % 2 ? (u32x4){w[2], w[3], w[0], w[1]} : w;
-        };
-        // Rows of tile (s, t) = (tile / 2, tile % 2), 32 s + 4 t behind the lane's own: pieces there are exchanged by the same bits.
-        const uint32_t own_rows = row_piece(8 * (r >> 2) + (r & 3), g);
-        const auto operand = [&](const uint16_t *plane, int tile, int p) __attribute__((always_inline)) {
-            return *(const u32x4 *)((const char *)plane + (own_rows ^ (p * 64)) + ((tile / 2) * 32 + (tile % 2) * 4) * 2 * kRow);
-        };
-        if (begin < end) load_chunk(begin, number);
-        // The first chunk's loads are waited for here: with any of them under way at the loop's head, the compiler's wait there would be for all that the wave has
-        // issued, the stores of the chunk before among them.
-        __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0)
-        for (uint32_t t0 = begin; t0 < end; t0 += kChunk, ++number) {
-            const uint32_t m = min(kChunk, end - t0);
+        const auto write_chunk = [&](Stage &to_stage) __attribute__((always_inline)) {
 #pragma unroll
             for (int b = 0; b < kPer; ++b) {
                 const Part p = part_of(b);
@@ -574,12 +614,12 @@ template <int KD, typename T, bool kStates> __global__ __launch_bounds__(64 * kD
                                 input_terms<T, kIn>(staged[b][j][i], terms);
                                 w[j][i] = terms[a];
                             }
-                        char *const to = p.is_q ? (char *)lds_q[a] : (char *)lds_k[a];
+                        char *const to = p.is_q ? (char *)to_stage.q[a] : (char *)to_stage.k[a];
 #pragma unroll
                         for (int j = 0; j < 4; ++j) *(u32x4 *)(to + row_piece(p.row + j, p.piece)) = (u32x4){w[j][0], w[j][1], w[j][2], w[j][3]};
                         if (!p.is_q) {
                             const uint32_t place = p.row / 8 ^ (p.piece & 3) * 2 ^ (p.piece / 4 & 1), half = (p.row / 4 & 1) ^ (p.piece / 8 & 1);
-                            char *const kt = (char *)lds_kt[a] + p.piece * 8 * 128 + half * 8;
+                            char *const kt = (char *)to_stage.kt[a] + p.piece * 8 * 128 + half * 8;
 #pragma unroll
                             for (int c = 0; c < 8; ++c) {   // component c of the four tokens
                                 const uint32_t sel = c % 2 ? 0x07060302u : 0x05040100u;
@@ -589,20 +629,103 @@ template <int KD, typename T, bool kStates> __global__ __launch_bounds__(64 * kD
                     }
                 }
             }
+        };
+        if (kApart && threadIdx.x >= 64 * NW) {
+            if (begin < end) {
+                bring_matrices(number, made[0]);
+                load_chunk(begin);
+                write_chunk(stages[0]);
+                if (begin + kChunk < end) load_chunk(begin + kChunk);
+                have_matrices(made[0]);
+            }
+            lds_barrier();
+            uint32_t next = 1;
+            for (uint32_t t0 = begin; t0 < end; t0 += kChunk) {
+                const bool more = end - t0 > kChunk;
+                if (more) bring_matrices(++number, made[next]);
+                if constexpr (kStages == 1) lds_barrier();
+                if (more) {
+                    write_chunk(stages[kStages == 1 ? 0 : next]);
+                    if (end - t0 > 2 * kChunk) load_chunk(t0 + 2 * kChunk);
+                    have_matrices(made[next]);
+                }
+                lds_barrier();
+                next ^= 1;
+            }
+            continue;
+        }
+        f32x4 S[2 * KD];
+        const float *const from = kStates ? nullptr : at.blocks > 1 ? block_state : P.state_in && state != ~0ull ? P.state_in + state_at : nullptr;
+        // (through a buffer of the state's size: rows and columns that are not there read 0 and are not written, without a branch for each)
+        const auto state_rows = [&](const float *base, uint32_t stride) __attribute__((always_inline)) {
+            return make_rsrc((const void *)uniform64((uint64_t)base), uniform(base ? P.dk * stride * 4 : 0u));
+        };
+        const uint32_t from_stride = at.blocks > 1 ? P.dv + P.dk : P.dv;
+        const auto from_rows = state_rows(from, from_stride);
 #pragma unroll
-            for (int b = 0; b < kMatrixPer; ++b)
-                if (b * 64 * NW + wave * 64 < kMatrix) lds_m[b * 64 * NW + tid] = matrices[b];
-            if (tid < 2 * kChunk) lds_d[tid] = decays;
+        for (int i = 0; i < 2 * KD; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t d = (i / 2) * 32 + g * 8 + (i % 2) * 4 + e;
+                if constexpr (kStates) S[i][e] = column == P.dv + d ? 1.f : 0.f;
+                else S[i][e] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(from_rows, live_column ? (d * from_stride + column) * 4 : kNowhere, 0, 0));
+            }
+        uint32_t values[2][4];
+        const auto load_values = [&](uint32_t t0) __attribute__((always_inline)) {
+            const uint32_t m = min(kChunk, end - t0);
+            const uint32_t stride = 2 * (uint32_t)P.v_stride, off = (anew(g) * 8 + (odd_lane ? 4 : 0)) * stride;
+            const auto rows = chunk_rows((const T *)P.v + (uint64_t)h * P.dv + t0 * P.v_stride, m, stride, 2 * P.dv);
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) values[s][j] = __builtin_amdgcn_raw_buffer_load_b32(rows, off + (s * 32 + j) * stride + column2, 0, 0);
+        };
+#pragma unroll
+        for (int i = 0; i < 8; ++i) values[i / 4][i % 4] = 0;
+        if (begin < end) {
+            if constexpr (!kApart) bring_matrices(number, made[0]), load_chunk(begin);
+            load_values(begin);
+            if constexpr (!kApart) write_chunk(stages[0]), have_matrices(made[0]);
+        }
+        // The state and the first chunk's values are waited for here: with any of them under way at the loop's head, the compiler's wait there would be for all that the wave has
+        // issued, the stores of the chunk before among them.
+#pragma unroll
+        for (int i = 0; i < 2 * KD; ++i) asm volatile("" : "+v"(S[i]));
+#pragma unroll
+        for (int i = 0; i < 8; ++i) asm volatile("" : "+v"(values[i / 4][i % 4]));
+        lds_barrier();
+        uint32_t stage = 0;
+        for (uint32_t t0 = begin; t0 < end; t0 += kChunk) {
+            const uint32_t m = min(kChunk, end - t0);
+            const Stage &now = stages[kStages == 1 ? 0 : stage];
+            const Matrices &matrices = made[stage];
+            const auto kt_tile = [&](int a, int t, int s) __attribute__((always_inline)) {   // components of tile t, tokens 32 s + 8 g .. + 7
+                const u32x4 w = *(const u32x4 *)((const char *)now.kt[a] + (own_kt ^ (s * 64) ^ (t / 2 % 2 * 16)) + (t / 2) * 32 * 128 + (t % 2) * 4 * 128);
+                return t / 4 % 2 ? (u32x4){w[2], w[3], w[0], w[1]} : w;
+            };
+            const auto operand = [&](const uint16_t *plane, int tile, int p) __attribute__((always_inline)) {
+                return *(const u32x4 *)((const char *)plane + (own_rows ^ (p * 64)) + ((tile / 2) * 32 + (tile % 2) * 4) * 2 * kRow);
+            };
             // values: tokens 32 s + 8 g + 2 i, + 1 of the lane's columns
             u32x4 V[2];
 #pragma unroll
             for (int s = 0; s < 2; ++s) V[s] = own_column(values[s], odd_lane);
-            __syncthreads();
-            if (t0 + kChunk < end) load_chunk(t0 + kChunk, number + 1);
-            if (live_wave) {
+            const bool more = t0 + kChunk < end;
+            if (more) {
+                if constexpr (!kApart) bring_matrices(++number, made[stage ^ 1]), load_chunk(t0 + kChunk);
+                load_values(t0 + kChunk);
+            }
+            const auto bring = [&] __attribute__((always_inline)) {   // the next chunk, where it does not take this one's place
+                __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0): loads that have been under way since the chunk's beginning, those into LDS too
+                if (kApart || !more) return;
+                have_matrices(made[stage ^ 1]);
+                if constexpr (kStages == 2) write_chunk(stages[stage ^ 1]);
+            };
+            if (!live_wave) bring();
+            else {
                 const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
                 f32x4 O[4], R[4], U[4];
-                constexpr bool kAhead = KD == 2;
+                constexpr bool kAhead = true;
                 u32x4 A[kAhead ? 2 : 1][4], B[2][3];
                 // The products of a chunk in steps of up to four rows of operands: K S and Q S by 32 components and term of the inputs; then E R by its terms and M R by its, for the tokens
                 // 32 s .. 32 s + 31; then K^T E R.  kAhead: a step's loads from LDS are under way while the step before is multiplied, and nothing is moved from step to step (up to 64 components:
@@ -615,16 +738,29 @@ template <int KD, typename T, bool kStates> __global__ __launch_bounds__(64 * kD
                     if constexpr (k < kState) {
                         constexpr int p = k / (kOfS * kIn), a = k / kOfS % kIn;
 #pragma unroll
-                        for (int tile = 0; tile < 4; ++tile) to[tile] = operand(k % kOfS ? &lds_q[a][0][0] : &lds_k[a][0][0], tile, p);
+                        for (int tile = 0; tile < 4; ++tile) to[tile] = operand(k % kOfS ? &now.q[a][0][0] : &now.k[a][0][0], tile, p);
                     } else if constexpr (k < kSystem) {
                         constexpr int s = (k - kState) / kOfR, a = (k - kState) % kOfR, first = s == 0 ? 0 : 4, last = s == 0 ? 4 : 6;
 #pragma unroll
-                        for (int f = first; f < last; ++f) to[f - first] = lds_m[(a < kTermsE ? f * kTermsE + a : kOperands * kTermsE + f * kTermsM + a - kTermsE) * 64 + lane];
+                        for (int f = first; f < last; ++f) to[f - first] = matrices.m[(a < kTermsE ? f * kTermsE + a : kOperands * kTermsE + f * kTermsM + a - kTermsE) * 64 + lane];
                     } else if constexpr (k < kSteps) {
                         constexpr int a = (k - kSystem) % kIn, each = kUpdate / 2, s = (k - kSystem) / each, first = (k - kSystem) % each / kIn * 4;
 #pragma unroll
                         for (int i = 0; i < 4 && first + i < 2 * KD; ++i) to[i] = kt_tile(a, first + i, s);
                     }
+                };
+                const auto decay_of = [&](int which, int tile) __attribute__((always_inline)) { return *(const f32x4 *)&matrices.d[which * kChunk + (tile / 2) * 32 + g * 8 + (tile % 2) * 4]; };
+                const float decay = matrices.d[kChunk - 1];
+                T *const out = (T *)P.out + ((uint64_t)t0 * P.heads + h) * P.dv;
+                const uint32_t out_stride = 2 * P.heads * P.dv;
+                const auto out_rows = chunk_rows(out, m, out_stride, 2 * P.dv);
+                const auto store = [&](int tile) __attribute__((always_inline)) {   // tokens 0, 1 of a tile's four are the even lane's, 2, 3 the odd one's, both columns of each
+                    const uint32_t a = pack2<T>(O[tile][0], O[tile][1]), b = pack2<T>(O[tile][2], O[tile][3]);   // own column
+                    const uint32_t got = of_neighbour(odd_lane ? a : b), mine = odd_lane ? b : a;              // the lane's two tokens, the other column and this one
+                    const uint32_t left = odd_lane ? got : mine, right = odd_lane ? mine : got;
+                    const uint32_t off = (anew(g) * 8 + (odd_lane ? 2 : 0)) * out_stride + column2 + ((tile / 2) * 32 + (tile % 2) * 4) * out_stride;
+                    __builtin_amdgcn_raw_buffer_store_b32(__builtin_amdgcn_perm(right, left, 0x05040100u), out_rows, off, 0, 0);
+                    __builtin_amdgcn_raw_buffer_store_b32(__builtin_amdgcn_perm(right, left, 0x07060302u), out_rows, off + out_stride, 0, 0);
                 };
                 const auto step = [&](auto number) __attribute__((always_inline)) {
                     constexpr int k = decltype(number)::value;
@@ -638,7 +774,10 @@ template <int KD, typename T, bool kStates> __global__ __launch_bounds__(64 * kD
                         for (int c = 0; c < terms; ++c)
 #pragma unroll
                             for (int tile = 0; tile < 4; ++tile) to[tile] = mfma_bf16(from[tile], B[p % 2][c], p == 0 && a == 0 && c == 0 ? zero : to[tile]);
-                        if constexpr (k % (kOfS * kIn) == kOfS - 1 && p + 1 < KD) three_terms({S[2 * p + 2], S[2 * p + 3]}, B[(p + 1) % 2]);
+                        if constexpr (p + 1 < KD) {   // the next components' state
+                            if constexpr (k % (kOfS * kIn) == 0) half_terms<0>(S[2 * p + 2], B[(p + 1) % 2]);
+                            if constexpr (k % (kOfS * kIn) == kOfS * kIn - 1) half_terms<1>(S[2 * p + 3], B[(p + 1) % 2]);
+                        }
                     } else if constexpr (k < kSystem) {
                         constexpr int s = (k - kState) / kOfR, a = (k - kState) % kOfR, first = s == 0 ? 0 : 4, last = s == 0 ? 4 : 6;   // operands; the tile of one behind the fourth is two before it
                         constexpr int terms = a < kTermsE ? kTermsE - a : kTermsM - (a - kTermsE);
@@ -651,13 +790,26 @@ template <int KD, typename T, bool kStates> __global__ __launch_bounds__(64 * kD
                                 else O[tile] = mfma_bf16(from[f - first], B[s][c], O[tile]);
                             }
                         if constexpr (s == 0 && a == 0) three_terms({R[2], R[3]}, B[1]);
+                        if constexpr (!kStates && s == 0 && a == 1) {
+#pragma unroll
+                            for (int tile = 0; tile < 4; ++tile) O[tile] *= decay_of(1, tile);
+                        }
                     } else {
                         constexpr int a = (k - kSystem) % kIn, each = kUpdate / 2, s = (k - kSystem) / each, first = (k - kSystem) % each / kIn * 4;
 #pragma unroll
                         for (int c = 0; c + a < 3; ++c)
 #pragma unroll
                             for (int i = 0; i < 4 && first + i < 2 * KD; ++i) S[first + i] = mfma_bf16(from[i], B[s][c], S[first + i]);
-                        if constexpr (s == 0 && (k - kSystem) % each == 0) three_terms({U[2], U[3]}, B[1]);
+                        if constexpr (s == 0 && first == 0 && a == 0) three_terms({U[2], U[3]}, B[1]);
+                        if constexpr (s == 0 && a == 0) {   // the next four rows' state
+#pragma unroll
+                            for (int i = first + 4; i < first + 8 && i < 2 * KD; ++i) S[i] *= decay;
+                        }
+                        if constexpr (!kStates) {
+#pragma unroll
+                            for (int tile = 0; tile < 4; ++tile)
+                                if (tile * kUpdate / 4 == k - kSystem) store(tile);
+                        }
                     }
                     if constexpr (kAhead) __builtin_amdgcn_sched_barrier(0);
                 };
@@ -665,11 +817,9 @@ template <int KD, typename T, bool kStates> __global__ __launch_bounds__(64 * kD
                 if constexpr (kAhead) fetch(Number<0>());
                 in_order<0, kState>(step);
                 // R, from the values
-                const auto decay_of = [&](int which, int tile) __attribute__((always_inline)) { return *(const f32x4 *)&lds_d[which * kChunk + (tile / 2) * 32 + g * 8 + (tile % 2) * 4]; };
 #pragma unroll
                 for (int tile = 0; tile < 4; ++tile) {
                     const f32x4 by = decay_of(0, tile);
-                    if (!kStates) O[tile] *= decay_of(1, tile);
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
                         const uint32_t w = V[tile / 2][tile % 2 * 2 + i];   // (of an element of a vector itself, a bit cast takes the first)
@@ -686,33 +836,17 @@ template <int KD, typename T, bool kStates> __global__ __launch_bounds__(64 * kD
                 }
                 three_terms({R[0], R[1]}, B[0]);
                 in_order<kState, kSystem>(step);
+                bring();
                 float odd = 0.f;   // NaN if anything that is written is not finite
 #pragma unroll
                 for (int tile = 0; tile < 4; ++tile)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) odd = __builtin_fmaf(U[tile][e], 0.f, odd);
-                T *const out = (T *)P.out + ((uint64_t)t0 * P.heads + h) * P.dv;
                 if (kStates || !__any(odd != 0.f)) {   // (what is not finite leaves no finite state)
-                    const float decay = lds_d[kChunk - 1];
 #pragma unroll
-                    for (int i = 0; i < 2 * KD; ++i) S[i] *= decay;
+                    for (int i = 0; i < 4 && i < 2 * KD; ++i) S[i] *= decay;
                     three_terms({U[0], U[1]}, B[0]);
                     in_order<kSystem, kSteps>(step);
-                    __builtin_amdgcn_s_waitcnt(0x0F70);   // (the next chunk's loads, under way all this time: waited for behind the stores they would be waited for with those)
-                    if constexpr (!kStates) {   // tokens 0, 1 of a tile's four are the even lane's, 2, 3 the odd one's, both columns of each
-                        const uint32_t stride = 2 * P.heads * P.dv;
-                        const uint32_t own = (anew(g) * 8 + (odd_lane ? 2 : 0)) * stride + column2;
-                        const auto rows = chunk_rows(out, m, stride, 2 * P.dv);
-#pragma unroll
-                        for (int tile = 0; tile < 4; ++tile) {
-                            const uint32_t a = pack2<T>(O[tile][0], O[tile][1]), b = pack2<T>(O[tile][2], O[tile][3]);   // own column
-                            const uint32_t got = of_neighbour(odd_lane ? a : b), mine = odd_lane ? b : a;              // the lane's two tokens, the other column and this one
-                            const uint32_t left = odd_lane ? got : mine, right = odd_lane ? mine : got;
-                            const uint32_t off = own + ((tile / 2) * 32 + (tile % 2) * 4) * stride;
-                            __builtin_amdgcn_raw_buffer_store_b32(__builtin_amdgcn_perm(right, left, 0x05040100u), rows, off, 0, 0);
-                            __builtin_amdgcn_raw_buffer_store_b32(__builtin_amdgcn_perm(right, left, 0x07060302u), rows, off + stride, 0, 0);
-                        }
-                    }
                 } else if constexpr (!kStates) {   // token by token: what is not finite must not meet the zeros of earlier ones
                     for (uint32_t j = 0; j < m; ++j) {
                         const uint64_t at_token = (uint64_t)(t0 + j) * P.heads + h;
@@ -731,7 +865,7 @@ template <int KD, typename T, bool kStates> __global__ __launch_bounds__(64 * kD
                             for (int c = 0; c < 8; ++c) {
                                 float &x = ((float *)&S[2 * p + c / 4])[c % 4];
                                 x *= by;
-                                if (p * 32 + g * 8 < P.dk) y += component(lds_k, p, c) * x;
+                                if (p * 32 + g * 8 < P.dk) y += component(now.k, p, c) * x;
                             }
                         y += __shfl_xor(y, 16);
                         y += __shfl_xor(y, 32);
@@ -742,8 +876,8 @@ template <int KD, typename T, bool kStates> __global__ __launch_bounds__(64 * kD
                             for (int c = 0; c < 8; ++c)
                                 if (p * 32 + g * 8 < P.dk) {
                                     float &x = ((float *)&S[2 * p + c / 4])[c % 4];
-                                    x += component(lds_k, p, c) * u;
-                                    o += component(lds_q, p, c) * x;
+                                    x += component(now.k, p, c) * u;
+                                    o += component(now.q, p, c) * x;
                                 }
                         o += __shfl_xor(o, 16);
                         o += __shfl_xor(o, 32);
@@ -751,18 +885,24 @@ template <int KD, typename T, bool kStates> __global__ __launch_bounds__(64 * kD
                     }
                 }
             }
-            __syncthreads();   // (keys, queries and matrices are free)
+            lds_barrier();   // (keys, queries and matrices are free)
+            if constexpr (kStages == 1) {
+                if (!kApart && more) write_chunk(stages[0]);
+                lds_barrier();
+            }
+            stage ^= 1;
         }
         float *const to = kStates ? block_state : at.block + 1 == at.blocks && P.state_out && state != ~0ull ? P.state_out + state_at : nullptr;
         const uint32_t to_stride = kStates ? P.dv + P.dk : P.dv;
-        if (to && live_column)
+        const auto to_rows = state_rows(to, to_stride);
 #pragma unroll
-            for (int i = 0; i < 2 * KD; ++i)
+        for (int i = 0; i < 2 * KD; ++i)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const uint32_t d = (i / 2) * 32 + g * 8 + (i % 2) * 4 + e;
-                    if (d < P.dk) to[(uint64_t)d * to_stride + column] = S[i][e];
-                }
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t d = (i / 2) * 32 + g * 8 + (i % 2) * 4 + e;
+                const float x = S[i][e];   // (of an element of a vector itself, a bit cast takes the first)
+                __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, x), to_rows, live_column ? (d * to_stride + column) * 4 : kNowhere, 0, 0);
+            }
     }
 }
 

@@ -6,8 +6,8 @@
 #include "mmvseg.h"
 
 #include "values.h"
-#include "delta.h"
 #include "call_checks.h"
+#include "delta.h"
 #include "delta_host.h"
 
 extern "C" {

@@ -47,9 +47,8 @@ mmv_status delta_step_call(const DeltaParams &P, int type, hipStream_t s) { retu
 
 // Chunks that the requests can have together, and blocks of a head that the device has at once (two workgroups on a compute unit).
 inline uint64_t delta_chunks(uint64_t n, uint64_t tokens) { return tokens / kChunk + (n < tokens ? n : tokens); }
-inline uint32_t delta_slices(uint32_t columns) { return (columns + 16 * kDeltaWaves - 1) / (16 * kDeltaWaves); }
 // States of blocks: a request of more than one block fills more than half of its own, and a block is as large as the plan on the device makes it, or kLeastBlock.  0: never taken apart.
-inline uint32_t delta_round(uint32_t heads, uint32_t dv) { return 2 * kUnits / (heads * delta_slices(dv)); }
+inline uint32_t delta_round(uint32_t heads, uint32_t dv) { return kUnits / (heads * delta_slices(dv, 4)); }
 inline uint64_t delta_slots(uint64_t n, uint64_t tokens, uint32_t heads, uint32_t dv) {
     const uint64_t chunks = delta_chunks(n, tokens), round = delta_round(heads, dv), most = 2 * round;
     const uint64_t longest = ceil_div(tokens, kChunk);
@@ -69,20 +68,22 @@ template <typename T> mmv_status launch_chunks(DeltaPromptParams P, hipStream_t 
     return MMV_OK;
 }
 // Workgroups go on to the next block by themselves: where nothing is taken apart, the launches for that are of as many as the device holds.
+constexpr uint32_t kFilledTwice = 2 * kUnits;
 constexpr uint64_t kMostWorkgroups = 1u << 22;
-template <int KD, typename T> mmv_status launch_delta_prompts(const DeltaPromptParams &P, hipStream_t s) {
+template <int KD, typename T, int kCompute> mmv_status launch_delta_prompts(const DeltaPromptParams &P, hipStream_t s) {
     if (P.block_states) {
-        const uint32_t slices = delta_slices(P.d.dv + P.d.dk);
-        delta_prompt_kernel<KD, T, true><<<4 * kUnits, 64 * kDeltaWaves, 0, s>>>(P, slices);
+        delta_prompt_kernel<KD, T, true, kCompute><<<4 * kUnits, 512, 0, s>>>(P);
         if (const mmv_status st = launched()) return st;
         delta_states_kernel<KD><<<4 * kUnits, 64 * KD, 0, s>>>(P);
         if (const mmv_status st = launched()) return st;
     }
-    const uint32_t slices = delta_slices(P.d.dv);
-    uint64_t blocks = (uint64_t)P.d.n * P.d.heads * slices;
+    uint64_t blocks = (uint64_t)P.d.n * P.d.heads * delta_slices(P.d.dv, kCompute);
     if (P.block_states && blocks < 4 * kUnits) blocks = 4 * kUnits;
-    delta_prompt_kernel<KD, T, false><<<(unsigned)(blocks < kMostWorkgroups ? blocks : kMostWorkgroups), 64 * kDeltaWaves, 0, s>>>(P, slices);
+    delta_prompt_kernel<KD, T, false, kCompute><<<(unsigned)(blocks < kMostWorkgroups ? blocks : kMostWorkgroups), 512, 0, s>>>(P);
     return launched();
+}
+template <int KD, typename T> mmv_status launch_delta_prompts(const DeltaPromptParams &P, hipStream_t s) {
+    return P.d.n * P.d.heads * delta_slices(P.d.dv, 8) >= kFilledTwice && P.d.dv > 64 ? launch_delta_prompts<KD, T, 8>(P, s) : launch_delta_prompts<KD, T, 4>(P, s);
 }
 template <typename T> mmv_status delta_prompts(const DeltaPromptParams &P, hipStream_t s) {
     if (const mmv_status st = launch_chunks<T>(P, s)) return st;
