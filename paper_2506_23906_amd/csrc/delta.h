@@ -181,12 +181,13 @@ __device__ __forceinline__ ChunkPlace find_chunk(const DeltaParams &P, uint32_t 
 
 // Requests in blocks.  Chunks of a request depend on each other through the state.  Where few long requests would leave the device idle they are taken apart into blocks of as many chunks: what a
 // block makes of a state, S -> A S + B, is found for all blocks at once (A from the columns of the identity, B from a state of zeros), then the state before each block, then all blocks' outputs.
-// That is 2.3 times the work and two more launches, so it is done where the longest request has more than 13 / 4 of an even share of the chunks and ten more, 16 at least (a call that cannot have so many is not charged with the two launches): us of a call, whole / in blocks, where
-// the longest of the requests has as many chunks and as many times an even share (16 heads of 128 x 128; 8 of 64 x 64 and 4 of 128 x 256 change sides at the same places):
-//   16 chunks, 6 times 99 / 105, 12 times 95 / 85;   32, 4 times 193 / 205, 6 times 183 / 170;   64, 3 times 453 / 525, 4 times 391 / 348;   128, 3 times 874 / 947, 4 times 769 / 638
-// Blocks have four chunks at least: 16 chunks, 12 times: 2 93, 4 85, 8 97 us; and as many as fill the device once: filled 3, 2, 1 times, one of 32768 tokens 843, 773, 709 us.
-constexpr uint32_t kLeastBlock = 4, kLeastApart = 16, kApartFixed = 10, kApartQuarters = 13;
-__host__ __device__ constexpr bool worth_taking_apart(uint64_t most, uint64_t all, uint32_t round) { return most >= kLeastApart && 4 * (most - kApartFixed) * round > kApartQuarters * all; }
+// That is 2.3 times the work and two more launches, so it is done where the longest request has more than three times an even share of the chunks and twelve more, 16 at least (a call that cannot
+// have so many is not charged with the two launches): us of a call, whole / in blocks, where the longest of the requests has as many chunks and as many times an even share (16 heads of 128 x 128;
+// 8 of 64 x 64 and 4 of 128 x 256 change sides at the same places):
+//   16 chunks, 8 times 64 / 74;   24, 6 times 90 / 101, 12 times (4 heads) 88 / 79;   32, 4 times 118 / 134, 8 times 114 / 107;   64, 3 times 238 / 271, 4 times 224 / 205;   128, 3 times 457 / 491, 4 times 429 / 373
+// Blocks have four chunks at least, and are as many as fill the device once (filled once, twice, three times: one of 32768 tokens 687, 743, 803 us; 45000 tokens of eight requests 991, 912, 973).
+constexpr uint32_t kLeastBlock = 4, kLeastApart = 16, kApartFixed = 12, kApartShare = 3;
+__host__ __device__ constexpr bool worth_taking_apart(uint64_t most, uint64_t all, uint32_t round) { return most >= kLeastApart && (most - kApartFixed) * round > kApartShare * all; }
 constexpr uint32_t kMostOrdered = 256;
 struct BlockPlan {
     uint32_t chunks, blocks;   // chunks of a block (~0: all of a request), blocks in all

@@ -259,3 +259,43 @@ def test_streams_views_and_marshalling(monkeypatch):
                       lambda: B.mmv_delta_attention(*views, ends, ldg, bg, state_in=state, state_out=state, out=out[:5])):
             with pytest.raises(B.MmvError):
                 wrong()
+
+
+LENGTHS = [(37 * i * i + 11 * i) % 110 for i in range(64)]
+
+
+@pytest.mark.parametrize("heads,group,dk,dv,dtype", [(8, 2, 64, 128, BF16), (8, 1, 128, 128, BF16), (8, 4, 96, 256, F16), (8, 2, 128, 128, F16), (8, 8, 80, 112, BF16)])
+def test_requests_that_fill_the_device(heads, group, dk, dv, dtype):
+    """Workgroups of 128 columns; and with one request that is taken apart among them."""
+    run_delta(LENGTHS, heads, group, dk, dv, dtype, seed=21, states="in place")
+    run_delta(LENGTHS[:40] + [2600] + LENGTHS[40:], heads, group, dk, dv, dtype, seed=22, before=5)
+
+
+@pytest.mark.parametrize("n", [24, 64, 65, 255, 256, 257])
+def test_the_longest_requests_come_first(n):
+    """In every order of lengths: all of them are done, and none twice (states that are updated in place)."""
+    for lengths in ([i % 71 for i in range(n)], [70 - i % 71 for i in range(n)], [7] * n, [0] * (n - 1) + [200], [65, 64] * (n // 2) + [0] * (n % 2)):
+        run_delta(lengths, 12, 2, 16, 24, BF16, seed=23, states="in place")
+
+
+@pytest.mark.parametrize("dk,dtype", [(64, BF16), (128, BF16), (128, F16)])
+def test_what_is_not_finite_where_requests_fill_the_device(dk, dtype):
+    heads, dv, n = 8, 128, 64
+    lengths, tokens = [150] * n, 150 * n
+    q, k, v = inputs(31, tokens, heads, 2, dk, dv, dtype)
+    ld, beta = gates(32, tokens, heads, "spread")
+    ends = ints([150 * i for i in range(n + 1)])
+    args = (q.cuda(), k.cuda()), (ends, ld.cuda(), beta.cuda())
+    whole = B.mmv_delta_attention(*args[0], v.cuda(), *args[1]).cpu()
+    at, head, column = 150 * 20 + 70, 3, 77
+    v[at, head, column] = math.inf
+    got = B.mmv_delta_attention(*args[0], v.cuda(), *args[1]).cpu()
+    rest = torch.ones(got.shape, dtype=torch.bool)
+    rest[150 * 20:150 * 21, head] = False
+    assert torch.equal(got[rest], whole[rest])
+    own = slice(150 * 20, 150 * 21)
+    want, _, by, _ = plain_delta(q[own], k[own], v[own], [0, 150], ld[own], beta[own], dk ** -0.5)
+    fine = want.isfinite()
+    assert torch.equal(fine, got[own].isfinite()) and not bool(fine[70:, head, column].any())
+    keep = fine & by.isfinite()
+    check(got[own][keep], want[keep], by[keep], "out")

@@ -64,11 +64,12 @@ WHOLE, LIST, JOIN = "whole_attention_kernel", "paged_attention_kernel", "join_at
     ("read((1 << 31) - 1)", [(READ, (1 << 24) - 1, 256)] * 32 + [(READ, 32, 256)]),
     ("attention(3, 1)", [(WHOLE, 24, 64)]), ("attention(3, 16)", [(WHOLE, 24, 512)]), ("attention(3, 17)", [(LIST, 102, 256), (JOIN, 96, 256)]), ("attention(0, 1)", []),
     # chunks, then requests; where long ones may be taken apart, two launches for that, and as many workgroups as the device holds
-    ("delta(3, 900)", [(CHUNKS, 136, 256), (PROMPT, 24, 256)]), ("delta(3, 0)", [(PROMPT, 24, 256)]), ("delta(0, 100)", []), ("delta(3, 960)", [(CHUNKS, 144, 256), (PROMPT, 24, 256)]),
-    ("delta(3, 961)", [(CHUNKS, 144, 256), (PROMPT, 1024, 256), (STATES, 1024, 128), (PROMPT, 1024, 256)]),
-    ("delta(700, 9000, dk=128, dv=256, type=1)", [(CHUNKS, 6720, 256), (PROMPT, 1024, 256), (STATES, 1024, 256), (PROMPT, 22400, 256)]),
-    ("delta(3, 9000, heads=64, dk=96, dv=128)", [(CHUNKS, 9152, 256), (PROMPT, 1024, 256), (STATES, 1024, 192), (PROMPT, 1024, 256)]),
-    ("delta(3, 9000, heads=128, dk=96, dv=128)", [(CHUNKS, 18304, 256), (PROMPT, 768, 256)]),   # (two of a head at once: nothing to gain)
+    ("delta(3, 900)", [(CHUNKS, 136, 256), (PROMPT, 24, 512)]), ("delta(3, 0)", [(PROMPT, 24, 512)]), ("delta(0, 100)", []), ("delta(3, 960)", [(CHUNKS, 144, 256), (PROMPT, 24, 512)]),
+    ("delta(3, 961)", [(CHUNKS, 144, 256), (PROMPT, 1024, 512), (STATES, 1024, 128), (PROMPT, 1024, 512)]),
+    ("delta(700, 9000, dk=128, dv=256, type=1)", [(CHUNKS, 6720, 256), (PROMPT, 1024, 512), (STATES, 1024, 256), (PROMPT, 11200, 512)]),   # (128 columns to a workgroup)
+    ("delta(3, 9000, heads=32, dk=96, dv=128)", [(CHUNKS, 4576, 256), (PROMPT, 1024, 512), (STATES, 1024, 192), (PROMPT, 1024, 512)]),
+    ("delta(3, 9000, heads=64, dk=96, dv=128)", [(CHUNKS, 9152, 256), (PROMPT, 384, 512)]),   # (two of a head at once: nothing to gain)
+    ("delta(63, 100, heads=8, dv=128)", [(CHUNKS, 512, 256), (PROMPT, 1008, 512)]), ("delta(64, 100, heads=8, dv=128)", [(CHUNKS, 520, 256), (PROMPT, 512, 512)]),   # the device filled twice
     ("step(5)", [(STEP, 40, 256)]), ("step(5, dv=256)", [(STEP, 40, 512)]),
 ])
 def test_launches(record, call, want):
