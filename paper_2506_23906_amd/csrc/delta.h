@@ -121,7 +121,7 @@ template <typename T, int kRows, int kThreads> __global__ __launch_bounds__(kThr
 //   E = diag(e^(G_63 - G)) T,   M = W T.
 // delta_prompt_kernel then goes through a request's chunks: R = V - diag(e^G) K S, out = scale diag(e^G) Q S + M R, S' = e^(G_63) S + K^T E R.
 constexpr uint32_t kChunk = 64;
-// Workgroups go to the eight dies in turn, and each has a cache of its own: of `each` (the heads of a chunk; of a request, with their slices of columns), neighbours, which read the same, to one.
+// Workgroups go to the eight dies in turn, and each has a cache of its own: of `each` (the heads of a chunk; of a request, with their slices of columns), neighbours, which read the same, to one (64 prompts of 1024 tokens, 16 heads: 755 us, so 711).
 __device__ __forceinline__ uint32_t by_die(uint32_t i, uint32_t each) { return each % 8 ? i : (i & 7) * (each / 8) + i / 8; }
 
 // What a chunk of a head leaves: matrices as operands of 16x16x32 products, 1 KB (64 lanes of 16 bytes) each: rows 32 s + 8 (r / 4) + 4 t + r % 4 (s, t = 0, 1), columns 32 c + 8 g + 0..7 in
@@ -247,7 +247,7 @@ __device__ __forceinline__ BlockPlace find_block(const DeltaPromptParams &PP, ui
 }
 
 // The same where requests are whole and more than the device takes at once: the longest first, so that none of them begins when the others are done (24 requests of 64 to 4096 tokens, the longest
-// ones last: 380 us as they come, 290).  Up to 256 requests: a lane has four of them, and the length that a place in that order has is found by bisection.
+// ones last: 318 us as they come, 283).  Up to 256 requests: a lane has four of them, and the length that a place in that order has is found by bisection.
 __device__ __forceinline__ BlockPlace find_longest(const DeltaParams &P, uint32_t place) {
     const uint32_t lane = threadIdx.x & 63;
     uint32_t chunks[kMostOrdered / 64], most = 0;   // and one: 0 where there is no request
@@ -491,15 +491,18 @@ __device__ __forceinline__ u32x4 own_column(const uint32_t (&row)[4], bool odd) 
     return odd ? (u32x4){c, d, a, b} : (u32x4){a, b, c, d};
 }
 
-// A workgroup takes a request's chunks for one head and 16 NW columns, a wave 16 of them, whose state stays in its registers (fp32).
+// A workgroup takes a request's chunks for one head and 16 columns for each of kCompute waves, whose state stays in the wave's registers (fp32).
 // Layout (products 16x16x32, lane = 16 g + r): the lane has column r and, of a pair of result tiles, the rows 32 s + 8 g + 0..7 (operand rows are those of kOperands' comment): as B
 // of the next product those are its own, so the state goes into K S and Q S, R into M R and E R, and that into K^T E R, each from the registers where it is.
 // What is no 16-bit input meets the matrix cores as bf16 terms, each the upper half of what the ones before left, the last one rounded: three (fp32's 24 bits) of E, the state, R and E R on
 // their way to a state, two of the state, M and R on their way to an output, which is rounded to 16 bits: 2^-16 relative to the largest summand, beside bf16's 2^-8 and fp16's 2^-11 (rms errors of
 // fp16 outputs 2.082e-4, with a state in fp32 products 2.074e-4; of states 1.9e-7).  Inputs in fp16 are two terms each (exact).
-// Bound by matrix instructions and the waits between a chunk's three dependent products (24 prompts of 24000 tokens in all, 16 heads, 128 x 128, bf16: 386 us; a copy that only multiplies reaches
-// 906 TFLOP/s of terms, 74 % of what a large library product does).  Four waves, two workgroups on a compute unit: a workgroup of eight waves 448 us where four had 443, and one of 45000 tokens
-// in blocks 2197, so 1763; two groups of 16 columns to a wave, which halve the reads of LDS, need twice the registers and are slower.
+// A chunk is brought into LDS while the one before is computed: matrices straight from memory, keys and queries through registers (a second copy of keys lies by component), one barrier a chunk;
+// fp16 with more than 64 components has room for one chunk's keys only, and two barriers.  kCompute 4: four waves compute and four bring.  A chunk of 128 x 64 takes 7000 cycles, 2900 of them the
+// matrix instructions', the rest vector instructions (terms) and waits between the chunk's three dependent products: bound by that chain, a request after the other's end.  kCompute 8: all do both,
+// 128 columns, two waves to a vector unit fill each other's waits: 12600 cycles for twice the columns, so more in all but later for each.  launch_delta_prompts has the rule and both sides.
+// 24 prompts of 24000 tokens in all, 16 heads, 128 x 128, bf16: 238 us, where four waves that did everything in turn, two workgroups on a compute unit, took 386.  Two groups of 16 columns to a
+// wave, which halve the reads of LDS, need twice the registers and were slower; so was an order of matrix and vector instructions by hand (7500 cycles).
 // kStates: what blocks make of a state (columns dv and on: of the identity), without outputs.
 constexpr size_t kLdsBytes = 160 * 1024;
 template <int KD, int kIn, bool kStates> struct DeltaStage {   // what a chunk needs in LDS; planes of terms
@@ -512,7 +515,7 @@ template <int KD, typename T, bool kStates, int kCompute> __global__ __launch_bo
     constexpr int NW = kCompute, kIn = __is_same(T, f16_t) ? 2 : 1, kPieces = KD * 4;
     typedef DeltaStage<KD, kIn, kStates> Stage;
     constexpr uint32_t kRow = Stage::kRow;
-    constexpr bool kApart = kCompute < 8;   // four waves compute, four bring the chunks
+    constexpr bool kBringers = kCompute < 8;   // four waves compute, four bring the chunks
     struct Matrices {
         u32x4 m[Stage::kMatrix];
         float d[2 * kChunk];
@@ -631,7 +634,8 @@ template <int KD, typename T, bool kStates, int kCompute> __global__ __launch_bo
                 }
             }
         };
-        if (kApart && threadIdx.x >= 64 * NW) {
+        // (whole waves take either branch, and come by as many barriers in both: one before the first chunk, kStages == 1 ? 2 : 1 for each)
+        if (kBringers && threadIdx.x >= 64 * NW) {
             if (begin < end) {
                 bring_matrices(number, made[0]);
                 load_chunk(begin);
@@ -684,9 +688,9 @@ template <int KD, typename T, bool kStates, int kCompute> __global__ __launch_bo
 #pragma unroll
         for (int i = 0; i < 8; ++i) values[i / 4][i % 4] = 0;
         if (begin < end) {
-            if constexpr (!kApart) bring_matrices(number, made[0]), load_chunk(begin);
+            if constexpr (!kBringers) bring_matrices(number, made[0]), load_chunk(begin);
             load_values(begin);
-            if constexpr (!kApart) write_chunk(stages[0]), have_matrices(made[0]);
+            if constexpr (!kBringers) write_chunk(stages[0]), have_matrices(made[0]);
         }
         // The state and the first chunk's values are waited for here: with any of them under way at the loop's head, the compiler's wait there would be for all that the wave has
         // issued, the stores of the chunk before among them.
@@ -713,12 +717,12 @@ template <int KD, typename T, bool kStates, int kCompute> __global__ __launch_bo
             for (int s = 0; s < 2; ++s) V[s] = own_column(values[s], odd_lane);
             const bool more = t0 + kChunk < end;
             if (more) {
-                if constexpr (!kApart) bring_matrices(++number, made[stage ^ 1]), load_chunk(t0 + kChunk);
+                if constexpr (!kBringers) bring_matrices(++number, made[stage ^ 1]), load_chunk(t0 + kChunk);
                 load_values(t0 + kChunk);
             }
             const auto bring = [&] __attribute__((always_inline)) {   // the next chunk, where it does not take this one's place
                 __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0): loads that have been under way since the chunk's beginning, those into LDS too
-                if (kApart || !more) return;
+                if (kBringers || !more) return;
                 have_matrices(made[stage ^ 1]);
                 if constexpr (kStages == 2) write_chunk(stages[stage ^ 1]);
             };
@@ -726,16 +730,14 @@ template <int KD, typename T, bool kStates, int kCompute> __global__ __launch_bo
             else {
                 const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
                 f32x4 O[4], R[4], U[4];
-                constexpr bool kAhead = true;
-                u32x4 A[kAhead ? 2 : 1][4], B[2][3];
+                u32x4 A[2][4], B[2][3];
                 // The products of a chunk in steps of up to four rows of operands: K S and Q S by 32 components and term of the inputs; then E R by its terms and M R by its, for the tokens
-                // 32 s .. 32 s + 31; then K^T E R.  kAhead: a step's loads from LDS are under way while the step before is multiplied, and nothing is moved from step to step (up to 64 components:
-                // 3 prompts of 900 tokens 42 -> 39 us; with more there are no registers for it).
+                // 32 s .. 32 s + 31; then K^T E R.  A step's loads from LDS are under way while the step before is multiplied, and nothing is moved from step to step.
                 constexpr int kOfS = kStates ? 1 : 2, kOfR = kStates ? kTermsE : kTermsE + kTermsM;   // (states alone: without queries and M)
                 constexpr int kState = kOfS * kIn * KD, kSystem = kState + 2 * kOfR, kUpdate = 2 * ((2 * KD + 3) / 4) * kIn, kSteps = kSystem + kUpdate;
                 const auto fetch = [&](auto number) __attribute__((always_inline)) {
                     constexpr int k = decltype(number)::value;
-                    u32x4 (&to)[4] = A[kAhead ? k % 2 : 0];
+                    u32x4 (&to)[4] = A[k % 2];
                     if constexpr (k < kState) {
                         constexpr int p = k / (kOfS * kIn), a = k / kOfS % kIn;
 #pragma unroll
@@ -765,9 +767,8 @@ template <int KD, typename T, bool kStates, int kCompute> __global__ __launch_bo
                 };
                 const auto step = [&](auto number) __attribute__((always_inline)) {
                     constexpr int k = decltype(number)::value;
-                    if constexpr (kAhead) fetch(Number<k + 1>());
-                    else fetch(number);
-                    const u32x4 (&from)[4] = A[kAhead ? k % 2 : 0];
+                    fetch(Number<k + 1>());
+                    const u32x4 (&from)[4] = A[k % 2];
                     if constexpr (k < kState) {
                         constexpr int p = k / (kOfS * kIn), a = k / kOfS % kIn, terms = (k % kOfS ? 2 : 3) - a;
                         f32x4 (&to)[4] = k % kOfS ? O : R;
@@ -812,10 +813,10 @@ template <int KD, typename T, bool kStates, int kCompute> __global__ __launch_bo
                                 if (tile * kUpdate / 4 == k - kSystem) store(tile);
                         }
                     }
-                    if constexpr (kAhead) __builtin_amdgcn_sched_barrier(0);
+                    __builtin_amdgcn_sched_barrier(0);
                 };
                 three_terms({S[0], S[1]}, B[0]);
-                if constexpr (kAhead) fetch(Number<0>());
+                fetch(Number<0>());
                 in_order<0, kState>(step);
                 // R, from the values
 #pragma unroll
@@ -888,7 +889,7 @@ template <int KD, typename T, bool kStates, int kCompute> __global__ __launch_bo
             }
             lds_barrier();   // (keys, queries and matrices are free)
             if constexpr (kStages == 1) {
-                if (!kApart && more) write_chunk(stages[0]);
+                if (!kBringers && more) write_chunk(stages[0]);
                 lds_barrier();
             }
             stage ^= 1;
