@@ -667,13 +667,14 @@ template <int KD, typename T, bool kStates, int kCompute> __global__ __launch_bo
         };
         const uint32_t from_stride = at.blocks > 1 ? P.dv + P.dk : P.dv;
         const auto from_rows = state_rows(from, from_stride);
+        const uint32_t from_first = live_column ? (g * 8 * from_stride + column) * 4 : kNowhere;
 #pragma unroll
         for (int i = 0; i < 2 * KD; ++i)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const uint32_t d = (i / 2) * 32 + g * 8 + (i % 2) * 4 + e;
                 if constexpr (kStates) S[i][e] = column == P.dv + d ? 1.f : 0.f;
-                else S[i][e] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(from_rows, live_column ? (d * from_stride + column) * 4 : kNowhere, 0, 0));
+                else S[i][e] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(from_rows, from_first + ((i / 2) * 32 + (i % 2) * 4 + e) * from_stride * 4, 0, 0));
             }
         uint32_t values[2][4];
         const auto load_values = [&](uint32_t t0) __attribute__((always_inline)) {
@@ -897,13 +898,14 @@ template <int KD, typename T, bool kStates, int kCompute> __global__ __launch_bo
         float *const to = kStates ? block_state : at.block + 1 == at.blocks && P.state_out && state != ~0ull ? P.state_out + state_at : nullptr;
         const uint32_t to_stride = kStates ? P.dv + P.dk : P.dv;
         const auto to_rows = state_rows(to, to_stride);
+        // (places made anew: kept from the state's loads on they would go through memory, one wait each: 4 prompts of 4000 tokens 318 us, so 300)
+        const uint32_t to_first = live_column ? (anew(g) * 8 * to_stride + column) * 4 : kNowhere;
 #pragma unroll
         for (int i = 0; i < 2 * KD; ++i)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const uint32_t d = (i / 2) * 32 + g * 8 + (i % 2) * 4 + e;
                 const float x = S[i][e];   // (of an element of a vector itself, a bit cast takes the first)
-                __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, x), to_rows, live_column ? (d * to_stride + column) * 4 : kNowhere, 0, 0);
+                __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, x), to_rows, to_first + ((i / 2) * 32 + (i % 2) * 4 + e) * to_stride * 4, 0, 0);
             }
     }
 }
