@@ -26,6 +26,7 @@ namespace {
 // Kinds of caches: 16-bit values of the queries' type, e4m3 with one scale for all keys and one for all values (factors of all scores and of the result), and
 // 8-bit values (e4m3, whole numbers) with a scale for each block of slots and head.  A block has a multiple of 8 slots and a lane eight consecutive positions in
 // both products, so that a lane needs one scale of each kind for a tile: a factor of its scores, and of its probabilities before they meet the values.
+// Blocks against one scale for all, e4m3 / whole numbers / one scale: 193 MB of ragged rows 48.4 / 50.2 / 46.9 us, 535 MB of long ones 98 / 105 / 96 (widening whole numbers takes more instructions).
 enum : int { kSixteenBits, kE4m3, kBlocksE4m3, kBlocksInt8 };
 constexpr bool eight_bits(int cache) { return cache != kSixteenBits; }
 constexpr bool in_blocks(int cache) { return cache == kBlocksE4m3 || cache == kBlocksInt8; }
