@@ -124,10 +124,14 @@ constexpr uint32_t kChunk = 64;
 // Workgroups go to the eight dies in turn, and each has a cache of its own: of `each` (the heads of a chunk; of a request, with their slices of columns), neighbours, which read the same, to one (64 prompts of 1024 tokens, 16 heads: 755 us, so 711).
 __device__ __forceinline__ uint32_t by_die(uint32_t i, uint32_t each) { return each % 8 ? i : (i & 7) * (each / 8) + i / 8; }
 
-// What a chunk of a head leaves: matrices as operands of 16x16x32 products, 1 KB (64 lanes of 16 bytes) each: rows 32 s + 8 (r / 4) + 4 t + r % 4 (s, t = 0, 1), columns 32 c + 8 g + 0..7 in
-// lane 16 g + r, c <= s (above the diagonal there is nothing): the operands (s, t, c) = (0,0,0) (0,1,0) (1,0,0) (1,1,0) (1,0,1) (1,1,1), E in three bf16 terms, M in two.
-constexpr uint32_t kOperands = 6, kTermsE = 3, kTermsM = 2;
-constexpr uint32_t kMatrixPieces = kOperands * (kTermsE + kTermsM) * 64;                        // of 16 bytes
+// What a chunk of a head leaves: E and M, three bf16 terms (fp32's 24 bits) of each, as operands of 16x16x32 products: rows 32 s + 8 (r / 4) + 4 t + r % 4 (s, t = 0, 1), columns
+// 32 c + 8 g + 0..7 in lane 16 g + r, c <= s (above the diagonal there is nothing): the operands (s, t, c) = (0,0,0) (0,1,0) (1,0,0) (1,1,0) (1,0,1) (1,1,1).  One below the diagonal has 64
+// pieces of 16 bytes, one on it 40, for the lanes with g <= r / 4, and behind them one of zeros that the other lanes read: a term takes 5 KB instead of 6, and three terms of M the place of two.
+constexpr uint32_t kOperands = 6, kTerms = 3, kCorner = 48, kZeros = 40, kPlane = 4 * kCorner + 2 * 64;   // (kCorner, kPlane: pieces of an operand on the diagonal, of a term)
+__host__ __device__ constexpr bool on_diagonal(uint32_t f) { return f < 2 || f >= 4; }
+__host__ __device__ constexpr uint32_t operand_at(uint32_t f) { return f < 2 ? f * kCorner : f < 4 ? 2 * kCorner + (f - 2) * 64 : 2 * kCorner + 2 * 64 + (f - 4) * kCorner; }
+__device__ __forceinline__ uint32_t corner_piece(uint32_t g, uint32_t r) { return g <= r >> 2 ? ((r >> 2) * ((r >> 2) + 1) / 2 + g) * 4 + (r & 3) : kZeros; }
+constexpr uint32_t kMatrixPieces = 2 * kTerms * kPlane;                                          // E's terms, then M's
 constexpr uint32_t kChunkBytes = kMatrixPieces * 16 + 512;                                     // behind the matrices: e^(G_i), scale e^(G_i)
 
 struct DeltaPromptParams {
@@ -459,8 +463,7 @@ template <typename T> __global__ __launch_bounds__(256, 5) void delta_chunks_ker
             }
         }
     __syncthreads();
-    const auto write_operands = [&](auto terms_of, uint32_t first, auto rows_by) __attribute__((always_inline)) {
-        constexpr int kTerms = decltype(terms_of)::value;
+    const auto write_operands = [&](uint32_t first, auto rows_by) __attribute__((always_inline)) {
         for (uint32_t f = wave; f < kOperands; f += 4) {
             const uint32_t row = (f >= 2 ? 32 : 0) + 8 * (r >> 2) + 4 * (f & 1) + (r & 3), column = (f >= 4 ? 32 : 0) + 8 * g;
             const float *const x = X(row) + column, *const by = &betas[column], row_by = rows_by(row);
@@ -470,13 +473,17 @@ template <typename T> __global__ __launch_bounds__(256, 5) void delta_chunks_ker
                 uint32_t terms[kTerms];
                 take_apart<kTerms>(x[2 * i] * by[2 * i] * row_by, x[2 * i + 1] * by[2 * i + 1] * row_by, terms);
 #pragma unroll
-                for (int c = 0; c < kTerms; ++c) out[c][i] = terms[c];
+                for (int c = 0; c < (int)kTerms; ++c) out[c][i] = terms[c];
             }
+            const uint32_t piece = on_diagonal(f) ? corner_piece(g, r) : lane;
+            const bool zeros = on_diagonal(f) && piece == kZeros;
+            if (!zeros || lane == 48) {
 #pragma unroll
-            for (int c = 0; c < kTerms; ++c) ((u32x4 *)to)[(first + f * kTerms + c) * 64 + lane] = out[c];
+                for (int c = 0; c < (int)kTerms; ++c) ((u32x4 *)to)[first + c * kPlane + operand_at(f) + piece] = zeros ? (u32x4){0, 0, 0, 0} : out[c];
+            }
         }
     };
-    write_operands(Number<kTermsE>(), 0, [&](uint32_t row) __attribute__((always_inline)) { return left[row]; });
+    write_operands(0, [&](uint32_t row) __attribute__((always_inline)) { return left[row]; });
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < 4; ++i)
@@ -485,7 +492,7 @@ template <typename T> __global__ __launch_bounds__(256, 5) void delta_chunks_ker
             for (int e = 0; e < 4; ++e) X(i * 16 + 4 * g + e)[wave * 16 + r] = M[i][e];
         }
     __syncthreads();
-    write_operands(Number<kTermsM>(), kOperands * kTermsE, [](uint32_t) __attribute__((always_inline)) { return 1.f; });
+    write_operands(kTerms * kPlane, [](uint32_t) __attribute__((always_inline)) { return 1.f; });
 }
 
 __device__ __forceinline__ uint32_t of_neighbour(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xF, 0xF, false); }   // lanes 2 i and 2 i + 1 swapped
@@ -501,9 +508,10 @@ __device__ __forceinline__ u32x4 own_column(const uint32_t (&row)[4], bool odd) 
 // A workgroup takes a request's chunks for one head and 16 columns for each of kCompute waves, whose state stays in the wave's registers (fp32).
 // Layout (products 16x16x32, lane = 16 g + r): the lane has column r and, of a pair of result tiles, the rows 32 s + 8 g + 0..7 (operand rows are those of kOperands' comment): as B
 // of the next product those are its own, so the state goes into K S and Q S, R into M R and E R, and that into K^T E R, each from the registers where it is.
-// What is no 16-bit input meets the matrix cores as bf16 terms, each the upper half of what the ones before left, the last one rounded: three (fp32's 24 bits) of E, the state, R and E R on
-// their way to a state, two of the state, M and R on their way to an output, which is rounded to 16 bits: 2^-16 relative to the largest summand, beside bf16's 2^-8 and fp16's 2^-11 (rms errors of
-// fp16 outputs 2.082e-4, with a state in fp32 products 2.074e-4; of states 1.9e-7).  Inputs in fp16 are two terms each (exact).
+// What is no 16-bit input meets the matrix cores as three bf16 terms (fp32's 24 bits), each the upper half of what the ones before left, the last one rounded: E, M, the state, R and E R.  For outputs
+// too, though they are rounded to 16 bits: with two terms of the state, M and R there an output was off by up to 2^-17 of its largest summand, which is all of it where summands cancel, and it cost as much
+// time (24 prompts of 24000 tokens 302 us, so 295; 6 of 45000 946 and 950; 3 of 1000, 8 heads of 64, 32.4 and 34.7).  Errors of fp16 outputs 2.074e-4, the rounding's own; of states 1.9e-7.  Inputs in fp16 are
+// two terms each (exact).
 // A chunk is brought into LDS while the one before is computed: matrices straight from memory, keys and queries through registers (a second copy of keys lies by component), one barrier a chunk;
 // fp16 with more than 64 components has room for one chunk's keys only, and two barriers.  kCompute 4: four waves compute and four bring.  A chunk of 128 x 64 takes 7000 cycles, 2900 of them the
 // matrix instructions', the rest vector instructions (terms) and waits between the chunk's three dependent products: bound by that chain, a request after the other's end.  kCompute 8: all do both,
@@ -513,7 +521,7 @@ __device__ __forceinline__ u32x4 own_column(const uint32_t (&row)[4], bool odd) 
 // kStates: what blocks make of a state (columns dv and on: of the identity), without outputs.
 constexpr size_t kLdsBytes = 160 * 1024;
 template <int KD, int kIn, bool kStates> struct DeltaStage {   // what a chunk needs in LDS; planes of terms
-    static constexpr uint32_t kRow = KD == 2 ? 64 : 128, kMatrix = kStates ? kOperands * kTermsE * 64 : kMatrixPieces;
+    static constexpr uint32_t kRow = KD == 2 ? 64 : 128, kMatrix = kStates ? kTerms * kPlane : kMatrixPieces;
     uint16_t k[kIn][kChunk][kRow], q[kStates ? 0 : kIn][kChunk][kRow], kt[kIn][KD * 32][kChunk];
 };
 // A barrier for what lies in LDS alone: output stores stay under way (loads into LDS are waited for where the next chunk is taken in).
@@ -581,6 +589,7 @@ template <int KD, typename T, bool kStates, int kCompute> __global__ __launch_bo
         };
         const uint32_t own_kt = ((r >> 2) * 8 + (r & 3)) * 128 + (g ^ (r >> 1)) * 16;
         // Rows of tile (s, t) = (tile / 2, tile % 2), 32 s + 4 t behind the lane's own: pieces there are exchanged by the same bits.
+        const uint32_t own_corner = corner_piece(g, r);
         const uint32_t own_rows = row_piece(8 * (r >> 2) + (r & 3), g);
         u32x4 staged[kPer][4];
         float decays = 0.f;
@@ -712,6 +721,7 @@ template <int KD, typename T, bool kStates, int kCompute> __global__ __launch_bo
             const uint32_t m = min(kChunk, end - t0);
             const Stage &now = stages[kStages == 1 ? 0 : stage];
             const Matrices &matrices = made[stage];
+            const u32x4 *const whole = matrices.m + lane, *const corners = matrices.m + own_corner;
             const auto kt_tile = [&](int a, int t, int s) __attribute__((always_inline)) {   // components of tile t, tokens 32 s + 8 g .. + 7
                 const u32x4 w = *(const u32x4 *)((const char *)now.kt[a] + (own_kt ^ (s * 64) ^ (t / 2 % 2 * 16)) + (t / 2) * 32 * 128 + (t % 2) * 4 * 128);
                 return t / 4 % 2 ? (u32x4){w[2], w[3], w[0], w[1]} : w;
@@ -741,8 +751,9 @@ template <int KD, typename T, bool kStates, int kCompute> __global__ __launch_bo
                 u32x4 A[2][4], B[2][3];
                 // The products of a chunk in steps of up to four rows of operands: K S and Q S by 32 components and term of the inputs; then E R by its terms and M R by its, for the tokens
                 // 32 s .. 32 s + 31; then K^T E R.  A step's loads from LDS are under way while the step before is multiplied, and nothing is moved from step to step.
-                constexpr int kOfS = kStates ? 1 : 2, kOfR = kStates ? kTermsE : kTermsE + kTermsM;   // (states alone: without queries and M)
+                constexpr int kOfS = kStates ? 1 : 2, kOfR = kStates ? kTerms : 2 * kTerms;   // (states alone: without queries and M)
                 constexpr int kState = kOfS * kIn * KD, kSystem = kState + 2 * kOfR, kUpdate = 2 * ((2 * KD + 3) / 4) * kIn, kSteps = kSystem + kUpdate;
+                const auto plane_of = [](int a) constexpr { return kStates ? a : a / 2 + a % 2 * (int)kTerms; };   // by turns a term of E and of M: those of R are needed the less long
                 const auto fetch = [&](auto number) __attribute__((always_inline)) {
                     constexpr int k = decltype(number)::value;
                     u32x4 (&to)[4] = A[k % 2];
@@ -753,7 +764,7 @@ template <int KD, typename T, bool kStates, int kCompute> __global__ __launch_bo
                     } else if constexpr (k < kSystem) {
                         constexpr int s = (k - kState) / kOfR, a = (k - kState) % kOfR, first = s == 0 ? 0 : 4, last = s == 0 ? 4 : 6;
 #pragma unroll
-                        for (int f = first; f < last; ++f) to[f - first] = matrices.m[(a < kTermsE ? f * kTermsE + a : kOperands * kTermsE + f * kTermsM + a - kTermsE) * 64 + lane];
+                        for (int f = first; f < last; ++f) to[f - first] = (on_diagonal(f) ? corners : whole)[plane_of(a) * kPlane + operand_at(f)];
                     } else if constexpr (k < kSteps) {
                         constexpr int a = (k - kSystem) % kIn, each = kUpdate / 2, s = (k - kSystem) / each, first = (k - kSystem) % each / kIn * 4;
 #pragma unroll
@@ -778,7 +789,7 @@ template <int KD, typename T, bool kStates, int kCompute> __global__ __launch_bo
                     fetch(Number<k + 1>());
                     const u32x4 (&from)[4] = A[k % 2];
                     if constexpr (k < kState) {
-                        constexpr int p = k / (kOfS * kIn), a = k / kOfS % kIn, terms = (k % kOfS ? 2 : 3) - a;
+                        constexpr int p = k / (kOfS * kIn), a = k / kOfS % kIn, terms = 3 - a;
                         f32x4 (&to)[4] = k % kOfS ? O : R;
 #pragma unroll
                         for (int c = 0; c < terms; ++c)
@@ -790,17 +801,17 @@ template <int KD, typename T, bool kStates, int kCompute> __global__ __launch_bo
                         }
                     } else if constexpr (k < kSystem) {
                         constexpr int s = (k - kState) / kOfR, a = (k - kState) % kOfR, first = s == 0 ? 0 : 4, last = s == 0 ? 4 : 6;   // operands; the tile of one behind the fourth is two before it
-                        constexpr int terms = a < kTermsE ? kTermsE - a : kTermsM - (a - kTermsE);
+                        constexpr int terms = kTerms - plane_of(a) % kTerms;
 #pragma unroll
                         for (int c = 0; c < terms; ++c)
 #pragma unroll
                             for (int f = first; f < last; ++f) {
                                 const int tile = f < 4 ? f : f - 2;
-                                if (a < kTermsE) U[tile] = mfma_bf16(from[f - first], B[s][c], f < 4 && a == 0 && c == 0 ? zero : U[tile]);
+                                if (plane_of(a) < (int)kTerms) U[tile] = mfma_bf16(from[f - first], B[s][c], f < 4 && a == 0 && c == 0 ? zero : U[tile]);
                                 else O[tile] = mfma_bf16(from[f - first], B[s][c], O[tile]);
                             }
-                        if constexpr (s == 0 && a == 0) three_terms({R[2], R[3]}, B[1]);
-                        if constexpr (!kStates && s == 0 && a == 1) {
+                        if constexpr (s == 0 && a == 1) three_terms({R[2], R[3]}, B[1]);
+                        if constexpr (!kStates && s == 0 && a == 0) {
 #pragma unroll
                             for (int tile = 0; tile < 4; ++tile) O[tile] *= decay_of(1, tile);
                         }
@@ -826,6 +837,10 @@ template <int KD, typename T, bool kStates, int kCompute> __global__ __launch_bo
                 three_terms({S[0], S[1]}, B[0]);
                 fetch(Number<0>());
                 in_order<0, kState>(step);
+                if constexpr (!kStates) {   // (products that nothing waits for are put off otherwise, past the barriers of the schedule, and their operands fill the registers)
+#pragma unroll
+                    for (int tile = 0; tile < 4; ++tile) asm volatile("" : "+v"(O[tile]));
+                }
                 // R, from the values
 #pragma unroll
                 for (int tile = 0; tile < 4; ++tile) {
