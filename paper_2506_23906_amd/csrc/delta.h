@@ -141,6 +141,7 @@ struct DeltaPromptParams {
     uint32_t first;          // chunk of a launch
     float *block_states;     // [slots][heads][dk][dv + dk]; null: requests are not taken apart
     uint32_t round, slots;   // blocks of a head that the device has at once; states of blocks that there is room for
+    uint32_t *ends, *block_ends, *slot_ends, *plan;   // (more than kCountedByAll requests) chunks up to each request, its own too; where they may be taken apart, blocks and slots, and a BlockPlan
 };
 
 __device__ __forceinline__ uint32_t wave_sum32(uint32_t v) {
@@ -151,6 +152,7 @@ __device__ __forceinline__ uint32_t wave_sum32(uint32_t v) {
     v += dpp_or_zero<0x142, 0xA>(v);
     return lane_value(v + dpp_or_zero<0x143, 0xC>(v), 63);
 }
+constexpr uint32_t kMostOfLane = (1u << 26) - 1;   // more chunks than there are; where offsets go backwards a lane's sum is cut there, so that 64 of them do not wrap
 __device__ __forceinline__ uint32_t chunks_of(Span s) { return (s.end - s.begin + kChunk - 1) / kChunk; }
 
 // Which request chunk `number` is of, and its first token; chunks are numbered request after request.
@@ -158,8 +160,31 @@ struct ChunkPlace {
     uint32_t request, begin, end;   // the chunk's tokens
     bool found;
 };
-__device__ __forceinline__ ChunkPlace find_chunk(const DeltaParams &P, uint32_t number) {
+__device__ __forceinline__ uint32_t counted_before(const uint32_t *ends, uint32_t r) { return r ? ends[r - 1] : 0u; }
+// The first request whose end is behind a number; n if there is none.  64 at a time.
+__device__ __forceinline__ uint32_t first_behind(const uint32_t *ends, uint32_t n, uint32_t number) {
     const uint32_t lane = threadIdx.x & 63;
+    uint32_t from = 0, size = n;
+    while (size > 64) {
+        const uint32_t step = (size + 63) / 64, last = min((lane + 1) * step, size) - 1;   // (a lane's share may lie beyond the others': the last request again)
+        const uint64_t hit = __ballot(ends[from + last] > number);
+        if (!hit) return n;
+        const uint32_t l = __builtin_ctzll(hit);
+        from += l * step, size = min(step, size - l * step);
+    }
+    const uint64_t hit = __ballot(lane < size && ends[from + min(lane, size - 1)] > number);
+    return hit ? from + (uint32_t)__builtin_ctzll(hit) : n;
+}
+__device__ __forceinline__ ChunkPlace find_chunk(const DeltaPromptParams &PP, uint32_t number) {
+    const DeltaParams &P = PP.d;
+    const uint32_t lane = threadIdx.x & 63;
+    if (PP.ends) {
+        const uint32_t r = first_behind(PP.ends, P.n, number);
+        if (r == P.n) return {0, 0, 0, false};
+        const Span s = span_of(P, r);
+        const uint32_t begin = s.begin + (number - counted_before(PP.ends, r)) * kChunk;
+        return {r, begin, s.end - begin < kChunk ? s.end : begin + kChunk, true};
+    }
     uint32_t before = 0;
     for (uint32_t first = 0; first < P.n; first += 64) {
         const uint32_t r = first + lane;
@@ -201,13 +226,14 @@ __device__ __forceinline__ uint32_t blocks_in(uint32_t chunks, uint32_t block) {
 __device__ __forceinline__ BlockPlan plan_blocks(const DeltaPromptParams &PP) {
     const DeltaParams &P = PP.d;
     if (!PP.block_states) return {~0u, P.n};
+    if (PP.plan) return {uniform(PP.plan[0]), uniform(PP.plan[1])};
     const uint32_t lane = threadIdx.x & 63;
     uint32_t all = 0, most = 0;
     for (uint32_t r = lane; r < P.n; r += 64) {
         const uint32_t own = chunks_of(span_of(P, r));
         all += own, most = max(most, own);
     }
-    all = wave_sum32(all);
+    all = wave_sum32(min(all, kMostOfLane));
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) most = max(most, (uint32_t)__shfl_xor((int)most, d));
     most = uniform(most);
@@ -217,15 +243,81 @@ __device__ __forceinline__ BlockPlan plan_blocks(const DeltaPromptParams &PP) {
     for (uint32_t r = lane; r < P.n; r += 64) blocks += blocks_in(chunks_of(span_of(P, r)), block);
     return {block, wave_sum32(blocks)};
 }
+
+// Up to kCountedByAll requests every workgroup counts the chunks before its own by itself; for more, which would take time with the square of their number, one workgroup counts them for all first, in
+// a launch more.  us a prompt of 8 tokens, 8 heads of 64, counted by all / first: 256 prompts 0.45 / 0.43, 512 0.41 / 0.33, 768 0.45 / 0.33, 1024 0.48 / 0.33; counted by all 4096 0.9, 16384 2.8, so 0.31
+// for both.  (Where there are few heads the launch counts for more: short calls are left without it.)  Sums of requests that overlap, where offsets go backwards, are cut: behind all that there is room for.
+constexpr uint32_t kCountedByAll = 768, kCountThreads = 1024;
+__device__ __forceinline__ uint32_t cut31(uint64_t v) { return v > 0x7fffffffu ? 0x7fffffffu : (uint32_t)v; }
+struct Counted {
+    uint64_t upto, all;   // with the thread's own; of the workgroup
+};
+__device__ __forceinline__ Counted count(uint64_t own, uint64_t *waves) {
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const uint64_t o = __shfl_up((unsigned long long)own, d);
+        own += lane >= (uint32_t)d ? o : 0u;
+    }
+    if (lane == 63) waves[wave] = own;
+    __syncthreads();
+    uint64_t before = 0, all = 0;
+    for (uint32_t w = 0; w < kCountThreads / 64; ++w) before += w < wave ? waves[w] : 0u, all += waves[w];
+    __syncthreads();
+    return {before + own, all};
+}
+__global__ __launch_bounds__(kCountThreads) void delta_count_kernel(DeltaPromptParams PP) {
+    __shared__ uint64_t waves[kCountThreads / 64];
+    __shared__ uint32_t longest;
+    const DeltaParams &P = PP.d;
+    const uint32_t tid = threadIdx.x;
+    if (tid == 0) longest = 0;
+    uint64_t all = 0;
+    uint32_t most = 0;
+    for (uint32_t first = 0; first < P.n; first += kCountThreads) {
+        const uint32_t r = first + tid, own = r < P.n ? chunks_of(span_of(P, r)) : 0u;
+        const Counted c = count(own, waves);
+        if (r < P.n) PP.ends[r] = cut31(all + c.upto);
+        all += c.all, most = max(most, own);
+    }
+    if (!PP.block_states) return;
+    atomicMax(&longest, most);
+    __syncthreads();
+    if (!worth_taking_apart(longest, all, PP.round)) {
+        if (tid == 0) PP.plan[0] = ~0u, PP.plan[1] = P.n;
+        return;
+    }
+    const uint32_t block = max(kLeastBlock, cut31((all + PP.round - 1) / PP.round));
+    uint64_t blocks = 0, slots = 0;
+    for (uint32_t first = 0; first < P.n; first += kCountThreads) {
+        const uint32_t r = first + tid, own = r < P.n ? blocks_in(chunks_of(span_of(P, r)), block) : 0u;
+        const Counted b = count(own, waves), s = count(own > 1 ? own : 0u, waves);
+        if (r < P.n) PP.block_ends[r] = cut31(blocks + b.upto), PP.slot_ends[r] = cut31(slots + s.upto);
+        blocks += b.all, slots += s.all;
+    }
+    if (tid == 0) PP.plan[0] = block, PP.plan[1] = cut31(blocks);
+}
+
 // Which block of which request has a number, counted request after request.
 struct BlockPlace {
     uint32_t request, block, blocks;   // the block's number in its request, and how many that has
     uint32_t slot, chunk;              // its state's place, if there are several; its first chunk
     bool found;
 };
+__device__ __forceinline__ bool room_for(const DeltaPromptParams &PP, uint32_t first_slot, uint32_t blocks) { return blocks == 1 || (first_slot <= PP.slots && blocks <= PP.slots - first_slot); }
 __device__ __forceinline__ BlockPlace find_block(const DeltaPromptParams &PP, uint32_t block, uint32_t number) {
     const DeltaParams &P = PP.d;
     const uint32_t lane = threadIdx.x & 63;
+    if (PP.ends) {
+        const uint32_t r = uniform(first_behind(PP.block_ends, P.n, number));
+        if (r == P.n) return {0, 0, 0, 0, 0, false};
+        BlockPlace at;
+        const uint32_t first = counted_before(PP.block_ends, r), first_slot = counted_before(PP.slot_ends, r);
+        at.request = r, at.block = number - first, at.blocks = uniform(PP.block_ends[r] - first);
+        at.slot = first_slot + at.block, at.chunk = counted_before(PP.ends, r) + (at.block ? at.block * block : 0u);
+        at.found = uniform(room_for(PP, first_slot, at.blocks)) != 0;
+        return at;
+    }
     uint32_t before = 0, chunks_before = 0, slots_before = 0;
     for (uint32_t first = 0; first < P.n; first += 64) {
         const uint32_t r = first + lane, chunks = r < P.n ? chunks_of(span_of(P, r)) : 0u, own = r < P.n ? blocks_in(chunks, block) : 0u, slots = own > 1 ? own : 0u;
@@ -242,7 +334,7 @@ __device__ __forceinline__ BlockPlace find_block(const DeltaPromptParams &PP, ui
             at.request = first + l, at.blocks = lane_value(own, l), at.block = number - (before + lane_value(upto, l) - at.blocks);
             const uint32_t first_slot = slots_before + wave_sum32((int)lane < l ? slots : 0u);
             at.slot = first_slot + at.block, at.chunk = chunks_before + wave_sum32((int)lane < l ? chunks : 0u) + (at.block ? at.block * block : 0u);
-            at.found = at.blocks == 1 || (first_slot <= PP.slots && at.blocks <= PP.slots - first_slot);   // (there is room for all of them, unless offsets go backwards)
+            at.found = room_for(PP, first_slot, at.blocks);   // (there is room for all of them, unless offsets go backwards)
             return at;
         }
         before += lane_value(upto, 63), chunks_before += wave_sum32(chunks), slots_before += wave_sum32(slots);
@@ -251,11 +343,14 @@ __device__ __forceinline__ BlockPlace find_block(const DeltaPromptParams &PP, ui
 }
 
 // The same where requests are whole.
-__device__ __forceinline__ BlockPlace find_whole(const DeltaParams &P, uint32_t request) {
+__device__ __forceinline__ BlockPlace find_whole(const DeltaPromptParams &PP, uint32_t request) {
+    const DeltaParams &P = PP.d;
+    if (!PP.most_chunks) return {request, 0, 1, 0, 0, true};   // (no tokens)
+    if (PP.ends) return {request, 0, 1, 0, uniform(counted_before(PP.ends, request)), true};
     uint32_t before = 0;
 #pragma unroll 4
     for (uint32_t r = threadIdx.x & 63; r < request; r += 64) before += chunks_of(span_of(P, r));
-    return {request, 0, 1, 0, wave_sum32(before), true};
+    return {request, 0, 1, 0, wave_sum32(min(before, kMostOfLane)), true};
 }
 // Where they are more than the device takes at once: the longest first, so that none of them begins when the others are done (24 requests of 64 to 4096 tokens, the longest
 // ones last: 318 us as they come, 283).  Up to 256 requests: a lane has four of them, and the length that a place in that order has is found by bisection.
@@ -345,7 +440,7 @@ template <typename T> __global__ __launch_bounds__(256, 5) void delta_chunks_ker
     const DeltaParams &P = PP.d;
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), g = lane >> 4, r = lane & 15;
     const uint32_t in_launch = uniform(blockIdx.x / P.heads), h = uniform(by_die(blockIdx.x - in_launch * P.heads, P.heads)), shared = uniform(h / P.group), number = PP.first + in_launch;
-    const ChunkPlace at = find_chunk(P, number);
+    const ChunkPlace at = find_chunk(PP, number);
     if (!at.found || number >= PP.most_chunks) return;
     const uint32_t t0 = uniform(at.begin), m = uniform(at.end - at.begin), pieces = P.dk / 8;
     char *const to = PP.chunks + ((uint64_t)number * P.heads + h) * kChunkBytes;
@@ -549,7 +644,7 @@ template <int KD, typename T, bool kStates, int kCompute> __global__ __launch_bo
         const uint32_t ordinal = uniform((uint32_t)(item / each)), rest = uniform(by_die((uint32_t)(item - (uint64_t)ordinal * each), each)), h = uniform(rest / slices), slice = uniform(rest - h * slices);
         const uint32_t shared = uniform(h / P.group);
         const bool ordered = plan.chunks == ~0u && P.n <= kMostOrdered && (uint64_t)P.n * each > kUnits;
-        const BlockPlace at = ordered ? find_longest(P, ordinal) : plan.chunks == ~0u ? find_whole(P, ordinal) : find_block(PP, plan.chunks, ordinal);
+        const BlockPlace at = ordered ? find_longest(P, ordinal) : plan.chunks == ~0u ? find_whole(PP, ordinal) : find_block(PP, plan.chunks, ordinal);
         const Span span = span_of(P, at.request);
         const uint32_t block_tokens = plan.chunks == ~0u ? 0u : plan.chunks * kChunk;
         const uint32_t begin = uniform(span.begin + at.block * block_tokens), end = uniform(at.block + 1 == at.blocks ? span.end : begin + block_tokens);
@@ -945,12 +1040,17 @@ template <int KD> __global__ __launch_bounds__(64 * KD) void delta_states_kernel
         const uint32_t request = uniform((uint32_t)(item / each)), rest = uniform((uint32_t)(item - (uint64_t)request * each)), h = uniform(rest / slices), slice = uniform(rest - h * slices);
         const uint32_t blocks = uniform(blocks_in(chunks_of(span_of(P, request)), plan.chunks));
         if (blocks == 1) continue;
-        uint32_t mine = 0;   // slots before this request's
-        for (uint32_t i = lane; i < request; i += 64) {
-            const uint32_t b = blocks_in(chunks_of(span_of(P, i)), plan.chunks);
-            mine += b > 1 ? b : 0u;
+        uint32_t slot = 0;   // of its first block
+        if (PP.ends) slot = uniform(counted_before(PP.slot_ends, request));
+        else {
+            uint32_t mine = 0;
+            for (uint32_t i = lane; i < request; i += 64) {
+                const uint32_t b = blocks_in(chunks_of(span_of(P, i)), plan.chunks);
+                mine += b > 1 ? b : 0u;
+            }
+            slot = wave_sum32(mine);
         }
-        const uint32_t slot = wave_sum32(mine), column = slice * 16 + r, first_row = wave * 32 + g * 8;
+        const uint32_t column = slice * 16 + r, first_row = wave * 32 + g * 8;
         if (slot > PP.slots || blocks > PP.slots - slot) continue;
         const uint64_t step = P.heads * (uint64_t)P.dk * wide, state = state_of(P, request);
         float *const matrices = PP.block_states + ((uint64_t)slot * P.heads + h) * ((uint64_t)P.dk * wide);

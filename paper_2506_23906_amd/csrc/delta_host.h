@@ -56,8 +56,12 @@ inline uint64_t delta_slots(uint64_t n, uint64_t tokens, uint32_t heads, uint32_
     return 2 * chunks / kLeastBlock < most ? 2 * chunks / kLeastBlock : most;
 }
 inline size_t delta_chunk_bytes(uint64_t n, uint64_t tokens, uint32_t heads) { return (size_t)delta_chunks(n, tokens) * heads * kChunkBytes; }
+inline size_t delta_state_bytes(uint64_t slots, uint32_t heads, uint32_t dk, uint32_t dv) { return round256((size_t)slots * heads * dk * (dk + dv) * 4); }
+inline bool delta_counted(uint64_t n, uint64_t tokens) { return n > kCountedByAll && tokens; }
+inline size_t delta_count_bytes(uint64_t n, uint64_t tokens, uint64_t slots) { return delta_counted(n, tokens) ? round256(4 * (slots ? 3 * n + 2 : n)) : 0; }
 inline size_t delta_workspace(uint64_t n, uint64_t tokens, uint32_t heads, uint32_t dk, uint32_t dv) {
-    return delta_chunk_bytes(n, tokens, heads) + round256((size_t)delta_slots(n, tokens, heads, dv) * heads * dk * (dk + dv) * 4);
+    const uint64_t slots = delta_slots(n, tokens, heads, dv);
+    return delta_chunk_bytes(n, tokens, heads) + delta_state_bytes(slots, heads, dk, dv) + delta_count_bytes(n, tokens, slots);
 }
 template <typename T> mmv_status launch_chunks(DeltaPromptParams P, hipStream_t s) {
     const uint32_t most = most_of_a_launch(256, P.d.heads);
@@ -89,6 +93,10 @@ template <int KD, typename T> mmv_status launch_delta_prompts(const DeltaPromptP
     return P.d.n * P.d.heads * delta_slices(P.d.dv, 8) >= kFilledTwice && P.d.dv > 64 ? launch_delta_prompts<KD, T, 8>(P, s) : launch_delta_prompts<KD, T, 4>(P, s);
 }
 template <typename T> mmv_status delta_prompts(const DeltaPromptParams &P, hipStream_t s) {
+    if (P.ends) {
+        delta_count_kernel<<<1, kCountThreads, 0, s>>>(P);
+        if (const mmv_status st = launched()) return st;
+    }
     if (const mmv_status st = launch_chunks<T>(P, s)) return st;
     if (P.d.dk <= 64) return launch_delta_prompts<2, T>(P, s);
     if constexpr (__is_same(T, bf16_t))
@@ -99,7 +107,12 @@ mmv_status delta_call(const DeltaParams &d, int type, void *d_ws, hipStream_t s)
     DeltaPromptParams P = {};
     P.d = d, P.chunks = (char *)d_ws, P.most_chunks = (uint32_t)delta_chunks(d.n, d.tokens);
     P.slots = (uint32_t)delta_slots(d.n, d.tokens, d.heads, d.dv), P.round = delta_round(d.heads, d.dv);
-    if (P.slots) P.block_states = (float *)((char *)d_ws + delta_chunk_bytes(d.n, d.tokens, d.heads));
+    char *const behind = (char *)d_ws + delta_chunk_bytes(d.n, d.tokens, d.heads);
+    if (P.slots) P.block_states = (float *)behind;
+    if (delta_counted(d.n, d.tokens)) {
+        P.ends = (uint32_t *)(behind + delta_state_bytes(P.slots, d.heads, d.dk, d.dv));
+        if (P.slots) P.block_ends = P.ends + d.n, P.slot_ends = P.block_ends + d.n, P.plan = P.slot_ends + d.n;
+    }
     return type == MMV_TYPE_F16 ? delta_prompts<f16_t>(P, s) : delta_prompts<bf16_t>(P, s);
 }
 
