@@ -126,11 +126,12 @@ __device__ __forceinline__ uint32_t by_die(uint32_t i, uint32_t each) { return e
 
 // What a chunk of a head leaves: E and M, three bf16 terms (fp32's 24 bits) of each, as operands of 16x16x32 products: rows 32 s + 8 (r / 4) + 4 t + r % 4 (s, t = 0, 1), columns
 // 32 c + 8 g + 0..7 in lane 16 g + r, c <= s (above the diagonal there is nothing): the operands (s, t, c) = (0,0,0) (0,1,0) (1,0,0) (1,1,0) (1,0,1) (1,1,1).  One below the diagonal has 64
-// pieces of 16 bytes, one on it 40, for the lanes with g <= r / 4, and behind them one of zeros that the other lanes read: a term takes 5 KB instead of 6, and three terms of M the place of two.
-constexpr uint32_t kOperands = 6, kTerms = 3, kCorner = 48, kZeros = 40, kPlane = 4 * kCorner + 2 * 64;   // (kCorner, kPlane: pieces of an operand on the diagonal, of a term)
+// pieces of 16 bytes, one on it 40, for the lanes with g <= r / 4, and one of zeros that the other lanes read: a term takes 5 KB instead of 6, and three terms of M the place of two.
+constexpr uint32_t kOperands = 6, kTerms = 3, kCorner = 48, kZeros = 44, kPlane = 4 * kCorner + 2 * 64;   // (kCorner, kPlane: pieces of an operand on the diagonal, of a term)
 __host__ __device__ constexpr bool on_diagonal(uint32_t f) { return f < 2 || f >= 4; }
 __host__ __device__ constexpr uint32_t operand_at(uint32_t f) { return f < 2 ? f * kCorner : f < 4 ? 2 * kCorner + (f - 2) * 64 : 2 * kCorner + 2 * 64 + (f - 4) * kCorner; }
-__device__ __forceinline__ uint32_t corner_piece(uint32_t g, uint32_t r) { return g <= r >> 2 ? ((r >> 2) * ((r >> 2) + 1) / 2 + g) * 4 + (r & 3) : kZeros; }
+// (a piece's place, in fours: those that the lanes of a read bring at once, 0-3 12-15 20-23 24-27 and so on, lie in different banks; 11: the zeros)
+__device__ __forceinline__ uint32_t corner_piece(uint32_t g, uint32_t r) { return g <= r >> 2 ? 4 * (uint32_t)(0xA861B935BB24BBB0ull >> 4 * ((r & 12) + g) & 15) + (r & 3) : kZeros; }
 constexpr uint32_t kMatrixPieces = 2 * kTerms * kPlane;                                          // E's terms, then M's
 constexpr uint32_t kChunkBytes = kMatrixPieces * 16 + 512;                                     // behind the matrices: e^(G_i), scale e^(G_i)
 
@@ -571,7 +572,7 @@ template <typename T> __global__ __launch_bounds__(256, 5) void delta_chunks_ker
                 for (int c = 0; c < (int)kTerms; ++c) out[c][i] = terms[c];
             }
             const uint32_t piece = on_diagonal(f) ? corner_piece(g, r) : lane;
-            const bool zeros = on_diagonal(f) && piece == kZeros;
+            const bool zeros = on_diagonal(f) && g > r >> 2;
             if (!zeros || lane == 48) {
 #pragma unroll
                 for (int c = 0; c < (int)kTerms; ++c) ((u32x4 *)to)[first + c * kPlane + operand_at(f) + piece] = zeros ? (u32x4){0, 0, 0, 0} : out[c];
