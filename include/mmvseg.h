@@ -493,7 +493,9 @@ mmv_status mmv_block_attention(uint64_t n, uint32_t q_heads, const void *d_q, ui
  *   d_v         elements t * stride + h * dv ... for each of `heads` heads
  *   d_log_decay, d_beta  tokens * heads fp32; log_decay 0 or below (below -200 as -200), beta from 0 to 1, or to 2
  *   d_offsets, d_state_in, d_state_out, d_state_index, d_out, limits  as for mmv_decay_attention
- * States and what a token writes are fp32 throughout.  An infinity, or what is not a number, in a token reaches no earlier token and no other request or head. */
+ * States, what a token writes and what outputs are made of are fp32 throughout (24 bits meet the matrix cores), outputs rounded once.  An infinity, or what is not a number, in a token reaches no earlier token and no
+ * other request or head.
+ *   d_ws        31232 bytes for each head and 64 tokens of a request (what is left over, too: tokens / 64 + min(n, tokens) pieces in all), and where a request may be long, matrices of blocks */
 size_t mmv_delta_attention_workspace_bytes(uint64_t n, uint64_t tokens, uint32_t heads, uint32_t dk, uint32_t dv);
 mmv_status mmv_delta_attention(uint64_t n, uint64_t tokens, uint32_t heads, uint32_t k_heads, uint32_t dk, uint32_t dv,
                                const void *d_q, uint64_t q_stride, const void *d_k, uint64_t k_stride, const void *d_v, uint64_t v_stride,

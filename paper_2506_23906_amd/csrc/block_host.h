@@ -29,7 +29,8 @@ inline BlockCacheParams block_cache_params(const mmv_block_cache &c) {
 // Tokens whose runs one wave looks after: one where there are few waves' worth of them (every run in a wave of its own, at once), else as many as a
 // block holds: most windows of a prompt then have one run to begin (windows of 16 and 8 tokens for blocks of 32 take 11 % and 40 % longer, by the waves that find nothing to do).  us, one / a block
 // (16 tokens), 8 heads of 128: single tokens of 256 requests 4.3 / 18.3, of 1024 9.6 / 19.0, of 2048 17.0 / 22.9; prompts of 128 tokens, 8 of them 6.5 / 5.4, 16 10.2 / 6.8.  At 1024 tokens single
-// tokens, which a program appends at every step, still gain more than prompts lose.
+// tokens, which a program appends at every step, gain more than prompts lose.  At 2048 they would still (5.9 of 22.9 us, prompts lose 3.4); there the rule takes the prompts' side: a call of so many tokens is
+// more often prompts than one token each of as many requests, which take a third longer for it.
 constexpr uint64_t kFewWaves = 16384;
 template <int kHeld> mmv_status launch_append(const BlockAppendParams &P, unsigned blocks, int type, bool int8, hipStream_t s) {
     if (type == MMV_TYPE_F16) int8 ? block_append_kernel<kHeld, f16_t, true><<<blocks, 256, 0, s>>>(P) : block_append_kernel<kHeld, f16_t, false><<<blocks, 256, 0, s>>>(P);

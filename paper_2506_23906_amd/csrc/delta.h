@@ -121,7 +121,7 @@ template <typename T, int kRows, int kThreads> __global__ __launch_bounds__(kThr
 //   E = diag(e^(G_63 - G)) T,   M = W T.
 // delta_prompt_kernel then goes through a request's chunks: R = V - diag(e^G) K S, out = scale diag(e^G) Q S + M R, S' = e^(G_63) S + K^T E R.
 constexpr uint32_t kChunk = 64;
-// Workgroups go to the eight dies in turn, and each has a cache of its own: of `each` (the heads of a chunk; of a request, with their slices of columns), neighbours, which read the same, to one (64 prompts of 1024 tokens, 16 heads: 755 us, so 711).
+// Workgroups go to the eight dies in turn, and each has a cache of its own: of `each` (the heads of a chunk; of a request, with their slices of columns), neighbours, which read the same, to one (64 prompts of 1024 tokens, 16 heads: 735 to 748 us, so 731 to 741).
 __device__ __forceinline__ uint32_t by_die(uint32_t i, uint32_t each) { return each % 8 ? i : (i & 7) * (each / 8) + i / 8; }
 
 // What a chunk of a head leaves: E and M, three bf16 terms (fp32's 24 bits) of each, as operands of 16x16x32 products: rows 32 s + 8 (r / 4) + 4 t + r % 4 (s, t = 0, 1), columns
@@ -212,10 +212,13 @@ __device__ __forceinline__ ChunkPlace find_chunk(const DeltaPromptParams &PP, ui
 // Requests in blocks.  Chunks of a request depend on each other through the state.  Where few long requests would leave the device idle they are taken apart into blocks of as many chunks: what a
 // block makes of a state, S -> A S + B, is found for all blocks at once (A from the columns of the identity, B from a state of zeros), then the state before each block, then all blocks' outputs.
 // That is 2.3 times the work and two more launches, so it is done where the longest request has more than three times an even share of the chunks and twelve more, 16 at least (a call that cannot
-// have so many is not charged with the two launches): us of a call, whole / in blocks, where the longest of the requests has as many chunks and as many times an even share (16 heads of 128 x 128;
-// 8 of 64 x 64 and 4 of 128 x 256 change sides at the same places):
-//   16 chunks, 8 times 64 / 74;   24, 6 times 90 / 101, 12 times (4 heads) 88 / 79;   32, 4 times 118 / 134, 8 times 114 / 107;   64, 3 times 238 / 271, 4 times 224 / 205;   128, 3 times 457 / 491, 4 times 429 / 373
-// Blocks have four chunks at least, and are as many as fill the device once (filled once, twice, three times: one of 32768 tokens 687, 743, 803 us; 45000 tokens of eight requests 991, 912, 973).
+// have so many is not charged with the two launches): us of a call, whole / in blocks, where the longest of the requests has as many chunks and as many times an even share, and the others are up to a
+// quarter as long (16 heads of 128 x 128):
+//   16 chunks, 8 times 70 / 69;   24, 6 times 100 / 100, 12 times (4 heads) 96 / 86;   32, 4 times 129 / 104, 8 times 123 / 99;   64, 3 times 258 / 226, 4 times 246 / 159;   128, 3 times 494 / 412, 4 times 469 / 272
+// Where sides change depends on the others' lengths too, which the rule leaves out; it takes the later places (24 chunks, 6 times: 4 heads of 128 x 128 101 / 123, 8 of 64 x 64 84 / 99, 4 of
+// 128 x 256 96 / 107).
+// Blocks have four chunks at least, and are as many as fill the device once (once, twice: one of 4096 tokens 133, 173 us, of 32768 685, 722; 45000 tokens of eight requests 938, 937; but
+// of six, one with most of them, 953, 861).
 constexpr uint32_t kLeastBlock = 4, kLeastApart = 16, kApartFixed = 12, kApartShare = 3;
 __host__ __device__ constexpr bool worth_taking_apart(uint64_t most, uint64_t all, uint32_t round) { return most >= kLeastApart && (most - kApartFixed) * round > kApartShare * all; }
 constexpr uint32_t kMostOrdered = 256;
@@ -354,7 +357,7 @@ __device__ __forceinline__ BlockPlace find_whole(const DeltaPromptParams &PP, ui
     return {request, 0, 1, 0, wave_sum32(min(before, kMostOfLane)), true};
 }
 // Where they are more than the device takes at once: the longest first, so that none of them begins when the others are done (24 requests of 64 to 4096 tokens, the longest
-// ones last: 318 us as they come, 283).  Up to 256 requests: a lane has four of them, and the length that a place in that order has is found by bisection.
+// ones last: 369 us as they come, 298).  Up to 256 requests: a lane has four of them, and the length that a place in that order has is found by bisection.
 __device__ __forceinline__ BlockPlace find_longest(const DeltaParams &P, uint32_t place) {
     const uint32_t lane = threadIdx.x & 63;
     uint32_t chunks[kMostOrdered / 64], most = 0;   // and one: 0 where there is no request
@@ -428,9 +431,9 @@ __device__ __forceinline__ f32x4 mfma_f32(float a, float b, f32x4 c) { return __
 // I + L, a column a lane, by substitution (which loses nothing where keys are alike, as powers of L would); then wave j the blocks below the diagonal of block column j, and those of M,
 //   T_ij = -T_ii sum_(j <= m < i) L_im T_mj,   M_ij = sum_(j <= m <= i) W_im T_mj
 // in fp32 products (16x16x4): the column of a step of the operand is 4 g + step, so that a result's registers are the next product's operand.
-// fp32, not bf16 terms: with keys alike and beta 2, T's entries cancel in sums of 64.  Bound by the phases of a workgroup, which wait for each other (32 KB written for 16 KB of keys and queries
-// read, 2.3 TB/s): 24 prompts of 24000 tokens in all, 16 heads, 90 us; one of 45000, 171 us.  Five workgroups on a compute unit, for which keys go through T's place in LDS and T's empty quarter
-// is left out, for four 96 and 185 us.
+// fp32, not bf16 terms: with keys alike and beta 2, T's entries cancel in sums of 64.  Bound by the phases of a workgroup, which wait for each other (28 KB written for 16 KB of keys and queries
+// read, 2.2 TB/s): 24 prompts of 24000 tokens in all, 16 heads, 89 us; six of 45000, 149 us.  Five workgroups on a compute unit, for which keys go through T's place in LDS and T's empty quarter
+// is left out, for four 96 us in place of 90.
 template <typename T> __global__ __launch_bounds__(256, 5) void delta_chunks_kernel(DeltaPromptParams PP) {
     constexpr uint32_t kWide = kChunk + 4, kHalf = kChunk / 2, kNarrow = kHalf + 4;
     // below the diagonal L, from it on W transposed; T, later M, the first 32 rows without columns 32 .. 63: five workgroups on a compute unit.  Before T is there, keys lie in its place.
@@ -609,11 +612,12 @@ __device__ __forceinline__ u32x4 own_column(const uint32_t (&row)[4], bool odd) 
 // time (24 prompts of 24000 tokens 302 us, so 295; 6 of 45000 946 and 950; 3 of 1000, 8 heads of 64, 32.4 and 34.7).  Errors of fp16 outputs 2.074e-4, the rounding's own; of states 1.9e-7.  Inputs in fp16 are
 // two terms each (exact).
 // A chunk is brought into LDS while the one before is computed: matrices straight from memory, keys and queries through registers (a second copy of keys lies by component), one barrier a chunk;
-// fp16 with more than 64 components has room for one chunk's keys only, and two barriers.  kCompute 4: four waves compute and four bring.  A chunk of 128 x 64 takes 7000 cycles, 2900 of them the
-// matrix instructions', the rest vector instructions (terms) and waits between the chunk's three dependent products: bound by that chain, a request after the other's end.  kCompute 8: all do both,
-// 128 columns, two waves to a vector unit fill each other's waits: 12600 cycles for twice the columns, so more in all but later for each.  launch_delta_prompts has the rule and both sides.
-// 24 prompts of 24000 tokens in all, 16 heads, 128 x 128, bf16: 238 us, where four waves that did everything in turn, two workgroups on a compute unit, took 386.  Two groups of 16 columns to a
-// wave, which halve the reads of LDS, need twice the registers and were slower; so was an order of matrix and vector instructions by hand (7500 cycles).
+// fp16 with more than 64 components has room for one chunk's keys only, and two barriers.  kCompute 4: four waves compute and four bring.  A chunk of 128 x 64 takes 3.2 us in bf16 (5.8 in fp16), 1.4
+// of them the matrix instructions' (216 of 16 cycles), the rest vector instructions (terms) and waits between the chunk's three dependent products: bound by that chain, a request after the other's
+// end.  kCompute 8: all do both, 128 columns, two waves to a vector unit fill each other's waits: 5.7 us for twice the columns, so more in all but later for each.  launch_delta_prompts has the rule and
+// both sides.  24 prompts of 24000 tokens in all, 16 heads, 128 x 128, bf16: 224 us, where four waves that did everything in turn, two workgroups on a compute unit, took 386.  Two groups of 16 columns
+// to a wave, which halve the reads of LDS, need twice the registers and were slower; so was an order of matrix and vector instructions by hand (7 % more).  What is not finite is
+// done again token by token, 0.5 us each.
 // kStates: what blocks make of a state (columns dv and on: of the identity), without outputs.
 constexpr size_t kLdsBytes = 160 * 1024;
 template <int KD, int kIn, bool kStates> struct DeltaStage {   // what a chunk needs in LDS; planes of terms
@@ -1029,7 +1033,7 @@ template <int KD, typename T, bool kStates, int kCompute> __global__ __launch_bo
 }
 
 // The state before each block of the requests that are taken apart, over the blocks' B: S_(b + 1) = A_b S_b + B_b.  A workgroup has 16 columns, wave w the rows 32 w .. 32 w + 31; the rows
-// go from wave to wave through LDS.  Both operands are fp32: three terms each.  Bound by the way from one block's state to the next, once for each block: 45000 tokens in 32 blocks of 16 heads 46 us.
+// go from wave to wave through LDS.  Both operands are fp32: three terms each.  Bound by the way from one block's state to the next, once for each block: six requests of 45000 tokens, 16 heads of 128 x 128, 27 us.
 template <int KD> __global__ __launch_bounds__(64 * KD) void delta_states_kernel(DeltaPromptParams PP) {
     __shared__ __align__(16) float state_rows[2][16][KD * 32 + 4];
     const DeltaParams &P = PP.d;

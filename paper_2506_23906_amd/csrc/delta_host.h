@@ -72,8 +72,9 @@ template <typename T> mmv_status launch_chunks(DeltaPromptParams P, hipStream_t 
     return MMV_OK;
 }
 // Workgroups go on to the next block by themselves: where nothing is taken apart, the launches for that are of as many as the device holds.
-// Workgroups of 128 columns where they fill the device twice, of 64 and four more waves that bring chunks where a request's own time counts (and where 64 are all).  us, 64 / 128: 240 workgroups (of 128)
-// 178 / 229, 384 347 / 383, 1024 825 / 733, 3200 of 100 tokens 666 / 409.
+// Workgroups of 128 columns where they fill the device twice, of 64 and four more waves that bring chunks where a request's own time counts (and where 64 are all).  us, 64 / 128: requests from 64 to
+// 4096 tokens, 240 workgroups (of 128) 266 / 412, 384 306 / 463 (fp16 474 / 597), 512 388 / 505; requests of one length, 512 393 / 376, 1024 765 / 722 (fp16 1082 / 868), 3200 (100 tokens) 486 / 386.  Lengths
+// are not known here, so that uneven ones lose at 512 what even ones gain from there on.
 constexpr uint32_t kFilledTwice = 2 * kUnits;
 constexpr uint64_t kMostWorkgroups = 1u << 22;
 template <int KD, typename T, int kCompute> mmv_status launch_delta_prompts(const DeltaPromptParams &P, hipStream_t s) {
