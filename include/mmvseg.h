@@ -495,7 +495,8 @@ mmv_status mmv_block_attention(uint64_t n, uint32_t q_heads, const void *d_q, ui
  *   d_offsets, d_state_in, d_state_out, d_state_index, d_out, limits  as for mmv_decay_attention
  * States, what a token writes and what outputs are made of are fp32 throughout (24 bits meet the matrix cores), outputs rounded once.  An infinity, or what is not a number, in a token reaches no earlier token and no
  * other request or head.
- *   d_ws        31232 bytes for each head and 64 tokens of a request (what is left over, too: tokens / 64 + min(n, tokens) pieces in all), and where a request may be long, matrices of blocks */
+ *   d_ws        31232 bytes for each head and 64 tokens of a request (what is left over, too: tokens / 64 + min(n, tokens) pieces in all), where a request may be long
+ *               matrices of blocks, and up to 12 bytes for each of many requests */
 size_t mmv_delta_attention_workspace_bytes(uint64_t n, uint64_t tokens, uint32_t heads, uint32_t dk, uint32_t dv);
 mmv_status mmv_delta_attention(uint64_t n, uint64_t tokens, uint32_t heads, uint32_t k_heads, uint32_t dk, uint32_t dv,
                                const void *d_q, uint64_t q_stride, const void *d_k, uint64_t k_stride, const void *d_v, uint64_t v_stride,
