@@ -853,7 +853,6 @@ template <int KD, typename T, bool kStates, int kCompute> __global__ __launch_bo
                 // 32 s .. 32 s + 31; then K^T E R.  A step's loads from LDS are under way while the step before is multiplied, and nothing is moved from step to step.
                 constexpr int kOfS = kStates ? 1 : 2, kOfR = kStates ? kTerms : 2 * kTerms;   // (states alone: without queries and M)
                 constexpr int kState = kOfS * kIn * KD, kSystem = kState + 2 * kOfR, kUpdate = 2 * ((2 * KD + 3) / 4) * kIn, kSteps = kSystem + kUpdate;
-                const auto plane_of = [](int a) constexpr { return kStates ? a : a / 2 + a % 2 * (int)kTerms; };   // by turns a term of E and of M: those of R are needed the less long
                 const auto fetch = [&](auto number) __attribute__((always_inline)) {
                     constexpr int k = decltype(number)::value;
                     u32x4 (&to)[4] = A[k % 2];
@@ -864,7 +863,7 @@ template <int KD, typename T, bool kStates, int kCompute> __global__ __launch_bo
                     } else if constexpr (k < kSystem) {
                         constexpr int s = (k - kState) / kOfR, a = (k - kState) % kOfR, first = s == 0 ? 0 : 4, last = s == 0 ? 4 : 6;
 #pragma unroll
-                        for (int f = first; f < last; ++f) to[f - first] = (on_diagonal(f) ? corners : whole)[plane_of(a) * kPlane + operand_at(f)];
+                        for (int f = first; f < last; ++f) to[f - first] = (on_diagonal(f) ? corners : whole)[a * kPlane + operand_at(f)];
                     } else if constexpr (k < kSteps) {
                         constexpr int a = (k - kSystem) % kIn, each = kUpdate / 2, s = (k - kSystem) / each, first = (k - kSystem) % each / kIn * 4;
 #pragma unroll
@@ -901,17 +900,17 @@ template <int KD, typename T, bool kStates, int kCompute> __global__ __launch_bo
                         }
                     } else if constexpr (k < kSystem) {
                         constexpr int s = (k - kState) / kOfR, a = (k - kState) % kOfR, first = s == 0 ? 0 : 4, last = s == 0 ? 4 : 6;   // operands; the tile of one behind the fourth is two before it
-                        constexpr int terms = kTerms - plane_of(a) % kTerms;
+                        constexpr int terms = kTerms - a % kTerms;
 #pragma unroll
                         for (int c = 0; c < terms; ++c)
 #pragma unroll
                             for (int f = first; f < last; ++f) {
                                 const int tile = f < 4 ? f : f - 2;
-                                if (plane_of(a) < (int)kTerms) U[tile] = mfma_bf16(from[f - first], B[s][c], f < 4 && a == 0 && c == 0 ? zero : U[tile]);
+                                if constexpr (a < (int)kTerms) U[tile] = mfma_bf16(from[f - first], B[s][c], f < 4 && a == 0 && c == 0 ? zero : U[tile]);
                                 else O[tile] = mfma_bf16(from[f - first], B[s][c], O[tile]);
                             }
-                        if constexpr (s == 0 && a == 1) three_terms({R[2], R[3]}, B[1]);
-                        if constexpr (!kStates && s == 0 && a == 0) {
+                        if constexpr (s == 0 && a == 0) three_terms({R[2], R[3]}, B[1]);
+                        if constexpr (!kStates && s == 0 && a == 1) {
 #pragma unroll
                             for (int tile = 0; tile < 4; ++tile) O[tile] *= decay_of(1, tile);
                         }
